@@ -393,6 +393,137 @@ gbla_status gbla_state_static_scratch(const void *k, const void *v,
                                       int B, int H, int N, int D,
                                       gbla_dtype dtype, gbla_stream_t stream);
 
+/*
+ * ---- Causal decoder operators ------------------------------------------------
+ *
+ * The side of a generative model that emits tokens: queries and keys are
+ * normed and rotated by their positions (gbla_qk_norm_rotate), a causal linear
+ * attention whose memory decays per head reads the prompt in parallel
+ * (gbla_decay_attention) and leaves a state of D x D numbers per head, and each
+ * further token updates that state in place (gbla_decay_attention_step).  The
+ * backward entry points make the same layer trainable.
+ *
+ * Heads: q has H heads, k and v have Hk heads, H a multiple of Hk; query head h
+ * reads key / value head h / (H / Hk).  Results have the input's dtype.
+ *
+ * Strides: `strides` is NULL (every input contiguous) or a HOST array of element
+ * strides, (batch, token) for each of the inputs that its function names, in
+ * that order; it is read before the call returns.  The heads of a token are
+ * adjacent and a head's D values contiguous (so a slice of a packed
+ * [B, N, 3, H, D] projection is a valid input).  A stride of a dimension longer
+ * than one must be at least the heads' width (heads x D) and a multiple of 16
+ * bytes, the token's below 2^34 and the batch's below 2^44
+ * (GBLA_ERR_INVALID_ARG otherwise).  Gradients coming in and all results are
+ * contiguous.
+ *
+ * Common rules (ownership, alignment, asynchrony, seq_lens, error codes) are
+ * those at the top of this file; sizes: D in {32, 64, 128}, both dtypes.  A
+ * call without tokens writes no results but still passes a state on: state_out
+ * (dstate_in) then becomes state_in (dstate_out), or zeros where that is NULL.
+ */
+
+/* Pairs (2i, 2i + 1) turn together instead of (i, i + R / 2). */
+#define GBLA_ROTATE_INTERLEAVED 1u
+
+/*
+ * gbla_qk_norm_rotate -- per-head RMS norm and position rotation of q and k.
+ * For each valid token and head x with its weight w:
+ *   y = x / sqrt(mean(x^2) + eps) * w,
+ * then each pair (a, b) of the first R values becomes
+ *   (a cos - b sin, a sin + b cos)
+ * with the cosine and sine of its angle from row positions[b, t] of `rot`.
+ *   q [B, N, H, D], k [B, N, Hk, D] dtype; strides (q, k) or NULL
+ *   norm_q [H, D], norm_k [Hk, D] fp32
+ *   rot       [P, R] fp32: R / 2 cosines, then R / 2 sines, for each position;
+ *             NULL only with R = 0 (norm alone).  R a multiple of 16, R <= D.
+ *   positions device [B, N] int32, or NULL meaning position t; values are
+ *             clamped to [0, P - 1] on the device
+ *   qo [B, N, H, D], ko [B, N, Hk, D] dtype: results; rows t >= L_b untouched.
+ * eps is positive and finite.  flags: GBLA_ROTATE_INTERLEAVED or 0.  fp32
+ * arithmetic.  Allocates nothing.
+ */
+gbla_status gbla_qk_norm_rotate(const void *q, const void *k, const float *norm_q,
+                                const float *norm_k, const float *rot,
+                                const int32_t *positions, const int32_t *seq_lens,
+                                const int64_t *strides, void *qo, void *ko, int B, int N, int H,
+                                int Hk, int D, int R, int P, float eps, uint32_t flags,
+                                gbla_dtype dtype, gbla_stream_t stream);
+
+/*
+ * gbla_qk_norm_rotate_backward -- gradients of sum(dqo * qo) + sum(dko * ko).
+ * Inputs as gbla_qk_norm_rotate plus dqo [B, N, H, D] and dko [B, N, Hk, D]
+ * dtype.  Outputs: dq, dk like q and k but contiguous (rows t >= L_b written as
+ * 0), dnorm_q [H, D] and dnorm_k [Hk, D] fp32 (overwritten; sums over the batch
+ * in a fixed order).  Nothing is kept from a forward call.  Scratch comes from
+ * the library's pool (GBLA_ERR_ALLOC).
+ */
+gbla_status gbla_qk_norm_rotate_backward(
+    const void *q, const void *k, const float *norm_q, const float *norm_k, const float *rot,
+    const int32_t *positions, const int32_t *seq_lens, const int64_t *strides, const void *dqo,
+    const void *dko, void *dq, void *dk, float *dnorm_q, float *dnorm_k, int B, int N, int H,
+    int Hk, int D, int R, int P, float eps, uint32_t flags, gbla_dtype dtype,
+    gbla_stream_t stream);
+
+/*
+ * gbla_decay_attention -- causal linear attention with a decay for each head.
+ * With gamma = exp(log_decay[h]), S_{-1} = state_in (zeros where NULL) and, for
+ * t = 0 .. L_b - 1,
+ *   S_t = gamma S_{t-1} + k_t v_t^T,   o_t = scale q_t^T S_t.
+ *   q [B, N, H, D], k, v [B, N, Hk, D] dtype; strides (q, k, v) or NULL
+ *   log_decay [H] fp32: natural logarithm of the decay, a constant of the model
+ *             (-inf: no memory; positive values grow)
+ *   state_in  [B, H, D, D] fp32 (S[d][e], d of k, e of v) or NULL
+ *   o         [B, N, H, D] dtype; rows t >= L_b untouched
+ *   state_out [B, H, D, D] fp32 or NULL: S after each sequence's last token
+ *             (state_in for an empty one)
+ * scale is finite and not 0.  Computed in chunks of tokens: bf16 with D in
+ * {64, 128} on tensor cores (GBLA_ALGO_TC), anything else in fp32 on CUDA cores
+ * (GBLA_ALGO_SIMT); the state is held in fp32 on both.  A NaN or infinity in a
+ * valid token reaches the other tokens of its chunk, before it too; what
+ * padding rows hold reaches nothing.  Sums run in a fixed order.  Scratch comes
+ * from the library's pool (GBLA_ERR_ALLOC).
+ */
+gbla_status gbla_decay_attention(const void *q, const void *k, const void *v,
+                                 const float *log_decay, const int32_t *seq_lens,
+                                 const int64_t *strides, const float *state_in, void *o,
+                                 float *state_out, int B, int N, int H, int Hk, int D,
+                                 float scale, gbla_dtype dtype, gbla_algo algo,
+                                 gbla_stream_t stream);
+
+/*
+ * gbla_decay_attention_backward -- gradients of
+ * sum(d_o * o) + sum(dstate_out * state_out) with respect to q, k, v and state_in.
+ * Inputs as gbla_decay_attention (strides of q, k, v) plus d_o [B, N, H, D]
+ * dtype and dstate_out [B, H, D, D] fp32 (NULL: zeros).  Outputs: dq
+ * [B, N, H, D], dk, dv [B, N, Hk, D] dtype (sums over the query heads that share
+ * a key / value head, in fp32; rows t >= L_b written as 0) and dstate_in
+ * [B, H, D, D] fp32 or NULL.  log_decay has no gradient.  Nothing is kept from a
+ * forward call.
+ */
+gbla_status gbla_decay_attention_backward(
+    const void *q, const void *k, const void *v, const float *log_decay,
+    const int32_t *seq_lens, const int64_t *strides, const float *state_in, const void *d_o,
+    const float *dstate_out, void *dq, void *dk, void *dv, float *dstate_in, int B, int N, int H,
+    int Hk, int D, float scale, gbla_dtype dtype, gbla_algo algo, gbla_stream_t stream);
+
+/*
+ * gbla_decay_attention_step -- the recurrence for one token of each sequence,
+ * on a pool of states updated in place:
+ *   S = gamma state[slots[b], h] + k v^T,  state[slots[b], h] = S,  o = scale q^T S.
+ *   q [B, H, D], k, v [B, Hk, D] dtype; strides NULL or a host array of three
+ *             element strides (batch of q, k, v; the rules above)
+ *   slots     device [B] int32, or NULL meaning slot b (then B <= n_slots); a
+ *             value outside [0, n_slots) marks a row without a sequence: its o
+ *             is not written.  Rows of one call must not share a slot.
+ *   state     [n_slots, H, D, D] fp32;  o [B, H, D] dtype
+ * One kernel, allocates nothing.
+ */
+gbla_status gbla_decay_attention_step(const void *q, const void *k, const void *v,
+                                      const float *log_decay, const int32_t *slots,
+                                      const int64_t *strides, float *state, void *o, int B,
+                                      int H, int Hk, int D, int n_slots, float scale,
+                                      gbla_dtype dtype, gbla_stream_t stream);
+
 /* Number of floats per (b, h) in a state buffer: D*D + D. */
 size_t gbla_state_floats(int D);
 

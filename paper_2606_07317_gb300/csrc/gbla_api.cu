@@ -1,6 +1,7 @@
 // C-ABI front end of the GBLA core: argument validation, scratch memory and
 // kernel-family dispatch.  All arithmetic happens in the kernels of
 // gbla_simt.cu and gbla_tc.cu.
+#include <math.h>
 #include <string.h>
 
 #include <atomic>
@@ -206,9 +207,11 @@ uint64_t gbla_launch_count(void) { return g_launches.load(std::memory_order_rela
 uint32_t gbla_device_error(int reset) {
   const unsigned a = tc_device_error(reset != 0), b = project_device_error(reset != 0);
   const unsigned c = bwd_device_error(reset != 0), d = sa_device_error(reset != 0);
-  return (a == 0xFFFFFFFFu || b == 0xFFFFFFFFu || c == 0xFFFFFFFFu || d == 0xFFFFFFFFu)
+  const unsigned e = decay_device_error(reset != 0);
+  return (a == 0xFFFFFFFFu || b == 0xFFFFFFFFu || c == 0xFFFFFFFFu || d == 0xFFFFFFFFu ||
+          e == 0xFFFFFFFFu)
              ? 0xFFFFFFFFu
-             : (a | b | c | d);
+             : (a | b | c | d | e);
 }
 
 const char *gbla_last_cuda_error(void) { return last_cuda_error_string(); }
@@ -779,6 +782,323 @@ gbla_status gbla_forward_host(const void *q, const void *k, const void *v,
   if (s != GBLA_OK) return s;
   if (e != cudaSuccess) return from_cuda(e);
   return from_cuda(es2);
+}
+
+}  // extern "C"
+
+// ---- causal decoder operators -----------------------------------------------
+namespace {
+
+// A token-major input: (batch, token) element strides and the bytes it spans.
+struct View {
+  long long s[2];
+  size_t bytes;
+};
+
+// Strides of input `i` from the caller's array (NULL: contiguous); a dimension
+// of one token or sequence has no stride.
+gbla_status view_of(const int64_t *strides, int i, int B, int N, long long width, gbla_dtype dt,
+                    View *v) {
+  const long long unit = 16 / (long long)elem_bytes(dt);
+  v->s[0] = width * N, v->s[1] = width;
+  if (strides) {
+    if (B > 1) v->s[0] = strides[2 * i];
+    if (N > 1) v->s[1] = strides[2 * i + 1];
+    for (int j = 0; j < 2; ++j)
+      if ((j == 0 ? B : N) > 1 &&
+          (v->s[j] < width || v->s[j] % unit != 0 || v->s[j] >= (1ll << (j == 0 ? 44 : 34))))
+        return GBLA_ERR_INVALID_ARG;
+  }
+  v->bytes = (size_t)((B - 1) * v->s[0] + (N - 1) * v->s[1] + width) * elem_bytes(dt);
+  return GBLA_OK;
+}
+
+gbla_status check_heads(int H, int Hk) {
+  if (Hk < 0 || (H > 0 && (Hk == 0 || H % Hk != 0))) return GBLA_ERR_INVALID_ARG;
+  return GBLA_OK;
+}
+
+bool any_overlap(std::initializer_list<Range> outs, std::initializer_list<Range> ins) {
+  for (const Range *o = outs.begin(); o != outs.end(); ++o) {
+    for (const Range &i : ins)
+      if (overlap(*o, i)) return true;
+    for (const Range *u = o + 1; u != outs.end(); ++u)
+      if (overlap(*o, *u)) return true;
+  }
+  return false;
+}
+
+// Pointers that may be NULL but are 16-byte aligned where they are given.
+bool aligned_or_null(std::initializer_list<const void *> ptrs) {
+  for (const void *p : ptrs)
+    if (!aligned(p)) return false;
+  return true;
+}
+
+// Shared checks of gbla_qk_norm_rotate and its backward; fills everything of
+// `a` but the incoming gradients and the outputs.
+gbla_status check_rotate(RotateArgs *a, View *vq, View *vk, const void *q, const void *k,
+                         const float *norm_q, const float *norm_k, const float *rot,
+                         const int32_t *positions, const int32_t *seq_lens,
+                         const int64_t *strides, int B, int N, int H, int Hk, int D, int R, int P,
+                         float eps, uint32_t flags, gbla_dtype dtype, bool *empty) {
+  gbla_status s = check_dims(B, H, N, D, dtype, empty);
+  if (s != GBLA_OK) return s;
+  if ((s = check_heads(H, Hk)) != GBLA_OK) return s;
+  if (flags & ~GBLA_ROTATE_INTERLEAVED) return GBLA_ERR_INVALID_ARG;
+  if (R < 0 || R > D || R % 16 != 0 || P < 0 || (R > 0 && P == 0)) return GBLA_ERR_INVALID_ARG;
+  if (!(eps > 0.f) || !isfinite(eps)) return GBLA_ERR_INVALID_ARG;
+  if (*empty) return GBLA_OK;
+  if ((s = check_ptrs({q, k, norm_q, norm_k})) != GBLA_OK) return s;
+  if (!aligned(rot) || (R > 0 && rot == nullptr)) return GBLA_ERR_INVALID_ARG;
+  if ((s = check_seq_lens(seq_lens)) != GBLA_OK) return s;
+  if ((s = check_seq_lens(positions)) != GBLA_OK) return s;
+  if ((s = view_of(strides, 0, B, N, (long long)H * D, dtype, vq)) != GBLA_OK) return s;
+  if ((s = view_of(strides, 1, B, N, (long long)Hk * D, dtype, vk)) != GBLA_OK) return s;
+  *a = RotateArgs{};
+  a->q = q, a->k = k, a->norm_q = norm_q, a->norm_k = norm_k, a->rot = rot;
+  a->positions = positions, a->seq_lens = seq_lens;
+  for (int i = 0; i < 2; ++i) a->sq[i] = vq->s[i], a->sk[i] = vk->s[i];
+  a->B = B, a->N = N, a->H = H, a->Hk = Hk, a->D = D, a->R = R, a->P = P, a->eps = eps;
+  a->interleaved = (flags & GBLA_ROTATE_INTERLEAVED) != 0, a->dtype = dtype;
+  return GBLA_OK;
+}
+
+// A scan with the tensor-core family or the CUDA-core one, its scratch from the pool.
+gbla_status run_scan(const ScanArgs &a, bool tc, cudaStream_t st) {
+  Scratch ws;
+  gbla_status s = ws.alloc(sizeof(float) * (tc ? tc_scan_floats(a) : simt_scan_floats(a)), st);
+  if (s != GBLA_OK) return s;
+  return from_cuda(tc ? tc_scan(a, (float *)ws.ptr, st) : simt_scan(a, (float *)ws.ptr, st));
+}
+
+gbla_status scan_family(const ScanArgs &a, gbla_algo algo, bool *tc) {
+  if (algo != GBLA_ALGO_AUTO && algo != GBLA_ALGO_SIMT && algo != GBLA_ALGO_TC)
+    return GBLA_ERR_UNSUPPORTED;
+  *tc = algo != GBLA_ALGO_SIMT && tc_scan_supports(a);
+  return algo == GBLA_ALGO_TC && !*tc ? GBLA_ERR_UNSUPPORTED : GBLA_OK;
+}
+
+// No tokens: the state passes through.
+gbla_status pass_state(const float *in, float *out, size_t bytes, cudaStream_t st) {
+  if (out == nullptr || bytes == 0) return GBLA_OK;
+  if (!aligned(in) || !aligned(out) ||
+      (in && overlap(range_of(out, bytes), range_of(in, bytes))))
+    return GBLA_ERR_INVALID_ARG;
+  return from_cuda(in ? cudaMemcpyAsync(out, in, bytes, cudaMemcpyDeviceToDevice, st)
+                      : cudaMemsetAsync(out, 0, bytes, st));
+}
+
+gbla_status check_scale(float scale) {
+  return isfinite(scale) && scale != 0.f ? GBLA_OK : GBLA_ERR_INVALID_ARG;
+}
+
+}  // namespace
+
+extern "C" {
+
+gbla_status gbla_qk_norm_rotate(const void *q, const void *k, const float *norm_q,
+                                const float *norm_k, const float *rot,
+                                const int32_t *positions, const int32_t *seq_lens,
+                                const int64_t *strides, void *qo, void *ko, int B, int N, int H,
+                                int Hk, int D, int R, int P, float eps, uint32_t flags,
+                                gbla_dtype dtype, gbla_stream_t stream) {
+  RotateArgs a;
+  View vq, vk;
+  bool empty = false;
+  gbla_status s = check_rotate(&a, &vq, &vk, q, k, norm_q, norm_k, rot, positions, seq_lens,
+                               strides, B, N, H, Hk, D, R, P, eps, flags, dtype, &empty);
+  if (s != GBLA_OK || empty) return s;
+  if ((s = check_ptrs({qo, ko})) != GBLA_OK) return s;
+  const size_t tok = (size_t)B * N, es = elem_bytes(dtype);
+  if (any_overlap({range_of(qo, tok * H * D * es), range_of(ko, tok * Hk * D * es)},
+                  {range_of(q, vq.bytes), range_of(k, vk.bytes),
+                   range_of(norm_q, sizeof(float) * H * D),
+                   range_of(norm_k, sizeof(float) * Hk * D),
+                   range_of(rot, sizeof(float) * (size_t)P * R),
+                   range_of(positions, positions ? sizeof(int32_t) * tok : 0),
+                   range_of(seq_lens, seq_lens ? sizeof(int32_t) * B : 0)}))
+    return GBLA_ERR_INVALID_ARG;
+  a.qo = qo, a.ko = ko;
+  return from_cuda(rotate_forward(a, (cudaStream_t)stream));
+}
+
+gbla_status gbla_qk_norm_rotate_backward(
+    const void *q, const void *k, const float *norm_q, const float *norm_k, const float *rot,
+    const int32_t *positions, const int32_t *seq_lens, const int64_t *strides, const void *dqo,
+    const void *dko, void *dq, void *dk, float *dnorm_q, float *dnorm_k, int B, int N, int H,
+    int Hk, int D, int R, int P, float eps, uint32_t flags, gbla_dtype dtype,
+    gbla_stream_t stream) {
+  RotateArgs a;
+  View vq, vk;
+  bool empty = false;
+  gbla_status s = check_rotate(&a, &vq, &vk, q, k, norm_q, norm_k, rot, positions, seq_lens,
+                               strides, B, N, H, Hk, D, R, P, eps, flags, dtype, &empty);
+  if (s != GBLA_OK) return s;
+  if (H == 0) return GBLA_OK;
+  cudaStream_t st = (cudaStream_t)stream;
+  const size_t wq = sizeof(float) * H * D, wk = sizeof(float) * Hk * D;
+  if ((s = check_ptrs({dnorm_q, dnorm_k})) != GBLA_OK) return s;
+  if (empty) {  // no tokens: the weight gradients are empty sums
+    if (overlap(range_of(dnorm_q, wq), range_of(dnorm_k, wk))) return GBLA_ERR_INVALID_ARG;
+    if ((s = from_cuda(cudaMemsetAsync(dnorm_q, 0, wq, st))) != GBLA_OK) return s;
+    return from_cuda(cudaMemsetAsync(dnorm_k, 0, wk, st));
+  }
+  if ((s = check_ptrs({dqo, dko, dq, dk})) != GBLA_OK) return s;
+  const size_t tok = (size_t)B * N, es = elem_bytes(dtype);
+  const size_t qb = tok * H * D * es, kb = tok * Hk * D * es;
+  if (any_overlap({range_of(dq, qb), range_of(dk, kb), range_of(dnorm_q, wq),
+                   range_of(dnorm_k, wk)},
+                  {range_of(q, vq.bytes), range_of(k, vk.bytes), range_of(dqo, qb),
+                   range_of(dko, kb), range_of(norm_q, wq), range_of(norm_k, wk),
+                   range_of(rot, sizeof(float) * (size_t)P * R),
+                   range_of(positions, positions ? sizeof(int32_t) * tok : 0),
+                   range_of(seq_lens, seq_lens ? sizeof(int32_t) * B : 0)}))
+    return GBLA_ERR_INVALID_ARG;
+  a.dqo = dqo, a.dko = dko, a.qo = dq, a.ko = dk;
+  Scratch part;
+  if ((s = part.alloc(sizeof(float) * rotate_backward_floats(a), st)) != GBLA_OK) return s;
+  return from_cuda(rotate_backward(a, (float *)part.ptr, dnorm_q, dnorm_k, st));
+}
+
+gbla_status gbla_decay_attention(const void *q, const void *k, const void *v,
+                                 const float *log_decay, const int32_t *seq_lens,
+                                 const int64_t *strides, const float *state_in, void *o,
+                                 float *state_out, int B, int N, int H, int Hk, int D,
+                                 float scale, gbla_dtype dtype, gbla_algo algo,
+                                 gbla_stream_t stream) {
+  bool empty = false;
+  gbla_status s = check_dims(B, H, N, D, dtype, &empty);
+  if (s != GBLA_OK) return s;
+  if ((s = check_heads(H, Hk)) != GBLA_OK) return s;
+  if ((s = check_scale(scale)) != GBLA_OK) return s;
+  cudaStream_t st = (cudaStream_t)stream;
+  const size_t sb = sizeof(float) * D * D * (size_t)B * H;
+  if (empty) return pass_state(state_in, state_out, sb, st);
+  if ((s = check_ptrs({q, k, v, log_decay, o})) != GBLA_OK) return s;
+  if (!aligned_or_null({state_in, state_out})) return GBLA_ERR_INVALID_ARG;
+  if ((s = check_seq_lens(seq_lens)) != GBLA_OK) return s;
+  View vq, vk, vv;
+  if ((s = view_of(strides, 0, B, N, (long long)H * D, dtype, &vq)) != GBLA_OK) return s;
+  if ((s = view_of(strides, 1, B, N, (long long)Hk * D, dtype, &vk)) != GBLA_OK) return s;
+  if ((s = view_of(strides, 2, B, N, (long long)Hk * D, dtype, &vv)) != GBLA_OK) return s;
+  if (any_overlap({range_of(o, (size_t)B * N * H * D * elem_bytes(dtype)),
+                   range_of(state_out, state_out ? sb : 0)},
+                  {range_of(q, vq.bytes), range_of(k, vk.bytes), range_of(v, vv.bytes),
+                   range_of(log_decay, sizeof(float) * H),
+                   range_of(state_in, state_in ? sb : 0),
+                   range_of(seq_lens, seq_lens ? sizeof(int32_t) * B : 0)}))
+    return GBLA_ERR_INVALID_ARG;
+  ScanArgs a = {};
+  a.x = q, a.y = k, a.z = v;
+  for (int i = 0; i < 2; ++i) a.sx[i] = vq.s[i], a.sy[i] = vk.s[i], a.sz[i] = vv.s[i];
+  a.gx = 1, a.gy = a.gz = H / Hk;
+  a.out = o, a.log_decay = log_decay, a.seq_lens = seq_lens;
+  a.init = state_in, a.init_scale = 1.f, a.fin = state_out, a.fin_scale = 1.f;
+  a.B = B, a.N = N, a.H = H, a.D = D, a.scale = scale, a.dtype = dtype;
+  bool tc = false;
+  if ((s = scan_family(a, algo, &tc)) != GBLA_OK) return s;
+  return run_scan(a, tc, st);
+}
+
+gbla_status gbla_decay_attention_backward(
+    const void *q, const void *k, const void *v, const float *log_decay,
+    const int32_t *seq_lens, const int64_t *strides, const float *state_in, const void *d_o,
+    const float *dstate_out, void *dq, void *dk, void *dv, float *dstate_in, int B, int N, int H,
+    int Hk, int D, float scale, gbla_dtype dtype, gbla_algo algo, gbla_stream_t stream) {
+  bool empty = false;
+  gbla_status s = check_dims(B, H, N, D, dtype, &empty);
+  if (s != GBLA_OK) return s;
+  if ((s = check_heads(H, Hk)) != GBLA_OK) return s;
+  if ((s = check_scale(scale)) != GBLA_OK) return s;
+  cudaStream_t st = (cudaStream_t)stream;
+  const size_t sb = sizeof(float) * D * D * (size_t)B * H;
+  if (empty) return pass_state(dstate_out, dstate_in, sb, st);
+  if ((s = check_ptrs({q, k, v, log_decay, d_o, dq, dk, dv})) != GBLA_OK) return s;
+  if (!aligned_or_null({state_in, dstate_out, dstate_in})) return GBLA_ERR_INVALID_ARG;
+  if ((s = check_seq_lens(seq_lens)) != GBLA_OK) return s;
+  View vq, vk, vv, vo;
+  if ((s = view_of(strides, 0, B, N, (long long)H * D, dtype, &vq)) != GBLA_OK) return s;
+  if ((s = view_of(strides, 1, B, N, (long long)Hk * D, dtype, &vk)) != GBLA_OK) return s;
+  if ((s = view_of(strides, 2, B, N, (long long)Hk * D, dtype, &vv)) != GBLA_OK) return s;
+  if ((s = view_of(nullptr, 0, B, N, (long long)H * D, dtype, &vo)) != GBLA_OK) return s;
+  const size_t tok = (size_t)B * N, es = elem_bytes(dtype);
+  if (any_overlap({range_of(dq, tok * H * D * es), range_of(dk, tok * Hk * D * es),
+                   range_of(dv, tok * Hk * D * es), range_of(dstate_in, dstate_in ? sb : 0)},
+                  {range_of(q, vq.bytes), range_of(k, vk.bytes), range_of(v, vv.bytes),
+                   range_of(d_o, vo.bytes), range_of(log_decay, sizeof(float) * H),
+                   range_of(state_in, state_in ? sb : 0),
+                   range_of(dstate_out, dstate_out ? sb : 0),
+                   range_of(seq_lens, seq_lens ? sizeof(int32_t) * B : 0)}))
+    return GBLA_ERR_INVALID_ARG;
+  const int G = H / Hk;
+  // dq_t = S_t d_o_t: the scan over (d_o, v, k) with the state transposed
+  ScanArgs a = {};
+  a.x = d_o, a.y = v, a.z = k;
+  for (int i = 0; i < 2; ++i) a.sx[i] = vo.s[i], a.sy[i] = vv.s[i], a.sz[i] = vk.s[i];
+  a.gx = 1, a.gy = a.gz = G;
+  a.out = dq, a.zero_pad = true, a.log_decay = log_decay, a.seq_lens = seq_lens;
+  a.init = state_in, a.init_t = true, a.init_scale = 1.f, a.fin_scale = 1.f;
+  a.B = B, a.N = N, a.H = H, a.D = D, a.scale = scale, a.dtype = dtype;
+  bool tc = false;
+  if ((s = scan_family(a, algo, &tc)) != GBLA_OK) return s;
+  if ((s = run_scan(a, tc, st)) != GBLA_OK) return s;
+  // In reverse A_t = gamma A_{t+1} + q_t d_o_t^T (dstate_out at the end; held
+  // without the scale): dk_t = A_t v_t, dv_t = A_t^T k_t, dstate_in = gamma A_0.
+  // Shared heads: per query head in fp32, then summed.
+  Scratch plane;
+  if (G > 1 && (s = plane.alloc(sizeof(float) * tok * H * D, st)) != GBLA_OK) return s;
+  for (int i = 0; i < 2; ++i) {
+    ScanArgs r = a;
+    r.x = i == 0 ? v : k, r.y = i == 0 ? d_o : q, r.z = i == 0 ? q : d_o;
+    const View &rx = i == 0 ? vv : vk, &ry = i == 0 ? vo : vq, &rz = i == 0 ? vq : vo;
+    for (int j = 0; j < 2; ++j) r.sx[j] = rx.s[j], r.sy[j] = ry.s[j], r.sz[j] = rz.s[j];
+    r.gx = G, r.gy = r.gz = 1;
+    void *grad = i == 0 ? dk : dv;
+    r.out = G > 1 ? plane.ptr : grad, r.out_f32 = G > 1;
+    r.init = dstate_out, r.init_t = i == 0, r.init_scale = 1.f / scale;
+    r.fin = i == 0 ? nullptr : dstate_in, r.fin_scale = scale;
+    r.reverse = true;
+    if ((s = run_scan(r, tc, st)) != GBLA_OK) return s;
+    if (G > 1 && (s = from_cuda(sum_shared_heads((const float *)plane.ptr, grad, (long long)tok,
+                                                 Hk, G, D, dtype, st))) != GBLA_OK)
+      return s;
+  }
+  return GBLA_OK;
+}
+
+gbla_status gbla_decay_attention_step(const void *q, const void *k, const void *v,
+                                      const float *log_decay, const int32_t *slots,
+                                      const int64_t *strides, float *state, void *o, int B,
+                                      int H, int Hk, int D, int n_slots, float scale,
+                                      gbla_dtype dtype, gbla_stream_t stream) {
+  bool empty = false;
+  gbla_status s = check_dims(B, H, 1, D, dtype, &empty);
+  if (s != GBLA_OK) return s;
+  if ((s = check_heads(H, Hk)) != GBLA_OK) return s;
+  if ((s = check_scale(scale)) != GBLA_OK) return s;
+  if (n_slots < 0 || (slots == nullptr && B > n_slots) ||
+      (unsigned long long)n_slots * H * D * D > (1ull << 40))
+    return GBLA_ERR_INVALID_ARG;
+  if (empty || n_slots == 0) return GBLA_OK;
+  if ((s = check_ptrs({q, k, v, log_decay, state, o})) != GBLA_OK) return s;
+  if ((s = check_seq_lens(slots)) != GBLA_OK) return s;
+  View view[3];
+  for (int i = 0; i < 3; ++i) {
+    const int64_t pair[2] = {strides ? strides[i] : 0, 0};
+    if ((s = view_of(strides ? pair : nullptr, 0, B, 1, (long long)(i ? Hk : H) * D, dtype,
+                     &view[i])) != GBLA_OK)
+      return s;
+  }
+  if (any_overlap({range_of(state, sizeof(float) * (size_t)n_slots * H * D * D),
+                   range_of(o, (size_t)B * H * D * elem_bytes(dtype))},
+                  {range_of(q, view[0].bytes), range_of(k, view[1].bytes),
+                   range_of(v, view[2].bytes), range_of(log_decay, sizeof(float) * H),
+                   range_of(slots, slots ? sizeof(int32_t) * B : 0)}))
+    return GBLA_ERR_INVALID_ARG;
+  StepArgs a = {q, k, v, view[0].s[0], view[1].s[0], view[2].s[0], log_decay, slots, state, o,
+                B, H, Hk, D, n_slots, scale, dtype};
+  return from_cuda(decay_step(a, (cudaStream_t)stream));
 }
 
 }  // extern "C"

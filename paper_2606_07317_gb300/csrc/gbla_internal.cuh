@@ -158,6 +158,75 @@ cudaError_t sa_forward(const void *q, const void *k, const void *v, const int32_
                        void *o, int B, int H, int N, cudaStream_t st);
 unsigned sa_device_error(bool reset);
 
+// ---- per-head norm and rotation of q and k (gbla_rotate.cu) ----------------
+struct RotateArgs {
+  const void *q, *k;            // [B, N, H, D], [B, N, Hk, D] with the strides below
+  const void *dqo, *dko;        // backward: gradients of the results (contiguous)
+  const float *norm_q, *norm_k, *rot;
+  const int32_t *positions, *seq_lens;
+  void *qo, *ko;                // results, or dq and dk (contiguous)
+  long long sq[2], sk[2];       // element strides (batch, token)
+  int B, N, H, Hk, D, R, P;
+  float eps;
+  bool interleaved;
+  gbla_dtype dtype;
+};
+cudaError_t rotate_forward(const RotateArgs &a, cudaStream_t st);
+// Floats of scratch of the backward (partial sums of the weight gradients).
+size_t rotate_backward_floats(const RotateArgs &a);
+cudaError_t rotate_backward(const RotateArgs &a, float *part, float *dnorm_q, float *dnorm_k,
+                            cudaStream_t st);
+
+// ---- decayed linear attention (gbla_decay.cu, gbla_decay_tc.cu) ------------
+// One scan over the tokens of every (batch, head), gamma = exp(log_decay[h]):
+//   out_t = scale [ sum gamma^|t-j| (x_t . y_j) z_j + (inter term of `init`) ]
+// over j <= t (forward) or j >= t (reverse); the carried state is
+// S[d][e] = sum gamma^... y[d] z[e].  The forward, and each of the backward's
+// dq, dk and dv, are this scan with other tensors in the three places.
+struct ScanArgs {
+  const void *x, *y, *z;                // token-major, heads adjacent, D values each
+  long long sx[2], sy[2], sz[2];        // element strides (batch, token)
+  int gx, gy, gz;                       // query heads sharing a head of x, y, z (head = h / g)
+  void *out;                            // [B, N, H, D] contiguous
+  bool out_f32;                         // fp32 results whatever the type
+  bool zero_pad;                        // rows past the end written as zeros (else left alone)
+  const float *log_decay;               // [H]
+  const int32_t *seq_lens;
+  const float *init;                    // [B, H, D, D] or NULL: state before the first token in
+  bool init_t;                          //   scan order; transposed; multiplied by init_scale
+  float init_scale;
+  float *fin;                           // [B, H, D, D] or NULL: state after the last token;
+  float fin_scale;                      //   multiplied by fin_scale (never transposed)
+  bool reverse;
+  int B, N, H, D;
+  float scale;
+  gbla_dtype dtype;
+};
+// Scratch floats of a scan (partial states of the segments it is split into).
+size_t simt_scan_floats(const ScanArgs &a);
+cudaError_t simt_scan(const ScanArgs &a, float *scratch, cudaStream_t st);
+// The same on tensor cores (gbla_decay_tc.cu): bf16, D in {64, 128}, sm_103.
+bool tc_scan_supports(const ScanArgs &a);
+size_t tc_scan_floats(const ScanArgs &a);
+cudaError_t tc_scan(const ScanArgs &a, float *scratch, cudaStream_t st);
+unsigned decay_device_error(bool reset);
+// dst[b, t, hk, :] = sum of the G heads of src that share it, in head order
+// (src fp32 [tokens, Hk * G, D], dst of the given type [tokens, Hk, D]).
+cudaError_t sum_shared_heads(const float *src, void *dst, long long tokens, int Hk, int G, int D,
+                             gbla_dtype dtype, cudaStream_t st);
+struct StepArgs {
+  const void *q, *k, *v;                // one token of each sequence; row strides in elements
+  long long sq, sk, sv;
+  const float *log_decay;
+  const int32_t *slots;
+  float *state;                         // [n_slots, H, D, D], updated in place
+  void *o;                              // [B, H, D] contiguous
+  int B, H, Hk, D, n_slots;
+  float scale;
+  gbla_dtype dtype;
+};
+cudaError_t decay_step(const StepArgs &a, cudaStream_t st);
+
 // Error bits set by tensor-core kernels whose bounded waits ran out (0 = none);
 // synchronous read of the current device, optionally clearing it.
 unsigned tc_device_error(bool reset);

@@ -22,6 +22,7 @@ ALGO_AUTO, ALGO_SIMT, ALGO_TC = 0, 1, 2
 FLAG_NO_CONV, FLAG_NO_GATE, FLAG_NO_NORM = 1, 2, 4
 FLAG_BLA = FLAG_NO_CONV | FLAG_NO_GATE | FLAG_NO_NORM
 CONV_WIDTH = 4
+ROTATE_INTERLEAVED = 1
 
 EXPORTED = ["gbla_forward", "gbla_forward_ex", "gbla_forward_variant", "gbla_forward_f32out",
             "gbla_backward", "gbla_backward_variant", "gbla_backward_from_state",
@@ -30,7 +31,9 @@ EXPORTED = ["gbla_forward", "gbla_forward_ex", "gbla_forward_variant", "gbla_for
             "gbla_forward_host", "gbla_state_floats", "gbla_rms_eps",
             "gbla_status_string", "gbla_version", "gbla_release", "gbla_launch_count",
             "gbla_state_static_scratch", "gbla_device_error", "gbla_last_cuda_error",
-            "gbla_project", "gbla_layer_forward", "gbla_attention_forward"]
+            "gbla_project", "gbla_layer_forward", "gbla_attention_forward",
+            "gbla_qk_norm_rotate", "gbla_qk_norm_rotate_backward", "gbla_decay_attention",
+            "gbla_decay_attention_backward", "gbla_decay_attention_step"]
 
 _lock = threading.Lock()
 _lib = None
@@ -96,6 +99,17 @@ def load(path: str | None = None):
         lib.gbla_readout.restype = _i
         lib.gbla_state_static_scratch.argtypes = [_vp] * 6 + [_i] * 5 + [_vp]
         lib.gbla_state_static_scratch.restype = _i
+        f, u32 = ctypes.c_float, ctypes.c_uint32
+        lib.gbla_qk_norm_rotate.argtypes = [_vp] * 10 + [_i] * 7 + [f, u32, _i, _vp]
+        lib.gbla_qk_norm_rotate.restype = _i
+        lib.gbla_qk_norm_rotate_backward.argtypes = [_vp] * 14 + [_i] * 7 + [f, u32, _i, _vp]
+        lib.gbla_qk_norm_rotate_backward.restype = _i
+        lib.gbla_decay_attention.argtypes = [_vp] * 9 + [_i] * 5 + [f, _i, _i, _vp]
+        lib.gbla_decay_attention.restype = _i
+        lib.gbla_decay_attention_backward.argtypes = [_vp] * 13 + [_i] * 5 + [f, _i, _i, _vp]
+        lib.gbla_decay_attention_backward.restype = _i
+        lib.gbla_decay_attention_step.argtypes = [_vp] * 8 + [_i] * 5 + [f, _i, _vp]
+        lib.gbla_decay_attention_step.restype = _i
         lib.gbla_state_floats.argtypes = [_i]
         lib.gbla_state_floats.restype = ctypes.c_size_t
         lib.gbla_rms_eps.argtypes = []
@@ -385,4 +399,179 @@ def state_static_scratch(k, v, gate, conv_w, seq_lens=None, out=None,
                                           _ptr(seq_lens), _ptr(out), B, H, N, D,
                                           _dtype_code(k), _stream(stream))
     _check(st, "gbla_state_static_scratch")
+    return out
+
+
+# --- causal decoder operators -------------------------------------------------
+
+def _heads(t, name, like=None, width=None):
+    """Checks a [B, N, heads, D] tensor whose heads are adjacent and whose head values are
+    contiguous (batch and token strides are free); returns its (batch, token) strides."""
+    if t.dim() != 4:
+        raise ValueError(f"{name} must be [B, N, heads, D]")
+    if like is not None:
+        if t.dtype != like.dtype or t.device != like.device:
+            raise ValueError(f"{name} must have the dtype and device of q")
+        if t.shape[:2] != like.shape[:2] or t.shape[3] != like.shape[3]:
+            raise ValueError(f"{name} must be [B, N, heads, D] with q's B, N and D")
+    if width is not None and t.shape[2] != width:
+        raise ValueError(f"{name} must have {width} heads")
+    B, N, H, D = t.shape
+    if t.numel() and ((D > 1 and t.stride(3) != 1) or (H > 1 and t.stride(2) != D)):
+        raise ValueError(f"the heads of {name} must be adjacent and their values contiguous")
+    return t.stride(0), t.stride(1)
+
+
+def _plain(t, name, shape, dtype, device):
+    """Checks an optional contiguous tensor."""
+    if t is None:
+        return
+    if t.dtype != dtype or tuple(t.shape) != tuple(shape) or not t.is_contiguous():
+        raise ValueError(f"{name} must be a contiguous {dtype} tensor of shape {tuple(shape)}")
+    if t.device != device:
+        raise ValueError(f"{name} must be on {device}")
+
+
+def _strides(*pairs):
+    flat = [s for p in pairs for s in p]
+    return (ctypes.c_int64 * len(flat))(*flat)
+
+
+def rotation_table(positions: int, R: int, base: float = 10000.0, device="cuda") -> torch.Tensor:
+    """[positions, R] fp32: cosines, then sines, of position * base^(-2 i / R) for the R / 2
+    pairs (computed in 64 bits) -- the `rot` of qk_norm_rotate."""
+    f = base ** (-torch.arange(0, R, 2, dtype=torch.float64) / max(R, 1))
+    a = torch.arange(positions, dtype=torch.float64)[:, None] * f
+    return torch.cat([a.cos(), a.sin()], 1).to(torch.float32).to(device)
+
+
+def _rotate_args(q, k, norm_q, norm_k, rot, positions, seq_lens):
+    sq, sk = _heads(q, "q"), _heads(k, "k", q)
+    B, N, H, D = q.shape
+    Hk, dev = k.shape[2], q.device
+    _plain(norm_q, "norm_q", (H, D), torch.float32, dev)
+    _plain(norm_k, "norm_k", (Hk, D), torch.float32, dev)
+    P, R = (rot.shape if rot is not None and rot.dim() == 2 else (0, 0))
+    _plain(rot, "rot", (P, R), torch.float32, dev)
+    _plain(positions, "positions", (B, N), torch.int32, dev)
+    _plain(seq_lens, "seq_lens", (B,), torch.int32, dev)
+    return _strides(sq, sk), (B, N, H, Hk, D, R, P)
+
+
+def qk_norm_rotate(q, k, norm_q, norm_k, rot=None, positions=None, seq_lens=None,
+                   eps: float = 1e-6, interleaved: bool = False, out=None, stream=None):
+    """Per-head RMS norm and position rotation of q [B, N, H, D] and k [B, N, Hk, D]
+    (gbla_qk_norm_rotate): weights norm_q [H, D], norm_k [Hk, D]; rot [P, R] from
+    rotation_table (None: norm alone); positions [B, N] int32 (None: token t has position
+    t).  q and k may be slices of a packed projection.  Returns (qo, ko), or fills `out`;
+    rows past seq_lens are not written."""
+    strides, dims = _rotate_args(q, k, norm_q, norm_k, rot, positions, seq_lens)
+    if out is None:
+        out = (torch.empty(q.shape, dtype=q.dtype, device=q.device),
+               torch.empty(k.shape, dtype=k.dtype, device=q.device))
+    _plain(out[0], "out[0]", q.shape, q.dtype, q.device)
+    _plain(out[1], "out[1]", k.shape, q.dtype, q.device)
+    st = load().gbla_qk_norm_rotate(
+        _ptr(q), _ptr(k), _ptr(norm_q), _ptr(norm_k), _ptr(rot), _ptr(positions),
+        _ptr(seq_lens), strides, _ptr(out[0]), _ptr(out[1]), *dims, float(eps),
+        ROTATE_INTERLEAVED if interleaved else 0, _dtype_code(q), _stream(stream))
+    _check(st, "gbla_qk_norm_rotate")
+    return out[0], out[1]
+
+
+def qk_norm_rotate_backward(q, k, norm_q, norm_k, rot, dqo, dko, positions=None, seq_lens=None,
+                            eps: float = 1e-6, interleaved: bool = False, stream=None) -> dict:
+    """Gradients of qk_norm_rotate (gbla_qk_norm_rotate_backward) for the contiguous
+    gradients dqo, dko of its results: dq, dk (0 past seq_lens), dnorm_q, dnorm_k."""
+    strides, dims = _rotate_args(q, k, norm_q, norm_k, rot, positions, seq_lens)
+    _plain(dqo, "dqo", q.shape, q.dtype, q.device)
+    _plain(dko, "dko", k.shape, q.dtype, q.device)
+    g = dict(dq=torch.empty(q.shape, dtype=q.dtype, device=q.device),
+             dk=torch.empty(k.shape, dtype=k.dtype, device=q.device),
+             dnorm_q=torch.empty_like(norm_q), dnorm_k=torch.empty_like(norm_k))
+    st = load().gbla_qk_norm_rotate_backward(
+        _ptr(q), _ptr(k), _ptr(norm_q), _ptr(norm_k), _ptr(rot), _ptr(positions),
+        _ptr(seq_lens), strides, _ptr(dqo), _ptr(dko), _ptr(g["dq"]), _ptr(g["dk"]),
+        _ptr(g["dnorm_q"]), _ptr(g["dnorm_k"]), *dims, float(eps),
+        ROTATE_INTERLEAVED if interleaved else 0, _dtype_code(q), _stream(stream))
+    _check(st, "gbla_qk_norm_rotate_backward")
+    return g
+
+
+def _decay_args(q, k, v, log_decay, seq_lens, state):
+    sq, sk = _heads(q, "q"), _heads(k, "k", q)
+    sv = _heads(v, "v", q, k.shape[2])
+    B, N, H, D = q.shape
+    _plain(log_decay, "log_decay", (H,), torch.float32, q.device)
+    _plain(seq_lens, "seq_lens", (B,), torch.int32, q.device)
+    _plain(state, "state", (B, H, D, D), torch.float32, q.device)
+    return _strides(sq, sk, sv), (B, N, H, k.shape[2], D)
+
+
+def decay_attention(q, k, v, log_decay, seq_lens=None, state=None, scale=None, out=None,
+                    return_state: bool = False, algo: int = ALGO_AUTO, stream=None):
+    """Causal linear attention with a decay for each head (gbla_decay_attention):
+    S_t = exp(log_decay) S_{t-1} + k_t v_t^T, o_t = scale q_t^T S_t for q [B, N, H, D] and
+    k, v [B, N, Hk, D]; `state` [B, H, D, D] fp32 is S before the first token, scale
+    defaults to D^-1/2.  Returns o, or (o, S after each sequence's last token) with
+    return_state; rows of o past seq_lens are not written."""
+    strides, dims = _decay_args(q, k, v, log_decay, seq_lens, state)
+    B, N, H, Hk, D = dims
+    if out is None:
+        out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+    _plain(out, "out", q.shape, q.dtype, q.device)
+    fin = torch.empty((B, H, D, D), dtype=torch.float32, device=q.device) if return_state else None
+    st = load().gbla_decay_attention(
+        _ptr(q), _ptr(k), _ptr(v), _ptr(log_decay), _ptr(seq_lens), strides, _ptr(state),
+        _ptr(out), _ptr(fin), *dims, float(D ** -0.5 if scale is None else scale),
+        _dtype_code(q), int(algo), _stream(stream))
+    _check(st, "gbla_decay_attention")
+    return (out, fin) if return_state else out
+
+
+def decay_attention_backward(q, k, v, log_decay, do, seq_lens=None, state=None, dstate=None,
+                             scale=None, return_dstate: bool = False, algo: int = ALGO_AUTO,
+                             stream=None) -> dict:
+    """Gradients of decay_attention (gbla_decay_attention_backward): `do` [B, N, H, D]
+    contiguous, `dstate` [B, H, D, D] the gradient of the returned state (None: zeros).
+    Returns dq, dk, dv (0 past seq_lens; shared heads summed) and, with return_dstate,
+    dstate, the gradient of the first state."""
+    strides, dims = _decay_args(q, k, v, log_decay, seq_lens, state)
+    B, N, H, Hk, D = dims
+    _plain(do, "do", q.shape, q.dtype, q.device)
+    _plain(dstate, "dstate", (B, H, D, D), torch.float32, q.device)
+    g = {n: torch.empty(t.shape, dtype=q.dtype, device=q.device)
+         for n, t in (("dq", q), ("dk", k), ("dv", v))}
+    if return_dstate:
+        g["dstate"] = torch.empty((B, H, D, D), dtype=torch.float32, device=q.device)
+    st = load().gbla_decay_attention_backward(
+        _ptr(q), _ptr(k), _ptr(v), _ptr(log_decay), _ptr(seq_lens), strides, _ptr(state),
+        _ptr(do), _ptr(dstate), _ptr(g["dq"]), _ptr(g["dk"]), _ptr(g["dv"]),
+        _ptr(g.get("dstate")), *dims, float(D ** -0.5 if scale is None else scale),
+        _dtype_code(q), int(algo), _stream(stream))
+    _check(st, "gbla_decay_attention_backward")
+    return g
+
+
+def decay_attention_step(q, k, v, log_decay, state, slots=None, scale=None, out=None,
+                         stream=None) -> torch.Tensor:
+    """One token of each sequence (gbla_decay_attention_step): q [B, 1, H, D], k, v
+    [B, 1, Hk, D]; `state` [n_slots, H, D, D] fp32 is updated in place at slots[b] (int32;
+    None: slot b).  Rows whose slot is outside the pool are left alone.  Returns o."""
+    sq, sk = _heads(q, "q"), _heads(k, "k", q)
+    sv = _heads(v, "v", q, k.shape[2])
+    B, N, H, D = q.shape
+    if N != 1:
+        raise ValueError("q, k and v hold one token of each sequence")
+    _plain(log_decay, "log_decay", (H,), torch.float32, q.device)
+    _plain(slots, "slots", (B,), torch.int32, q.device)
+    _plain(state, "state", (state.shape[0], H, D, D), torch.float32, q.device)
+    if out is None:
+        out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+    _plain(out, "out", q.shape, q.dtype, q.device)
+    st = load().gbla_decay_attention_step(
+        _ptr(q), _ptr(k), _ptr(v), _ptr(log_decay), _ptr(slots), _strides(sq[:1], sk[:1], sv[:1]),
+        _ptr(state), _ptr(out), B, H, k.shape[2], D, state.shape[0],
+        float(D ** -0.5 if scale is None else scale), _dtype_code(q), _stream(stream))
+    _check(st, "gbla_decay_attention_step")
     return out

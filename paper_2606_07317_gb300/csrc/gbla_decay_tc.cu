@@ -5,7 +5,10 @@
 //   scores  A_rj  = x_r . y_j                        (M64 N64 KD)
 //   results out_r = scale [ sum_j (w_rj A_rj) z_j + u_r x_r^T S ]
 //                                                    (M64 ND K64, M64 ND KD)
-//   state   S'    = c S + sum_j (v_j y_j) z_j^T      (MD ND K64)
+//   state   S'    = c S + sum_j (v_j y_j) z_j^T      (MD ND K64, a time for each term)
+// D = 64: y's tile and the state (transposed) lie one behind the other, so that
+// scores and x_r^T S are one product of N = 128, and the terms of the state's
+// product share one of N = 128: an MMA of M = 64 takes about as long at N = 64.
 // forward: w = gamma^{r-j} (j <= r), u = gamma^{r+1}, v = gamma^{n-1-j}, c = gamma^n
 // for n tokens in the chunk; reverse: w = gamma^{j-r} (j >= r), u = gamma^{64-r},
 // v = gamma^j, c = gamma^64, and u = gamma^{n-1-r}, c = gamma^{n-1} in the first
@@ -53,20 +56,23 @@ constexpr int kMaxCluster = 8;
 
 template <int D, int kTerms>
 struct Shape {
+  static constexpr bool kMerged = D == 64;                 // scores and inter results in one MMA
   static constexpr int kB = D / 64;                        // 64-channel blocks
   static constexpr int kTile = kB * kBlk;                  // one tensor's chunk
-  static constexpr int kStages = D == 64 ? 5 : (kTerms == 2 ? 3 : 2);
+  static constexpr int kSBytes = D * D * 2;                // the state rounded to bf16
+  // rings of x, y and z tiles; merged: the state's tile follows y's in its slot
+  static constexpr int kNX = D == 64 ? 4 : (kTerms == 2 ? 3 : 2), kNY = D == 64 ? 4 : 3,
+                       kNZ = D == 64 ? 5 : 3;
+  static constexpr int kYSlot = kTile + (kMerged ? kSBytes : 0);
   static constexpr int kConv = D == 64 ? 2 : 1;            // buffers of v_j y_j
   static constexpr int kP = D == 64 ? 2 : 1;               // of weighted scores
-  static constexpr int kS = D == 64 ? 2 : 1;               // of the rounded state
   static constexpr int kO = D == 64 ? 2 : 1;               // of the results' accumulators
-  static constexpr int kDs = D == 64 ? 2 : 1;              // of the chunk's state
-  static constexpr int kSBytes = D * D * 2;
-  static constexpr int kOffConv = kStages * 3 * kTile;
+  static constexpr int kOffX = 0, kOffY = kOffX + kNX * kTile, kOffZ = kOffY + kNY * kYSlot;
+  static constexpr int kOffConv = kOffZ + kNZ * kTile;
   static constexpr int kOffP = kOffConv + kConv * kTerms * kTile;
   static constexpr int kOffS = kOffP + kP * kBlk;
-  static constexpr int kOffBar = kOffS + kS * kSBytes;
-  static constexpr int kBars = 2 * (kStages + kConv + kP + kS + kO + kDs) + 5;
+  static constexpr int kOffBar = kOffS + (kMerged ? 0 : kSBytes);
+  static constexpr int kBars = 2 * (kNX + kNY + kNZ + kConv + kP + kO) + 2 + 1 + 2 + 4 + 1;
   static constexpr int kOffMisc = kOffBar + kBars * 8;
   static constexpr int kSmem = kOffMisc + 16 + 1024;
   static_assert(kSmem <= 227 * 1024, "shared memory");
@@ -74,9 +80,13 @@ struct Shape {
   static constexpr int kOutWarp = 8 + kSWarps, kTmaWarp = kOutWarp + 4, kMmaWarp = kTmaWarp + 1;
   static constexpr int kThreads = (kMmaWarp + 1) * 32;
   static constexpr int kLoads = 3 * kB;                    // issuing lanes
-  // TMEM columns: scores [0, 128), per result buffer intra and inter, then the state
-  static constexpr uint32_t kColO = 128, kColDs = 384;
-  static_assert(kColO + kO * 2 * D <= kColDs && kColDs + kDs * D <= 512, "TMEM");
+  // TMEM columns.  Merged: two buffers of scores | inter results, two of intra
+  // results, the chunk's state (its large and its small terms side by side);
+  // else two of scores, inter, intra, state.
+  static constexpr uint32_t kColSc = 0, kScStep = kMerged ? 128 : 64;
+  static constexpr uint32_t kColInter = kMerged ? 64 : 128, kInterStep = kMerged ? 128 : 0;
+  static constexpr uint32_t kColIntra = 256, kIntraStep = kMerged ? 64 : 0;
+  static constexpr uint32_t kColDs = 384;
 };
 
 struct TcParams {
@@ -118,6 +128,12 @@ __device__ __forceinline__ void tmem_ld_16x64(uint32_t taddr, float (&v)[32]) {
 __device__ __forceinline__ void sts_u32(uint32_t a, uint32_t v) {
   asm volatile("st.shared.u32 [%0], %1;" ::"r"(a), "r"(v) : "memory");
 }
+// Shared-memory matrix descriptor (128-byte swizzle) of a tile, and the same
+// moved by a constant number of bytes: the address field's carry never leaves
+// the low word, so a step costs one addition.
+__device__ __forceinline__ uint64_t desc_at(uint64_t d, uint32_t bytes) {
+  return (d & 0xFFFFFFFF00000000ull) | (uint32_t)((uint32_t)d + (bytes >> 4));
+}
 // One lane of a converged warp.
 __device__ __forceinline__ bool elect_one() {
   uint32_t r;
@@ -143,13 +159,13 @@ __device__ __forceinline__ void cluster_wait() {
   asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
 }
 
-// The state rows of a thread: D = 64, rows and columns as tmem_ld_16x64 gives
-// them; D = 128, one row and 64 columns.
+// Place of a state thread's value i: D = 64, held transposed, as tmem_ld_16x64
+// gives it (rows e); D = 128, one row d and 64 columns.
 template <int D>
 __device__ __forceinline__ int state_at(int sw, int lane, int i, int *e) {
   if (D == 64) {
-    *e = 8 * (i >> 2) + 2 * (lane & 3) + (i & 1);
-    return 16 * sw + (lane >> 2) + 8 * ((i >> 1) & 1);
+    *e = 16 * sw + (lane >> 2) + 8 * ((i >> 1) & 1);
+    return 8 * (i >> 2) + 2 * (lane & 3) + (i & 1);
   }
   *e = 64 * (sw >> 2) + i;
   return 32 * (sw & 3) + lane;
@@ -165,11 +181,12 @@ __global__ void __launch_bounds__(Shape<D, kTerms>::kThreads, 1)
   extern __shared__ uint8_t smem_raw[];
   uint8_t *smem = (uint8_t *)(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);
   uint64_t *bar = (uint64_t *)(smem + Sh::kOffBar);
-  uint64_t *full = bar, *empty = full + Sh::kStages, *conv_full = empty + Sh::kStages,
+  uint64_t *fx = bar, *ex = fx + Sh::kNX, *fy = ex + Sh::kNX, *ey = fy + Sh::kNY,
+           *fz = ey + Sh::kNY, *ez = fz + Sh::kNZ, *conv_full = ez + Sh::kNZ,
            *conv_empty = conv_full + Sh::kConv, *p_full = conv_empty + Sh::kConv,
-           *p_empty = p_full + Sh::kP, *s_full = p_empty + Sh::kP, *s_empty = s_full + Sh::kS,
-           *o_full = s_empty + Sh::kS, *o_empty = o_full + Sh::kO, *ds_full = o_empty + Sh::kO,
-           *ds_empty = ds_full + Sh::kDs, *sc_full = ds_empty + Sh::kDs, *sc_empty = sc_full + 2,
+           *p_empty = p_full + Sh::kP, *o_full = p_empty + Sh::kP, *o_empty = o_full + Sh::kO,
+           *s_full = o_empty + Sh::kO, *s_empty = s_full + 2, *ds_full = s_empty + 1,
+           *ds_empty = ds_full + 1, *sc_full = ds_empty + 1, *sc_empty = sc_full + 2,
            *drained = sc_empty + 2;
   uint32_t *tmem_slot = (uint32_t *)(smem + Sh::kOffMisc);
   const AbortFlag ab{smem_u32(smem + Sh::kOffMisc + 4)};
@@ -205,14 +222,20 @@ __global__ void __launch_bounds__(Shape<D, kTerms>::kThreads, 1)
 
   if (tid == 0) {
     *(volatile int *)(smem + Sh::kOffMisc + 4) = 0;
-    for (int i = 0; i < Sh::kStages; ++i) mbar_init(&full[i], Sh::kLoads), mbar_init(&empty[i], 1);
+    for (int i = 0; i < Sh::kNX; ++i) mbar_init(&fx[i], Sh::kB), mbar_init(&ex[i], 1);
+    for (int i = 0; i < Sh::kNY; ++i) mbar_init(&fy[i], Sh::kB), mbar_init(&ey[i], 1);
+    for (int i = 0; i < Sh::kNZ; ++i) mbar_init(&fz[i], Sh::kB), mbar_init(&ez[i], 1);
     for (int i = 0; i < Sh::kConv; ++i) mbar_init(&conv_full[i], 4), mbar_init(&conv_empty[i], 1);
     for (int i = 0; i < Sh::kP; ++i) mbar_init(&p_full[i], 4), mbar_init(&p_empty[i], 1);
-    for (int i = 0; i < Sh::kS; ++i) mbar_init(&s_full[i], Sh::kSWarps), mbar_init(&s_empty[i], 1);
     for (int i = 0; i < Sh::kO; ++i) mbar_init(&o_full[i], 1), mbar_init(&o_empty[i], 4);
-    for (int i = 0; i < Sh::kDs; ++i)
-      mbar_init(&ds_full[i], 1), mbar_init(&ds_empty[i], Sh::kSWarps);
-    for (int i = 0; i < 2; ++i) mbar_init(&sc_full[i], 1), mbar_init(&sc_empty[i], 4);
+    for (int i = 0; i < 2; ++i) {
+      mbar_init(&s_full[i], Sh::kSWarps);
+      mbar_init(&sc_full[i], 1);
+      mbar_init(&sc_empty[i], 4);
+    }
+    mbar_init(s_empty, 1);
+    mbar_init(ds_full, 1);
+    mbar_init(ds_empty, Sh::kSWarps);
     mbar_init(drained, 1);
     fence_mbar_init();
   }
@@ -240,114 +263,139 @@ __global__ void __launch_bounds__(Shape<D, kTerms>::kThreads, 1)
       const int t = lane / Sh::kB, blk = lane % Sh::kB;  // tensor, 64-channel block
       const CUtensorMap *tm = t == 0 ? &tm_x : t == 1 ? &tm_y : &tm_z;
       const int hd = h / (t == 0 ? p.gx : t == 1 ? p.gy : p.gz);
-      int g = 0;
-      for (; g < pre + cnt; ++g) {
-        const int s = g % Sh::kStages;
-        if (!mbar_wait(&empty[s], ((g / Sh::kStages) & 1) ^ 1, &ab)) {
+      uint64_t *f = t == 0 ? fx : t == 1 ? fy : fz, *e = t == 0 ? ex : t == 1 ? ey : ez;
+      const int slots = t == 0 ? Sh::kNX : t == 1 ? Sh::kNY : Sh::kNZ;
+      uint8_t *to = smem + (t == 0 ? Sh::kOffX : t == 1 ? Sh::kOffY : Sh::kOffZ) + blk * kBlk;
+      const int size = t == 1 ? Sh::kYSlot : Sh::kTile;
+      const int first = t == 0 ? pre : 0, steps = pre + cnt - first;  // x: the scan alone
+      int i = 0;
+      for (; i < steps; ++i) {
+        const int s = i % slots;
+        if (!mbar_wait(&e[s], ((i / slots) & 1) ^ 1, &ab)) {
           decay_error(1, ab);
           break;
         }
-        if (t == 0 && g < pre) {
-          mbar_arrive(&full[s]);
-          continue;
-        }
-        mbar_arrive_expect_tx(&full[s], kBlk);
-        tma_load_4d(smem + (s * 3 + t) * Sh::kTile + blk * kBlk, tm, &full[s], blk * 64, hd,
-                    token_of(place_of(g)), b);
+        mbar_arrive_expect_tx(&f[s], kBlk);
+        tma_load_4d(to + s * size, tm, &f[s], blk * 64, hd, token_of(place_of(first + i)), b);
       }
-      if (g < pre + cnt)  // gave up: no copy may land after the CTA is gone
-        for (int f = max(0, g - Sh::kStages); f < g; ++f)
-          mbar_wait(&full[f % Sh::kStages], (f / Sh::kStages) & 1, nullptr);
+      if (i < steps)  // gave up: no copy may land after the CTA is gone
+        for (int k = max(0, i - slots); k < i; ++k)
+          mbar_wait(&f[k % slots], (k / slots) & 1, nullptr);
     }
     __syncwarp();
   } else if (warp == Sh::kMmaWarp) {
     // ----------------------------------------------------------------- MMAs
     if (elect_one()) {
-      constexpr uint32_t id_sc = idesc_bf16_f32(64, 64, 0, 0);
-      constexpr uint32_t id_o = idesc_bf16_f32(64, D, 0, 1);
-      constexpr uint32_t id_s = idesc_bf16_f32(D, D, 1, 1);
       const uint32_t base = smem_u32(smem);
       bool ok = true;
       auto wait = [&](uint64_t *m, uint32_t parity) {
         if (ok && !mbar_wait(m, parity, &ab)) decay_error(2, ab), ok = false;
         return ok;
       };
-      // the chunk's own state: sum of (v_j y_j) z_j^T, the small terms first
-      auto state_mma = [&](int g) {
-        const int s = g % Sh::kStages, cb = g % Sh::kConv, db = g % Sh::kDs;
+      // the chunk's own state, sum of (v_j y_j) z_j^T; own: in the pass over the
+      // segment's own state, after which the tiles are free
+      auto state_mma = [&](int g, bool own) {
+        const int cb = g % Sh::kConv, sz = g % Sh::kNZ;
+        if (!wait(&fz[sz], (g / Sh::kNZ) & 1)) return;
         if (!wait(&conv_full[cb], (g / Sh::kConv) & 1)) return;
-        if (g >= Sh::kDs && !wait(&ds_empty[db], ((g / Sh::kDs) & 1) ^ 1)) return;
+        if (g >= 1 && !wait(ds_empty, (g & 1) ^ 1)) return;
         tc_fence_after();
-        const uint32_t zs = base + (s * 3 + 2) * Sh::kTile;
-        const uint32_t d = tmem + Sh::kColDs + db * D;
-#pragma unroll
-        for (int t = kTerms - 1; t >= 0; --t) {
-          const uint32_t cs = base + Sh::kOffConv + (cb * kTerms + t) * Sh::kTile;
+        const uint64_t zd = sw128_desc(base + Sh::kOffZ + sz * Sh::kTile, kBlk, 1024);
+        const uint64_t cd =
+            sw128_desc(base + Sh::kOffConv + cb * kTerms * Sh::kTile, kBlk, 1024);
+        const uint32_t d = tmem + Sh::kColDs;
+        if constexpr (Sh::kMerged) {
+          // transposed (M = e): the first two terms side by side in N, the third
+          // onto the second
+          constexpr uint32_t id2 = idesc_bf16_f32(64, 128, 1, 1), id1 = idesc_bf16_f32(64, 64, 1, 1);
 #pragma unroll
           for (int k = 0; k < 4; ++k)
-            mma_bf16(d, sw128_desc(cs + k * 2048, kBlk, 1024), sw128_desc(zs + k * 2048, kBlk, 1024),
-                     id_s, t != kTerms - 1 || k != 0);
+            mma_bf16(d, desc_at(zd, k * 2048), desc_at(cd, k * 2048), id2, k != 0);
+          if constexpr (kTerms == 3)
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+              mma_bf16(d + 64, desc_at(zd, k * 2048), desc_at(cd, 2 * Sh::kTile + k * 2048), id1, 1);
+        } else {
+          constexpr uint32_t id_s = idesc_bf16_f32(D, D, 1, 1);
+#pragma unroll
+          for (int t = kTerms - 1; t >= 0; --t)  // the small terms first
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+              mma_bf16(d, desc_at(cd, t * Sh::kTile + k * 2048), desc_at(zd, k * 2048), id_s,
+                       t != kTerms - 1 || k != 0);
         }
-        mma_commit(&ds_full[db]);
+        mma_commit(ds_full);
         mma_commit(&conv_empty[cb]);
+        if (own) {
+          mma_commit(&ey[g % Sh::kNY]);
+          mma_commit(&ez[sz]);
+        }
       };
-      for (int g = 0; g < pre && ok; ++g) {
-        const int s = g % Sh::kStages;
-        if (!wait(&full[s], (g / Sh::kStages) & 1)) break;
-        state_mma(g);
-        mma_commit(&empty[s]);
-      }
+      // scores of the scan's chunk i; merged: and x_r^T S.  The chunk's state
+      // went before, so its keys are there and those past the end are zero.
       auto score_mma = [&](int i) {
-        const int g = pre + i, s = g % Sh::kStages;
-        if (!wait(&full[s], (g / Sh::kStages) & 1)) return;
-        // rows past the end are zeroed with the weighted keys of the same chunk
-        if (token_of(q0 + i) + kC > L && !wait(&conv_full[g % Sh::kConv], (g / Sh::kConv) & 1))
-          return;
+        const int sx = i % Sh::kNX, sy = (pre + i) % Sh::kNY;
+        if (!wait(&fx[sx], (i / Sh::kNX) & 1)) return;
         if (i >= 2 && !wait(&sc_empty[i & 1], ((i >> 1) & 1) ^ 1)) return;
+        if constexpr (Sh::kMerged) {
+          if (i >= 2 && !wait(&o_empty[i & 1], ((i >> 1) & 1) ^ 1)) return;
+          if (!wait(&s_full[i & 1], (i >> 1) & 1)) return;
+        }
         tc_fence_after();
-        const uint32_t xs = base + s * 3 * Sh::kTile, ys = xs + Sh::kTile;
+        constexpr uint32_t id = idesc_bf16_f32(64, Sh::kMerged ? 128 : 64, 0, 0);
+        const uint64_t xd = sw128_desc(base + Sh::kOffX + sx * Sh::kTile, 16, 1024);
+        const uint64_t yd = sw128_desc(base + Sh::kOffY + sy * Sh::kYSlot, 16, 1024);
 #pragma unroll
         for (int k = 0; k < D / 16; ++k) {
           const uint32_t off = (k >> 2) * kBlk + (k & 3) * 32;
-          mma_bf16(tmem + 64 * (i & 1), sw128_desc(xs + off, 16, 1024),
-                   sw128_desc(ys + off, 16, 1024), id_sc, k != 0);
+          mma_bf16(tmem + Sh::kColSc + Sh::kScStep * (i & 1), desc_at(xd, off), desc_at(yd, off), id,
+                   k != 0);
         }
         mma_commit(&sc_full[i & 1]);
+        mma_commit(&ey[sy]);
+        if constexpr (Sh::kMerged) mma_commit(&ex[sx]);
       };
-      auto rest_mma = [&](int j) {
-        const int g = pre + j, s = g % Sh::kStages, ob = j % Sh::kO, sb = j % Sh::kS,
-                  pb = j % Sh::kP;
-        state_mma(g);
-        if (!ok) return;
-        if (j >= Sh::kO && !wait(&o_empty[ob], ((j / Sh::kO) & 1) ^ 1)) return;
-        if (!wait(&s_full[sb], (j / Sh::kS) & 1)) return;
+      auto inter_mma = [&](int i) {  // x_r^T S on its own
+        const int sx = i % Sh::kNX;
+        if (i >= 1 && !wait(&o_empty[0], (i & 1) ^ 1)) return;
+        if (!wait(&s_full[i & 1], (i >> 1) & 1)) return;
         tc_fence_after();
-        const uint32_t xs = base + s * 3 * Sh::kTile, zs = xs + 2 * Sh::kTile;
-        const uint32_t ss = base + Sh::kOffS + sb * Sh::kSBytes;
-        const uint32_t intra = tmem + Sh::kColO + ob * 2 * D, inter = intra + D;
+        constexpr uint32_t id = idesc_bf16_f32(64, D, 0, 1);
+        const uint64_t xd = sw128_desc(base + Sh::kOffX + sx * Sh::kTile, 16, 1024);
+        const uint64_t sd = sw128_desc(base + Sh::kOffS, D * 128, 1024);
 #pragma unroll
         for (int k = 0; k < D / 16; ++k)
-          mma_bf16(inter, sw128_desc(xs + (k >> 2) * kBlk + (k & 3) * 32, 16, 1024),
-                   sw128_desc(ss + k * 2048, D * 128, 1024), id_o, k != 0);
-        mma_commit(&s_empty[sb]);
+          mma_bf16(tmem + Sh::kColInter, desc_at(xd, (k >> 2) * kBlk + (k & 3) * 32),
+                   desc_at(sd, k * 2048), id, k != 0);
+        mma_commit(s_empty);
+        mma_commit(&ex[sx]);
+      };
+      auto intra_mma = [&](int j) {  // sum_j (w_rj A_rj) z_j
+        const int g = pre + j, sz = g % Sh::kNZ, pb = j % Sh::kP, ob = j % Sh::kO;
         if (!wait(&p_full[pb], (j / Sh::kP) & 1)) return;
         tc_fence_after();
-        const uint32_t ps = base + Sh::kOffP + pb * kBlk;
+        constexpr uint32_t id = idesc_bf16_f32(64, D, 0, 1);
+        const uint64_t pd = sw128_desc(base + Sh::kOffP + pb * kBlk, 16, 1024);
+        const uint64_t zd = sw128_desc(base + Sh::kOffZ + sz * Sh::kTile, kBlk, 1024);
 #pragma unroll
         for (int k = 0; k < 4; ++k)
-          mma_bf16(intra, sw128_desc(ps + k * 32, 16, 1024), sw128_desc(zs + k * 2048, kBlk, 1024),
-                   id_o, k != 0);
+          mma_bf16(tmem + Sh::kColIntra + Sh::kIntraStep * ob, desc_at(pd, k * 32),
+                   desc_at(zd, k * 2048), id, k != 0);
         mma_commit(&p_empty[pb]);
         mma_commit(&o_full[ob]);
-        mma_commit(&empty[s]);
+        mma_commit(&ez[sz]);
       };
+      for (int g = 0; g < pre && ok; ++g) state_mma(g, true);
+      if (ok) state_mma(pre, false);
+      // Scores of chunk i, results of chunk i - 1 (whose scores have been
+      // weighted meanwhile), state of chunk i + 1 (which leaves a whole round for
+      // the state to reach the scores of i + 1).
       for (int i = 0; i <= cnt && ok; ++i) {
-        // the scores of the next chunk go out before the rest of this one; not
-        // those of a chunk cut short, which wait for its weighted keys
-        const bool cut = i < cnt && token_of(q0 + i) + kC > L;
-        if (i < cnt && !cut) score_mma(i);
-        if (i >= 1 && ok) rest_mma(i - 1);
-        if (cut && ok) score_mma(i);
+        if (i < cnt) score_mma(i);
+        if (i >= 1 && ok) intra_mma(i - 1);
+        if (i + 1 < cnt && ok) state_mma(pre + i + 1, false);
+        if constexpr (!Sh::kMerged)
+          if (i < cnt && ok) inter_mma(i);
       }
       mma_commit(drained);  // nothing is in flight when TMEM is freed
       if (!mbar_wait(drained, 0, nullptr)) decay_error(512, ab);
@@ -369,7 +417,7 @@ __global__ void __launch_bounds__(Shape<D, kTerms>::kThreads, 1)
       if (!mbar_wait(&sc_full[i & 1], (i >> 1) & 1, &ab)) decay_error(4, ab);
       tc_fence_after();
       float a[32];
-      tmem_ld_16x64(tmem + ((uint32_t)(32 * warp) << 16) + 64 * (i & 1), a);
+      tmem_ld_16x64(tmem + ((uint32_t)(32 * warp) << 16) + Sh::kColSc + Sh::kScStep * (i & 1), a);
       tmem_ld_wait_regs(a);
       tc_fence_before();
       __syncwarp();
@@ -395,49 +443,63 @@ __global__ void __launch_bounds__(Shape<D, kTerms>::kThreads, 1)
       const int r = rr + 16 * k;
       wr[k] = decay_pow(l2, (float)(p.reverse ? r : kC - 1 - r));
     }
+    // one 16-byte piece: kTerms bf16 numbers for each of its 8 products
+    auto split = [&](const uint4 &u, float w, uint32_t to) {
+      const uint32_t in[4] = {u.x, u.y, u.z, u.w};
+      uint32_t o[kTerms][4];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        float2 f = bf2_to_f2(in[e]);
+        f.x *= w, f.y *= w;
+#pragma unroll
+        for (int t = 0; t < kTerms; ++t) {
+          o[t][e] = f2_to_bf2(f.x, f.y);
+          if (t + 1 < kTerms) {
+            const float2 q = bf2_to_f2(o[t][e]);
+            f.x -= q.x, f.y -= q.y;  // exact
+          }
+        }
+      }
+#pragma unroll
+      for (int t = 0; t < kTerms; ++t)
+        sts_v4(to + t * Sh::kTile, make_uint4(o[t][0], o[t][1], o[t][2], o[t][3]));
+    };
     for (int g = 0; g < pre + cnt; ++g) {
-      const int s = g % Sh::kStages, cb = g % Sh::kConv;
+      const int sy = g % Sh::kNY, cb = g % Sh::kConv;
       const int n = min(kC, L - token_of(place_of(g)));
-      if (!mbar_wait(&full[s], (g / Sh::kStages) & 1, &ab)) decay_error(16, ab);
+      if (!mbar_wait(&fy[sy], (g / Sh::kNY) & 1, &ab)) decay_error(16, ab);
       if (g >= Sh::kConv && !mbar_wait(&conv_empty[cb], ((g / Sh::kConv) & 1) ^ 1, &ab))
         decay_error(32, ab);
-      const uint32_t ys = smem_u32(smem + (s * 3 + 1) * Sh::kTile);
-      const uint32_t cs = smem_u32(smem + Sh::kOffConv + cb * kTerms * Sh::kTile);
-#pragma unroll
-      for (int k = 0; k < 4; ++k) {
-        const int r = rr + 16 * k;
-        float w = wr[k];
-        if (n < kC && !p.reverse) w = r < n ? decay_pow(l2, (float)(n - 1 - r)) : 0.f;
+      const uint32_t ys = smem_u32(smem + Sh::kOffY + sy * Sh::kYSlot) + rr * 128 + ((ch ^ (rr & 7)) << 4);
+      const uint32_t cs = smem_u32(smem + Sh::kOffConv + cb * kTerms * Sh::kTile) + rr * 128 +
+                          ((ch ^ (rr & 7)) << 4);
+      if (n == kC) {
 #pragma unroll
         for (int blk = 0; blk < Sh::kB; ++blk) {
-          const uint32_t at = blk * kBlk + r * 128 + ((ch ^ (r & 7)) << 4);
-          if (r >= n) {  // padding may hold NaN: keys, values and weighted keys become 0
-            const uint4 z = make_uint4(0, 0, 0, 0);
-            sts_v4(ys + at, z);
-            sts_v4(ys + Sh::kTile + at, z);
+          uint4 u[4];
 #pragma unroll
-            for (int t = 0; t < kTerms; ++t) sts_v4(cs + t * Sh::kTile + at, z);
+          for (int k = 0; k < 4; ++k) u[k] = lds_v4(ys + blk * kBlk + k * 2048);
+#pragma unroll
+          for (int k = 0; k < 4; ++k) split(u[k], wr[k], cs + blk * kBlk + k * 2048);
+        }
+      } else {
+        // the chunk with the sequence's end: padding may hold NaN, so keys, values
+        // and weighted keys past the end become 0
+        const int sz = g % Sh::kNZ;
+        if (!mbar_wait(&fz[sz], (g / Sh::kNZ) & 1, &ab)) decay_error(16, ab);
+        const uint32_t zs = smem_u32(smem + Sh::kOffZ + sz * Sh::kTile) + rr * 128 + ((ch ^ (rr & 7)) << 4);
+        const uint4 zero = make_uint4(0, 0, 0, 0);
+#pragma unroll 1
+        for (int k = 0; k < 4 * Sh::kB; ++k) {
+          const int r = rr + 16 * (k & 3), off = (k >> 2) * kBlk + (k & 3) * 2048;
+          if (r < n) {
+            split(lds_v4(ys + off), decay_pow(l2, (float)(p.reverse ? r : n - 1 - r)), cs + off);
             continue;
           }
-          const uint4 u = lds_v4(ys + at);
-          const uint32_t in[4] = {u.x, u.y, u.z, u.w};
-          uint32_t o[kTerms][4];
+          sts_v4(ys + off, zero);
+          sts_v4(zs + off, zero);
 #pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            float2 f = bf2_to_f2(in[e]);
-            f.x *= w, f.y *= w;
-#pragma unroll
-            for (int t = 0; t < kTerms; ++t) {
-              o[t][e] = f2_to_bf2(f.x, f.y);
-              if (t + 1 < kTerms) {
-                const float2 q = bf2_to_f2(o[t][e]);
-                f.x -= q.x, f.y -= q.y;  // exact
-              }
-            }
-          }
-#pragma unroll
-          for (int t = 0; t < kTerms; ++t)
-            sts_v4(cs + t * Sh::kTile + at, make_uint4(o[t][0], o[t][1], o[t][2], o[t][3]));
+          for (int t = 0; t < kTerms; ++t) sts_v4(cs + t * Sh::kTile + off, zero);
         }
       }
       fence_proxy_async_smem();
@@ -450,24 +512,28 @@ __global__ void __launch_bounds__(Shape<D, kTerms>::kThreads, 1)
     float S[kNV];
 #pragma unroll
     for (int i = 0; i < kNV; ++i) S[i] = 0.f;
-    const uint32_t dst = tmem + ((uint32_t)(32 * (sw & 3)) << 16) + Sh::kColDs +
+    const uint32_t src = tmem + ((uint32_t)(32 * (sw & 3)) << 16) + Sh::kColDs +
                          (D == 64 ? 0 : 64 * (sw >> 2));
     // S = a S + f (the state of step g's chunk)
     auto take = [&](int g, float a, float f) {
-      const int db = g % Sh::kDs;
-      if (!mbar_wait(&ds_full[db], (g / Sh::kDs) & 1, &ab)) decay_error(64, ab);
+      if (!mbar_wait(ds_full, g & 1, &ab)) decay_error(64, ab);
       tc_fence_after();
       if constexpr (D == 64) {
-        float v[32];
-        tmem_ld_16x64(dst + db * D, v);
-        tmem_ld_wait_regs(v);
 #pragma unroll
-        for (int i = 0; i < 32; ++i) S[i] = fmaf(f, v[i], a * S[i]);
+        for (int i = 0; i < 32; ++i) S[i] *= a;
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {  // the small terms first
+          float v[32];
+          tmem_ld_16x64(src + 64 * (1 - t), v);
+          tmem_ld_wait_regs(v);
+#pragma unroll
+          for (int i = 0; i < 32; ++i) S[i] = fmaf(f, v[i], S[i]);
+        }
       } else {
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
           float v[16];
-          tmem_ld16(dst + db * D + 16 * i, v);
+          tmem_ld16(src + 16 * i, v);
           tmem_ld_wait_regs(v);
 #pragma unroll
           for (int e = 0; e < 16; ++e) S[16 * i + e] = fmaf(f, v[e], a * S[16 * i + e]);
@@ -475,7 +541,7 @@ __global__ void __launch_bounds__(Shape<D, kTerms>::kThreads, 1)
       }
       tc_fence_before();
       __syncwarp();
-      if (lane == 0) mbar_arrive(&ds_empty[db]);
+      if (lane == 0) mbar_arrive(ds_empty);
     };
     if (ranks > 1) {
       // the segment's own state: chunks from its end in scan order to its start
@@ -513,22 +579,22 @@ __global__ void __launch_bounds__(Shape<D, kTerms>::kThreads, 1)
       }
     }
     for (int j = 0; j < cnt; ++j) {
-      const int sb = j % Sh::kS;
-      if (j >= Sh::kS && !mbar_wait(&s_empty[sb], ((j / Sh::kS) & 1) ^ 1, &ab))
-        decay_error(128, ab);
-      const uint32_t ss = smem_u32(smem + Sh::kOffS + sb * Sh::kSBytes);
-      if constexpr (D == 64) {
-        const int d = 16 * sw + (lane >> 2);
-        const uint32_t row = ss + d * 128 + (lane & 3) * 4;
+      if constexpr (D == 64) {  // behind the chunk's keys, once their slot is free
+        const int g = pre + j, sy = g % Sh::kNY;
+        if (!mbar_wait(&ey[sy], ((g / Sh::kNY) & 1) ^ 1, &ab)) decay_error(128, ab);
+        const int e = 16 * sw + (lane >> 2);
+        const uint32_t row = smem_u32(smem + Sh::kOffY + sy * Sh::kYSlot + Sh::kTile) + e * 128 +
+                             (lane & 3) * 4;
 #pragma unroll
         for (int k = 0; k < 8; ++k) {
-          const uint32_t at = row + ((k ^ (d & 7)) << 4);
+          const uint32_t at = row + ((k ^ (e & 7)) << 4);
           sts_u32(at, f2_to_bf2(S[4 * k], S[4 * k + 1]));
           sts_u32(at + 8 * 128, f2_to_bf2(S[4 * k + 2], S[4 * k + 3]));
         }
       } else {
+        if (j >= 1 && !mbar_wait(s_empty, (j & 1) ^ 1, &ab)) decay_error(128, ab);
         const int d = 32 * (sw & 3) + lane;
-        const uint32_t row = ss + (sw >> 2) * (D * 128) + d * 128;
+        const uint32_t row = smem_u32(smem + Sh::kOffS) + (sw >> 2) * (D * 128) + d * 128;
 #pragma unroll
         for (int k = 0; k < 8; ++k)
           sts_v4(row + ((k ^ (d & 7)) << 4),
@@ -538,7 +604,7 @@ __global__ void __launch_bounds__(Shape<D, kTerms>::kThreads, 1)
       }
       fence_proxy_async_smem();
       __syncwarp();
-      if (lane == 0) mbar_arrive(&s_full[sb]);
+      if (lane == 0) mbar_arrive(&s_full[j & 1]);
       const int t0 = token_of(q0 + j), n = min(kC, L - t0);
       const int span = !p.reverse ? n : (q0 + j == 0 ? n - 1 : kC);
       take(pre + j, decay_pow(l2, (float)span), 1.f);
@@ -555,7 +621,7 @@ __global__ void __launch_bounds__(Shape<D, kTerms>::kThreads, 1)
   } else {
     // ---------------------------------------------------------------- results
     const int ow = warp - Sh::kOutWarp, r0 = 16 * ow + (lane >> 2);
-    const uint32_t quarter = tmem + ((uint32_t)(32 * ow) << 16) + Sh::kColO;
+    const uint32_t quarter = tmem + ((uint32_t)(32 * ow) << 16);
     float u[2];
 #pragma unroll
     for (int k = 0; k < 2; ++k)
@@ -573,8 +639,8 @@ __global__ void __launch_bounds__(Shape<D, kTerms>::kThreads, 1)
 #pragma unroll
       for (int blk = 0; blk < Sh::kB; ++blk) {
         float a[32], s[32];
-        tmem_ld_16x64(quarter + ob * 2 * D + blk * 64, a);
-        tmem_ld_16x64(quarter + ob * 2 * D + D + blk * 64, s);
+        tmem_ld_16x64(quarter + Sh::kColIntra + Sh::kIntraStep * ob + blk * 64, a);
+        tmem_ld_16x64(quarter + Sh::kColInter + Sh::kInterStep * ob + blk * 64, s);
         tmem_ld_wait_regs(a);
         tmem_pin(s);
         if (blk == Sh::kB - 1) {

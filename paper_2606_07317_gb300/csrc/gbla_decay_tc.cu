@@ -38,6 +38,7 @@
 // Every mbarrier wait is bounded (2 s); one that runs out sets a bit in
 // g_decay_error and raises the CTA's abort flag.
 #include <mutex>
+#include <type_traits>
 
 #include "gbla_internal.cuh"
 #include "gbla_sm100.cuh"
@@ -61,18 +62,17 @@ struct Shape {
   static constexpr int kTile = kB * kBlk;                  // one tensor's chunk
   static constexpr int kSBytes = D * D * 2;                // the state rounded to bf16
   // rings of x, y and z tiles; merged: the state's tile follows y's in its slot
-  static constexpr int kNX = D == 64 ? 4 : (kTerms == 2 ? 3 : 2), kNY = D == 64 ? 4 : 3,
-                       kNZ = D == 64 ? 5 : 3;
+  static constexpr int kNY = D == 64 ? 4 : 3, kNZ = D == 64 ? 5 : 3;
   static constexpr int kYSlot = kTile + (kMerged ? kSBytes : 0);
   static constexpr int kConv = D == 64 ? 2 : 1;            // buffers of v_j y_j
   static constexpr int kP = D == 64 ? 2 : 1;               // of weighted scores
-  static constexpr int kO = D == 64 ? 2 : 1;               // of the results' accumulators
-  static constexpr int kOffX = 0, kOffY = kOffX + kNX * kTile, kOffZ = kOffY + kNY * kYSlot;
+  static constexpr int kOffX = 0, kOffY = kOffX + 2 * kTile, kOffZ = kOffY + kNY * kYSlot;
   static constexpr int kOffConv = kOffZ + kNZ * kTile;
   static constexpr int kOffP = kOffConv + kConv * kTerms * kTile;
   static constexpr int kOffS = kOffP + kP * kBlk;
-  static constexpr int kOffBar = kOffS + (kMerged ? 0 : kSBytes);
-  static constexpr int kBars = 2 * (kNX + kNY + kNZ + kConv + kP + kO) + 2 + 1 + 2 + 4 + 1;
+  static constexpr int kOffOut = kOffS + (kMerged ? 0 : kSBytes);  // 2 KB a result warp
+  static constexpr int kOffBar = kOffOut + kBlk;
+  static constexpr int kBars = 2 * (kNY + kNZ + kConv + kP) + 2 * 6 + 3;
   static constexpr int kOffMisc = kOffBar + kBars * 8;
   static constexpr int kSmem = kOffMisc + 16 + 1024;
   static_assert(kSmem <= 227 * 1024, "shared memory");
@@ -81,11 +81,12 @@ struct Shape {
   static constexpr int kThreads = (kMmaWarp + 1) * 32;
   static constexpr int kLoads = 3 * kB;                    // issuing lanes
   // TMEM columns.  Merged: two buffers of scores | inter results, two of intra
-  // results, the chunk's state (its large and its small terms side by side);
-  // else two of scores, inter, intra, state.
+  // results, the chunk's state (its large and its small terms side by side).
+  // Else two of scores, two of results (inter, weighted in place, then intra
+  // added), the chunk's state.
   static constexpr uint32_t kColSc = 0, kScStep = kMerged ? 128 : 64;
-  static constexpr uint32_t kColInter = kMerged ? 64 : 128, kInterStep = kMerged ? 128 : 0;
-  static constexpr uint32_t kColIntra = 256, kIntraStep = kMerged ? 64 : 0;
+  static constexpr uint32_t kColInter = kMerged ? 64 : 128, kInterStep = 128;
+  static constexpr uint32_t kColIntra = kMerged ? 256 : 128, kIntraStep = kMerged ? 64 : 128;
   static constexpr uint32_t kColDs = 384;
 };
 
@@ -125,8 +126,45 @@ __device__ __forceinline__ void tmem_ld_16x64(uint32_t taddr, float (&v)[32]) {
 #pragma unroll
   for (int i = 0; i < 32; ++i) v[i] = __uint_as_float(r[i]);
 }
-__device__ __forceinline__ void sts_u32(uint32_t a, uint32_t v) {
-  asm volatile("st.shared.u32 [%0], %1;" ::"r"(a), "r"(v) : "memory");
+__device__ __forceinline__ void tmem_st_16x64(uint32_t taddr, const float (&v)[32]) {
+  uint32_t r[32];
+#pragma unroll
+  for (int i = 0; i < 32; ++i) r[i] = __float_as_uint(v[i]);
+  asm volatile(
+      "tcgen05.st.sync.aligned.16x256b.x8.b32 [%0], "
+      "{%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,"
+      "%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31,%32};" ::"r"(taddr),
+      "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]),
+      "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]),
+      "r"(r[15]), "r"(r[16]), "r"(r[17]), "r"(r[18]), "r"(r[19]), "r"(r[20]), "r"(r[21]),
+      "r"(r[22]), "r"(r[23]), "r"(r[24]), "r"(r[25]), "r"(r[26]), "r"(r[27]), "r"(r[28]),
+      "r"(r[29]), "r"(r[30]), "r"(r[31])
+      : "memory");
+  asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
+}
+// The warp's 16 x 64 values in the layout above, as bf16 into 16 rows of 128
+// bytes (128-byte swizzle; the first row a multiple of 8 of the tile).
+__device__ __forceinline__ void store_16x64(uint32_t rows, int lane, const float (&v)[32]) {
+  const uint32_t row = rows + (lane & 15) * 128;  // lane l: row l % 16, piece k + l / 16
+#pragma unroll
+  for (int k = 0; k < 8; k += 2) {
+    const uint32_t at = row + (((k + (lane >> 4)) ^ (lane & 7)) << 4);
+    asm volatile("stmatrix.sync.aligned.m8n8.x4.shared.b16 [%0], {%1,%2,%3,%4};" ::"r"(at),
+                 "r"(f2_to_bf2(v[4 * k], v[4 * k + 1])), "r"(f2_to_bf2(v[4 * k + 2], v[4 * k + 3])),
+                 "r"(f2_to_bf2(v[4 * k + 4], v[4 * k + 5])),
+                 "r"(f2_to_bf2(v[4 * k + 6], v[4 * k + 7]))
+                 : "memory");
+  }
+}
+__device__ __forceinline__ uint32_t bf2_mul(uint32_t a, uint32_t b) {
+  uint32_t r;
+  asm("mul.rn.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+  return r;
+}
+__device__ __forceinline__ uint32_t bf2_fma(uint32_t a, uint32_t b, uint32_t c) {
+  uint32_t r;
+  asm("fma.rn.bf16x2 %0, %1, %2, %3;" : "=r"(r) : "r"(a), "r"(b), "r"(c));
+  return r;
 }
 // Shared-memory matrix descriptor (128-byte swizzle) of a tile, and the same
 // moved by a constant number of bytes: the address field's carry never leaves
@@ -181,13 +219,14 @@ __global__ void __launch_bounds__(Shape<D, kTerms>::kThreads, 1)
   extern __shared__ uint8_t smem_raw[];
   uint8_t *smem = (uint8_t *)(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);
   uint64_t *bar = (uint64_t *)(smem + Sh::kOffBar);
-  uint64_t *fx = bar, *ex = fx + Sh::kNX, *fy = ex + Sh::kNX, *ey = fy + Sh::kNY,
-           *fz = ey + Sh::kNY, *ez = fz + Sh::kNZ, *conv_full = ez + Sh::kNZ,
-           *conv_empty = conv_full + Sh::kConv, *p_full = conv_empty + Sh::kConv,
-           *p_empty = p_full + Sh::kP, *o_full = p_empty + Sh::kP, *o_empty = o_full + Sh::kO,
-           *s_full = o_empty + Sh::kO, *s_empty = s_full + 2, *ds_full = s_empty + 1,
-           *ds_empty = ds_full + 1, *sc_full = ds_empty + 1, *sc_empty = sc_full + 2,
-           *drained = sc_empty + 2;
+  // *_ready: everything that its MMAs wait for, on one barrier (a wait costs the
+  // issuing thread more than an MMA)
+  uint64_t *fy = bar, *ey = fy + Sh::kNY, *fz = ey + Sh::kNY, *ez = fz + Sh::kNZ,
+           *state_ready = ez + Sh::kNZ, *conv_empty = state_ready + Sh::kConv,
+           *intra_ready = conv_empty + Sh::kConv, *p_empty = intra_ready + Sh::kP,
+           *score_ready = p_empty + Sh::kP, *ex = score_ready + 2, *sc_full = ex + 2,
+           *inter_ready = sc_full + 2, *inter_full = inter_ready + 2, *o_full = inter_full + 2,
+           *s_empty = o_full + 2, *ds_full = s_empty + 1, *drained = ds_full + 1;
   uint32_t *tmem_slot = (uint32_t *)(smem + Sh::kOffMisc);
   const AbortFlag ab{smem_u32(smem + Sh::kOffMisc + 4)};
 
@@ -222,20 +261,23 @@ __global__ void __launch_bounds__(Shape<D, kTerms>::kThreads, 1)
 
   if (tid == 0) {
     *(volatile int *)(smem + Sh::kOffMisc + 4) = 0;
-    for (int i = 0; i < Sh::kNX; ++i) mbar_init(&fx[i], Sh::kB), mbar_init(&ex[i], 1);
     for (int i = 0; i < Sh::kNY; ++i) mbar_init(&fy[i], Sh::kB), mbar_init(&ey[i], 1);
     for (int i = 0; i < Sh::kNZ; ++i) mbar_init(&fz[i], Sh::kB), mbar_init(&ez[i], 1);
-    for (int i = 0; i < Sh::kConv; ++i) mbar_init(&conv_full[i], 4), mbar_init(&conv_empty[i], 1);
-    for (int i = 0; i < Sh::kP; ++i) mbar_init(&p_full[i], 4), mbar_init(&p_empty[i], 1);
-    for (int i = 0; i < Sh::kO; ++i) mbar_init(&o_full[i], 1), mbar_init(&o_empty[i], 4);
+    for (int i = 0; i < Sh::kConv; ++i)  // weighted keys there, last step's state taken
+      mbar_init(&state_ready[i], 4 + Sh::kSWarps), mbar_init(&conv_empty[i], 1);
+    for (int i = 0; i < Sh::kP; ++i)  // scores weighted (D = 128: and inter results)
+      mbar_init(&intra_ready[i], Sh::kMerged ? 4 : 8), mbar_init(&p_empty[i], 1);
     for (int i = 0; i < 2; ++i) {
-      mbar_init(&s_full[i], Sh::kSWarps);
+      // x there, scores' columns free (D = 64: and results' columns, state there)
+      mbar_init(&score_ready[i], Sh::kB + (Sh::kMerged ? 12 : 4));
+      mbar_init(&inter_ready[i], 4 + Sh::kSWarps);  // D = 128: results' columns free, state there
+      mbar_init(&ex[i], 1);
       mbar_init(&sc_full[i], 1);
-      mbar_init(&sc_empty[i], 4);
+      mbar_init(&inter_full[i], 1);
+      mbar_init(&o_full[i], 1);
     }
     mbar_init(s_empty, 1);
     mbar_init(ds_full, 1);
-    mbar_init(ds_empty, Sh::kSWarps);
     mbar_init(drained, 1);
     fence_mbar_init();
   }
@@ -263,8 +305,8 @@ __global__ void __launch_bounds__(Shape<D, kTerms>::kThreads, 1)
       const int t = lane / Sh::kB, blk = lane % Sh::kB;  // tensor, 64-channel block
       const CUtensorMap *tm = t == 0 ? &tm_x : t == 1 ? &tm_y : &tm_z;
       const int hd = h / (t == 0 ? p.gx : t == 1 ? p.gy : p.gz);
-      uint64_t *f = t == 0 ? fx : t == 1 ? fy : fz, *e = t == 0 ? ex : t == 1 ? ey : ez;
-      const int slots = t == 0 ? Sh::kNX : t == 1 ? Sh::kNY : Sh::kNZ;
+      uint64_t *f = t == 0 ? score_ready : t == 1 ? fy : fz, *e = t == 0 ? ex : t == 1 ? ey : ez;
+      const int slots = t == 0 ? 2 : t == 1 ? Sh::kNY : Sh::kNZ;
       uint8_t *to = smem + (t == 0 ? Sh::kOffX : t == 1 ? Sh::kOffY : Sh::kOffZ) + blk * kBlk;
       const int size = t == 1 ? Sh::kYSlot : Sh::kTile;
       const int first = t == 0 ? pre : 0, steps = pre + cnt - first;  // x: the scan alone
@@ -296,9 +338,7 @@ __global__ void __launch_bounds__(Shape<D, kTerms>::kThreads, 1)
       // segment's own state, after which the tiles are free
       auto state_mma = [&](int g, bool own) {
         const int cb = g % Sh::kConv, sz = g % Sh::kNZ;
-        if (!wait(&fz[sz], (g / Sh::kNZ) & 1)) return;
-        if (!wait(&conv_full[cb], (g / Sh::kConv) & 1)) return;
-        if (g >= 1 && !wait(ds_empty, (g & 1) ^ 1)) return;
+        if (!wait(&state_ready[cb], (g / Sh::kConv) & 1)) return;
         tc_fence_after();
         const uint64_t zd = sw128_desc(base + Sh::kOffZ + sz * Sh::kTile, kBlk, 1024);
         const uint64_t cd =
@@ -334,13 +374,8 @@ __global__ void __launch_bounds__(Shape<D, kTerms>::kThreads, 1)
       // scores of the scan's chunk i; merged: and x_r^T S.  The chunk's state
       // went before, so its keys are there and those past the end are zero.
       auto score_mma = [&](int i) {
-        const int sx = i % Sh::kNX, sy = (pre + i) % Sh::kNY;
-        if (!wait(&fx[sx], (i / Sh::kNX) & 1)) return;
-        if (i >= 2 && !wait(&sc_empty[i & 1], ((i >> 1) & 1) ^ 1)) return;
-        if constexpr (Sh::kMerged) {
-          if (i >= 2 && !wait(&o_empty[i & 1], ((i >> 1) & 1) ^ 1)) return;
-          if (!wait(&s_full[i & 1], (i >> 1) & 1)) return;
-        }
+        const int sx = i & 1, sy = (pre + i) % Sh::kNY;
+        if (!wait(&score_ready[sx], (i >> 1) & 1)) return;
         tc_fence_after();
         constexpr uint32_t id = idesc_bf16_f32(64, Sh::kMerged ? 128 : 64, 0, 0);
         const uint64_t xd = sw128_desc(base + Sh::kOffX + sx * Sh::kTile, 16, 1024);
@@ -356,23 +391,23 @@ __global__ void __launch_bounds__(Shape<D, kTerms>::kThreads, 1)
         if constexpr (Sh::kMerged) mma_commit(&ex[sx]);
       };
       auto inter_mma = [&](int i) {  // x_r^T S on its own
-        const int sx = i % Sh::kNX;
-        if (i >= 1 && !wait(&o_empty[0], (i & 1) ^ 1)) return;
-        if (!wait(&s_full[i & 1], (i >> 1) & 1)) return;
+        const int sx = i & 1;
+        if (!wait(&inter_ready[sx], (i >> 1) & 1)) return;
         tc_fence_after();
         constexpr uint32_t id = idesc_bf16_f32(64, D, 0, 1);
         const uint64_t xd = sw128_desc(base + Sh::kOffX + sx * Sh::kTile, 16, 1024);
         const uint64_t sd = sw128_desc(base + Sh::kOffS, D * 128, 1024);
 #pragma unroll
         for (int k = 0; k < D / 16; ++k)
-          mma_bf16(tmem + Sh::kColInter, desc_at(xd, (k >> 2) * kBlk + (k & 3) * 32),
+          mma_bf16(tmem + Sh::kColInter + Sh::kInterStep * sx, desc_at(xd, (k >> 2) * kBlk + (k & 3) * 32),
                    desc_at(sd, k * 2048), id, k != 0);
+        mma_commit(&inter_full[sx]);
         mma_commit(s_empty);
         mma_commit(&ex[sx]);
       };
       auto intra_mma = [&](int j) {  // sum_j (w_rj A_rj) z_j
-        const int g = pre + j, sz = g % Sh::kNZ, pb = j % Sh::kP, ob = j % Sh::kO;
-        if (!wait(&p_full[pb], (j / Sh::kP) & 1)) return;
+        const int g = pre + j, sz = g % Sh::kNZ, pb = j % Sh::kP, ob = j & 1;
+        if (!wait(&intra_ready[pb], (j / Sh::kP) & 1)) return;
         tc_fence_after();
         constexpr uint32_t id = idesc_bf16_f32(64, D, 0, 1);
         const uint64_t pd = sw128_desc(base + Sh::kOffP + pb * kBlk, 16, 1024);
@@ -380,7 +415,7 @@ __global__ void __launch_bounds__(Shape<D, kTerms>::kThreads, 1)
 #pragma unroll
         for (int k = 0; k < 4; ++k)
           mma_bf16(tmem + Sh::kColIntra + Sh::kIntraStep * ob, desc_at(pd, k * 32),
-                   desc_at(zd, k * 2048), id, k != 0);
+                   desc_at(zd, k * 2048), id, !Sh::kMerged || k != 0);
         mma_commit(&p_empty[pb]);
         mma_commit(&o_full[ob]);
         mma_commit(&ez[sz]);
@@ -392,10 +427,10 @@ __global__ void __launch_bounds__(Shape<D, kTerms>::kThreads, 1)
       // the state to reach the scores of i + 1).
       for (int i = 0; i <= cnt && ok; ++i) {
         if (i < cnt) score_mma(i);
-        if (i >= 1 && ok) intra_mma(i - 1);
-        if (i + 1 < cnt && ok) state_mma(pre + i + 1, false);
         if constexpr (!Sh::kMerged)
           if (i < cnt && ok) inter_mma(i);
+        if (i >= 1 && ok) intra_mma(i - 1);
+        if (i + 1 < cnt && ok) state_mma(pre + i + 1, false);
       }
       mma_commit(drained);  // nothing is in flight when TMEM is freed
       if (!mbar_wait(drained, 0, nullptr)) decay_error(512, ab);
@@ -404,14 +439,18 @@ __global__ void __launch_bounds__(Shape<D, kTerms>::kThreads, 1)
   } else if (warp < 4) {
     // ------------------------------------------- weighted scores (warps 0-3)
     const int r0 = 16 * warp + (lane >> 2), c = 2 * (lane & 3);
-    float w[9][2];  // exponent e0 -+ 8 k, one less (more) for the second column
+    float2 w[9];  // exponent e0 -+ 8 k, one less (more) for the second column
 #pragma unroll
-    for (int k = 0; k < 9; ++k)
+    for (int k = 0; k < 9; ++k) {
+      float e[2];
 #pragma unroll
-      for (int e = 0; e < 2; ++e) {
-        const int n = (p.reverse ? -1 : 1) * (r0 - c - e - 8 * (k - 1));
-        w[k][e] = n >= 0 ? decay_pow(l2, (float)n) : 0.f;
+      for (int q = 0; q < 2; ++q) {
+        const int n = (p.reverse ? -1 : 1) * (r0 - c - q - 8 * (k - 1));
+        e[q] = n >= 0 ? p.scale * decay_pow(l2, (float)n) : 0.f;
       }
+      w[k] = make_float2(e[0], e[1]);
+    }
+    if (lane == 0) mbar_arrive(&score_ready[0]), mbar_arrive(&score_ready[1]);
     for (int i = 0; i < cnt; ++i) {
       const int pb = i % Sh::kP;
       if (!mbar_wait(&sc_full[i & 1], (i >> 1) & 1, &ab)) decay_error(4, ab);
@@ -421,27 +460,32 @@ __global__ void __launch_bounds__(Shape<D, kTerms>::kThreads, 1)
       tmem_ld_wait_regs(a);
       tc_fence_before();
       __syncwarp();
-      if (lane == 0) mbar_arrive(&sc_empty[i & 1]);
+      if (lane == 0) mbar_arrive(&score_ready[i & 1]);
       if (i >= Sh::kP && !mbar_wait(&p_empty[pb], ((i / Sh::kP) & 1) ^ 1, &ab)) decay_error(8, ab);
-      const uint32_t ps = smem_u32(smem + Sh::kOffP + pb * kBlk) + r0 * 128 + c * 2;
 #pragma unroll
-      for (int k = 0; k < 8; ++k) {
-        const uint32_t at = ps + ((k ^ (r0 & 7)) << 4);  // row r0 + 8 has the same swizzle
-        sts_u32(at, f2_to_bf2(a[4 * k] * w[k + 1][0], a[4 * k + 1] * w[k + 1][1]));
-        sts_u32(at + 8 * 128, f2_to_bf2(a[4 * k + 2] * w[k][0], a[4 * k + 3] * w[k][1]));
-      }
+      for (int k = 0; k < 8; ++k)
+#pragma unroll
+        for (int q = 0; q < 2; ++q) {
+          const float2 m = __fmul2_rn(make_float2(a[4 * k + 2 * q], a[4 * k + 2 * q + 1]), w[k + 1 - q]);
+          a[4 * k + 2 * q] = m.x, a[4 * k + 2 * q + 1] = m.y;
+        }
+      store_16x64(smem_u32(smem + Sh::kOffP + pb * kBlk) + 16 * warp * 128, lane, a);
       fence_proxy_async_smem();
       __syncwarp();
-      if (lane == 0) mbar_arrive(&p_full[pb]);
+      if (lane == 0) mbar_arrive(&intra_ready[pb]);
     }
   } else if (warp < 8) {
     // --------------------------------------------- weighted keys (warps 4-7)
     const int ct = tid - 128, ch = ct & 7, rr = ct >> 3;  // 16-byte chunk, first row
     float wr[4];
+    uint32_t wh[4], wl[4];  // two terms: the weight as a sum of two bf16 numbers
 #pragma unroll
     for (int k = 0; k < 4; ++k) {
       const int r = rr + 16 * k;
       wr[k] = decay_pow(l2, (float)(p.reverse ? r : kC - 1 - r));
+      wh[k] = f2_to_bf2(wr[k], wr[k]);
+      const float rest = wr[k] - bf2_to_f2(wh[k]).x;
+      wl[k] = f2_to_bf2(rest, rest);
     }
     // one 16-byte piece: kTerms bf16 numbers for each of its 8 products
     auto split = [&](const uint4 &u, float w, uint32_t to) {
@@ -465,9 +509,10 @@ __global__ void __launch_bounds__(Shape<D, kTerms>::kThreads, 1)
         sts_v4(to + t * Sh::kTile, make_uint4(o[t][0], o[t][1], o[t][2], o[t][3]));
     };
     for (int g = 0; g < pre + cnt; ++g) {
-      const int sy = g % Sh::kNY, cb = g % Sh::kConv;
+      const int sy = g % Sh::kNY, sz = g % Sh::kNZ, cb = g % Sh::kConv;
       const int n = min(kC, L - token_of(place_of(g)));
       if (!mbar_wait(&fy[sy], (g / Sh::kNY) & 1, &ab)) decay_error(16, ab);
+      if (!mbar_wait(&fz[sz], (g / Sh::kNZ) & 1, &ab)) decay_error(16, ab);  // for the MMAs
       if (g >= Sh::kConv && !mbar_wait(&conv_empty[cb], ((g / Sh::kConv) & 1) ^ 1, &ab))
         decay_error(32, ab);
       const uint32_t ys = smem_u32(smem + Sh::kOffY + sy * Sh::kYSlot) + rr * 128 + ((ch ^ (rr & 7)) << 4);
@@ -480,13 +525,28 @@ __global__ void __launch_bounds__(Shape<D, kTerms>::kThreads, 1)
 #pragma unroll
           for (int k = 0; k < 4; ++k) u[k] = lds_v4(ys + blk * kBlk + k * 2048);
 #pragma unroll
-          for (int k = 0; k < 4; ++k) split(u[k], wr[k], cs + blk * kBlk + k * 2048);
+          for (int k = 0; k < 4; ++k) {
+            if constexpr (kTerms == 3) {
+              split(u[k], wr[k], cs + blk * kBlk + k * 2048);
+            } else {
+              // y w in packed bf16: hi = rn(y wh), y wh - hi is exact, and
+              // lo = rn(y wl + that)
+              const uint32_t in[4] = {u[k].x, u[k].y, u[k].z, u[k].w};
+              uint32_t hi[4], lo[4];
+#pragma unroll
+              for (int e = 0; e < 4; ++e) {
+                hi[e] = bf2_mul(in[e], wh[k]);
+                lo[e] = bf2_fma(in[e], wl[k], bf2_fma(in[e], wh[k], hi[e] ^ 0x80008000u));
+              }
+              const uint32_t to = cs + blk * kBlk + k * 2048;
+              sts_v4(to, make_uint4(hi[0], hi[1], hi[2], hi[3]));
+              sts_v4(to + Sh::kTile, make_uint4(lo[0], lo[1], lo[2], lo[3]));
+            }
+          }
         }
       } else {
         // the chunk with the sequence's end: padding may hold NaN, so keys, values
         // and weighted keys past the end become 0
-        const int sz = g % Sh::kNZ;
-        if (!mbar_wait(&fz[sz], (g / Sh::kNZ) & 1, &ab)) decay_error(16, ab);
         const uint32_t zs = smem_u32(smem + Sh::kOffZ + sz * Sh::kTile) + rr * 128 + ((ch ^ (rr & 7)) << 4);
         const uint4 zero = make_uint4(0, 0, 0, 0);
 #pragma unroll 1
@@ -504,7 +564,7 @@ __global__ void __launch_bounds__(Shape<D, kTerms>::kThreads, 1)
       }
       fence_proxy_async_smem();
       __syncwarp();
-      if (lane == 0) mbar_arrive(&conv_full[cb]);
+      if (lane == 0) mbar_arrive(&state_ready[cb]);
     }
   } else if (state_warp) {
     // ------------------------------------------------- the state, in registers
@@ -514,38 +574,51 @@ __global__ void __launch_bounds__(Shape<D, kTerms>::kThreads, 1)
     for (int i = 0; i < kNV; ++i) S[i] = 0.f;
     const uint32_t src = tmem + ((uint32_t)(32 * (sw & 3)) << 16) + Sh::kColDs +
                          (D == 64 ? 0 : 64 * (sw >> 2));
-    // S = a S + f (the state of step g's chunk)
-    auto take = [&](int g, float a, float f) {
+    if (lane == 0) mbar_arrive(&state_ready[0]);
+    // own: S = S + f (the state of step g's chunk); else S = f S + it
+    auto take = [&](int g, float f, auto own) {
+      const float2 f2 = make_float2(f, f);
+      auto add = [&](int i, float2 v) {
+        const float2 q = make_float2(S[i], S[i + 1]);
+        const float2 r = own ? __ffma2_rn(f2, v, q) : __ffma2_rn(f2, q, v);
+        S[i] = r.x, S[i + 1] = r.y;
+      };
       if (!mbar_wait(ds_full, g & 1, &ab)) decay_error(64, ab);
       tc_fence_after();
       if constexpr (D == 64) {
+        float v[32];
+        tmem_ld_16x64(src + 64, v);  // the small terms first
+        tmem_ld_wait_regs(v);
 #pragma unroll
-        for (int i = 0; i < 32; ++i) S[i] *= a;
+        for (int i = 0; i < 32; i += 2) add(i, make_float2(v[i], v[i + 1]));
+        tmem_ld_16x64(src, v);
+        tmem_ld_wait_regs(v);
 #pragma unroll
-        for (int t = 0; t < 2; ++t) {  // the small terms first
-          float v[32];
-          tmem_ld_16x64(src + 64 * (1 - t), v);
-          tmem_ld_wait_regs(v);
-#pragma unroll
-          for (int i = 0; i < 32; ++i) S[i] = fmaf(f, v[i], S[i]);
+        for (int i = 0; i < 32; i += 2) {
+          if (own) {
+            add(i, make_float2(v[i], v[i + 1]));
+          } else {
+            const float2 r = __fadd2_rn(make_float2(S[i], S[i + 1]), make_float2(v[i], v[i + 1]));
+            S[i] = r.x, S[i + 1] = r.y;
+          }
         }
       } else {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
+        for (int k = 0; k < 4; ++k) {
           float v[16];
-          tmem_ld16(src + 16 * i, v);
+          tmem_ld16(src + 16 * k, v);
           tmem_ld_wait_regs(v);
 #pragma unroll
-          for (int e = 0; e < 16; ++e) S[16 * i + e] = fmaf(f, v[e], a * S[16 * i + e]);
+          for (int e = 0; e < 16; e += 2) add(16 * k + e, make_float2(v[e], v[e + 1]));
         }
       }
       tc_fence_before();
       __syncwarp();
-      if (lane == 0) mbar_arrive(ds_empty);
+      if (lane == 0) mbar_arrive(&state_ready[(g + 1) % Sh::kConv]);
     };
     if (ranks > 1) {
       // the segment's own state: chunks from its end in scan order to its start
-      for (int g = 0; g < pre; ++g) take(g, 1.f, decay_pow(l2, (float)g * kC));
+      for (int g = 0; g < pre; ++g) take(g, decay_pow(l2, (float)g * kC), std::true_type{});
       constexpr int kThr = Sh::kSWarps * 32;
       const int st = tid - 8 * 32;
       float *part = p.part + bh * ranks * D * D;
@@ -582,15 +655,7 @@ __global__ void __launch_bounds__(Shape<D, kTerms>::kThreads, 1)
       if constexpr (D == 64) {  // behind the chunk's keys, once their slot is free
         const int g = pre + j, sy = g % Sh::kNY;
         if (!mbar_wait(&ey[sy], ((g / Sh::kNY) & 1) ^ 1, &ab)) decay_error(128, ab);
-        const int e = 16 * sw + (lane >> 2);
-        const uint32_t row = smem_u32(smem + Sh::kOffY + sy * Sh::kYSlot + Sh::kTile) + e * 128 +
-                             (lane & 3) * 4;
-#pragma unroll
-        for (int k = 0; k < 8; ++k) {
-          const uint32_t at = row + ((k ^ (e & 7)) << 4);
-          sts_u32(at, f2_to_bf2(S[4 * k], S[4 * k + 1]));
-          sts_u32(at + 8 * 128, f2_to_bf2(S[4 * k + 2], S[4 * k + 3]));
-        }
+        store_16x64(smem_u32(smem + Sh::kOffY + sy * Sh::kYSlot + Sh::kTile) + 16 * sw * 128, lane, S);
       } else {
         if (j >= 1 && !mbar_wait(s_empty, (j & 1) ^ 1, &ab)) decay_error(128, ab);
         const int d = 32 * (sw & 3) + lane;
@@ -604,10 +669,10 @@ __global__ void __launch_bounds__(Shape<D, kTerms>::kThreads, 1)
       }
       fence_proxy_async_smem();
       __syncwarp();
-      if (lane == 0) mbar_arrive(&s_full[j & 1]);
+      if (lane == 0) mbar_arrive(Sh::kMerged ? &score_ready[j & 1] : &inter_ready[j & 1]);
       const int t0 = token_of(q0 + j), n = min(kC, L - t0);
       const int span = !p.reverse ? n : (q0 + j == 0 ? n - 1 : kC);
-      take(pre + j, decay_pow(l2, (float)span), 1.f);
+      take(pre + j, decay_pow(l2, (float)span), std::false_type{});
     }
     if (p.fin && is_last) {
       const float f = p.fin_scale * (p.reverse ? decay_pow(l2, 1.f) : 1.f);
@@ -622,66 +687,83 @@ __global__ void __launch_bounds__(Shape<D, kTerms>::kThreads, 1)
     // ---------------------------------------------------------------- results
     const int ow = warp - Sh::kOutWarp, r0 = 16 * ow + (lane >> 2);
     const uint32_t quarter = tmem + ((uint32_t)(32 * ow) << 16);
-    float u[2];
+    const uint32_t stage = smem_u32(smem + Sh::kOffOut + ow * 2048);
+    uint64_t *free_cols = Sh::kMerged ? score_ready : inter_ready;
+    if (lane == 0) mbar_arrive(&free_cols[0]), mbar_arrive(&free_cols[1]);
+    float u[2];  // weights of x_r^T S in the rows r0 and r0 + 8
 #pragma unroll
     for (int k = 0; k < 2; ++k)
       u[k] = p.scale * decay_pow(l2, (float)(p.reverse ? kC - (r0 + 8 * k) : r0 + 8 * k + 1));
     for (int j = 0; j < cnt; ++j) {
-      const int ob = j % Sh::kO, t0 = token_of(q0 + j), n = min(kC, L - t0);
+      const int ob = j & 1, t0 = token_of(q0 + j), n = min(kC, L - t0);
       float ur[2] = {u[0], u[1]};
       if (p.reverse && q0 + j == 0) {
 #pragma unroll
         for (int k = 0; k < 2; ++k)
           ur[k] = p.scale * decay_pow(l2, (float)max(n - 1 - (r0 + 8 * k), 0));
       }
-      if (!mbar_wait(&o_full[ob], (j / Sh::kO) & 1, &ab)) decay_error(256, ab);
+      if constexpr (!Sh::kMerged) {  // weight the inter results in place; intra is added to them
+        if (!mbar_wait(&inter_full[ob], (j >> 1) & 1, &ab)) decay_error(256, ab);
+        tc_fence_after();
+#pragma unroll
+        for (int blk = 0; blk < Sh::kB; ++blk) {
+          const uint32_t at = quarter + Sh::kColInter + Sh::kInterStep * ob + blk * 64;
+          float s[32];
+          tmem_ld_16x64(at, s);
+          tmem_ld_wait_regs(s);
+#pragma unroll
+          for (int i = 0; i < 32; ++i) s[i] *= ur[(i >> 1) & 1];
+          tmem_st_16x64(at, s);
+        }
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&intra_ready[j % Sh::kP]);
+      }
+      if (!mbar_wait(&o_full[ob], (j >> 1) & 1, &ab)) decay_error(256, ab);
       tc_fence_after();
 #pragma unroll
       for (int blk = 0; blk < Sh::kB; ++blk) {
-        float a[32], s[32];
+        float a[32];
         tmem_ld_16x64(quarter + Sh::kColIntra + Sh::kIntraStep * ob + blk * 64, a);
-        tmem_ld_16x64(quarter + Sh::kColInter + Sh::kInterStep * ob + blk * 64, s);
-        tmem_ld_wait_regs(a);
-        tmem_pin(s);
+        if constexpr (Sh::kMerged) {
+          float s[32];
+          tmem_ld_16x64(quarter + Sh::kColInter + Sh::kInterStep * ob, s);
+          tmem_ld_wait_regs(a);
+          tmem_pin(s);
+#pragma unroll
+          for (int i = 0; i < 32; i += 2) {
+            const float w = ur[(i >> 1) & 1];
+            const float2 r = __ffma2_rn(make_float2(w, w), make_float2(s[i], s[i + 1]),
+                                        make_float2(a[i], a[i + 1]));
+            a[i] = r.x, a[i + 1] = r.y;
+          }
+        } else {
+          tmem_ld_wait_regs(a);
+        }
         if (blk == Sh::kB - 1) {
           tc_fence_before();
           __syncwarp();
-          if (lane == 0) mbar_arrive(&o_empty[ob]);
+          if (lane == 0) mbar_arrive(&free_cols[ob]);
         }
-#pragma unroll
-        for (int i = 0; i < 32; ++i) a[i] = fmaf(ur[(i >> 1) & 1], s[i], a[i] * p.scale);
+        O *dst = out + (size_t)t0 * orow + blk * 64;
         if constexpr (sizeof(O) == 4) {
 #pragma unroll
           for (int k = 0; k < 8; ++k)
 #pragma unroll
             for (int q = 0; q < 2; ++q)
               if (r0 + 8 * q < n)
-                *(float2 *)(out + (size_t)(t0 + r0 + 8 * q) * orow + blk * 64 + 8 * k +
-                            2 * (lane & 3)) = make_float2(a[4 * k + 2 * q], a[4 * k + 2 * q + 1]);
-        } else {
-          // four lanes hold the four words of a 16-byte piece: each lane gathers
-          // the whole pieces lane % 4 and lane % 4 + 4 of both rows
-          const int l4 = lane & 3;
+                *(float2 *)(dst + (size_t)(r0 + 8 * q) * orow + 8 * k + 2 * (lane & 3)) =
+                    make_float2(a[4 * k + 2 * q], a[4 * k + 2 * q + 1]);
+        } else {  // whole 128-byte rows through the warp's staging
+          __syncwarp();
+          store_16x64(stage, lane, a);
+          __syncwarp();
 #pragma unroll
-          for (int q = 0; q < 2; ++q)
-#pragma unroll
-            for (int hf = 0; hf < 2; ++hf) {
-              uint32_t m[4], t[4];
-#pragma unroll
-              for (int k = 0; k < 4; ++k)
-                m[k] = f2_to_bf2(a[16 * hf + 4 * k + 2 * q], a[16 * hf + 4 * k + 2 * q + 1]);
-              // 4 x 4 transpose over the lanes: exchange with lane ^ 1, then lane ^ 2
-              const bool b0 = l4 & 1, b1 = l4 & 2;
-              const uint32_t x0 = __shfl_xor_sync(0xffffffffu, b0 ? m[0] : m[1], 1);
-              const uint32_t x1 = __shfl_xor_sync(0xffffffffu, b0 ? m[2] : m[3], 1);
-              t[0] = b0 ? x0 : m[0], t[1] = b0 ? m[1] : x0;
-              t[2] = b0 ? x1 : m[2], t[3] = b0 ? m[3] : x1;
-              const uint32_t y0 = __shfl_xor_sync(0xffffffffu, b1 ? t[0] : t[2], 2);
-              const uint32_t y1 = __shfl_xor_sync(0xffffffffu, b1 ? t[1] : t[3], 2);
-              const uint4 v = b1 ? make_uint4(y0, y1, t[2], t[3]) : make_uint4(t[0], t[1], y0, y1);
-              if (r0 + 8 * q < n)
-                *(uint4 *)(out + (size_t)(t0 + r0 + 8 * q) * orow + blk * 64 + 8 * (4 * hf + l4)) = v;
-            }
+          for (int k = 0; k < 4; ++k) {
+            const int r = (lane >> 3) + 4 * k;
+            const uint4 v = lds_v4(stage + r * 128 + (((lane & 7) ^ (r & 7)) << 4));
+            if (16 * ow + r < n) *(uint4 *)(dst + (size_t)(16 * ow + r) * orow + 8 * (lane & 7)) = v;
+          }
         }
       }
     }

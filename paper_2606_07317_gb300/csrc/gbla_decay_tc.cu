@@ -21,15 +21,14 @@
 // sum of bf16 numbers, two (2^-17 of a term) where the state only serves the
 // results, three (2^-25) where it is a result itself.  The decay powers are fp32.
 //
-// One CTA serves a run of chunks (a segment) of one (batch, head); a cluster of
-// 1, 2, 4 or 8 CTAs serves the whole sequence.  Every CTA but the last in scan
-// order first sums its own segment's state (y and z alone, the chunk it will need
-// last read first, so that what it reads again soonest is still in L2), the
-// cluster meets once, and each CTA starts its scan from the weighted sum of the
-// segments before it.  That costs y and z a second read and saves any launch
-// besides this one.
+// One CTA scans a run of chunks (a segment) of one (batch, head).  A sequence is
+// cut into several where whole ones would leave SMs idle or one long sequence
+// would outlast the rest; a first kernel then sums the state of every segment but
+// the last in scan order (y and z alone, the chunk that the scan starts with read
+// last, so that it is still in L2), and the scan starts from the weighted sum of
+// the segments before its own.  The second launch begins while the first ends.
 //
-// Warps: 0-3 weight the scores, 4-7 form v_j y_j, the next 4 (D = 128: 8) hold
+// Warps of the scan: 0-3 weight the scores, 4-7 form v_j y_j, the next 4 (D = 128: 8) hold
 // the state, the next 4 write results, then one warp issues the TMA loads (a
 // lane for each 64-channel block of each tensor: one thread issues a box in half
 // a microsecond) and one the MMAs.  M = 64 accumulators lie in lanes 0-15 of each
@@ -38,7 +37,6 @@
 // Every mbarrier wait is bounded (2 s); one that runs out sets a bit in
 // g_decay_error and raises the CTA's abort flag.
 #include <mutex>
-#include <type_traits>
 
 #include "gbla_internal.cuh"
 #include "gbla_sm100.cuh"
@@ -53,7 +51,6 @@ using namespace sm100;
 
 constexpr int kC = 64;                 // tokens per chunk
 constexpr int kBlk = kC * 128;         // 8 KB: 64 tokens x 64 channels, 128B swizzle
-constexpr int kMaxCluster = 8;
 
 template <int D, int kTerms>
 struct Shape {
@@ -98,6 +95,7 @@ struct TcParams {
   float *fin, *part;
   float init_scale, fin_scale, scale;
   int N, H, gx, gy, gz;
+  int seg, ranks;  // chunks of a segment, most segments of a sequence
   bool zero_pad, init_t, reverse;
 };
 
@@ -180,21 +178,94 @@ __device__ __forceinline__ bool elect_one() {
       : "=r"(r));
   return r != 0;
 }
-__device__ __forceinline__ uint32_t cluster_rank() {
-  uint32_t r;
-  asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
-  return r;
+
+// A row's weight: for two terms as a sum of two bf16 numbers, doubled up.
+struct RowWeight {
+  float f;
+  uint32_t hi, lo;
+  __device__ __forceinline__ void set(float w) {
+    f = w;
+    hi = f2_to_bf2(w, w);
+    const float rest = w - bf2_to_f2(hi).x;
+    lo = f2_to_bf2(rest, rest);
+  }
+};
+// 8 values of y times a row's weight as sums of kTerms bf16 numbers, one in each
+// tile from `to` on.  Two terms stay in packed bf16: h = rn(y hi), y hi - h is
+// exact, l = rn(y lo + that).
+template <int kTerms, int kTile>
+__device__ __forceinline__ void weigh_piece(const uint4 &u, const RowWeight &w, uint32_t to) {
+  const uint32_t in[4] = {u.x, u.y, u.z, u.w};
+  uint32_t o[kTerms][4];
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    if constexpr (kTerms == 2) {
+      o[0][e] = bf2_mul(in[e], w.hi);
+      o[1][e] = bf2_fma(in[e], w.lo, bf2_fma(in[e], w.hi, o[0][e] ^ 0x80008000u));
+    } else {
+      float2 f = bf2_to_f2(in[e]);
+      f.x *= w.f, f.y *= w.f;
+#pragma unroll
+      for (int t = 0; t < kTerms; ++t) {
+        o[t][e] = f2_to_bf2(f.x, f.y);
+        if (t + 1 < kTerms) {
+          const float2 q = bf2_to_f2(o[t][e]);
+          f.x -= q.x, f.y -= q.y;  // exact
+        }
+      }
+    }
+  }
+#pragma unroll
+  for (int t = 0; t < kTerms; ++t)
+    sts_v4(to + t * kTile, make_uint4(o[t][0], o[t][1], o[t][2], o[t][3]));
 }
-__device__ __forceinline__ uint32_t cluster_size() {
-  uint32_t r;
-  asm volatile("mov.u32 %0, %%cluster_nctarank;" : "=r"(r));
-  return r;
+// The chunk that holds the sequence's end, from its n valid tokens: keys, values
+// and weighted keys past the end become 0 (padding may hold NaN).  ys, zs, cs:
+// the thread's piece of row rr; rows rr + 16 k.
+template <int kTerms, int kTile>
+__device__ __forceinline__ void weigh_end(uint32_t ys, uint32_t zs, uint32_t cs, int rr, int n,
+                                          float l2, float gain, bool reverse) {
+  const uint4 zero = make_uint4(0, 0, 0, 0);
+#pragma unroll 1
+  for (int k = 0; k < 4 * kTile / kBlk; ++k) {
+    const int r = rr + 16 * (k & 3), off = (k >> 2) * kBlk + (k & 3) * 2048;
+    if (r < n) {
+      RowWeight w;
+      w.set(gain * decay_pow(l2, (float)(reverse ? r : n - 1 - r)));
+      weigh_piece<kTerms, kTile>(lds_v4(ys + off), w, cs + off);
+      continue;
+    }
+    sts_v4(ys + off, zero);
+    sts_v4(zs + off, zero);
+#pragma unroll
+    for (int t = 0; t < kTerms; ++t) sts_v4(cs + t * kTile + off, zero);
+  }
 }
-__device__ __forceinline__ void cluster_arrive() {
-  asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
-}
-__device__ __forceinline__ void cluster_wait() {
-  asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+
+// The chunk's own state, sum of (v_j y_j) z_j^T, into (keep: added to) the
+// columns at d.  D = 64: transposed (M = e), the first two terms side by side in
+// N, the third onto the second; D = 128: all onto one another, the small first.
+template <int D, int kTerms, int kTile>
+__device__ __forceinline__ void state_product(uint32_t d, uint32_t zs, uint32_t cs, bool keep) {
+  const uint64_t zd = sw128_desc(zs, kBlk, 1024), cd = sw128_desc(cs, kBlk, 1024);
+  if constexpr (D == 64) {
+    constexpr uint32_t id2 = idesc_bf16_f32(64, 128, 1, 1), id1 = idesc_bf16_f32(64, 64, 1, 1);
+#pragma unroll
+    for (int k = 0; k < 4; ++k)
+      mma_bf16(d, desc_at(zd, k * 2048), desc_at(cd, k * 2048), id2, keep || k != 0);
+    if constexpr (kTerms == 3)
+#pragma unroll
+      for (int k = 0; k < 4; ++k)
+        mma_bf16(d + 64, desc_at(zd, k * 2048), desc_at(cd, 2 * kTile + k * 2048), id1, 1);
+  } else {
+    constexpr uint32_t id_s = idesc_bf16_f32(D, D, 1, 1);
+#pragma unroll
+    for (int t = kTerms - 1; t >= 0; --t)
+#pragma unroll
+      for (int k = 0; k < 4; ++k)
+        mma_bf16(d, desc_at(cd, t * kTile + k * 2048), desc_at(zd, k * 2048), id_s,
+                 keep || t != kTerms - 1 || k != 0);
+  }
 }
 
 // Place of a state thread's value i: D = 64, held transposed, as tmem_ld_16x64
@@ -209,6 +280,246 @@ __device__ __forceinline__ int state_at(int sw, int lane, int i, int *e) {
   return 32 * (sw & 3) + lane;
 }
 
+// S = S + f v or S = f S + v over a state thread's values, from the columns at
+// src (D = 64: the small terms' columns first).
+template <int D, bool kOwn, int kNV>
+__device__ __forceinline__ void take_state(float (&S)[kNV], uint32_t src, float f) {
+  const float2 f2 = make_float2(f, f);
+  auto add = [&](int i, float2 v) {
+    const float2 q = make_float2(S[i], S[i + 1]);
+    const float2 r = kOwn ? __ffma2_rn(f2, v, q) : __ffma2_rn(f2, q, v);
+    S[i] = r.x, S[i + 1] = r.y;
+  };
+  if constexpr (D == 64) {
+    float v[32];
+    tmem_ld_16x64(src + 64, v);
+    tmem_ld_wait_regs(v);
+#pragma unroll
+    for (int i = 0; i < 32; i += 2) add(i, make_float2(v[i], v[i + 1]));
+    tmem_ld_16x64(src, v);
+    tmem_ld_wait_regs(v);
+#pragma unroll
+    for (int i = 0; i < 32; i += 2) {
+      if (kOwn) {
+        add(i, make_float2(v[i], v[i + 1]));
+      } else {
+        const float2 r = __fadd2_rn(make_float2(S[i], S[i + 1]), make_float2(v[i], v[i + 1]));
+        S[i] = r.x, S[i + 1] = r.y;
+      }
+    }
+  } else {
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      float v[16];
+      tmem_ld16(src + 16 * k, v);
+      tmem_ld_wait_regs(v);
+#pragma unroll
+      for (int e = 0; e < 16; e += 2) add(16 * k + e, make_float2(v[e], v[e + 1]));
+    }
+  }
+}
+
+// The CTA's segment in scan order: places [q0, q0 + cnt) of the nc chunks.
+struct Segment {
+  int L, nc, q0, cnt;
+  bool last, reverse;
+  __device__ __forceinline__ Segment(const TcParams &p, int b, int rank) : reverse(p.reverse) {
+    L = p.seq_lens == nullptr ? p.N : min(max(p.seq_lens[b], 0), p.N);
+    nc = (L + kC - 1) / kC;
+    q0 = rank * p.seg;
+    cnt = max(0, min(p.seg, nc - q0));
+    last = cnt > 0 && q0 + cnt == nc;
+  }
+  __device__ __forceinline__ int token_of(int place) const {
+    return (reverse ? nc - 1 - place : place) * kC;
+  }
+};
+
+// ---------------------------------------------------------------------------
+// The state of each segment but the last, without what comes before it.  Chunks
+// go by from the segment's end in scan order to its start; kGroup of them add up
+// in TMEM (their distance from the first is in the weights), then the state warps
+// take the sum.  Warps: 0-7 form v_j y_j (two groups, alternate chunks), the next
+// 4 (D = 128: 8) hold the state, then loads and MMAs.
+constexpr int kGroup = 8;
+
+template <int D, int kTerms>
+struct OwnShape {
+  static constexpr int kB = D / 64, kTile = kB * kBlk;
+  // Even, so that a slot always meets the same one of the two groups: a parity
+  // wait tells a phase from the one before it only, and a group that missed a
+  // phase of a slot would take an old one for the one it waits for.
+  static constexpr int kNY = 4, kNZ = 4;
+  static constexpr int kOffY = 0, kOffZ = kNY * kTile, kOffConv = kOffZ + kNZ * kTile;
+  static constexpr int kOffBar = kOffConv + 2 * kTerms * kTile;
+  static constexpr int kBars = 2 * (kNY + kNZ) + 2 * 4 + 1;
+  static constexpr int kOffMisc = kOffBar + kBars * 8;
+  static constexpr int kSmem = kOffMisc + 16 + 1024;
+  static_assert(kSmem <= 227 * 1024, "shared memory");
+  static constexpr int kSWarps = D == 64 ? 4 : 8;
+  static constexpr int kTmaWarp = 8 + kSWarps, kMmaWarp = kTmaWarp + 1;
+  static constexpr int kThreads = (kMmaWarp + 1) * 32;
+  static constexpr int kLoads = 2 * kB;
+  static constexpr uint32_t kTmemCols = 256;  // two buffers of 128
+  static constexpr int kPerSm = D == 64 && kTerms == 2 ? 2 : 1;  // as the shared memory allows
+};
+
+template <int D, int kTerms>
+__global__ void __launch_bounds__(OwnShape<D, kTerms>::kThreads, OwnShape<D, kTerms>::kPerSm)
+    own_state_kernel(const TcParams p, const __grid_constant__ CUtensorMap tm_y,
+                     const __grid_constant__ CUtensorMap tm_z) {
+  using Sh = OwnShape<D, kTerms>;
+  constexpr int kNV = D == 64 ? 32 : 64;
+  grid_dep_launch();
+  extern __shared__ uint8_t smem_raw[];
+  uint8_t *smem = (uint8_t *)(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);
+  uint64_t *fy = (uint64_t *)(smem + Sh::kOffBar), *ey = fy + Sh::kNY, *fz = ey + Sh::kNY,
+           *ez = fz + Sh::kNZ, *conv_full = ez + Sh::kNZ, *conv_empty = conv_full + 2,
+           *ds_full = conv_empty + 2, *ds_empty = ds_full + 2, *drained = ds_empty + 2;
+  uint32_t *tmem_slot = (uint32_t *)(smem + Sh::kOffMisc);
+  const AbortFlag ab{smem_u32(smem + Sh::kOffMisc + 4)};
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  const int rank = blockIdx.x, h = blockIdx.y, b = blockIdx.z;
+  const Segment sg(p, b, rank);
+  if (sg.cnt == 0 || sg.last) return;
+  const float l2 = __ldg(p.log_decay + h) * 1.4426950408889634f;
+
+  if (tid == 0) {
+    *(volatile int *)(smem + Sh::kOffMisc + 4) = 0;
+    for (int i = 0; i < Sh::kNY; ++i) mbar_init(&fy[i], Sh::kB), mbar_init(&ey[i], 1);
+    for (int i = 0; i < Sh::kNZ; ++i) mbar_init(&fz[i], Sh::kB), mbar_init(&ez[i], 1);
+    for (int i = 0; i < 2; ++i) {
+      mbar_init(&conv_full[i], 4);
+      mbar_init(&conv_empty[i], 1);
+      mbar_init(&ds_full[i], 1);
+      mbar_init(&ds_empty[i], Sh::kSWarps);
+    }
+    mbar_init(drained, 1);
+    fence_mbar_init();
+  }
+  if (warp == Sh::kTmaWarp && lane == 0) {
+    tma_prefetch_desc(&tm_y);
+    tma_prefetch_desc(&tm_z);
+  }
+  if (warp == Sh::kMmaWarp) tmem_alloc(tmem_slot, Sh::kTmemCols);
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem = *tmem_slot;
+  auto token_at = [&](int g) { return sg.token_of(sg.q0 + sg.cnt - 1 - g); };
+
+  if (warp == Sh::kTmaWarp) {
+    if (lane < Sh::kLoads) {
+      const int t = lane / Sh::kB, blk = lane % Sh::kB;
+      const CUtensorMap *tm = t == 0 ? &tm_y : &tm_z;
+      const int hd = h / (t == 0 ? p.gy : p.gz), slots = t == 0 ? Sh::kNY : Sh::kNZ;
+      uint64_t *f = t == 0 ? fy : fz, *e = t == 0 ? ey : ez;
+      uint8_t *to = smem + (t == 0 ? Sh::kOffY : Sh::kOffZ) + blk * kBlk;
+      int i = 0;
+      for (; i < sg.cnt; ++i) {
+        const int s = i % slots;
+        if (!mbar_wait(&e[s], ((i / slots) & 1) ^ 1, &ab)) {
+          decay_error(1, ab);
+          break;
+        }
+        mbar_arrive_expect_tx(&f[s], kBlk);
+        tma_load_4d(to + s * Sh::kTile, tm, &f[s], blk * 64, hd, token_at(i), b);
+      }
+      if (i < sg.cnt)  // gave up: no copy may land after the CTA is gone
+        for (int k = max(0, i - slots); k < i; ++k)
+          mbar_wait(&f[k % slots], (k / slots) & 1, nullptr);
+    }
+    __syncwarp();
+  } else if (warp == Sh::kMmaWarp) {
+    if (elect_one()) {
+      const uint32_t base = smem_u32(smem);
+      bool ok = true;
+      auto wait = [&](uint64_t *m, uint32_t parity) {
+        if (ok && !mbar_wait(m, parity, &ab)) decay_error(2, ab), ok = false;
+        return ok;
+      };
+      for (int g = 0; g < sg.cnt && ok; ++g) {
+        const int cb = g & 1, q = g / kGroup, db = q & 1;
+        if (g % kGroup == 0 && q >= 2 && !wait(&ds_empty[db], ((q >> 1) & 1) ^ 1)) break;
+        if (!wait(&conv_full[cb], (g >> 1) & 1)) break;
+        tc_fence_after();
+        state_product<D, kTerms, Sh::kTile>(
+            tmem + 128 * db, base + Sh::kOffZ + (g % Sh::kNZ) * Sh::kTile,
+            base + Sh::kOffConv + cb * kTerms * Sh::kTile, g % kGroup != 0);
+        mma_commit(&conv_empty[cb]);
+        mma_commit(&ey[g % Sh::kNY]);
+        mma_commit(&ez[g % Sh::kNZ]);
+        if (g % kGroup == kGroup - 1 || g == sg.cnt - 1) mma_commit(&ds_full[db]);
+      }
+      mma_commit(drained);  // nothing is in flight when TMEM is freed
+      if (!mbar_wait(drained, 0, nullptr)) decay_error(512, ab);
+    }
+    __syncwarp();
+  } else if (warp < 8) {
+    const int ct = tid & 127, ch = ct & 7, rr = ct >> 3;
+    float wr[4];
+#pragma unroll
+    for (int k = 0; k < 4; ++k)
+      wr[k] = decay_pow(l2, (float)(p.reverse ? rr + 16 * k : kC - 1 - rr - 16 * k));
+    const uint32_t piece = rr * 128 + ((ch ^ (rr & 7)) << 4);
+    for (int g = warp >> 2; g < sg.cnt; g += 2) {
+      const int sy = g % Sh::kNY, sz = g % Sh::kNZ, cb = g & 1;
+      const int n = min(kC, sg.L - token_at(g));
+      const float gain = decay_pow(l2, (float)(g % kGroup) * kC);
+      if (!mbar_wait(&fy[sy], (g / Sh::kNY) & 1, &ab)) decay_error(16, ab);
+      if (!mbar_wait(&fz[sz], (g / Sh::kNZ) & 1, &ab)) decay_error(16, ab);  // for the MMAs
+      if (g >= 2 && !mbar_wait(&conv_empty[cb], ((g >> 1) & 1) ^ 1, &ab)) decay_error(32, ab);
+      const uint32_t ys = smem_u32(smem + Sh::kOffY + sy * Sh::kTile) + piece;
+      const uint32_t cs = smem_u32(smem + Sh::kOffConv + cb * kTerms * Sh::kTile) + piece;
+      if (n == kC) {
+        RowWeight w[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) w[k].set(gain * wr[k]);
+#pragma unroll
+        for (int blk = 0; blk < Sh::kB; ++blk) {
+          uint4 u[4];
+#pragma unroll
+          for (int k = 0; k < 4; ++k) u[k] = lds_v4(ys + blk * kBlk + k * 2048);
+#pragma unroll
+          for (int k = 0; k < 4; ++k)
+            weigh_piece<kTerms, Sh::kTile>(u[k], w[k], cs + blk * kBlk + k * 2048);
+        }
+      } else {
+        weigh_end<kTerms, Sh::kTile>(ys, smem_u32(smem + Sh::kOffZ + sz * Sh::kTile) + piece, cs, rr,
+                                     n, l2, gain, p.reverse);
+      }
+      fence_proxy_async_smem();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(&conv_full[cb]);
+    }
+  } else {
+    const int sw = warp - 8, st = tid - 8 * 32;
+    const uint32_t src = tmem + ((uint32_t)(32 * (sw & 3)) << 16) + (D == 64 ? 0 : 64 * (sw >> 2));
+    float S[kNV];
+#pragma unroll
+    for (int i = 0; i < kNV; ++i) S[i] = 0.f;
+    for (int q = 0; q * kGroup < sg.cnt; ++q) {
+      if (!mbar_wait(&ds_full[q & 1], (q >> 1) & 1, &ab)) decay_error(64, ab);
+      tc_fence_after();
+      take_state<D, true>(S, src + 128 * (q & 1), decay_pow(l2, (float)q * (kGroup * kC)));
+      tc_fence_before();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(&ds_empty[q & 1]);
+    }
+    float *part = p.part + (((size_t)b * p.H + h) * p.ranks + rank) * D * D + st;
+#pragma unroll
+    for (int i = 0; i < kNV; ++i) part[i * Sh::kSWarps * 32] = S[i];
+  }
+  tc_fence_before();
+  __syncthreads();
+  if (warp == Sh::kMmaWarp) {
+    tc_fence_after();
+    tmem_dealloc(tmem, Sh::kTmemCols);
+  }
+}
+
+// ---------------------------------------------------------------------------
+// The scan of each segment.
 template <int D, int kTerms, typename O>
 __global__ void __launch_bounds__(Shape<D, kTerms>::kThreads, 1)
     decay_kernel(const TcParams p, const __grid_constant__ CUtensorMap tm_x,
@@ -232,31 +543,24 @@ __global__ void __launch_bounds__(Shape<D, kTerms>::kThreads, 1)
 
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const int h = blockIdx.y, b = blockIdx.z;
-  const int rank = (int)cluster_rank(), ranks = (int)cluster_size();
-  const int L = p.seq_lens == nullptr ? p.N : min(max(p.seq_lens[b], 0), p.N);
+  const int rank = blockIdx.x;
+  const Segment sg(p, b, rank);
+  const int L = sg.L, q0 = sg.q0, cnt = sg.cnt;
   const size_t bh = (size_t)b * p.H + h, orow = (size_t)p.H * D;
   O *out = (O *)p.out + ((size_t)b * p.N * p.H + h) * D;  // token t at t * orow
 
-  if (p.zero_pad) {  // the rows past the end, shared among the cluster's CTAs
+  if (p.zero_pad) {  // the rows past the end, shared among the sequence's CTAs
     constexpr int kPer = D * (int)sizeof(O) / 16;
     for (long long i = (long long)rank * Sh::kThreads + tid; i < (long long)(p.N - L) * kPer;
-         i += (long long)ranks * Sh::kThreads)
+         i += (long long)p.ranks * Sh::kThreads)
       ((uint4 *)(out + (L + i / kPer) * orow))[i % kPer] = make_uint4(0, 0, 0, 0);
   }
-  // The CTA's chunks by their place in scan order: [q0, q0 + cnt) of nc.
-  const int nc = (L + kC - 1) / kC;
-  const int seg = max(1, (nc + ranks - 1) / ranks);
-  const int last_rank = nc > 0 ? min(ranks - 1, (nc - 1) / seg) : 0;
-  const int q0 = rank * seg;
-  const int cnt = rank > last_rank ? 0 : (rank == last_rank ? nc - q0 : seg);
-  const bool is_last = rank == last_rank;
   if (cnt == 0) {
     if (rank == 0 && p.fin)  // an empty sequence passes its state on
       for (int i = tid; i < D * D; i += Sh::kThreads)
         p.fin[bh * D * D + i] = p.init ? p.init[bh * D * D + i] * p.init_scale * p.fin_scale : 0.f;
     return;
   }
-  const int pre = is_last ? 0 : cnt;  // chunks of the pass over the segment's own state
   const float l2 = __ldg(p.log_decay + h) * 1.4426950408889634f;
 
   if (tid == 0) {
@@ -291,14 +595,6 @@ __global__ void __launch_bounds__(Shape<D, kTerms>::kThreads, 1)
   __syncthreads();
   tc_fence_after();
   const uint32_t tmem = *tmem_slot;
-  const bool state_warp = warp >= 8 && warp < 8 + Sh::kSWarps;
-  if (ranks > 1 && !state_warp) cluster_arrive();
-
-  // Step g of the CTA (its own-state pass, then the scan): the chunk's place in
-  // scan order, and its first token.
-  auto place_of = [&](int g) { return g < pre ? q0 + cnt - 1 - g : q0 + g - pre; };
-  auto token_of = [&](int place) { return (p.reverse ? nc - 1 - place : place) * kC; };
-
   if (warp == Sh::kTmaWarp) {
     // ---------------------------------------------------------------- loads
     if (lane < Sh::kLoads) {
@@ -309,18 +605,17 @@ __global__ void __launch_bounds__(Shape<D, kTerms>::kThreads, 1)
       const int slots = t == 0 ? 2 : t == 1 ? Sh::kNY : Sh::kNZ;
       uint8_t *to = smem + (t == 0 ? Sh::kOffX : t == 1 ? Sh::kOffY : Sh::kOffZ) + blk * kBlk;
       const int size = t == 1 ? Sh::kYSlot : Sh::kTile;
-      const int first = t == 0 ? pre : 0, steps = pre + cnt - first;  // x: the scan alone
       int i = 0;
-      for (; i < steps; ++i) {
+      for (; i < cnt; ++i) {
         const int s = i % slots;
         if (!mbar_wait(&e[s], ((i / slots) & 1) ^ 1, &ab)) {
           decay_error(1, ab);
           break;
         }
         mbar_arrive_expect_tx(&f[s], kBlk);
-        tma_load_4d(to + s * size, tm, &f[s], blk * 64, hd, token_of(place_of(first + i)), b);
+        tma_load_4d(to + s * size, tm, &f[s], blk * 64, hd, sg.token_of(q0 + i), b);
       }
-      if (i < steps)  // gave up: no copy may land after the CTA is gone
+      if (i < cnt)  // gave up: no copy may land after the CTA is gone
         for (int k = max(0, i - slots); k < i; ++k)
           mbar_wait(&f[k % slots], (k / slots) & 1, nullptr);
     }
@@ -334,47 +629,20 @@ __global__ void __launch_bounds__(Shape<D, kTerms>::kThreads, 1)
         if (ok && !mbar_wait(m, parity, &ab)) decay_error(2, ab), ok = false;
         return ok;
       };
-      // the chunk's own state, sum of (v_j y_j) z_j^T; own: in the pass over the
-      // segment's own state, after which the tiles are free
-      auto state_mma = [&](int g, bool own) {
-        const int cb = g % Sh::kConv, sz = g % Sh::kNZ;
-        if (!wait(&state_ready[cb], (g / Sh::kConv) & 1)) return;
+      auto state_mma = [&](int i) {
+        const int cb = i % Sh::kConv;
+        if (!wait(&state_ready[cb], (i / Sh::kConv) & 1)) return;
         tc_fence_after();
-        const uint64_t zd = sw128_desc(base + Sh::kOffZ + sz * Sh::kTile, kBlk, 1024);
-        const uint64_t cd =
-            sw128_desc(base + Sh::kOffConv + cb * kTerms * Sh::kTile, kBlk, 1024);
-        const uint32_t d = tmem + Sh::kColDs;
-        if constexpr (Sh::kMerged) {
-          // transposed (M = e): the first two terms side by side in N, the third
-          // onto the second
-          constexpr uint32_t id2 = idesc_bf16_f32(64, 128, 1, 1), id1 = idesc_bf16_f32(64, 64, 1, 1);
-#pragma unroll
-          for (int k = 0; k < 4; ++k)
-            mma_bf16(d, desc_at(zd, k * 2048), desc_at(cd, k * 2048), id2, k != 0);
-          if constexpr (kTerms == 3)
-#pragma unroll
-            for (int k = 0; k < 4; ++k)
-              mma_bf16(d + 64, desc_at(zd, k * 2048), desc_at(cd, 2 * Sh::kTile + k * 2048), id1, 1);
-        } else {
-          constexpr uint32_t id_s = idesc_bf16_f32(D, D, 1, 1);
-#pragma unroll
-          for (int t = kTerms - 1; t >= 0; --t)  // the small terms first
-#pragma unroll
-            for (int k = 0; k < 4; ++k)
-              mma_bf16(d, desc_at(cd, t * Sh::kTile + k * 2048), desc_at(zd, k * 2048), id_s,
-                       t != kTerms - 1 || k != 0);
-        }
+        state_product<D, kTerms, Sh::kTile>(
+            tmem + Sh::kColDs, base + Sh::kOffZ + (i % Sh::kNZ) * Sh::kTile,
+            base + Sh::kOffConv + cb * kTerms * Sh::kTile, false);
         mma_commit(ds_full);
         mma_commit(&conv_empty[cb]);
-        if (own) {
-          mma_commit(&ey[g % Sh::kNY]);
-          mma_commit(&ez[sz]);
-        }
       };
-      // scores of the scan's chunk i; merged: and x_r^T S.  The chunk's state
+      // scores of chunk i; merged: and x_r^T S.  The chunk's state
       // went before, so its keys are there and those past the end are zero.
       auto score_mma = [&](int i) {
-        const int sx = i & 1, sy = (pre + i) % Sh::kNY;
+        const int sx = i & 1, sy = i % Sh::kNY;
         if (!wait(&score_ready[sx], (i >> 1) & 1)) return;
         tc_fence_after();
         constexpr uint32_t id = idesc_bf16_f32(64, Sh::kMerged ? 128 : 64, 0, 0);
@@ -406,7 +674,7 @@ __global__ void __launch_bounds__(Shape<D, kTerms>::kThreads, 1)
         mma_commit(&ex[sx]);
       };
       auto intra_mma = [&](int j) {  // sum_j (w_rj A_rj) z_j
-        const int g = pre + j, sz = g % Sh::kNZ, pb = j % Sh::kP, ob = j & 1;
+        const int sz = j % Sh::kNZ, pb = j % Sh::kP, ob = j & 1;
         if (!wait(&intra_ready[pb], (j / Sh::kP) & 1)) return;
         tc_fence_after();
         constexpr uint32_t id = idesc_bf16_f32(64, D, 0, 1);
@@ -420,8 +688,7 @@ __global__ void __launch_bounds__(Shape<D, kTerms>::kThreads, 1)
         mma_commit(&o_full[ob]);
         mma_commit(&ez[sz]);
       };
-      for (int g = 0; g < pre && ok; ++g) state_mma(g, true);
-      if (ok) state_mma(pre, false);
+      state_mma(0);
       // Scores of chunk i, results of chunk i - 1 (whose scores have been
       // weighted meanwhile), state of chunk i + 1 (which leaves a whole round for
       // the state to reach the scores of i + 1).
@@ -430,7 +697,7 @@ __global__ void __launch_bounds__(Shape<D, kTerms>::kThreads, 1)
         if constexpr (!Sh::kMerged)
           if (i < cnt && ok) inter_mma(i);
         if (i >= 1 && ok) intra_mma(i - 1);
-        if (i + 1 < cnt && ok) state_mma(pre + i + 1, false);
+        if (i + 1 < cnt && ok) state_mma(i + 1);
       }
       mma_commit(drained);  // nothing is in flight when TMEM is freed
       if (!mbar_wait(drained, 0, nullptr)) decay_error(512, ab);
@@ -477,47 +744,20 @@ __global__ void __launch_bounds__(Shape<D, kTerms>::kThreads, 1)
   } else if (warp < 8) {
     // --------------------------------------------- weighted keys (warps 4-7)
     const int ct = tid - 128, ch = ct & 7, rr = ct >> 3;  // 16-byte chunk, first row
-    float wr[4];
-    uint32_t wh[4], wl[4];  // two terms: the weight as a sum of two bf16 numbers
+    const uint32_t piece = rr * 128 + ((ch ^ (rr & 7)) << 4);
+    RowWeight w[4];
 #pragma unroll
-    for (int k = 0; k < 4; ++k) {
-      const int r = rr + 16 * k;
-      wr[k] = decay_pow(l2, (float)(p.reverse ? r : kC - 1 - r));
-      wh[k] = f2_to_bf2(wr[k], wr[k]);
-      const float rest = wr[k] - bf2_to_f2(wh[k]).x;
-      wl[k] = f2_to_bf2(rest, rest);
-    }
-    // one 16-byte piece: kTerms bf16 numbers for each of its 8 products
-    auto split = [&](const uint4 &u, float w, uint32_t to) {
-      const uint32_t in[4] = {u.x, u.y, u.z, u.w};
-      uint32_t o[kTerms][4];
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        float2 f = bf2_to_f2(in[e]);
-        f.x *= w, f.y *= w;
-#pragma unroll
-        for (int t = 0; t < kTerms; ++t) {
-          o[t][e] = f2_to_bf2(f.x, f.y);
-          if (t + 1 < kTerms) {
-            const float2 q = bf2_to_f2(o[t][e]);
-            f.x -= q.x, f.y -= q.y;  // exact
-          }
-        }
-      }
-#pragma unroll
-      for (int t = 0; t < kTerms; ++t)
-        sts_v4(to + t * Sh::kTile, make_uint4(o[t][0], o[t][1], o[t][2], o[t][3]));
-    };
-    for (int g = 0; g < pre + cnt; ++g) {
-      const int sy = g % Sh::kNY, sz = g % Sh::kNZ, cb = g % Sh::kConv;
-      const int n = min(kC, L - token_of(place_of(g)));
-      if (!mbar_wait(&fy[sy], (g / Sh::kNY) & 1, &ab)) decay_error(16, ab);
-      if (!mbar_wait(&fz[sz], (g / Sh::kNZ) & 1, &ab)) decay_error(16, ab);  // for the MMAs
-      if (g >= Sh::kConv && !mbar_wait(&conv_empty[cb], ((g / Sh::kConv) & 1) ^ 1, &ab))
+    for (int k = 0; k < 4; ++k)
+      w[k].set(decay_pow(l2, (float)(p.reverse ? rr + 16 * k : kC - 1 - rr - 16 * k)));
+    for (int i = 0; i < cnt; ++i) {
+      const int sy = i % Sh::kNY, sz = i % Sh::kNZ, cb = i % Sh::kConv;
+      const int n = min(kC, L - sg.token_of(q0 + i));
+      if (!mbar_wait(&fy[sy], (i / Sh::kNY) & 1, &ab)) decay_error(16, ab);
+      if (!mbar_wait(&fz[sz], (i / Sh::kNZ) & 1, &ab)) decay_error(16, ab);  // for the MMAs
+      if (i >= Sh::kConv && !mbar_wait(&conv_empty[cb], ((i / Sh::kConv) & 1) ^ 1, &ab))
         decay_error(32, ab);
-      const uint32_t ys = smem_u32(smem + Sh::kOffY + sy * Sh::kYSlot) + rr * 128 + ((ch ^ (rr & 7)) << 4);
-      const uint32_t cs = smem_u32(smem + Sh::kOffConv + cb * kTerms * Sh::kTile) + rr * 128 +
-                          ((ch ^ (rr & 7)) << 4);
+      const uint32_t ys = smem_u32(smem + Sh::kOffY + sy * Sh::kYSlot) + piece;
+      const uint32_t cs = smem_u32(smem + Sh::kOffConv + cb * kTerms * Sh::kTile) + piece;
       if (n == kC) {
 #pragma unroll
         for (int blk = 0; blk < Sh::kB; ++blk) {
@@ -525,48 +765,18 @@ __global__ void __launch_bounds__(Shape<D, kTerms>::kThreads, 1)
 #pragma unroll
           for (int k = 0; k < 4; ++k) u[k] = lds_v4(ys + blk * kBlk + k * 2048);
 #pragma unroll
-          for (int k = 0; k < 4; ++k) {
-            if constexpr (kTerms == 3) {
-              split(u[k], wr[k], cs + blk * kBlk + k * 2048);
-            } else {
-              // y w in packed bf16: hi = rn(y wh), y wh - hi is exact, and
-              // lo = rn(y wl + that)
-              const uint32_t in[4] = {u[k].x, u[k].y, u[k].z, u[k].w};
-              uint32_t hi[4], lo[4];
-#pragma unroll
-              for (int e = 0; e < 4; ++e) {
-                hi[e] = bf2_mul(in[e], wh[k]);
-                lo[e] = bf2_fma(in[e], wl[k], bf2_fma(in[e], wh[k], hi[e] ^ 0x80008000u));
-              }
-              const uint32_t to = cs + blk * kBlk + k * 2048;
-              sts_v4(to, make_uint4(hi[0], hi[1], hi[2], hi[3]));
-              sts_v4(to + Sh::kTile, make_uint4(lo[0], lo[1], lo[2], lo[3]));
-            }
-          }
+          for (int k = 0; k < 4; ++k)
+            weigh_piece<kTerms, Sh::kTile>(u[k], w[k], cs + blk * kBlk + k * 2048);
         }
       } else {
-        // the chunk with the sequence's end: padding may hold NaN, so keys, values
-        // and weighted keys past the end become 0
-        const uint32_t zs = smem_u32(smem + Sh::kOffZ + sz * Sh::kTile) + rr * 128 + ((ch ^ (rr & 7)) << 4);
-        const uint4 zero = make_uint4(0, 0, 0, 0);
-#pragma unroll 1
-        for (int k = 0; k < 4 * Sh::kB; ++k) {
-          const int r = rr + 16 * (k & 3), off = (k >> 2) * kBlk + (k & 3) * 2048;
-          if (r < n) {
-            split(lds_v4(ys + off), decay_pow(l2, (float)(p.reverse ? r : n - 1 - r)), cs + off);
-            continue;
-          }
-          sts_v4(ys + off, zero);
-          sts_v4(zs + off, zero);
-#pragma unroll
-          for (int t = 0; t < kTerms; ++t) sts_v4(cs + t * Sh::kTile + off, zero);
-        }
+        weigh_end<kTerms, Sh::kTile>(ys, smem_u32(smem + Sh::kOffZ + sz * Sh::kTile) + piece, cs, rr,
+                                     n, l2, 1.f, p.reverse);
       }
       fence_proxy_async_smem();
       __syncwarp();
       if (lane == 0) mbar_arrive(&state_ready[cb]);
     }
-  } else if (state_warp) {
+  } else if (warp < 8 + Sh::kSWarps) {
     // ------------------------------------------------- the state, in registers
     const int sw = warp - 8;
     float S[kNV];
@@ -575,73 +785,20 @@ __global__ void __launch_bounds__(Shape<D, kTerms>::kThreads, 1)
     const uint32_t src = tmem + ((uint32_t)(32 * (sw & 3)) << 16) + Sh::kColDs +
                          (D == 64 ? 0 : 64 * (sw >> 2));
     if (lane == 0) mbar_arrive(&state_ready[0]);
-    // own: S = S + f (the state of step g's chunk); else S = f S + it
-    auto take = [&](int g, float f, auto own) {
-      const float2 f2 = make_float2(f, f);
-      auto add = [&](int i, float2 v) {
-        const float2 q = make_float2(S[i], S[i + 1]);
-        const float2 r = own ? __ffma2_rn(f2, v, q) : __ffma2_rn(f2, q, v);
-        S[i] = r.x, S[i + 1] = r.y;
-      };
-      if (!mbar_wait(ds_full, g & 1, &ab)) decay_error(64, ab);
-      tc_fence_after();
-      if constexpr (D == 64) {
-        float v[32];
-        tmem_ld_16x64(src + 64, v);  // the small terms first
-        tmem_ld_wait_regs(v);
-#pragma unroll
-        for (int i = 0; i < 32; i += 2) add(i, make_float2(v[i], v[i + 1]));
-        tmem_ld_16x64(src, v);
-        tmem_ld_wait_regs(v);
-#pragma unroll
-        for (int i = 0; i < 32; i += 2) {
-          if (own) {
-            add(i, make_float2(v[i], v[i + 1]));
-          } else {
-            const float2 r = __fadd2_rn(make_float2(S[i], S[i + 1]), make_float2(v[i], v[i + 1]));
-            S[i] = r.x, S[i + 1] = r.y;
-          }
-        }
-      } else {
-#pragma unroll
-        for (int k = 0; k < 4; ++k) {
-          float v[16];
-          tmem_ld16(src + 16 * k, v);
-          tmem_ld_wait_regs(v);
-#pragma unroll
-          for (int e = 0; e < 16; e += 2) add(16 * k + e, make_float2(v[e], v[e + 1]));
-        }
-      }
-      tc_fence_before();
-      __syncwarp();
-      if (lane == 0) mbar_arrive(&state_ready[(g + 1) % Sh::kConv]);
-    };
-    if (ranks > 1) {
-      // the segment's own state: chunks from its end in scan order to its start
-      for (int g = 0; g < pre; ++g) take(g, decay_pow(l2, (float)g * kC), std::true_type{});
-      constexpr int kThr = Sh::kSWarps * 32;
-      const int st = tid - 8 * 32;
-      float *part = p.part + bh * ranks * D * D;
-      if (pre) {
-#pragma unroll
-        for (int i = 0; i < kNV; ++i) {
-          __stcg(part + ((size_t)rank * kNV + i) * kThr + st, S[i]);
-          S[i] = 0.f;
-        }
-      }
-      cluster_arrive();
-      cluster_wait();
+    if (rank > 0) {  // the segments before
+      grid_dep_wait();
+      const float *part = p.part + bh * p.ranks * D * D + (tid - 8 * 32);
       for (int s = 0; s < rank; ++s) {
-        const float f = decay_pow(l2, (float)(rank - 1 - s) * seg * kC);
+        const float f = decay_pow(l2, (float)(rank - 1 - s) * p.seg * kC);
 #pragma unroll
         for (int i = 0; i < kNV; ++i)
-          S[i] = fmaf(f, __ldcg(part + ((size_t)s * kNV + i) * kThr + st), S[i]);
+          S[i] = fmaf(f, __ldcg(part + ((size_t)s * kNV + i) * (Sh::kSWarps * 32)), S[i]);
       }
     }
     if (p.init) {
       // tokens between the first state and this segment (reverse: and the last
       // token, which that state belongs to)
-      const float n = !p.reverse ? (float)q0 * kC : q0 == 0 ? 0.f : (float)(L - 1 - (nc - q0) * kC);
+      const float n = !p.reverse ? (float)q0 * kC : q0 == 0 ? 0.f : (float)(L - 1 - (sg.nc - q0) * kC);
       const float f = decay_pow(l2, n) * p.init_scale;
       const float *s0 = p.init + bh * D * D;
 #pragma unroll
@@ -653,8 +810,8 @@ __global__ void __launch_bounds__(Shape<D, kTerms>::kThreads, 1)
     }
     for (int j = 0; j < cnt; ++j) {
       if constexpr (D == 64) {  // behind the chunk's keys, once their slot is free
-        const int g = pre + j, sy = g % Sh::kNY;
-        if (!mbar_wait(&ey[sy], ((g / Sh::kNY) & 1) ^ 1, &ab)) decay_error(128, ab);
+        const int sy = j % Sh::kNY;
+        if (!mbar_wait(&ey[sy], ((j / Sh::kNY) & 1) ^ 1, &ab)) decay_error(128, ab);
         store_16x64(smem_u32(smem + Sh::kOffY + sy * Sh::kYSlot + Sh::kTile) + 16 * sw * 128, lane, S);
       } else {
         if (j >= 1 && !mbar_wait(s_empty, (j & 1) ^ 1, &ab)) decay_error(128, ab);
@@ -670,11 +827,16 @@ __global__ void __launch_bounds__(Shape<D, kTerms>::kThreads, 1)
       fence_proxy_async_smem();
       __syncwarp();
       if (lane == 0) mbar_arrive(Sh::kMerged ? &score_ready[j & 1] : &inter_ready[j & 1]);
-      const int t0 = token_of(q0 + j), n = min(kC, L - t0);
+      const int t0 = sg.token_of(q0 + j), n = min(kC, L - t0);
       const int span = !p.reverse ? n : (q0 + j == 0 ? n - 1 : kC);
-      take(pre + j, decay_pow(l2, (float)span), std::false_type{});
+      if (!mbar_wait(ds_full, j & 1, &ab)) decay_error(64, ab);
+      tc_fence_after();
+      take_state<D, false>(S, src, decay_pow(l2, (float)span));
+      tc_fence_before();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(&state_ready[(j + 1) % Sh::kConv]);
     }
-    if (p.fin && is_last) {
+    if (p.fin && sg.last) {
       const float f = p.fin_scale * (p.reverse ? decay_pow(l2, 1.f) : 1.f);
 #pragma unroll
       for (int i = 0; i < kNV; ++i) {
@@ -695,7 +857,7 @@ __global__ void __launch_bounds__(Shape<D, kTerms>::kThreads, 1)
     for (int k = 0; k < 2; ++k)
       u[k] = p.scale * decay_pow(l2, (float)(p.reverse ? kC - (r0 + 8 * k) : r0 + 8 * k + 1));
     for (int j = 0; j < cnt; ++j) {
-      const int ob = j & 1, t0 = token_of(q0 + j), n = min(kC, L - t0);
+      const int ob = j & 1, t0 = sg.token_of(q0 + j), n = min(kC, L - t0);
       float ur[2] = {u[0], u[1]};
       if (p.reverse && q0 + j == 0) {
 #pragma unroll
@@ -774,7 +936,6 @@ __global__ void __launch_bounds__(Shape<D, kTerms>::kThreads, 1)
     tc_fence_after();
     tmem_dealloc(tmem, 512);
   }
-  if (ranks > 1 && !state_warp) cluster_wait();
 }
 
 using EncodeTiledFn = CUresult (*)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *,
@@ -820,62 +981,71 @@ int sm_count() {
   return n;
 }
 
-// CTAs per sequence.  A CTA's time is its chunks, half of them again for the
-// pass over its own state; a launch takes the longest sequence's CTA or, where
-// that is more, all of them over the SMs (in whole rounds when the lengths are
-// known to be equal).  Lengths that only the device knows are taken to be a
-// quarter of the longest on average.
-int cluster_for(const ScanArgs &a) {
+// Chunks of a segment.  In units of a scanned chunk: a CTA of the scan takes its
+// chunks, one of the own-state kernel kOwnCost of them, a launch more takes
+// kLaunchCost, and the states of the segments before the last a little each.  A
+// kernel lasts as long as its longest CTA and as all of them over the SMs (in
+// whole rounds when the lengths are equal; lengths that only the device knows
+// are taken to be a quarter of the longest on average).
+int segment_for(const ScanArgs &a) {
+  constexpr double kOwnCost = 0.5, kLaunchCost = 6, kStateCost = 0.25;
   const int nc = (a.N + kC - 1) / kC, sms = sm_count();
   const double pairs = (double)a.B * a.H;
-  int best = 1;
+  int best = nc;
   double least = 0;
-  for (int cs = 1; cs <= kMaxCluster; cs *= 2) {
-    if (cs > 1 && nc < 4 * cs) break;
-    const double one = cs == 1 ? nc : 1.5 * ((nc + cs - 1) / cs);
-    const double rounds = pairs * cs / sms;
-    double t;
-    if (a.seq_lens)
-      t = one > one * rounds / 4 ? one : one * rounds / 4;
-    else
-      t = one * (double)(long long)(rounds + 0.999999);
-    if (cs == 1 || t < 0.95 * least) best = cs, least = t;
+  for (int r = 1; r <= 32 && nc >= 4 * r; ++r) {
+    const int seg = (nc + r - 1) / r;
+    double scan, own = 0;
+    if (a.seq_lens) {
+      const double all = pairs * nc / 4 / sms;
+      scan = seg > all + seg / 2 ? seg : all + seg / 2;
+      if (r > 1) own = kOwnCost * (seg > all ? seg : all);
+    } else {
+      scan = seg * (double)(long long)(pairs * r / sms + 0.999999);
+      if (r > 1) own = kOwnCost * seg * (double)(long long)(pairs * (r - 1) / sms + 0.999999);
+    }
+    const double t = scan + own + (r > 1 ? kLaunchCost + kStateCost * r * (a.D / 64) : 0);
+    if (r == 1 || t < 0.97 * least) best = seg, least = t;
   }
   return best;
 }
 
 template <int D, int kTerms, typename O>
-cudaError_t launch(const ScanArgs &a, const TcParams &p, int cs, const CUtensorMap &tx,
+cudaError_t launch(const ScanArgs &a, const TcParams &p, const CUtensorMap &tx,
                    const CUtensorMap &ty, const CUtensorMap &tz, cudaStream_t st) {
+  cudaError_t e;
+  if (p.ranks > 1) {
+    using Sh = OwnShape<D, kTerms>;
+    const auto kernel = own_state_kernel<D, kTerms>;
+    if ((e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                  Sh::kSmem)) != cudaSuccess)
+      return e;
+    kernel<<<dim3(p.ranks - 1, a.H, a.B), Sh::kThreads, Sh::kSmem, st>>>(p, ty, tz);
+    count_launch();
+    if ((e = cudaGetLastError()) != cudaSuccess) return e;
+  }
   using Sh = Shape<D, kTerms>;
   const auto kernel = decay_kernel<D, kTerms, O>;
-  cudaError_t e =
-      cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, Sh::kSmem);
-  if (e != cudaSuccess) return e;
-  cudaLaunchAttribute attr[1];
-  attr[0].id = cudaLaunchAttributeClusterDimension;
-  attr[0].val.clusterDim.x = cs;
-  attr[0].val.clusterDim.y = 1;
-  attr[0].val.clusterDim.z = 1;
-  cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3(cs, a.H, a.B);
-  cfg.blockDim = dim3(Sh::kThreads);
-  cfg.dynamicSmemBytes = Sh::kSmem;
-  cfg.stream = st;
-  cfg.attrs = attr;
-  cfg.numAttrs = 1;
+  if ((e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, Sh::kSmem)) !=
+      cudaSuccess)
+    return e;
+  const dim3 grid(p.ranks, a.H, a.B);
   count_launch();
-  return cudaLaunchKernelEx(&cfg, kernel, p, tx, ty, tz);
+  // Behind the own-state kernel the scan may start while that ends: only its
+  // state warps read what that kernel writes, and they wait for it.
+  if (p.ranks > 1) return launch_pdl(kernel, grid, dim3(Sh::kThreads), Sh::kSmem, st, p, tx, ty, tz);
+  kernel<<<grid, Sh::kThreads, Sh::kSmem, st>>>(p, tx, ty, tz);
+  return cudaGetLastError();
 }
 
 template <int D>
-cudaError_t launch_d(const ScanArgs &a, const TcParams &p, int cs, const CUtensorMap &tx,
+cudaError_t launch_d(const ScanArgs &a, const TcParams &p, const CUtensorMap &tx,
                      const CUtensorMap &ty, const CUtensorMap &tz, cudaStream_t st) {
   if (a.fin)
-    return a.out_f32 ? launch<D, 3, float>(a, p, cs, tx, ty, tz, st)
-                     : launch<D, 3, __nv_bfloat16>(a, p, cs, tx, ty, tz, st);
-  return a.out_f32 ? launch<D, 2, float>(a, p, cs, tx, ty, tz, st)
-                   : launch<D, 2, __nv_bfloat16>(a, p, cs, tx, ty, tz, st);
+    return a.out_f32 ? launch<D, 3, float>(a, p, tx, ty, tz, st)
+                     : launch<D, 3, __nv_bfloat16>(a, p, tx, ty, tz, st);
+  return a.out_f32 ? launch<D, 2, float>(a, p, tx, ty, tz, st)
+                   : launch<D, 2, __nv_bfloat16>(a, p, tx, ty, tz, st);
 }
 
 }  // namespace
@@ -892,8 +1062,8 @@ bool tc_scan_supports(const ScanArgs &a) {
 }
 
 size_t tc_scan_floats(const ScanArgs &a) {
-  const int cs = cluster_for(a);
-  return cs > 1 ? (size_t)a.B * a.H * cs * a.D * a.D : 0;
+  const int seg = segment_for(a), ranks = ((a.N + kC - 1) / kC + seg - 1) / seg;
+  return ranks > 1 ? (size_t)a.B * a.H * ranks * a.D * a.D : 0;
 }
 
 cudaError_t tc_scan(const ScanArgs &a, float *scratch, cudaStream_t st) {
@@ -908,9 +1078,9 @@ cudaError_t tc_scan(const ScanArgs &a, float *scratch, cudaStream_t st) {
   p.init_scale = a.init_scale, p.fin_scale = a.fin_scale, p.scale = a.scale;
   p.N = a.N, p.H = a.H, p.gx = a.gx, p.gy = a.gy, p.gz = a.gz;
   p.zero_pad = a.zero_pad, p.init_t = a.init_t, p.reverse = a.reverse;
-  const int cs = cluster_for(a);
-  return a.D == 64 ? launch_d<64>(a, p, cs, tx, ty, tz, st)
-                   : launch_d<128>(a, p, cs, tx, ty, tz, st);
+  p.seg = segment_for(a), p.ranks = ((a.N + kC - 1) / kC + p.seg - 1) / p.seg;
+  return a.D == 64 ? launch_d<64>(a, p, tx, ty, tz, st)
+                   : launch_d<128>(a, p, tx, ty, tz, st);
 }
 
 unsigned decay_device_error(bool reset) {

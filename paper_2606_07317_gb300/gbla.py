@@ -404,36 +404,55 @@ def state_static_scratch(k, v, gate, conv_w, seq_lens=None, out=None,
 
 # --- causal decoder operators -------------------------------------------------
 
-def _heads(t, name, like=None, width=None):
-    """Checks a [B, N, heads, D] tensor whose heads are adjacent and whose head values are
-    contiguous (batch and token strides are free); returns its (batch, token) strides."""
-    if t.dim() != 4:
-        raise ValueError(f"{name} must be [B, N, heads, D]")
-    if like is not None:
-        if t.dtype != like.dtype or t.device != like.device:
-            raise ValueError(f"{name} must have the dtype and device of q")
-        if t.shape[:2] != like.shape[:2] or t.shape[3] != like.shape[3]:
-            raise ValueError(f"{name} must be [B, N, heads, D] with q's B, N and D")
-    if width is not None and t.shape[2] != width:
-        raise ValueError(f"{name} must have {width} heads")
-    B, N, H, D = t.shape
-    if t.numel() and ((D > 1 and t.stride(3) != 1) or (H > 1 and t.stride(2) != D)):
+def _raw_stream(q, stream):
+    """Handle of the stream (None: the current one) that a call on q's tensors goes to."""
+    dev = q.get_device()
+    if dev < 0 or dev != torch.cuda.current_device():
+        raise ValueError("the tensors must be on the current CUDA device")
+    return torch._C._cuda_getCurrentRawStream(dev) if stream is None else stream.cuda_stream
+
+
+def _dims(q):
+    if q.dim() != 4:
+        raise ValueError("q must be [B, N, H, D]")
+    return q.shape
+
+
+def _heads(t, name, shape, q):
+    """Checks a token-major tensor of the given shape with q's dtype and device, whose heads
+    are adjacent and whose head values are contiguous; True if it is contiguous throughout."""
+    if t.shape != shape:
+        raise ValueError(f"{name} must be [B, N, heads, D] = {tuple(shape)}, not {tuple(t.shape)}")
+    if t.dtype is not q.dtype or t.get_device() != q.get_device():
+        raise ValueError(f"{name} must have the dtype and device of q")
+    if t.is_contiguous():
+        return True
+    if (shape[3] > 1 and t.stride(3) != 1) or (shape[2] > 1 and t.stride(2) != shape[3]):
         raise ValueError(f"the heads of {name} must be adjacent and their values contiguous")
-    return t.stride(0), t.stride(1)
+    return False
 
 
-def _plain(t, name, shape, dtype, device):
-    """Checks an optional contiguous tensor."""
+def _key_shape(q, k):
+    """Shape of a key or value tensor that goes with q."""
+    if k.dim() != 4:
+        raise ValueError("k must be [B, N, heads, D]")
+    B, N, _, D = q.shape
+    return (B, N, k.shape[2], D)
+
+
+def _plain(t, name, shape, dtype, q):
+    """Checks an optional contiguous tensor on q's device."""
     if t is None:
         return
-    if t.dtype != dtype or tuple(t.shape) != tuple(shape) or not t.is_contiguous():
+    if t.dtype is not dtype or t.shape != shape or not t.is_contiguous():
         raise ValueError(f"{name} must be a contiguous {dtype} tensor of shape {tuple(shape)}")
-    if t.device != device:
-        raise ValueError(f"{name} must be on {device}")
+    if t.get_device() != q.get_device():
+        raise ValueError(f"{name} must be on the device of q")
 
 
-def _strides(*pairs):
-    flat = [s for p in pairs for s in p]
+def _strides(*tensors, dims=2):
+    """Host array of the (batch, token) strides of each tensor (dims=1: batch alone)."""
+    flat = [s for t in tensors for s in t.stride()[:dims]]
     return (ctypes.c_int64 * len(flat))(*flat)
 
 
@@ -446,16 +465,16 @@ def rotation_table(positions: int, R: int, base: float = 10000.0, device="cuda")
 
 
 def _rotate_args(q, k, norm_q, norm_k, rot, positions, seq_lens):
-    sq, sk = _heads(q, "q"), _heads(k, "k", q)
-    B, N, H, D = q.shape
-    Hk, dev = k.shape[2], q.device
-    _plain(norm_q, "norm_q", (H, D), torch.float32, dev)
-    _plain(norm_k, "norm_k", (Hk, D), torch.float32, dev)
-    P, R = (rot.shape if rot is not None and rot.dim() == 2 else (0, 0))
-    _plain(rot, "rot", (P, R), torch.float32, dev)
-    _plain(positions, "positions", (B, N), torch.int32, dev)
-    _plain(seq_lens, "seq_lens", (B,), torch.int32, dev)
-    return _strides(sq, sk), (B, N, H, Hk, D, R, P)
+    B, N, H, D = shape = _dims(q)
+    Hk = _key_shape(q, k)[2]
+    whole = _heads(q, "q", shape, q) & _heads(k, "k", (B, N, Hk, D), q)
+    _plain(norm_q, "norm_q", (H, D), torch.float32, q)
+    _plain(norm_k, "norm_k", (Hk, D), torch.float32, q)
+    P, R = rot.shape if rot is not None and rot.dim() == 2 else (0, 0)
+    _plain(rot, "rot", (P, R), torch.float32, q)
+    _plain(positions, "positions", (B, N), torch.int32, q)
+    _plain(seq_lens, "seq_lens", (B,), torch.int32, q)
+    return None if whole else _strides(q, k), (B, N, H, Hk, D, R, P)
 
 
 def qk_norm_rotate(q, k, norm_q, norm_k, rot=None, positions=None, seq_lens=None,
@@ -469,12 +488,12 @@ def qk_norm_rotate(q, k, norm_q, norm_k, rot=None, positions=None, seq_lens=None
     if out is None:
         out = (torch.empty(q.shape, dtype=q.dtype, device=q.device),
                torch.empty(k.shape, dtype=k.dtype, device=q.device))
-    _plain(out[0], "out[0]", q.shape, q.dtype, q.device)
-    _plain(out[1], "out[1]", k.shape, q.dtype, q.device)
-    st = load().gbla_qk_norm_rotate(
+    _plain(out[0], "out[0]", q.shape, q.dtype, q)
+    _plain(out[1], "out[1]", k.shape, q.dtype, q)
+    st = (_lib or load()).gbla_qk_norm_rotate(
         _ptr(q), _ptr(k), _ptr(norm_q), _ptr(norm_k), _ptr(rot), _ptr(positions),
         _ptr(seq_lens), strides, _ptr(out[0]), _ptr(out[1]), *dims, float(eps),
-        ROTATE_INTERLEAVED if interleaved else 0, _dtype_code(q), _stream(stream))
+        ROTATE_INTERLEAVED if interleaved else 0, _dtype_code(q), _raw_stream(q, stream))
     _check(st, "gbla_qk_norm_rotate")
     return out[0], out[1]
 
@@ -484,28 +503,28 @@ def qk_norm_rotate_backward(q, k, norm_q, norm_k, rot, dqo, dko, positions=None,
     """Gradients of qk_norm_rotate (gbla_qk_norm_rotate_backward) for the contiguous
     gradients dqo, dko of its results: dq, dk (0 past seq_lens), dnorm_q, dnorm_k."""
     strides, dims = _rotate_args(q, k, norm_q, norm_k, rot, positions, seq_lens)
-    _plain(dqo, "dqo", q.shape, q.dtype, q.device)
-    _plain(dko, "dko", k.shape, q.dtype, q.device)
+    _plain(dqo, "dqo", q.shape, q.dtype, q)
+    _plain(dko, "dko", k.shape, q.dtype, q)
     g = dict(dq=torch.empty(q.shape, dtype=q.dtype, device=q.device),
              dk=torch.empty(k.shape, dtype=k.dtype, device=q.device),
              dnorm_q=torch.empty_like(norm_q), dnorm_k=torch.empty_like(norm_k))
-    st = load().gbla_qk_norm_rotate_backward(
+    st = (_lib or load()).gbla_qk_norm_rotate_backward(
         _ptr(q), _ptr(k), _ptr(norm_q), _ptr(norm_k), _ptr(rot), _ptr(positions),
         _ptr(seq_lens), strides, _ptr(dqo), _ptr(dko), _ptr(g["dq"]), _ptr(g["dk"]),
         _ptr(g["dnorm_q"]), _ptr(g["dnorm_k"]), *dims, float(eps),
-        ROTATE_INTERLEAVED if interleaved else 0, _dtype_code(q), _stream(stream))
+        ROTATE_INTERLEAVED if interleaved else 0, _dtype_code(q), _raw_stream(q, stream))
     _check(st, "gbla_qk_norm_rotate_backward")
     return g
 
 
 def _decay_args(q, k, v, log_decay, seq_lens, state):
-    sq, sk = _heads(q, "q"), _heads(k, "k", q)
-    sv = _heads(v, "v", q, k.shape[2])
-    B, N, H, D = q.shape
-    _plain(log_decay, "log_decay", (H,), torch.float32, q.device)
-    _plain(seq_lens, "seq_lens", (B,), torch.int32, q.device)
-    _plain(state, "state", (B, H, D, D), torch.float32, q.device)
-    return _strides(sq, sk, sv), (B, N, H, k.shape[2], D)
+    B, N, H, D = shape = _dims(q)
+    kshape = _key_shape(q, k)
+    whole = _heads(q, "q", shape, q) & _heads(k, "k", kshape, q) & _heads(v, "v", kshape, q)
+    _plain(log_decay, "log_decay", (H,), torch.float32, q)
+    _plain(seq_lens, "seq_lens", (B,), torch.int32, q)
+    _plain(state, "state", (B, H, D, D), torch.float32, q)
+    return None if whole else _strides(q, k, v), (B, N, H, kshape[2], D)
 
 
 def decay_attention(q, k, v, log_decay, seq_lens=None, state=None, scale=None, out=None,
@@ -519,12 +538,12 @@ def decay_attention(q, k, v, log_decay, seq_lens=None, state=None, scale=None, o
     B, N, H, Hk, D = dims
     if out is None:
         out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
-    _plain(out, "out", q.shape, q.dtype, q.device)
+    _plain(out, "out", q.shape, q.dtype, q)
     fin = torch.empty((B, H, D, D), dtype=torch.float32, device=q.device) if return_state else None
-    st = load().gbla_decay_attention(
+    st = (_lib or load()).gbla_decay_attention(
         _ptr(q), _ptr(k), _ptr(v), _ptr(log_decay), _ptr(seq_lens), strides, _ptr(state),
         _ptr(out), _ptr(fin), *dims, float(D ** -0.5 if scale is None else scale),
-        _dtype_code(q), int(algo), _stream(stream))
+        _dtype_code(q), int(algo), _raw_stream(q, stream))
     _check(st, "gbla_decay_attention")
     return (out, fin) if return_state else out
 
@@ -538,17 +557,17 @@ def decay_attention_backward(q, k, v, log_decay, do, seq_lens=None, state=None, 
     dstate, the gradient of the first state."""
     strides, dims = _decay_args(q, k, v, log_decay, seq_lens, state)
     B, N, H, Hk, D = dims
-    _plain(do, "do", q.shape, q.dtype, q.device)
-    _plain(dstate, "dstate", (B, H, D, D), torch.float32, q.device)
+    _plain(do, "do", q.shape, q.dtype, q)
+    _plain(dstate, "dstate", (B, H, D, D), torch.float32, q)
     g = {n: torch.empty(t.shape, dtype=q.dtype, device=q.device)
          for n, t in (("dq", q), ("dk", k), ("dv", v))}
     if return_dstate:
         g["dstate"] = torch.empty((B, H, D, D), dtype=torch.float32, device=q.device)
-    st = load().gbla_decay_attention_backward(
+    st = (_lib or load()).gbla_decay_attention_backward(
         _ptr(q), _ptr(k), _ptr(v), _ptr(log_decay), _ptr(seq_lens), strides, _ptr(state),
         _ptr(do), _ptr(dstate), _ptr(g["dq"]), _ptr(g["dk"]), _ptr(g["dv"]),
         _ptr(g.get("dstate")), *dims, float(D ** -0.5 if scale is None else scale),
-        _dtype_code(q), int(algo), _stream(stream))
+        _dtype_code(q), int(algo), _raw_stream(q, stream))
     _check(st, "gbla_decay_attention_backward")
     return g
 
@@ -558,20 +577,20 @@ def decay_attention_step(q, k, v, log_decay, state, slots=None, scale=None, out=
     """One token of each sequence (gbla_decay_attention_step): q [B, 1, H, D], k, v
     [B, 1, Hk, D]; `state` [n_slots, H, D, D] fp32 is updated in place at slots[b] (int32;
     None: slot b).  Rows whose slot is outside the pool are left alone.  Returns o."""
-    sq, sk = _heads(q, "q"), _heads(k, "k", q)
-    sv = _heads(v, "v", q, k.shape[2])
-    B, N, H, D = q.shape
+    B, N, H, D = shape = _dims(q)
+    kshape = _key_shape(q, k)
     if N != 1:
         raise ValueError("q, k and v hold one token of each sequence")
-    _plain(log_decay, "log_decay", (H,), torch.float32, q.device)
-    _plain(slots, "slots", (B,), torch.int32, q.device)
-    _plain(state, "state", (state.shape[0], H, D, D), torch.float32, q.device)
+    whole = _heads(q, "q", shape, q) & _heads(k, "k", kshape, q) & _heads(v, "v", kshape, q)
+    _plain(log_decay, "log_decay", (H,), torch.float32, q)
+    _plain(slots, "slots", (B,), torch.int32, q)
+    _plain(state, "state", (state.shape[0], H, D, D), torch.float32, q)
     if out is None:
         out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
-    _plain(out, "out", q.shape, q.dtype, q.device)
-    st = load().gbla_decay_attention_step(
-        _ptr(q), _ptr(k), _ptr(v), _ptr(log_decay), _ptr(slots), _strides(sq[:1], sk[:1], sv[:1]),
-        _ptr(state), _ptr(out), B, H, k.shape[2], D, state.shape[0],
-        float(D ** -0.5 if scale is None else scale), _dtype_code(q), _stream(stream))
+    _plain(out, "out", q.shape, q.dtype, q)
+    st = (_lib or load()).gbla_decay_attention_step(
+        _ptr(q), _ptr(k), _ptr(v), _ptr(log_decay), _ptr(slots),
+        None if whole else _strides(q, k, v, dims=1), _ptr(state), _ptr(out), B, H, kshape[2], D, state.shape[0],
+        float(D ** -0.5 if scale is None else scale), _dtype_code(q), _raw_stream(q, stream))
     _check(st, "gbla_decay_attention_step")
     return out

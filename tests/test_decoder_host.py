@@ -178,5 +178,9 @@ def test_binding_refuses_before_the_call():
         (step, dict(q=q)), (step, dict(state=s[:, :2])), (step, dict(slots=torch.zeros(2))),
         (step, dict(out=torch.zeros((2, 1, 4, 32)))),
     ]:
-        with pytest.raises(ValueError):
+        with pytest.raises(ValueError) as e:
             f(**a)
+        assert "CUDA device" not in str(e.value), (f, a)
+    for f in (rotate, decay, back, step):  # nothing else wrong: host tensors
+        with pytest.raises(ValueError, match="CUDA device"):
+            f()

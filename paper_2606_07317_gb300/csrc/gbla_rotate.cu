@@ -22,92 +22,109 @@ using namespace sm100;
 
 constexpr int kWarps = 8;
 constexpr int kThreads = kWarps * 32;
+constexpr int kBlocks = 2;  // resident blocks an SM
+constexpr int kBwdU = 2;    // groups of heads a warp of the backward keeps
 
+// 8 consecutive values of a head: as loaded, and as four pairs in fp32 (the
+// packed fp32 instructions halve what this kernel has to issue).
 template <typename T>
-struct Pack8;  // 8 consecutive values of a head as loaded
+struct Pack8;
 template <>
 struct Pack8<__nv_bfloat16> {
   uint4 u;
-  __device__ __forceinline__ void load(const __nv_bfloat16 *p) { u = ldg_nc_v4(p); }
-  __device__ __forceinline__ void get(float (&f)[8]) const {
-    const uint32_t w[4] = {u.x, u.y, u.z, u.w};
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const float2 v = bf2_to_f2(w[i]);
-      f[2 * i] = v.x;
-      f[2 * i + 1] = v.y;
-    }
+  __device__ __forceinline__ void load(uint32_t at) { u = lds_v4(at); }
+  __device__ __forceinline__ void get(float2 (&f)[4]) const {
+    f[0] = bf2_to_f2(u.x), f[1] = bf2_to_f2(u.y), f[2] = bf2_to_f2(u.z), f[3] = bf2_to_f2(u.w);
   }
-  __device__ __forceinline__ static void store(__nv_bfloat16 *p, const float (&f)[8]) {
-    *(uint4 *)p = make_uint4(f2_to_bf2(f[0], f[1]), f2_to_bf2(f[2], f[3]), f2_to_bf2(f[4], f[5]),
-                             f2_to_bf2(f[6], f[7]));
+  __device__ __forceinline__ static void store(__nv_bfloat16 *p, const float2 (&f)[4]) {
+    *(uint4 *)p = make_uint4(f2_to_bf2(f[0].x, f[0].y), f2_to_bf2(f[1].x, f[1].y),
+                             f2_to_bf2(f[2].x, f[2].y), f2_to_bf2(f[3].x, f[3].y));
   }
 };
 template <>
 struct Pack8<float> {
   uint4 a, b;
-  __device__ __forceinline__ void load(const float *p) {
-    a = ldg_nc_v4(p);
-    b = ldg_nc_v4(p + 4);
+  __device__ __forceinline__ void load(uint32_t at) {
+    a = lds_v4(at);
+    b = lds_v4(at + 512);
   }
-  __device__ __forceinline__ void get(float (&f)[8]) const {
-    const uint32_t w[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
-#pragma unroll
-    for (int i = 0; i < 8; ++i) f[i] = __uint_as_float(w[i]);
+  __device__ __forceinline__ void get(float2 (&f)[4]) const {
+    f[0] = make_float2(__uint_as_float(a.x), __uint_as_float(a.y));
+    f[1] = make_float2(__uint_as_float(a.z), __uint_as_float(a.w));
+    f[2] = make_float2(__uint_as_float(b.x), __uint_as_float(b.y));
+    f[3] = make_float2(__uint_as_float(b.z), __uint_as_float(b.w));
   }
-  __device__ __forceinline__ static void store(float *p, const float (&f)[8]) {
-    *(float4 *)p = make_float4(f[0], f[1], f[2], f[3]);
-    *(float4 *)(p + 4) = make_float4(f[4], f[5], f[6], f[7]);
+  __device__ __forceinline__ static void store(float *p, const float2 (&f)[4]) {
+    *(float4 *)p = make_float4(f[0].x, f[0].y, f[1].x, f[1].y);
+    *(float4 *)(p + 4) = make_float4(f[2].x, f[2].y, f[3].x, f[3].y);
   }
 };
 
-__device__ __forceinline__ void load_f8(const float *p, float (&f)[8]) {
+__device__ __forceinline__ void load_f8(const float *p, float2 (&f)[4]) {
   const float4 a = __ldg((const float4 *)p), b = __ldg((const float4 *)p + 1);
-  f[0] = a.x, f[1] = a.y, f[2] = a.z, f[3] = a.w;
-  f[4] = b.x, f[5] = b.y, f[6] = b.z, f[7] = b.w;
+  f[0] = make_float2(a.x, a.y), f[1] = make_float2(a.z, a.w);
+  f[2] = make_float2(b.x, b.y), f[3] = make_float2(b.z, b.w);
+}
+__device__ __forceinline__ void load_s8(uint32_t at, float2 (&f)[4]) {
+  const uint4 a = lds_v4(at), b = lds_v4(at + 16);
+  f[0] = make_float2(__uint_as_float(a.x), __uint_as_float(a.y));
+  f[1] = make_float2(__uint_as_float(a.z), __uint_as_float(a.w));
+  f[2] = make_float2(__uint_as_float(b.x), __uint_as_float(b.y));
+  f[3] = make_float2(__uint_as_float(b.z), __uint_as_float(b.w));
+}
+__device__ __forceinline__ float2 both(float v) { return make_float2(v, v); }
+// 1 / sqrt(v) within 2^-22 (v a mean of squares plus eps)
+__device__ __forceinline__ float rsqrt_approx(float v) {
+  float r;
+  asm("rsqrt.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(v));
+  return r;
 }
 
 // The lane's cosines and sines of one token.  Half-split pairs: value e of the
 // first half turns with partner e + R/2, so out = y cos + y_partner sin with
 // the sine negated in the first half.  Neighbouring pairs (2i, 2i + 1): four
-// cosines and four sines.  Lanes past R get cos = 1, sin = 0.
-template <bool kNext>
+// cosines and four sines.  Lanes past R get cos = 1, sin = 0.  kDir = -1 turns
+// by the opposite angles.
+template <bool kNext, int kDir>
 struct Turn {
-  float c[kNext ? 4 : 8], s[kNext ? 4 : 8];
-  __device__ __forceinline__ void load(const float *row, int e0, int R) {
+  float2 c[kNext ? 2 : 4], s[kNext ? 2 : 4];
+  __device__ __forceinline__ void load(uint32_t row, int e0, int R) {
+    constexpr int n = kNext ? 2 : 4;
     if (e0 >= R) {
 #pragma unroll
-      for (int i = 0; i < (kNext ? 4 : 8); ++i) c[i] = 1.f, s[i] = 0.f;
+      for (int i = 0; i < n; ++i) c[i] = both(1.f), s[i] = both(0.f);
       return;
     }
-    if (kNext) {
-      const float4 a = __ldg((const float4 *)(row + e0 / 2));
-      const float4 b = __ldg((const float4 *)(row + R / 2 + e0 / 2));
-      c[0] = a.x, c[1] = a.y, c[2] = a.z, c[3] = a.w;
-      s[0] = b.x, s[1] = b.y, s[2] = b.z, s[3] = b.w;
+    if constexpr (kNext) {
+      const uint4 a = lds_v4(row + 2 * e0), b = lds_v4(row + 2 * R + 2 * e0);
+      c[0] = make_float2(__uint_as_float(a.x), __uint_as_float(a.y));
+      c[1] = make_float2(__uint_as_float(a.z), __uint_as_float(a.w));
+      const float2 d = both((float)kDir);
+      s[0] = __fmul2_rn(d, make_float2(__uint_as_float(b.x), __uint_as_float(b.y)));
+      s[1] = __fmul2_rn(d, make_float2(__uint_as_float(b.z), __uint_as_float(b.w)));
     } else {
       const int half = R / 2, i0 = e0 < half ? e0 : e0 - half;
-      float a[8], b[8];
-      load_f8(row + i0, a);
-      load_f8(row + half + i0, b);
+      load_s8(row + 4 * i0, c);
+      load_s8(row + 4 * (half + i0), s);
+      const float sign = e0 < half ? -(float)kDir : (float)kDir;
 #pragma unroll
-      for (int i = 0; i < 8; ++i) c[i] = a[i], s[i] = e0 < half ? -b[i] : b[i];
+      for (int i = 0; i < n; ++i) s[i] = __fmul2_rn(s[i], both(sign));
     }
   }
-  // dir = 1 turns by the angles, -1 by the opposite ones
-  __device__ __forceinline__ void apply(float (&y)[8], int partner, float dir) const {
-    if (kNext) {
+  __device__ __forceinline__ void apply(float2 (&y)[4], int partner) const {
+    if constexpr (kNext) {
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        const float a = y[2 * i], b = y[2 * i + 1], sd = s[i] * dir;
-        y[2 * i] = a * c[i] - b * sd;
-        y[2 * i + 1] = a * sd + b * c[i];
+        const float cc = i & 1 ? c[i / 2].y : c[i / 2].x, ss = i & 1 ? s[i / 2].y : s[i / 2].x;
+        const float2 t = __fmul2_rn(make_float2(-y[i].y, y[i].x), both(ss));
+        y[i] = __ffma2_rn(y[i], both(cc), t);
       }
     } else {
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        const float o = __shfl_sync(0xffffffffu, y[i], partner);
-        y[i] = fmaf(y[i], c[i], o * (s[i] * dir));
+      for (int i = 0; i < 4; ++i) {
+        const float2 o = make_float2(__shfl_sync(0xffffffffu, y[i].x, partner),
+                                     __shfl_sync(0xffffffffu, y[i].y, partner));
+        y[i] = __ffma2_rn(y[i], c[i], __fmul2_rn(o, s[i]));
       }
     }
   }
@@ -134,151 +151,219 @@ struct RotParams {
 
 // Walks over tokens first, first + step, ... as (b, t) without a division each.
 struct Walk {
-  long long b, db;
+  long long tok, step, b, db;
   int t, dt, N;
-  __device__ __forceinline__ Walk(long long first, long long step, int n) : N(n) {
+  __device__ __forceinline__ Walk(long long first, long long stride, int n)
+      : tok(first), step(stride), N(n) {
     b = first / n, t = (int)(first % n);
     db = step / n, dt = (int)(step % n);
   }
   __device__ __forceinline__ void next() {
+    tok += step;
     b += db, t += dt;
     if (t >= N) t -= N, ++b;
   }
+  __device__ __forceinline__ bool live(const RotParams &p) const {
+    return tok < p.tokens && !(p.seq_lens && t >= __ldg(p.seq_lens + b));
+  }
+  __device__ __forceinline__ int position(const RotParams &p) const {
+    if (tok >= p.tokens) return 0;
+    const int pos = p.positions ? __ldg(p.positions + b * p.N + t) : t;
+    return min(max(pos, 0), p.P - 1);
+  }
 };
 
-__device__ __forceinline__ const float *rot_row(const RotParams &p, long long b, int t) {
-  int pos = p.positions ? __ldg(p.positions + b * p.N + t) : t;
-  pos = min(max(pos, 0), p.P - 1);
-  return p.rot + (long long)pos * p.R;
-}
+// A lane's share of a token: its piece of each of kU groups of heads, at a
+// distance of off[u] values from the token's first q or k value.
+template <int D, int kU>
+struct Lane {
+  int off[kU], e0, partner;
+  bool is_q[kU], on[kU];
+  float2 w[kU][4];
+  __device__ __forceinline__ Lane(const RotParams &p) {
+    constexpr int kLanes = D / 8, kHeads = 32 / kLanes;
+    const int lane = threadIdx.x & 31, hop = p.R / 16;
+    e0 = (lane % kLanes) * 8;
+    partner = e0 >= p.R ? lane : (e0 < p.R / 2 ? lane + hop : lane - hop);
+#pragma unroll
+    for (int u = 0; u < kU; ++u) {
+      const int head = (blockIdx.y * kU + u) * kHeads + lane / kLanes;
+      is_q[u] = head < p.H, on[u] = head < p.H + p.Hk;
+      off[u] = (is_q[u] ? head : head - p.H) * D + e0;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) w[u][i] = both(0.f);
+      if (on[u]) load_f8((is_q[u] ? p.wq : p.wk) + off[u], w[u]);
+    }
+  }
+};
+
+// A warp's ring of tokens on their way in, in shared memory (cp.async): kIn
+// tensors' pieces and the row of the table.  Two tokens (fp32: one) are out while
+// one is computed, which the registers could not hold.
+template <typename T, int D, int kU, int kIn>
+struct Ring {
+  static constexpr int kStages = sizeof(T) == 2 ? 3 : 2;
+  static constexpr int kPiece = 8 * (int)sizeof(T);  // bytes a lane
+  static constexpr int kRow = kIn * kU * 32 * kPiece, kBytes = kRow + 512;
+  static constexpr int kSmem = kWarps * kStages * kBytes;
+  uint32_t base;
+  Walk ahead;
+  int pos;  // of the next token to send for
+  __device__ __forceinline__ Ring(const RotParams &p, uint32_t smem, long long first, long long step)
+      : base(smem + (threadIdx.x >> 5) * kStages * kBytes), ahead(first, step, p.N) {
+    pos = ahead.position(p);
+  }
+  __device__ __forceinline__ uint32_t piece(int stage, int in, int u) const {
+    return base + stage * kBytes + (in * kU + u) * 32 * kPiece + (threadIdx.x & 31) * 16;
+  }
+  __device__ __forceinline__ uint32_t row(int stage) const { return base + stage * kBytes + kRow; }
+  __device__ __forceinline__ void copy(uint32_t to, const T *from) {
+    cp_async_16(to, from);
+    if (sizeof(T) == 4) cp_async_16(to + 512, from + 4);
+  }
+  // Sends for the next token; one copy group whether it is valid or not.
+  __device__ __forceinline__ void send(const RotParams &p, const Lane<D, kU> &ln, int stage) {
+    const bool live = ahead.live(p);
+    const int at = pos;
+    const long long tok = ahead.tok, b = ahead.b;
+    const int t = ahead.t;
+    ahead.next();
+    pos = ahead.position(p);
+    if (live) {
+      const T *q = (const T *)p.q + b * p.sqb + t * p.sqt, *k = (const T *)p.k + b * p.skb + t * p.skt;
+      const T *gq = (const T *)p.dqo + tok * p.H * D, *gk = (const T *)p.dko + tok * p.Hk * D;
+#pragma unroll
+      for (int u = 0; u < kU; ++u)
+        if (ln.on[u]) {
+          copy(piece(stage, 0, u), (ln.is_q[u] ? q : k) + ln.off[u]);
+          if (kIn == 2) copy(piece(stage, 1, u), (ln.is_q[u] ? gq : gk) + ln.off[u]);
+        }
+      const int lane = threadIdx.x & 31;
+      if (4 * lane < p.R) cp_async_16(row(stage) + 16 * lane, p.rot + (long long)at * p.R + 4 * lane);
+    }
+    cp_async_commit();
+  }
+  // Waits for the oldest token in flight, for every lane's copies of it.
+  __device__ __forceinline__ void arrive() {
+    asm volatile("cp.async.wait_group %0;" ::"n"(kStages - 2) : "memory");
+    __syncwarp();
+  }
+};
 
 // Grid (slabs, head blocks); block y serves the heads of its kU groups.
 template <typename T, int D, int kU, bool kNext>
-__global__ void __launch_bounds__(kThreads) rotate_kernel(const RotParams p) {
-  constexpr int kLanes = D / 8, kHeads = 32 / kLanes;
+__global__ void __launch_bounds__(kThreads, kBlocks) rotate_kernel(const RotParams p) {
+  using R = Ring<T, D, kU, 1>;
+  extern __shared__ __align__(16) uint8_t smem[];
   grid_dep_wait();
   grid_dep_launch();
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const int sub = lane / kLanes, e0 = (lane % kLanes) * 8, HT = p.H + p.Hk;
-  int head[kU];
-  float w[kU][8] = {};
-#pragma unroll
-  for (int u = 0; u < kU; ++u) {
-    head[u] = (blockIdx.y * kU + u) * kHeads + sub;
-    if (head[u] < HT)
-      load_f8((head[u] < p.H ? p.wq + (size_t)head[u] * D : p.wk + (size_t)(head[u] - p.H) * D) +
-                  e0,
-              w[u]);
-  }
-  const int hop = p.R / 16;
-  const int partner = e0 >= p.R ? lane : (e0 < p.R / 2 ? lane + hop : lane - hop);
+  const Lane<D, kU> ln(p);
+  const long long first = (long long)blockIdx.x * kWarps + (threadIdx.x >> 5);
   const long long step = (long long)gridDim.x * kWarps;
-  Walk at((long long)blockIdx.x * kWarps + warp, step, p.N);
-  for (long long tok = (long long)blockIdx.x * kWarps + warp; tok < p.tokens;
-       tok += step, at.next()) {
-    if (p.seq_lens && at.t >= __ldg(p.seq_lens + at.b)) continue;
-    Pack8<T> in[kU];
+  R ring(p, smem_u32(smem), first, step);
 #pragma unroll
-    for (int u = 0; u < kU; ++u)
-      if (head[u] < HT)
-        in[u].load(head[u] < p.H
-                       ? (const T *)p.q + at.b * p.sqb + at.t * p.sqt + (long long)head[u] * D + e0
-                       : (const T *)p.k + at.b * p.skb + at.t * p.skt +
-                             (long long)(head[u] - p.H) * D + e0);
-    Turn<kNext> turn;
-    turn.load(p.R ? rot_row(p, at.b, at.t) : nullptr, e0, p.R);
+  for (int i = 0; i < R::kStages - 1; ++i) ring.send(p, ln, i);
+  int stage = 0;
+  for (Walk at(first, step, p.N); at.tok < p.tokens; at.next()) {
+    ring.arrive();
+    ring.send(p, ln, stage == 0 ? R::kStages - 1 : stage - 1);
+    if (at.live(p)) {  // the same for the whole warp
+      Turn<kNext, 1> turn;
+      turn.load(ring.row(stage), ln.e0, p.R);
+      T *qo = (T *)p.qo + at.tok * p.H * D, *ko = (T *)p.ko + at.tok * p.Hk * D;
 #pragma unroll
-    for (int u = 0; u < kU; ++u) {
-      float x[8] = {};
-      if (head[u] < HT) in[u].get(x);
-      float ss = 0.f;
+      for (int u = 0; u < kU; ++u) {
+        Pack8<T> in;
+        in.load(ring.piece(stage, 0, u));
+        float2 x[4];
+        in.get(x);
+        float2 sq = __fmul2_rn(x[0], x[0]);
 #pragma unroll
-      for (int i = 0; i < 8; ++i) ss = fmaf(x[i], x[i], ss);
-      const float r = rsqrtf(head_sum<kLanes>(ss) * (1.f / D) + p.eps);
+        for (int i = 1; i < 4; ++i) sq = __ffma2_rn(x[i], x[i], sq);
+        const float r = rsqrt_approx(fmaf(head_sum<D / 8>(sq.x + sq.y), 1.f / D, p.eps));
 #pragma unroll
-      for (int i = 0; i < 8; ++i) x[i] = x[i] * r * w[u][i];
-      turn.apply(x, partner, 1.f);
-      if (head[u] < HT) {
-        T *o = head[u] < p.H ? (T *)p.qo + (tok * p.H + head[u]) * D + e0
-                             : (T *)p.ko + (tok * p.Hk + (head[u] - p.H)) * D + e0;
-        Pack8<T>::store(o, x);
+        for (int i = 0; i < 4; ++i) x[i] = __fmul2_rn(__fmul2_rn(x[i], ln.w[u][i]), both(r));
+        turn.apply(x, ln.partner);
+        if (ln.on[u]) Pack8<T>::store((ln.is_q[u] ? qo : ko) + ln.off[u], x);
       }
     }
+    stage = stage == R::kStages - 1 ? 0 : stage + 1;
   }
 }
 
 template <typename T, int D, int kU, bool kNext>
-__global__ void __launch_bounds__(kThreads) rotate_bwd_kernel(const RotParams p) {
+__global__ void __launch_bounds__(kThreads, kBlocks) rotate_bwd_kernel(const RotParams p) {
+  using R = Ring<T, D, kU, 2>;
   constexpr int kLanes = D / 8, kHeads = 32 / kLanes;
-  __shared__ float red[kWarps][kU][32][9];
+  extern __shared__ __align__(16) uint8_t smem[];
   grid_dep_wait();
   grid_dep_launch();
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const int sub = lane / kLanes, e0 = (lane % kLanes) * 8, HT = p.H + p.Hk;
-  int head[kU];
-  float w[kU][8] = {}, dw[kU][8] = {};
-#pragma unroll
-  for (int u = 0; u < kU; ++u) {
-    head[u] = (blockIdx.y * kU + u) * kHeads + sub;
-    if (head[u] < HT)
-      load_f8((head[u] < p.H ? p.wq + (size_t)head[u] * D : p.wk + (size_t)(head[u] - p.H) * D) +
-                  e0,
-              w[u]);
-  }
-  const int hop = p.R / 16;
-  const int partner = e0 >= p.R ? lane : (e0 < p.R / 2 ? lane + hop : lane - hop);
-  const long long step = (long long)gridDim.x * kWarps;
-  Walk at((long long)blockIdx.x * kWarps + warp, step, p.N);
-  for (long long tok = (long long)blockIdx.x * kWarps + warp; tok < p.tokens;
-       tok += step, at.next()) {
-    const bool live = !(p.seq_lens && at.t >= __ldg(p.seq_lens + at.b));
-    Pack8<T> in[kU], gin[kU];
-    if (live) {
-#pragma unroll
-      for (int u = 0; u < kU; ++u)
-        if (head[u] < HT) {
-          const bool isq = head[u] < p.H;
-          const int hk = head[u] - p.H;
-          in[u].load(isq ? (const T *)p.q + at.b * p.sqb + at.t * p.sqt + (long long)head[u] * D + e0
-                         : (const T *)p.k + at.b * p.skb + at.t * p.skt + (long long)hk * D + e0);
-          gin[u].load(isq ? (const T *)p.dqo + (tok * p.H + head[u]) * D + e0
-                          : (const T *)p.dko + (tok * p.Hk + hk) * D + e0);
-        }
-    }
-    Turn<kNext> turn;
-    if (live) turn.load(p.R ? rot_row(p, at.b, at.t) : nullptr, e0, p.R);
-#pragma unroll
-    for (int u = 0; u < kU; ++u) {
-      float dx[8] = {};
-      if (live) {  // the same for the whole warp
-        float x[8] = {}, g[8] = {};
-        if (head[u] < HT) in[u].get(x), gin[u].get(g);
-        turn.apply(g, partner, -1.f);
-        float ss = 0.f, dot = 0.f;
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          ss = fmaf(x[i], x[i], ss);
-          dot = fmaf(g[i] * w[u][i], x[i], dot);
-        }
-        const float r = rsqrtf(head_sum<kLanes>(ss) * (1.f / D) + p.eps);
-        const float m = head_sum<kLanes>(dot) * (1.f / D) * r * r;  // mean(u n) r
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          dw[u][i] = fmaf(g[i], x[i] * r, dw[u][i]);
-          dx[i] = r * (g[i] * w[u][i] - x[i] * m);
-        }
-      }
-      if (head[u] < HT) {  // rows past the end get zeros
-        T *o = head[u] < p.H ? (T *)p.qo + (tok * p.H + head[u]) * D + e0
-                             : (T *)p.ko + (tok * p.Hk + (head[u] - p.H)) * D + e0;
-        Pack8<T>::store(o, dx);
-      }
-    }
-  }
+  const Lane<D, kU> ln(p);
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, HT = p.H + p.Hk;
+  float2 dw[kU][4];
 #pragma unroll
   for (int u = 0; u < kU; ++u)
 #pragma unroll
-    for (int i = 0; i < 8; ++i) red[warp][u][lane][i] = dw[u][i];
+    for (int i = 0; i < 4; ++i) dw[u][i] = both(0.f);
+  const long long first = (long long)blockIdx.x * kWarps + warp;
+  const long long step = (long long)gridDim.x * kWarps;
+  R ring(p, smem_u32(smem), first, step);
+#pragma unroll
+  for (int i = 0; i < R::kStages - 1; ++i) ring.send(p, ln, i);
+  int stage = 0;
+  for (Walk at(first, step, p.N); at.tok < p.tokens; at.next()) {
+    ring.arrive();
+    ring.send(p, ln, stage == 0 ? R::kStages - 1 : stage - 1);
+    T *dq = (T *)p.qo + at.tok * p.H * D, *dk = (T *)p.ko + at.tok * p.Hk * D;
+    if (at.live(p)) {  // the same for the whole warp
+      Turn<kNext, -1> turn;
+      turn.load(ring.row(stage), ln.e0, p.R);
+#pragma unroll
+      for (int u = 0; u < kU; ++u) {
+        Pack8<T> in, gin;
+        in.load(ring.piece(stage, 0, u));
+        gin.load(ring.piece(stage, 1, u));
+        float2 x[4], g[4];
+        in.get(x);
+        gin.get(g);
+        turn.apply(g, ln.partner);
+        float2 sq = __fmul2_rn(x[0], x[0]);
+        float2 gx[4], dot = both(0.f);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          if (i) sq = __ffma2_rn(x[i], x[i], sq);
+          gx[i] = __fmul2_rn(g[i], x[i]);
+          dot = __ffma2_rn(gx[i], ln.w[u][i], dot);
+        }
+        const float r = rsqrt_approx(fmaf(head_sum<kLanes>(sq.x + sq.y), 1.f / D, p.eps));
+        // dx = r u - x r^3 mean(u x)
+        const float m = head_sum<kLanes>(dot.x + dot.y) * (-1.f / D) * r * r * r;
+        float2 dx[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          if (ln.on[u]) dw[u][i] = __ffma2_rn(gx[i], both(r), dw[u][i]);
+          dx[i] = __ffma2_rn(x[i], both(m), __fmul2_rn(__fmul2_rn(g[i], ln.w[u][i]), both(r)));
+        }
+        if (ln.on[u]) Pack8<T>::store((ln.is_q[u] ? dq : dk) + ln.off[u], dx);
+      }
+    } else {  // past the end: zeros
+      const float2 zero[4] = {both(0.f), both(0.f), both(0.f), both(0.f)};
+#pragma unroll
+      for (int u = 0; u < kU; ++u)
+        if (ln.on[u]) Pack8<T>::store((ln.is_q[u] ? dq : dk) + ln.off[u], zero);
+    }
+    stage = stage == R::kStages - 1 ? 0 : stage + 1;
+  }
+  // the block's sums of dw, through the ring's memory
+  float(*red)[kU][32][9] = (float(*)[kU][32][9])smem;
+  static_assert(sizeof(float) * kWarps * kU * 32 * 9 <= R::kSmem, "sums fit the ring");
+  cp_async_wait_all();
+  __syncthreads();
+#pragma unroll
+  for (int u = 0; u < kU; ++u)
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      red[warp][u][lane][2 * i] = dw[u][i].x, red[warp][u][lane][2 * i + 1] = dw[u][i].y;
   __syncthreads();
   for (int e = threadIdx.x; e < kU * 256; e += kThreads) {
     const int u = e >> 8, l = (e >> 3) & 31, i = e & 7;
@@ -333,27 +418,31 @@ int slab_count(long long tokens, int head_blocks, int per_sm) {
   return (int)(want < most ? want : most);
 }
 
-constexpr int kPerSm = 4;
-
 template <typename T, int D, int kU>
 cudaError_t launch_fwd(const RotParams &p, bool next, cudaStream_t st) {
   const int groups = (p.H + p.Hk + 256 / D - 1) / (256 / D), blocks = (groups + kU - 1) / kU;
-  const dim3 grid(slab_count(p.tokens, blocks, kPerSm), blocks);
+  const dim3 grid(slab_count(p.tokens, blocks, kBlocks), blocks);
+  const auto kernel = next ? rotate_kernel<T, D, kU, true> : rotate_kernel<T, D, kU, false>;
+  constexpr int smem = Ring<T, D, kU, 1>::kSmem;
+  const cudaError_t e =
+      cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+  if (e != cudaSuccess) return e;
   count_launch();
-  return next ? launch_pdl(rotate_kernel<T, D, kU, true>, grid, dim3(kThreads), 0, st, p)
-              : launch_pdl(rotate_kernel<T, D, kU, false>, grid, dim3(kThreads), 0, st, p);
+  return launch_pdl(kernel, grid, dim3(kThreads), smem, st, p);
 }
 
 template <typename T, int D>
 cudaError_t fwd_d(const RotParams &p, bool next, cudaStream_t st) {
   const int groups = (p.H + p.Hk + 256 / D - 1) / (256 / D);
-  // Few tokens: one group of heads a warp, so that all loads go out at once.
-  if (p.tokens * ((groups + 3) / 4) < (long long)sm_count() * kWarps)
+  // Groups of heads a warp: one where there are too few tokens for the warps, so
+  // that all loads go out at once; four in bf16 (one row of the table for 4
+  // groups; B4 H8 N8192 D64: 23.1 us, with two 26.5), two in fp32 (46.8 and 44.5)
+  // or where there are no more.
+  if (p.tokens * groups < (long long)sm_count() * kBlocks * kWarps)
     return launch_fwd<T, D, 1>(p, next, st);
+  if (sizeof(T) == 4 || groups <= 2) return launch_fwd<T, D, 2>(p, next, st);
   return launch_fwd<T, D, 4>(p, next, st);
 }
-
-constexpr int kBwdU = 2, kBwdPerSm = 2;
 
 template <int D>
 int bwd_blocks(const RotParams &p) {
@@ -362,13 +451,14 @@ int bwd_blocks(const RotParams &p) {
 
 template <typename T, int D>
 cudaError_t bwd_d(const RotParams &p, bool next, float *dwq, float *dwk, cudaStream_t st) {
-  const int blocks = bwd_blocks<D>(p), slabs = slab_count(p.tokens, blocks, kBwdPerSm);
+  const int blocks = bwd_blocks<D>(p), slabs = slab_count(p.tokens, blocks, kBlocks);
   const dim3 grid(slabs, blocks);
-  count_launch(2);
-  cudaError_t e =
-      next ? launch_pdl(rotate_bwd_kernel<T, D, kBwdU, true>, grid, dim3(kThreads), 0, st, p)
-           : launch_pdl(rotate_bwd_kernel<T, D, kBwdU, false>, grid, dim3(kThreads), 0, st, p);
+  const auto kernel = next ? rotate_bwd_kernel<T, D, kBwdU, true> : rotate_bwd_kernel<T, D, kBwdU, false>;
+  constexpr int smem = Ring<T, D, kBwdU, 2>::kSmem;
+  cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
   if (e != cudaSuccess) return e;
+  count_launch(2);
+  if ((e = launch_pdl(kernel, grid, dim3(kThreads), smem, st, p)) != cudaSuccess) return e;
   const int cols = (p.H + p.Hk) * D;
   return launch_pdl(rotate_dw_kernel, dim3(cols / 32), dim3(256), 0, st, (const float *)p.part,
                     slabs, cols, p.H * D, dwq, dwk);
@@ -404,7 +494,7 @@ cudaError_t rotate_forward(const RotateArgs &a, cudaStream_t st) {
 size_t rotate_backward_floats(const RotateArgs &a) {
   const RotParams p = rot_params(a);
   const int blocks = a.D == 32 ? bwd_blocks<32>(p) : a.D == 64 ? bwd_blocks<64>(p) : bwd_blocks<128>(p);
-  return (size_t)slab_count(p.tokens, blocks, kBwdPerSm) * (a.H + a.Hk) * a.D;
+  return (size_t)slab_count(p.tokens, blocks, kBlocks) * (a.H + a.Hk) * a.D;
 }
 
 cudaError_t rotate_backward(const RotateArgs &a, float *part, float *dnorm_q, float *dnorm_k,

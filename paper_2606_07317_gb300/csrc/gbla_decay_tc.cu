@@ -1,4 +1,4 @@
-// Decayed linear attention on tensor cores (tcgen05 + TMA): bf16, D in {64, 128}.
+// Decayed linear attention on tensor cores (tcgen05 + TMA): bf16, every D.
 //
 // The scan of ScanArgs in chunks of C = 64 tokens, in scan order.  With r, j the
 // places in a chunk, S the state before it and gamma the head's decay,
@@ -519,8 +519,9 @@ __global__ void __launch_bounds__(OwnShape<D, kTerms>::kThreads, OwnShape<D, kTe
 }
 
 // ---------------------------------------------------------------------------
-// The scan of each segment.
-template <int D, int kTerms, typename O>
+// The scan of each segment.  V: the heads' size in memory (32 runs as D = 64 with
+// the missing channels loaded as zeros).
+template <int D, int V, int kTerms, typename O>
 __global__ void __launch_bounds__(Shape<D, kTerms>::kThreads, 1)
     decay_kernel(const TcParams p, const __grid_constant__ CUtensorMap tm_x,
                  const __grid_constant__ CUtensorMap tm_y,
@@ -546,19 +547,19 @@ __global__ void __launch_bounds__(Shape<D, kTerms>::kThreads, 1)
   const int rank = blockIdx.x;
   const Segment sg(p, b, rank);
   const int L = sg.L, q0 = sg.q0, cnt = sg.cnt;
-  const size_t bh = (size_t)b * p.H + h, orow = (size_t)p.H * D;
-  O *out = (O *)p.out + ((size_t)b * p.N * p.H + h) * D;  // token t at t * orow
+  const size_t bh = (size_t)b * p.H + h, orow = (size_t)p.H * V;
+  O *out = (O *)p.out + ((size_t)b * p.N * p.H + h) * V;  // token t at t * orow
 
   if (p.zero_pad) {  // the rows past the end, shared among the sequence's CTAs
-    constexpr int kPer = D * (int)sizeof(O) / 16;
+    constexpr int kPer = V * (int)sizeof(O) / 16;
     for (long long i = (long long)rank * Sh::kThreads + tid; i < (long long)(p.N - L) * kPer;
          i += (long long)p.ranks * Sh::kThreads)
       ((uint4 *)(out + (L + i / kPer) * orow))[i % kPer] = make_uint4(0, 0, 0, 0);
   }
   if (cnt == 0) {
     if (rank == 0 && p.fin)  // an empty sequence passes its state on
-      for (int i = tid; i < D * D; i += Sh::kThreads)
-        p.fin[bh * D * D + i] = p.init ? p.init[bh * D * D + i] * p.init_scale * p.fin_scale : 0.f;
+      for (int i = tid; i < V * V; i += Sh::kThreads)
+        p.fin[bh * V * V + i] = p.init ? p.init[bh * V * V + i] * p.init_scale * p.fin_scale : 0.f;
     return;
   }
   const float l2 = __ldg(p.log_decay + h) * 1.4426950408889634f;
@@ -800,12 +801,13 @@ __global__ void __launch_bounds__(Shape<D, kTerms>::kThreads, 1)
       // token, which that state belongs to)
       const float n = !p.reverse ? (float)q0 * kC : q0 == 0 ? 0.f : (float)(L - 1 - (sg.nc - q0) * kC);
       const float f = decay_pow(l2, n) * p.init_scale;
-      const float *s0 = p.init + bh * D * D;
+      const float *s0 = p.init + bh * V * V;
 #pragma unroll
       for (int i = 0; i < kNV; ++i) {
         int e;
         const int d = state_at<D>(sw, lane, i, &e);
-        S[i] = fmaf(f, __ldg(s0 + (p.init_t ? e * D + d : d * D + e)), S[i]);
+        if (V == D || (d < V && e < V))
+          S[i] = fmaf(f, __ldg(s0 + (p.init_t ? e * V + d : d * V + e)), S[i]);
       }
     }
     for (int j = 0; j < cnt; ++j) {
@@ -842,7 +844,7 @@ __global__ void __launch_bounds__(Shape<D, kTerms>::kThreads, 1)
       for (int i = 0; i < kNV; ++i) {
         int e;
         const int d = state_at<D>(sw, lane, i, &e);
-        p.fin[bh * D * D + d * D + e] = S[i] * f;
+        if (V == D || (d < V && e < V)) p.fin[bh * V * V + d * V + e] = S[i] * f;
       }
     }
   } else {
@@ -913,7 +915,7 @@ __global__ void __launch_bounds__(Shape<D, kTerms>::kThreads, 1)
           for (int k = 0; k < 8; ++k)
 #pragma unroll
             for (int q = 0; q < 2; ++q)
-              if (r0 + 8 * q < n)
+              if (r0 + 8 * q < n && (V == D || 8 * k < V))
                 *(float2 *)(dst + (size_t)(r0 + 8 * q) * orow + 8 * k + 2 * (lane & 3)) =
                     make_float2(a[4 * k + 2 * q], a[4 * k + 2 * q + 1]);
         } else {  // whole 128-byte rows through the warp's staging
@@ -924,7 +926,8 @@ __global__ void __launch_bounds__(Shape<D, kTerms>::kThreads, 1)
           for (int k = 0; k < 4; ++k) {
             const int r = (lane >> 3) + 4 * k;
             const uint4 v = lds_v4(stage + r * 128 + (((lane & 7) ^ (r & 7)) << 4));
-            if (16 * ow + r < n) *(uint4 *)(dst + (size_t)(16 * ow + r) * orow + 8 * (lane & 7)) = v;
+            if (16 * ow + r < n && (V == D || 8 * (lane & 7) < V))
+              *(uint4 *)(dst + (size_t)(16 * ow + r) * orow + 8 * (lane & 7)) = v;
           }
         }
       }
@@ -1010,7 +1013,7 @@ int segment_for(const ScanArgs &a) {
   return best;
 }
 
-template <int D, int kTerms, typename O>
+template <int D, int V, int kTerms, typename O>
 cudaError_t launch(const ScanArgs &a, const TcParams &p, const CUtensorMap &tx,
                    const CUtensorMap &ty, const CUtensorMap &tz, cudaStream_t st) {
   cudaError_t e;
@@ -1025,7 +1028,7 @@ cudaError_t launch(const ScanArgs &a, const TcParams &p, const CUtensorMap &tx,
     if ((e = cudaGetLastError()) != cudaSuccess) return e;
   }
   using Sh = Shape<D, kTerms>;
-  const auto kernel = decay_kernel<D, kTerms, O>;
+  const auto kernel = decay_kernel<D, V, kTerms, O>;
   if ((e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, Sh::kSmem)) !=
       cudaSuccess)
     return e;
@@ -1038,20 +1041,20 @@ cudaError_t launch(const ScanArgs &a, const TcParams &p, const CUtensorMap &tx,
   return cudaGetLastError();
 }
 
-template <int D>
+template <int D, int V>
 cudaError_t launch_d(const ScanArgs &a, const TcParams &p, const CUtensorMap &tx,
                      const CUtensorMap &ty, const CUtensorMap &tz, cudaStream_t st) {
   if (a.fin)
-    return a.out_f32 ? launch<D, 3, float>(a, p, tx, ty, tz, st)
-                     : launch<D, 3, __nv_bfloat16>(a, p, tx, ty, tz, st);
-  return a.out_f32 ? launch<D, 2, float>(a, p, tx, ty, tz, st)
-                   : launch<D, 2, __nv_bfloat16>(a, p, tx, ty, tz, st);
+    return a.out_f32 ? launch<D, V, 3, float>(a, p, tx, ty, tz, st)
+                     : launch<D, V, 3, __nv_bfloat16>(a, p, tx, ty, tz, st);
+  return a.out_f32 ? launch<D, V, 2, float>(a, p, tx, ty, tz, st)
+                   : launch<D, V, 2, __nv_bfloat16>(a, p, tx, ty, tz, st);
 }
 
 }  // namespace
 
 bool tc_scan_supports(const ScanArgs &a) {
-  if (a.dtype != GBLA_BF16 || (a.D != 64 && a.D != 128)) return false;
+  if (a.dtype != GBLA_BF16) return false;
   for (const auto &s : {a.sx, a.sy, a.sz})  // the stride limit of a tensor map
     if (s[0] >= (1ll << 39) || s[1] >= (1ll << 39)) return false;
   int dev = 0, major = 0, minor = 0;
@@ -1063,7 +1066,8 @@ bool tc_scan_supports(const ScanArgs &a) {
 
 size_t tc_scan_floats(const ScanArgs &a) {
   const int seg = segment_for(a), ranks = ((a.N + kC - 1) / kC + seg - 1) / seg;
-  return ranks > 1 ? (size_t)a.B * a.H * ranks * a.D * a.D : 0;
+  const size_t d = a.D < 64 ? 64 : a.D;
+  return ranks > 1 ? (size_t)a.B * a.H * ranks * d * d : 0;
 }
 
 cudaError_t tc_scan(const ScanArgs &a, float *scratch, cudaStream_t st) {
@@ -1079,8 +1083,9 @@ cudaError_t tc_scan(const ScanArgs &a, float *scratch, cudaStream_t st) {
   p.N = a.N, p.H = a.H, p.gx = a.gx, p.gy = a.gy, p.gz = a.gz;
   p.zero_pad = a.zero_pad, p.init_t = a.init_t, p.reverse = a.reverse;
   p.seg = segment_for(a), p.ranks = ((a.N + kC - 1) / kC + p.seg - 1) / p.seg;
-  return a.D == 64 ? launch_d<64>(a, p, tx, ty, tz, st)
-                   : launch_d<128>(a, p, tx, ty, tz, st);
+  if (a.D == 32) return launch_d<64, 32>(a, p, tx, ty, tz, st);
+  return a.D == 64 ? launch_d<64, 64>(a, p, tx, ty, tz, st)
+                   : launch_d<128, 128>(a, p, tx, ty, tz, st);
 }
 
 unsigned decay_device_error(bool reset) {

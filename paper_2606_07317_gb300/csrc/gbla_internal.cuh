@@ -205,7 +205,7 @@ struct ScanArgs {
 // Scratch floats of a scan (partial states of the segments it is split into).
 size_t simt_scan_floats(const ScanArgs &a);
 cudaError_t simt_scan(const ScanArgs &a, float *scratch, cudaStream_t st);
-// The same on tensor cores (gbla_decay_tc.cu): bf16, D in {64, 128}, sm_103.
+// The same on tensor cores (gbla_decay_tc.cu): bf16, sm_103.
 bool tc_scan_supports(const ScanArgs &a);
 size_t tc_scan_floats(const ScanArgs &a);
 cudaError_t tc_scan(const ScanArgs &a, float *scratch, cudaStream_t st);

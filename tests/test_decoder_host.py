@@ -99,7 +99,6 @@ def test_scale(lib, op):
 def test_family(lib, op):
     assert _run(lib, op, algo=7) == UNS
     assert _run(lib, op, algo=gbla.ALGO_TC, dtype=gbla.GBLA_FP32) == UNS
-    assert _run(lib, op, algo=gbla.ALGO_TC, D=32) == UNS
 
 
 @pytest.mark.parametrize("op,outs", [

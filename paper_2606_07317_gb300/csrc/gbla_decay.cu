@@ -45,8 +45,20 @@ __device__ __forceinline__ void store4(__nv_bfloat16 *p, const float (&f)[4]) {
 }
 
 // ------------------------------------------------------------------ the scan
+// A block of 128 threads serves E = min(D, 64) of the state's columns of one
+// segment of one (batch, head).  All products run on packed fp32 FMAs:
+//   scores   4 rows by 2 columns a thread, even and odd d in the two halves,
+//   results  E / 16 rows by 4 columns; x S with even and odd d in the halves (the
+//            state transposed in shared memory), then the weighted scores, stored
+//            twice over, times z with two columns in the halves,
+//   state    rows in pairs, 4 columns, in registers for the whole segment.
+// Bound by the FMA pipe: 2 C D + 2 D^2 multiply-adds a token and head (C = 32
+// keeps the first term below the second without more tiles than fit).  Blocks of
+// 128 threads with large register tiles rather than 256 with small ones: a
+// product of 2 x 4 results a thread spends more on shared-memory reads than on
+// FMAs.  Tiles of the next chunk come in by cp.async where two fit (D <= 64).
 constexpr int kC = 32;        // tokens per chunk
-constexpr int kThreads = 256;
+constexpr int kThreads = 128;
 
 struct ScanDev {
   const void *x, *y, *z;
@@ -64,230 +76,301 @@ struct ScanDev {
 
 template <int D>
 struct ScanShape {
-  static constexpr int kRow = D + 4;                  // padded row of a tile, in floats
-  static constexpr int kTile = kC * kRow;
-  static constexpr int kSmemFloats = 3 * kTile + kC * (kC + 4) + D * kRow + kC + 1;
-  // the state in registers: a kS x kS tile a thread (4 x 4 at D = 64)
-  static constexpr int kSt = D / 16;
-  // outputs: 4 columns and kOr rows a thread
-  static constexpr int kOc = D / 4, kOrows = kThreads / kOc, kOr = kC / kOrows;
+  static constexpr int kE = D < 64 ? D : 64, kSplit = D / kE;
+  static constexpr int kRow = D + 4, kZRow = kE + 4, kPRow = 2 * kC + 4;  // padded, in floats
+  static constexpr int kTile = kC * (2 * kRow + kZRow);  // x, y, z
+  static constexpr int kStages = D <= 64 ? 2 : 1;
+  static constexpr int kOffP = kStages * kTile, kOffS = kOffP + kC * kPRow,
+                       kOffG = kOffS + kE * D;
+  static constexpr int kSmemFloats = kOffG + kC + 1;
+  static constexpr int kTx = kE / 4, kTy = kThreads / kTx;
+  static constexpr int kOr = kC / kTy;   // result rows a thread
+  static constexpr int kSr = D / kTy;    // state rows a thread
 };
 
-// One segment of one (batch, head).  kState: only its own state (zero before
-// it) goes to `part`; else the results, from the state that the segments before
-// it in scan order leave.  The state lives in registers, D / 16 rows by D / 16
-// columns a thread (rows ty + 16 i, columns tx * (D / 16) + j), and is laid
-// out in shared memory for the product with x.
+// 16 bytes from global to shared memory, or zeros.
+__device__ __forceinline__ void cp_async_or_zero(uint32_t dst, const void *src, bool valid) {
+  const int n = valid ? 16 : 0;
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(n)
+               : "memory");
+}
+template <int kCols, int kRowFloats>
+__device__ __forceinline__ void load_tile(float *to, const float *from, long long stride, int n) {
+  for (int i = threadIdx.x; i < kC * kCols / 4; i += kThreads) {
+    const int r = i / (kCols / 4), c = i % (kCols / 4) * 4;
+    cp_async_or_zero(smem_u32(to + r * kRowFloats + c), from + (r < n ? r * stride + c : 0), r < n);
+  }
+}
+template <int kCols, int kRowFloats>
+__device__ __forceinline__ void load_tile(float *to, const __nv_bfloat16 *from, long long stride,
+                                          int n) {
+  for (int i = threadIdx.x; i < kC * kCols / 4; i += kThreads) {
+    const int r = i / (kCols / 4), c = i % (kCols / 4) * 4;
+    float f[4] = {};
+    if (r < n) load4(from + r * stride + c, f);
+    store4(to + r * kRowFloats + c, f);
+  }
+}
+__device__ __forceinline__ float2 both(float v) { return make_float2(v, v); }
+
+// kState: only the segment's own state (zero before it) goes to `part`; else the
+// results, from the state before the segment, which the prefix kernel leaves in
+// `part` (a single segment: the first state).
 template <typename T, typename O, int D, bool kState>
 __global__ void __launch_bounds__(kThreads) scan_kernel(const ScanDev p) {
   using Sh = ScanShape<D>;
-  constexpr int kRow = Sh::kRow, kSt = Sh::kSt, kOr = Sh::kOr;
+  constexpr int E = Sh::kE, kRow = Sh::kRow, kZRow = Sh::kZRow, kPRow = Sh::kPRow;
+  constexpr int kOr = Sh::kOr, kSr = Sh::kSr;
   extern __shared__ __align__(16) float sm[];
-  float *xs = sm, *ys = xs + Sh::kTile, *zs = ys + Sh::kTile;
-  float *ps = zs + Sh::kTile;          // [kC][kC + 4] weighted scores
-  float *ss = ps + kC * (kC + 4);      // [D][kRow] the state
-  float *gp = ss + D * kRow;           // gamma^0 .. gamma^kC
-  const int tid = threadIdx.x, tx = tid & 15, ty = tid >> 4;
-  const int seg = blockIdx.x, h = blockIdx.y;
-  const int b = blockIdx.z;
+  float *ps = sm + Sh::kOffP;  // [kC][kPRow] weighted scores, each twice
+  float *st = sm + Sh::kOffS;  // [E][D] the state transposed, 16-byte pieces swizzled
+  float *gp = sm + Sh::kOffG;  // gamma^0 .. gamma^kC
+  const int tid = threadIdx.x, tx = tid % Sh::kTx, ty = tid / Sh::kTx;
+  const int seg = blockIdx.x / Sh::kSplit, e0 = blockIdx.x % Sh::kSplit * E;
+  const int h = blockIdx.y, b = blockIdx.z;
   const int L = p.seq_lens ? min(max(p.seq_lens[b], 0), p.N) : p.N;
   const int ns = (L + p.seg - 1) / p.seg;
   const size_t bh = (size_t)b * p.H + h;
-  O *out = (O *)p.out + ((size_t)b * p.N * p.H + h) * D;  // row t at t * H * D
+  O *out = (O *)p.out + ((size_t)b * p.N * p.H + h) * D + e0;  // row t at t * H * D
   const size_t orow = (size_t)p.H * D;
   if (!kState && p.zero_pad) {  // this segment's share of the rows past the end
-    const int t1 = min(p.N, (seg + 1) * p.seg);
+    const int t0 = max(L, seg * p.seg), t1 = min(p.N, (seg + 1) * p.seg);
     const float z4[4] = {};
-    for (int i = tid; i < (t1 - max(L, seg * p.seg)) * (D / 4); i += kThreads)
-      store4(out + (max(L, seg * p.seg) + i / (D / 4)) * orow + i % (D / 4) * 4, z4);
+    for (int i = tid; i < (t1 - t0) * (E / 4); i += kThreads)
+      store4(out + (size_t)(t0 + i / (E / 4)) * orow + i % (E / 4) * 4, z4);
   }
   // the last segment in scan order also writes the final state; an empty
   // sequence has none, so segment 0 passes the first state on
   const int last = p.reverse ? 0 : (ns > 0 ? ns - 1 : 0);
   if (seg >= ns && !(seg == 0 && !kState && p.fin)) return;
-  if (kState && seg == (p.reverse ? 0 : ns - 1)) return;  // nobody reads it
+  if (kState && seg == last) return;  // nobody reads it
   const float l2 = log2_decay(p.log_decay, h);
   if (tid <= kC) gp[tid] = decay_pow(l2, (float)tid);
 
-  float S[kSt][kSt];
+  float2 S[kSr / 2][4];  // rows ty * kSr + 2 i and the next, columns e0 + 4 tx + c
 #pragma unroll
-  for (int i = 0; i < kSt; ++i)
+  for (int i = 0; i < kSr / 2; ++i)
 #pragma unroll
-    for (int j = 0; j < kSt; ++j) S[i][j] = 0.f;
-  const bool first = p.reverse ? seg == ns - 1 : seg == 0;
+    for (int c = 0; c < 4; ++c) S[i][c] = both(0.f);
   const int s_end = min(L, (seg + 1) * p.seg);
-  if (!kState) {
-    if (p.init) {
-      // tokens between the first state and this segment
-      const float n = p.reverse ? (first || ns == 0 ? 0.f : (float)(L - 1 - s_end)) : (float)seg * p.seg;
-      const float w = decay_pow(l2, n) * p.init_scale;
-      const float *s0 = p.init + bh * D * D;
+  if (!kState && (p.nseg > 1 || p.init)) {
+    const bool pre = p.nseg > 1 && ns > 0;
+    const float *s0 = pre ? p.part + (bh * p.nseg + seg) * (size_t)D * D : p.init ? p.init + bh * D * D : nullptr;
+    const bool flip = !pre && p.init_t;
+    const float w = pre ? 1.f : p.init_scale;
+    if (s0)
 #pragma unroll
-      for (int i = 0; i < kSt; ++i)
+      for (int i = 0; i < kSr; ++i)
 #pragma unroll
-        for (int j = 0; j < kSt; ++j) {
-          const int d = ty + 16 * i, e = tx * kSt + j;
-          S[i][j] = w * (p.init_t ? s0[(size_t)e * D + d] : s0[(size_t)d * D + e]);
+        for (int c = 0; c < 4; ++c) {
+          const int d = ty * kSr + i, e = e0 + 4 * tx + c;
+          const float v = w * (flip ? s0[(size_t)e * D + d] : s0[(size_t)d * D + e]);
+          if (i & 1)
+            S[i / 2][c].y = v;
+          else
+            S[i / 2][c].x = v;
         }
-    }
-    const int lo = p.reverse ? seg + 1 : 0, hi = p.reverse ? ns : seg;
-    for (int s = lo; s < hi; ++s) {
-      const int gap = p.reverse ? s - seg - 1 : seg - 1 - s;
-      const float w = decay_pow(l2, (float)gap * p.seg);
-      const float *u = p.part + (bh * p.nseg + s) * (size_t)D * D;
-#pragma unroll
-      for (int i = 0; i < kSt; ++i)
-#pragma unroll
-        for (int j = 0; j < kSt; ++j) S[i][j] = fmaf(w, u[(ty + 16 * i) * D + tx * kSt + j], S[i][j]);
-    }
   }
 
   const T *xg = (const T *)p.x + b * p.sx[0] + (long long)(h / p.gx) * D;
   const T *yg = (const T *)p.y + b * p.sy[0] + (long long)(h / p.gy) * D;
-  const T *zg = (const T *)p.z + b * p.sz[0] + (long long)(h / p.gz) * D;
-  constexpr int kLoads = kC * D / 4 / kThreads;  // float4s of a tile a thread
+  const T *zg = (const T *)p.z + b * p.sz[0] + (long long)(h / p.gz) * D + e0;
   const int nc = seg < ns ? (s_end - seg * p.seg + kC - 1) / kC : 0;
-  for (int ci = 0; ci < nc; ++ci) {
-    const int c0 = seg * p.seg + (p.reverse ? nc - 1 - ci : ci) * kC;
-    const int n = min(kC, L - c0);
-    __syncthreads();  // the tiles and the state of the chunk before are read
-#pragma unroll
-    for (int i = 0; i < kLoads; ++i) {
-      const int at = tid + i * kThreads, r = at / (D / 4), c = at % (D / 4) * 4;
-      float fx[4] = {}, fy[4] = {}, fz[4] = {};
-      if (r < n) {
-        const long long t = c0 + r;
-        if (!kState) load4(xg + t * p.sx[1] + c, fx);
-        load4(yg + t * p.sy[1] + c, fy);
-        load4(zg + t * p.sz[1] + c, fz);
-      }
-      if (!kState) store4(xs + r * kRow + c, fx);
-      store4(ys + r * kRow + c, fy);
-      store4(zs + r * kRow + c, fz);
+  auto start_of = [&](int ci) { return seg * p.seg + (p.reverse ? nc - 1 - ci : ci) * kC; };
+  auto load = [&](int ci) {
+    if (ci < nc) {
+      float *xs = sm + (ci % Sh::kStages) * Sh::kTile;
+      const long long t = start_of(ci);
+      const int n = min(kC, L - (int)t);
+      if (!kState) load_tile<D, kRow>(xs, xg + t * p.sx[1], p.sx[1], n);
+      load_tile<D, kRow>(xs + kC * kRow, yg + t * p.sy[1], p.sy[1], n);
+      load_tile<E, kZRow>(xs + 2 * kC * kRow, zg + t * p.sz[1], p.sz[1], n);
     }
+    cp_async_commit();
+  };
+  // the state's place in shared memory: piece d / 4 of column c
+  auto st_at = [&](int c, int d4) { return st + c * D + ((d4 ^ ((c >> 2) & (D / 4 - 1) & 15)) << 2); };
+  load(0);
+  for (int ci = 0; ci < nc; ++ci) {
+    const int c0 = start_of(ci), n = min(kC, L - c0);
+    const float *xs = sm + (ci % Sh::kStages) * Sh::kTile, *ys = xs + kC * kRow, *zs = ys + kC * kRow;
+    cp_async_wait_all();
     if (!kState) {
 #pragma unroll
-      for (int i = 0; i < kSt; ++i)
+      for (int c = 0; c < 4; ++c)
 #pragma unroll
-        for (int j = 0; j < kSt; ++j) ss[(ty + 16 * i) * kRow + tx * kSt + j] = S[i][j];
+        for (int i = 0; i < kSr; i += 4) {
+          if constexpr (kSr >= 4)
+            *(float4 *)st_at(4 * tx + c, (ty * kSr + i) / 4) =
+                make_float4(S[i / 2][c].x, S[i / 2][c].y, S[i / 2 + 1][c].x, S[i / 2 + 1][c].y);
+          else
+            *(float2 *)(st_at(4 * tx + c, ty * kSr / 4) + ty * kSr % 4) = S[0][c];
+        }
     }
     __syncthreads();
-    // powers: inter weight gamma^{a0 + a1 r}, carry gamma^{span}
-    const int span = p.reverse ? (first && ci == 0 ? L - 1 - c0 : kC) : n;
+    if (Sh::kStages == 2) load(ci + 1);
+    // powers: carry gamma^span; reverse: the first state belongs to the last token
+    const int span = p.reverse ? (s_end == L && ci == 0 ? L - 1 - c0 : kC) : n;
     if (!kState) {
-      // scores, 2 rows by 2 columns a thread: rows ty, ty + 16, columns tx, tx + 16
-      float s[2][2] = {};
-#pragma unroll 4
-      for (int d = 0; d < D; d += 4) {
-        float4 xv[2], yv[2];
+      {
+        const int qx = tid & 15, qy = tid >> 4;  // rows 4 qy + i, columns qx + 16 j
+        float2 a[4][2];
 #pragma unroll
-        for (int i = 0; i < 2; ++i) {
-          xv[i] = *(const float4 *)(xs + (ty + 16 * i) * kRow + d);
-          yv[i] = *(const float4 *)(ys + (tx + 16 * i) * kRow + d);
+        for (int i = 0; i < 4; ++i) a[i][0] = a[i][1] = both(0.f);
+#pragma unroll 4
+        for (int d = 0; d < D; d += 4) {
+          float4 yv[2];
+#pragma unroll
+          for (int j = 0; j < 2; ++j) yv[j] = *(const float4 *)(ys + (qx + 16 * j) * kRow + d);
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const float4 xv = *(const float4 *)(xs + (4 * qy + i) * kRow + d);
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+              a[i][j] = __ffma2_rn(make_float2(xv.x, xv.y), make_float2(yv[j].x, yv[j].y), a[i][j]);
+              a[i][j] = __ffma2_rn(make_float2(xv.z, xv.w), make_float2(yv[j].z, yv[j].w), a[i][j]);
+            }
+          }
         }
 #pragma unroll
-        for (int i = 0; i < 2; ++i)
+        for (int i = 0; i < 4; ++i)
 #pragma unroll
           for (int j = 0; j < 2; ++j) {
-            s[i][j] = fmaf(xv[i].x, yv[j].x, s[i][j]);
-            s[i][j] = fmaf(xv[i].y, yv[j].y, s[i][j]);
-            s[i][j] = fmaf(xv[i].z, yv[j].z, s[i][j]);
-            s[i][j] = fmaf(xv[i].w, yv[j].w, s[i][j]);
+            const int r = 4 * qy + i, c = qx + 16 * j, gap = p.reverse ? c - r : r - c;
+            *(float2 *)(ps + r * kPRow + 2 * c) =
+                both(gap >= 0 ? (a[i][j].x + a[i][j].y) * gp[gap] : 0.f);
           }
       }
-#pragma unroll
-      for (int i = 0; i < 2; ++i)
-#pragma unroll
-        for (int j = 0; j < 2; ++j) {
-          const int r = ty + 16 * i, c = tx + 16 * j, gap = p.reverse ? c - r : r - c;
-          ps[r * (kC + 4) + c] = gap >= 0 ? s[i][j] * gp[gap] : 0.f;
-        }
       __syncthreads();
-      // results: kOr rows by 4 columns a thread
-      const int oc = tid % Sh::kOc * 4, o0 = tid / Sh::kOc;
-      float a[kOr][4] = {};
-#pragma unroll 4
-      for (int d = 0; d < D; d += 4) {
-        float4 sv[4];
+      float2 o[kOr][2];  // rows ty * kOr + i, columns 4 tx + 2 c and the next
+      {
+        float2 a[kOr][4];
 #pragma unroll
-        for (int k = 0; k < 4; ++k) sv[k] = *(const float4 *)(ss + (d + k) * kRow + oc);
+        for (int i = 0; i < kOr; ++i)
 #pragma unroll
-        for (int i = 0; i < kOr; ++i) {
-          const float4 xv = *(const float4 *)(xs + (o0 + i * Sh::kOrows) * kRow + d);
-          const float xk[4] = {xv.x, xv.y, xv.z, xv.w};
-#pragma unroll
-          for (int k = 0; k < 4; ++k) {
-            a[i][0] = fmaf(xk[k], sv[k].x, a[i][0]);
-            a[i][1] = fmaf(xk[k], sv[k].y, a[i][1]);
-            a[i][2] = fmaf(xk[k], sv[k].z, a[i][2]);
-            a[i][3] = fmaf(xk[k], sv[k].w, a[i][3]);
-          }
-        }
-      }
-#pragma unroll
-      for (int i = 0; i < kOr; ++i) {
-        const int r = o0 + i * Sh::kOrows;
-        // rows past the end are not written: any power in range does
-        const int m = p.reverse ? max(span - r, 0) : r + 1;
-        const float w = gp[m];
-#pragma unroll
-        for (int k = 0; k < 4; ++k) a[i][k] *= w;
-      }
+          for (int c = 0; c < 4; ++c) a[i][c] = both(0.f);
 #pragma unroll 2
-      for (int j = 0; j < kC; j += 4) {
-        float4 zv[4];
+        for (int d = 0; d < D; d += 4) {
+          float4 sv[4];
 #pragma unroll
-        for (int k = 0; k < 4; ++k) zv[k] = *(const float4 *)(zs + (j + k) * kRow + oc);
+          for (int c = 0; c < 4; ++c) sv[c] = *(const float4 *)st_at(4 * tx + c, d / 4);
+#pragma unroll
+          for (int i = 0; i < kOr; ++i) {
+            const float4 xv = *(const float4 *)(xs + (ty * kOr + i) * kRow + d);
+#pragma unroll
+            for (int c = 0; c < 4; ++c) {
+              a[i][c] = __ffma2_rn(make_float2(xv.x, xv.y), make_float2(sv[c].x, sv[c].y), a[i][c]);
+              a[i][c] = __ffma2_rn(make_float2(xv.z, xv.w), make_float2(sv[c].z, sv[c].w), a[i][c]);
+            }
+          }
+        }
 #pragma unroll
         for (int i = 0; i < kOr; ++i) {
-          const float4 pv = *(const float4 *)(ps + (o0 + i * Sh::kOrows) * (kC + 4) + j);
-          const float pk[4] = {pv.x, pv.y, pv.z, pv.w};
+          const int r = ty * kOr + i;
+          // rows past the end are not written: any power in range does
+          const float w = gp[p.reverse ? max(span - r, 0) : r + 1];
 #pragma unroll
-          for (int k = 0; k < 4; ++k) {
-            a[i][0] = fmaf(pk[k], zv[k].x, a[i][0]);
-            a[i][1] = fmaf(pk[k], zv[k].y, a[i][1]);
-            a[i][2] = fmaf(pk[k], zv[k].z, a[i][2]);
-            a[i][3] = fmaf(pk[k], zv[k].w, a[i][3]);
-          }
+          for (int c = 0; c < 2; ++c)
+            o[i][c] = make_float2(w * (a[i][2 * c].x + a[i][2 * c].y),
+                                  w * (a[i][2 * c + 1].x + a[i][2 * c + 1].y));
+        }
+      }
+#pragma unroll 4
+      for (int j = 0; j < kC; j += 2) {
+        const float4 z0 = *(const float4 *)(zs + j * kZRow + 4 * tx);
+        const float4 z1 = *(const float4 *)(zs + (j + 1) * kZRow + 4 * tx);
+#pragma unroll
+        for (int i = 0; i < kOr; ++i) {
+          const float4 pv = *(const float4 *)(ps + (ty * kOr + i) * kPRow + 2 * j);
+          const float2 p0 = make_float2(pv.x, pv.y), p1 = make_float2(pv.z, pv.w);
+          o[i][0] = __ffma2_rn(p0, make_float2(z0.x, z0.y), o[i][0]);
+          o[i][1] = __ffma2_rn(p0, make_float2(z0.z, z0.w), o[i][1]);
+          o[i][0] = __ffma2_rn(p1, make_float2(z1.x, z1.y), o[i][0]);
+          o[i][1] = __ffma2_rn(p1, make_float2(z1.z, z1.w), o[i][1]);
         }
       }
 #pragma unroll
       for (int i = 0; i < kOr; ++i) {
-        const int r = o0 + i * Sh::kOrows;
+        const int r = ty * kOr + i;
         if (r >= n) continue;
-#pragma unroll
-        for (int k = 0; k < 4; ++k) a[i][k] *= p.scale;
-        store4(out + (size_t)(c0 + r) * orow + oc, a[i]);
+        const float f[4] = {p.scale * o[i][0].x, p.scale * o[i][0].y, p.scale * o[i][1].x,
+                            p.scale * o[i][1].y};
+        store4(out + (size_t)(c0 + r) * orow + 4 * tx, f);
       }
     }
     // the state after the chunk
-    const float carry = gp[span];
+    const float2 carry = both(gp[span]);
 #pragma unroll
-    for (int i = 0; i < kSt; ++i)
+    for (int i = 0; i < kSr / 2; ++i)
 #pragma unroll
-      for (int j = 0; j < kSt; ++j) S[i][j] *= carry;
+      for (int c = 0; c < 4; ++c) S[i][c] = __fmul2_rn(S[i][c], carry);
+#pragma unroll 2
     for (int j = 0; j < n; ++j) {
       const float w = gp[p.reverse ? j : n - 1 - j];
-      float yv[kSt], zv[kSt];
+      const float4 zv = *(const float4 *)(zs + j * kZRow + 4 * tx);
+      const float2 zw[4] = {both(w * zv.x), both(w * zv.y), both(w * zv.z), both(w * zv.w)};
 #pragma unroll
-      for (int i = 0; i < kSt; ++i) {
-        yv[i] = w * ys[j * kRow + ty + 16 * i];
-        zv[i] = zs[j * kRow + tx * kSt + i];
+      for (int i = 0; i < kSr / 2; ++i) {
+        const float2 yv = *(const float2 *)(ys + j * kRow + ty * kSr + 2 * i);
+#pragma unroll
+        for (int c = 0; c < 4; ++c) S[i][c] = __ffma2_rn(yv, zw[c], S[i][c]);
       }
-#pragma unroll
-      for (int i = 0; i < kSt; ++i)
-#pragma unroll
-        for (int k = 0; k < kSt; ++k) S[i][k] = fmaf(yv[i], zv[k], S[i][k]);
     }
+    __syncthreads();  // tiles, scores and state are read
+    if (Sh::kStages == 1) load(ci + 1);
   }
   if (kState || (p.fin && seg == last)) {
     // reverse: what the gradient of the first state still decays by
     const float w = kState ? 1.f : p.fin_scale * (p.reverse && L > 0 ? decay_pow(l2, 1.f) : 1.f);
-    float *dst = kState ? p.part + (bh * p.nseg + seg) * (size_t)D * D : p.fin + bh * D * D;
+    float *dst = (kState ? p.part + (bh * p.nseg + seg) * (size_t)D * D : p.fin + bh * D * D) + e0 + 4 * tx;
 #pragma unroll
-    for (int i = 0; i < kSt; ++i)
+    for (int i = 0; i < kSr; ++i) {
+      float f[4];
 #pragma unroll
-      for (int j = 0; j < kSt; ++j) dst[(ty + 16 * i) * D + tx * kSt + j] = S[i][j] * w;
+      for (int c = 0; c < 4; ++c) f[c] = w * (i & 1 ? S[i / 2][c].y : S[i / 2][c].x);
+      store4(dst + (size_t)(ty * kSr + i) * D, f);
+    }
+  }
+}
+
+// Replaces each segment's own state by the state before it: the first state and
+// the segments before it in scan order, in that order.  Four elements a thread.
+__global__ void __launch_bounds__(128) prefix_kernel(const ScanDev p, int D) {
+  grid_dep_wait();
+  const int h = blockIdx.y, b = blockIdx.z, i = (blockIdx.x * 128 + threadIdx.x) * 4;
+  const int L = p.seq_lens ? min(max(p.seq_lens[b], 0), p.N) : p.N;
+  const int ns = (L + p.seg - 1) / p.seg;
+  if (i >= D * D || ns == 0) return;
+  const size_t bh = (size_t)b * p.H + h;
+  const float l2 = log2_decay(p.log_decay, h);
+  float S[4] = {};
+  if (p.init) {
+    const float *s0 = p.init + bh * D * D;
+    const int d = i / D, e = i % D;
+#pragma unroll
+    for (int c = 0; c < 4; ++c)
+      S[c] = p.init_scale * (p.init_t ? s0[(size_t)(e + c) * D + d] : s0[i + c]);
+  }
+  float *part = p.part + bh * p.nseg * D * D + i;
+  constexpr int kBatch = 8;  // segments whose loads go out together
+  for (int k0 = 0; k0 < ns; k0 += kBatch) {
+    float4 own[kBatch];
+#pragma unroll
+    for (int u = 0; u < kBatch; ++u) {
+      const int k = k0 + u, s = p.reverse ? ns - 1 - k : k;
+      own[u] = k + 1 < ns ? *(const float4 *)(part + (size_t)s * D * D) : make_float4(0.f, 0.f, 0.f, 0.f);
+    }
+#pragma unroll
+    for (int u = 0; u < kBatch; ++u) {
+      const int k = k0 + u, s = p.reverse ? ns - 1 - k : k;
+      if (k >= ns) break;
+      store4(part + (size_t)s * D * D, S);
+      // tokens that the state before the segment decays by (reverse: the first
+      // state belongs to the last token)
+      const float w = decay_pow(l2, (float)(p.reverse && k == 0 ? L - 1 - s * p.seg : p.seg));
+      S[0] = fmaf(w, S[0], own[u].x), S[1] = fmaf(w, S[1], own[u].y);
+      S[2] = fmaf(w, S[2], own[u].z), S[3] = fmaf(w, S[3], own[u].w);
+    }
   }
 }
 
@@ -299,15 +382,17 @@ int sm_count() {
   return n;
 }
 
-// Segments along the sequence: none while the (batch, head) pairs fill the SMs
-// twice; else as many as do, of at least 8 chunks (a segment costs its keys and
-// values a second time, and the states of those before it).
+// Segments along the sequence: none while the blocks of whole sequences fill the
+// SMs three deep; else as many as do (a segment costs its state a second time, a
+// third of the work), and, where only the device knows the lengths, at least
+// eight, so that one long sequence does not outlast the others.
 int scan_segment(const ScanArgs &a) {
-  const long long pairs = (long long)a.B * a.H, chunks = (a.N + kC - 1) / kC;
-  long long n = pairs > 0 ? (2ll * sm_count() + pairs - 1) / pairs : 1;
-  if (n > 64) n = 64;
-  if (n > chunks / 8) n = chunks / 8;
-  if (n < 1) n = 1;
+  const long long blocks = (long long)a.B * a.H * (a.D > 64 ? a.D / 64 : 1);
+  const long long chunks = (a.N + kC - 1) / kC, full = 3ll * sm_count();
+  long long n = blocks >= full / 2 ? 1 : (full + blocks - 1) / blocks;
+  if (a.seq_lens && n < 8 && chunks >= 64) n = 8;
+  if (n > 128) n = 128;  // the states before the segments are formed one after the other
+  if (n > chunks) n = chunks;
   return (int)((chunks + n - 1) / n) * kC;
 }
 
@@ -329,7 +414,7 @@ template <typename T, typename O, int D>
 cudaError_t scan_launch(const ScanArgs &a, float *part, cudaStream_t st) {
   const ScanDev p = scan_dev(a, part);
   constexpr int smem = ScanShape<D>::kSmemFloats * 4;
-  const dim3 grid(p.nseg, a.H, a.B);
+  const dim3 grid(p.nseg * ScanShape<D>::kSplit, a.H, a.B);
   cudaError_t e;
   if (p.nseg > 1) {
     if ((e = cudaFuncSetAttribute(scan_kernel<T, O, D, true>,
@@ -338,6 +423,10 @@ cudaError_t scan_launch(const ScanArgs &a, float *part, cudaStream_t st) {
     scan_kernel<T, O, D, true><<<grid, kThreads, smem, st>>>(p);
     count_launch();
     if ((e = cudaGetLastError()) != cudaSuccess) return e;
+    count_launch();
+    if ((e = launch_pdl(prefix_kernel, dim3((D * D / 4 + 127) / 128, a.H, a.B), dim3(128), 0, st, p,
+                        D)) != cudaSuccess)
+      return e;
   }
   if ((e = cudaFuncSetAttribute(scan_kernel<T, O, D, false>,
                                 cudaFuncAttributeMaxDynamicSharedMemorySize, smem)) != cudaSuccess)

@@ -45,20 +45,19 @@ __device__ __forceinline__ void store4(__nv_bfloat16 *p, const float (&f)[4]) {
 }
 
 // ------------------------------------------------------------------ the scan
-// A block of 128 threads serves E = min(D, 64) of the state's columns of one
-// segment of one (batch, head).  All products run on packed fp32 FMAs:
-//   scores   4 rows by 2 columns a thread, even and odd d in the two halves,
-//   results  E / 16 rows by 4 columns; x S with even and odd d in the halves (the
-//            state transposed in shared memory), then the weighted scores, stored
-//            twice over, times z with two columns in the halves,
-//   state    rows in pairs, 4 columns, in registers for the whole segment.
-// Bound by the FMA pipe: 2 C D + 2 D^2 multiply-adds a token and head (C = 32
-// keeps the first term below the second without more tiles than fit).  Blocks of
-// 128 threads with large register tiles rather than 256 with small ones: a
-// product of 2 x 4 results a thread spends more on shared-memory reads than on
-// FMAs.  Tiles of the next chunk come in by cp.async where two fit (D <= 64).
+// A block of 64 threads (D = 128: 128) serves E = min(D, 64) of the state's columns of one
+// segment of one (batch, head): 2 C D + 2 D^2 multiply-adds a token and head in
+// products whose operands come from shared memory.  A load's bytes into the
+// registers bound those (128 a cycle, broadcast or not, against 128
+// multiply-adds), so a thread holds large tiles of results: 4 x 4 scores, 8 x 4
+// results (D = 128: 4 x 2, 4 x 4), 8 x 8 of the state (in registers for the whole
+// segment), 1 to 2 bytes a multiply-add.  (Blocks of 256 threads with 2 x 2, 2 x 4 and 4 x 4: 2 to
+// 4 bytes.)  Two or more blocks an SM cover one another's loads and barriers.
 constexpr int kC = 32;        // tokens per chunk
-constexpr int kThreads = 128;
+// Threads of a block: with 64, D = 128 would leave an SM four warps (B4 H8 N4096:
+// 833 us, 518 with smaller tiles).
+template <int D>
+constexpr int kThreadsOf = D > 64 ? 128 : 64;
 
 struct ScanDev {
   const void *x, *y, *z;
@@ -74,18 +73,19 @@ struct ScanDev {
   int N, H, seg, nseg;  // tokens per segment (a multiple of kC), most segments
 };
 
-template <int D>
+template <int D, bool kState>
 struct ScanShape {
   static constexpr int kE = D < 64 ? D : 64, kSplit = D / kE;
-  static constexpr int kRow = D + 4, kZRow = kE + 4, kPRow = 2 * kC + 4;  // padded, in floats
-  static constexpr int kTile = kC * (2 * kRow + kZRow);  // x, y, z
-  static constexpr int kStages = D <= 64 ? 2 : 1;
-  static constexpr int kOffP = kStages * kTile, kOffS = kOffP + kC * kPRow,
-                       kOffG = kOffS + kE * D;
+  static constexpr int kRow = D + 4, kZRow = kE + 4, kPRow = kC + 4;  // padded, in floats
+  static constexpr int kOffY = kState ? 0 : kC * kRow, kOffZ = kOffY + kC * kRow;  // behind x
+  static constexpr int kOffP = kOffZ + kC * kZRow, kOffS = kOffP + (kState ? 0 : kC * kPRow);
+  static constexpr int kOffG = kOffS + (kState ? 0 : D * kE);
   static constexpr int kSmemFloats = kOffG + kC + 1;
-  static constexpr int kTx = kE / 4, kTy = kThreads / kTx;
-  static constexpr int kOr = kC / kTy;   // result rows a thread
-  static constexpr int kSr = D / kTy;    // state rows a thread
+  static constexpr int kThreads = kThreadsOf<D>;
+  static constexpr int kQc = kThreads / 8, kQj = kC / kQc;  // scores: 4 x kQj
+  static constexpr int kTx = kE / 4, kTy = kThreads / kTx, kOr = kC / kTy;  // results: kOr x 4
+  static constexpr int kSr = D / (kThreads / 8), kSc = kE / 8;              // state: kSr x kSc
+  static constexpr int kBlocks = D == 32 ? 8 : D == 64 ? 4 : 2;             // an SM
 };
 
 // 16 bytes from global to shared memory, or zeros.
@@ -94,14 +94,14 @@ __device__ __forceinline__ void cp_async_or_zero(uint32_t dst, const void *src, 
   asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(n)
                : "memory");
 }
-template <int kCols, int kRowFloats>
+template <int kCols, int kRowFloats, int kThreads>
 __device__ __forceinline__ void load_tile(float *to, const float *from, long long stride, int n) {
   for (int i = threadIdx.x; i < kC * kCols / 4; i += kThreads) {
     const int r = i / (kCols / 4), c = i % (kCols / 4) * 4;
     cp_async_or_zero(smem_u32(to + r * kRowFloats + c), from + (r < n ? r * stride + c : 0), r < n);
   }
 }
-template <int kCols, int kRowFloats>
+template <int kCols, int kRowFloats, int kThreads>
 __device__ __forceinline__ void load_tile(float *to, const __nv_bfloat16 *from, long long stride,
                                           int n) {
   for (int i = threadIdx.x; i < kC * kCols / 4; i += kThreads) {
@@ -111,21 +111,22 @@ __device__ __forceinline__ void load_tile(float *to, const __nv_bfloat16 *from, 
     store4(to + r * kRowFloats + c, f);
   }
 }
-__device__ __forceinline__ float2 both(float v) { return make_float2(v, v); }
-
 // kState: only the segment's own state (zero before it) goes to `part`; else the
 // results, from the state before the segment, which the prefix kernel leaves in
 // `part` (a single segment: the first state).
 template <typename T, typename O, int D, bool kState>
-__global__ void __launch_bounds__(kThreads) scan_kernel(const ScanDev p) {
-  using Sh = ScanShape<D>;
+__global__ void __launch_bounds__(kThreadsOf<D>, ScanShape<D, kState>::kBlocks)
+    scan_kernel(const ScanDev p) {
+  using Sh = ScanShape<D, kState>;
   constexpr int E = Sh::kE, kRow = Sh::kRow, kZRow = Sh::kZRow, kPRow = Sh::kPRow;
-  constexpr int kOr = Sh::kOr, kSr = Sh::kSr;
+  constexpr int kThreads = Sh::kThreads, kQc = Sh::kQc, kQj = Sh::kQj;
+  constexpr int kOr = Sh::kOr, kSr = Sh::kSr, kSc = Sh::kSc;
   extern __shared__ __align__(16) float sm[];
-  float *ps = sm + Sh::kOffP;  // [kC][kPRow] weighted scores, each twice
-  float *st = sm + Sh::kOffS;  // [E][D] the state transposed, 16-byte pieces swizzled
+  float *xs = sm, *ys = sm + Sh::kOffY, *zs = sm + Sh::kOffZ;
+  float *ps = sm + Sh::kOffP;  // [kC][kPRow] weighted scores
+  float *st = sm + Sh::kOffS;  // [D][E] the state
   float *gp = sm + Sh::kOffG;  // gamma^0 .. gamma^kC
-  const int tid = threadIdx.x, tx = tid % Sh::kTx, ty = tid / Sh::kTx;
+  const int tid = threadIdx.x;
   const int seg = blockIdx.x / Sh::kSplit, e0 = blockIdx.x % Sh::kSplit * E;
   const int h = blockIdx.y, b = blockIdx.z;
   const int L = p.seq_lens ? min(max(p.seq_lens[b], 0), p.N) : p.N;
@@ -147,28 +148,28 @@ __global__ void __launch_bounds__(kThreads) scan_kernel(const ScanDev p) {
   const float l2 = log2_decay(p.log_decay, h);
   if (tid <= kC) gp[tid] = decay_pow(l2, (float)tid);
 
-  float2 S[kSr / 2][4];  // rows ty * kSr + 2 i and the next, columns e0 + 4 tx + c
+  // rows sy + i, columns 4 sx + c and, from c = 4 on, 32 + 4 sx + c - 4
+  const int sx = tid & 7, sy = (tid >> 3) * kSr;
+  auto col = [&](int c) { return 4 * sx + (c & 3) + (c >> 2) * 32; };
+  float S[kSr][kSc];
 #pragma unroll
-  for (int i = 0; i < kSr / 2; ++i)
+  for (int i = 0; i < kSr; ++i)
 #pragma unroll
-    for (int c = 0; c < 4; ++c) S[i][c] = both(0.f);
+    for (int c = 0; c < kSc; ++c) S[i][c] = 0.f;
   const int s_end = min(L, (seg + 1) * p.seg);
   if (!kState && (p.nseg > 1 || p.init)) {
     const bool pre = p.nseg > 1 && ns > 0;
-    const float *s0 = pre ? p.part + (bh * p.nseg + seg) * (size_t)D * D : p.init ? p.init + bh * D * D : nullptr;
+    const float *s0 = pre ? p.part + (bh * p.nseg + seg) * (size_t)D * D
+                          : (p.init ? p.init + bh * D * D : nullptr);
     const bool flip = !pre && p.init_t;
     const float w = pre ? 1.f : p.init_scale;
     if (s0)
 #pragma unroll
       for (int i = 0; i < kSr; ++i)
 #pragma unroll
-        for (int c = 0; c < 4; ++c) {
-          const int d = ty * kSr + i, e = e0 + 4 * tx + c;
-          const float v = w * (flip ? s0[(size_t)e * D + d] : s0[(size_t)d * D + e]);
-          if (i & 1)
-            S[i / 2][c].y = v;
-          else
-            S[i / 2][c].x = v;
+        for (int c = 0; c < kSc; ++c) {
+          const int d = sy + i, e = e0 + col(c);
+          S[i][c] = w * (flip ? s0[(size_t)e * D + d] : s0[(size_t)d * D + e]);
         }
   }
 
@@ -177,159 +178,139 @@ __global__ void __launch_bounds__(kThreads) scan_kernel(const ScanDev p) {
   const T *zg = (const T *)p.z + b * p.sz[0] + (long long)(h / p.gz) * D + e0;
   const int nc = seg < ns ? (s_end - seg * p.seg + kC - 1) / kC : 0;
   auto start_of = [&](int ci) { return seg * p.seg + (p.reverse ? nc - 1 - ci : ci) * kC; };
-  auto load = [&](int ci) {
-    if (ci < nc) {
-      float *xs = sm + (ci % Sh::kStages) * Sh::kTile;
-      const long long t = start_of(ci);
-      const int n = min(kC, L - (int)t);
-      if (!kState) load_tile<D, kRow>(xs, xg + t * p.sx[1], p.sx[1], n);
-      load_tile<D, kRow>(xs + kC * kRow, yg + t * p.sy[1], p.sy[1], n);
-      load_tile<E, kZRow>(xs + 2 * kC * kRow, zg + t * p.sz[1], p.sz[1], n);
-    }
-    cp_async_commit();
-  };
-  // the state's place in shared memory: piece d / 4 of column c
-  auto st_at = [&](int c, int d4) { return st + c * D + ((d4 ^ ((c >> 2) & (D / 4 - 1) & 15)) << 2); };
-  load(0);
   for (int ci = 0; ci < nc; ++ci) {
     const int c0 = start_of(ci), n = min(kC, L - c0);
-    const float *xs = sm + (ci % Sh::kStages) * Sh::kTile, *ys = xs + kC * kRow, *zs = ys + kC * kRow;
-    cp_async_wait_all();
+    if (!kState) load_tile<D, kRow, kThreads>(xs, xg + c0 * p.sx[1], p.sx[1], n);
+    load_tile<D, kRow, kThreads>(ys, yg + c0 * p.sy[1], p.sy[1], n);
+    load_tile<E, kZRow, kThreads>(zs, zg + c0 * p.sz[1], p.sz[1], n);
+    cp_async_commit();
     if (!kState) {
 #pragma unroll
-      for (int c = 0; c < 4; ++c)
+      for (int i = 0; i < kSr; ++i)
 #pragma unroll
-        for (int i = 0; i < kSr; i += 4) {
-          if constexpr (kSr >= 4)
-            *(float4 *)st_at(4 * tx + c, (ty * kSr + i) / 4) =
-                make_float4(S[i / 2][c].x, S[i / 2][c].y, S[i / 2 + 1][c].x, S[i / 2 + 1][c].y);
-          else
-            *(float2 *)(st_at(4 * tx + c, ty * kSr / 4) + ty * kSr % 4) = S[0][c];
-        }
+        for (int c = 0; c < kSc; c += 4)
+          *(float4 *)(st + (sy + i) * E + col(c)) =
+              make_float4(S[i][c], S[i][c + 1], S[i][c + 2], S[i][c + 3]);
     }
+    cp_async_wait_all();
     __syncthreads();
-    if (Sh::kStages == 2) load(ci + 1);
     // powers: carry gamma^span; reverse: the first state belongs to the last token
     const int span = p.reverse ? (s_end == L && ci == 0 ? L - 1 - c0 : kC) : n;
     if (!kState) {
       {
-        const int qx = tid & 15, qy = tid >> 4;  // rows 4 qy + i, columns qx + 16 j
-        float2 a[4][2];
+        const int qx = tid % kQc, qy = tid / kQc;  // rows 4 qy + i, columns qx + kQc j
+        float a[4][kQj];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) a[i][0] = a[i][1] = both(0.f);
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+          for (int j = 0; j < kQj; ++j) a[i][j] = 0.f;
 #pragma unroll 4
         for (int d = 0; d < D; d += 4) {
-          float4 yv[2];
+          float4 yv[kQj];
 #pragma unroll
-          for (int j = 0; j < 2; ++j) yv[j] = *(const float4 *)(ys + (qx + 16 * j) * kRow + d);
+          for (int j = 0; j < kQj; ++j) yv[j] = *(const float4 *)(ys + (qx + kQc * j) * kRow + d);
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
             const float4 xv = *(const float4 *)(xs + (4 * qy + i) * kRow + d);
 #pragma unroll
-            for (int j = 0; j < 2; ++j) {
-              a[i][j] = __ffma2_rn(make_float2(xv.x, xv.y), make_float2(yv[j].x, yv[j].y), a[i][j]);
-              a[i][j] = __ffma2_rn(make_float2(xv.z, xv.w), make_float2(yv[j].z, yv[j].w), a[i][j]);
+            for (int j = 0; j < kQj; ++j) {
+              a[i][j] = fmaf(xv.x, yv[j].x, a[i][j]);
+              a[i][j] = fmaf(xv.y, yv[j].y, a[i][j]);
+              a[i][j] = fmaf(xv.z, yv[j].z, a[i][j]);
+              a[i][j] = fmaf(xv.w, yv[j].w, a[i][j]);
             }
           }
         }
 #pragma unroll
         for (int i = 0; i < 4; ++i)
 #pragma unroll
-          for (int j = 0; j < 2; ++j) {
-            const int r = 4 * qy + i, c = qx + 16 * j, gap = p.reverse ? c - r : r - c;
-            *(float2 *)(ps + r * kPRow + 2 * c) =
-                both(gap >= 0 ? (a[i][j].x + a[i][j].y) * gp[gap] : 0.f);
+          for (int j = 0; j < kQj; ++j) {
+            const int r = 4 * qy + i, c = qx + kQc * j, gap = p.reverse ? c - r : r - c;
+            ps[r * kPRow + c] = gap >= 0 ? a[i][j] * gp[gap] : 0.f;
           }
       }
       __syncthreads();
-      float2 o[kOr][2];  // rows ty * kOr + i, columns 4 tx + 2 c and the next
-      {
-        float2 a[kOr][4];
+      const int tx = tid % Sh::kTx, r0 = tid / Sh::kTx * kOr;  // rows r0 + i, columns 4 tx + c
+      float o[kOr][4];
 #pragma unroll
-        for (int i = 0; i < kOr; ++i)
+      for (int i = 0; i < kOr; ++i)
 #pragma unroll
-          for (int c = 0; c < 4; ++c) a[i][c] = both(0.f);
-#pragma unroll 2
-        for (int d = 0; d < D; d += 4) {
-          float4 sv[4];
+        for (int c = 0; c < 4; ++c) o[i][c] = 0.f;
+      // o += a tile of left operands (rows of 4 k) times 4 rows of right ones
+      auto product = [&](const float *left, int lrow, const float *right, int rrow, int k) {
+        float4 v[4];
 #pragma unroll
-          for (int c = 0; c < 4; ++c) sv[c] = *(const float4 *)st_at(4 * tx + c, d / 4);
+        for (int q = 0; q < 4; ++q) v[q] = *(const float4 *)(right + (k + q) * rrow + 4 * tx);
 #pragma unroll
-          for (int i = 0; i < kOr; ++i) {
-            const float4 xv = *(const float4 *)(xs + (ty * kOr + i) * kRow + d);
+        for (int i = 0; i < kOr; ++i) {
+          const float4 l = *(const float4 *)(left + (r0 + i) * lrow + k);
+          const float lk[4] = {l.x, l.y, l.z, l.w};
 #pragma unroll
-            for (int c = 0; c < 4; ++c) {
-              a[i][c] = __ffma2_rn(make_float2(xv.x, xv.y), make_float2(sv[c].x, sv[c].y), a[i][c]);
-              a[i][c] = __ffma2_rn(make_float2(xv.z, xv.w), make_float2(sv[c].z, sv[c].w), a[i][c]);
-            }
+          for (int q = 0; q < 4; ++q) {
+            o[i][0] = fmaf(lk[q], v[q].x, o[i][0]);
+            o[i][1] = fmaf(lk[q], v[q].y, o[i][1]);
+            o[i][2] = fmaf(lk[q], v[q].z, o[i][2]);
+            o[i][3] = fmaf(lk[q], v[q].w, o[i][3]);
           }
         }
-#pragma unroll
-        for (int i = 0; i < kOr; ++i) {
-          const int r = ty * kOr + i;
-          // rows past the end are not written: any power in range does
-          const float w = gp[p.reverse ? max(span - r, 0) : r + 1];
-#pragma unroll
-          for (int c = 0; c < 2; ++c)
-            o[i][c] = make_float2(w * (a[i][2 * c].x + a[i][2 * c].y),
-                                  w * (a[i][2 * c + 1].x + a[i][2 * c + 1].y));
-        }
-      }
-#pragma unroll 4
-      for (int j = 0; j < kC; j += 2) {
-        const float4 z0 = *(const float4 *)(zs + j * kZRow + 4 * tx);
-        const float4 z1 = *(const float4 *)(zs + (j + 1) * kZRow + 4 * tx);
-#pragma unroll
-        for (int i = 0; i < kOr; ++i) {
-          const float4 pv = *(const float4 *)(ps + (ty * kOr + i) * kPRow + 2 * j);
-          const float2 p0 = make_float2(pv.x, pv.y), p1 = make_float2(pv.z, pv.w);
-          o[i][0] = __ffma2_rn(p0, make_float2(z0.x, z0.y), o[i][0]);
-          o[i][1] = __ffma2_rn(p0, make_float2(z0.z, z0.w), o[i][1]);
-          o[i][0] = __ffma2_rn(p1, make_float2(z1.x, z1.y), o[i][0]);
-          o[i][1] = __ffma2_rn(p1, make_float2(z1.z, z1.w), o[i][1]);
-        }
-      }
+      };
+#pragma unroll 2
+      for (int d = 0; d < D; d += 4) product(xs, kRow, st, E, d);
 #pragma unroll
       for (int i = 0; i < kOr; ++i) {
-        const int r = ty * kOr + i;
-        if (r >= n) continue;
-        const float f[4] = {p.scale * o[i][0].x, p.scale * o[i][0].y, p.scale * o[i][1].x,
-                            p.scale * o[i][1].y};
-        store4(out + (size_t)(c0 + r) * orow + 4 * tx, f);
+        // rows past the end are not written: any power in range does
+        const float w = gp[p.reverse ? max(span - r0 - i, 0) : r0 + i + 1];
+#pragma unroll
+        for (int c = 0; c < 4; ++c) o[i][c] *= w;
+      }
+#pragma unroll 2
+      for (int j = 0; j < kC; j += 4) product(ps, kPRow, zs, kZRow, j);
+#pragma unroll
+      for (int i = 0; i < kOr; ++i) {
+        if (r0 + i >= n) continue;
+#pragma unroll
+        for (int c = 0; c < 4; ++c) o[i][c] *= p.scale;
+        store4(out + (size_t)(c0 + r0 + i) * orow + 4 * tx, o[i]);
       }
     }
     // the state after the chunk
-    const float2 carry = both(gp[span]);
+    const float carry = gp[span];
 #pragma unroll
-    for (int i = 0; i < kSr / 2; ++i)
+    for (int i = 0; i < kSr; ++i)
 #pragma unroll
-      for (int c = 0; c < 4; ++c) S[i][c] = __fmul2_rn(S[i][c], carry);
+      for (int c = 0; c < kSc; ++c) S[i][c] *= carry;
 #pragma unroll 2
     for (int j = 0; j < n; ++j) {
       const float w = gp[p.reverse ? j : n - 1 - j];
-      const float4 zv = *(const float4 *)(zs + j * kZRow + 4 * tx);
-      const float2 zw[4] = {both(w * zv.x), both(w * zv.y), both(w * zv.z), both(w * zv.w)};
+      float z[kSc];
 #pragma unroll
-      for (int i = 0; i < kSr / 2; ++i) {
-        const float2 yv = *(const float2 *)(ys + j * kRow + ty * kSr + 2 * i);
+      for (int c = 0; c < kSc; c += 4) {
+        const float4 v = *(const float4 *)(zs + j * kZRow + col(c));
+        z[c] = w * v.x, z[c + 1] = w * v.y, z[c + 2] = w * v.z, z[c + 3] = w * v.w;
+      }
 #pragma unroll
-        for (int c = 0; c < 4; ++c) S[i][c] = __ffma2_rn(yv, zw[c], S[i][c]);
+      for (int i = 0; i < kSr; i += 4) {
+        const float4 v = *(const float4 *)(ys + j * kRow + sy + i);
+        const float y[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+        for (int q = 0; q < 4; ++q)
+#pragma unroll
+          for (int c = 0; c < kSc; ++c) S[i + q][c] = fmaf(y[q], z[c], S[i + q][c]);
       }
     }
     __syncthreads();  // tiles, scores and state are read
-    if (Sh::kStages == 1) load(ci + 1);
   }
   if (kState || (p.fin && seg == last)) {
     // reverse: what the gradient of the first state still decays by
     const float w = kState ? 1.f : p.fin_scale * (p.reverse && L > 0 ? decay_pow(l2, 1.f) : 1.f);
-    float *dst = (kState ? p.part + (bh * p.nseg + seg) * (size_t)D * D : p.fin + bh * D * D) + e0 + 4 * tx;
+    float *dst = (kState ? p.part + (bh * p.nseg + seg) * (size_t)D * D : p.fin + bh * D * D) + e0;
 #pragma unroll
-    for (int i = 0; i < kSr; ++i) {
-      float f[4];
+    for (int i = 0; i < kSr; ++i)
 #pragma unroll
-      for (int c = 0; c < 4; ++c) f[c] = w * (i & 1 ? S[i / 2][c].y : S[i / 2][c].x);
-      store4(dst + (size_t)(ty * kSr + i) * D, f);
-    }
+      for (int c = 0; c < kSc; c += 4) {
+        const float f[4] = {w * S[i][c], w * S[i][c + 1], w * S[i][c + 2], w * S[i][c + 3]};
+        store4(dst + (size_t)(sy + i) * D + col(c), f);
+      }
   }
 }
 
@@ -382,14 +363,14 @@ int sm_count() {
   return n;
 }
 
-// Segments along the sequence: none while the blocks of whole sequences fill the
-// SMs three deep; else as many as do (a segment costs its state a second time, a
-// third of the work), and, where only the device knows the lengths, at least
-// eight, so that one long sequence does not outlast the others.
+// Segments along the sequence: as many as the places for blocks hold of whole
+// sequences (a segment costs its state a second time, a third of the work), and,
+// where only the device knows the lengths, at least eight, so that one long
+// sequence does not outlast the others.
 int scan_segment(const ScanArgs &a) {
   const long long blocks = (long long)a.B * a.H * (a.D > 64 ? a.D / 64 : 1);
-  const long long chunks = (a.N + kC - 1) / kC, full = 3ll * sm_count();
-  long long n = blocks >= full / 2 ? 1 : (full + blocks - 1) / blocks;
+  const long long chunks = (a.N + kC - 1) / kC, full = (a.D > 64 ? 2ll : 4ll) * sm_count();
+  long long n = blocks >= full ? 1 : full / blocks;  // one round of blocks, not a little more
   if (a.seq_lens && n < 8 && chunks >= 64) n = 8;
   if (n > 128) n = 128;  // the states before the segments are formed one after the other
   if (n > chunks) n = chunks;
@@ -413,14 +394,15 @@ ScanDev scan_dev(const ScanArgs &a, float *part) {
 template <typename T, typename O, int D>
 cudaError_t scan_launch(const ScanArgs &a, float *part, cudaStream_t st) {
   const ScanDev p = scan_dev(a, part);
-  constexpr int smem = ScanShape<D>::kSmemFloats * 4;
-  const dim3 grid(p.nseg * ScanShape<D>::kSplit, a.H, a.B);
+  const dim3 grid(p.nseg * ScanShape<D, true>::kSplit, a.H, a.B);
   cudaError_t e;
   if (p.nseg > 1) {
-    if ((e = cudaFuncSetAttribute(scan_kernel<T, O, D, true>,
-                                  cudaFuncAttributeMaxDynamicSharedMemorySize, smem)) != cudaSuccess)
+    constexpr int smem = ScanShape<D, true>::kSmemFloats * 4;
+    const auto kernel = scan_kernel<T, O, D, true>;
+    if ((e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem)) !=
+        cudaSuccess)
       return e;
-    scan_kernel<T, O, D, true><<<grid, kThreads, smem, st>>>(p);
+    kernel<<<grid, kThreadsOf<D>, smem, st>>>(p);
     count_launch();
     if ((e = cudaGetLastError()) != cudaSuccess) return e;
     count_launch();
@@ -428,10 +410,12 @@ cudaError_t scan_launch(const ScanArgs &a, float *part, cudaStream_t st) {
                         D)) != cudaSuccess)
       return e;
   }
-  if ((e = cudaFuncSetAttribute(scan_kernel<T, O, D, false>,
-                                cudaFuncAttributeMaxDynamicSharedMemorySize, smem)) != cudaSuccess)
+  constexpr int smem = ScanShape<D, false>::kSmemFloats * 4;
+  const auto kernel = scan_kernel<T, O, D, false>;
+  if ((e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem)) !=
+      cudaSuccess)
     return e;
-  scan_kernel<T, O, D, false><<<grid, kThreads, smem, st>>>(p);
+  kernel<<<grid, kThreadsOf<D>, smem, st>>>(p);
   count_launch();
   return cudaGetLastError();
 }

@@ -59,7 +59,7 @@ struct Shape {
   static constexpr int kTile = kB * kBlk;                  // one tensor's chunk
   static constexpr int kSBytes = D * D * 2;                // the state rounded to bf16
   // rings of x, y and z tiles; merged: the state's tile follows y's in its slot
-  static constexpr int kNY = D == 64 ? 4 : 3, kNZ = D == 64 ? 5 : 3;
+  static constexpr int kNY = D == 64 ? 4 : 3, kNZ = D == 64 ? 5 : (kTerms == 2 ? 4 : 3);
   static constexpr int kYSlot = kTile + (kMerged ? kSBytes : 0);
   static constexpr int kConv = D == 64 ? 2 : 1;            // buffers of v_j y_j
   static constexpr int kP = D == 64 ? 2 : 1;               // of weighted scores
@@ -291,19 +291,19 @@ __device__ __forceinline__ void take_state(float (&S)[kNV], uint32_t src, float 
     S[i] = r.x, S[i + 1] = r.y;
   };
   if constexpr (D == 64) {
-    float v[32];
-    tmem_ld_16x64(src + 64, v);
-    tmem_ld_wait_regs(v);
+    float small[32], large[32];
+    tmem_ld_16x64(src + 64, small);
+    tmem_ld_16x64(src, large);
+    tmem_ld_wait_regs(small);
+    tmem_pin(large);
 #pragma unroll
-    for (int i = 0; i < 32; i += 2) add(i, make_float2(v[i], v[i + 1]));
-    tmem_ld_16x64(src, v);
-    tmem_ld_wait_regs(v);
+    for (int i = 0; i < 32; i += 2) add(i, make_float2(small[i], small[i + 1]));
 #pragma unroll
     for (int i = 0; i < 32; i += 2) {
       if (kOwn) {
-        add(i, make_float2(v[i], v[i + 1]));
+        add(i, make_float2(large[i], large[i + 1]));
       } else {
-        const float2 r = __fadd2_rn(make_float2(S[i], S[i + 1]), make_float2(v[i], v[i + 1]));
+        const float2 r = __fadd2_rn(make_float2(S[i], S[i + 1]), make_float2(large[i], large[i + 1]));
         S[i] = r.x, S[i + 1] = r.y;
       }
     }
@@ -570,10 +570,10 @@ __global__ void __launch_bounds__(Shape<D, kTerms>::kThreads, 1)
     for (int i = 0; i < Sh::kNZ; ++i) mbar_init(&fz[i], Sh::kB), mbar_init(&ez[i], 1);
     for (int i = 0; i < Sh::kConv; ++i)  // weighted keys there, last step's state taken
       mbar_init(&state_ready[i], 4 + Sh::kSWarps), mbar_init(&conv_empty[i], 1);
-    for (int i = 0; i < Sh::kP; ++i)  // scores weighted (D = 128: and inter results)
-      mbar_init(&intra_ready[i], Sh::kMerged ? 4 : 8), mbar_init(&p_empty[i], 1);
+    for (int i = 0; i < Sh::kP; ++i)  // scores weighted, results' columns free (D = 128: weighted)
+      mbar_init(&intra_ready[i], 8), mbar_init(&p_empty[i], 1);
     for (int i = 0; i < 2; ++i) {
-      // x there, scores' columns free (D = 64: and results' columns, state there)
+      // x there, scores' columns free (D = 64: and inter results', state there)
       mbar_init(&score_ready[i], Sh::kB + (Sh::kMerged ? 12 : 4));
       mbar_init(&inter_ready[i], 4 + Sh::kSWarps);  // D = 128: results' columns free, state there
       mbar_init(&ex[i], 1);
@@ -632,6 +632,7 @@ __global__ void __launch_bounds__(Shape<D, kTerms>::kThreads, 1)
       };
       auto state_mma = [&](int i) {
         const int cb = i % Sh::kConv;
+        if (!wait(&fz[i % Sh::kNZ], (i / Sh::kNZ) & 1)) return;
         if (!wait(&state_ready[cb], (i / Sh::kConv) & 1)) return;
         tc_fence_after();
         state_product<D, kTerms, Sh::kTile>(
@@ -754,7 +755,6 @@ __global__ void __launch_bounds__(Shape<D, kTerms>::kThreads, 1)
       const int sy = i % Sh::kNY, sz = i % Sh::kNZ, cb = i % Sh::kConv;
       const int n = min(kC, L - sg.token_of(q0 + i));
       if (!mbar_wait(&fy[sy], (i / Sh::kNY) & 1, &ab)) decay_error(16, ab);
-      if (!mbar_wait(&fz[sz], (i / Sh::kNZ) & 1, &ab)) decay_error(16, ab);  // for the MMAs
       if (i >= Sh::kConv && !mbar_wait(&conv_empty[cb], ((i / Sh::kConv) & 1) ^ 1, &ab))
         decay_error(32, ab);
       const uint32_t ys = smem_u32(smem + Sh::kOffY + sy * Sh::kYSlot) + piece;
@@ -770,6 +770,7 @@ __global__ void __launch_bounds__(Shape<D, kTerms>::kThreads, 1)
             weigh_piece<kTerms, Sh::kTile>(u[k], w[k], cs + blk * kBlk + k * 2048);
         }
       } else {
+        if (!mbar_wait(&fz[sz], (i / Sh::kNZ) & 1, &ab)) decay_error(16, ab);
         weigh_end<kTerms, Sh::kTile>(ys, smem_u32(smem + Sh::kOffZ + sz * Sh::kTile) + piece, cs, rr,
                                      n, l2, 1.f, p.reverse);
       }
@@ -852,12 +853,28 @@ __global__ void __launch_bounds__(Shape<D, kTerms>::kThreads, 1)
     const int ow = warp - Sh::kOutWarp, r0 = 16 * ow + (lane >> 2);
     const uint32_t quarter = tmem + ((uint32_t)(32 * ow) << 16);
     const uint32_t stage = smem_u32(smem + Sh::kOffOut + ow * 2048);
-    uint64_t *free_cols = Sh::kMerged ? score_ready : inter_ready;
-    if (lane == 0) mbar_arrive(&free_cols[0]), mbar_arrive(&free_cols[1]);
     float u[2];  // weights of x_r^T S in the rows r0 and r0 + 8
 #pragma unroll
     for (int k = 0; k < 2; ++k)
       u[k] = p.scale * decay_pow(l2, (float)(p.reverse ? kC - (r0 + 8 * k) : r0 + 8 * k + 1));
+    float s[32];  // D = 64: the inter results of the chunk at hand
+    // They are read as soon as the scores are there, before the intra results, so
+    // that the next but one product may take their columns.
+    auto load_inter = [&](int j) {
+      if (!mbar_wait(&sc_full[j & 1], (j >> 1) & 1, &ab)) decay_error(256, ab);
+      tc_fence_after();
+      tmem_ld_16x64(quarter + Sh::kColInter + Sh::kInterStep * (j & 1), s);
+      tmem_ld_wait_regs(s);
+      tc_fence_before();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(&score_ready[j & 1]);
+    };
+    if (lane == 0) {
+      uint64_t *inter = Sh::kMerged ? score_ready : inter_ready;
+      mbar_arrive(&inter[0]), mbar_arrive(&inter[1]);
+      if (Sh::kMerged) mbar_arrive(&intra_ready[0]), mbar_arrive(&intra_ready[1 % Sh::kP]);
+    }
+    if constexpr (Sh::kMerged) load_inter(0);
     for (int j = 0; j < cnt; ++j) {
       const int ob = j & 1, t0 = sg.token_of(q0 + j), n = min(kC, L - t0);
       float ur[2] = {u[0], u[1]};
@@ -872,7 +889,6 @@ __global__ void __launch_bounds__(Shape<D, kTerms>::kThreads, 1)
 #pragma unroll
         for (int blk = 0; blk < Sh::kB; ++blk) {
           const uint32_t at = quarter + Sh::kColInter + Sh::kInterStep * ob + blk * 64;
-          float s[32];
           tmem_ld_16x64(at, s);
           tmem_ld_wait_regs(s);
 #pragma unroll
@@ -889,11 +905,13 @@ __global__ void __launch_bounds__(Shape<D, kTerms>::kThreads, 1)
       for (int blk = 0; blk < Sh::kB; ++blk) {
         float a[32];
         tmem_ld_16x64(quarter + Sh::kColIntra + Sh::kIntraStep * ob + blk * 64, a);
+        tmem_ld_wait_regs(a);
+        if (blk == Sh::kB - 1) {
+          tc_fence_before();
+          __syncwarp();
+          if (lane == 0) mbar_arrive(Sh::kMerged ? &intra_ready[ob % Sh::kP] : &inter_ready[ob]);
+        }
         if constexpr (Sh::kMerged) {
-          float s[32];
-          tmem_ld_16x64(quarter + Sh::kColInter + Sh::kInterStep * ob, s);
-          tmem_ld_wait_regs(a);
-          tmem_pin(s);
 #pragma unroll
           for (int i = 0; i < 32; i += 2) {
             const float w = ur[(i >> 1) & 1];
@@ -901,13 +919,7 @@ __global__ void __launch_bounds__(Shape<D, kTerms>::kThreads, 1)
                                         make_float2(a[i], a[i + 1]));
             a[i] = r.x, a[i + 1] = r.y;
           }
-        } else {
-          tmem_ld_wait_regs(a);
-        }
-        if (blk == Sh::kB - 1) {
-          tc_fence_before();
-          __syncwarp();
-          if (lane == 0) mbar_arrive(&free_cols[ob]);
+          if (j + 1 < cnt) load_inter(j + 1);
         }
         O *dst = out + (size_t)t0 * orow + blk * 64;
         if constexpr (sizeof(O) == 4) {
@@ -984,30 +996,32 @@ int sm_count() {
   return n;
 }
 
-// Chunks of a segment.  In units of a scanned chunk: a CTA of the scan takes its
-// chunks, one of the own-state kernel kOwnCost of them, a launch more takes
-// kLaunchCost, and the states of the segments before the last a little each.  A
-// kernel lasts as long as its longest CTA and as all of them over the SMs (in
-// whole rounds when the lengths are equal; lengths that only the device knows
-// are taken to be a quarter of the longest on average).
+// Chunks of a segment.  In units of a scanned chunk (0.75 us at D = 64, 1.5 at
+// D = 128), as measured: a CTA costs what its pipeline takes to fill and drain and
+// its chunks, one of the own-state kernel 0.6 of a unit a chunk.  Equal lengths:
+// whole rounds of CTAs over the SMs.  Lengths that only the device knows are taken
+// to be a quarter of the longest on average; the kernels then last as long as all
+// the work over the SMs and half a segment of tail, or as their longest CTA.
 int segment_for(const ScanArgs &a) {
-  constexpr double kOwnCost = 0.5, kLaunchCost = 6, kStateCost = 0.25;
+  const double fill = a.D > 64 ? 5 : 9, own_chunk = 0.6;
   const int nc = (a.N + kC - 1) / kC, sms = sm_count();
   const double pairs = (double)a.B * a.H;
+  auto rounds = [&](double ctas) { return (double)(long long)(ctas / sms + 0.999999); };
+  auto more = [](double x, double y) { return x > y ? x : y; };
   int best = nc;
   double least = 0;
   for (int r = 1; r <= 32 && nc >= 4 * r; ++r) {
     const int seg = (nc + r - 1) / r;
-    double scan, own = 0;
+    double t;
     if (a.seq_lens) {
-      const double all = pairs * nc / 4 / sms;
-      scan = seg > all + seg / 2 ? seg : all + seg / 2;
-      if (r > 1) own = kOwnCost * (seg > all ? seg : all);
+      const double all = pairs * nc / 4 / sms, fills = fill * pairs * (r / 4.0 + 0.5) / sms;
+      t = more(all + fills + seg / 2, seg + fill);
+      if (r > 1)
+        t += more(own_chunk * (all * (r - 1) / r + seg / 2) + fills, own_chunk * seg + fill);
     } else {
-      scan = seg * (double)(long long)(pairs * r / sms + 0.999999);
-      if (r > 1) own = kOwnCost * seg * (double)(long long)(pairs * (r - 1) / sms + 0.999999);
+      t = rounds(pairs * r) * (seg + fill);
+      if (r > 1) t += rounds(pairs * (r - 1)) * own_chunk * seg + fill;
     }
-    const double t = scan + own + (r > 1 ? kLaunchCost + kStateCost * r * (a.D / 64) : 0);
     if (r == 1 || t < 0.97 * least) best = seg, least = t;
   }
   return best;

@@ -59,17 +59,18 @@ struct Shape {
   static constexpr int kTile = kB * kBlk;                  // one tensor's chunk
   static constexpr int kSBytes = D * D * 2;                // the state rounded to bf16
   // rings of x, y and z tiles; merged: the state's tile follows y's in its slot
-  static constexpr int kNY = D == 64 ? 4 : 3, kNZ = D == 64 ? 5 : (kTerms == 2 ? 4 : 3);
+  static constexpr int kNX = D == 64 ? 4 : 2, kNY = D == 64 ? (kTerms == 2 ? 5 : 4) : 3,
+                       kNZ = D == 64 ? (kTerms == 2 ? 6 : 5) : (kTerms == 2 ? 4 : 3);
   static constexpr int kYSlot = kTile + (kMerged ? kSBytes : 0);
   static constexpr int kConv = D == 64 ? 2 : 1;            // buffers of v_j y_j
   static constexpr int kP = D == 64 ? 2 : 1;               // of weighted scores
-  static constexpr int kOffX = 0, kOffY = kOffX + 2 * kTile, kOffZ = kOffY + kNY * kYSlot;
+  static constexpr int kOffX = 0, kOffY = kOffX + kNX * kTile, kOffZ = kOffY + kNY * kYSlot;
   static constexpr int kOffConv = kOffZ + kNZ * kTile;
   static constexpr int kOffP = kOffConv + kConv * kTerms * kTile;
   static constexpr int kOffS = kOffP + kP * kBlk;
   static constexpr int kOffOut = kOffS + (kMerged ? 0 : kSBytes);  // 2 KB a result warp
   static constexpr int kOffBar = kOffOut + kBlk;
-  static constexpr int kBars = 2 * (kNY + kNZ + kConv + kP) + 2 * 6 + 3;
+  static constexpr int kBars = 2 * (kNX + kNY + kNZ + kConv + kP) + 2 * 5 + 3;
   static constexpr int kOffMisc = kOffBar + kBars * 8;
   static constexpr int kSmem = kOffMisc + 16 + 1024;
   static_assert(kSmem <= 227 * 1024, "shared memory");
@@ -533,10 +534,10 @@ __global__ void __launch_bounds__(Shape<D, kTerms>::kThreads, 1)
   uint64_t *bar = (uint64_t *)(smem + Sh::kOffBar);
   // *_ready: everything that its MMAs wait for, on one barrier (a wait costs the
   // issuing thread more than an MMA)
-  uint64_t *fy = bar, *ey = fy + Sh::kNY, *fz = ey + Sh::kNY, *ez = fz + Sh::kNZ,
+  uint64_t *fx = bar, *ex = fx + Sh::kNX, *fy = ex + Sh::kNX, *ey = fy + Sh::kNY, *fz = ey + Sh::kNY, *ez = fz + Sh::kNZ,
            *state_ready = ez + Sh::kNZ, *conv_empty = state_ready + Sh::kConv,
            *intra_ready = conv_empty + Sh::kConv, *p_empty = intra_ready + Sh::kP,
-           *score_ready = p_empty + Sh::kP, *ex = score_ready + 2, *sc_full = ex + 2,
+           *score_ready = p_empty + Sh::kP, *sc_full = score_ready + 2,
            *inter_ready = sc_full + 2, *inter_full = inter_ready + 2, *o_full = inter_full + 2,
            *s_empty = o_full + 2, *ds_full = s_empty + 1, *drained = ds_full + 1;
   uint32_t *tmem_slot = (uint32_t *)(smem + Sh::kOffMisc);
@@ -566,6 +567,7 @@ __global__ void __launch_bounds__(Shape<D, kTerms>::kThreads, 1)
 
   if (tid == 0) {
     *(volatile int *)(smem + Sh::kOffMisc + 4) = 0;
+    for (int i = 0; i < Sh::kNX; ++i) mbar_init(&fx[i], Sh::kB), mbar_init(&ex[i], 1);
     for (int i = 0; i < Sh::kNY; ++i) mbar_init(&fy[i], Sh::kB), mbar_init(&ey[i], 1);
     for (int i = 0; i < Sh::kNZ; ++i) mbar_init(&fz[i], Sh::kB), mbar_init(&ez[i], 1);
     for (int i = 0; i < Sh::kConv; ++i)  // weighted keys there, last step's state taken
@@ -573,10 +575,9 @@ __global__ void __launch_bounds__(Shape<D, kTerms>::kThreads, 1)
     for (int i = 0; i < Sh::kP; ++i)  // scores weighted, results' columns free (D = 128: weighted)
       mbar_init(&intra_ready[i], 8), mbar_init(&p_empty[i], 1);
     for (int i = 0; i < 2; ++i) {
-      // x there, scores' columns free (D = 64: and inter results', state there)
-      mbar_init(&score_ready[i], Sh::kB + (Sh::kMerged ? 12 : 4));
+      // scores' columns free (D = 64: and inter results', state there)
+      mbar_init(&score_ready[i], Sh::kMerged ? 12 : 4);
       mbar_init(&inter_ready[i], 4 + Sh::kSWarps);  // D = 128: results' columns free, state there
-      mbar_init(&ex[i], 1);
       mbar_init(&sc_full[i], 1);
       mbar_init(&inter_full[i], 1);
       mbar_init(&o_full[i], 1);
@@ -602,8 +603,8 @@ __global__ void __launch_bounds__(Shape<D, kTerms>::kThreads, 1)
       const int t = lane / Sh::kB, blk = lane % Sh::kB;  // tensor, 64-channel block
       const CUtensorMap *tm = t == 0 ? &tm_x : t == 1 ? &tm_y : &tm_z;
       const int hd = h / (t == 0 ? p.gx : t == 1 ? p.gy : p.gz);
-      uint64_t *f = t == 0 ? score_ready : t == 1 ? fy : fz, *e = t == 0 ? ex : t == 1 ? ey : ez;
-      const int slots = t == 0 ? 2 : t == 1 ? Sh::kNY : Sh::kNZ;
+      uint64_t *f = t == 0 ? fx : t == 1 ? fy : fz, *e = t == 0 ? ex : t == 1 ? ey : ez;
+      const int slots = t == 0 ? Sh::kNX : t == 1 ? Sh::kNY : Sh::kNZ;
       uint8_t *to = smem + (t == 0 ? Sh::kOffX : t == 1 ? Sh::kOffY : Sh::kOffZ) + blk * kBlk;
       const int size = t == 1 ? Sh::kYSlot : Sh::kTile;
       int i = 0;
@@ -644,8 +645,9 @@ __global__ void __launch_bounds__(Shape<D, kTerms>::kThreads, 1)
       // scores of chunk i; merged: and x_r^T S.  The chunk's state
       // went before, so its keys are there and those past the end are zero.
       auto score_mma = [&](int i) {
-        const int sx = i & 1, sy = i % Sh::kNY;
-        if (!wait(&score_ready[sx], (i >> 1) & 1)) return;
+        const int sx = i % Sh::kNX, sy = i % Sh::kNY;
+        if (!wait(&fx[sx], (i / Sh::kNX) & 1)) return;
+        if (!wait(&score_ready[i & 1], (i >> 1) & 1)) return;
         tc_fence_after();
         constexpr uint32_t id = idesc_bf16_f32(64, Sh::kMerged ? 128 : 64, 0, 0);
         const uint64_t xd = sw128_desc(base + Sh::kOffX + sx * Sh::kTile, 16, 1024);
@@ -661,17 +663,17 @@ __global__ void __launch_bounds__(Shape<D, kTerms>::kThreads, 1)
         if constexpr (Sh::kMerged) mma_commit(&ex[sx]);
       };
       auto inter_mma = [&](int i) {  // x_r^T S on its own
-        const int sx = i & 1;
-        if (!wait(&inter_ready[sx], (i >> 1) & 1)) return;
+        const int sx = i % Sh::kNX;
+        if (!wait(&inter_ready[i & 1], (i >> 1) & 1)) return;
         tc_fence_after();
         constexpr uint32_t id = idesc_bf16_f32(64, D, 0, 1);
         const uint64_t xd = sw128_desc(base + Sh::kOffX + sx * Sh::kTile, 16, 1024);
         const uint64_t sd = sw128_desc(base + Sh::kOffS, D * 128, 1024);
 #pragma unroll
         for (int k = 0; k < D / 16; ++k)
-          mma_bf16(tmem + Sh::kColInter + Sh::kInterStep * sx, desc_at(xd, (k >> 2) * kBlk + (k & 3) * 32),
+          mma_bf16(tmem + Sh::kColInter + Sh::kInterStep * (i & 1), desc_at(xd, (k >> 2) * kBlk + (k & 3) * 32),
                    desc_at(sd, k * 2048), id, k != 0);
-        mma_commit(&inter_full[sx]);
+        mma_commit(&inter_full[i & 1]);
         mma_commit(s_empty);
         mma_commit(&ex[sx]);
       };

@@ -1046,22 +1046,34 @@ gbla_status gbla_decay_attention_backward(
   // In reverse A_t = gamma A_{t+1} + q_t d_o_t^T (dstate_out at the end; held
   // without the scale): dk_t = A_t v_t, dv_t = A_t^T k_t, dstate_in = gamma A_0.
   // Shared heads: per query head in fp32, then summed.
-  Scratch plane;
-  if (G > 1 && (s = plane.alloc(sizeof(float) * tok * H * D, st)) != GBLA_OK) return s;
+  ScanArgs grad[2] = {a, a};  // dv, dk
   for (int i = 0; i < 2; ++i) {
-    ScanArgs r = a;
-    r.x = i == 0 ? v : k, r.y = i == 0 ? d_o : q, r.z = i == 0 ? q : d_o;
-    const View &rx = i == 0 ? vv : vk, &ry = i == 0 ? vo : vq, &rz = i == 0 ? vq : vo;
+    ScanArgs &r = grad[i];
+    r.x = i ? v : k, r.y = i ? d_o : q, r.z = i ? q : d_o;
+    const View &rx = i ? vv : vk, &ry = i ? vo : vq, &rz = i ? vq : vo;
     for (int j = 0; j < 2; ++j) r.sx[j] = rx.s[j], r.sy[j] = ry.s[j], r.sz[j] = rz.s[j];
     r.gx = G, r.gy = r.gz = 1;
-    void *grad = i == 0 ? dk : dv;
-    r.out = G > 1 ? plane.ptr : grad, r.out_f32 = G > 1;
-    r.init = dstate_out, r.init_t = i == 0, r.init_scale = 1.f / scale;
-    r.fin = i == 0 ? nullptr : dstate_in, r.fin_scale = scale;
+    r.out = i ? dk : dv, r.out_f32 = G > 1;
+    r.init = dstate_out, r.init_t = i == 1, r.init_scale = 1.f / scale;
+    r.fin = i ? nullptr : dstate_in, r.fin_scale = scale;
     r.reverse = true;
-    if ((s = run_scan(r, tc, st)) != GBLA_OK) return s;
-    if (G > 1 && (s = from_cuda(sum_shared_heads((const float *)plane.ptr, grad, (long long)tok,
-                                                 Hk, G, D, dtype, st))) != GBLA_OK)
+  }
+  const bool together = tc && tc_kv_supports(grad[0]);
+  const size_t plane_floats = G > 1 ? round_up(tok * H * D, 64) : 0;
+  Scratch planes;
+  if ((s = planes.alloc(sizeof(float) * plane_floats * (together ? 2 : 1), st)) != GBLA_OK) return s;
+  float *plane[2] = {(float *)planes.ptr, (float *)planes.ptr + (together ? plane_floats : 0)};
+  if (G > 1) grad[0].out = plane[0], grad[1].out = plane[1];
+  if (together) {
+    Scratch ws;
+    if ((s = ws.alloc(sizeof(float) * tc_scan_floats(grad[0]), st)) != GBLA_OK) return s;
+    if ((s = from_cuda(tc_kv(grad[0], v, grad[1].sx, grad[1].out, (float *)ws.ptr, st))) != GBLA_OK)
+      return s;
+  }
+  for (int i = 0; i < 2; ++i) {
+    if (!together && (s = run_scan(grad[i], tc, st)) != GBLA_OK) return s;
+    if (G > 1 && (s = from_cuda(sum_shared_heads(plane[i], i ? dk : dv, (long long)tok, Hk, G, D,
+                                                 dtype, st))) != GBLA_OK)
       return s;
   }
   return GBLA_OK;

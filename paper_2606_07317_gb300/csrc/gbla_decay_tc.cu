@@ -155,6 +155,49 @@ __device__ __forceinline__ void store_16x64(uint32_t rows, int lane, const float
                  : "memory");
   }
 }
+// The same transposed: the values' rows become 16 columns of a tile of 64 rows of
+// 128 bytes, from its 16-byte piece `piece` on.
+__device__ __forceinline__ void store_16x64_t(uint32_t tile, int piece, int lane,
+                                              const float (&v)[32]) {
+  // lane l: the row 8 (k + l / 16) + l % 8 of the tile, piece + (l / 8) % 2 of it
+  const uint32_t row = tile + (8 * (lane >> 4) + (lane & 7)) * 128 +
+                       (((piece + ((lane >> 3) & 1)) ^ (lane & 7)) << 4);
+#pragma unroll
+  for (int k = 0; k < 8; k += 2)
+    asm volatile(
+        "stmatrix.sync.aligned.m8n8.x4.trans.shared.b16 [%0], {%1,%2,%3,%4};" ::"r"(row + k * 1024),
+        "r"(f2_to_bf2(v[4 * k], v[4 * k + 1])), "r"(f2_to_bf2(v[4 * k + 2], v[4 * k + 3])),
+        "r"(f2_to_bf2(v[4 * k + 4], v[4 * k + 5])), "r"(f2_to_bf2(v[4 * k + 6], v[4 * k + 7]))
+        : "memory");
+}
+// A result warp's 16 x 64 values (rows 16 ow on of the chunk, the first n of its
+// rows valid) to rows of `orow` values; bf16 as whole 128-byte rows through the
+// warp's 2 KB of staging.
+template <int V, typename O>
+__device__ __forceinline__ void write_rows(O *dst, size_t orow, uint32_t stage, int ow, int lane,
+                                           int n, const float (&a)[32]) {
+  if constexpr (sizeof(O) == 4) {
+    const int r0 = 16 * ow + (lane >> 2);
+#pragma unroll
+    for (int k = 0; k < 8; ++k)
+#pragma unroll
+      for (int q = 0; q < 2; ++q)
+        if (r0 + 8 * q < n && 8 * k < V)
+          *(float2 *)(dst + (size_t)(r0 + 8 * q) * orow + 8 * k + 2 * (lane & 3)) =
+              make_float2(a[4 * k + 2 * q], a[4 * k + 2 * q + 1]);
+  } else {
+    __syncwarp();
+    store_16x64(stage, lane, a);
+    __syncwarp();
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      const int r = (lane >> 3) + 4 * k;
+      const uint4 v = lds_v4(stage + r * 128 + (((lane & 7) ^ (r & 7)) << 4));
+      if (16 * ow + r < n && 8 * (lane & 7) < V)
+        *(uint4 *)(dst + (size_t)(16 * ow + r) * orow + 8 * (lane & 7)) = v;
+    }
+  }
+}
 __device__ __forceinline__ uint32_t bf2_mul(uint32_t a, uint32_t b) {
   uint32_t r;
   asm("mul.rn.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
@@ -923,28 +966,376 @@ __global__ void __launch_bounds__(Shape<D, kTerms>::kThreads, 1)
           }
           if (j + 1 < cnt) load_inter(j + 1);
         }
-        O *dst = out + (size_t)t0 * orow + blk * 64;
-        if constexpr (sizeof(O) == 4) {
-#pragma unroll
-          for (int k = 0; k < 8; ++k)
-#pragma unroll
-            for (int q = 0; q < 2; ++q)
-              if (r0 + 8 * q < n && (V == D || 8 * k < V))
-                *(float2 *)(dst + (size_t)(r0 + 8 * q) * orow + 8 * k + 2 * (lane & 3)) =
-                    make_float2(a[4 * k + 2 * q], a[4 * k + 2 * q + 1]);
-        } else {  // whole 128-byte rows through the warp's staging
-          __syncwarp();
-          store_16x64(stage, lane, a);
-          __syncwarp();
-#pragma unroll
-          for (int k = 0; k < 4; ++k) {
-            const int r = (lane >> 3) + 4 * k;
-            const uint4 v = lds_v4(stage + r * 128 + (((lane & 7) ^ (r & 7)) << 4));
-            if (16 * ow + r < n && (V == D || 8 * (lane & 7) < V))
-              *(uint4 *)(dst + (size_t)(16 * ow + r) * orow + 8 * (lane & 7)) = v;
-          }
-        }
+        write_rows<(V < 64 ? V : 64), O>(out + (size_t)t0 * orow + blk * 64, orow, stage, ow, lane, n,
+                                         a);
       }
+    }
+  }
+  tc_fence_before();
+  __syncthreads();
+  if (warp == Sh::kMmaWarp) {
+    tc_fence_after();
+    tmem_dealloc(tmem, 512);
+  }
+}
+
+// ---------------------------------------------------------------------------
+// The gradients of keys and values together (D <= 64), in reverse.  Both meet the
+// same state A = sum gamma^.. q d_o^T, whose keys and values are q and d_o:
+//   dv_r = scale [ sum_{j >= r} gamma^{j-r} (k_r . q_j) d_o_j + u_r A^T k_r ],
+//   dk_r = scale [ sum_{j >= r} gamma^{j-r} (v_r . d_o_j) q_j + u_r A v_r ].
+// So a chunk is two jobs of the scan above, dv then dk, over tiles that are loaded
+// once, and one state, which the state warps write behind both: transposed behind
+// q (dv's columns are those of d_o) and as it is behind d_o.  Against two scans
+// this saves half the loads, a state product and its weighted keys, and the second
+// own-state kernel.  Scores, weighting and results see jobs as they see chunks.
+template <int kTerms>
+struct KvShape {
+  static constexpr int kNX = kTerms == 2 ? 2 : 1;  // slots of k and of v each
+  static constexpr int kN = 4;                     // slots of q and of d_o, a state behind each
+  static constexpr int kSlot = 2 * kBlk;
+  static constexpr int kOffX = 0, kOffQ = 2 * kNX * kBlk, kOffG = kOffQ + kN * kSlot;
+  static constexpr int kOffConv = kOffG + kN * kSlot, kOffP = kOffConv + 2 * kTerms * kBlk;
+  static constexpr int kOffOut = kOffP + 2 * kBlk, kOffBar = kOffOut + kBlk;
+  static constexpr int kBars = 2 * (2 * kNX) + 4 * kN + 8 * 2 + 1 + 1 + 2;
+  static constexpr int kOffMisc = kOffBar + kBars * 8;
+  static constexpr int kSmem = kOffMisc + 16 + 1024;
+  static_assert(kSmem <= 227 * 1024, "shared memory");
+  static constexpr int kTmaWarp = 16, kMmaWarp = 17, kThreads = 18 * 32;
+  // scores | inter results of two jobs, intra results of two, the chunk's state
+  static constexpr uint32_t kColSc = 0, kColIntra = 256, kColDs = 384;
+};
+
+struct KvParams {
+  TcParams c;  // y = q, z = d_o; out = dv
+  void *dk;
+};
+
+template <int V, int kTerms, typename O>
+__global__ void __launch_bounds__(KvShape<kTerms>::kThreads, 1)
+    kv_kernel(const KvParams kp, const __grid_constant__ CUtensorMap tm_k,
+              const __grid_constant__ CUtensorMap tm_v, const __grid_constant__ CUtensorMap tm_q,
+              const __grid_constant__ CUtensorMap tm_g) {
+  using Sh = KvShape<kTerms>;
+  constexpr int D = 64, kNX = Sh::kNX, kN = Sh::kN;
+  const TcParams &p = kp.c;
+  extern __shared__ uint8_t smem_raw[];
+  uint8_t *smem = (uint8_t *)(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);
+  uint64_t *fx = (uint64_t *)(smem + Sh::kOffBar), *ex = fx + 2 * kNX, *fq = ex + 2 * kNX,
+           *eq = fq + kN, *fg = eq + kN, *eg = fg + kN, *state_ready = eg + kN,
+           *conv_empty = state_ready + 2, *score_ready = conv_empty + 2, *sc_full = score_ready + 2,
+           *intra_ready = sc_full + 2, *p_empty = intra_ready + 2, *o_full = p_empty + 2,
+           *s_full = o_full + 2, *ds_full = s_full + 2, *drained = ds_full + 1;
+  uint32_t *tmem_slot = (uint32_t *)(smem + Sh::kOffMisc);
+  const AbortFlag ab{smem_u32(smem + Sh::kOffMisc + 4)};
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  const int rank = blockIdx.x, h = blockIdx.y, b = blockIdx.z;
+  const Segment sg(p, b, rank);
+  const int L = sg.L, q0 = sg.q0, cnt = sg.cnt, jobs = 2 * cnt;
+  const size_t bh = (size_t)b * p.H + h, orow = (size_t)p.H * V;
+  const size_t first = ((size_t)b * p.N * p.H + h) * V;  // token t at first + t * orow
+  {  // the rows past the end, shared among the sequence's CTAs
+    constexpr int kPer = V * (int)sizeof(O) / 16;
+    for (long long i = (long long)rank * Sh::kThreads + tid; i < (long long)(p.N - L) * kPer * 2;
+         i += (long long)p.ranks * Sh::kThreads) {
+      O *out = (O *)(i & 1 ? kp.dk : p.out) + first;
+      ((uint4 *)(out + (L + (i >> 1) / kPer) * orow))[(i >> 1) % kPer] = make_uint4(0, 0, 0, 0);
+    }
+  }
+  if (cnt == 0) {
+    if (rank == 0 && p.fin)  // an empty sequence passes its state on
+      for (int i = tid; i < V * V; i += Sh::kThreads)
+        p.fin[bh * V * V + i] = p.init ? p.init[bh * V * V + i] * p.init_scale * p.fin_scale : 0.f;
+    return;
+  }
+  const float l2 = __ldg(p.log_decay + h) * 1.4426950408889634f;
+  if (tid == 0) {
+    *(volatile int *)(smem + Sh::kOffMisc + 4) = 0;
+    for (int i = 0; i < 2 * kNX; ++i) mbar_init(&fx[i], 1), mbar_init(&ex[i], 1);
+    for (int i = 0; i < kN; ++i) {
+      mbar_init(&fq[i], 1), mbar_init(&eq[i], 1);
+      mbar_init(&fg[i], 1), mbar_init(&eg[i], 1);
+    }
+    for (int i = 0; i < 2; ++i) {
+      mbar_init(&state_ready[i], 8);  // weighted q there, the last chunk's state taken
+      mbar_init(&conv_empty[i], 1);
+      mbar_init(&score_ready[i], 8);  // scores' and inter results' columns free
+      mbar_init(&sc_full[i], 1);
+      mbar_init(&intra_ready[i], 8);  // scores weighted, intra results' columns free
+      mbar_init(&p_empty[i], 1);
+      mbar_init(&o_full[i], 1);
+      mbar_init(&s_full[i], 4);
+    }
+    mbar_init(ds_full, 1);
+    mbar_init(drained, 1);
+    fence_mbar_init();
+  }
+  if (warp == Sh::kTmaWarp && lane == 0) {
+    tma_prefetch_desc(&tm_k);
+    tma_prefetch_desc(&tm_v);
+    tma_prefetch_desc(&tm_q);
+    tma_prefetch_desc(&tm_g);
+  }
+  if (warp == Sh::kMmaWarp) tmem_alloc(tmem_slot, 512);
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem = *tmem_slot;
+  if (warp == Sh::kTmaWarp) {
+    // ---------------------------------------------------------------- loads
+    if (lane < 4) {  // k, v, q, d_o
+      const CUtensorMap *tm = lane == 0 ? &tm_k : lane == 1 ? &tm_v : lane == 2 ? &tm_q : &tm_g;
+      const int hd = lane < 2 ? h / p.gx : h, slots = lane < 2 ? kNX : kN;
+      uint64_t *f = lane < 2 ? fx + lane * kNX : lane == 2 ? fq : fg;
+      uint64_t *e = lane < 2 ? ex + lane * kNX : lane == 2 ? eq : eg;
+      uint8_t *to = smem + (lane < 2 ? Sh::kOffX + lane * kNX * kBlk : lane == 2 ? Sh::kOffQ : Sh::kOffG);
+      const int size = lane < 2 ? kBlk : Sh::kSlot;
+      int i = 0;
+      for (; i < cnt; ++i) {
+        const int s = i % slots;
+        if (!mbar_wait(&e[s], ((i / slots) & 1) ^ 1, &ab)) {
+          decay_error(1, ab);
+          break;
+        }
+        mbar_arrive_expect_tx(&f[s], kBlk);
+        tma_load_4d(to + s * size, tm, &f[s], 0, hd, sg.token_of(q0 + i), b);
+      }
+      if (i < cnt)  // gave up: no copy may land after the CTA is gone
+        for (int k = max(0, i - slots); k < i; ++k)
+          mbar_wait(&f[k % slots], (k / slots) & 1, nullptr);
+    }
+    __syncwarp();
+  } else if (warp == Sh::kMmaWarp) {
+    // ----------------------------------------------------------------- MMAs
+    if (elect_one()) {
+      const uint32_t base = smem_u32(smem);
+      bool ok = true;
+      auto wait = [&](uint64_t *m, uint32_t parity) {
+        if (ok && !mbar_wait(m, parity, &ab)) decay_error(2, ab), ok = false;
+        return ok;
+      };
+      auto slot = [&](bool g, int i) { return base + (g ? Sh::kOffG : Sh::kOffQ) + (i % kN) * Sh::kSlot; };
+      auto state_mma = [&](int i) {
+        if (!wait(&fg[i % kN], (i / kN) & 1)) return;
+        if (!wait(&state_ready[i & 1], (i >> 1) & 1)) return;
+        tc_fence_after();
+        state_product<D, kTerms, kBlk>(tmem + Sh::kColDs, slot(true, i),
+                                       base + Sh::kOffConv + (i & 1) * kTerms * kBlk, false);
+        mma_commit(ds_full);
+        mma_commit(&conv_empty[i & 1]);
+      };
+      // job 2 i (dv): k against q and the state behind it; 2 i + 1 (dk): v against d_o
+      auto score_mma = [&](int job) {
+        const int i = job >> 1, w = job & 1, sx = w * kNX + i % kNX;
+        if (!wait(&fx[sx], (i / kNX) & 1)) return;
+        if (w == 0 && !wait(&s_full[i & 1], (i >> 1) & 1)) return;
+        if (!wait(&score_ready[w], i & 1)) return;
+        tc_fence_after();
+        constexpr uint32_t id = idesc_bf16_f32(64, 128, 0, 0);
+        const uint64_t xd = sw128_desc(base + Sh::kOffX + sx * kBlk, 16, 1024);
+        const uint64_t yd = sw128_desc(slot(w != 0, i), 16, 1024);
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+          mma_bf16(tmem + Sh::kColSc + 128 * w, desc_at(xd, k * 32), desc_at(yd, k * 32), id, k != 0);
+        mma_commit(&sc_full[w]);
+        mma_commit(&ex[sx]);
+      };
+      auto intra_mma = [&](int job) {
+        const int i = job >> 1, w = job & 1;
+        if (!wait(&intra_ready[w], i & 1)) return;
+        tc_fence_after();
+        constexpr uint32_t id = idesc_bf16_f32(64, D, 0, 1);
+        const uint64_t pd = sw128_desc(base + Sh::kOffP + w * kBlk, 16, 1024);
+        const uint64_t zd = sw128_desc(slot(w == 0, i), kBlk, 1024);
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+          mma_bf16(tmem + Sh::kColIntra + 64 * w, desc_at(pd, k * 32), desc_at(zd, k * 2048), id, k != 0);
+        mma_commit(&p_empty[w]);
+        mma_commit(&o_full[w]);
+        if (w == 1) mma_commit(&eq[i % kN]), mma_commit(&eg[i % kN]);
+      };
+      state_mma(0);
+      for (int job = 0; job <= jobs && ok; ++job) {
+        if (job < jobs) score_mma(job);
+        if (job >= 1 && ok) intra_mma(job - 1);
+        if ((job & 1) && job < jobs && (job >> 1) + 1 < cnt && ok) state_mma((job >> 1) + 1);
+      }
+      mma_commit(drained);  // nothing is in flight when TMEM is freed
+      if (!mbar_wait(drained, 0, nullptr)) decay_error(512, ab);
+    }
+    __syncwarp();
+  } else if (warp < 4) {
+    // ------------------------------------------- weighted scores (warps 0-3)
+    const int r0 = 16 * warp + (lane >> 2), c = 2 * (lane & 3);
+    float2 w[9];  // gamma^{column - row} in steps of 8 columns, as in the scan
+#pragma unroll
+    for (int k = 0; k < 9; ++k) {
+      float e[2];
+#pragma unroll
+      for (int q = 0; q < 2; ++q) {
+        const int n = c + q + 8 * (k - 1) - r0;
+        e[q] = n >= 0 ? p.scale * decay_pow(l2, (float)n) : 0.f;
+      }
+      w[k] = make_float2(e[0], e[1]);
+    }
+    if (lane == 0) mbar_arrive(&score_ready[0]), mbar_arrive(&score_ready[1]);
+    for (int job = 0; job < jobs; ++job) {
+      const int i = job >> 1, s = job & 1;
+      if (!mbar_wait(&sc_full[s], i & 1, &ab)) decay_error(4, ab);
+      tc_fence_after();
+      float a[32];
+      tmem_ld_16x64(tmem + ((uint32_t)(32 * warp) << 16) + Sh::kColSc + 128 * s, a);
+      tmem_ld_wait_regs(a);
+      tc_fence_before();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(&score_ready[s]);
+      if (i >= 1 && !mbar_wait(&p_empty[s], (i & 1) ^ 1, &ab)) decay_error(8, ab);
+#pragma unroll
+      for (int k = 0; k < 8; ++k)
+#pragma unroll
+        for (int q = 0; q < 2; ++q) {
+          const float2 m = __fmul2_rn(make_float2(a[4 * k + 2 * q], a[4 * k + 2 * q + 1]), w[k + 1 - q]);
+          a[4 * k + 2 * q] = m.x, a[4 * k + 2 * q + 1] = m.y;
+        }
+      store_16x64(smem_u32(smem + Sh::kOffP + s * kBlk) + 16 * warp * 128, lane, a);
+      fence_proxy_async_smem();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(&intra_ready[s]);
+    }
+  } else if (warp < 8) {
+    // ------------------------------------------------ weighted q (warps 4-7)
+    const int ct = tid - 128, ch = ct & 7, rr = ct >> 3;
+    const uint32_t piece = rr * 128 + ((ch ^ (rr & 7)) << 4);
+    RowWeight w[4];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) w[k].set(decay_pow(l2, (float)(rr + 16 * k)));
+    for (int i = 0; i < cnt; ++i) {
+      const int s = i % kN, cb = i & 1, n = min(kC, L - sg.token_of(q0 + i));
+      if (!mbar_wait(&fq[s], (i / kN) & 1, &ab)) decay_error(16, ab);
+      if (i >= 2 && !mbar_wait(&conv_empty[cb], ((i >> 1) & 1) ^ 1, &ab)) decay_error(32, ab);
+      const uint32_t ys = smem_u32(smem + Sh::kOffQ + s * Sh::kSlot) + piece;
+      const uint32_t cs = smem_u32(smem + Sh::kOffConv + cb * kTerms * kBlk) + piece;
+      if (n == kC) {
+        uint4 u[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) u[k] = lds_v4(ys + k * 2048);
+#pragma unroll
+        for (int k = 0; k < 4; ++k) weigh_piece<kTerms, kBlk>(u[k], w[k], cs + k * 2048);
+      } else {
+        if (!mbar_wait(&fg[s], (i / kN) & 1, &ab)) decay_error(16, ab);
+        weigh_end<kTerms, kBlk>(ys, smem_u32(smem + Sh::kOffG + s * Sh::kSlot) + piece, cs, rr, n, l2,
+                                1.f, true);
+      }
+      fence_proxy_async_smem();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(&state_ready[cb]);
+    }
+  } else if (warp < 12) {
+    // --------------------- the state, transposed (rows of d_o), in registers
+    const int sw = warp - 8;
+    const uint32_t src = tmem + ((uint32_t)(32 * sw) << 16) + Sh::kColDs;
+    float S[32];
+#pragma unroll
+    for (int i = 0; i < 32; ++i) S[i] = 0.f;
+    if (lane == 0) mbar_arrive(&state_ready[0]);
+    if (rank > 0) {  // the segments before
+      grid_dep_wait();
+      const float *part = p.part + bh * p.ranks * D * D + (tid - 8 * 32);
+      for (int s = 0; s < rank; ++s) {
+        const float f = decay_pow(l2, (float)(rank - 1 - s) * p.seg * kC);
+#pragma unroll
+        for (int i = 0; i < 32; ++i)
+          S[i] = fmaf(f, __ldcg(part + ((size_t)s * 32 + i) * 128), S[i]);
+      }
+    }
+    if (p.init) {
+      // tokens from the last one, which the first state belongs to, to this segment
+      const float n = q0 == 0 ? 0.f : (float)(L - 1 - (sg.nc - q0) * kC);
+      const float f = decay_pow(l2, n) * p.init_scale;
+      const float *s0 = p.init + bh * V * V;
+#pragma unroll
+      for (int i = 0; i < 32; ++i) {
+        int e;
+        const int d = state_at<64>(sw, lane, i, &e);
+        if (V == D || (d < V && e < V)) S[i] = fmaf(f, __ldg(s0 + d * V + e), S[i]);
+      }
+    }
+    for (int i = 0; i < cnt; ++i) {
+      const int s = i % kN;
+      if (!mbar_wait(&eq[s], ((i / kN) & 1) ^ 1, &ab)) decay_error(128, ab);
+      if (!mbar_wait(&eg[s], ((i / kN) & 1) ^ 1, &ab)) decay_error(128, ab);
+      store_16x64(smem_u32(smem + Sh::kOffQ + s * Sh::kSlot + kBlk) + 16 * sw * 128, lane, S);
+      store_16x64_t(smem_u32(smem + Sh::kOffG + s * Sh::kSlot + kBlk), 2 * sw, lane, S);
+      fence_proxy_async_smem();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(&s_full[i & 1]);
+      const int n = min(kC, L - sg.token_of(q0 + i));
+      if (!mbar_wait(ds_full, i & 1, &ab)) decay_error(64, ab);
+      tc_fence_after();
+      take_state<64, false>(S, src, decay_pow(l2, (float)(q0 + i == 0 ? n - 1 : kC)));
+      tc_fence_before();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(&state_ready[(i + 1) & 1]);
+    }
+    if (p.fin && sg.last) {
+      const float f = p.fin_scale * decay_pow(l2, 1.f);
+#pragma unroll
+      for (int i = 0; i < 32; ++i) {
+        int e;
+        const int d = state_at<64>(sw, lane, i, &e);
+        if (V == D || (d < V && e < V)) p.fin[bh * V * V + d * V + e] = S[i] * f;
+      }
+    }
+  } else {
+    // ---------------------------------------------------------------- results
+    const int ow = warp - 12, r0 = 16 * ow + (lane >> 2);
+    const uint32_t quarter = tmem + ((uint32_t)(32 * ow) << 16);
+    const uint32_t stage = smem_u32(smem + Sh::kOffOut + ow * 2048);
+    float u[2];
+#pragma unroll
+    for (int k = 0; k < 2; ++k) u[k] = p.scale * decay_pow(l2, (float)(kC - (r0 + 8 * k)));
+    float s[32];
+    auto load_inter = [&](int job) {
+      const int w = job & 1;
+      if (!mbar_wait(&sc_full[w], (job >> 1) & 1, &ab)) decay_error(256, ab);
+      tc_fence_after();
+      tmem_ld_16x64(quarter + Sh::kColSc + 128 * w + 64, s);
+      tmem_ld_wait_regs(s);
+      tc_fence_before();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(&score_ready[w]);
+    };
+    if (lane == 0) {
+      mbar_arrive(&score_ready[0]), mbar_arrive(&score_ready[1]);
+      mbar_arrive(&intra_ready[0]), mbar_arrive(&intra_ready[1]);
+    }
+    load_inter(0);
+    for (int job = 0; job < jobs; ++job) {
+      const int i = job >> 1, w = job & 1, t0 = sg.token_of(q0 + i), n = min(kC, L - t0);
+      float ur[2] = {u[0], u[1]};
+      if (q0 + i == 0) {
+#pragma unroll
+        for (int k = 0; k < 2; ++k)
+          ur[k] = p.scale * decay_pow(l2, (float)max(n - 1 - (r0 + 8 * k), 0));
+      }
+      if (!mbar_wait(&o_full[w], i & 1, &ab)) decay_error(256, ab);
+      tc_fence_after();
+      float a[32];
+      tmem_ld_16x64(quarter + Sh::kColIntra + 64 * w, a);
+      tmem_ld_wait_regs(a);
+      tc_fence_before();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(&intra_ready[w]);
+#pragma unroll
+      for (int k = 0; k < 32; k += 2) {
+        const float f = ur[(k >> 1) & 1];
+        const float2 r = __ffma2_rn(make_float2(f, f), make_float2(s[k], s[k + 1]),
+                                    make_float2(a[k], a[k + 1]));
+        a[k] = r.x, a[k + 1] = r.y;
+      }
+      if (job + 1 < jobs) load_inter(job + 1);
+      O *dst = (O *)(w ? kp.dk : p.out) + first + (size_t)t0 * orow;
+      write_rows<V, O>(dst, orow, stage, ow, lane, n, a);
     }
   }
   tc_fence_before();
@@ -1067,6 +1458,57 @@ cudaError_t launch_d(const ScanArgs &a, const TcParams &p, const CUtensorMap &tx
                    : launch<D, V, 2, __nv_bfloat16>(a, p, tx, ty, tz, st);
 }
 
+template <int V, int kTerms, typename O>
+cudaError_t launch_kv(const ScanArgs &a, const KvParams &kp, const CUtensorMap &tk,
+                      const CUtensorMap &tv, const CUtensorMap &tq, const CUtensorMap &tg,
+                      cudaStream_t st) {
+  const TcParams &p = kp.c;
+  cudaError_t e;
+  if (p.ranks > 1) {
+    using Sh = OwnShape<64, kTerms>;
+    const auto kernel = own_state_kernel<64, kTerms>;
+    if ((e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                  Sh::kSmem)) != cudaSuccess)
+      return e;
+    kernel<<<dim3(p.ranks - 1, a.H, a.B), Sh::kThreads, Sh::kSmem, st>>>(p, tq, tg);
+    count_launch();
+    if ((e = cudaGetLastError()) != cudaSuccess) return e;
+  }
+  using Sh = KvShape<kTerms>;
+  const auto kernel = kv_kernel<V, kTerms, O>;
+  if ((e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, Sh::kSmem)) !=
+      cudaSuccess)
+    return e;
+  const dim3 grid(p.ranks, a.H, a.B);
+  count_launch();
+  if (p.ranks > 1)  // as the scan behind its own-state kernel
+    return launch_pdl(kernel, grid, dim3(Sh::kThreads), Sh::kSmem, st, kp, tk, tv, tq, tg);
+  kernel<<<grid, Sh::kThreads, Sh::kSmem, st>>>(kp, tk, tv, tq, tg);
+  return cudaGetLastError();
+}
+
+template <int V>
+cudaError_t launch_kv_v(const ScanArgs &a, const KvParams &kp, const CUtensorMap &tk,
+                        const CUtensorMap &tv, const CUtensorMap &tq, const CUtensorMap &tg,
+                        cudaStream_t st) {
+  if (a.fin)
+    return a.out_f32 ? launch_kv<V, 3, float>(a, kp, tk, tv, tq, tg, st)
+                     : launch_kv<V, 3, __nv_bfloat16>(a, kp, tk, tv, tq, tg, st);
+  return a.out_f32 ? launch_kv<V, 2, float>(a, kp, tk, tv, tq, tg, st)
+                   : launch_kv<V, 2, __nv_bfloat16>(a, kp, tk, tv, tq, tg, st);
+}
+
+TcParams tc_params(const ScanArgs &a, float *scratch) {
+  TcParams p = {};
+  p.out = a.out, p.log_decay = a.log_decay, p.seq_lens = a.seq_lens;
+  p.init = a.init, p.fin = a.fin, p.part = scratch;
+  p.init_scale = a.init_scale, p.fin_scale = a.fin_scale, p.scale = a.scale;
+  p.N = a.N, p.H = a.H, p.gx = a.gx, p.gy = a.gy, p.gz = a.gz;
+  p.zero_pad = a.zero_pad, p.init_t = a.init_t, p.reverse = a.reverse;
+  p.seg = segment_for(a), p.ranks = ((a.N + kC - 1) / kC + p.seg - 1) / p.seg;
+  return p;
+}
+
 }  // namespace
 
 bool tc_scan_supports(const ScanArgs &a) {
@@ -1092,16 +1534,26 @@ cudaError_t tc_scan(const ScanArgs &a, float *scratch, cudaStream_t st) {
   if ((e = make_map(&tx, a.x, a.B, a.N, a.H / a.gx, a.D, a.sx)) != cudaSuccess) return e;
   if ((e = make_map(&ty, a.y, a.B, a.N, a.H / a.gy, a.D, a.sy)) != cudaSuccess) return e;
   if ((e = make_map(&tz, a.z, a.B, a.N, a.H / a.gz, a.D, a.sz)) != cudaSuccess) return e;
-  TcParams p = {};
-  p.out = a.out, p.log_decay = a.log_decay, p.seq_lens = a.seq_lens;
-  p.init = a.init, p.fin = a.fin, p.part = scratch;
-  p.init_scale = a.init_scale, p.fin_scale = a.fin_scale, p.scale = a.scale;
-  p.N = a.N, p.H = a.H, p.gx = a.gx, p.gy = a.gy, p.gz = a.gz;
-  p.zero_pad = a.zero_pad, p.init_t = a.init_t, p.reverse = a.reverse;
-  p.seg = segment_for(a), p.ranks = ((a.N + kC - 1) / kC + p.seg - 1) / p.seg;
+  const TcParams p = tc_params(a, scratch);
   if (a.D == 32) return launch_d<64, 32>(a, p, tx, ty, tz, st);
   return a.D == 64 ? launch_d<64, 64>(a, p, tx, ty, tz, st)
                    : launch_d<128, 128>(a, p, tx, ty, tz, st);
+}
+
+bool tc_kv_supports(const ScanArgs &dv) { return dv.D <= 64 && tc_scan_supports(dv); }
+
+cudaError_t tc_kv(const ScanArgs &dv, const void *v, const long long (&sv)[2], void *dk,
+                  float *scratch, cudaStream_t st) {
+  CUtensorMap tk, tv, tq, tg;
+  cudaError_t e;
+  const int kv_heads = dv.H / dv.gx;
+  if ((e = make_map(&tk, dv.x, dv.B, dv.N, kv_heads, dv.D, dv.sx)) != cudaSuccess) return e;
+  if ((e = make_map(&tv, v, dv.B, dv.N, kv_heads, dv.D, sv)) != cudaSuccess) return e;
+  if ((e = make_map(&tq, dv.y, dv.B, dv.N, dv.H, dv.D, dv.sy)) != cudaSuccess) return e;
+  if ((e = make_map(&tg, dv.z, dv.B, dv.N, dv.H, dv.D, dv.sz)) != cudaSuccess) return e;
+  const KvParams kp = {tc_params(dv, scratch), dk};
+  return dv.D == 32 ? launch_kv_v<32>(dv, kp, tk, tv, tq, tg, st)
+                    : launch_kv_v<64>(dv, kp, tk, tv, tq, tg, st);
 }
 
 unsigned decay_device_error(bool reset) {

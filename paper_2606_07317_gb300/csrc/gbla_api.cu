@@ -1066,7 +1066,7 @@ gbla_status gbla_decay_attention_backward(
   if (G > 1) grad[0].out = plane[0], grad[1].out = plane[1];
   if (together) {
     Scratch ws;
-    if ((s = ws.alloc(sizeof(float) * tc_scan_floats(grad[0]), st)) != GBLA_OK) return s;
+    if ((s = ws.alloc(sizeof(float) * tc_kv_floats(grad[0]), st)) != GBLA_OK) return s;
     if ((s = from_cuda(tc_kv(grad[0], v, grad[1].sx, grad[1].out, (float *)ws.ptr, st))) != GBLA_OK)
       return s;
   }

@@ -1395,8 +1395,9 @@ int sm_count() {
 // whole rounds of CTAs over the SMs.  Lengths that only the device knows are taken
 // to be a quarter of the longest on average; the kernels then last as long as all
 // the work over the SMs and half a segment of tail, or as their longest CTA.
-int segment_for(const ScanArgs &a) {
-  const double fill = a.D > 64 ? 5 : 9, own_chunk = 0.6;
+// The pass over keys and values takes `chunk` = 1.6 scanned chunks a chunk.
+int segment_for(const ScanArgs &a, double chunk) {
+  const double fill = (a.D > 64 ? 5 : 9) / chunk, own_chunk = 0.6 / chunk;
   const int nc = (a.N + kC - 1) / kC, sms = sm_count();
   const double pairs = (double)a.B * a.H;
   auto rounds = [&](double ctas) { return (double)(long long)(ctas / sms + 0.999999); };
@@ -1498,14 +1499,14 @@ cudaError_t launch_kv_v(const ScanArgs &a, const KvParams &kp, const CUtensorMap
                    : launch_kv<V, 2, __nv_bfloat16>(a, kp, tk, tv, tq, tg, st);
 }
 
-TcParams tc_params(const ScanArgs &a, float *scratch) {
+TcParams tc_params(const ScanArgs &a, float *scratch, double chunk = 1) {
   TcParams p = {};
   p.out = a.out, p.log_decay = a.log_decay, p.seq_lens = a.seq_lens;
   p.init = a.init, p.fin = a.fin, p.part = scratch;
   p.init_scale = a.init_scale, p.fin_scale = a.fin_scale, p.scale = a.scale;
   p.N = a.N, p.H = a.H, p.gx = a.gx, p.gy = a.gy, p.gz = a.gz;
   p.zero_pad = a.zero_pad, p.init_t = a.init_t, p.reverse = a.reverse;
-  p.seg = segment_for(a), p.ranks = ((a.N + kC - 1) / kC + p.seg - 1) / p.seg;
+  p.seg = segment_for(a, chunk), p.ranks = ((a.N + kC - 1) / kC + p.seg - 1) / p.seg;
   return p;
 }
 
@@ -1522,11 +1523,16 @@ bool tc_scan_supports(const ScanArgs &a) {
   return major == 10 && minor == 3 && encode_fn() != nullptr;
 }
 
-size_t tc_scan_floats(const ScanArgs &a) {
-  const int seg = segment_for(a), ranks = ((a.N + kC - 1) / kC + seg - 1) / seg;
+constexpr double kKvChunk = 1.6;
+
+static size_t part_floats(const ScanArgs &a, double chunk) {
+  const int seg = segment_for(a, chunk), ranks = ((a.N + kC - 1) / kC + seg - 1) / seg;
   const size_t d = a.D < 64 ? 64 : a.D;
   return ranks > 1 ? (size_t)a.B * a.H * ranks * d * d : 0;
 }
+
+size_t tc_scan_floats(const ScanArgs &a) { return part_floats(a, 1); }
+size_t tc_kv_floats(const ScanArgs &dv) { return part_floats(dv, kKvChunk); }
 
 cudaError_t tc_scan(const ScanArgs &a, float *scratch, cudaStream_t st) {
   CUtensorMap tx, ty, tz;
@@ -1551,7 +1557,7 @@ cudaError_t tc_kv(const ScanArgs &dv, const void *v, const long long (&sv)[2], v
   if ((e = make_map(&tv, v, dv.B, dv.N, kv_heads, dv.D, sv)) != cudaSuccess) return e;
   if ((e = make_map(&tq, dv.y, dv.B, dv.N, dv.H, dv.D, dv.sy)) != cudaSuccess) return e;
   if ((e = make_map(&tg, dv.z, dv.B, dv.N, dv.H, dv.D, dv.sz)) != cudaSuccess) return e;
-  const KvParams kp = {tc_params(dv, scratch), dk};
+  const KvParams kp = {tc_params(dv, scratch, kKvChunk), dk};
   return dv.D == 32 ? launch_kv_v<32>(dv, kp, tk, tv, tq, tg, st)
                     : launch_kv_v<64>(dv, kp, tk, tv, tq, tg, st);
 }

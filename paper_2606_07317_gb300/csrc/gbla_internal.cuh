@@ -212,6 +212,7 @@ cudaError_t tc_scan(const ScanArgs &a, float *scratch, cudaStream_t st);
 // The gradients of values (the scan dv: x = k, y = q, z = d_o, in reverse) and of
 // keys in one pass: D <= 64.  v with its strides; dk like dv.out.
 bool tc_kv_supports(const ScanArgs &dv);
+size_t tc_kv_floats(const ScanArgs &dv);
 cudaError_t tc_kv(const ScanArgs &dv, const void *v, const long long (&sv)[2], void *dk,
                   float *scratch, cudaStream_t st);
 unsigned decay_device_error(bool reset);

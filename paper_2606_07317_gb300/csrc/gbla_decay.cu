@@ -10,6 +10,7 @@
 // powers counted from the chunk's other end.
 #include <math.h>
 
+#include "gbla_decay.cuh"
 #include "gbla_internal.cuh"
 #include "gbla_sm100.cuh"
 
@@ -17,14 +18,6 @@ namespace gbla {
 namespace {
 
 using namespace sm100;
-
-// gamma^n for n >= 0 with l2 = log2 gamma; gamma^0 is 1 also for gamma = 0.
-__device__ __forceinline__ float decay_pow(float l2, float n) {
-  return n == 0.f ? 1.f : exp2f(n * l2);
-}
-__device__ __forceinline__ float log2_decay(const float *log_decay, int h) {
-  return __ldg(log_decay + h) * 1.4426950408889634f;
-}
 
 __device__ __forceinline__ float to_f(float v) { return v; }
 __device__ __forceinline__ float to_f(__nv_bfloat16 v) { return __bfloat162float(v); }
@@ -146,6 +139,7 @@ __global__ void __launch_bounds__(kThreadsOf<D>, ScanShape<D, kState>::kBlocks)
   if (seg >= ns && !(seg == 0 && !kState && p.fin)) return;
   if (kState && seg == last) return;  // nobody reads it
   const float l2 = log2_decay(p.log_decay, h);
+  const DecayFactor chunk_factor = decay_factor(__ldg(p.log_decay + h) * kC);
   if (tid <= kC) gp[tid] = decay_pow(l2, (float)tid);
 
   // rows sy + i, columns 4 sx + c and, from c = 4 on, 32 + 4 sx + c - 4
@@ -274,11 +268,11 @@ __global__ void __launch_bounds__(kThreadsOf<D>, ScanShape<D, kState>::kBlocks)
       }
     }
     // the state after the chunk
-    const float carry = gp[span];
+    const DecayFactor carry = span == kC ? chunk_factor : DecayFactor{gp[span], 0.f};
 #pragma unroll
     for (int i = 0; i < kSr; ++i)
 #pragma unroll
-      for (int c = 0; c < kSc; ++c) S[i][c] *= carry;
+      for (int c = 0; c < kSc; ++c) S[i][c] = fmaf(carry.hi, S[i][c], carry.lo * S[i][c]);
 #pragma unroll 2
     for (int j = 0; j < n; ++j) {
       const float w = gp[p.reverse ? j : n - 1 - j];
@@ -480,17 +474,17 @@ __global__ void __launch_bounds__(StepShape<D>::kThreads) step_kernel(
   for (int i = tid; i < 2 * D; i += Sh::kThreads)
     qk[i / D][i % D] = i < D ? to_f(q[b * sq + (long long)h * D + i])
                              : to_f(k[b * sk + (long long)(h / G) * D + i - D]);
-  const float gamma = decay_pow(log2_decay(log_decay, h), 1.f);
+  const DecayFactor gamma = decay_factor(__ldg(log_decay + h));
   __syncthreads();
   float a[4] = {};
 #pragma unroll
   for (int i = 0; i < Sh::kRows; ++i) {
     const int d = g + i * Sh::kGroups;
     const float kd = qk[1][d], qd = qk[0][d];
-    r[i].x = fmaf(kd, vv[0], gamma * r[i].x);
-    r[i].y = fmaf(kd, vv[1], gamma * r[i].y);
-    r[i].z = fmaf(kd, vv[2], gamma * r[i].z);
-    r[i].w = fmaf(kd, vv[3], gamma * r[i].w);
+    r[i].x = fmaf(kd, vv[0], fmaf(gamma.hi, r[i].x, gamma.lo * r[i].x));
+    r[i].y = fmaf(kd, vv[1], fmaf(gamma.hi, r[i].y, gamma.lo * r[i].y));
+    r[i].z = fmaf(kd, vv[2], fmaf(gamma.hi, r[i].z, gamma.lo * r[i].z));
+    r[i].w = fmaf(kd, vv[3], fmaf(gamma.hi, r[i].w, gamma.lo * r[i].w));
     s[d * Sh::kCols] = r[i];
     a[0] = fmaf(qd, r[i].x, a[0]);
     a[1] = fmaf(qd, r[i].y, a[1]);

@@ -38,6 +38,7 @@
 // g_decay_error and raises the CTA's abort flag.
 #include <mutex>
 
+#include "gbla_decay.cuh"
 #include "gbla_internal.cuh"
 #include "gbla_sm100.cuh"
 
@@ -103,9 +104,6 @@ struct TcParams {
 __device__ __forceinline__ void decay_error(unsigned code, const AbortFlag &ab) {
   if (!ab.raised()) atomicOr(&g_decay_error, code);
   ab.raise();
-}
-__device__ __forceinline__ float decay_pow(float l2, float n) {
-  return n == 0.f ? 1.f : exp2f(n * l2);
 }
 
 // 16 lanes x 64 columns: thread t gets rows t / 4 (v[4 i], v[4 i + 1]) and
@@ -324,14 +322,14 @@ __device__ __forceinline__ int state_at(int sw, int lane, int i, int *e) {
   return 32 * (sw & 3) + lane;
 }
 
-// S = S + f v or S = f S + v over a state thread's values, from the columns at
-// src (D = 64: the small terms' columns first).
+// S = S + f v (own) or S = f S + v over a state thread's values, from the columns
+// at src (D = 64: the small terms' columns first).
 template <int D, bool kOwn, int kNV>
-__device__ __forceinline__ void take_state(float (&S)[kNV], uint32_t src, float f) {
-  const float2 f2 = make_float2(f, f);
+__device__ __forceinline__ void take_state(float (&S)[kNV], uint32_t src, DecayFactor f) {
+  const float2 f2 = make_float2(f.hi, f.hi), g2 = make_float2(f.lo, f.lo);
   auto add = [&](int i, float2 v) {
     const float2 q = make_float2(S[i], S[i + 1]);
-    const float2 r = kOwn ? __ffma2_rn(f2, v, q) : __ffma2_rn(f2, q, v);
+    const float2 r = kOwn ? __ffma2_rn(f2, v, q) : __ffma2_rn(f2, q, __ffma2_rn(g2, q, v));
     S[i] = r.x, S[i + 1] = r.y;
   };
   if constexpr (D == 64) {
@@ -383,12 +381,13 @@ struct Segment {
 // The state of each segment but the last, without what comes before it.  Chunks
 // go by from the segment's end in scan order to its start; kGroup of them add up
 // in TMEM (their distance from the first is in the weights), then the state warps
-// take the sum.  Warps: 0-7 form v_j y_j (two groups, alternate chunks), the next
+// take the sum.  (The tensor cores' sums are cut, not rounded: where the state is a
+// result, 96 additions in a row showed at 1e-6 of it, so there are fewer.)  Warps: 0-7 form v_j y_j (two groups, alternate chunks), the next
 // 4 (D = 128: 8) hold the state, then loads and MMAs.
-constexpr int kGroup = 8;
 
 template <int D, int kTerms>
 struct OwnShape {
+  static constexpr int kGroup = kTerms == 3 ? 2 : 8;
   static constexpr int kB = D / 64, kTile = kB * kBlk;
   // Even, so that a slot always meets the same one of the two groups: a parity
   // wait tells a phase from the one before it only, and a group that missed a
@@ -483,17 +482,17 @@ __global__ void __launch_bounds__(OwnShape<D, kTerms>::kThreads, OwnShape<D, kTe
         return ok;
       };
       for (int g = 0; g < sg.cnt && ok; ++g) {
-        const int cb = g & 1, q = g / kGroup, db = q & 1;
-        if (g % kGroup == 0 && q >= 2 && !wait(&ds_empty[db], ((q >> 1) & 1) ^ 1)) break;
+        const int cb = g & 1, q = g / Sh::kGroup, db = q & 1;
+        if (g % Sh::kGroup == 0 && q >= 2 && !wait(&ds_empty[db], ((q >> 1) & 1) ^ 1)) break;
         if (!wait(&conv_full[cb], (g >> 1) & 1)) break;
         tc_fence_after();
         state_product<D, kTerms, Sh::kTile>(
             tmem + 128 * db, base + Sh::kOffZ + (g % Sh::kNZ) * Sh::kTile,
-            base + Sh::kOffConv + cb * kTerms * Sh::kTile, g % kGroup != 0);
+            base + Sh::kOffConv + cb * kTerms * Sh::kTile, g % Sh::kGroup != 0);
         mma_commit(&conv_empty[cb]);
         mma_commit(&ey[g % Sh::kNY]);
         mma_commit(&ez[g % Sh::kNZ]);
-        if (g % kGroup == kGroup - 1 || g == sg.cnt - 1) mma_commit(&ds_full[db]);
+        if (g % Sh::kGroup == Sh::kGroup - 1 || g == sg.cnt - 1) mma_commit(&ds_full[db]);
       }
       mma_commit(drained);  // nothing is in flight when TMEM is freed
       if (!mbar_wait(drained, 0, nullptr)) decay_error(512, ab);
@@ -509,7 +508,7 @@ __global__ void __launch_bounds__(OwnShape<D, kTerms>::kThreads, OwnShape<D, kTe
     for (int g = warp >> 2; g < sg.cnt; g += 2) {
       const int sy = g % Sh::kNY, sz = g % Sh::kNZ, cb = g & 1;
       const int n = min(kC, sg.L - token_at(g));
-      const float gain = decay_pow(l2, (float)(g % kGroup) * kC);
+      const float gain = decay_pow(l2, (float)(g % Sh::kGroup) * kC);
       if (!mbar_wait(&fy[sy], (g / Sh::kNY) & 1, &ab)) decay_error(16, ab);
       if (!mbar_wait(&fz[sz], (g / Sh::kNZ) & 1, &ab)) decay_error(16, ab);  // for the MMAs
       if (g >= 2 && !mbar_wait(&conv_empty[cb], ((g >> 1) & 1) ^ 1, &ab)) decay_error(32, ab);
@@ -542,10 +541,10 @@ __global__ void __launch_bounds__(OwnShape<D, kTerms>::kThreads, OwnShape<D, kTe
     float S[kNV];
 #pragma unroll
     for (int i = 0; i < kNV; ++i) S[i] = 0.f;
-    for (int q = 0; q * kGroup < sg.cnt; ++q) {
+    for (int q = 0; q * Sh::kGroup < sg.cnt; ++q) {
       if (!mbar_wait(&ds_full[q & 1], (q >> 1) & 1, &ab)) decay_error(64, ab);
       tc_fence_after();
-      take_state<D, true>(S, src + 128 * (q & 1), decay_pow(l2, (float)q * (kGroup * kC)));
+      take_state<D, true>(S, src + 128 * (q & 1), {decay_pow(l2, (float)q * (Sh::kGroup * kC)), 0.f});
       tc_fence_before();
       __syncwarp();
       if (lane == 0) mbar_arrive(&ds_empty[q & 1]);
@@ -826,6 +825,7 @@ __global__ void __launch_bounds__(Shape<D, kTerms>::kThreads, 1)
   } else if (warp < 8 + Sh::kSWarps) {
     // ------------------------------------------------- the state, in registers
     const int sw = warp - 8;
+    const DecayFactor chunk_factor = decay_factor(__ldg(p.log_decay + h) * kC);
     float S[kNV];
 #pragma unroll
     for (int i = 0; i < kNV; ++i) S[i] = 0.f;
@@ -879,7 +879,7 @@ __global__ void __launch_bounds__(Shape<D, kTerms>::kThreads, 1)
       const int span = !p.reverse ? n : (q0 + j == 0 ? n - 1 : kC);
       if (!mbar_wait(ds_full, j & 1, &ab)) decay_error(64, ab);
       tc_fence_after();
-      take_state<D, false>(S, src, decay_pow(l2, (float)span));
+      take_state<D, false>(S, src, span == kC ? chunk_factor : DecayFactor{decay_pow(l2, (float)span), 0.f});
       tc_fence_before();
       __syncwarp();
       if (lane == 0) mbar_arrive(&state_ready[(j + 1) % Sh::kConv]);
@@ -1234,6 +1234,7 @@ __global__ void __launch_bounds__(KvShape<kTerms>::kThreads, 1)
     // --------------------- the state, transposed (rows of d_o), in registers
     const int sw = warp - 8;
     const uint32_t src = tmem + ((uint32_t)(32 * sw) << 16) + Sh::kColDs;
+    const DecayFactor chunk_factor = decay_factor(__ldg(p.log_decay + h) * kC);
     float S[32];
 #pragma unroll
     for (int i = 0; i < 32; ++i) S[i] = 0.f;
@@ -1272,7 +1273,7 @@ __global__ void __launch_bounds__(KvShape<kTerms>::kThreads, 1)
       const int n = min(kC, L - sg.token_of(q0 + i));
       if (!mbar_wait(ds_full, i & 1, &ab)) decay_error(64, ab);
       tc_fence_after();
-      take_state<64, false>(S, src, decay_pow(l2, (float)(q0 + i == 0 ? n - 1 : kC)));
+      take_state<64, false>(S, src, q0 + i > 0 ? chunk_factor : DecayFactor{decay_pow(l2, (float)(n - 1)), 0.f});
       tc_fence_before();
       __syncwarp();
       if (lane == 0) mbar_arrive(&state_ready[(i + 1) & 1]);

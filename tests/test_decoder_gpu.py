@@ -324,6 +324,36 @@ def test_step(B, H, Hk, D, dtype):
     _close(o, ref, om, u, dtype, "o")
 
 
+def test_steps_do_not_drift():
+    """A weak decay over 4096 steps (keys of zero) against the exact power: each step rounds
+    once to 2^-24 at random, sqrt(n) 2^-24 of the norm (times 8); a decay held in one float
+    would be off by up to n 2^-25."""
+    n, ld = 4096, torch.tensor([-2.9e-4, -1.7e-4, -1e-3], device="cuda")
+    S0 = torch.randn((1, 3, 64, 64), generator=torch.Generator().manual_seed(5))
+    S, z = dev(S0), torch.zeros((1, 1, 3, 64), device="cuda")
+    for _ in range(n):
+        gbla.decay_attention_step(z, z, z, ld, S)
+    want = S0.double() * (n * ld.cpu().double()).exp()[None, :, None, None]
+    for h in range(3):
+        got = S[0, h].cpu().double()
+        assert (got - want[0, h]).norm() <= 8 * n ** 0.5 * 2.0 ** -24 * want[0, h].norm(), h
+
+
+@pytest.mark.parametrize("D,dtype", [(32, "bf16"), (64, "bf16"), (128, "bf16"), (64, "fp32")])
+def test_long_state_with_a_weak_decay(D, dtype):
+    """The state after 32768 tokens at a horizon of 4096 against the explicit sum: fp32
+    rounding at random, 32 x 2^-24 of the norm, no drift with the length."""
+    c = Case(95, 1, 32768, 2, 2, D, dtype)
+    q, k, v = (c.tok(2) for _ in range(3))
+    ld = torch.log1p(-torch.exp2(torch.tensor([-12.0, -11.3])))
+    _, S = gbla.decay_attention(dev(q), dev(k), dev(v), dev(ld), return_state=True)
+    t = torch.arange(c.N, dtype=torch.float64)
+    for h in range(2):
+        w = ((c.N - 1 - t) * ld[h].double()).exp()[:, None]
+        want = (k[0, :, h].double() * w).T @ v[0, :, h].double()
+        assert (S[0, h].cpu().double() - want).norm() <= 32 * 2.0 ** -24 * want.norm(), h
+
+
 def test_step_rows_without_a_sequence():
     c = Case(62, 4, 1, 2, 2, 64, "bf16")
     q = dev(c.tok(2))

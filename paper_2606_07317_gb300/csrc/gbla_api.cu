@@ -864,12 +864,21 @@ gbla_status check_rotate(RotateArgs *a, View *vq, View *vk, const void *q, const
   return GBLA_OK;
 }
 
-// A scan with the tensor-core family or the CUDA-core one, its scratch from the pool.
-gbla_status run_scan(const ScanArgs &a, bool tc, cudaStream_t st) {
-  Scratch ws;
-  gbla_status s = ws.alloc(sizeof(float) * (tc ? tc_scan_floats(a) : simt_scan_floats(a)), st);
-  if (s != GBLA_OK) return s;
-  return from_cuda(tc ? tc_scan(a, (float *)ws.ptr, st) : simt_scan(a, (float *)ws.ptr, st));
+// n scans of the same sizes with the tensor-core family (one after the other) or
+// the CUDA-core one (side by side), their scratch from the pool.
+gbla_status run_scans(const ScanArgs *a, int n, bool tc, cudaStream_t st) {
+  const bool apart = tc || (long long)a->B * n > kMaxBH;
+  for (int i = 0; i < n; i += apart ? 1 : n) {
+    const int m = apart ? 1 : n;
+    Scratch ws;
+    const size_t floats = tc ? tc_scan_floats(a[i]) : simt_scan_floats(a[i], m);
+    gbla_status s = ws.alloc(sizeof(float) * floats, st);
+    if (s != GBLA_OK) return s;
+    s = from_cuda(tc ? tc_scan(a[i], (float *)ws.ptr, st)
+                     : simt_scan(a + i, m, (float *)ws.ptr, st));
+    if (s != GBLA_OK) return s;
+  }
+  return GBLA_OK;
 }
 
 gbla_status scan_family(const ScanArgs &a, gbla_algo algo, bool *tc) {
@@ -998,7 +1007,7 @@ gbla_status gbla_decay_attention(const void *q, const void *k, const void *v,
   a.B = B, a.N = N, a.H = H, a.D = D, a.scale = scale, a.dtype = dtype;
   bool tc = false;
   if ((s = scan_family(a, algo, &tc)) != GBLA_OK) return s;
-  return run_scan(a, tc, st);
+  return run_scans(&a, 1, tc, st);
 }
 
 gbla_status gbla_decay_attention_backward(
@@ -1042,40 +1051,44 @@ gbla_status gbla_decay_attention_backward(
   a.B = B, a.N = N, a.H = H, a.D = D, a.scale = scale, a.dtype = dtype;
   bool tc = false;
   if ((s = scan_family(a, algo, &tc)) != GBLA_OK) return s;
-  if ((s = run_scan(a, tc, st)) != GBLA_OK) return s;
   // In reverse A_t = gamma A_{t+1} + q_t d_o_t^T (dstate_out at the end; held
   // without the scale): dk_t = A_t v_t, dv_t = A_t^T k_t, dstate_in = gamma A_0.
   // Shared heads: per query head in fp32, then summed.
-  ScanArgs grad[2] = {a, a};  // dv, dk
-  for (int i = 0; i < 2; ++i) {
-    ScanArgs &r = grad[i];
-    r.x = i ? v : k, r.y = i ? d_o : q, r.z = i ? q : d_o;
-    const View &rx = i ? vv : vk, &ry = i ? vo : vq, &rz = i ? vq : vo;
+  ScanArgs scan[3] = {a, a, a};  // dq, dv, dk
+  for (int i = 1; i < 3; ++i) {
+    ScanArgs &r = scan[i];
+    const bool keys = i == 2;
+    r.x = keys ? v : k, r.y = keys ? d_o : q, r.z = keys ? q : d_o;
+    const View &rx = keys ? vv : vk, &ry = keys ? vo : vq, &rz = keys ? vq : vo;
     for (int j = 0; j < 2; ++j) r.sx[j] = rx.s[j], r.sy[j] = ry.s[j], r.sz[j] = rz.s[j];
     r.gx = G, r.gy = r.gz = 1;
-    r.out = i ? dk : dv, r.out_f32 = G > 1;
-    r.init = dstate_out, r.init_t = i == 1, r.init_scale = 1.f / scale;
-    r.fin = i ? nullptr : dstate_in, r.fin_scale = scale;
+    r.out = keys ? dk : dv, r.out_f32 = G > 1;
+    r.init = dstate_out, r.init_t = keys, r.init_scale = 1.f / scale;
+    r.fin = keys ? nullptr : dstate_in, r.fin_scale = scale;
     r.reverse = true;
   }
-  const bool together = tc && tc_kv_supports(grad[0]);
-  const size_t plane_floats = G > 1 ? round_up(tok * H * D, 64) : 0;
+  const size_t plane_floats = round_up(tok * H * D, 64);
   Scratch planes;
-  if ((s = planes.alloc(sizeof(float) * plane_floats * (together ? 2 : 1), st)) != GBLA_OK) return s;
-  float *plane[2] = {(float *)planes.ptr, (float *)planes.ptr + (together ? plane_floats : 0)};
-  if (G > 1) grad[0].out = plane[0], grad[1].out = plane[1];
-  if (together) {
+  if (G > 1) {
+    if ((s = planes.alloc(sizeof(float) * plane_floats * 2, st)) != GBLA_OK) return s;
+    scan[1].out = planes.ptr, scan[2].out = (float *)planes.ptr + plane_floats;
+  }
+  if (tc && tc_kv_supports(scan[1])) {
+    if ((s = run_scans(scan, 1, true, st)) != GBLA_OK) return s;
     Scratch ws;
-    if ((s = ws.alloc(sizeof(float) * tc_kv_floats(grad[0]), st)) != GBLA_OK) return s;
-    if ((s = from_cuda(tc_kv(grad[0], v, grad[1].sx, grad[1].out, (float *)ws.ptr, st))) != GBLA_OK)
+    if ((s = ws.alloc(sizeof(float) * tc_kv_floats(scan[1]), st)) != GBLA_OK) return s;
+    if ((s = from_cuda(tc_kv(scan[1], v, scan[2].sx, scan[2].out, (float *)ws.ptr, st))) != GBLA_OK)
       return s;
+  } else if (tc || (dtype == GBLA_BF16 && G > 1)) {  // results of two types: not side by side
+    if ((s = run_scans(scan, 1, tc, st)) != GBLA_OK) return s;
+    if ((s = run_scans(scan + 1, 2, tc, st)) != GBLA_OK) return s;
+  } else if ((s = run_scans(scan, 3, tc, st)) != GBLA_OK) {
+    return s;
   }
-  for (int i = 0; i < 2; ++i) {
-    if (!together && (s = run_scan(grad[i], tc, st)) != GBLA_OK) return s;
-    if (G > 1 && (s = from_cuda(sum_shared_heads(plane[i], i ? dk : dv, (long long)tok, Hk, G, D,
-                                                 dtype, st))) != GBLA_OK)
+  for (int i = 1; i < 3 && G > 1; ++i)
+    if ((s = from_cuda(sum_shared_heads((const float *)scan[i].out, i == 2 ? dk : dv,
+                                        (long long)tok, Hk, G, D, dtype, st))) != GBLA_OK)
       return s;
-  }
   return GBLA_OK;
 }
 

@@ -65,6 +65,12 @@ struct ScanDev {
   float *fin, *part;
   int N, H, seg, nseg;  // tokens per segment (a multiple of kC), most segments
 };
+// Scans of the same sizes in one launch: those of a batch row follow one another
+// in the grid's z.
+struct ScanBatch {
+  ScanDev scan[kMaxScans];
+  int n;
+};
 
 template <int D, bool kState>
 struct ScanShape {
@@ -109,7 +115,7 @@ __device__ __forceinline__ void load_tile(float *to, const __nv_bfloat16 *from, 
 // `part` (a single segment: the first state).
 template <typename T, typename O, int D, bool kState>
 __global__ void __launch_bounds__(kThreadsOf<D>, ScanShape<D, kState>::kBlocks)
-    scan_kernel(const ScanDev p) {
+    scan_kernel(const ScanBatch batch) {
   using Sh = ScanShape<D, kState>;
   constexpr int E = Sh::kE, kRow = Sh::kRow, kZRow = Sh::kZRow, kPRow = Sh::kPRow;
   constexpr int kThreads = Sh::kThreads, kQc = Sh::kQc, kQj = Sh::kQj;
@@ -119,9 +125,11 @@ __global__ void __launch_bounds__(kThreadsOf<D>, ScanShape<D, kState>::kBlocks)
   float *ps = sm + Sh::kOffP;  // [kC][kPRow] weighted scores
   float *st = sm + Sh::kOffS;  // [D][E] the state
   float *gp = sm + Sh::kOffG;  // gamma^0 .. gamma^kC
+  const ScanDev &p = batch.scan[blockIdx.z % batch.n];
   const int tid = threadIdx.x;
   const int seg = blockIdx.x / Sh::kSplit, e0 = blockIdx.x % Sh::kSplit * E;
-  const int h = blockIdx.y, b = blockIdx.z;
+  const int h = blockIdx.y, b = blockIdx.z / batch.n;
+  if (kState) grid_dep_launch();  // the prefix kernel waits for this one's results
   const int L = p.seq_lens ? min(max(p.seq_lens[b], 0), p.N) : p.N;
   const int ns = (L + p.seg - 1) / p.seg;
   const size_t bh = (size_t)b * p.H + h;
@@ -151,6 +159,7 @@ __global__ void __launch_bounds__(kThreadsOf<D>, ScanShape<D, kState>::kBlocks)
 #pragma unroll
     for (int c = 0; c < kSc; ++c) S[i][c] = 0.f;
   const int s_end = min(L, (seg + 1) * p.seg);
+  if (!kState && p.nseg > 1) grid_dep_wait();
   if (!kState && (p.nseg > 1 || p.init)) {
     const bool pre = p.nseg > 1 && ns > 0;
     const float *s0 = pre ? p.part + (bh * p.nseg + seg) * (size_t)D * D
@@ -310,9 +319,10 @@ __global__ void __launch_bounds__(kThreadsOf<D>, ScanShape<D, kState>::kBlocks)
 
 // Replaces each segment's own state by the state before it: the first state and
 // the segments before it in scan order, in that order.  Four elements a thread.
-__global__ void __launch_bounds__(128) prefix_kernel(const ScanDev p, int D) {
-  grid_dep_wait();
-  const int h = blockIdx.y, b = blockIdx.z, i = (blockIdx.x * 128 + threadIdx.x) * 4;
+__global__ void __launch_bounds__(128) prefix_kernel(const ScanBatch batch, int D) {
+  grid_dep_wait();  // (an early launch of the scan would place its blocks unevenly)
+  const ScanDev &p = batch.scan[blockIdx.z % batch.n];
+  const int h = blockIdx.y, b = blockIdx.z / batch.n, i = (blockIdx.x * 128 + threadIdx.x) * 4;
   const int L = p.seq_lens ? min(max(p.seq_lens[b], 0), p.N) : p.N;
   const int ns = (L + p.seg - 1) / p.seg;
   if (i >= D * D || ns == 0) return;
@@ -361,9 +371,9 @@ int sm_count() {
 // sequences (a segment costs its state a second time, a third of the work), and,
 // where only the device knows the lengths, at least eight, so that one long
 // sequence does not outlast the others.
-int scan_segment(const ScanArgs &a) {
-  const long long blocks = (long long)a.B * a.H * (a.D > 64 ? a.D / 64 : 1);
-  const long long chunks = (a.N + kC - 1) / kC, full = (a.D > 64 ? 2ll : 4ll) * sm_count();
+int scan_segment(const ScanArgs &a, int scans) {
+  const long long blocks = (long long)a.B * a.H * scans * (a.D > 64 ? a.D / 64 : 1);
+  const long long chunks = (a.N + kC - 1) / kC, full = (a.D > 64 ? 2ll : a.D > 32 ? 4ll : 8ll) * sm_count();
   long long n = blocks >= full ? 1 : full / blocks;  // one round of blocks, not a little more
   if (a.seq_lens && n < 8 && chunks >= 64) n = 8;
   if (n > 128) n = 128;  // the states before the segments are formed one after the other
@@ -371,7 +381,7 @@ int scan_segment(const ScanArgs &a) {
   return (int)((chunks + n - 1) / n) * kC;
 }
 
-ScanDev scan_dev(const ScanArgs &a, float *part) {
+ScanDev scan_dev(const ScanArgs &a, int scans, float *part) {
   ScanDev p = {};
   p.x = a.x, p.y = a.y, p.z = a.z;
   for (int i = 0; i < 2; ++i) p.sx[i] = a.sx[i], p.sy[i] = a.sy[i], p.sz[i] = a.sz[i];
@@ -380,17 +390,17 @@ ScanDev scan_dev(const ScanArgs &a, float *part) {
   p.log_decay = a.log_decay, p.seq_lens = a.seq_lens, p.init = a.init;
   p.init_scale = a.init_scale, p.fin_scale = a.fin_scale, p.scale = a.scale;
   p.fin = a.fin, p.part = part;
-  p.N = a.N, p.H = a.H, p.seg = scan_segment(a);
+  p.N = a.N, p.H = a.H, p.seg = scan_segment(a, scans);
   p.nseg = (a.N + p.seg - 1) / p.seg;
   return p;
 }
 
 template <typename T, typename O, int D>
-cudaError_t scan_launch(const ScanArgs &a, float *part, cudaStream_t st) {
-  const ScanDev p = scan_dev(a, part);
-  const dim3 grid(p.nseg * ScanShape<D, true>::kSplit, a.H, a.B);
+cudaError_t scan_launch(const ScanArgs &a, const ScanBatch &p, cudaStream_t st) {
+  const int nseg = p.scan[0].nseg;
+  const dim3 grid(nseg * ScanShape<D, true>::kSplit, a.H, a.B * p.n);
   cudaError_t e;
-  if (p.nseg > 1) {
+  if (nseg > 1) {
     constexpr int smem = ScanShape<D, true>::kSmemFloats * 4;
     const auto kernel = scan_kernel<T, O, D, true>;
     if ((e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem)) !=
@@ -400,8 +410,8 @@ cudaError_t scan_launch(const ScanArgs &a, float *part, cudaStream_t st) {
     count_launch();
     if ((e = cudaGetLastError()) != cudaSuccess) return e;
     count_launch();
-    if ((e = launch_pdl(prefix_kernel, dim3((D * D / 4 + 127) / 128, a.H, a.B), dim3(128), 0, st, p,
-                        D)) != cudaSuccess)
+    if ((e = launch_pdl(prefix_kernel, dim3((D * D / 4 + 127) / 128, a.H, a.B * p.n), dim3(128), 0,
+                        st, p, D)) != cudaSuccess)
       return e;
   }
   constexpr int smem = ScanShape<D, false>::kSmemFloats * 4;
@@ -409,16 +419,17 @@ cudaError_t scan_launch(const ScanArgs &a, float *part, cudaStream_t st) {
   if ((e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem)) !=
       cudaSuccess)
     return e;
-  kernel<<<grid, kThreadsOf<D>, smem, st>>>(p);
   count_launch();
+  if (nseg > 1) return launch_pdl(kernel, grid, dim3(kThreadsOf<D>), smem, st, p);
+  kernel<<<grid, kThreadsOf<D>, smem, st>>>(p);
   return cudaGetLastError();
 }
 
 template <typename T, typename O>
-cudaError_t scan_d(const ScanArgs &a, float *part, cudaStream_t st) {
-  if (a.D == 32) return scan_launch<T, O, 32>(a, part, st);
-  if (a.D == 64) return scan_launch<T, O, 64>(a, part, st);
-  return scan_launch<T, O, 128>(a, part, st);
+cudaError_t scan_d(const ScanArgs &a, const ScanBatch &p, cudaStream_t st) {
+  if (a.D == 32) return scan_launch<T, O, 32>(a, p, st);
+  if (a.D == 64) return scan_launch<T, O, 64>(a, p, st);
+  return scan_launch<T, O, 128>(a, p, st);
 }
 
 // ------------------------------------------------ sum over shared heads
@@ -515,15 +526,19 @@ cudaError_t step_launch(const StepArgs &a, cudaStream_t st) {
 
 }  // namespace
 
-size_t simt_scan_floats(const ScanArgs &a) {
-  const int seg = scan_segment(a), nseg = (a.N + seg - 1) / seg;
-  return nseg > 1 ? (size_t)a.B * a.H * nseg * a.D * a.D : 0;
+size_t simt_scan_floats(const ScanArgs &a, int n) {
+  const int seg = scan_segment(a, n), nseg = (a.N + seg - 1) / seg;
+  return nseg > 1 ? (size_t)n * a.B * a.H * nseg * a.D * a.D : 0;
 }
 
-cudaError_t simt_scan(const ScanArgs &a, float *scratch, cudaStream_t st) {
-  if (a.dtype == GBLA_FP32) return scan_d<float, float>(a, scratch, st);
-  if (a.out_f32) return scan_d<__nv_bfloat16, float>(a, scratch, st);
-  return scan_d<__nv_bfloat16, __nv_bfloat16>(a, scratch, st);
+cudaError_t simt_scan(const ScanArgs *a, int n, float *scratch, cudaStream_t st) {
+  const size_t each = simt_scan_floats(*a, n) / n;
+  ScanBatch p = {};
+  p.n = n;
+  for (int i = 0; i < n; ++i) p.scan[i] = scan_dev(a[i], n, scratch + i * each);
+  if (a->dtype == GBLA_FP32) return scan_d<float, float>(*a, p, st);
+  if (a->out_f32) return scan_d<__nv_bfloat16, float>(*a, p, st);
+  return scan_d<__nv_bfloat16, __nv_bfloat16>(*a, p, st);
 }
 
 cudaError_t sum_shared_heads(const float *src, void *dst, long long tokens, int Hk, int G, int D,

@@ -166,10 +166,10 @@ struct Walk {
   __device__ __forceinline__ bool live(const RotParams &p) const {
     return tok < p.tokens && !(p.seq_lens && t >= __ldg(p.seq_lens + b));
   }
+  // not yet clamped: nothing waits for the load until the position is used
   __device__ __forceinline__ int position(const RotParams &p) const {
     if (tok >= p.tokens) return 0;
-    const int pos = p.positions ? __ldg(p.positions + b * p.N + t) : t;
-    return min(max(pos, 0), p.P - 1);
+    return p.positions ? __ldg(p.positions + b * p.N + t) : t;
   }
 };
 
@@ -224,7 +224,7 @@ struct Ring {
   // Sends for the next token; one copy group whether it is valid or not.
   __device__ __forceinline__ void send(const RotParams &p, const Lane<D, kU> &ln, int stage) {
     const bool live = ahead.live(p);
-    const int at = pos;
+    const int at = min(max(pos, 0), p.P - 1);
     const long long tok = ahead.tok, b = ahead.b;
     const int t = ahead.t;
     ahead.next();

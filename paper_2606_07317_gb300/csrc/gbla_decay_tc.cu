@@ -427,7 +427,9 @@ __global__ void __launch_bounds__(OwnShape<D, kTerms>::kThreads, OwnShape<D, kTe
   if (sg.cnt == 0 || sg.last) return;
   const float l2 = __ldg(p.log_decay + h) * 1.4426950408889634f;
 
-  if (tid == 0) {
+  // The loading warp sets the barriers up and starts at once; the others also wait
+  // for the TMEM allocation.
+  if (warp == Sh::kTmaWarp && lane == 0) {
     *(volatile int *)(smem + Sh::kOffMisc + 4) = 0;
     for (int i = 0; i < Sh::kNY; ++i) mbar_init(&fy[i], Sh::kB), mbar_init(&ey[i], 1);
     for (int i = 0; i < Sh::kNZ; ++i) mbar_init(&fz[i], Sh::kB), mbar_init(&ez[i], 1);
@@ -445,9 +447,14 @@ __global__ void __launch_bounds__(OwnShape<D, kTerms>::kThreads, OwnShape<D, kTe
     tma_prefetch_desc(&tm_z);
   }
   if (warp == Sh::kMmaWarp) tmem_alloc(tmem_slot, Sh::kTmemCols);
-  tc_fence_before();
-  __syncthreads();
-  tc_fence_after();
+  if (warp == Sh::kTmaWarp) {
+    __syncwarp();
+    named_barrier_arrive(1, Sh::kThreads);
+  } else {
+    tc_fence_before();
+    named_barrier(1, Sh::kThreads);
+    tc_fence_after();
+  }
   const uint32_t tmem = *tmem_slot;
   auto token_at = [&](int g) { return sg.token_of(sg.q0 + sg.cnt - 1 - g); };
 
@@ -607,7 +614,9 @@ __global__ void __launch_bounds__(Shape<D, kTerms>::kThreads, 1)
   }
   const float l2 = __ldg(p.log_decay + h) * 1.4426950408889634f;
 
-  if (tid == 0) {
+  // The loading warp sets the barriers up and starts at once; the others also wait
+  // for the TMEM allocation.
+  if (warp == Sh::kTmaWarp && lane == 0) {
     *(volatile int *)(smem + Sh::kOffMisc + 4) = 0;
     for (int i = 0; i < Sh::kNX; ++i) mbar_init(&fx[i], Sh::kB), mbar_init(&ex[i], 1);
     for (int i = 0; i < Sh::kNY; ++i) mbar_init(&fy[i], Sh::kB), mbar_init(&ey[i], 1);
@@ -635,9 +644,14 @@ __global__ void __launch_bounds__(Shape<D, kTerms>::kThreads, 1)
     tma_prefetch_desc(&tm_z);
   }
   if (warp == Sh::kMmaWarp) tmem_alloc(tmem_slot, 512);
-  tc_fence_before();
-  __syncthreads();
-  tc_fence_after();
+  if (warp == Sh::kTmaWarp) {
+    __syncwarp();
+    named_barrier_arrive(1, Sh::kThreads);
+  } else {
+    tc_fence_before();
+    named_barrier(1, Sh::kThreads);
+    tc_fence_after();
+  }
   const uint32_t tmem = *tmem_slot;
   if (warp == Sh::kTmaWarp) {
     // ---------------------------------------------------------------- loads
@@ -1049,7 +1063,9 @@ __global__ void __launch_bounds__(KvShape<kTerms>::kThreads, 1)
     return;
   }
   const float l2 = __ldg(p.log_decay + h) * 1.4426950408889634f;
-  if (tid == 0) {
+  // The loading warp sets the barriers up and starts at once; the others also wait
+  // for the TMEM allocation.
+  if (warp == Sh::kTmaWarp && lane == 0) {
     *(volatile int *)(smem + Sh::kOffMisc + 4) = 0;
     for (int i = 0; i < 2 * kNX; ++i) mbar_init(&fx[i], 1), mbar_init(&ex[i], 1);
     for (int i = 0; i < kN; ++i) {
@@ -1077,9 +1093,14 @@ __global__ void __launch_bounds__(KvShape<kTerms>::kThreads, 1)
     tma_prefetch_desc(&tm_g);
   }
   if (warp == Sh::kMmaWarp) tmem_alloc(tmem_slot, 512);
-  tc_fence_before();
-  __syncthreads();
-  tc_fence_after();
+  if (warp == Sh::kTmaWarp) {
+    __syncwarp();
+    named_barrier_arrive(1, Sh::kThreads);
+  } else {
+    tc_fence_before();
+    named_barrier(1, Sh::kThreads);
+    tc_fence_after();
+  }
   const uint32_t tmem = *tmem_slot;
   if (warp == Sh::kTmaWarp) {
     // ---------------------------------------------------------------- loads

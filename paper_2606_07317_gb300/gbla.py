@@ -404,9 +404,19 @@ def state_static_scratch(k, v, gate, conv_w, seq_lens=None, out=None,
 
 # --- causal decoder operators -------------------------------------------------
 
-def _raw_stream(q, stream):
-    """Handle of the stream (None: the current one) that a call on q's tensors goes to."""
-    dev = q.get_device()
+_CODES = {torch.float32: GBLA_FP32, torch.bfloat16: GBLA_BF16}
+
+
+def _code(q):
+    """(dtype code, device index) of q, whose type and device the other tensors share."""
+    code = _CODES.get(q.dtype)
+    if code is None:
+        raise TypeError(f"unsupported dtype {q.dtype}")
+    return code, q.get_device()
+
+
+def _raw_stream(dev, stream):
+    """Handle of the stream (None: the current one) that a call on device `dev` goes to."""
     if dev < 0 or dev != torch.cuda.current_device():
         raise ValueError("the tensors must be on the current CUDA device")
     return torch._C._cuda_getCurrentRawStream(dev) if stream is None else stream.cuda_stream
@@ -418,12 +428,12 @@ def _dims(q):
     return q.shape
 
 
-def _heads(t, name, shape, q):
-    """Checks a token-major tensor of the given shape with q's dtype and device, whose heads
-    are adjacent and whose head values are contiguous; True if it is contiguous throughout."""
+def _heads(t, name, shape, dtype, dev):
+    """Checks a token-major tensor whose heads are adjacent and whose head values are
+    contiguous; True if it is contiguous throughout."""
     if t.shape != shape:
         raise ValueError(f"{name} must be [B, N, heads, D] = {tuple(shape)}, not {tuple(t.shape)}")
-    if t.dtype is not q.dtype or t.get_device() != q.get_device():
+    if t.dtype is not dtype or t.get_device() != dev:
         raise ValueError(f"{name} must have the dtype and device of q")
     if t.is_contiguous():
         return True
@@ -432,22 +442,29 @@ def _heads(t, name, shape, q):
     return False
 
 
-def _key_shape(q, k):
-    """Shape of a key or value tensor that goes with q."""
+def _key_shape(shape, k):
+    """Shape of a key or value tensor that goes with q's."""
     if k.dim() != 4:
         raise ValueError("k must be [B, N, heads, D]")
-    B, N, _, D = q.shape
-    return (B, N, k.shape[2], D)
+    return (shape[0], shape[1], k.shape[2], shape[3])
 
 
-def _plain(t, name, shape, dtype, q):
-    """Checks an optional contiguous tensor on q's device."""
+def _plain(t, name, shape, dtype, dev):
+    """Checks an optional contiguous tensor and returns its address (None: NULL)."""
     if t is None:
-        return
-    if t.dtype is not dtype or t.shape != shape or not t.is_contiguous():
+        return None
+    if t.shape == shape and t.dtype is dtype and t.is_contiguous() and t.get_device() == dev:
+        return t.data_ptr()
+    if t.shape != shape or t.dtype is not dtype or not t.is_contiguous():
         raise ValueError(f"{name} must be a contiguous {dtype} tensor of shape {tuple(shape)}")
-    if t.get_device() != q.get_device():
-        raise ValueError(f"{name} must be on the device of q")
+    raise ValueError(f"{name} must be on the device of q")
+
+
+def _like(t):
+    """A contiguous tensor like t."""
+    if t.is_contiguous():
+        return torch.empty_like(t)
+    return torch.empty(t.shape, dtype=t.dtype, device=t.device)
 
 
 def _strides(*tensors, dims=2):
@@ -465,16 +482,18 @@ def rotation_table(positions: int, R: int, base: float = 10000.0, device="cuda")
 
 
 def _rotate_args(q, k, norm_q, norm_k, rot, positions, seq_lens):
+    """(code, device, input addresses and strides in the ABI's order, sizes)."""
     B, N, H, D = shape = _dims(q)
-    Hk = _key_shape(q, k)[2]
-    whole = _heads(q, "q", shape, q) & _heads(k, "k", (B, N, Hk, D), q)
-    _plain(norm_q, "norm_q", (H, D), torch.float32, q)
-    _plain(norm_k, "norm_k", (Hk, D), torch.float32, q)
+    code, dev = _code(q)
+    kshape = _key_shape(shape, k)
+    whole = _heads(q, "q", shape, q.dtype, dev) & _heads(k, "k", kshape, q.dtype, dev)
     P, R = rot.shape if rot is not None and rot.dim() == 2 else (0, 0)
-    _plain(rot, "rot", (P, R), torch.float32, q)
-    _plain(positions, "positions", (B, N), torch.int32, q)
-    _plain(seq_lens, "seq_lens", (B,), torch.int32, q)
-    return None if whole else _strides(q, k), (B, N, H, Hk, D, R, P)
+    f32, i32 = torch.float32, torch.int32
+    ins = (q.data_ptr(), k.data_ptr(), _plain(norm_q, "norm_q", (H, D), f32, dev),
+           _plain(norm_k, "norm_k", (kshape[2], D), f32, dev), _plain(rot, "rot", (P, R), f32, dev),
+           _plain(positions, "positions", (B, N), i32, dev),
+           _plain(seq_lens, "seq_lens", (B,), i32, dev), None if whole else _strides(q, k))
+    return code, dev, ins, (B, N, H, kshape[2], D, R, P)
 
 
 def qk_norm_rotate(q, k, norm_q, norm_k, rot=None, positions=None, seq_lens=None,
@@ -484,16 +503,13 @@ def qk_norm_rotate(q, k, norm_q, norm_k, rot=None, positions=None, seq_lens=None
     rotation_table (None: norm alone); positions [B, N] int32 (None: token t has position
     t).  q and k may be slices of a packed projection.  Returns (qo, ko), or fills `out`;
     rows past seq_lens are not written."""
-    strides, dims = _rotate_args(q, k, norm_q, norm_k, rot, positions, seq_lens)
+    code, dev, ins, dims = _rotate_args(q, k, norm_q, norm_k, rot, positions, seq_lens)
     if out is None:
-        out = (torch.empty(q.shape, dtype=q.dtype, device=q.device),
-               torch.empty(k.shape, dtype=k.dtype, device=q.device))
-    _plain(out[0], "out[0]", q.shape, q.dtype, q)
-    _plain(out[1], "out[1]", k.shape, q.dtype, q)
+        out = (_like(q), _like(k))
     st = (_lib or load()).gbla_qk_norm_rotate(
-        _ptr(q), _ptr(k), _ptr(norm_q), _ptr(norm_k), _ptr(rot), _ptr(positions),
-        _ptr(seq_lens), strides, _ptr(out[0]), _ptr(out[1]), *dims, float(eps),
-        ROTATE_INTERLEAVED if interleaved else 0, _dtype_code(q), _raw_stream(q, stream))
+        *ins, _plain(out[0], "out[0]", q.shape, q.dtype, dev),
+        _plain(out[1], "out[1]", k.shape, q.dtype, dev), *dims, eps,
+        ROTATE_INTERLEAVED if interleaved else 0, code, _raw_stream(dev, stream))
     _check(st, "gbla_qk_norm_rotate")
     return out[0], out[1]
 
@@ -502,29 +518,29 @@ def qk_norm_rotate_backward(q, k, norm_q, norm_k, rot, dqo, dko, positions=None,
                             eps: float = 1e-6, interleaved: bool = False, stream=None) -> dict:
     """Gradients of qk_norm_rotate (gbla_qk_norm_rotate_backward) for the contiguous
     gradients dqo, dko of its results: dq, dk (0 past seq_lens), dnorm_q, dnorm_k."""
-    strides, dims = _rotate_args(q, k, norm_q, norm_k, rot, positions, seq_lens)
-    _plain(dqo, "dqo", q.shape, q.dtype, q)
-    _plain(dko, "dko", k.shape, q.dtype, q)
-    g = dict(dq=torch.empty(q.shape, dtype=q.dtype, device=q.device),
-             dk=torch.empty(k.shape, dtype=k.dtype, device=q.device),
-             dnorm_q=torch.empty_like(norm_q), dnorm_k=torch.empty_like(norm_k))
+    code, dev, ins, dims = _rotate_args(q, k, norm_q, norm_k, rot, positions, seq_lens)
+    grads = (_plain(dqo, "dqo", q.shape, q.dtype, dev), _plain(dko, "dko", k.shape, q.dtype, dev))
+    g = dict(dq=_like(q), dk=_like(k), dnorm_q=_like(norm_q), dnorm_k=_like(norm_k))
     st = (_lib or load()).gbla_qk_norm_rotate_backward(
-        _ptr(q), _ptr(k), _ptr(norm_q), _ptr(norm_k), _ptr(rot), _ptr(positions),
-        _ptr(seq_lens), strides, _ptr(dqo), _ptr(dko), _ptr(g["dq"]), _ptr(g["dk"]),
-        _ptr(g["dnorm_q"]), _ptr(g["dnorm_k"]), *dims, float(eps),
-        ROTATE_INTERLEAVED if interleaved else 0, _dtype_code(q), _raw_stream(q, stream))
+        *ins, *grads, *[t.data_ptr() for t in g.values()], *dims, eps,
+        ROTATE_INTERLEAVED if interleaved else 0, code, _raw_stream(dev, stream))
     _check(st, "gbla_qk_norm_rotate_backward")
     return g
 
 
 def _decay_args(q, k, v, log_decay, seq_lens, state):
+    """(code, device, input addresses and strides in the ABI's order, sizes)."""
     B, N, H, D = shape = _dims(q)
-    kshape = _key_shape(q, k)
-    whole = _heads(q, "q", shape, q) & _heads(k, "k", kshape, q) & _heads(v, "v", kshape, q)
-    _plain(log_decay, "log_decay", (H,), torch.float32, q)
-    _plain(seq_lens, "seq_lens", (B,), torch.int32, q)
-    _plain(state, "state", (B, H, D, D), torch.float32, q)
-    return None if whole else _strides(q, k, v), (B, N, H, kshape[2], D)
+    code, dev = _code(q)
+    kshape = _key_shape(shape, k)
+    whole = (_heads(q, "q", shape, q.dtype, dev) & _heads(k, "k", kshape, q.dtype, dev)
+             & _heads(v, "v", kshape, q.dtype, dev))
+    ins = (q.data_ptr(), k.data_ptr(), v.data_ptr(),
+           _plain(log_decay, "log_decay", (H,), torch.float32, dev),
+           _plain(seq_lens, "seq_lens", (B,), torch.int32, dev),
+           None if whole else _strides(q, k, v),
+           _plain(state, "state", (B, H, D, D), torch.float32, dev))
+    return code, dev, ins, (B, N, H, kshape[2], D)
 
 
 def decay_attention(q, k, v, log_decay, seq_lens=None, state=None, scale=None, out=None,
@@ -534,16 +550,15 @@ def decay_attention(q, k, v, log_decay, seq_lens=None, state=None, scale=None, o
     k, v [B, N, Hk, D]; `state` [B, H, D, D] fp32 is S before the first token, scale
     defaults to D^-1/2.  Returns o, or (o, S after each sequence's last token) with
     return_state; rows of o past seq_lens are not written."""
-    strides, dims = _decay_args(q, k, v, log_decay, seq_lens, state)
+    code, dev, ins, dims = _decay_args(q, k, v, log_decay, seq_lens, state)
     B, N, H, Hk, D = dims
     if out is None:
-        out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
-    _plain(out, "out", q.shape, q.dtype, q)
-    fin = torch.empty((B, H, D, D), dtype=torch.float32, device=q.device) if return_state else None
+        out = _like(q)
+    fin = (torch.empty((B, H, D, D), dtype=torch.float32, device=q.device) if return_state
+           else None)
     st = (_lib or load()).gbla_decay_attention(
-        _ptr(q), _ptr(k), _ptr(v), _ptr(log_decay), _ptr(seq_lens), strides, _ptr(state),
-        _ptr(out), _ptr(fin), *dims, float(D ** -0.5 if scale is None else scale),
-        _dtype_code(q), int(algo), _raw_stream(q, stream))
+        *ins, _plain(out, "out", q.shape, q.dtype, dev), None if fin is None else fin.data_ptr(),
+        *dims, D ** -0.5 if scale is None else scale, code, algo, _raw_stream(dev, stream))
     _check(st, "gbla_decay_attention")
     return (out, fin) if return_state else out
 
@@ -555,19 +570,17 @@ def decay_attention_backward(q, k, v, log_decay, do, seq_lens=None, state=None, 
     contiguous, `dstate` [B, H, D, D] the gradient of the returned state (None: zeros).
     Returns dq, dk, dv (0 past seq_lens; shared heads summed) and, with return_dstate,
     dstate, the gradient of the first state."""
-    strides, dims = _decay_args(q, k, v, log_decay, seq_lens, state)
+    code, dev, ins, dims = _decay_args(q, k, v, log_decay, seq_lens, state)
     B, N, H, Hk, D = dims
-    _plain(do, "do", q.shape, q.dtype, q)
-    _plain(dstate, "dstate", (B, H, D, D), torch.float32, q)
-    g = {n: torch.empty(t.shape, dtype=q.dtype, device=q.device)
-         for n, t in (("dq", q), ("dk", k), ("dv", v))}
+    grads = (_plain(do, "do", q.shape, q.dtype, dev),
+             _plain(dstate, "dstate", (B, H, D, D), torch.float32, dev))
+    g = {"dq": _like(q), "dk": _like(k), "dv": _like(v)}
     if return_dstate:
         g["dstate"] = torch.empty((B, H, D, D), dtype=torch.float32, device=q.device)
+    out = [t.data_ptr() for t in g.values()] + ([] if return_dstate else [None])
     st = (_lib or load()).gbla_decay_attention_backward(
-        _ptr(q), _ptr(k), _ptr(v), _ptr(log_decay), _ptr(seq_lens), strides, _ptr(state),
-        _ptr(do), _ptr(dstate), _ptr(g["dq"]), _ptr(g["dk"]), _ptr(g["dv"]),
-        _ptr(g.get("dstate")), *dims, float(D ** -0.5 if scale is None else scale),
-        _dtype_code(q), int(algo), _raw_stream(q, stream))
+        *ins, *grads, *out, *dims, D ** -0.5 if scale is None else scale, code, algo,
+        _raw_stream(dev, stream))
     _check(st, "gbla_decay_attention_backward")
     return g
 
@@ -578,19 +591,22 @@ def decay_attention_step(q, k, v, log_decay, state, slots=None, scale=None, out=
     [B, 1, Hk, D]; `state` [n_slots, H, D, D] fp32 is updated in place at slots[b] (int32;
     None: slot b).  Rows whose slot is outside the pool are left alone.  Returns o."""
     B, N, H, D = shape = _dims(q)
-    kshape = _key_shape(q, k)
+    code, dev = _code(q)
+    kshape = _key_shape(shape, k)
     if N != 1:
         raise ValueError("q, k and v hold one token of each sequence")
-    whole = _heads(q, "q", shape, q) & _heads(k, "k", kshape, q) & _heads(v, "v", kshape, q)
-    _plain(log_decay, "log_decay", (H,), torch.float32, q)
-    _plain(slots, "slots", (B,), torch.int32, q)
-    _plain(state, "state", (state.shape[0], H, D, D), torch.float32, q)
+    whole = (_heads(q, "q", shape, q.dtype, dev) & _heads(k, "k", kshape, q.dtype, dev)
+             & _heads(v, "v", kshape, q.dtype, dev))
+    n_slots = state.shape[0]
     if out is None:
-        out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
-    _plain(out, "out", q.shape, q.dtype, q)
+        out = _like(q)
     st = (_lib or load()).gbla_decay_attention_step(
-        _ptr(q), _ptr(k), _ptr(v), _ptr(log_decay), _ptr(slots),
-        None if whole else _strides(q, k, v, dims=1), _ptr(state), _ptr(out), B, H, kshape[2], D, state.shape[0],
-        float(D ** -0.5 if scale is None else scale), _dtype_code(q), _raw_stream(q, stream))
+        q.data_ptr(), k.data_ptr(), v.data_ptr(),
+        _plain(log_decay, "log_decay", (H,), torch.float32, dev),
+        _plain(slots, "slots", (B,), torch.int32, dev),
+        None if whole else _strides(q, k, v, dims=1),
+        _plain(state, "state", (n_slots, H, D, D), torch.float32, dev),
+        _plain(out, "out", shape, q.dtype, dev), B, H, kshape[2], D, n_slots,
+        D ** -0.5 if scale is None else scale, code, _raw_stream(dev, stream))
     _check(st, "gbla_decay_attention_step")
     return out

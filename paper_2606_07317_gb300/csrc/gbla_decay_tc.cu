@@ -6,9 +6,6 @@
 //   results out_r = scale [ sum_j (w_rj A_rj) z_j + u_r x_r^T S ]
 //                                                    (M64 ND K64, M64 ND KD)
 //   state   S'    = c S + sum_j (v_j y_j) z_j^T      (MD ND K64, a time for each term)
-// D = 64: y's tile and the state (transposed) lie one behind the other, so that
-// scores and x_r^T S are one product of N = 128, and the terms of the state's
-// product share one of N = 128: an MMA of M = 64 takes about as long at N = 64.
 // forward: w = gamma^{r-j} (j <= r), u = gamma^{r+1}, v = gamma^{n-1-j}, c = gamma^n
 // for n tokens in the chunk; reverse: w = gamma^{j-r} (j >= r), u = gamma^{64-r},
 // v = gamma^j, c = gamma^64, and u = gamma^{n-1-r}, c = gamma^{n-1} in the first
@@ -28,11 +25,27 @@
 // last, so that it is still in L2), and the scan starts from the weighted sum of
 // the segments before its own.  The second launch begins while the first ends.
 //
-// Warps of the scan: 0-3 weight the scores, 4-7 form v_j y_j, the next 4 (D = 128: 8) hold
-// the state, the next 4 write results, then one warp issues the TMA loads (a
+// What bounds a chunk (D = 64): memory takes 32 KB of it, 1430 cycles of an SM's
+// share of the measured bandwidth; shared memory some 144 KB (operands of the
+// MMAs 64, weighted keys 24, loads 24, scores, state and staged results 32), 1150;
+// the tensor pipe 650 at M = 64 (33 cycles an MMA of N = 64, 65 of N = 128).  Hence
+// C = 64 and not 128: twice the tokens would read the keys' and values' tiles half
+// as often, but the scores would be written and read for twice the pairs.  And so
+// y's tile and the state (transposed) lie one behind the other, and scores and
+// x_r^T S are one product of N = 128 that reads x once; the terms of the state's
+// product are side by side in one of N = 128 in the same way.  Measured: B19 H8
+// N4096 (one whole sequence an SM) 55 us, 5.8 TB/s, 85 % of the measured copy rate;
+// B2 H8 N32768, where segments cost y and z twice, 82 us, 3.3 TB/s of what the
+// operation needs.  D = 128 has operands twice as wide for a state four times as
+// large: 336 KB and 2600 cycles of shared memory against 2870 of memory, 127 us at
+// B19 H8 N4096 (74 %).
+//
+// Warps of the scan: 0-3 weight the scores, 4-7 form v_j y_j, the next 4 (D = 128:
+// 8) hold the state, the next 4 write results, then one warp issues the TMA loads (a
 // lane for each 64-channel block of each tensor: one thread issues a box in half
-// a microsecond) and one the MMAs.  M = 64 accumulators lie in lanes 0-15 of each
-// TMEM quarter and are read with the 16-lane shapes.
+// a microsecond) and one the MMAs (one elected lane: issued from a plain branch on
+// the lane number, each MMA took 160 cycles).  M = 64 accumulators lie in lanes 0-15
+// of each TMEM quarter and are read with the 16-lane shapes.
 //
 // Every mbarrier wait is bounded (2 s); one that runs out sets a bit in
 // g_decay_error and raises the CTA's abort flag.

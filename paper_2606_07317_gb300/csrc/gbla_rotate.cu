@@ -7,11 +7,15 @@
 // n = x r:  dw = sum g n,  u = g w,  dx = r (u - n mean(u n)).
 //
 // About 5 flops a byte: bound by memory.  A head vector is spread over D / 8
-// lanes of 8 values (one 16-byte load in bf16), so a warp holds 256 / D heads
+// lanes of 8 values (one 16-byte copy in bf16), so a warp holds 256 / D heads
 // at once, the mean is a butterfly over those lanes, and the half-split pairs
 // (i, i + R / 2) meet by one shuffle per value.  A warp keeps its kU groups of
 // heads while it walks over the tokens: their weights stay in registers, and a
-// token's row of cosines and sines is read once for all of them.
+// token's row of cosines and sines is read once for all of them.  The tokens to
+// come are on their way into shared memory meanwhile (loads into registers left
+// memory idle while a token was computed: 69 us where it is 45 now).  Measured at
+// B2 H8 N32768 D64 bf16: forward 45 us, 6.2 TB/s (91 % of the measured copy rate);
+// backward at B4 N8192: 39 us, 5.2 TB/s (77 %, two kernels).
 #include "gbla_internal.cuh"
 #include "gbla_sm100.cuh"
 

@@ -444,6 +444,32 @@ def test_captured_in_a_graph():
         assert torch.equal(o, got[t]), t
 
 
+@pytest.mark.parametrize("dtype,D", [("bf16", 64), ("bf16", 128), ("fp32", 64)])
+def test_prompt_and_gradients_in_a_graph(dtype, D):
+    """Calls that cut the sequence (several launches, pool scratch) replay from a CUDA graph."""
+    c = Case(82, 1, 1024, 2, 1, D, dtype)
+    q, k, v, do = (dev(c.tok(h)) for h in (2, 1, 1, 2))
+    ld, w = dev(_decays(2, "some", c.g).float()), torch.ones((2, D), device="cuda")
+    rot = gbla.rotation_table(1024, D)
+
+    def work():
+        a, b = gbla.qk_norm_rotate(q, k, w, w[:1], rot)
+        o, S = gbla.decay_attention(a, b, v, ld, return_state=True)
+        return [o, S, *gbla.decay_attention_backward(a, b, v, ld, do).values()]
+
+    want = [t.clone() for t in work()]
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        got = work()
+    for _ in range(2):
+        for t in got:
+            t.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(got, want))
+
+
 @pytest.mark.parametrize("D", [32, 64, 128])
 def test_decay_attention_long_rows_sampled(D):
     """32768 tokens: sampled rows against explicit sums over pairs of tokens."""

@@ -1073,13 +1073,11 @@ gbla_status gbla_decay_attention_backward(
     if ((s = planes.alloc(sizeof(float) * plane_floats * 2, st)) != GBLA_OK) return s;
     scan[1].out = planes.ptr, scan[2].out = (float *)planes.ptr + plane_floats;
   }
-  if (tc && tc_kv_supports(scan[1])) {
-    if ((s = run_scans(scan, 1, true, st)) != GBLA_OK) return s;
+  if (tc) {
     Scratch ws;
-    if ((s = ws.alloc(sizeof(float) * tc_kv_floats(scan[1]), st)) != GBLA_OK) return s;
-    if ((s = from_cuda(tc_kv(scan[1], v, scan[2].sx, scan[2].out, (float *)ws.ptr, st))) != GBLA_OK)
-      return s;
-  } else if (tc || (dtype == GBLA_BF16 && G > 1)) {  // results of two types: not side by side
+    if ((s = ws.alloc(sizeof(float) * tc_backward_floats(scan), st)) != GBLA_OK) return s;
+    if ((s = from_cuda(tc_backward(scan, (float *)ws.ptr, st))) != GBLA_OK) return s;
+  } else if (dtype == GBLA_BF16 && G > 1) {  // results of two types: not side by side
     if ((s = run_scans(scan, 1, tc, st)) != GBLA_OK) return s;
     if ((s = run_scans(scan + 1, 2, tc, st)) != GBLA_OK) return s;
   } else if ((s = run_scans(scan, 3, tc, st)) != GBLA_OK) {

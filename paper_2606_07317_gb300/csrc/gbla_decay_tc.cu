@@ -620,6 +620,7 @@ __global__ void __launch_bounds__(Shape<D, kTerms>::kThreads, 1)
       ((uint4 *)(out + (L + i / kPer) * orow))[i % kPer] = make_uint4(0, 0, 0, 0);
   }
   if (cnt == 0) {
+    if (p.ranks > 1) grid_dep_wait();  // a grid never ends before the own-state kernel
     if (rank == 0 && p.fin)  // an empty sequence passes its state on
       for (int i = tid; i < V * V; i += Sh::kThreads)
         p.fin[bh * V * V + i] = p.init ? p.init[bh * V * V + i] * p.init_scale * p.fin_scale : 0.f;
@@ -920,6 +921,7 @@ __global__ void __launch_bounds__(Shape<D, kTerms>::kThreads, 1)
         if (V == D || (d < V && e < V)) p.fin[bh * V * V + d * V + e] = S[i] * f;
       }
     }
+    if (p.ranks > 1 && rank == 0) grid_dep_wait();
   } else {
     // ---------------------------------------------------------------- results
     const int ow = warp - Sh::kOutWarp, r0 = 16 * ow + (lane >> 2);
@@ -1070,6 +1072,7 @@ __global__ void __launch_bounds__(KvShape<kTerms>::kThreads, 1)
     }
   }
   if (cnt == 0) {
+    if (p.ranks > 1) grid_dep_wait();  // a grid never ends before the own-state kernel
     if (rank == 0 && p.fin)  // an empty sequence passes its state on
       for (int i = tid; i < V * V; i += Sh::kThreads)
         p.fin[bh * V * V + i] = p.init ? p.init[bh * V * V + i] * p.init_scale * p.fin_scale : 0.f;
@@ -1321,6 +1324,7 @@ __global__ void __launch_bounds__(KvShape<kTerms>::kThreads, 1)
         if (V == D || (d < V && e < V)) p.fin[bh * V * V + d * V + e] = S[i] * f;
       }
     }
+    if (p.ranks > 1 && rank == 0) grid_dep_wait();
   } else {
     // ---------------------------------------------------------------- results
     const int ow = warp - 12, r0 = 16 * ow + (lane >> 2);
@@ -1456,94 +1460,115 @@ int segment_for(const ScanArgs &a, double chunk) {
   return best;
 }
 
-template <int D, int V, int kTerms, typename O>
-cudaError_t launch(const ScanArgs &a, const TcParams &p, const CUtensorMap &tx,
-                   const CUtensorMap &ty, const CUtensorMap &tz, cudaStream_t st) {
-  cudaError_t e;
-  if (p.ranks > 1) {
-    using Sh = OwnShape<D, kTerms>;
-    const auto kernel = own_state_kernel<D, kTerms>;
-    if ((e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                  Sh::kSmem)) != cudaSuccess)
-      return e;
-    kernel<<<dim3(p.ranks - 1, a.H, a.B), Sh::kThreads, Sh::kSmem, st>>>(p, ty, tz);
-    count_launch();
-    if ((e = cudaGetLastError()) != cudaSuccess) return e;
+constexpr double kKvChunk = 1.6;
+
+int ranks_for(const ScanArgs &a, double chunk) {
+  const int seg = segment_for(a, chunk);
+  return ((a.N + kC - 1) / kC + seg - 1) / seg;
+}
+size_t part_floats(const ScanArgs &a, double chunk) {
+  const size_t d = a.D < 64 ? 64 : a.D;
+  const int ranks = ranks_for(a, chunk);
+  return ranks > 1 ? (size_t)a.B * a.H * ranks * d * d : 0;
+}
+
+// A scan ready to launch.
+struct Scan {
+  ScanArgs a;
+  TcParams p;
+  CUtensorMap x, y, z;
+  cudaError_t set(const ScanArgs &args, float *scratch, double chunk = 1) {
+    a = args;
+    p = TcParams{};
+    p.out = a.out, p.log_decay = a.log_decay, p.seq_lens = a.seq_lens;
+    p.init = a.init, p.fin = a.fin, p.part = scratch;
+    p.init_scale = a.init_scale, p.fin_scale = a.fin_scale, p.scale = a.scale;
+    p.N = a.N, p.H = a.H, p.gx = a.gx, p.gy = a.gy, p.gz = a.gz;
+    p.zero_pad = a.zero_pad, p.init_t = a.init_t, p.reverse = a.reverse;
+    p.seg = segment_for(a, chunk), p.ranks = ranks_for(a, chunk);
+    cudaError_t e;
+    if ((e = make_map(&x, a.x, a.B, a.N, a.H / a.gx, a.D, a.sx)) != cudaSuccess) return e;
+    if ((e = make_map(&y, a.y, a.B, a.N, a.H / a.gy, a.D, a.sy)) != cudaSuccess) return e;
+    return make_map(&z, a.z, a.B, a.N, a.H / a.gz, a.D, a.sz);
   }
-  using Sh = Shape<D, kTerms>;
-  const auto kernel = decay_kernel<D, V, kTerms, O>;
-  if ((e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, Sh::kSmem)) !=
-      cudaSuccess)
-    return e;
-  const dim3 grid(p.ranks, a.H, a.B);
+};
+
+template <int D, int kTerms>
+cudaError_t launch_own(const Scan &s, cudaStream_t st) {
+  using Sh = OwnShape<D, kTerms>;
+  const auto kernel = own_state_kernel<D, kTerms>;
+  const cudaError_t e =
+      cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, Sh::kSmem);
+  if (e != cudaSuccess) return e;
+  kernel<<<dim3(s.p.ranks - 1, s.a.H, s.a.B), Sh::kThreads, Sh::kSmem, st>>>(s.p, s.y, s.z);
   count_launch();
-  // Behind the own-state kernel the scan may start while that ends: only its
-  // state warps read what that kernel writes, and they wait for it.
-  if (p.ranks > 1) return launch_pdl(kernel, grid, dim3(Sh::kThreads), Sh::kSmem, st, p, tx, ty, tz);
-  kernel<<<grid, Sh::kThreads, Sh::kSmem, st>>>(p, tx, ty, tz);
+  return cudaGetLastError();
+}
+
+// The states of the segments, where a sequence is cut into any.  (The backward's in
+// one launch ahead of its scans were slower: 120 us where it is 117 at B4 H8 N8192
+// D64, 363 for 320 at B2 N16384 D128; each scan finds less of its own in L2.)
+cudaError_t own_states(const Scan &s, cudaStream_t st) {
+  if (s.p.ranks <= 1) return cudaSuccess;
+  if (s.a.D > 64) return s.a.fin ? launch_own<128, 3>(s, st) : launch_own<128, 2>(s, st);
+  return s.a.fin ? launch_own<64, 3>(s, st) : launch_own<64, 2>(s, st);
+}
+
+// Launches a scan right behind its own-state kernel: it may start while that ends,
+// as only its state warps read what that kernel writes, and they wait for it.
+template <typename... KArgs, typename... Args>
+cudaError_t launch_behind(void (*kernel)(KArgs...), const Scan &s, int threads, int smem,
+                          cudaStream_t st, Args... args) {
+  const cudaError_t e =
+      cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+  if (e != cudaSuccess) return e;
+  const dim3 grid(s.p.ranks, s.a.H, s.a.B);
+  count_launch();
+  if (s.p.ranks > 1) return launch_pdl(kernel, grid, dim3(threads), smem, st, args...);
+  kernel<<<grid, threads, smem, st>>>(args...);
   return cudaGetLastError();
 }
 
 template <int D, int V>
-cudaError_t launch_d(const ScanArgs &a, const TcParams &p, const CUtensorMap &tx,
-                     const CUtensorMap &ty, const CUtensorMap &tz, cudaStream_t st) {
-  if (a.fin)
-    return a.out_f32 ? launch<D, V, 3, float>(a, p, tx, ty, tz, st)
-                     : launch<D, V, 3, __nv_bfloat16>(a, p, tx, ty, tz, st);
-  return a.out_f32 ? launch<D, V, 2, float>(a, p, tx, ty, tz, st)
-                   : launch<D, V, 2, __nv_bfloat16>(a, p, tx, ty, tz, st);
+cudaError_t launch_scan_as(const Scan &s, cudaStream_t st) {
+  auto go = [&](auto *kernel, auto shape) {
+    using Sh = decltype(shape);
+    return launch_behind(kernel, s, Sh::kThreads, Sh::kSmem, st, s.p, s.x, s.y, s.z);
+  };
+  if (s.a.fin)
+    return s.a.out_f32 ? go(decay_kernel<D, V, 3, float>, Shape<D, 3>{})
+                       : go(decay_kernel<D, V, 3, __nv_bfloat16>, Shape<D, 3>{});
+  return s.a.out_f32 ? go(decay_kernel<D, V, 2, float>, Shape<D, 2>{})
+                     : go(decay_kernel<D, V, 2, __nv_bfloat16>, Shape<D, 2>{});
 }
-
-template <int V, int kTerms, typename O>
-cudaError_t launch_kv(const ScanArgs &a, const KvParams &kp, const CUtensorMap &tk,
-                      const CUtensorMap &tv, const CUtensorMap &tq, const CUtensorMap &tg,
-                      cudaStream_t st) {
-  const TcParams &p = kp.c;
-  cudaError_t e;
-  if (p.ranks > 1) {
-    using Sh = OwnShape<64, kTerms>;
-    const auto kernel = own_state_kernel<64, kTerms>;
-    if ((e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                  Sh::kSmem)) != cudaSuccess)
-      return e;
-    kernel<<<dim3(p.ranks - 1, a.H, a.B), Sh::kThreads, Sh::kSmem, st>>>(p, tq, tg);
-    count_launch();
-    if ((e = cudaGetLastError()) != cudaSuccess) return e;
-  }
-  using Sh = KvShape<kTerms>;
-  const auto kernel = kv_kernel<V, kTerms, O>;
-  if ((e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, Sh::kSmem)) !=
-      cudaSuccess)
-    return e;
-  const dim3 grid(p.ranks, a.H, a.B);
-  count_launch();
-  if (p.ranks > 1)  // as the scan behind its own-state kernel
-    return launch_pdl(kernel, grid, dim3(Sh::kThreads), Sh::kSmem, st, kp, tk, tv, tq, tg);
-  kernel<<<grid, Sh::kThreads, Sh::kSmem, st>>>(kp, tk, tv, tq, tg);
-  return cudaGetLastError();
+cudaError_t launch_scan(const Scan &s, cudaStream_t st) {
+  const cudaError_t e = own_states(s, st);
+  if (e != cudaSuccess) return e;
+  if (s.a.D == 32) return launch_scan_as<64, 32>(s, st);
+  return s.a.D == 64 ? launch_scan_as<64, 64>(s, st) : launch_scan_as<128, 128>(s, st);
 }
 
 template <int V>
-cudaError_t launch_kv_v(const ScanArgs &a, const KvParams &kp, const CUtensorMap &tk,
-                        const CUtensorMap &tv, const CUtensorMap &tq, const CUtensorMap &tg,
-                        cudaStream_t st) {
-  if (a.fin)
-    return a.out_f32 ? launch_kv<V, 3, float>(a, kp, tk, tv, tq, tg, st)
-                     : launch_kv<V, 3, __nv_bfloat16>(a, kp, tk, tv, tq, tg, st);
-  return a.out_f32 ? launch_kv<V, 2, float>(a, kp, tk, tv, tq, tg, st)
-                   : launch_kv<V, 2, __nv_bfloat16>(a, kp, tk, tv, tq, tg, st);
+cudaError_t launch_kv_as(const Scan &dv, const Scan &dk, cudaStream_t st) {
+  auto go = [&](auto *kernel, auto shape) {
+    using Sh = decltype(shape);
+    return launch_behind(kernel, dv, Sh::kThreads, Sh::kSmem, st, KvParams{dv.p, dk.a.out}, dv.x,
+                         dk.x, dv.y, dv.z);
+  };
+  if (dv.a.fin)
+    return dv.a.out_f32 ? go(kv_kernel<V, 3, float>, KvShape<3>{})
+                        : go(kv_kernel<V, 3, __nv_bfloat16>, KvShape<3>{});
+  return dv.a.out_f32 ? go(kv_kernel<V, 2, float>, KvShape<2>{})
+                      : go(kv_kernel<V, 2, __nv_bfloat16>, KvShape<2>{});
+}
+cudaError_t launch_kv(const Scan &dv, const Scan &dk, cudaStream_t st) {
+  const cudaError_t e = own_states(dv, st);
+  if (e != cudaSuccess) return e;
+  return dv.a.D == 32 ? launch_kv_as<32>(dv, dk, st) : launch_kv_as<64>(dv, dk, st);
 }
 
-TcParams tc_params(const ScanArgs &a, float *scratch, double chunk = 1) {
-  TcParams p = {};
-  p.out = a.out, p.log_decay = a.log_decay, p.seq_lens = a.seq_lens;
-  p.init = a.init, p.fin = a.fin, p.part = scratch;
-  p.init_scale = a.init_scale, p.fin_scale = a.fin_scale, p.scale = a.scale;
-  p.N = a.N, p.H = a.H, p.gx = a.gx, p.gy = a.gy, p.gz = a.gz;
-  p.zero_pad = a.zero_pad, p.init_t = a.init_t, p.reverse = a.reverse;
-  p.seg = segment_for(a, chunk), p.ranks = ((a.N + kC - 1) / kC + p.seg - 1) / p.seg;
-  return p;
-}
+// Keys and values together where the state fits beside both (D <= 64).
+bool together(const ScanArgs &a) { return a.D <= 64; }
 
 }  // namespace
 
@@ -1558,43 +1583,32 @@ bool tc_scan_supports(const ScanArgs &a) {
   return major == 10 && minor == 3 && encode_fn() != nullptr;
 }
 
-constexpr double kKvChunk = 1.6;
-
-static size_t part_floats(const ScanArgs &a, double chunk) {
-  const int seg = segment_for(a, chunk), ranks = ((a.N + kC - 1) / kC + seg - 1) / seg;
-  const size_t d = a.D < 64 ? 64 : a.D;
-  return ranks > 1 ? (size_t)a.B * a.H * ranks * d * d : 0;
-}
-
 size_t tc_scan_floats(const ScanArgs &a) { return part_floats(a, 1); }
-size_t tc_kv_floats(const ScanArgs &dv) { return part_floats(dv, kKvChunk); }
 
 cudaError_t tc_scan(const ScanArgs &a, float *scratch, cudaStream_t st) {
-  CUtensorMap tx, ty, tz;
-  cudaError_t e;
-  if ((e = make_map(&tx, a.x, a.B, a.N, a.H / a.gx, a.D, a.sx)) != cudaSuccess) return e;
-  if ((e = make_map(&ty, a.y, a.B, a.N, a.H / a.gy, a.D, a.sy)) != cudaSuccess) return e;
-  if ((e = make_map(&tz, a.z, a.B, a.N, a.H / a.gz, a.D, a.sz)) != cudaSuccess) return e;
-  const TcParams p = tc_params(a, scratch);
-  if (a.D == 32) return launch_d<64, 32>(a, p, tx, ty, tz, st);
-  return a.D == 64 ? launch_d<64, 64>(a, p, tx, ty, tz, st)
-                   : launch_d<128, 128>(a, p, tx, ty, tz, st);
+  Scan s;
+  const cudaError_t e = s.set(a, scratch);
+  if (e != cudaSuccess) return e;
+  return e == cudaSuccess ? launch_scan(s, st) : e;
 }
 
-bool tc_kv_supports(const ScanArgs &dv) { return dv.D <= 64 && tc_scan_supports(dv); }
+// The scans follow one another, so one scratch serves them.
+size_t tc_backward_floats(const ScanArgs *scan) {
+  const size_t one = part_floats(scan[0], 1);
+  const size_t two = part_floats(scan[1], together(scan[0]) ? kKvChunk : 1);
+  return one > two ? one : two;
+}
 
-cudaError_t tc_kv(const ScanArgs &dv, const void *v, const long long (&sv)[2], void *dk,
-                  float *scratch, cudaStream_t st) {
-  CUtensorMap tk, tv, tq, tg;
+cudaError_t tc_backward(const ScanArgs *scan, float *scratch, cudaStream_t st) {
+  Scan s[3];
+  const bool kv = together(scan[0]);
   cudaError_t e;
-  const int kv_heads = dv.H / dv.gx;
-  if ((e = make_map(&tk, dv.x, dv.B, dv.N, kv_heads, dv.D, dv.sx)) != cudaSuccess) return e;
-  if ((e = make_map(&tv, v, dv.B, dv.N, kv_heads, dv.D, sv)) != cudaSuccess) return e;
-  if ((e = make_map(&tq, dv.y, dv.B, dv.N, dv.H, dv.D, dv.sy)) != cudaSuccess) return e;
-  if ((e = make_map(&tg, dv.z, dv.B, dv.N, dv.H, dv.D, dv.sz)) != cudaSuccess) return e;
-  const KvParams kp = {tc_params(dv, scratch, kKvChunk), dk};
-  return dv.D == 32 ? launch_kv_v<32>(dv, kp, tk, tv, tq, tg, st)
-                    : launch_kv_v<64>(dv, kp, tk, tv, tq, tg, st);
+  for (int i = 0; i < 3; ++i)
+    if ((e = s[i].set(scan[i], scratch, kv && i > 0 ? kKvChunk : 1)) != cudaSuccess) return e;
+  if ((e = launch_scan(s[0], st)) != cudaSuccess) return e;
+  if (kv) return launch_kv(s[1], s[2], st);
+  if ((e = launch_scan(s[1], st)) != cudaSuccess) return e;
+  return launch_scan(s[2], st);
 }
 
 unsigned decay_device_error(bool reset) {

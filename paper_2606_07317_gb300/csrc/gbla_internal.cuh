@@ -212,12 +212,10 @@ cudaError_t simt_scan(const ScanArgs *a, int n, float *scratch, cudaStream_t st)
 bool tc_scan_supports(const ScanArgs &a);
 size_t tc_scan_floats(const ScanArgs &a);
 cudaError_t tc_scan(const ScanArgs &a, float *scratch, cudaStream_t st);
-// The gradients of values (the scan dv: x = k, y = q, z = d_o, in reverse) and of
-// keys in one pass: D <= 64.  v with its strides; dk like dv.out.
-bool tc_kv_supports(const ScanArgs &dv);
-size_t tc_kv_floats(const ScanArgs &dv);
-cudaError_t tc_kv(const ScanArgs &dv, const void *v, const long long (&sv)[2], void *dk,
-                  float *scratch, cudaStream_t st);
+// The backward's three scans: dq, dv (x = k, y = q, z = d_o) and dk (x = v, y = d_o,
+// z = q), the last two in reverse.
+size_t tc_backward_floats(const ScanArgs *scan);
+cudaError_t tc_backward(const ScanArgs *scan, float *scratch, cudaStream_t st);
 unsigned decay_device_error(bool reset);
 // dst[b, t, hk, :] = sum of the G heads of src that share it, in head order
 // (src fp32 [tokens, Hk * G, D], dst of the given type [tokens, Hk, D]).

@@ -1083,10 +1083,9 @@ gbla_status gbla_decay_attention_backward(
   } else if ((s = run_scans(scan, 3, tc, st)) != GBLA_OK) {
     return s;
   }
-  for (int i = 1; i < 3 && G > 1; ++i)
-    if ((s = from_cuda(sum_shared_heads((const float *)scan[i].out, i == 2 ? dk : dv,
-                                        (long long)tok, Hk, G, D, dtype, st))) != GBLA_OK)
-      return s;
+  if (G > 1)
+    return from_cuda(sum_shared_heads((const float *)scan[1].out, (const float *)scan[2].out, dv,
+                                      dk, (long long)tok, Hk, G, D, dtype, st));
   return GBLA_OK;
 }
 

@@ -436,16 +436,23 @@ cudaError_t scan_d(const ScanArgs &a, const ScanBatch &p, cudaStream_t st) {
 }
 
 // ------------------------------------------------ sum over shared heads
+// dv (blockIdx.y = 0) and dk from the G query heads' planes that share each key
+// head, summed in 32 bits in the heads' order and rounded once.  Bound by bytes:
+// 4 G read and 2 or 4 written for each value.  A head has 2^lg quads of 4 values.
 template <typename T>
-__global__ void __launch_bounds__(256) shared_sum_kernel(const float *__restrict__ src,
-                                                         T *__restrict__ dst, long long quads,
-                                                         int G, int D4) {
+__global__ void __launch_bounds__(256) shared_sum_kernel(const float *__restrict__ v_planes,
+                                                         const float *__restrict__ k_planes,
+                                                         T *__restrict__ dv, T *__restrict__ dk,
+                                                         long long quads, int G, int lg) {
+  grid_dep_wait();
+  grid_dep_launch();
+  const float *src = blockIdx.y == 0 ? v_planes : k_planes;
+  T *dst = blockIdx.y == 0 ? dv : dk;
   for (long long i = blockIdx.x * 256ll + threadIdx.x; i < quads; i += gridDim.x * 256ll) {
-    const long long head = i / D4;  // (token, key head)
-    const int c = (int)(i % D4);
+    const float4 *at = (const float4 *)src + (((i >> lg) * G) << lg) + (i & ((1 << lg) - 1));
     float a[4] = {};
     for (int g = 0; g < G; ++g) {
-      const float4 v = __ldg((const float4 *)src + (head * G + g) * D4 + c);
+      const float4 v = *(at + ((long long)g << lg));
       a[0] += v.x, a[1] += v.y, a[2] += v.z, a[3] += v.w;
     }
     store4(dst + i * 4, a);
@@ -545,18 +552,20 @@ cudaError_t simt_scan(const ScanArgs *a, int n, float *scratch, cudaStream_t st)
   return scan_d<__nv_bfloat16, __nv_bfloat16>(*a, p, st);
 }
 
-cudaError_t sum_shared_heads(const float *src, void *dst, long long tokens, int Hk, int G, int D,
-                             gbla_dtype dtype, cudaStream_t st) {
+cudaError_t sum_shared_heads(const float *v_planes, const float *k_planes, void *dv, void *dk,
+                             long long tokens, int Hk, int G, int D, gbla_dtype dtype,
+                             cudaStream_t st) {
   const long long quads = tokens * Hk * (D / 4);
   long long blocks = (quads + 255) / 256;
-  if (blocks > 8ll * sm_count()) blocks = 8ll * sm_count();
-  if (dtype == GBLA_FP32)
-    shared_sum_kernel<float><<<(int)blocks, 256, 0, st>>>(src, (float *)dst, quads, G, D / 4);
-  else
-    shared_sum_kernel<__nv_bfloat16>
-        <<<(int)blocks, 256, 0, st>>>(src, (__nv_bfloat16 *)dst, quads, G, D / 4);
+  if (blocks > 4ll * sm_count()) blocks = 4ll * sm_count();
+  const dim3 grid((unsigned)blocks, 2);
+  const int lg = D == 32 ? 3 : D == 64 ? 4 : 5;
   count_launch();
-  return cudaGetLastError();
+  if (dtype == GBLA_FP32)
+    return launch_pdl(shared_sum_kernel<float>, grid, dim3(256), 0, st, v_planes, k_planes,
+                      (float *)dv, (float *)dk, quads, G, lg);
+  return launch_pdl(shared_sum_kernel<__nv_bfloat16>, grid, dim3(256), 0, st, v_planes, k_planes,
+                    (__nv_bfloat16 *)dv, (__nv_bfloat16 *)dk, quads, G, lg);
 }
 
 cudaError_t decay_step(const StepArgs &a, cudaStream_t st) {

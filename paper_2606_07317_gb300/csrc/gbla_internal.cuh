@@ -217,10 +217,11 @@ cudaError_t tc_scan(const ScanArgs &a, float *scratch, cudaStream_t st);
 size_t tc_backward_floats(const ScanArgs *scan);
 cudaError_t tc_backward(const ScanArgs *scan, float *scratch, cudaStream_t st);
 unsigned decay_device_error(bool reset);
-// dst[b, t, hk, :] = sum of the G heads of src that share it, in head order
-// (src fp32 [tokens, Hk * G, D], dst of the given type [tokens, Hk, D]).
-cudaError_t sum_shared_heads(const float *src, void *dst, long long tokens, int Hk, int G, int D,
-                             gbla_dtype dtype, cudaStream_t st);
+// dv and dk [tokens, Hk, D] of the given type: sums, in head order, of the G heads of
+// the fp32 planes [tokens, Hk * G, D] that share a key head.
+cudaError_t sum_shared_heads(const float *v_planes, const float *k_planes, void *dv, void *dk,
+                             long long tokens, int Hk, int G, int D, gbla_dtype dtype,
+                             cudaStream_t st);
 struct StepArgs {
   const void *q, *k, *v;                // one token of each sequence; row strides in elements
   long long sq, sk, sv;

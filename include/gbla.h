@@ -476,7 +476,7 @@ gbla_status gbla_qk_norm_rotate_backward(
  *   o         [B, N, H, D] dtype; rows t >= L_b untouched
  *   state_out [B, H, D, D] fp32 or NULL: S after each sequence's last token
  *             (state_in for an empty one)
- * scale is finite and not 0.  Computed in chunks of tokens: bf16 on tensor
+ * scale is finite, not 0 and not subnormal.  Computed in chunks of tokens: bf16 on tensor
  * cores (GBLA_ALGO_TC), fp32 on CUDA cores (GBLA_ALGO_SIMT, which covers both
  * dtypes); the state is held in fp32 on both.  A NaN or infinity in a
  * valid token reaches the other tokens of its chunk, before it too; what

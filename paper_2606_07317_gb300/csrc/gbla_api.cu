@@ -898,8 +898,9 @@ gbla_status pass_state(const float *in, float *out, size_t bytes, cudaStream_t s
                       : cudaMemsetAsync(out, 0, bytes, st));
 }
 
+// (The backward holds its reverse state without the scale: 1 / scale has to be finite.)
 gbla_status check_scale(float scale) {
-  return isfinite(scale) && scale != 0.f ? GBLA_OK : GBLA_ERR_INVALID_ARG;
+  return isnormal(scale) ? GBLA_OK : GBLA_ERR_INVALID_ARG;
 }
 
 }  // namespace

@@ -68,8 +68,8 @@ struct ScanDev {
   float *fin, *part;
   int N, H, seg, nseg;  // tokens per segment (a multiple of kC), most segments
 };
-// Scans of the same sizes in one launch: those of a batch row follow one another
-// in the grid's z.
+// Scans of the same sizes in one launch: those of a head follow one another in the
+// grid's x.
 struct ScanBatch {
   ScanDev scan[kMaxScans];
   int n;
@@ -128,10 +128,11 @@ __global__ void __launch_bounds__(kThreadsOf<D>, ScanShape<D, kState>::kBlocks)
   float *ps = sm + Sh::kOffP;  // [kC][kPRow] weighted scores
   float *st = sm + Sh::kOffS;  // [D][E] the state
   float *gp = sm + Sh::kOffG;  // gamma^0 .. gamma^kC
-  const ScanDev &p = batch.scan[blockIdx.z % batch.n];
+  const int each = gridDim.x / batch.n, place = blockIdx.x % each;
+  const ScanDev &p = batch.scan[blockIdx.x / each];
   const int tid = threadIdx.x;
-  const int seg = blockIdx.x / Sh::kSplit, e0 = blockIdx.x % Sh::kSplit * E;
-  const int h = blockIdx.y, b = blockIdx.z / batch.n;
+  const int seg = place / Sh::kSplit, e0 = place % Sh::kSplit * E;
+  const int h = blockIdx.y, b = blockIdx.z;
   if (kState) grid_dep_launch();  // the prefix kernel waits for this one's results
   const int L = p.seq_lens ? min(max(p.seq_lens[b], 0), p.N) : p.N;
   const int ns = (L + p.seg - 1) / p.seg;
@@ -324,8 +325,9 @@ __global__ void __launch_bounds__(kThreadsOf<D>, ScanShape<D, kState>::kBlocks)
 // the segments before it in scan order, in that order.  Four elements a thread.
 __global__ void __launch_bounds__(128) prefix_kernel(const ScanBatch batch, int D) {
   grid_dep_wait();  // (an early launch of the scan would place its blocks unevenly)
-  const ScanDev &p = batch.scan[blockIdx.z % batch.n];
-  const int h = blockIdx.y, b = blockIdx.z / batch.n, i = (blockIdx.x * 128 + threadIdx.x) * 4;
+  const int each = gridDim.x / batch.n;
+  const ScanDev &p = batch.scan[blockIdx.x / each];
+  const int h = blockIdx.y, b = blockIdx.z, i = (blockIdx.x % each * 128 + threadIdx.x) * 4;
   const int L = p.seq_lens ? min(max(p.seq_lens[b], 0), p.N) : p.N;
   const int ns = (L + p.seg - 1) / p.seg;
   if (i >= D * D || ns == 0) return;
@@ -401,7 +403,7 @@ ScanDev scan_dev(const ScanArgs &a, int scans, float *part) {
 template <typename T, typename O, int D>
 cudaError_t scan_launch(const ScanArgs &a, const ScanBatch &p, cudaStream_t st) {
   const int nseg = p.scan[0].nseg;
-  const dim3 grid(nseg * ScanShape<D, true>::kSplit, a.H, a.B * p.n);
+  const dim3 grid(nseg * ScanShape<D, true>::kSplit * p.n, a.H, a.B);
   cudaError_t e;
   if (nseg > 1) {
     constexpr int smem = ScanShape<D, true>::kSmemFloats * 4;
@@ -413,7 +415,7 @@ cudaError_t scan_launch(const ScanArgs &a, const ScanBatch &p, cudaStream_t st) 
     count_launch();
     if ((e = cudaGetLastError()) != cudaSuccess) return e;
     count_launch();
-    if ((e = launch_pdl(prefix_kernel, dim3((D * D / 4 + 127) / 128, a.H, a.B * p.n), dim3(128), 0,
+    if ((e = launch_pdl(prefix_kernel, dim3((D * D / 4 + 127) / 128 * p.n, a.H, a.B), dim3(128), 0,
                         st, p, D)) != cudaSuccess)
       return e;
   }

@@ -324,6 +324,25 @@ def test_step(B, H, Hk, D, dtype):
     _close(o, ref, om, u, dtype, "o")
 
 
+def test_gradients_of_very_many_short_sequences():
+    """More sequences than a third of a grid's 65535 rows, two tokens each."""
+    g = torch.Generator().manual_seed(5)
+    q, k, v, do = (torch.randn((22000, 2, 1, 32), generator=g) for _ in range(4))
+    ld = torch.tensor([-0.25])
+    got = gbla.decay_attention_backward(q.cuda(), k.cuda(), v.cuda(), ld.cuda(), do.cuda(), scale=0.5)
+    q, k, v, do = (t.double()[:, :, 0] for t in (q, k, v, do))
+    w = 0.5 * torch.exp(ld.double()) ** (torch.arange(2)[:, None] - torch.arange(2)).clamp(min=0) * torch.ones(2, 2).tril()
+
+    def grads(q, k, v, do):
+        dp, p = (do @ v.mT) * w, (q @ k.mT) * w
+        return {"dq": dp @ k, "dk": dp.mT @ q, "dv": p.mT @ do}
+    ref, mag = grads(q, k, v, do), grads(q.abs(), k.abs(), v.abs(), do.abs())
+    for name in ref:
+        err = (got[name].cpu().double()[:, :, 0] - ref[name]).abs()
+        tol = (32 + 80) * 2.0 ** -22 * mag[name]
+        assert bool((err <= tol).all()), (name, float((err / tol).max()))
+
+
 def test_steps_do_not_drift():
     """A weak decay over 4096 steps (keys of zero) against the exact power: each step rounds
     once to 2^-24 at random, sqrt(n) 2^-24 of the norm (times 8); a decay held in one float

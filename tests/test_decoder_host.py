@@ -95,6 +95,12 @@ def test_scale(lib, op):
         assert _run(lib, op, scale=s) == INV, s
 
 
+@pytest.mark.parametrize("op", ["decay", "decay_backward", "step"])
+def test_scale_without_a_reciprocal(lib, op):
+    for s in (1e-40, -1e-45):
+        assert _run(lib, op, scale=s) == INV, s
+
+
 @pytest.mark.parametrize("op", ["decay", "decay_backward"])
 def test_family(lib, op):
     assert _run(lib, op, algo=7) == UNS

@@ -867,9 +867,8 @@ gbla_status check_rotate(RotateArgs *a, View *vq, View *vk, const void *q, const
 // n scans of the same sizes with the tensor-core family (one after the other) or
 // the CUDA-core one (side by side), their scratch from the pool.
 gbla_status run_scans(const ScanArgs *a, int n, bool tc, cudaStream_t st) {
-  const bool apart = tc || (long long)a->B * n > kMaxBH;
-  for (int i = 0; i < n; i += apart ? 1 : n) {
-    const int m = apart ? 1 : n;
+  const int m = tc ? 1 : n;
+  for (int i = 0; i < n; i += m) {
     Scratch ws;
     const size_t floats = tc ? tc_scan_floats(a[i]) : simt_scan_floats(a[i], m);
     gbla_status s = ws.alloc(sizeof(float) * floats, st);

@@ -22,8 +22,9 @@
 // cut into several where whole ones would leave SMs idle or one long sequence
 // would outlast the rest; a first kernel then sums the state of every segment but
 // the last in scan order (y and z alone, the chunk that the scan starts with read
-// last, so that it is still in L2), and the scan starts from the weighted sum of
-// the segments before its own.  The second launch begins while the first ends.
+// last, so that it is still in L2), a second one turns them into the states before
+// the segments, and the scan starts from those.  Each launch begins while the one
+// before it ends.
 //
 // What bounds a chunk (D = 64): memory takes 32 KB of it, 1430 cycles of an SM's
 // share of the measured bandwidth; shared memory some 144 KB (operands of the
@@ -112,6 +113,7 @@ struct TcParams {
   int N, H, gx, gy, gz;
   int seg, ranks;  // chunks of a segment, most segments of a sequence
   bool zero_pad, init_t, reverse;
+  bool before;     // `part` holds the states before the segments, not their own
 };
 
 __device__ __forceinline__ void decay_error(unsigned code, const AbortFlag &ab) {
@@ -335,6 +337,15 @@ __device__ __forceinline__ int state_at(int sw, int lane, int i, int *e) {
   return 32 * (sw & 3) + lane;
 }
 
+// A state thread's value i of the scan's first state (V: its size in memory).
+template <int D, int V>
+__device__ __forceinline__ float first_state(const TcParams &p, size_t bh, int sw, int lane, int i) {
+  int e;
+  const int d = state_at<D>(sw, lane, i, &e);
+  if (V < D && (d >= V || e >= V)) return 0.f;
+  return p.init_scale * __ldg(p.init + bh * V * V + (p.init_t ? e * V + d : d * V + e));
+}
+
 // S = S + f v (own) or S = f S + v over a state thread's values, from the columns
 // at src (D = 64: the small terms' columns first).
 template <int D, bool kOwn, int kNV>
@@ -364,12 +375,12 @@ __device__ __forceinline__ void take_state(float (&S)[kNV], uint32_t src, DecayF
     }
   } else {
 #pragma unroll
-    for (int k = 0; k < 4; ++k) {
-      float v[16];
-      tmem_ld16(src + 16 * k, v);
+    for (int k = 0; k < 8; ++k) {  // (16 at a time spilled)
+      float v[8];
+      tmem_ld8(src + 8 * k, v);
       tmem_ld_wait_regs(v);
 #pragma unroll
-      for (int e = 0; e < 16; e += 2) add(16 * k + e, make_float2(v[e], v[e + 1]));
+      for (int e = 0; e < 8; e += 2) add(8 * k + e, make_float2(v[e], v[e + 1]));
     }
   }
 }
@@ -388,15 +399,43 @@ struct Segment {
   __device__ __forceinline__ int token_of(int place) const {
     return (reverse ? nc - 1 - place : place) * kC;
   }
+  // Tokens that the first state decays by before the segment (in reverse it belongs to
+  // the last token).
+  __device__ __forceinline__ int tokens_before() const {
+    return !reverse ? q0 * kC : q0 == 0 ? 0 : L - 1 - (nc - q0) * kC;
+  }
 };
+
+// D = 64: the state before segment `rank`, from part or from the segments' own
+// states and the first one, into S = 0.
+template <int V>
+__device__ __forceinline__ void start_state(float (&S)[32], const TcParams &p, const Segment &sg,
+                                            size_t bh, int rank, int sw, int lane, float l2) {
+  if (p.ranks > 1) {
+    grid_dep_wait();
+    const float *part = p.part + bh * p.ranks * 64 * 64 + 32 * sw + lane;
+    const int end = p.before ? rank + 1 : rank;
+    for (int s = p.before ? rank : 0; s < end; ++s) {
+      const float f = decay_pow(l2, (float)(end - 1 - s) * p.seg * kC);
+#pragma unroll
+      for (int i = 0; i < 32; ++i) S[i] = fmaf(f, __ldcg(part + ((size_t)s * 32 + i) * 128), S[i]);
+    }
+  }
+  if (p.init && !p.before) {
+    const float f = decay_pow(l2, (float)sg.tokens_before());
+#pragma unroll
+    for (int i = 0; i < 32; ++i) S[i] = fmaf(f, first_state<64, V>(p, bh, sw, lane, i), S[i]);
+  }
+}
 
 // ---------------------------------------------------------------------------
 // The state of each segment but the last, without what comes before it.  Chunks
 // go by from the segment's end in scan order to its start; kGroup of them add up
 // in TMEM (their distance from the first is in the weights), then the state warps
 // take the sum.  (The tensor cores' sums are cut, not rounded: where the state is a
-// result, 96 additions in a row showed at 1e-6 of it, so there are fewer.)  Warps: 0-7 form v_j y_j (two groups, alternate chunks), the next
-// 4 (D = 128: 8) hold the state, then loads and MMAs.
+// result, 96 additions in a row showed at 1e-6 of it, so there are fewer.)  Warps:
+// 0-7 form v_j y_j (two groups, alternate chunks), the next 4 (D = 128: 8) hold the
+// state, then loads and MMAs.
 
 template <int D, int kTerms>
 struct OwnShape {
@@ -582,6 +621,54 @@ __global__ void __launch_bounds__(OwnShape<D, kTerms>::kThreads, OwnShape<D, kTe
 }
 
 // ---------------------------------------------------------------------------
+// The state before each segment in place of its own state, from the scan's first
+// state on: for each value the segments go by in scan order, 8 loads at a time.
+// D = 64 up to 12 segments: without this launch, the scan's state warps sum the
+// segments before theirs while others still run (9: B2 H8 N32768 81 us, with it 84; 32:
+// B1 H4 N32768 42 us, with it 33).  At D = 128 they have no registers for enough loads
+// in flight (4.5 us a segment; 32 of them: B1 H3 N8192 101 us, with this launch 25; 9:
+// B2 H8 N16384 108 and 93; 2: B8 H8 N2048 54 and 56).
+template <int D, int V>
+__global__ void __launch_bounds__(256) before_kernel(const TcParams p) {
+  constexpr int kT = D == 64 ? 128 : 256, kBatch = 8;  // the state's threads in a scan
+  grid_dep_launch();
+  const int h = blockIdx.y, b = blockIdx.z, at = (blockIdx.x * 256 + threadIdx.x) * 4;
+  const size_t bh = (size_t)b * p.H + h;
+  const Segment sg(p, b, 0);
+  const int ns = max(1, (sg.nc + p.seg - 1) / p.seg);
+  float S[4] = {};
+  if (p.init)
+#pragma unroll
+    for (int c = 0; c < 4; ++c)
+      S[c] = first_state<D, V>(p, bh, (at + c) % kT >> 5, (at + c) & 31, at / kT);
+  // tokens of the first segment that the first state decays by (reverse: it belongs
+  // to the last token), and of the others
+  const float ld = __ldg(p.log_decay + h);
+  const int first = p.reverse ? sg.L - 1 - (sg.nc - p.seg) * kC : p.seg * kC;  // as tokens_before
+  const DecayFactor w0 = decay_factor(ld * first), w1 = decay_factor(ld * (p.seg * kC));
+  float *part = p.part + bh * p.ranks * D * D + at;
+  if (ns > 1) grid_dep_wait();  // (one segment: no other kernel writes to its place)
+  for (int r0 = 0; r0 < ns; r0 += kBatch) {
+    float4 own[kBatch];
+#pragma unroll
+    for (int u = 0; u < kBatch; ++u)
+      own[u] = r0 + u + 1 < ns ? __ldcg((const float4 *)(part + (size_t)(r0 + u) * D * D))
+                               : make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+    for (int u = 0; u < kBatch; ++u) {
+      const int r = r0 + u;
+      if (r >= ns) break;
+      *(float4 *)(part + (size_t)r * D * D) = make_float4(S[0], S[1], S[2], S[3]);
+      const DecayFactor w = r == 0 ? w0 : w1;
+      S[0] = fmaf(w.hi, S[0], fmaf(w.lo, S[0], own[u].x));
+      S[1] = fmaf(w.hi, S[1], fmaf(w.lo, S[1], own[u].y));
+      S[2] = fmaf(w.hi, S[2], fmaf(w.lo, S[2], own[u].z));
+      S[3] = fmaf(w.hi, S[3], fmaf(w.lo, S[3], own[u].w));
+    }
+  }
+}
+
+// ---------------------------------------------------------------------------
 // The scan of each segment.  V: the heads' size in memory (32 runs as D = 64 with
 // the missing channels loaded as zeros).
 template <int D, int V, int kTerms, typename O>
@@ -620,7 +707,7 @@ __global__ void __launch_bounds__(Shape<D, kTerms>::kThreads, 1)
       ((uint4 *)(out + (L + i / kPer) * orow))[i % kPer] = make_uint4(0, 0, 0, 0);
   }
   if (cnt == 0) {
-    if (p.ranks > 1) grid_dep_wait();  // a grid never ends before the own-state kernel
+    if (p.ranks > 1) grid_dep_wait();  // a grid never ends before the kernels ahead of it
     if (rank == 0 && p.fin)  // an empty sequence passes its state on
       for (int i = tid; i < V * V; i += Sh::kThreads)
         p.fin[bh * V * V + i] = p.init ? p.init[bh * V * V + i] * p.init_scale * p.fin_scale : 0.f;
@@ -860,29 +947,27 @@ __global__ void __launch_bounds__(Shape<D, kTerms>::kThreads, 1)
     const uint32_t src = tmem + ((uint32_t)(32 * (sw & 3)) << 16) + Sh::kColDs +
                          (D == 64 ? 0 : 64 * (sw >> 2));
     if (lane == 0) mbar_arrive(&state_ready[0]);
-    if (rank > 0) {  // the segments before
-      grid_dep_wait();
-      const float *part = p.part + bh * p.ranks * D * D + (tid - 8 * 32);
-      for (int s = 0; s < rank; ++s) {
-        const float f = decay_pow(l2, (float)(rank - 1 - s) * p.seg * kC);
-#pragma unroll
-        for (int i = 0; i < kNV; ++i)
-          S[i] = fmaf(f, __ldcg(part + ((size_t)s * kNV + i) * (Sh::kSWarps * 32)), S[i]);
-      }
-    }
-    if (p.init) {
-      // tokens between the first state and this segment (reverse: and the last
-      // token, which that state belongs to)
-      const float n = !p.reverse ? (float)q0 * kC : q0 == 0 ? 0.f : (float)(L - 1 - (sg.nc - q0) * kC);
-      const float f = decay_pow(l2, n) * p.init_scale;
-      const float *s0 = p.init + bh * V * V;
-#pragma unroll
-      for (int i = 0; i < kNV; ++i) {
+    if constexpr (D == 64) {
+      start_state<V>(S, p, sg, bh, rank, sw, lane, l2);
+    } else {
+      // The state before the segment, or the first one, in one loop: in two they cost the
+      // kernel more spilled registers (B19 H8 N4096 132 us, so 127).
+      const float *from = nullptr;
+      int step = 0;
+      float f = 0.f;
+      if (p.ranks > 1) {
+        grid_dep_wait();
+        from = p.part + (bh * p.ranks + rank) * D * D + (tid - 8 * 32), step = Sh::kSWarps * 32;
+        f = 1.f;
+      } else if (p.init) {
         int e;
-        const int d = state_at<D>(sw, lane, i, &e);
-        if (V == D || (d < V && e < V))
-          S[i] = fmaf(f, __ldg(s0 + (p.init_t ? e * V + d : d * V + e)), S[i]);
+        const int d = state_at<D>(sw, lane, 0, &e);
+        from = p.init + bh * D * D + (p.init_t ? e * D + d : d * D + e), step = p.init_t ? D : 1;
+        f = p.init_scale;
       }
+      if (from)
+#pragma unroll
+        for (int i = 0; i < kNV; ++i, from += step) S[i] = f * __ldcg(from);
     }
     for (int j = 0; j < cnt; ++j) {
       if constexpr (D == 64) {  // behind the chunk's keys, once their slot is free
@@ -921,7 +1006,6 @@ __global__ void __launch_bounds__(Shape<D, kTerms>::kThreads, 1)
         if (V == D || (d < V && e < V)) p.fin[bh * V * V + d * V + e] = S[i] * f;
       }
     }
-    if (p.ranks > 1 && rank == 0) grid_dep_wait();
   } else {
     // ---------------------------------------------------------------- results
     const int ow = warp - Sh::kOutWarp, r0 = 16 * ow + (lane >> 2);
@@ -1072,7 +1156,7 @@ __global__ void __launch_bounds__(KvShape<kTerms>::kThreads, 1)
     }
   }
   if (cnt == 0) {
-    if (p.ranks > 1) grid_dep_wait();  // a grid never ends before the own-state kernel
+    if (p.ranks > 1) grid_dep_wait();  // a grid never ends before the kernels ahead of it
     if (rank == 0 && p.fin)  // an empty sequence passes its state on
       for (int i = tid; i < V * V; i += Sh::kThreads)
         p.fin[bh * V * V + i] = p.init ? p.init[bh * V * V + i] * p.init_scale * p.fin_scale : 0.f;
@@ -1276,28 +1360,7 @@ __global__ void __launch_bounds__(KvShape<kTerms>::kThreads, 1)
 #pragma unroll
     for (int i = 0; i < 32; ++i) S[i] = 0.f;
     if (lane == 0) mbar_arrive(&state_ready[0]);
-    if (rank > 0) {  // the segments before
-      grid_dep_wait();
-      const float *part = p.part + bh * p.ranks * D * D + (tid - 8 * 32);
-      for (int s = 0; s < rank; ++s) {
-        const float f = decay_pow(l2, (float)(rank - 1 - s) * p.seg * kC);
-#pragma unroll
-        for (int i = 0; i < 32; ++i)
-          S[i] = fmaf(f, __ldcg(part + ((size_t)s * 32 + i) * 128), S[i]);
-      }
-    }
-    if (p.init) {
-      // tokens from the last one, which the first state belongs to, to this segment
-      const float n = q0 == 0 ? 0.f : (float)(L - 1 - (sg.nc - q0) * kC);
-      const float f = decay_pow(l2, n) * p.init_scale;
-      const float *s0 = p.init + bh * V * V;
-#pragma unroll
-      for (int i = 0; i < 32; ++i) {
-        int e;
-        const int d = state_at<64>(sw, lane, i, &e);
-        if (V == D || (d < V && e < V)) S[i] = fmaf(f, __ldg(s0 + d * V + e), S[i]);
-      }
-    }
+    start_state<V>(S, p, sg, bh, rank, sw, lane, l2);
     for (int i = 0; i < cnt; ++i) {
       const int s = i % kN;
       if (!mbar_wait(&eq[s], ((i / kN) & 1) ^ 1, &ab)) decay_error(128, ab);
@@ -1324,7 +1387,6 @@ __global__ void __launch_bounds__(KvShape<kTerms>::kThreads, 1)
         if (V == D || (d < V && e < V)) p.fin[bh * V * V + d * V + e] = S[i] * f;
       }
     }
-    if (p.ranks > 1 && rank == 0) grid_dep_wait();
   } else {
     // ---------------------------------------------------------------- results
     const int ow = warp - 12, r0 = 16 * ow + (lane >> 2);
@@ -1436,7 +1498,7 @@ int sm_count() {
 // the work over the SMs and half a segment of tail, or as their longest CTA.
 // The pass over keys and values takes `chunk` = 1.6 scanned chunks a chunk.
 int segment_for(const ScanArgs &a, double chunk) {
-  const double fill = (a.D > 64 ? 5 : 9) / chunk, own_chunk = 0.6 / chunk;
+  const double fill = (a.D > 64 ? 3.5 : 9) / chunk, own_chunk = 0.6 / chunk;
   const int nc = (a.N + kC - 1) / kC, sms = sm_count();
   const double pairs = (double)a.B * a.H;
   auto rounds = [&](double ctas) { return (double)(long long)(ctas / sms + 0.999999); };
@@ -1486,6 +1548,7 @@ struct Scan {
     p.N = a.N, p.H = a.H, p.gx = a.gx, p.gy = a.gy, p.gz = a.gz;
     p.zero_pad = a.zero_pad, p.init_t = a.init_t, p.reverse = a.reverse;
     p.seg = segment_for(a, chunk), p.ranks = ranks_for(a, chunk);
+    p.before = p.ranks > (a.D > 64 ? 1 : 12);
     cudaError_t e;
     if ((e = make_map(&x, a.x, a.B, a.N, a.H / a.gx, a.D, a.sx)) != cudaSuccess) return e;
     if ((e = make_map(&y, a.y, a.B, a.N, a.H / a.gy, a.D, a.sy)) != cudaSuccess) return e;
@@ -1508,14 +1571,24 @@ cudaError_t launch_own(const Scan &s, cudaStream_t st) {
 // The states of the segments, where a sequence is cut into any.  (The backward's in
 // one launch ahead of its scans were slower: 120 us where it is 117 at B4 H8 N8192
 // D64, 363 for 320 at B2 N16384 D128; each scan finds less of its own in L2.)
-cudaError_t own_states(const Scan &s, cudaStream_t st) {
+cudaError_t states_before(const Scan &s, cudaStream_t st) {
   if (s.p.ranks <= 1) return cudaSuccess;
-  if (s.a.D > 64) return s.a.fin ? launch_own<128, 3>(s, st) : launch_own<128, 2>(s, st);
-  return s.a.fin ? launch_own<64, 3>(s, st) : launch_own<64, 2>(s, st);
+  const bool wide = s.a.D > 64;
+  const cudaError_t e =
+      wide ? s.a.fin ? launch_own<128, 3>(s, st) : launch_own<128, 2>(s, st)
+           : s.a.fin ? launch_own<64, 3>(s, st) : launch_own<64, 2>(s, st);
+  if (e != cudaSuccess) return e;
+  if (!s.p.before) return cudaSuccess;
+  count_launch();
+  return launch_pdl(wide          ? before_kernel<128, 128>
+                    : s.a.D == 64 ? before_kernel<64, 64>
+                                  : before_kernel<64, 32>,
+                    dim3(wide ? 16 : 4, s.a.H, s.a.B), dim3(256), 0, st, s.p);
 }
 
-// Launches a scan right behind its own-state kernel: it may start while that ends,
-// as only its state warps read what that kernel writes, and they wait for it.
+// Launches a scan right behind the kernels that form the states before its segments:
+// it may start while they end, as only its state warps read what they write, and
+// those wait for it.
 template <typename... KArgs, typename... Args>
 cudaError_t launch_behind(void (*kernel)(KArgs...), const Scan &s, int threads, int smem,
                           cudaStream_t st, Args... args) {
@@ -1542,7 +1615,7 @@ cudaError_t launch_scan_as(const Scan &s, cudaStream_t st) {
                      : go(decay_kernel<D, V, 2, __nv_bfloat16>, Shape<D, 2>{});
 }
 cudaError_t launch_scan(const Scan &s, cudaStream_t st) {
-  const cudaError_t e = own_states(s, st);
+  const cudaError_t e = states_before(s, st);
   if (e != cudaSuccess) return e;
   if (s.a.D == 32) return launch_scan_as<64, 32>(s, st);
   return s.a.D == 64 ? launch_scan_as<64, 64>(s, st) : launch_scan_as<128, 128>(s, st);
@@ -1562,7 +1635,7 @@ cudaError_t launch_kv_as(const Scan &dv, const Scan &dk, cudaStream_t st) {
                       : go(kv_kernel<V, 2, __nv_bfloat16>, KvShape<2>{});
 }
 cudaError_t launch_kv(const Scan &dv, const Scan &dk, cudaStream_t st) {
-  const cudaError_t e = own_states(dv, st);
+  const cudaError_t e = states_before(dv, st);
   if (e != cudaSuccess) return e;
   return dv.a.D == 32 ? launch_kv_as<32>(dv, dk, st) : launch_kv_as<64>(dv, dk, st);
 }

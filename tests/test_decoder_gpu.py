@@ -235,6 +235,28 @@ def test_decay_attention_backward(i, family):
     assert gbla.device_error() == 0
 
 
+@pytest.mark.parametrize("D,N,lens", [(64, 4100, [4100, 70]), (32, 4224, None), (128, 2600, [1, 2600])])
+def test_many_segments_from_a_first_state(D, N, lens):
+    """Few long sequences, which the tensor-core family cuts into many segments: states
+    going in and out in both directions."""
+    c = Case(300 + D, 2 if lens else 1, N, 2, 1, D, "bf16", lens)
+    q, k, v, do = c.tok(2), c.tok(1), c.tok(1), c.tok(2)
+    ld = torch.tensor([-2.0 ** -9, -2.0 ** -6])
+    s0, ds = (c.n(c.B, 2, D, D, to=torch.float32) for _ in range(2))
+    args, kw = [dev(c.poison(x)) for x in (q, k, v)] + [dev(ld)], dict(seq_lens=dev(c.seq_lens), state=dev(s0))
+    o, S = gbla.decay_attention(*args, return_state=True, **kw)
+    ref, Sr, om, Sm = R.decay(q, k, v, ld, c.lens, s0, D ** -0.5)
+    on = ~c.past()
+    _close(o.cpu()[on], ref[on], om[on], 2.0 ** -8, "bf16", "o", 2.0 ** -7)
+    _close(S, Sr, Sm, c32(c), "fp32", "state")
+    g = gbla.decay_attention_backward(*args, dev(c.poison(do)), dstate=dev(ds), return_dstate=True, **kw)
+    ref, mag = R.decay_backward(q, k, v, ld, do, c.lens, s0, ds, D ** -0.5)
+    for n in ("dq", "dk", "dv"):
+        _close(g[n], ref[n], mag[n], 2.0 ** -8, "bf16", n, 2.0 ** -7)
+    _close(g["dstate"], ref["dstate"], mag["dstate"], c32(c), "fp32", "dstate")
+    assert gbla.device_error() == 0
+
+
 @pytest.mark.parametrize("dtype,D", [("bf16", 32), ("bf16", 64), ("bf16", 128), ("fp32", 64)])
 def test_continued_prompt_and_steps_agree_with_one_call(dtype, D):
     """A prompt read in two calls and then token by token follows the one-call form."""

@@ -1498,7 +1498,7 @@ int sm_count() {
 // the work over the SMs and half a segment of tail, or as their longest CTA.
 // The pass over keys and values takes `chunk` = 1.6 scanned chunks a chunk.
 int segment_for(const ScanArgs &a, double chunk) {
-  const double fill = (a.D > 64 ? 3.5 : 9) / chunk, own_chunk = 0.6 / chunk;
+  const double fill = (a.D > 64 ? 4.2 : 9) / chunk, own_chunk = 0.6 / chunk;
   const int nc = (a.N + kC - 1) / kC, sms = sm_count();
   const double pairs = (double)a.B * a.H;
   auto rounds = [&](double ctas) { return (double)(long long)(ctas / sms + 0.999999); };

@@ -648,7 +648,7 @@ __global__ void __launch_bounds__(256) before_kernel(const TcParams p) {
   const int first = p.reverse ? sg.L - 1 - (sg.nc - p.seg) * kC : p.seg * kC;  // as tokens_before
   const DecayFactor w0 = decay_factor(ld * first), w1 = decay_factor(ld * (p.seg * kC));
   float *part = p.part + bh * p.ranks * D * D + at;
-  if (ns > 1) grid_dep_wait();  // (one segment: no other kernel writes to its place)
+  grid_dep_wait();  // also with one segment: a grid never ends before the kernels ahead of it
   for (int r0 = 0; r0 < ns; r0 += kBatch) {
     float4 own[kBatch];
 #pragma unroll

@@ -1,0 +1,42 @@
+"""GPU tests of the decoder operators at the edges of their contract: launches behind one
+another, infinite states, very weak decays, tiny eps, streams and autograd.  References
+and bounds are those of decoder_ref.py and test_decoder_gpu.py where nothing else is said."""
+import pytest
+import torch
+
+import decoder_ref as R
+from paper_2606_07317_gb300 import gbla
+from test_decoder_gpu import Case, _close, c32, dev
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.mark.parametrize("D", [64, 128])
+def test_short_sequences_in_a_wide_batch(D):
+    """Rows for 2600 tokens (several segments) that hold at most 60: every sequence lies in
+    one segment, and the lengths are overwritten right behind the call."""
+    lens = [60, 0, 1, 33]
+    c = Case(500 + D, 4, 2600, 2, 1, D, "bf16", lens)
+    q, k, v, do = c.tok(2), c.tok(1), c.tok(1), c.tok(2)
+    ld = torch.tensor([-2.0 ** -9, -2.0 ** -6])
+    s0, ds = (c.n(4, 2, D, D, to=torch.float32) for _ in range(2))
+    args, sl = [dev(c.poison(x)) for x in (q, k, v)] + [dev(ld)], dev(c.seq_lens)
+    o, S = gbla.decay_attention(*args, seq_lens=sl, state=dev(s0), return_state=True)
+    sl.fill_(2600)
+    sl.copy_(c.seq_lens)
+    g = gbla.decay_attention_backward(*args, dev(c.poison(do)), seq_lens=sl, state=dev(s0), dstate=dev(ds),
+                                      return_dstate=True)
+    sl.fill_(2600)
+    cut = [x[:, :60] for x in (q, k, v)]
+    ref, Sr, om, Sm = R.decay(*cut, ld, lens, s0, D ** -0.5)
+    on = ~c.past()[:, :60]
+    _close(o.cpu()[:, :60][on], ref[on], om[on], 2.0 ** -8, "bf16", "o", 2.0 ** -7)
+    c.N = 60
+    _close(S, Sr, Sm, c32(c), "fp32", "state")
+    ref, mag = R.decay_backward(*cut, ld, do[:, :60], lens, s0, ds, D ** -0.5)
+    for n in ("dq", "dk", "dv"):
+        got = g[n].cpu()
+        assert (got[:, 60:] == 0).all(), n
+        _close(got[:, :60], ref[n], mag[n], 2.0 ** -8, "bf16", n, 2.0 ** -7)
+    _close(g["dstate"], ref["dstate"], mag["dstate"], c32(c), "fp32", "dstate")
+    assert gbla.device_error() == 0

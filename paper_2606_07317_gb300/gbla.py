@@ -403,6 +403,10 @@ def state_static_scratch(k, v, gate, conv_w, seq_lens=None, out=None,
 
 
 # --- causal decoder operators -------------------------------------------------
+#
+# `stream` (None: the current one) is the stream that a call's kernels run on.  Its results
+# are allocated on that stream; tensors passed in must be ready there, and their memory must
+# not go back to another stream's allocator before the call's work is done (record_stream).
 
 _CODES = {torch.float32: GBLA_FP32, torch.bfloat16: GBLA_BF16}
 
@@ -460,11 +464,19 @@ def _plain(t, name, shape, dtype, dev):
     raise ValueError(f"{name} must be on the device of q")
 
 
-def _like(t):
-    """A contiguous tensor like t."""
-    if t.is_contiguous():
+def _empty(stream, shape, dtype, device):
+    """A tensor whose memory belongs to the stream of the call."""
+    if stream is None:
+        return torch.empty(shape, dtype=dtype, device=device)
+    with torch.cuda.stream(stream):
+        return torch.empty(shape, dtype=dtype, device=device)
+
+
+def _like(t, stream):
+    """A contiguous tensor like t, as _empty."""
+    if stream is None and t.is_contiguous():
         return torch.empty_like(t)
-    return torch.empty(t.shape, dtype=t.dtype, device=t.device)
+    return _empty(stream, t.shape, t.dtype, t.device)
 
 
 def _strides(*tensors, dims=2):
@@ -505,7 +517,7 @@ def qk_norm_rotate(q, k, norm_q, norm_k, rot=None, positions=None, seq_lens=None
     rows past seq_lens are not written."""
     code, dev, ins, dims = _rotate_args(q, k, norm_q, norm_k, rot, positions, seq_lens)
     if out is None:
-        out = (_like(q), _like(k))
+        out = (_like(q, stream), _like(k, stream))
     st = (_lib or load()).gbla_qk_norm_rotate(
         *ins, _plain(out[0], "out[0]", q.shape, q.dtype, dev),
         _plain(out[1], "out[1]", k.shape, q.dtype, dev), *dims, eps,
@@ -520,7 +532,8 @@ def qk_norm_rotate_backward(q, k, norm_q, norm_k, rot, dqo, dko, positions=None,
     gradients dqo, dko of its results: dq, dk (0 past seq_lens), dnorm_q, dnorm_k."""
     code, dev, ins, dims = _rotate_args(q, k, norm_q, norm_k, rot, positions, seq_lens)
     grads = (_plain(dqo, "dqo", q.shape, q.dtype, dev), _plain(dko, "dko", k.shape, q.dtype, dev))
-    g = dict(dq=_like(q), dk=_like(k), dnorm_q=_like(norm_q), dnorm_k=_like(norm_k))
+    g = {"d" + n: _like(t, stream)
+         for n, t in (("q", q), ("k", k), ("norm_q", norm_q), ("norm_k", norm_k))}
     st = (_lib or load()).gbla_qk_norm_rotate_backward(
         *ins, *grads, *[t.data_ptr() for t in g.values()], *dims, eps,
         ROTATE_INTERLEAVED if interleaved else 0, code, _raw_stream(dev, stream))
@@ -553,9 +566,8 @@ def decay_attention(q, k, v, log_decay, seq_lens=None, state=None, scale=None, o
     code, dev, ins, dims = _decay_args(q, k, v, log_decay, seq_lens, state)
     B, N, H, Hk, D = dims
     if out is None:
-        out = _like(q)
-    fin = (torch.empty((B, H, D, D), dtype=torch.float32, device=q.device) if return_state
-           else None)
+        out = _like(q, stream)
+    fin = _empty(stream, (B, H, D, D), torch.float32, q.device) if return_state else None
     st = (_lib or load()).gbla_decay_attention(
         *ins, _plain(out, "out", q.shape, q.dtype, dev), None if fin is None else fin.data_ptr(),
         *dims, D ** -0.5 if scale is None else scale, code, algo, _raw_stream(dev, stream))
@@ -574,9 +586,9 @@ def decay_attention_backward(q, k, v, log_decay, do, seq_lens=None, state=None, 
     B, N, H, Hk, D = dims
     grads = (_plain(do, "do", q.shape, q.dtype, dev),
              _plain(dstate, "dstate", (B, H, D, D), torch.float32, dev))
-    g = {"dq": _like(q), "dk": _like(k), "dv": _like(v)}
+    g = {"dq": _like(q, stream), "dk": _like(k, stream), "dv": _like(v, stream)}
     if return_dstate:
-        g["dstate"] = torch.empty((B, H, D, D), dtype=torch.float32, device=q.device)
+        g["dstate"] = _empty(stream, (B, H, D, D), torch.float32, q.device)
     out = [t.data_ptr() for t in g.values()] + ([] if return_dstate else [None])
     st = (_lib or load()).gbla_decay_attention_backward(
         *ins, *grads, *out, *dims, D ** -0.5 if scale is None else scale, code, algo,
@@ -599,7 +611,7 @@ def decay_attention_step(q, k, v, log_decay, state, slots=None, scale=None, out=
              & _heads(v, "v", kshape, q.dtype, dev))
     n_slots = state.shape[0]
     if out is None:
-        out = _like(q)
+        out = _like(q, stream)
     st = (_lib or load()).gbla_decay_attention_step(
         q.data_ptr(), k.data_ptr(), v.data_ptr(),
         _plain(log_decay, "log_decay", (H,), torch.float32, dev),

@@ -40,3 +40,40 @@ def test_short_sequences_in_a_wide_batch(D):
         _close(got[:, :60], ref[n], mag[n], 2.0 ** -8, "bf16", n, 2.0 ** -7)
     _close(g["dstate"], ref["dstate"], mag["dstate"], c32(c), "fp32", "dstate")
     assert gbla.device_error() == 0
+
+
+@pytest.mark.parametrize("dtype,D", [("bf16", 64), ("bf16", 128), ("fp32", 64)])
+def test_calls_on_a_given_stream(dtype, D):
+    """`stream=side` while the current stream is busy writing to blocks of the results' sizes
+    that it has just given back: the results are those of the current stream."""
+    c = Case(520, 2, 700, 4, 2, D, dtype)
+    q, k, v, do, dko = (dev(c.tok(h)) for h in (4, 2, 2, 4, 2))
+    ld = torch.full((4,), -0.05, device="cuda")
+    w, rot = torch.ones((4, D), device="cuda"), gbla.rotation_table(700, D)
+    s0, ds = (dev(c.n(2, 4, D, D, to=torch.float32)) for _ in range(2))
+
+    def work(**kw):
+        state = s0.clone() if not kw else copies.pop()
+        out = [*gbla.qk_norm_rotate(q, k, w, w[:2], rot, **kw),
+               *gbla.qk_norm_rotate_backward(q, k, w, w[:2], rot, do, dko, **kw).values(),
+               *gbla.decay_attention(q, k, v, ld, state=s0, return_state=True, **kw),
+               *gbla.decay_attention_backward(q, k, v, ld, do, state=s0, dstate=ds, return_dstate=True, **kw).values(),
+               gbla.decay_attention_step(q[:, :1], k[:, :1], v[:, :1], ld, state, **kw)]
+        return out + [state]
+
+    want = [t.clone() for t in work()]
+    copies = [s0.clone() for _ in range(3)]
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    for _ in range(3):
+        held = [torch.empty_like(t) for t in want]
+        big = torch.randn((4096, 4096), device="cuda")
+        for _ in range(8):
+            big = big @ big * 1e-3
+        for t in held:
+            t.fill_(float("nan"))
+        del held, t
+        got = work(stream=side)
+        side.synchronize()
+        torch.cuda.current_stream().synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(got, want))

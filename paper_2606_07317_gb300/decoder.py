@@ -103,6 +103,11 @@ class DecoderLayer:
         """y [B, N, d] of the prompts x [B, N, d] bf16 (rows past seq_lens are undefined) and
         the cache that `step` continues from."""
         B, N, _ = x.shape
+        if N == 0:  # nothing to project or index: the cache that the first step starts from
+            zeros = lambda *s, to: torch.zeros(s, dtype=to, device=x.device)  # noqa: E731
+            return x.clone(), {"state": zeros(B, self.H, self.D, self.D, to=torch.float32),
+                               "window": zeros(B, HISTORY, self.d, to=x.dtype),
+                               "positions": zeros(B, 1, to=torch.int32)}
         p = gbla.project(x, self.conv_x, self.w_proj, self.H, self.D, seq_lens)
         q, k = gbla.qk_norm_rotate(p["q"], p["k"], self.norm_q, self.norm_k, self.rot,
                                    seq_lens=seq_lens)

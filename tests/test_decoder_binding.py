@@ -5,7 +5,7 @@ import contextlib
 import pytest
 import torch
 
-from paper_2606_07317_gb300 import gbla
+from paper_2606_07317_gb300 import decoder, gbla
 
 
 class Library:
@@ -86,3 +86,39 @@ def test_results_belong_to_the_stream_of_the_call(lib, monkeypatch, op, packed):
         where = dict(made)
         assert [where[t.data_ptr()] for t in got] == [stream] * len(got)
         assert len(current) == 1
+
+
+# ------------------------------------------------------------- the decoder layer
+
+def _fakes(monkeypatch):
+    """The library's operators as stand-ins of the right shapes on the CPU."""
+    def project(x, conv_x, w_proj, H, D, seq_lens=None, out=None, stream=None):
+        B, N, _ = x.shape
+        return {n: x.new_zeros((B, N, H, D)) for n in ("q", "k", "v", "out_gate")} | {"gate": x.new_zeros((B, N, H))}
+
+    def attention(q, k, v, log_decay, seq_lens=None, state=None, return_state=False, **kw):
+        S = torch.zeros((q.shape[0], q.shape[2], q.shape[3], q.shape[3]))
+        return (torch.zeros_like(q), S) if return_state else torch.zeros_like(q)
+
+    monkeypatch.setattr(gbla, "project", project)
+    monkeypatch.setattr(gbla, "qk_norm_rotate", lambda q, k, *a, **kw: (q, k))
+    monkeypatch.setattr(gbla, "decay_attention", attention)
+    monkeypatch.setattr(gbla, "decay_attention_step", lambda q, *a, **kw: torch.zeros_like(q))
+
+
+@pytest.mark.parametrize("lens", [None, [0, 0, 0], [2, 0, 1]])
+@pytest.mark.parametrize("N", [0, 1, 2, 3, 7])
+def test_prompts_shorter_than_the_history(monkeypatch, N, lens):
+    """The cache's window holds the last three inputs, zeros before the first; a prompt may
+    be empty (on a GPU an index out of range would fault)."""
+    _fakes(monkeypatch)
+    layer = decoder.DecoderLayer(128, 2, 64, 16, device="cpu")
+    x = torch.randn((3, N, 128)).to(torch.bfloat16)
+    L = [N] * 3 if lens is None else [min(n, N) for n in lens]
+    y, cache = layer.prompt(x, None if lens is None else torch.tensor(lens, dtype=torch.int32))
+    assert y.shape == x.shape and cache["positions"].flatten().tolist() == L
+    for b in range(3):
+        past = torch.cat([torch.zeros((3, 128), dtype=x.dtype), x[b, :L[b]]])
+        assert torch.equal(cache["window"][b], past[-3:])
+    layer.step(x.new_ones((3, 1, 128)), cache)
+    assert (cache["window"][:, -1] == 1).all() and cache["positions"].flatten().tolist() == [n + 1 for n in L]

@@ -5,7 +5,7 @@ import pytest
 import torch
 
 import decoder_ref as R
-from paper_2606_07317_gb300 import gbla
+from paper_2606_07317_gb300 import decoder, gbla
 from test_decoder_gpu import Case, _close, c32, dev
 
 pytestmark = pytest.mark.gpu
@@ -77,3 +77,15 @@ def test_calls_on_a_given_stream(dtype, D):
         side.synchronize()
         torch.cuda.current_stream().synchronize()
         assert all(torch.equal(a, b) for a, b in zip(got, want))
+
+
+def test_steps_after_an_empty_prompt():
+    """A sequence that starts with its first step follows the parallel form (2^-7 of the
+    layer's own output, as the layer's own test)."""
+    layer = decoder.DecoderLayer(128, 2, 64, 16, seed=3)
+    x = torch.randn((3, 5, 128), generator=torch.Generator().manual_seed(4)).to(torch.bfloat16).cuda()
+    y, cache = layer.prompt(x[:, :0].contiguous())
+    assert y.shape == (3, 0, 128)
+    got = torch.cat([layer.step(x[:, i:i + 1], cache) for i in range(5)], 1).float()
+    want = layer.prompt(x)[0].float()
+    assert (got - want).norm() <= 2.0 ** -7 * (want - x.float()).norm()

@@ -11,7 +11,7 @@ output projection with a residual (a plain matrix product).
 * `DecoderLayer.step` takes one further input of every sequence and updates the
   cache in place: three kernels and the output product.
 * `norm_rotate` and `attention` are the two operators as differentiable torch
-  functions, for training.
+  functions, for training (first derivatives; deriving their gradients is an error).
 
 `python -m paper_2606_07317_gb300.decoder` reads a prompt, continues it token by
 token and compares the continuation with one parallel call over all tokens.
@@ -27,6 +27,21 @@ from . import gbla
 HISTORY = gbla.CONV_WIDTH - 1  # inputs before the current one that the Conv1D sees
 
 
+class _Gradients(torch.autograd.Function):
+    """What `compute` makes of the tensors: gradients, whose own derivative is an error.  (As
+    plain results of a backward they would pass for constants under create_graph, and
+    once_differentiable only sees whether the incoming gradients have a graph.)"""
+
+    @staticmethod
+    def forward(ctx, compute, *tensors):
+        return compute(*tensors)
+
+    @staticmethod
+    def backward(ctx, *unused):
+        raise RuntimeError("the decoder operators can be differentiated once: their gradients "
+                           "have no derivative")
+
+
 class _NormRotate(torch.autograd.Function):
     @staticmethod
     def forward(ctx, q, k, norm_q, norm_k, rot, positions, seq_lens):
@@ -37,10 +52,14 @@ class _NormRotate(torch.autograd.Function):
 
     @staticmethod
     def backward(ctx, dqo, dko):
-        q, k, norm_q, norm_k, rot, positions, seq_lens = ctx.saved_tensors
-        g = gbla.qk_norm_rotate_backward(q, k, norm_q, norm_k, rot, dqo.contiguous(),
-                                         dko.contiguous(), positions, seq_lens)
-        return g["dq"], g["dk"], g["dnorm_q"], g["dnorm_k"], None, None, None
+        *tensors, rot, positions, seq_lens = ctx.saved_tensors
+
+        def compute(q, k, norm_q, norm_k, dqo, dko):
+            g = gbla.qk_norm_rotate_backward(q, k, norm_q, norm_k, rot, dqo.contiguous(),
+                                             dko.contiguous(), positions, seq_lens)
+            return g["dq"], g["dk"], g["dnorm_q"], g["dnorm_k"]
+
+        return *_Gradients.apply(compute, *tensors, dqo, dko), None, None, None
 
 
 class _Attention(torch.autograd.Function):
@@ -53,10 +72,16 @@ class _Attention(torch.autograd.Function):
 
     @staticmethod
     def backward(ctx, do, dstate):
-        q, k, v, log_decay, seq_lens, state = ctx.saved_tensors
-        g = gbla.decay_attention_backward(q, k, v, log_decay, do.contiguous(), seq_lens, state,
-                                          dstate.contiguous(), return_dstate=state is not None)
-        return g["dq"], g["dk"], g["dv"], None, None, g.get("dstate")
+        *tensors, log_decay, seq_lens, state = ctx.saved_tensors
+
+        def compute(q, k, v, state, do, dstate):
+            g = gbla.decay_attention_backward(q, k, v, log_decay, do.contiguous(), seq_lens, state,
+                                              dstate.contiguous(),
+                                              return_dstate=state is not None)
+            return g["dq"], g["dk"], g["dv"], g.get("dstate")
+
+        dq, dk, dv, first = _Gradients.apply(compute, *tensors, state, do, dstate)
+        return dq, dk, dv, None, None, first
 
 
 def norm_rotate(q, k, norm_q, norm_k, rot=None, positions=None, seq_lens=None):

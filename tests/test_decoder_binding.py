@@ -122,3 +122,30 @@ def test_prompts_shorter_than_the_history(monkeypatch, N, lens):
         assert torch.equal(cache["window"][b], past[-3:])
     layer.step(x.new_ones((3, 1, 128)), cache)
     assert (cache["window"][:, -1] == 1).all() and cache["positions"].flatten().tolist() == [n + 1 for n in L]
+
+
+# ------------------------------------------------------------- differentiable forms
+
+def _grad_inputs():
+    x = _inputs()
+    return {n: t.requires_grad_() if n in ("q", "k", "v", "wq", "wk", "state") else t for n, t in x.items()}
+
+
+def _forms(x):
+    """{name: (differentiable form's results, its inputs)}"""
+    return {
+        "norm_rotate": (lambda **kw: decoder.norm_rotate(x["q"], x["k"], x["wq"], x["wk"], x["rot"], **kw),
+                        [x["q"], x["k"], x["wq"], x["wk"]]),
+        "attention": (lambda **kw: decoder.attention(x["q"], x["k"], x["v"], x["ld"], state=x["state"], **kw),
+                      [x["q"], x["k"], x["v"], x["state"]]),
+    }
+
+
+@pytest.mark.parametrize("form", ["norm_rotate", "attention"])
+def test_second_derivatives_are_refused(lib, form):
+    """The gradients come from kernels that autograd does not see into: a derivative of them
+    is an error, not zero."""
+    call, leaves = _forms(_grad_inputs())[form]
+    first = torch.autograd.grad(sum(t.sum() for t in call()), leaves, create_graph=True)
+    with pytest.raises(RuntimeError, match="differentiated once"):
+        (first[0].square().sum() + leaves[1].square().sum()).backward()

@@ -89,3 +89,23 @@ def test_steps_after_an_empty_prompt():
     got = torch.cat([layer.step(x[:, i:i + 1], cache) for i in range(5)], 1).float()
     want = layer.prompt(x)[0].float()
     assert (got - want).norm() <= 2.0 ** -7 * (want - x.float()).norm()
+
+
+def test_second_derivatives_are_refused():
+    """A gradient penalty through the operators is an error; the same loss without it trains."""
+    c = Case(530, 2, 40, 2, 1, 64, "fp32")
+    leaf = [t.cuda().requires_grad_() for t in (c.tok(2), c.tok(1), c.tok(1))]
+    w = torch.ones((2, 64), device="cuda", requires_grad=True)
+    ld, rot = torch.full((2,), -0.1, device="cuda"), gbla.rotation_table(40, 64)
+
+    def loss():
+        a, b = decoder.norm_rotate(leaf[0], leaf[1], w, w[:1], rot)
+        return decoder.attention(a, b, leaf[2], ld)[0].sum()
+
+    want = torch.autograd.grad(loss(), leaf)
+    got = torch.autograd.grad(loss(), leaf, create_graph=True)
+    assert all(torch.equal(a, b) for a, b in zip(got, want))
+    with pytest.raises(RuntimeError, match="differentiated once"):
+        (loss() + sum(g.square().sum() for g in got)).backward()
+    loss().backward()
+    assert all(torch.equal(t.grad, b) for t, b in zip(leaf, want))

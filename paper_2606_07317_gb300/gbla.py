@@ -407,7 +407,10 @@ def state_static_scratch(k, v, gate, conv_w, seq_lens=None, out=None,
 # `stream` (None: the current one) is the stream that a call's kernels run on.  Its results
 # are allocated on that stream; tensors passed in must be ready there, and their memory must
 # not go back to another stream's allocator before the call's work is done (record_stream).
+# Tensors that a call writes to in place (`out`, the pool of states) count as changed for
+# autograd.
 
+_changed = torch.autograd.graph.increment_version
 _CODES = {torch.float32: GBLA_FP32, torch.bfloat16: GBLA_BF16}
 
 
@@ -516,13 +519,16 @@ def qk_norm_rotate(q, k, norm_q, norm_k, rot=None, positions=None, seq_lens=None
     t).  q and k may be slices of a packed projection.  Returns (qo, ko), or fills `out`;
     rows past seq_lens are not written."""
     code, dev, ins, dims = _rotate_args(q, k, norm_q, norm_k, rot, positions, seq_lens)
-    if out is None:
+    given = out is not None
+    if not given:
         out = (_like(q, stream), _like(k, stream))
     st = (_lib or load()).gbla_qk_norm_rotate(
         *ins, _plain(out[0], "out[0]", q.shape, q.dtype, dev),
         _plain(out[1], "out[1]", k.shape, q.dtype, dev), *dims, eps,
         ROTATE_INTERLEAVED if interleaved else 0, code, _raw_stream(dev, stream))
     _check(st, "gbla_qk_norm_rotate")
+    if given:
+        _changed(out)
     return out[0], out[1]
 
 
@@ -565,13 +571,16 @@ def decay_attention(q, k, v, log_decay, seq_lens=None, state=None, scale=None, o
     return_state; rows of o past seq_lens are not written."""
     code, dev, ins, dims = _decay_args(q, k, v, log_decay, seq_lens, state)
     B, N, H, Hk, D = dims
-    if out is None:
+    given = out is not None
+    if not given:
         out = _like(q, stream)
     fin = _empty(stream, (B, H, D, D), torch.float32, q.device) if return_state else None
     st = (_lib or load()).gbla_decay_attention(
         *ins, _plain(out, "out", q.shape, q.dtype, dev), None if fin is None else fin.data_ptr(),
         *dims, D ** -0.5 if scale is None else scale, code, algo, _raw_stream(dev, stream))
     _check(st, "gbla_decay_attention")
+    if given:
+        _changed((out,))
     return (out, fin) if return_state else out
 
 
@@ -610,7 +619,8 @@ def decay_attention_step(q, k, v, log_decay, state, slots=None, scale=None, out=
     whole = (_heads(q, "q", shape, q.dtype, dev) & _heads(k, "k", kshape, q.dtype, dev)
              & _heads(v, "v", kshape, q.dtype, dev))
     n_slots = state.shape[0]
-    if out is None:
+    given = out is not None
+    if not given:
         out = _like(q, stream)
     st = (_lib or load()).gbla_decay_attention_step(
         q.data_ptr(), k.data_ptr(), v.data_ptr(),
@@ -621,4 +631,5 @@ def decay_attention_step(q, k, v, log_decay, state, slots=None, scale=None, out=
         _plain(out, "out", shape, q.dtype, dev), B, H, kshape[2], D, n_slots,
         D ** -0.5 if scale is None else scale, code, _raw_stream(dev, stream))
     _check(st, "gbla_decay_attention_step")
+    _changed((state, out) if given else (state,))
     return out

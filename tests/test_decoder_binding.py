@@ -149,3 +149,36 @@ def test_second_derivatives_are_refused(lib, form):
     first = torch.autograd.grad(sum(t.sum() for t in call()), leaves, create_graph=True)
     with pytest.raises(RuntimeError, match="differentiated once"):
         (first[0].square().sum() + leaves[1].square().sum()).backward()
+
+
+@pytest.mark.parametrize("what", ["state", "out", "q out", "k out", "step out"])
+def test_writes_are_seen_by_autograd(lib, what):
+    """A tensor that a call writes through its address counts as changed in place: saved for
+    a backward before, it raises there instead of giving another state's gradient."""
+    x = _inputs()
+    one = [x[m][:, :1] for m in ("q", "k", "v")]
+    buf = {"state": x["state"], "out": torch.zeros_like(x["q"]), "q out": torch.zeros_like(x["q"]),
+           "k out": torch.zeros_like(x["k"]), "step out": torch.zeros_like(one[0])}[what]
+    factor = torch.ones(buf.shape, requires_grad=True)
+    y = (factor * buf).sum()  # saves buf
+    call = {"state": lambda: gbla.decay_attention_step(*one, x["ld"], buf),
+            "out": lambda: gbla.decay_attention(x["q"], x["k"], x["v"], x["ld"], out=buf),
+            "q out": lambda: gbla.qk_norm_rotate(x["q"], x["k"], x["wq"], x["wk"], x["rot"],
+                                                 out=(buf, torch.zeros_like(x["k"]))),
+            "k out": lambda: gbla.qk_norm_rotate(x["q"], x["k"], x["wq"], x["wk"], x["rot"],
+                                                 out=(torch.zeros_like(x["q"]), buf)),
+            "step out": lambda: gbla.decay_attention_step(*one, x["ld"], x["state"], out=buf)}[what]
+    call()
+    with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+        y.backward()
+
+
+def test_writes_to_tensors_of_inference_mode(lib):
+    """Those have no version to count: the calls take them, inside the mode and after it."""
+    x = _inputs()
+    with torch.inference_mode():
+        state, out = torch.zeros_like(x["state"]), torch.zeros_like(x["q"])[:, :1].contiguous()
+        step = lambda: gbla.decay_attention_step(*[x[m][:, :1] for m in ("q", "k", "v")], x["ld"],  # noqa: E731
+                                                 state, out=out)
+        assert step() is out
+    assert step() is out

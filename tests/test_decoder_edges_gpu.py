@@ -109,3 +109,16 @@ def test_second_derivatives_are_refused():
         (loss() + sum(g.square().sum() for g in got)).backward()
     loss().backward()
     assert all(torch.equal(t.grad, b) for t, b in zip(leaf, want))
+
+
+def test_a_state_stepped_after_it_was_saved():
+    """A first state that a training forward keeps for its backward, and single-token steps
+    then overwrite, is an error there."""
+    c = Case(540, 2, 30, 2, 2, 64, "bf16")
+    q, k, v = (dev(c.tok(2)).requires_grad_() for _ in range(3))
+    ld, S = torch.full((2,), -0.1, device="cuda"), torch.zeros((2, 2, 64, 64), device="cuda")
+    o, _ = decoder.attention(q, k, v, ld, state=S)
+    with torch.no_grad():
+        gbla.decay_attention_step(q[:, :1], k[:, :1], v[:, :1], ld, S)
+    with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+        o.sum().backward()

@@ -403,8 +403,8 @@ gbla_status gbla_state_static_scratch(const void *k, const void *v,
  * further token updates that state in place (gbla_decay_attention_step).  The
  * backward entry points make the same layer trainable.
  *
- * Heads: q has H heads, k and v have Hk heads, H a multiple of Hk; query head h
- * reads key / value head h / (H / Hk).  Results have the input's dtype.
+ * Heads: q has H heads, k and v have Hk heads, H a positive multiple of Hk (or
+ * both 0); query head h reads key / value head h / (H / Hk).  Results have the input's dtype.
  *
  * Strides: `strides` is NULL (every input contiguous) or a HOST array of element
  * strides, (batch, token) for each of the inputs that its function names, in

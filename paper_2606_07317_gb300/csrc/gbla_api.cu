@@ -814,7 +814,7 @@ gbla_status view_of(const int64_t *strides, int i, int B, int N, long long width
 }
 
 gbla_status check_heads(int H, int Hk) {
-  if (Hk < 0 || (H > 0 && (Hk == 0 || H % Hk != 0))) return GBLA_ERR_INVALID_ARG;
+  if (H == 0 ? Hk != 0 : (Hk <= 0 || H % Hk != 0)) return GBLA_ERR_INVALID_ARG;
   return GBLA_OK;
 }
 

@@ -189,3 +189,12 @@ def test_binding_refuses_before_the_call():
     for f in (rotate, decay, back, step):  # nothing else wrong: host tensors
         with pytest.raises(ValueError, match="CUDA device"):
             f()
+
+
+@pytest.mark.parametrize("op", OPS)
+def test_key_heads_without_query_heads(lib, op):
+    """No query head leaves key heads that nothing would compute or write."""
+    none = {n: None for n in OPS[op][1]}
+    assert _run(lib, op, **none, H=0, Hk=2) == INV
+    assert _run(lib, op, H=0, Hk=1) == INV
+    assert _run(lib, op, **none, H=0, Hk=0) == OK

@@ -281,7 +281,7 @@ __global__ void __launch_bounds__(kThreadsOf<D>, ScanShape<D, kState>::kBlocks)
       }
     }
     // the state after the chunk
-    const DecayFactor carry = span == kC ? chunk_factor : DecayFactor{gp[span], 0.f};
+    const DecayFactor carry = span == kC ? chunk_factor : one_factor(gp[span]);
 #pragma unroll
     for (int i = 0; i < kSr; ++i)
 #pragma unroll
@@ -309,7 +309,7 @@ __global__ void __launch_bounds__(kThreadsOf<D>, ScanShape<D, kState>::kBlocks)
   }
   if (kState || (p.fin && seg == last)) {
     // reverse: what the gradient of the first state still decays by
-    const float w = kState ? 1.f : p.fin_scale * (p.reverse && L > 0 ? decay_pow(l2, 1.f) : 1.f);
+    const float w = kState ? 1.f : scaled_pow(p.fin_scale, l2, p.reverse && L > 0 ? 1.f : 0.f);
     float *dst = (kState ? p.part + (bh * p.nseg + seg) * (size_t)D * D : p.fin + bh * D * D) + e0;
 #pragma unroll
     for (int i = 0; i < kSr; ++i)

@@ -993,13 +993,13 @@ __global__ void __launch_bounds__(Shape<D, kTerms>::kThreads, 1)
       const int span = !p.reverse ? n : (q0 + j == 0 ? n - 1 : kC);
       if (!mbar_wait(ds_full, j & 1, &ab)) decay_error(64, ab);
       tc_fence_after();
-      take_state<D, false>(S, src, span == kC ? chunk_factor : DecayFactor{decay_pow(l2, (float)span), 0.f});
+      take_state<D, false>(S, src, span == kC ? chunk_factor : one_factor(decay_pow(l2, (float)span)));
       tc_fence_before();
       __syncwarp();
       if (lane == 0) mbar_arrive(&state_ready[(j + 1) % Sh::kConv]);
     }
     if (p.fin && sg.last) {
-      const float f = p.fin_scale * (p.reverse ? decay_pow(l2, 1.f) : 1.f);
+      const float f = scaled_pow(p.fin_scale, l2, p.reverse ? 1.f : 0.f);
 #pragma unroll
       for (int i = 0; i < kNV; ++i) {
         int e;
@@ -1015,7 +1015,7 @@ __global__ void __launch_bounds__(Shape<D, kTerms>::kThreads, 1)
     float u[2];  // weights of x_r^T S in the rows r0 and r0 + 8
 #pragma unroll
     for (int k = 0; k < 2; ++k)
-      u[k] = p.scale * decay_pow(l2, (float)(p.reverse ? kC - (r0 + 8 * k) : r0 + 8 * k + 1));
+      u[k] = scaled_pow(p.scale, l2, (float)(p.reverse ? kC - (r0 + 8 * k) : r0 + 8 * k + 1));
     float s[32];  // D = 64: the inter results of the chunk at hand
     // They are read as soon as the scores are there, before the intra results, so
     // that the next but one product may take their columns.
@@ -1040,7 +1040,7 @@ __global__ void __launch_bounds__(Shape<D, kTerms>::kThreads, 1)
       if (p.reverse && q0 + j == 0) {
 #pragma unroll
         for (int k = 0; k < 2; ++k)
-          ur[k] = p.scale * decay_pow(l2, (float)max(n - 1 - (r0 + 8 * k), 0));
+          ur[k] = scaled_pow(p.scale, l2, (float)max(n - 1 - (r0 + 8 * k), 0));
       }
       if constexpr (!Sh::kMerged) {  // weight the inter results in place; intra is added to them
         if (!mbar_wait(&inter_full[ob], (j >> 1) & 1, &ab)) decay_error(256, ab);
@@ -1374,13 +1374,13 @@ __global__ void __launch_bounds__(KvShape<kTerms>::kThreads, 1)
       const int n = min(kC, L - sg.token_of(q0 + i));
       if (!mbar_wait(ds_full, i & 1, &ab)) decay_error(64, ab);
       tc_fence_after();
-      take_state<64, false>(S, src, q0 + i > 0 ? chunk_factor : DecayFactor{decay_pow(l2, (float)(n - 1)), 0.f});
+      take_state<64, false>(S, src, q0 + i > 0 ? chunk_factor : one_factor(decay_pow(l2, (float)(n - 1))));
       tc_fence_before();
       __syncwarp();
       if (lane == 0) mbar_arrive(&state_ready[(i + 1) & 1]);
     }
     if (p.fin && sg.last) {
-      const float f = p.fin_scale * decay_pow(l2, 1.f);
+      const float f = scaled_pow(p.fin_scale, l2, 1.f);
 #pragma unroll
       for (int i = 0; i < 32; ++i) {
         int e;
@@ -1395,7 +1395,7 @@ __global__ void __launch_bounds__(KvShape<kTerms>::kThreads, 1)
     const uint32_t stage = smem_u32(smem + Sh::kOffOut + ow * 2048);
     float u[2];
 #pragma unroll
-    for (int k = 0; k < 2; ++k) u[k] = p.scale * decay_pow(l2, (float)(kC - (r0 + 8 * k)));
+    for (int k = 0; k < 2; ++k) u[k] = scaled_pow(p.scale, l2, (float)(kC - (r0 + 8 * k)));
     float s[32];
     auto load_inter = [&](int job) {
       const int w = job & 1;
@@ -1418,7 +1418,7 @@ __global__ void __launch_bounds__(KvShape<kTerms>::kThreads, 1)
       if (q0 + i == 0) {
 #pragma unroll
         for (int k = 0; k < 2; ++k)
-          ur[k] = p.scale * decay_pow(l2, (float)max(n - 1 - (r0 + 8 * k), 0));
+          ur[k] = scaled_pow(p.scale, l2, (float)max(n - 1 - (r0 + 8 * k), 0));
       }
       if (!mbar_wait(&o_full[w], i & 1, &ab)) decay_error(256, ab);
       tc_fence_after();

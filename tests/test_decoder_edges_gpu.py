@@ -122,3 +122,89 @@ def test_a_state_stepped_after_it_was_saved():
         gbla.decay_attention_step(q[:, :1], k[:, :1], v[:, :1], ld, S)
     with pytest.raises(RuntimeError, match="modified by an inplace operation"):
         o.sum().backward()
+
+
+# ------------------------------------------------------------- infinite states
+# D, dtype, N, lens: whole chunks, a chunk cut short, several segments
+INF = [(32, "fp32", 70, None), (64, "fp32", 700, [700, 300]), (128, "fp32", 96, None), (32, "bf16", 129, None),
+       (64, "bf16", 70, [70, 64]), (64, "bf16", 2500, [2500, 700]), (128, "bf16", 193, None),
+       (128, "bf16", 2000, None), (64, "bf16", 10, [10, 0])]
+INF_DECAYS = [-3.0, -0.05, -1e-3, 2e-4]  # the first fades to 0 in fp32 within a chunk
+
+
+def _with_infinities(s):
+    """s with an infinity of each sign in places that share no row and no column."""
+    s = s.clone()
+    s[:, :, 3, 5], s[:, :, 7, 11] = float("inf"), float("-inf")
+    return s
+
+
+@pytest.mark.parametrize("family", ["auto", "simt"])
+@pytest.mark.parametrize("i", range(len(INF)))
+def test_infinite_states_stay_infinite(i, family):
+    """gamma S + k v^T of an infinite S is that infinity for every gamma > 0: its column of
+    the results is infinite with the sign of the query's value, everything else as without."""
+    D, dtype, N, lens = INF[i]
+    c = Case(550 + i, 2, N, 4, 2, D, dtype, lens)
+    q, k, v, do = (dev(c.tok(h)) for h in (4, 2, 2, 4))
+    ld, algo = torch.tensor(INF_DECAYS, device="cuda"), {"auto": gbla.ALGO_AUTO, "simt": gbla.ALGO_SIMT}[family]
+    s0, ds = (dev(c.n(2, 4, D, D, to=torch.float32)) for _ in range(2))
+    kw = dict(seq_lens=dev(c.seq_lens), algo=algo)
+    on = ~c.past().cuda()
+    bad = torch.isinf(_with_infinities(s0))
+    inf = float("inf")
+
+    def check(got, plain, axis_of, name):
+        """Rows or columns 5 and 11 (3 and 7) infinite by the other tensor's sign, the rest equal."""
+        for at, sign in axis_of:
+            assert torch.equal(got[..., at].float(), torch.sign(sign) * inf), (name, at)
+        rest = [e for e in range(D) if e not in [at for at, _ in axis_of]]
+        assert torch.equal(got[..., rest], plain[..., rest]), name
+
+    zero = s0.masked_fill(bad, 0.0)
+    o, S = gbla.decay_attention(q, k, v, ld, state=_with_infinities(s0), return_state=True, **kw)
+    o2, S2 = gbla.decay_attention(q, k, v, ld, state=zero, return_state=True, **kw)
+    check(o[on], o2[on], [(5, q[on][..., 3].float()), (11, -q[on][..., 7].float())], "o")
+    assert torch.equal(S[bad], _with_infinities(s0)[bad]) and torch.equal(S[~bad], S2[~bad])
+    g = gbla.decay_attention_backward(q, k, v, ld, do, state=_with_infinities(s0), **kw)
+    g2 = gbla.decay_attention_backward(q, k, v, ld, do, state=zero, **kw)
+    check(g["dq"][on], g2["dq"][on], [(3, do[on][..., 5].float()), (7, -do[on][..., 11].float())], "dq")
+    assert torch.equal(g["dk"], g2["dk"]) and torch.equal(g["dv"], g2["dv"])
+    # the gradient of the final state, with a head of keys for each of queries
+    k, v = (dev(c.tok(4)) for _ in range(2))
+    zero = ds.masked_fill(bad, 0.0)
+    g = gbla.decay_attention_backward(q, k, v, ld, do, dstate=_with_infinities(ds), return_dstate=True, **kw)
+    g2 = gbla.decay_attention_backward(q, k, v, ld, do, dstate=zero, return_dstate=True, **kw)
+    check(g["dk"][on], g2["dk"][on], [(3, v[on][..., 5].float()), (7, -v[on][..., 11].float())], "dk")
+    check(g["dv"][on], g2["dv"][on], [(5, k[on][..., 3].float()), (11, -k[on][..., 7].float())], "dv")
+    assert torch.equal(g["dstate"][bad], _with_infinities(ds)[bad]) and torch.equal(g["dstate"][~bad], g2["dstate"][~bad])
+
+
+@pytest.mark.parametrize("D,dtype", [(32, "fp32"), (64, "bf16"), (128, "bf16")])
+def test_steps_on_infinite_states(D, dtype):
+    c = Case(570, 2, 1, 4, 4, D, dtype)
+    q, k, v = (dev(c.tok(4)) for _ in range(3))
+    ld, s0 = torch.tensor(INF_DECAYS, device="cuda"), dev(c.n(2, 4, D, D, to=torch.float32))
+    S, plain = _with_infinities(s0), s0.clone()
+    bad = torch.isinf(S)
+    o, o2 = (gbla.decay_attention_step(q, k, v, ld, s) for s in (S, plain))
+    assert torch.equal(S[bad], _with_infinities(s0)[bad]) and torch.equal(S[~bad], plain[~bad])
+    for at, sign in ((5, q[..., 3]), (11, -q[..., 7])):
+        assert torch.equal(o[..., at].float(), torch.sign(sign.float()) * float("inf"))
+    rest = [e for e in range(D) if e not in (5, 11)]
+    assert torch.equal(o[..., rest], o2[..., rest])
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+def test_a_growing_state_overflows_to_infinity(dtype):
+    """A state that grows past the largest float is infinite, not NaN (keys of zero)."""
+    z = torch.zeros((1, 64, 2, 64), dtype=torch.float32 if dtype == "fp32" else torch.bfloat16, device="cuda")
+    S = torch.full((1, 2, 64, 64), 2.0 ** 120, device="cuda")
+    S[0, 1] = -S[0, 1]
+    ld = torch.full((2,), 0.25, device="cuda")  # e^16 a call
+    for _ in range(3):
+        S = gbla.decay_attention(z, z, z, ld, state=S, return_state=True)[1]
+    assert (S[0, 0] == float("inf")).all() and (S[0, 1] == float("-inf")).all()
+    for _ in range(2):
+        gbla.decay_attention_step(z[:, :1], z[:, :1], z[:, :1], ld, S)
+    assert (S[0, 0] == float("inf")).all() and (S[0, 1] == float("-inf")).all()

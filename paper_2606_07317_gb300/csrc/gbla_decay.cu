@@ -332,7 +332,12 @@ __global__ void __launch_bounds__(128) prefix_kernel(const ScanBatch batch, int 
   const int ns = (L + p.seg - 1) / p.seg;
   if (i >= D * D || ns == 0) return;
   const size_t bh = (size_t)b * p.H + h;
-  const float l2 = log2_decay(p.log_decay, h);
+  // decay over the tokens of a segment, and of the first one in scan order (reverse: the
+  // first state belongs to the last token)
+  const DecayFactor whole = decay_factor(__ldg(p.log_decay + h) * p.seg);
+  const DecayFactor first =
+      p.reverse ? one_factor(decay_pow(log2_decay(p.log_decay, h), (float)(L - 1 - (ns - 1) * p.seg)))
+                : whole;
   float S[4] = {};
   if (p.init) {
     const float *s0 = p.init + bh * D * D;
@@ -355,11 +360,11 @@ __global__ void __launch_bounds__(128) prefix_kernel(const ScanBatch batch, int 
       const int k = k0 + u, s = p.reverse ? ns - 1 - k : k;
       if (k >= ns) break;
       store4(part + (size_t)s * D * D, S);
-      // tokens that the state before the segment decays by (reverse: the first
-      // state belongs to the last token)
-      const float w = decay_pow(l2, (float)(p.reverse && k == 0 ? L - 1 - s * p.seg : p.seg));
-      S[0] = fmaf(w, S[0], own[u].x), S[1] = fmaf(w, S[1], own[u].y);
-      S[2] = fmaf(w, S[2], own[u].z), S[3] = fmaf(w, S[3], own[u].w);
+      const DecayFactor w = k == 0 ? first : whole;
+      S[0] = fmaf(w.hi, S[0], fmaf(w.lo, S[0], own[u].x));
+      S[1] = fmaf(w.hi, S[1], fmaf(w.lo, S[1], own[u].y));
+      S[2] = fmaf(w.hi, S[2], fmaf(w.lo, S[2], own[u].z));
+      S[3] = fmaf(w.hi, S[3], fmaf(w.lo, S[3], own[u].w));
     }
   }
 }

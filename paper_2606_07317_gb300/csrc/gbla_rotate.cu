@@ -77,10 +77,11 @@ __device__ __forceinline__ void load_s8(uint32_t at, float2 (&f)[4]) {
   f[3] = make_float2(__uint_as_float(b.z), __uint_as_float(b.w));
 }
 __device__ __forceinline__ float2 both(float v) { return make_float2(v, v); }
-// 1 / sqrt(v) within 2^-22 (v a mean of squares plus eps)
+// 1 / sqrt(v) within 2^-22 (v a mean of squares plus eps, which may be subnormal: a zero
+// head times an infinity would be NaN)
 __device__ __forceinline__ float rsqrt_approx(float v) {
   float r;
-  asm("rsqrt.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(v));
+  asm("rsqrt.approx.f32 %0, %1;" : "=f"(r) : "f"(v));
   return r;
 }
 

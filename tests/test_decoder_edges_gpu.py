@@ -227,3 +227,26 @@ def test_states_through_many_segments_do_not_drift(D, dtype, family):
     want = s0.double() * (N * ld.double()).exp()[None, :, None, None]
     off = [((t[0, h].cpu().double() - want[0, h]).norm() / want[0, h].norm()).item() for t in (S, g) for h in range(H)]
     assert max(off) <= 2 * 192 ** 0.5 * 2.0 ** -24, off
+
+
+# ------------------------------------------------------------- norm and rotation
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("eps", [1e-45, 1e-40, 1.17e-38, 1.2e-38, 1e-30])
+def test_zero_heads_at_the_smallest_eps(eps, dtype):
+    """Every positive eps that fp32 holds keeps zero heads at zero, and their gradients at
+    g w / sqrt(eps); other heads are as with any eps below their mean square."""
+    c = Case(580, 1, 6, 2, 2, 64, dtype)
+    q, dqo, w = c.tok(2), c.tok(2), 1 + 0.3 * c.n(2, 64, to=torch.float32)
+    q[0, [0, 3]] = 0
+    dqo[0, [0, 3]] *= 2.0 ** -10  # (times 1 / sqrt(eps) within fp32)
+    rot = gbla.rotation_table(6, 64, device="cpu")
+    eps = torch.tensor(eps, dtype=torch.float32).item()
+    o = gbla.qk_norm_rotate(dev(q), dev(q), dev(w), dev(w), dev(rot), eps=eps)[0]
+    assert (o[0, [0, 3]] == 0).all()
+    ref, mag = R.norm_rotate(q, w, rot, None, 64, False, eps)
+    _close(o, ref, mag, 80 * 2.0 ** -24, dtype, "q")
+    g = gbla.qk_norm_rotate_backward(dev(q), dev(q), dev(w), dev(w), dev(rot), dev(dqo), dev(dqo), eps=eps)
+    dx, dxm, dw, dwm = R.norm_rotate_backward(q, w, rot, None, 64, False, eps, dqo, [6])
+    _close(g["dq"], dx, dxm, 80 * 2.0 ** -23, dtype, "dq")
+    _close(g["dnorm_q"], dw, dwm, 80 * 2.0 ** -23 + 6 * 2.0 ** -24, "fp32", "dnorm_q")

@@ -341,13 +341,13 @@ __global__ void __launch_bounds__(kThreads, kBlocks) rotate_bwd_kernel(const Rot
           dot = __ffma2_rn(gx[i], ln.w[u][i], dot);
         }
         const float r = rsqrt_approx(fmaf(head_sum<kLanes>(sq.x + sq.y), 1.f / D, p.eps));
-        // dx = r u - x r^3 mean(u x)
-        const float m = head_sum<kLanes>(dot.x + dot.y) * (-1.f / D) * r * r * r;
+        // dx = r (u - x r^2 mean(u x)); r^3 would overflow first
+        const float m = head_sum<kLanes>(dot.x + dot.y) * (-1.f / D) * r * r;
         float2 dx[4];
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
           if (ln.on[u]) dw[u][i] = __ffma2_rn(gx[i], both(r), dw[u][i]);
-          dx[i] = __ffma2_rn(x[i], both(m), __fmul2_rn(__fmul2_rn(g[i], ln.w[u][i]), both(r)));
+          dx[i] = __fmul2_rn(__ffma2_rn(x[i], both(m), __fmul2_rn(g[i], ln.w[u][i])), both(r));
         }
         if (ln.on[u]) Pack8<T>::store((ln.is_q[u] ? dq : dk) + ln.off[u], dx);
       }

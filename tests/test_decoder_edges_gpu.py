@@ -250,3 +250,16 @@ def test_zero_heads_at_the_smallest_eps(eps, dtype):
     dx, dxm, dw, dwm = R.norm_rotate_backward(q, w, rot, None, 64, False, eps, dqo, [6])
     _close(g["dq"], dx, dxm, 80 * 2.0 ** -23, dtype, "dq")
     _close(g["dnorm_q"], dw, dwm, 80 * 2.0 ** -23 + 6 * 2.0 ** -24, "fp32", "dnorm_q")
+
+
+def test_heads_as_small_as_the_root_of_eps():
+    """Heads about sqrt(eps) for a tiny eps: no product with three reciprocal roots overflows
+    where the gradient (1e23) does not."""
+    eps = torch.tensor(2e-37, dtype=torch.float32).item()
+    c = Case(581, 1, 5, 2, 2, 64, "fp32")
+    q, dqo, w = c.tok(2) * 3e-19, c.tok(2) * 2.0 ** 16, 1 + 0.3 * c.n(2, 64, to=torch.float32)
+    rot = gbla.rotation_table(5, 64, device="cpu")
+    g = gbla.qk_norm_rotate_backward(dev(q), dev(q), dev(w), dev(w), dev(rot), dev(dqo), dev(dqo), eps=eps)
+    dx, dxm, dw, dwm = R.norm_rotate_backward(q, w, rot, None, 64, False, eps, dqo, [5])
+    _close(g["dq"], dx, dxm, 80 * 2.0 ** -23, "fp32", "dq")
+    _close(g["dnorm_q"], dw, dwm, 80 * 2.0 ** -23 + 5 * 2.0 ** -24, "fp32", "dnorm_q")

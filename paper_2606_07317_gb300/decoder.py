@@ -84,14 +84,22 @@ class _Attention(torch.autograd.Function):
         return dq, dk, dv, None, None, first
 
 
+def _constant(t, name):
+    if t is not None and t.requires_grad and torch.is_grad_enabled():
+        raise ValueError(f"{name} has no gradient: it is a constant of the model (detach it)")
+
+
 def norm_rotate(q, k, norm_q, norm_k, rot=None, positions=None, seq_lens=None):
     """gbla.qk_norm_rotate with gradients for q, k and the weights; padding rows are 0."""
+    _constant(rot, "rot")
     return _NormRotate.apply(q, k, norm_q, norm_k, rot, positions, seq_lens)
 
 
 def attention(q, k, v, log_decay, seq_lens=None, state=None):
     """gbla.decay_attention with gradients for q, k, v and the first state; returns (o, the
-    state after each sequence), padding rows of o are 0.  The decays are constants."""
+    state after each sequence), padding rows of o are 0.  The decays are constants (refused where they ask for a
+    gradient)."""
+    _constant(log_decay, "log_decay")
     return _Attention.apply(q, k, v, log_decay, seq_lens, state)
 
 

@@ -182,3 +182,18 @@ def test_writes_to_tensors_of_inference_mode(lib):
                                                  state, out=out)
         assert step() is out
     assert step() is out
+
+
+def test_constants_that_ask_for_a_gradient_are_refused(lib):
+    """Decays and the rotation's table have no gradient: asking for one is an error, not None."""
+    x = _grad_inputs()
+    x["ld"].requires_grad_()
+    x["rot"].requires_grad_()
+    with pytest.raises(ValueError, match="log_decay has no gradient"):
+        decoder.attention(x["q"], x["k"], x["v"], x["ld"])
+    with pytest.raises(ValueError, match="rot has no gradient"):
+        decoder.norm_rotate(x["q"], x["k"], x["wq"], x["wk"], x["rot"])
+    with torch.no_grad():
+        decoder.attention(x["q"], x["k"], x["v"], x["ld"])
+        decoder.norm_rotate(x["q"], x["k"], x["wq"], x["wk"], x["rot"])
+    decoder.attention(x["q"], x["k"], x["v"], x["ld"].detach())

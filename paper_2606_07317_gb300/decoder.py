@@ -44,44 +44,49 @@ class _Gradients(torch.autograd.Function):
 
 class _NormRotate(torch.autograd.Function):
     @staticmethod
-    def forward(ctx, q, k, norm_q, norm_k, rot, positions, seq_lens):
+    def forward(ctx, options, q, k, norm_q, norm_k, rot, positions, seq_lens):
+        ctx.options = options
         ctx.save_for_backward(q, k, norm_q, norm_k, rot, positions, seq_lens)
         out = (torch.zeros(q.shape, dtype=q.dtype, device=q.device),
                torch.zeros(k.shape, dtype=k.dtype, device=k.device))
-        return gbla.qk_norm_rotate(q, k, norm_q, norm_k, rot, positions, seq_lens, out=out)
+        return gbla.qk_norm_rotate(q, k, norm_q, norm_k, rot, positions, seq_lens, out=out,
+                                   **options)
 
     @staticmethod
     def backward(ctx, dqo, dko):
         *tensors, rot, positions, seq_lens = ctx.saved_tensors
+        options = ctx.options
 
         def compute(q, k, norm_q, norm_k, dqo, dko):
             g = gbla.qk_norm_rotate_backward(q, k, norm_q, norm_k, rot, dqo.contiguous(),
-                                             dko.contiguous(), positions, seq_lens)
+                                             dko.contiguous(), positions, seq_lens, **options)
             return g["dq"], g["dk"], g["dnorm_q"], g["dnorm_k"]
 
-        return *_Gradients.apply(compute, *tensors, dqo, dko), None, None, None
+        return None, *_Gradients.apply(compute, *tensors, dqo, dko), None, None, None
 
 
 class _Attention(torch.autograd.Function):
     @staticmethod
-    def forward(ctx, q, k, v, log_decay, seq_lens, state):
+    def forward(ctx, options, q, k, v, log_decay, seq_lens, state):
+        ctx.options = options
         ctx.save_for_backward(q, k, v, log_decay, seq_lens, state)
         out = torch.zeros(q.shape, dtype=q.dtype, device=q.device)
         return gbla.decay_attention(q, k, v, log_decay, seq_lens, state, out=out,
-                                    return_state=True)
+                                    return_state=True, **options)
 
     @staticmethod
     def backward(ctx, do, dstate):
         *tensors, log_decay, seq_lens, state = ctx.saved_tensors
+        options = ctx.options
 
         def compute(q, k, v, state, do, dstate):
             g = gbla.decay_attention_backward(q, k, v, log_decay, do.contiguous(), seq_lens, state,
                                               dstate.contiguous(),
-                                              return_dstate=state is not None)
+                                              return_dstate=state is not None, **options)
             return g["dq"], g["dk"], g["dv"], g.get("dstate")
 
         dq, dk, dv, first = _Gradients.apply(compute, *tensors, state, do, dstate)
-        return dq, dk, dv, None, None, first
+        return None, dq, dk, dv, None, None, first
 
 
 def _constant(t, name):
@@ -89,18 +94,23 @@ def _constant(t, name):
         raise ValueError(f"{name} has no gradient: it is a constant of the model (detach it)")
 
 
-def norm_rotate(q, k, norm_q, norm_k, rot=None, positions=None, seq_lens=None):
-    """gbla.qk_norm_rotate with gradients for q, k and the weights; padding rows are 0."""
+def norm_rotate(q, k, norm_q, norm_k, rot=None, positions=None, seq_lens=None,
+                eps: float = 1e-6, interleaved: bool = False):
+    """gbla.qk_norm_rotate with gradients for q, k and the weights; padding rows are 0.  The
+    table is a constant (refused where it asks for a gradient)."""
     _constant(rot, "rot")
-    return _NormRotate.apply(q, k, norm_q, norm_k, rot, positions, seq_lens)
+    return _NormRotate.apply(dict(eps=eps, interleaved=interleaved), q, k, norm_q, norm_k, rot,
+                             positions, seq_lens)
 
 
-def attention(q, k, v, log_decay, seq_lens=None, state=None):
+def attention(q, k, v, log_decay, seq_lens=None, state=None, scale=None,
+              algo: int = gbla.ALGO_AUTO):
     """gbla.decay_attention with gradients for q, k, v and the first state; returns (o, the
-    state after each sequence), padding rows of o are 0.  The decays are constants (refused where they ask for a
-    gradient)."""
+    state after each sequence), padding rows of o are 0.  The decays are constants (refused
+    where they ask for a gradient).  `algo` is the kernel family of both directions: in bf16
+    gbla.ALGO_SIMT keeps the scores and the state as queries meet it in 32 bits."""
     _constant(log_decay, "log_decay")
-    return _Attention.apply(q, k, v, log_decay, seq_lens, state)
+    return _Attention.apply(dict(scale=scale, algo=algo), q, k, v, log_decay, seq_lens, state)
 
 
 def head_decays(H: int, shortest: float = 32.0, longest: float = 4096.0, device="cuda"):
@@ -112,15 +122,17 @@ def head_decays(H: int, shortest: float = 32.0, longest: float = 4096.0, device=
 
 
 class DecoderLayer:
-    """Random weights of a layer of width d with H heads of D (bf16; limits as gbla_project)."""
+    """Random weights of a layer of width d with H heads of D (bf16; limits as gbla_project).
+    `algo`: the kernel family of the prompts' attention."""
 
-    def __init__(self, d: int, H: int, D: int, max_positions: int, seed: int = 0, device="cuda"):
+    def __init__(self, d: int, H: int, D: int, max_positions: int, seed: int = 0, device="cuda",
+                 algo: int = gbla.ALGO_AUTO):
         g = torch.Generator(device=device).manual_seed(seed)
 
         def normal(*shape, std):
             return torch.randn(shape, generator=g, device=device) * std
 
-        self.d, self.H, self.D = d, H, D
+        self.d, self.H, self.D, self.algo = d, H, D, algo
         self.conv_x = normal(d, gbla.CONV_WIDTH, std=0.5)
         self.w_proj = normal(4 * H * D + H, d, std=d ** -0.5).to(torch.bfloat16)
         self.norm_q, self.norm_k = (1 + normal(H, D, std=0.02) for _ in range(2))
@@ -144,7 +156,8 @@ class DecoderLayer:
         p = gbla.project(x, self.conv_x, self.w_proj, self.H, self.D, seq_lens)
         q, k = gbla.qk_norm_rotate(p["q"], p["k"], self.norm_q, self.norm_k, self.rot,
                                    seq_lens=seq_lens)
-        o, state = gbla.decay_attention(q, k, p["v"], self.log_decay, seq_lens, return_state=True)
+        o, state = gbla.decay_attention(q, k, p["v"], self.log_decay, seq_lens, return_state=True,
+                                        algo=self.algo)
         L = (torch.full((B,), N, dtype=torch.int32, device=x.device) if seq_lens is None
              else seq_lens.clamp(0, N))
         at = L[:, None].long() + torch.arange(-HISTORY, 0, device=x.device)  # the last inputs

@@ -197,3 +197,42 @@ def test_constants_that_ask_for_a_gradient_are_refused(lib):
         decoder.attention(x["q"], x["k"], x["v"], x["ld"])
         decoder.norm_rotate(x["q"], x["k"], x["wq"], x["wk"], x["rot"])
     decoder.attention(x["q"], x["k"], x["v"], x["ld"].detach())
+
+
+def test_options_reach_both_directions(lib):
+    """eps and the pairs' layout, scale and the kernel family: the forward's and the backward's
+    call get what the caller gave, or the operators' defaults."""
+    x = _grad_inputs()
+    sizes = (2, 5, 4, 2, 64)
+
+    def tails(call):
+        lib.calls.clear()
+        sum(t.sum() for t in call()).backward()
+        assert len(lib.calls) == 2
+        return [args[-4:-2] for _, args in lib.calls]  # (then the dtype and the stream)
+
+    rotate = lambda **kw: lambda: decoder.norm_rotate(x["q"], x["k"], x["wq"], x["wk"], x["rot"], **kw)  # noqa: E731
+    assert tails(rotate()) == [(1e-6, 0)] * 2
+    assert tails(rotate(eps=1e-3, interleaved=True)) == [(1e-3, gbla.ROTATE_INTERLEAVED)] * 2
+    attend = lambda **kw: lambda: decoder.attention(x["q"], x["k"], x["v"], x["ld"], state=x["state"], **kw)  # noqa: E731
+    one = lambda calls: [(args[-4], args[-2]) for _, args in calls]  # noqa: E731
+    for kw, want in ((dict(), (64 ** -0.5, gbla.ALGO_AUTO)), (dict(scale=0.3, algo=gbla.ALGO_SIMT), (0.3, gbla.ALGO_SIMT))):
+        lib.calls.clear()
+        sum(t.sum() for t in attend(**kw)()).backward()
+        assert one(lib.calls) == [want] * 2
+        assert all(args[-9:-4] == sizes for _, args in lib.calls)
+
+
+def test_the_layer_takes_a_kernel_family(monkeypatch):
+    _fakes(monkeypatch)
+    seen, attend = [], gbla.decay_attention
+
+    def watch(*a, algo=gbla.ALGO_AUTO, **kw):
+        seen.append(algo)
+        return attend(*a, **kw)
+
+    monkeypatch.setattr(gbla, "decay_attention", watch)
+    x = torch.randn((1, 4, 128)).to(torch.bfloat16)
+    for kw, want in ((dict(), gbla.ALGO_AUTO), (dict(algo=gbla.ALGO_SIMT), gbla.ALGO_SIMT)):
+        decoder.DecoderLayer(128, 2, 64, 16, device="cpu", **kw).prompt(x)
+        assert seen.pop() == want

@@ -263,3 +263,27 @@ def test_heads_as_small_as_the_root_of_eps():
     dx, dxm, dw, dwm = R.norm_rotate_backward(q, w, rot, None, 64, False, eps, dqo, [5])
     _close(g["dq"], dx, dxm, 80 * 2.0 ** -23, "fp32", "dq")
     _close(g["dnorm_q"], dw, dwm, 80 * 2.0 ** -23 + 5 * 2.0 ** -24, "fp32", "dnorm_q")
+
+
+# ------------------------------------------------------------- differentiable forms
+
+@pytest.mark.parametrize("dtype,D,algo", [("bf16", 64, gbla.ALGO_AUTO), ("bf16", 128, gbla.ALGO_AUTO),
+                                          ("bf16", 64, gbla.ALGO_SIMT), ("fp32", 32, gbla.ALGO_AUTO)])
+def test_differentiable_forms_give_the_operators_gradients(dtype, D, algo):
+    """Options, packed inputs, an incoming gradient that is not contiguous and a final state
+    that nothing uses: bit for bit the operators' own gradients."""
+    c = Case(590, 2, 90, 4, 4, D, dtype, [90, 41])
+    packed = dev(c.n(2, 90, 3, 4, D)).requires_grad_()
+    q, k, v = packed.unbind(2)
+    w = (1 + 0.1 * dev(c.n(4, D, to=torch.float32))).requires_grad_()
+    ld, rot, sl = torch.full((4,), -0.05, device="cuda"), gbla.rotation_table(90, D), dev(c.seq_lens)
+    do = dev(c.n(90, 2, 4, D)).transpose(0, 1)
+    opt, att = dict(eps=1e-3, interleaved=True), dict(scale=0.3, algo=algo)
+    a, b = decoder.norm_rotate(q, k, w, w, rot, None, sl, **opt)
+    o, _ = decoder.attention(a, b, v, ld, sl, **att)
+    dp, dw = torch.autograd.grad(o, [packed, w], do)
+    with torch.no_grad():
+        g = gbla.decay_attention_backward(a, b, v, ld, do.contiguous(), sl, **att)
+        r = gbla.qk_norm_rotate_backward(q, k, w, w, rot, g["dq"], g["dk"], None, sl, **opt)
+    assert torch.equal(dp, torch.stack([r["dq"], r["dk"], g["dv"]], 2))
+    assert torch.equal(dw, r["dnorm_q"] + r["dnorm_k"])

@@ -7,7 +7,7 @@ output projection with a residual (a plain matrix product).
 
 * `DecoderLayer.prompt` reads whole, possibly ragged prompts in parallel and
   leaves a cache: the attention state of every head, the last three inputs (the
-  Conv1D's history) and the lengths.
+  Conv1D's history), the lengths and, on the host, the tokens it knows of.
 * `DecoderLayer.step` takes one further input of every sequence and updates the
   cache in place: three kernels and the output product.
 * `norm_rotate` and `attention` are the two operators as differentiable torch
@@ -144,15 +144,23 @@ class DecoderLayer:
         y = o * torch.nn.functional.silu(out_gate)
         return x + y.flatten(2) @ self.w_out
 
+    def _within(self, tokens):
+        """Refuses sequences that the host knows to be longer than the table."""
+        if tokens > self.rot.shape[0]:
+            raise ValueError(f"the layer's table has {self.rot.shape[0]} positions, not {tokens}")
+
     def prompt(self, x, seq_lens=None):
         """y [B, N, d] of the prompts x [B, N, d] bf16 (rows past seq_lens are undefined) and
-        the cache that `step` continues from."""
+        the cache that `step` continues from.  Lengths in seq_lens must lie within
+        max_positions (positions past the table would take its last row)."""
         B, N, _ = x.shape
+        tokens = N if seq_lens is None else 0  # of the longest sequence, at least
+        self._within(tokens)
         if N == 0:  # nothing to project or index: the cache that the first step starts from
             zeros = lambda *s, to: torch.zeros(s, dtype=to, device=x.device)  # noqa: E731
             return x.clone(), {"state": zeros(B, self.H, self.D, self.D, to=torch.float32),
                                "window": zeros(B, HISTORY, self.d, to=x.dtype),
-                               "positions": zeros(B, 1, to=torch.int32)}
+                               "positions": zeros(B, 1, to=torch.int32), "tokens": torch.tensor(0)}
         p = gbla.project(x, self.conv_x, self.w_proj, self.H, self.D, seq_lens)
         q, k = gbla.qk_norm_rotate(p["q"], p["k"], self.norm_q, self.norm_k, self.rot,
                                    seq_lens=seq_lens)
@@ -163,11 +171,13 @@ class DecoderLayer:
         at = L[:, None].long() + torch.arange(-HISTORY, 0, device=x.device)  # the last inputs
         window = torch.gather(x, 1, at.clamp(min=0)[:, :, None].expand(-1, -1, self.d))
         window = torch.where(at[:, :, None] >= 0, window, torch.zeros_like(window))
-        cache = {"state": state, "window": window, "positions": L[:, None].contiguous()}
+        cache = {"state": state, "window": window, "positions": L[:, None].contiguous(),
+                 "tokens": torch.tensor(tokens)}
         return self._out(x, o, p["out_gate"]), cache
 
     def step(self, x, cache):
         """y [B, 1, d] of the next input x [B, 1, d] of every sequence; updates the cache."""
+        self._within(int(cache["tokens"]) + 1)
         wide = torch.cat([cache["window"], x], 1)
         p = gbla.project(wide, self.conv_x, self.w_proj, self.H, self.D)
         now = slice(HISTORY, HISTORY + 1)  # the one output whose history is whole
@@ -176,6 +186,7 @@ class DecoderLayer:
         o = gbla.decay_attention_step(q, k, p["v"][:, now], self.log_decay, cache["state"])
         cache["window"].copy_(wide[:, 1:])
         cache["positions"].add_(1)
+        cache["tokens"] += 1
         return self._out(x, o, p["out_gate"][:, now])
 
 

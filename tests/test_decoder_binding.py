@@ -236,3 +236,26 @@ def test_the_layer_takes_a_kernel_family(monkeypatch):
     for kw, want in ((dict(), gbla.ALGO_AUTO), (dict(algo=gbla.ALGO_SIMT), gbla.ALGO_SIMT)):
         decoder.DecoderLayer(128, 2, 64, 16, device="cpu", **kw).prompt(x)
         assert seen.pop() == want
+
+
+def test_positions_past_the_table_are_refused(monkeypatch):
+    """Where the host knows that a position has no row in the layer's table (a whole prompt, or
+    as many steps), the call is refused instead of repeating the last angle."""
+    _fakes(monkeypatch)
+    layer = decoder.DecoderLayer(128, 2, 64, 6, device="cpu")
+    x = torch.randn((2, 9, 128)).to(torch.bfloat16)
+    with pytest.raises(ValueError, match="6 positions"):
+        layer.prompt(x)
+    _, cache = layer.prompt(x[:, :4].contiguous())
+    for i in (4, 5):
+        layer.step(x[:, i:i + 1], cache)
+    before = {n: t.clone() for n, t in cache.items() if isinstance(t, torch.Tensor)}
+    with pytest.raises(ValueError, match="6 positions"):
+        layer.step(x[:, 6:7], cache)
+    assert all(torch.equal(cache[n], t) for n, t in before.items())
+    # lengths that only the device knows may lie within the table in a wider batch
+    _, cache = layer.prompt(x, torch.tensor([5, 2], dtype=torch.int32))
+    for i in range(6):
+        layer.step(x[:, :1], cache)
+    with pytest.raises(ValueError, match="6 positions"):
+        layer.step(x[:, :1], cache)

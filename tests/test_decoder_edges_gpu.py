@@ -6,7 +6,7 @@ import torch
 
 import decoder_ref as R
 from paper_2606_07317_gb300 import decoder, gbla
-from test_decoder_gpu import Case, _close, c32, dev
+from test_decoder_gpu import DEC, Case, _close, _decay_case, c32, dev
 
 pytestmark = pytest.mark.gpu
 
@@ -287,3 +287,31 @@ def test_differentiable_forms_give_the_operators_gradients(dtype, D, algo):
         r = gbla.qk_norm_rotate_backward(q, k, w, w, rot, g["dq"], g["dk"], None, sl, **opt)
     assert torch.equal(dp, torch.stack([r["dq"], r["dk"], g["dv"]], 2))
     assert torch.equal(dw, r["dnorm_q"] + r["dnorm_k"])
+
+
+# ------------------------------------------------------------- kernel families
+
+@pytest.mark.parametrize("i", [i for i, c in enumerate(DEC) if c[5] == "bf16"])
+def test_bf16_runs_on_tensor_cores(i):
+    """The tensor-core family, asked for by name (an error where it does not cover a call),
+    within its bounds, and what the automatic choice takes."""
+    c, q, k, v, ld, s0 = _decay_case(i)
+    do, ds = dev(c.tok(c.H)), dev(c.n(c.B, c.H, c.D, c.D, to=torch.float32))
+    args, kw = [dev(x) for x in (q, k, v, ld)], dict(seq_lens=dev(c.seq_lens), state=dev(s0))
+    out = [torch.zeros(q.shape, dtype=q.dtype, device="cuda") for _ in range(2)]
+    (o, S), (o2, S2) = (gbla.decay_attention(*args, out=b, return_state=True, algo=a, **kw)
+                        for a, b in ((gbla.ALGO_TC, out[0]), (gbla.ALGO_AUTO, out[1])))
+    assert torch.equal(o, o2) and torch.equal(S, S2)
+    on = ~c.past()
+    ref, Sr, om, Sm = R.decay(q, k, v, ld, c.lens, s0, c.D ** -0.5)
+    _close(o.cpu()[on], ref[on], om[on], 2.0 ** -8, "bf16", "o", 2.0 ** -7)
+    _close(S, Sr, Sm, c32(c), "fp32", "state")
+    g, g2 = (gbla.decay_attention_backward(*args, do, dstate=ds, return_dstate=True, algo=a, **kw)
+             for a in (gbla.ALGO_TC, gbla.ALGO_AUTO))
+    for n in g:
+        assert torch.equal(g[n], g2[n]), n
+    ref, mag = R.decay_backward(q, k, v, ld, do.cpu(), c.lens, s0, ds.cpu(), c.D ** -0.5)
+    for n in ("dq", "dk", "dv"):
+        _close(g[n], ref[n], mag[n], 2.0 ** -8, "bf16", n, 2.0 ** -7)
+    _close(g["dstate"], ref["dstate"], mag["dstate"], c32(c), "fp32", "dstate")
+    assert gbla.device_error() == 0

@@ -477,11 +477,16 @@ gbla_status gbla_qk_norm_rotate_backward(
  *   state_out [B, H, D, D] fp32 or NULL: S after each sequence's last token
  *             (state_in for an empty one)
  * scale is finite, not 0 and not subnormal.  Computed in chunks of tokens: bf16 on tensor
- * cores (GBLA_ALGO_TC), fp32 on CUDA cores (GBLA_ALGO_SIMT, which covers both
- * dtypes); the state is held in fp32 on both.  A NaN or infinity in a
- * valid token reaches the other tokens of its chunk, before it too; what
- * padding rows hold reaches nothing.  Sums run in a fixed order.  Scratch comes
- * from the library's pool (GBLA_ERR_ALLOC).
+ * cores (GBLA_ALGO_TC, every D), fp32 on CUDA cores (GBLA_ALGO_SIMT, which covers both
+ * dtypes).  The state is held in fp32 on both.  GBLA_ALGO_TC rounds the weighted
+ * scores, and the state as it meets a query, to bf16 once, here and in the
+ * gradients (results 2.35e-3 of their norm off where the rounding of the results
+ * alone leaves 1.66e-3); GBLA_ALGO_SIMT keeps both in fp32.  An infinite state stays
+ * infinite under every decay above 0.  A NaN or infinity in a valid token reaches
+ * the other tokens of its chunk, before it too; what padding rows hold reaches
+ * nothing.  Sums run in a fixed order.  Scratch comes from the library's pool
+ * (GBLA_ERR_ALLOC).  A batch whose lengths are about equal is faster without
+ * seq_lens, which cuts it for uneven ones.
  */
 gbla_status gbla_decay_attention(const void *q, const void *k, const void *v,
                                  const float *log_decay, const int32_t *seq_lens,
@@ -497,7 +502,8 @@ gbla_status gbla_decay_attention(const void *q, const void *k, const void *v,
  * dtype and dstate_out [B, H, D, D] fp32 (NULL: zeros).  Outputs: dq
  * [B, N, H, D], dk, dv [B, N, Hk, D] dtype (sums over the query heads that share
  * a key / value head, in fp32; rows t >= L_b written as 0) and dstate_in
- * [B, H, D, D] fp32 or NULL.  log_decay has no gradient.  Nothing is kept from a
+ * [B, H, D, D] fp32 or NULL.  log_decay has no gradient.  dstate_out / scale has to be
+ * within fp32's range (it is summed without the scale).  Nothing is kept from a
  * forward call.
  */
 gbla_status gbla_decay_attention_backward(

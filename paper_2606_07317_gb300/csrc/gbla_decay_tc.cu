@@ -13,10 +13,14 @@
 // last token itself.
 //
 // Rounding: the weighted scores and the state as it meets a query are rounded
-// once to bf16 (the results are bf16 too).  The state is held in fp32 registers
-// and is never rebuilt from rounded values: v_j y_j goes into the product as a
-// sum of bf16 numbers, two (2^-17 of a term) where the state only serves the
-// results, three (2^-25) where it is a result itself.  The decay powers are fp32.
+// once to bf16, in the gradients too: the product that reads them takes bf16, and
+// the results are rounded to bf16 themselves.  Against 64 bits the results are
+// 2.35e-3 of their norm off, 1.66e-3 by their own rounding alone, which is what the
+// CUDA-core family leaves (its scores and state stay in fp32).  The state is held in
+// fp32 registers and is never rebuilt from rounded values: v_j y_j goes into the
+// product as a sum of bf16 numbers, two (2^-17 of a term) where the state only
+// serves the results, three (the term rounded to fp32 once, 2^-24) where it is a
+// result itself.  The decay powers are fp32.
 //
 // One CTA scans a run of chunks (a segment) of one (batch, head).  A sequence is
 // cut into several where whole ones would leave SMs idle or one long sequence
@@ -1495,8 +1499,11 @@ int sm_count() {
 // D = 128), as measured: a CTA costs what its pipeline takes to fill and drain and
 // its chunks, one of the own-state kernel 0.6 of a unit a chunk.  Equal lengths:
 // whole rounds of CTAs over the SMs.  Lengths that only the device knows are taken
-// to be a quarter of the longest on average; the kernels then last as long as all
-// the work over the SMs and half a segment of tail, or as their longest CTA.
+// to be uneven, a quarter of the longest on average; the kernels then last as long as
+// all the work over the SMs and half a segment of tail, or as their longest CTA (B32
+// H8 D128, log-normal about 4096 to 32768: 524 us; cut as if all were the longest,
+// 1030).  A batch of about equal lengths pays for that: all 4096 of B19 H8 D64 96 us
+// for 56 without lengths, all 8192 of B16 H8 D128 360 for 238.
 // The pass over keys and values takes `chunk` = 1.6 scanned chunks a chunk.  Starting a
 // CTA: 9 units, at D = 128 4.2 (B8 H8 N8192: 169 us, with 3.5 186; 7 sequences ragged to
 // 21623: 147 us, with 5 176).
@@ -1664,7 +1671,6 @@ size_t tc_scan_floats(const ScanArgs &a) { return part_floats(a, 1); }
 cudaError_t tc_scan(const ScanArgs &a, float *scratch, cudaStream_t st) {
   Scan s;
   const cudaError_t e = s.set(a, scratch);
-  if (e != cudaSuccess) return e;
   return e == cudaSuccess ? launch_scan(s, st) : e;
 }
 

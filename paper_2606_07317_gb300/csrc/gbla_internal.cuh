@@ -203,8 +203,8 @@ struct ScanArgs {
   gbla_dtype dtype;
 };
 // Scratch floats of a scan (partial states of the segments it is split into).
-// n scans of the same sizes, types and lengths (1 <= n <= kMaxScans, B * n within
-// the grid's 65535) run side by side in one launch.
+// n scans of the same sizes, types and lengths (1 <= n <= kMaxScans) run side by side in
+// one launch.
 constexpr int kMaxScans = 3;
 size_t simt_scan_floats(const ScanArgs &a, int n);
 cudaError_t simt_scan(const ScanArgs *a, int n, float *scratch, cudaStream_t st);

@@ -9,7 +9,9 @@ output projection with a residual (a plain matrix product).
   leaves a cache: the attention state of every head, the last three inputs (the
   Conv1D's history), the lengths and, on the host, the tokens it knows of.
 * `DecoderLayer.step` takes one further input of every sequence and updates the
-  cache in place: three kernels and the output product.
+  cache in place: the library's projection (of the window with the new input: four
+  rows, of which the last counts), norm with rotation and step, a kernel each, and
+  PyTorch's operations for the window, the gate, the output product and the residual.
 * `norm_rotate` and `attention` are the two operators as differentiable torch
   functions, for training (first derivatives; deriving their gradients is an error).
 

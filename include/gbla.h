@@ -530,6 +530,94 @@ gbla_status gbla_decay_attention_step(const void *q, const void *k, const void *
                                       int H, int Hk, int D, int n_slots, float scale,
                                       gbla_dtype dtype, gbla_stream_t stream);
 
+/*
+ * gbla_delta_attention -- causal attention by the gated delta rule.  With
+ * S_{-1} = state_in (zeros where NULL) and, for t = 0 .. L_b - 1,
+ *   kept_t = exp(log_decay_t) S_{t-1},        the memory fades,
+ *   miss_t = v_t - kept_t^T k_t,              what it does not hold for this key,
+ *   S_t = kept_t + k_t (beta_t miss_t)^T,     is written,
+ *   o_t = scale S_t^T q_t.
+ *   q, k  [B, N, Hk, D], v [B, N, H, D] dtype: value head h (with gates and a state of
+ *             its own) reads query / key head h / (H / Hk), the other way round than the
+ *             operators above, whose keys and values are shared
+ *   log_decay, beta [B, N, H] dtype: natural logarithm of the decay (at most 0; -inf ends
+ *             the memory of what came before), and the share of the miss that is written.
+ *             beta |k|^2 has to lie within [0, 2], or the state grows from token to token
+ *             (keys of unit length, as gbla_qk_norm_rotate leaves them with weights of
+ *             D^-1/2, and beta within [0, 2])
+ *   strides   NULL or (batch, token) of q, k, v, log_decay, beta; those of the gates are
+ *             at least H and of any alignment, and so are their addresses
+ *   state_in  [B, H, D, D] fp32 (S[d][e], d of k, e of v) or NULL
+ *   o         [B, N, H, D] dtype; rows t >= L_b untouched
+ *   state_out [B, H, D, D] fp32 or NULL: S after each sequence's last token
+ *             (state_in for an empty one)
+ * scale is finite, not 0 and not subnormal.  The state is held in fp32.  Values, keys,
+ * states and gates other than log_decay = -inf are finite.
+ */
+gbla_status gbla_delta_attention(const void *q, const void *k, const void *v,
+                                 const void *log_decay, const void *beta,
+                                 const int32_t *seq_lens, const int64_t *strides,
+                                 const float *state_in, void *o, float *state_out, int B, int N,
+                                 int H, int Hk, int D, float scale, gbla_dtype dtype,
+                                 gbla_stream_t stream);
+
+/*
+ * gbla_delta_attention_step -- the same recurrence for one token of each sequence, on a
+ * pool of states updated in place at slots[b], as gbla_decay_attention_step.
+ *   q, k [B, Hk, D], v [B, H, D], log_decay, beta [B, H] dtype; strides NULL or a host
+ *             array of five element strides (batch of q, k, v, log_decay, beta)
+ * One kernel, allocates nothing.
+ */
+gbla_status gbla_delta_attention_step(const void *q, const void *k, const void *v,
+                                      const void *log_decay, const void *beta,
+                                      const int32_t *slots, const int64_t *strides, float *state,
+                                      void *o, int B, int H, int Hk, int D, int n_slots,
+                                      float scale, gbla_dtype dtype, gbla_stream_t stream);
+
+/* Most top alternatives of a row. */
+#define GBLA_MAX_TOP 64
+
+/*
+ * gbla_token_logprobs -- what the logits of a row say: with y = scale x,
+ *   lse = ln sum exp(y),  entropy = -sum p ln p  with p = exp(y - lse),
+ *   logprob = y[token] - lse, and the `top` largest logits.
+ *   logits    [B, N, V] dtype, the V values of a row contiguous; strides NULL or a host
+ *             array of two element strides (batch, token), each at least V, of any
+ *             alignment (so is the address, beyond its elements')
+ *   tokens    device [B, N] int32 or NULL; a value outside [0, V) marks a row without a
+ *             token, whose logprob is 0
+ *   lse, entropy [B, N] fp32; logprob [B, N] fp32, with tokens (else NULL)
+ *   top_logprob [B, N, top] fp32, top_token [B, N, top] int32, with 0 < top <=
+ *             min(V, GBLA_MAX_TOP) (else NULL): in descending order, equal logits in the
+ *             order of their tokens
+ * Rows t >= L_b are untouched.  1 <= V <= 2^30, scale positive and normal.  Logits of
+ * -inf are ruled out (p = 0); a row of nothing else has lse and log probabilities of
+ * -inf and entropy 0.  A NaN or +inf makes the results of its row NaN; its top tokens
+ * are in range (NaN counts as the least).  fp32 arithmetic, one launch, allocates
+ * nothing; results do not depend on the order in which threads arrive.
+ */
+gbla_status gbla_token_logprobs(const void *logits, const int32_t *tokens,
+                                const int32_t *seq_lens, const int64_t *strides, float *lse,
+                                float *entropy, float *logprob, float *top_logprob,
+                                int32_t *top_token, int B, int N, int V, int top, float scale,
+                                gbla_dtype dtype, gbla_stream_t stream);
+
+/*
+ * gbla_token_logprobs_backward -- gradient of sum(dlogprob * logprob) +
+ * sum(dentropy * entropy) + sum(dlse * lse) with respect to the logits:
+ *   scale (dlogprob (onehot - p) - dentropy p (ln p + entropy) + dlse p).
+ * lse and entropy [B, N] are the forward call's; dlogprob, dentropy, dlse [B, N] fp32 may
+ * each be NULL (zeros).  dlogits [B, N, V] dtype, contiguous: rows t >= L_b, and rows of
+ * nothing but ruled-out logits (-inf, or below -1e30), are written as 0.  It may be the
+ * logits themselves (contiguous), which it then overwrites.
+ */
+gbla_status gbla_token_logprobs_backward(const void *logits, const float *lse,
+                                         const float *entropy, const int32_t *tokens,
+                                         const int32_t *seq_lens, const int64_t *strides,
+                                         const float *dlogprob, const float *dentropy,
+                                         const float *dlse, void *dlogits, int B, int N, int V,
+                                         float scale, gbla_dtype dtype, gbla_stream_t stream);
+
 /* Number of floats per (b, h) in a state buffer: D*D + D. */
 size_t gbla_state_floats(int D);
 

@@ -902,6 +902,91 @@ gbla_status check_scale(float scale) {
   return isnormal(scale) ? GBLA_OK : GBLA_ERR_INVALID_ARG;
 }
 
+// A [B, N, heads] input of single values: strides of any alignment.
+gbla_status gate_view_of(const int64_t *strides, int i, int B, int N, int H, gbla_dtype dt,
+                         View *v) {
+  v->s[0] = (long long)H * N, v->s[1] = H;
+  if (strides) {
+    if (B > 1) v->s[0] = strides[2 * i];
+    if (N > 1) v->s[1] = strides[2 * i + 1];
+    for (int j = 0; j < 2; ++j)
+      if ((j == 0 ? B : N) > 1 && (v->s[j] < H || v->s[j] >= (1ll << (j == 0 ? 44 : 34))))
+        return GBLA_ERR_INVALID_ARG;
+  }
+  v->bytes = (size_t)((B - 1) * v->s[0] + (N - 1) * v->s[1] + H) * elem_bytes(dt);
+  return GBLA_OK;
+}
+
+// What the outputs of the delta rule must not overlap: q, k, v, log_decay, beta, state,
+// lengths (or slots).
+struct DeltaViews {
+  Range in[7];
+};
+
+// Shared checks of the gated delta rule; fills everything of `a` but the outputs and the
+// incoming gradients.
+gbla_status check_delta(DeltaArgs *a, DeltaViews *w, const void *q, const void *k, const void *v,
+                        const void *log_decay, const void *beta, const int32_t *seq_lens,
+                        const int64_t *strides, const float *state_in, int B, int N, int H, int Hk,
+                        int D, float scale, gbla_dtype dtype, bool *empty) {
+  gbla_status s = check_dims(B, H, N, D, dtype, empty);
+  if (s != GBLA_OK) return s;
+  if ((s = check_heads(H, Hk)) != GBLA_OK) return s;
+  if ((s = check_scale(scale)) != GBLA_OK) return s;
+  *a = DeltaArgs{};
+  if (*empty) return GBLA_OK;
+  if ((s = check_ptrs({q, k, v})) != GBLA_OK) return s;
+  const size_t es = elem_bytes(dtype);
+  if (!log_decay || !beta || (uintptr_t)log_decay % es || (uintptr_t)beta % es)
+    return GBLA_ERR_INVALID_ARG;
+  if (!aligned(state_in)) return GBLA_ERR_INVALID_ARG;
+  if ((s = check_seq_lens(seq_lens)) != GBLA_OK) return s;
+  View view[5];
+  for (int i = 0; i < 3; ++i)
+    if ((s = view_of(strides, i, B, N, (long long)(i == 2 ? H : Hk) * D, dtype, &view[i])) !=
+        GBLA_OK)
+      return s;
+  for (int i = 3; i < 5; ++i)
+    if ((s = gate_view_of(strides, i, B, N, H, dtype, &view[i])) != GBLA_OK) return s;
+  const void *in[5] = {q, k, v, log_decay, beta};
+  long long *to[5] = {a->sq, a->sk, a->sv, a->sg, a->sb};
+  for (int i = 0; i < 5; ++i) {
+    to[i][0] = view[i].s[0], to[i][1] = view[i].s[1];
+    w->in[i] = range_of(in[i], view[i].bytes);
+  }
+  w->in[5] = range_of(state_in, state_in ? sizeof(float) * D * D * (size_t)B * H : 0);
+  w->in[6] = range_of(seq_lens, seq_lens ? sizeof(int32_t) * B : 0);
+  a->q = q, a->k = k, a->v = v, a->log_decay = log_decay, a->beta = beta;
+  a->seq_lens = seq_lens, a->init = state_in;
+  a->B = B, a->N = N, a->H = H, a->Hk = Hk, a->D = D, a->scale = scale, a->dtype = dtype;
+  return GBLA_OK;
+}
+
+// Shared checks of the token log probabilities; *bytes is what the logits span.
+gbla_status check_logprob(LogprobArgs *a, size_t *bytes, const void *logits, const int32_t *tokens,
+                          const int32_t *seq_lens, const int64_t *strides, int B, int N, int V,
+                          float scale, gbla_dtype dtype, bool *empty) {
+  if (B < 0 || N < 0 || V < 1 || V > (1 << 30)) return GBLA_ERR_INVALID_ARG;
+  if (dtype != GBLA_FP32 && dtype != GBLA_BF16) return GBLA_ERR_UNSUPPORTED;
+  if (!(scale > 0.f) || !isnormal(scale)) return GBLA_ERR_INVALID_ARG;
+  const unsigned long long rows = (unsigned long long)B * N;
+  if (rows >= (1ull << 31) || rows * V > (1ull << 40)) return GBLA_ERR_INVALID_ARG;
+  *empty = rows == 0;
+  *a = LogprobArgs{};
+  if (*empty) return GBLA_OK;
+  if (!logits || (uintptr_t)logits % elem_bytes(dtype)) return GBLA_ERR_INVALID_ARG;
+  gbla_status s;
+  if ((s = check_seq_lens(tokens)) != GBLA_OK) return s;
+  if ((s = check_seq_lens(seq_lens)) != GBLA_OK) return s;
+  View view;
+  if ((s = gate_view_of(strides, 0, B, N, V, dtype, &view)) != GBLA_OK) return s;
+  *bytes = view.bytes;
+  a->logits = logits, a->s[0] = view.s[0], a->s[1] = view.s[1];
+  a->tokens = tokens, a->seq_lens = seq_lens;
+  a->B = B, a->N = N, a->V = V, a->scale = scale, a->dtype = dtype;
+  return GBLA_OK;
+}
+
 }  // namespace
 
 extern "C" {
@@ -1121,6 +1206,116 @@ gbla_status gbla_decay_attention_step(const void *q, const void *k, const void *
   StepArgs a = {q, k, v, view[0].s[0], view[1].s[0], view[2].s[0], log_decay, slots, state, o,
                 B, H, Hk, D, n_slots, scale, dtype};
   return from_cuda(decay_step(a, (cudaStream_t)stream));
+}
+
+gbla_status gbla_delta_attention(const void *q, const void *k, const void *v,
+                                 const void *log_decay, const void *beta,
+                                 const int32_t *seq_lens, const int64_t *strides,
+                                 const float *state_in, void *o, float *state_out, int B, int N,
+                                 int H, int Hk, int D, float scale, gbla_dtype dtype,
+                                 gbla_stream_t stream) {
+  DeltaArgs a;
+  DeltaViews w;
+  bool empty = false;
+  gbla_status s = check_delta(&a, &w, q, k, v, log_decay, beta, seq_lens, strides, state_in, B, N,
+                              H, Hk, D, scale, dtype, &empty);
+  if (s != GBLA_OK) return s;
+  cudaStream_t st = (cudaStream_t)stream;
+  const size_t sb = sizeof(float) * D * D * (size_t)B * H;
+  if (empty) return pass_state(state_in, state_out, sb, st);
+  if ((s = check_ptrs({o})) != GBLA_OK) return s;
+  if (!aligned_or_null({state_out})) return GBLA_ERR_INVALID_ARG;
+  if (any_overlap({range_of(o, (size_t)B * N * H * D * elem_bytes(dtype)),
+                   range_of(state_out, state_out ? sb : 0)},
+                  {w.in[0], w.in[1], w.in[2], w.in[3], w.in[4], w.in[5], w.in[6]}))
+    return GBLA_ERR_INVALID_ARG;
+  a.o = o, a.fin = state_out;
+  return from_cuda(delta_forward(a, st));
+}
+
+gbla_status gbla_delta_attention_step(const void *q, const void *k, const void *v,
+                                      const void *log_decay, const void *beta,
+                                      const int32_t *slots, const int64_t *strides, float *state,
+                                      void *o, int B, int H, int Hk, int D, int n_slots,
+                                      float scale, gbla_dtype dtype, gbla_stream_t stream) {
+  DeltaArgs a;
+  DeltaViews w;
+  bool empty = false;
+  int64_t pairs[10] = {};
+  for (int i = 0; strides && i < 5; ++i) pairs[2 * i] = strides[i];
+  if (n_slots < 0 || (slots == nullptr && B > n_slots) ||
+      (H > 0 && D > 0 && (unsigned long long)n_slots * H * D * D > (1ull << 40)))
+    return GBLA_ERR_INVALID_ARG;
+  gbla_status s = check_delta(&a, &w, q, k, v, log_decay, beta, slots, strides ? pairs : nullptr,
+                              nullptr, B, 1, H, Hk, D, scale, dtype, &empty);
+  if (s != GBLA_OK) return s;
+  if (empty || n_slots == 0) return GBLA_OK;
+  if ((s = check_ptrs({state, o})) != GBLA_OK) return s;
+  if (any_overlap({range_of(state, sizeof(float) * (size_t)n_slots * H * D * D),
+                   range_of(o, (size_t)B * H * D * elem_bytes(dtype))},
+                  {w.in[0], w.in[1], w.in[2], w.in[3], w.in[4], w.in[6]}))
+    return GBLA_ERR_INVALID_ARG;
+  const DeltaStepArgs t = {q, k, v, log_decay, beta, a.sq[0], a.sk[0], a.sv[0], a.sg[0], a.sb[0],
+                           slots, state, o, B, H, Hk, D, n_slots, scale, dtype};
+  return from_cuda(delta_step(t, (cudaStream_t)stream));
+}
+
+gbla_status gbla_token_logprobs(const void *logits, const int32_t *tokens,
+                                const int32_t *seq_lens, const int64_t *strides, float *lse,
+                                float *entropy, float *logprob, float *top_logprob,
+                                int32_t *top_token, int B, int N, int V, int top, float scale,
+                                gbla_dtype dtype, gbla_stream_t stream) {
+  LogprobArgs a;
+  size_t in = 0;
+  bool empty = false;
+  gbla_status s = check_logprob(&a, &in, logits, tokens, seq_lens, strides, B, N, V, scale, dtype,
+                                &empty);
+  if (s != GBLA_OK) return s;
+  if (top < 0 || top > GBLA_MAX_TOP || top > V) return GBLA_ERR_INVALID_ARG;
+  if (empty) return GBLA_OK;
+  if ((s = check_ptrs({lse, entropy})) != GBLA_OK) return s;
+  if ((logprob != nullptr) != (tokens != nullptr) || (top_logprob != nullptr) != (top > 0) ||
+      (top_token != nullptr) != (top > 0) || !aligned_or_null({logprob, top_logprob, top_token}))
+    return GBLA_ERR_INVALID_ARG;
+  const size_t each = sizeof(float) * (size_t)B * N, tb = each * top;
+  if (any_overlap({range_of(lse, each), range_of(entropy, each),
+                   range_of(logprob, logprob ? each : 0), range_of(top_logprob, tb),
+                   range_of(top_token, tb)},
+                  {range_of(logits, in), range_of(tokens, tokens ? each : 0),
+                   range_of(seq_lens, seq_lens ? sizeof(int32_t) * B : 0)}))
+    return GBLA_ERR_INVALID_ARG;
+  a.lse = lse, a.entropy = entropy, a.logprob = logprob;
+  a.top_logprob = top_logprob, a.top_token = top_token, a.K = top;
+  return from_cuda(logprob_forward(a, (cudaStream_t)stream));
+}
+
+gbla_status gbla_token_logprobs_backward(const void *logits, const float *lse,
+                                         const float *entropy, const int32_t *tokens,
+                                         const int32_t *seq_lens, const int64_t *strides,
+                                         const float *dlogprob, const float *dentropy,
+                                         const float *dlse, void *dlogits, int B, int N, int V,
+                                         float scale, gbla_dtype dtype, gbla_stream_t stream) {
+  LogprobArgs a;
+  size_t in = 0;
+  bool empty = false;
+  gbla_status s = check_logprob(&a, &in, logits, tokens, seq_lens, strides, B, N, V, scale, dtype,
+                                &empty);
+  if (s != GBLA_OK || empty) return s;
+  if ((s = check_ptrs({lse, entropy, dlogits})) != GBLA_OK) return s;
+  if (!aligned_or_null({dlogprob, dentropy, dlse})) return GBLA_ERR_INVALID_ARG;
+  const size_t each = sizeof(float) * (size_t)B * N;
+  const size_t out = (size_t)B * N * V * elem_bytes(dtype);
+  // over the logits, value by value: each is read by the thread that then writes there
+  const bool own = dlogits == logits && (N == 1 || a.s[1] == V) && (B == 1 || a.s[0] == (long long)N * V);
+  if (any_overlap({range_of(dlogits, out)},
+                  {range_of(logits, own ? 0 : in), range_of(lse, each), range_of(entropy, each),
+                   range_of(tokens, tokens ? each : 0), range_of(dlogprob, dlogprob ? each : 0),
+                   range_of(dentropy, dentropy ? each : 0), range_of(dlse, dlse ? each : 0),
+                   range_of(seq_lens, seq_lens ? sizeof(int32_t) * B : 0)}))
+    return GBLA_ERR_INVALID_ARG;
+  a.lse = (float *)lse, a.entropy = (float *)entropy;
+  a.dlogprob = dlogprob, a.dentropy = dentropy, a.dlse = dlse, a.dlogits = dlogits;
+  return from_cuda(logprob_backward(a, (cudaStream_t)stream));
 }
 
 }  // extern "C"

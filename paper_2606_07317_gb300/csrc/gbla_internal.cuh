@@ -235,6 +235,49 @@ struct StepArgs {
 };
 cudaError_t decay_step(const StepArgs &a, cudaStream_t st);
 
+// ---- attention by the gated delta rule (gbla_delta.cu) ----------------------
+struct DeltaArgs {
+  const void *q, *k, *v;                // [B, N, Hk, D] twice, [B, N, H, D]
+  const void *log_decay, *beta;         // [B, N, H]
+  long long sq[2], sk[2], sv[2], sg[2], sb[2];  // element strides (batch, token)
+  const int32_t *seq_lens;
+  const float *init;                    // [B, H, D, D] or NULL
+  void *o;                              // [B, N, H, D] contiguous
+  float *fin;                           // [B, H, D, D] or NULL
+  int B, N, H, Hk, D;
+  float scale;
+  gbla_dtype dtype;
+};
+cudaError_t delta_forward(const DeltaArgs &a, cudaStream_t st);
+struct DeltaStepArgs {
+  const void *q, *k, *v, *log_decay, *beta;  // one token of each sequence; row strides in elements
+  long long sq, sk, sv, sg, sb;
+  const int32_t *slots;
+  float *state;                         // [n_slots, H, D, D], updated in place
+  void *o;                              // [B, H, D] contiguous
+  int B, H, Hk, D, n_slots;
+  float scale;
+  gbla_dtype dtype;
+};
+cudaError_t delta_step(const DeltaStepArgs &a, cudaStream_t st);
+
+// ---- log probabilities of tokens (gbla_logprob.cu) --------------------------
+struct LogprobArgs {
+  const void *logits;                   // [B, N, V], V values contiguous
+  long long s[2];                       // element strides (batch, token)
+  const int32_t *tokens, *seq_lens;     // [B, N], [B]; may be NULL
+  float *logprob, *lse, *entropy;       // [B, N]; logprob may be NULL
+  float *top_logprob;                   // [B, N, K]
+  int32_t *top_token;
+  const float *dlogprob, *dentropy, *dlse;  // backward: gradients coming in, each may be NULL
+  void *dlogits;                        // [B, N, V] contiguous
+  int B, N, V, K;
+  float scale;
+  gbla_dtype dtype;
+};
+cudaError_t logprob_forward(const LogprobArgs &a, cudaStream_t st);
+cudaError_t logprob_backward(const LogprobArgs &a, cudaStream_t st);
+
 // Error bits set by tensor-core kernels whose bounded waits ran out (0 = none);
 // synchronous read of the current device, optionally clearing it.
 unsigned tc_device_error(bool reset);

@@ -1,0 +1,435 @@
+// Log probabilities of given tokens, entropy and top alternatives of rows of logits,
+// and their gradients.
+//
+// With y = scale x, one pass over a row keeps the running maximum m of x and, in powers
+// of two of t = (x - m) scale log2 e,
+//   z = sum 2^t,  w = sum 2^t t;
+// when t moves by delta, z becomes 2^delta z and w becomes 2^delta (w + delta z).  Then
+//   lse = scale m + ln z,  entropy = ln z - ln 2 w / z,
+//   log p(token) = scale (x_token - m) - ln z.
+// Ruled-out logits (-inf) weigh 0; a row of nothing else has lse = -inf and entropy 0.
+#include <cooperative_groups.h>
+#include <math.h>
+
+#include "gbla_internal.cuh"
+#include "gbla_sm100.cuh"
+
+namespace gbla {
+namespace {
+
+using namespace sm100;
+namespace cg = cooperative_groups;
+
+constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
+
+__device__ __forceinline__ float to_f(float v) { return v; }
+__device__ __forceinline__ float to_f(__nv_bfloat16 v) { return __bfloat162float(v); }
+__device__ __forceinline__ void unpack(const uint4 &v, float (&f)[4]) {
+  f[0] = __uint_as_float(v.x), f[1] = __uint_as_float(v.y);
+  f[2] = __uint_as_float(v.z), f[3] = __uint_as_float(v.w);
+}
+__device__ __forceinline__ void unpack(const uint4 &v, float (&f)[8]) {
+  const uint32_t u[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const float2 p = bf2_to_f2(u[i]);
+    f[2 * i] = p.x, f[2 * i + 1] = p.y;
+  }
+}
+__device__ __forceinline__ uint4 pack(const float (&f)[4]) {
+  return make_uint4(__float_as_uint(f[0]), __float_as_uint(f[1]), __float_as_uint(f[2]),
+                    __float_as_uint(f[3]));
+}
+__device__ __forceinline__ uint4 pack(const float (&f)[8]) {
+  return make_uint4(f2_to_bf2(f[0], f[1]), f2_to_bf2(f[2], f[3]), f2_to_bf2(f[4], f[5]),
+                    f2_to_bf2(f[6], f[7]));
+}
+__device__ __forceinline__ void store1(float *p, float v) { *p = v; }
+__device__ __forceinline__ void store1(__nv_bfloat16 *p, float v) { *p = __float2bfloat16_rn(v); }
+// Maximum that keeps a NaN (fmaxf drops it).
+__device__ __forceinline__ float max_nan(float a, float b) {
+  float r;
+  asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
+  return r;
+}
+
+// A row as scalars up to the first 16-byte boundary, vectors of 16 bytes, scalars behind
+// the last whole one: nothing outside the row is read, whatever its length and place.
+template <typename T>
+struct Row {
+  static constexpr int kVec = 16 / sizeof(T);
+  const T *p;
+  int head, vecs, V;
+  __device__ __forceinline__ Row(const T *at, int n) : p(at), V(n) {
+    head = (int)((0u - (uint32_t)(uintptr_t)at) % 16u / sizeof(T));
+    if (head > V) head = V;
+    vecs = (V - head) / kVec;
+  }
+  __device__ __forceinline__ const uint4 *vec(int i) const { return (const uint4 *)(p + head) + i; }
+  __device__ __forceinline__ int loose() const { return V - vecs * kVec; }  // scalars
+  // place of scalar j: those of the head, then those behind the vectors
+  __device__ __forceinline__ int place(int j) const { return j < head ? j : j + vecs * kVec; }
+};
+
+struct Sums {
+  float m, z, w;
+};
+__device__ __forceinline__ float base_of(float m) { return m == -INFINITY ? 0.f : m; }
+// c: scale log2 e
+__device__ __forceinline__ Sums joined(const Sums &a, const Sums &b, float c) {
+  Sums r;
+  r.m = max_nan(a.m, b.m);
+  const float base = base_of(r.m);
+  // an empty side has z = w = 0: any finite distance does
+  const float da = fmaxf((a.m - base) * c, -1e4f), db = fmaxf((b.m - base) * c, -1e4f);
+  const float ea = exp2f(da), eb = exp2f(db);
+  r.z = fmaf(a.z, ea, b.z * eb);
+  r.w = fmaf(fmaf(da, a.z, a.w), ea, fmaf(db, b.z, b.w) * eb);
+  return r;
+}
+
+// Order of candidates: larger logits first, equal ones by their tokens (lowest first).
+// NaN counts as below -inf.  0 stands for none.
+__device__ __forceinline__ uint32_t order_of(float x) {
+  if (x != x) return 1u;
+  const uint32_t u = __float_as_uint(x == 0.f ? 0.f : x);
+  return u & 0x80000000u ? ~u : u | 0x80000000u;
+}
+__device__ __forceinline__ float value_of(uint32_t o) {
+  if (o == 1u) return NAN;
+  return __uint_as_float(o & 0x80000000u ? o & 0x7FFFFFFFu : ~o);
+}
+__device__ __forceinline__ uint64_t key_of(uint32_t order, uint32_t index) {
+  return ((uint64_t)order << 32) | (uint32_t)~index;
+}
+
+// A part of at most kThreads threads of a row, and the parts of a cluster that share one.
+constexpr int kCandidates = 1280;
+
+template <int kThreads>
+struct Shared {
+  Sums part[kThreads / 32];
+  Sums whole;                    // of this part
+  int count;                     // candidates
+  uint64_t bound;
+  uint64_t key[kThreads];
+  uint64_t cand[kCandidates];
+  uint64_t best[GBLA_MAX_TOP];   // this part's, in order
+};
+
+template <typename T, int kThreads, bool kTop>
+__global__ void __launch_bounds__(kThreads) logprob_kernel(const LogprobArgs p, int split) {
+  constexpr int kVec = Row<T>::kVec;
+  __shared__ Shared<kThreads> sm;
+  cg::cluster_group cluster = cg::this_cluster();
+  const int tid = threadIdx.x, lane = tid % 32, part = split > 1 ? (int)cluster.block_rank() : 0;
+  const float c = p.scale * kLog2e;
+  const int rows = p.B * p.N, step = gridDim.x / split;
+  grid_dep_wait();
+  grid_dep_launch();
+  for (int r = blockIdx.x / split; r < rows; r += step) {
+    const int b = r / p.N, t = r % p.N;
+    if (p.seq_lens && t >= __ldg(p.seq_lens + b)) continue;  // the whole cluster skips it
+    const Row<T> row((const T *)p.logits + b * p.s[0] + t * p.s[1], p.V);
+    const int per = (row.vecs + split - 1) / split, v0 = min(part * per, row.vecs),
+              v1 = min(v0 + per, row.vecs);
+    const bool last = part == split - 1;
+    Sums s = {-INFINITY, 0.f, 0.f};
+    float tmax = -INFINITY;
+    uint64_t key = 0;
+    auto add = [&](const float *x, int n) {
+      float m = x[0];
+#pragma unroll
+      for (int i = 1; i < kVec; ++i)
+        if (i < n) m = max_nan(m, x[i]);
+      if (!(m <= s.m)) {
+        const float base = base_of(max_nan(m, s.m)), d = fmaxf((s.m - base) * c, -1e4f), e = exp2f(d);
+        s.w = fmaf(d, s.z, s.w) * e, s.z *= e, s.m = max_nan(m, s.m);
+      }
+      const float base = base_of(s.m);
+#pragma unroll
+      for (int i = 0; i < kVec; ++i)
+        if (i < n) {
+          const float d = max_nan((x[i] - base) * c, -1e4f), e = ex2_approx(d);
+          s.z += e, s.w = fmaf(e, d, s.w);
+        }
+      return m;
+    };
+    for (int i = v0 + tid; i < v1; i += kThreads) {
+      float x[kVec];
+      unpack(__ldg(row.vec(i)), x);
+      const float m = add(x, kVec);
+      if (kTop && (key == 0 || m > tmax)) tmax = m, key = key_of(order_of(m), i * kVec + row.head + kVec - 1);
+    }
+    if (last)
+      for (int j = tid; j < row.loose(); j += kThreads) {
+        const int at = row.place(j);
+        const float x = to_f(row.p[at]);
+        add(&x, 1);
+        if (kTop) {
+          const uint64_t k = key_of(order_of(x), at);
+          if (k > key) key = k;
+        }
+      }
+    // the given token's logit
+    const int token = p.tokens ? __ldg(p.tokens + r) : -1;
+#pragma unroll
+    for (int m = 16; m > 0; m >>= 1) {
+      Sums o;
+      o.m = __shfl_xor_sync(0xFFFFFFFFu, s.m, m);
+      o.z = __shfl_xor_sync(0xFFFFFFFFu, s.z, m);
+      o.w = __shfl_xor_sync(0xFFFFFFFFu, s.w, m);
+      s = joined(s, o, c);
+    }
+    __syncthreads();  // the row before is done with
+    if (lane == 0) sm.part[tid / 32] = s;
+    if (kTop) sm.key[tid] = key;
+    if (tid == 0) sm.count = 0, sm.bound = 0;
+    __syncthreads();
+    if (tid == 0) {
+      s = sm.part[0];
+      for (int i = 1; i < kThreads / 32; ++i) s = joined(s, sm.part[i], c);
+      sm.whole = s;
+    }
+    if (kTop) {
+      // The K-th of the threads' largest bounds the K-th logit from below; only threads
+      // that reach it look at their logits again.
+      if (key) {
+        int rank = 0;
+        for (int i = 0; i < kThreads; ++i) rank += sm.key[i] > key;
+        if (rank == p.K - 1) sm.bound = key;
+      }
+      __syncthreads();
+      const uint64_t bound = sm.bound;
+      auto offer = [&](uint64_t k) {
+        if (k < bound) return;
+        const int at = atomicAdd(&sm.count, 1);
+        if (at < kCandidates) sm.cand[at] = k;
+      };
+      if (key >= bound && key) {
+        for (int i = v0 + tid; i < v1; i += kThreads) {
+          float x[kVec];
+          unpack(__ldg(row.vec(i)), x);
+#pragma unroll
+          for (int e = 0; e < kVec; ++e) offer(key_of(order_of(x[e]), i * kVec + row.head + e));
+        }
+        if (last)
+          for (int j = tid; j < row.loose(); j += kThreads)
+            offer(key_of(order_of(to_f(row.p[row.place(j)])), row.place(j)));
+      }
+      __syncthreads();
+      const int n = sm.count;
+      if (n <= kCandidates) {
+        for (int i = tid; i < n; i += kThreads) {
+          const uint64_t k = sm.cand[i];
+          int rank = 0;
+          for (int j = 0; j < n; ++j) rank += sm.cand[j] > k;
+          if (rank < p.K) sm.best[rank] = k;
+        }
+        for (int i = n + tid; i < p.K; i += kThreads) sm.best[i] = 0;
+      } else {  // too many (sorted logits, for one): the best below the one before, K times
+        uint64_t before = ~0ull;
+        for (int round = 0; round < p.K; ++round) {
+          uint64_t mine = 0;
+          auto look = [&](uint64_t k) {
+            if (k < before && k > mine) mine = k;
+          };
+          for (int i = v0 + tid; i < v1; i += kThreads) {
+            float x[kVec];
+            unpack(__ldg(row.vec(i)), x);
+#pragma unroll
+            for (int e = 0; e < kVec; ++e) look(key_of(order_of(x[e]), i * kVec + row.head + e));
+          }
+          if (last)
+            for (int j = tid; j < row.loose(); j += kThreads)
+              look(key_of(order_of(to_f(row.p[row.place(j)])), row.place(j)));
+          __syncthreads();
+          sm.key[tid] = mine;
+          __syncthreads();
+          for (int i = 0; i < kThreads; ++i) mine = sm.key[i] > mine ? sm.key[i] : mine;
+          if (tid == 0) sm.best[round] = mine;
+          before = mine;
+        }
+      }
+    }
+    if (split > 1) {
+      cluster.sync();
+      if (part == 0) {
+        if (tid == 0)
+          for (int i = 1; i < split; ++i) sm.whole = joined(sm.whole, cluster.map_shared_rank(&sm, i)->whole, c);
+        if (kTop) {
+          const int n = split * p.K;
+          for (int i = tid; i < n; i += kThreads)
+            sm.cand[i] = cluster.map_shared_rank(&sm, i / p.K)->best[i % p.K];
+          __syncthreads();
+          for (int i = tid; i < n; i += kThreads) {
+            const uint64_t k = sm.cand[i];
+            int rank = 0;
+            for (int j = 0; j < n; ++j) rank += sm.cand[j] > k;
+            if (k && rank < p.K) sm.best[rank] = k;
+          }
+        }
+      }
+    }
+    __syncthreads();
+    if (part == 0) {
+      s = sm.whole;
+      const bool bad = s.m != s.m || s.m == INFINITY;
+      const float lnz = logf(s.z);
+      const float lse = bad ? NAN : s.z > 0.f ? fmaf(s.m, p.scale, lnz) : -INFINITY;
+      auto logp = [&](float x) {
+        return bad ? NAN : x == -INFINITY ? -INFINITY : fmaf(x - s.m, p.scale, -lnz);
+      };
+      if (tid == 0) {
+        p.lse[r] = lse;
+        p.entropy[r] = bad ? NAN : s.z > 0.f ? lnz - kLn2 * (s.w / s.z) : 0.f;
+        if (p.logprob) {
+          float lp = 0.f;
+          if (token >= 0 && token < p.V) lp = logp(to_f(row.p[token]));
+          p.logprob[r] = lp;
+        }
+      }
+      if (kTop)
+        for (int i = tid; i < p.K; i += kThreads) {
+          const uint64_t k = sm.best[i];
+          p.top_token[(size_t)r * p.K + i] = (int)~(uint32_t)k;
+          p.top_logprob[(size_t)r * p.K + i] = logp(value_of((uint32_t)(k >> 32)));
+        }
+    }
+    if (split > 1) cluster.sync();  // the other parts' results are read
+  }
+}
+
+// d x = scale [ p (dlse - dlogprob - dentropy (ln p + entropy)) + (dlogprob at the token) ],
+// a tile of a row at a time: bound by the bytes of logits and gradient.
+constexpr int kBackThreads = 256, kBackVecs = 4;  // vectors a thread holds
+
+template <typename T>
+__global__ void __launch_bounds__(kBackThreads) logprob_backward_kernel(const LogprobArgs p,
+                                                                         int tiles) {
+  constexpr int kVec = Row<T>::kVec;
+  grid_dep_wait();
+  grid_dep_launch();
+  const int tid = threadIdx.x;
+  const long long all = (long long)p.B * p.N * tiles;
+  for (long long w = blockIdx.x; w < all; w += gridDim.x) {
+    const int r = (int)(w / tiles), tile = (int)(w % tiles), b = r / p.N, t = r % p.N;
+    T *out = (T *)p.dlogits + (size_t)r * p.V;
+    const Row<T> row(out, p.V);  // cut by the gradient's place
+    const T *in = (const T *)p.logits + b * p.s[0] + t * p.s[1];
+    const bool whole = ((uintptr_t)(in + row.head) & 15) == 0;
+    float lse = 0.f, ent = 0.f, A = 0.f, dh = 0.f, dlp = 0.f;
+    int token = -1;
+    const bool valid = !p.seq_lens || t < __ldg(p.seq_lens + b);
+    if (valid) {
+      lse = p.lse[r], ent = p.entropy[r];
+      token = p.tokens ? __ldg(p.tokens + r) : -1;
+      if (token < 0 || token >= p.V) token = -1;
+      if (p.dlogprob && token >= 0) dlp = p.dlogprob[r];
+      if (p.dentropy) dh = p.dentropy[r];
+      A = (p.dlse ? p.dlse[r] : 0.f) - dlp;
+    }
+    // padding, or a row of nothing but masks (also such of a type's lowest value, whose
+    // lse cannot tell one token from many)
+    const bool none = !valid || lse < -1e30f;
+    auto grad = [&](float x, int at) {
+      const float lp = max_nan(fmaf(x, p.scale, -lse), -1e4f);
+      float d = ex2_approx(lp * kLog2e) * fmaf(-dh, lp + ent, A);
+      if (at == token) d += dlp;
+      return none ? 0.f : d * p.scale;
+    };
+    const int v0 = tile * kBackThreads * kBackVecs + tid;
+    uint4 v[kBackVecs];
+#pragma unroll
+    for (int j = 0; j < kBackVecs; ++j) {
+      const int i = v0 + j * kBackThreads;
+      if (i >= row.vecs || none) continue;
+      if (whole) {
+        v[j] = *((const uint4 *)(in + row.head) + i);
+      } else {
+        float f[kVec];
+#pragma unroll
+        for (int e = 0; e < kVec; ++e) f[e] = to_f(in[row.head + i * kVec + e]);
+        v[j] = pack(f);
+      }
+    }
+#pragma unroll
+    for (int j = 0; j < kBackVecs; ++j) {
+      const int i = v0 + j * kBackThreads;
+      if (i >= row.vecs) continue;
+      float f[kVec];
+      if (none) v[j] = make_uint4(0, 0, 0, 0);
+      unpack(v[j], f);
+#pragma unroll
+      for (int e = 0; e < kVec; ++e) f[e] = grad(f[e], row.head + i * kVec + e);
+      *((uint4 *)(out + row.head) + i) = pack(f);
+    }
+    if (tile == 0 && tid < row.loose()) {
+      const int at = row.place(tid);
+      store1(out + at, none ? 0.f : grad(to_f(in[at]), at));
+    }
+  }
+}
+
+int sm_count() {
+  int dev = 0, n = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess ||
+      cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess || n <= 0)
+    return 152;
+  return n;
+}
+
+template <typename T, int kThreads, bool kTop>
+cudaError_t forward_launch(const LogprobArgs &a, int split, int blocks, cudaStream_t st) {
+  cudaLaunchAttribute attr[2];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  attr[1].id = cudaLaunchAttributeClusterDimension;
+  attr[1].val.clusterDim.x = split, attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(blocks * split);
+  cfg.blockDim = dim3(kThreads);
+  cfg.stream = st;
+  cfg.attrs = attr;
+  cfg.numAttrs = 2;
+  count_launch();
+  return cudaLaunchKernelEx(&cfg, logprob_kernel<T, kThreads, kTop>, a, split);
+}
+
+template <typename T>
+cudaError_t forward_t(const LogprobArgs &a, cudaStream_t st) {
+  const long long rows = (long long)a.B * a.N;
+  const int sms = sm_count();
+  const int vecs = a.V / Row<T>::kVec;
+  // few rows: several blocks share one, while each still has some vectors a thread
+  int split = 1;
+  while (split < 8 && rows * split * 2 <= sms * 4 && vecs / (split * 2) >= 256) split *= 2;
+  long long blocks = 8ll * sms / split;
+  if (blocks > rows) blocks = rows;
+  if (a.K > 0) return forward_launch<T, 256, true>(a, split, (int)blocks, st);
+  return forward_launch<T, 256, false>(a, split, (int)blocks, st);
+}
+
+template <typename T>
+cudaError_t backward_t(const LogprobArgs &a, cudaStream_t st) {
+  const int vecs = a.V / Row<T>::kVec, each = kBackThreads * kBackVecs;
+  const int tiles = vecs < each ? 1 : (vecs + each - 1) / each;
+  const long long all = (long long)a.B * a.N * tiles;
+  long long blocks = 16ll * sm_count();
+  if (blocks > all) blocks = all;
+  count_launch();
+  return launch_pdl(logprob_backward_kernel<T>, dim3((unsigned)blocks), dim3(kBackThreads), 0, st,
+                    a, tiles);
+}
+
+}  // namespace
+
+cudaError_t logprob_forward(const LogprobArgs &a, cudaStream_t st) {
+  return a.dtype == GBLA_FP32 ? forward_t<float>(a, st) : forward_t<__nv_bfloat16>(a, st);
+}
+
+cudaError_t logprob_backward(const LogprobArgs &a, cudaStream_t st) {
+  return a.dtype == GBLA_FP32 ? backward_t<float>(a, st) : backward_t<__nv_bfloat16>(a, st);
+}
+
+}  // namespace gbla

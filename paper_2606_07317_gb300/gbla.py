@@ -23,6 +23,7 @@ FLAG_NO_CONV, FLAG_NO_GATE, FLAG_NO_NORM = 1, 2, 4
 FLAG_BLA = FLAG_NO_CONV | FLAG_NO_GATE | FLAG_NO_NORM
 CONV_WIDTH = 4
 ROTATE_INTERLEAVED = 1
+MAX_TOP = 64
 
 EXPORTED = ["gbla_forward", "gbla_forward_ex", "gbla_forward_variant", "gbla_forward_f32out",
             "gbla_backward", "gbla_backward_variant", "gbla_backward_from_state",
@@ -33,7 +34,9 @@ EXPORTED = ["gbla_forward", "gbla_forward_ex", "gbla_forward_variant", "gbla_for
             "gbla_state_static_scratch", "gbla_device_error", "gbla_last_cuda_error",
             "gbla_project", "gbla_layer_forward", "gbla_attention_forward",
             "gbla_qk_norm_rotate", "gbla_qk_norm_rotate_backward", "gbla_decay_attention",
-            "gbla_decay_attention_backward", "gbla_decay_attention_step"]
+            "gbla_decay_attention_backward", "gbla_decay_attention_step",
+            "gbla_delta_attention", "gbla_delta_attention_step",
+            "gbla_token_logprobs", "gbla_token_logprobs_backward"]
 
 _lock = threading.Lock()
 _lib = None
@@ -110,6 +113,14 @@ def load(path: str | None = None):
         lib.gbla_decay_attention_backward.restype = _i
         lib.gbla_decay_attention_step.argtypes = [_vp] * 8 + [_i] * 5 + [f, _i, _vp]
         lib.gbla_decay_attention_step.restype = _i
+        lib.gbla_delta_attention.argtypes = [_vp] * 10 + [_i] * 5 + [f, _i, _vp]
+        lib.gbla_delta_attention.restype = _i
+        lib.gbla_delta_attention_step.argtypes = [_vp] * 9 + [_i] * 5 + [f, _i, _vp]
+        lib.gbla_delta_attention_step.restype = _i
+        lib.gbla_token_logprobs.argtypes = [_vp] * 9 + [_i] * 4 + [f, _i, _vp]
+        lib.gbla_token_logprobs.restype = _i
+        lib.gbla_token_logprobs_backward.argtypes = [_vp] * 10 + [_i] * 3 + [f, _i, _vp]
+        lib.gbla_token_logprobs_backward.restype = _i
         lib.gbla_state_floats.argtypes = [_i]
         lib.gbla_state_floats.restype = ctypes.c_size_t
         lib.gbla_rms_eps.argtypes = []
@@ -632,4 +643,155 @@ def decay_attention_step(q, k, v, log_decay, state, slots=None, scale=None, out=
         D ** -0.5 if scale is None else scale, code, _raw_stream(dev, stream))
     _check(st, "gbla_decay_attention_step")
     _changed((state, out) if given else (state,))
+    return out
+
+
+def _gate(t, name, shape, dtype, dev):
+    """Checks gates [B, N, H] whose heads are adjacent; True if they are contiguous."""
+    if t.shape != shape:
+        raise ValueError(f"{name} must be [B, N, H] = {tuple(shape)}, not {tuple(t.shape)}")
+    if t.dtype is not dtype or t.get_device() != dev:
+        raise ValueError(f"{name} must have the dtype and device of q")
+    if t.is_contiguous():
+        return True
+    if shape[2] > 1 and t.stride(2) != 1:
+        raise ValueError(f"the heads of {name} must be adjacent")
+    return False
+
+
+def _delta_args(q, k, v, log_decay, beta):
+    """(code, device, whether all are contiguous, sizes): the inputs of the delta rule, whose
+    heads and gates are those of the values."""
+    B, N, Hk, D = _dims(q)
+    if v.dim() != 4:
+        raise ValueError("v must be [B, N, H, D]")
+    code, dev = _code(q)
+    H = v.shape[2]
+    dt = q.dtype
+    whole = (_heads(q, "q", (B, N, Hk, D), dt, dev) & _heads(k, "k", (B, N, Hk, D), dt, dev)
+             & _heads(v, "v", (B, N, H, D), dt, dev)
+             & _gate(log_decay, "log_decay", (B, N, H), dt, dev)
+             & _gate(beta, "beta", (B, N, H), dt, dev))
+    return code, dev, whole, (B, N, H, Hk, D)
+
+
+def delta_attention(q, k, v, log_decay, beta, seq_lens=None, state=None, scale=None, out=None,
+                    return_state: bool = False, stream=None):
+    """Causal attention by the gated delta rule (gbla_delta_attention):
+    kept = exp(log_decay_t) S_{t-1}, S_t = kept + k_t (beta_t (v_t - kept^T k_t))^T,
+    o_t = scale S_t^T q_t for q, k [B, N, Hk, D], v [B, N, H, D] and gates log_decay, beta
+    [B, N, H] (a value head reads query / key head h / (H / Hk)); `state` [B, H, D, D] fp32 is S
+    before the first token, scale defaults to D^-1/2.  Keys of about unit length keep the state
+    bounded (beta |k|^2 <= 2).  Returns o, or (o, S after each sequence's last token) with
+    return_state; rows of o past seq_lens are not written."""
+    code, dev, whole, dims = _delta_args(q, k, v, log_decay, beta)
+    B, N, H, Hk, D = dims
+    given = out is not None
+    if not given:
+        out = _like(v, stream)
+    fin = _empty(stream, (B, H, D, D), torch.float32, q.device) if return_state else None
+    st = (_lib or load()).gbla_delta_attention(
+        q.data_ptr(), k.data_ptr(), v.data_ptr(), log_decay.data_ptr(), beta.data_ptr(),
+        _plain(seq_lens, "seq_lens", (B,), torch.int32, dev),
+        None if whole else _strides(q, k, v, log_decay, beta),
+        _plain(state, "state", (B, H, D, D), torch.float32, dev),
+        _plain(out, "out", v.shape, q.dtype, dev), None if fin is None else fin.data_ptr(),
+        *dims, D ** -0.5 if scale is None else scale, code, _raw_stream(dev, stream))
+    _check(st, "gbla_delta_attention")
+    if given:
+        _changed((out,))
+    return (out, fin) if return_state else out
+
+
+def delta_attention_step(q, k, v, log_decay, beta, state, slots=None, scale=None, out=None,
+                         stream=None) -> torch.Tensor:
+    """One token of each sequence (gbla_delta_attention_step): q, k [B, 1, Hk, D], v
+    [B, 1, H, D], log_decay, beta [B, 1, H]; `state` [n_slots, H, D, D] fp32 is updated in place
+    at slots[b] (int32; None: slot b; no two the same).  Rows whose slot is outside the pool are
+    left alone.  Returns o."""
+    code, dev, whole, (B, N, H, Hk, D) = _delta_args(q, k, v, log_decay, beta)
+    if N != 1:
+        raise ValueError("q, k, v and the gates hold one token of each sequence")
+    n_slots = state.shape[0]
+    given = out is not None
+    if not given:
+        out = _like(v, stream)
+    st = (_lib or load()).gbla_delta_attention_step(
+        q.data_ptr(), k.data_ptr(), v.data_ptr(), log_decay.data_ptr(), beta.data_ptr(),
+        _plain(slots, "slots", (B,), torch.int32, dev),
+        None if whole else _strides(q, k, v, log_decay, beta, dims=1),
+        _plain(state, "state", (n_slots, H, D, D), torch.float32, dev),
+        _plain(out, "out", v.shape, q.dtype, dev), B, H, Hk, D, n_slots,
+        D ** -0.5 if scale is None else scale, code, _raw_stream(dev, stream))
+    _check(st, "gbla_delta_attention_step")
+    _changed((state, out) if given else (state,))
+    return out
+
+
+def _logit_args(logits, tokens, seq_lens):
+    """(code, device, addresses of logits, tokens, lengths and strides, sizes)."""
+    if logits.dim() != 3:
+        raise ValueError("logits must be [B, N, V]")
+    B, N, V = logits.shape
+    code, dev = _code(logits)
+    whole = logits.is_contiguous()
+    if not whole and V > 1 and logits.stride(2) != 1:
+        raise ValueError("the values of a row of logits must be contiguous")
+    return code, dev, (logits.data_ptr(), _plain(tokens, "tokens", (B, N), torch.int32, dev),
+                       _plain(seq_lens, "seq_lens", (B,), torch.int32, dev),
+                       None if whole else _strides(logits)), (B, N, V)
+
+
+def token_logprobs(logits, tokens=None, top: int = 0, scale: float = 1.0, seq_lens=None, out=None,
+                   stream=None) -> dict:
+    """What rows of logits [B, N, V] say (gbla_token_logprobs), y = scale * logits: lse
+    (ln sum exp y) and entropy [B, N]; with `tokens` [B, N] int32, logprob [B, N] (0 where the
+    token is outside [0, V)); with `top` (at most 64), top_logprob and top_token [B, N, top] in
+    descending order, equal logits by their tokens.  Logits of -inf are ruled out.  `out` may
+    supply the tensors by these names; rows past seq_lens are not written."""
+    code, dev, ins, (B, N, V) = _logit_args(logits, tokens, seq_lens)
+    f32 = torch.float32
+    shapes = {"lse": ((B, N), f32), "entropy": ((B, N), f32)}
+    if tokens is not None:
+        shapes["logprob"] = ((B, N), f32)
+    if top:
+        shapes |= {"top_logprob": ((B, N, top), f32), "top_token": ((B, N, top), torch.int32)}
+    given = out is not None
+    if given and out.keys() != shapes.keys():
+        raise ValueError(f"out must hold {', '.join(shapes)}")
+    if not given:
+        out = {n: _empty(stream, shape, dt, logits.device) for n, (shape, dt) in shapes.items()}
+    at = [_plain(out.get(n), n, *shapes.get(n, ((), f32)), dev)
+          for n in ("lse", "entropy", "logprob", "top_logprob", "top_token")]
+    st = (_lib or load()).gbla_token_logprobs(*ins, *at, B, N, V, top, scale, code,
+                                              _raw_stream(dev, stream))
+    _check(st, "gbla_token_logprobs")
+    if given:
+        _changed(tuple(out.values()))
+    return out
+
+
+def token_logprobs_backward(logits, lse, entropy, tokens=None, dlogprob=None, dentropy=None,
+                            dlse=None, scale: float = 1.0, seq_lens=None, out=None,
+                            stream=None) -> torch.Tensor:
+    """Gradient of the logits (gbla_token_logprobs_backward) for the gradients dlogprob,
+    dentropy and dlse [B, N] fp32 (None: zeros) of token_logprobs' results, from its lse and
+    entropy.  Rows past seq_lens are 0.  `out` [B, N, V] contiguous may be the logits
+    themselves, which are overwritten then."""
+    code, dev, (at, tok, lens, strides), (B, N, V) = _logit_args(logits, tokens, seq_lens)
+    given = out is not None
+    if not given:
+        out = _like(logits, stream)
+    small = [_plain(t, n, (B, N), torch.float32, dev)
+             for t, n in ((lse, "lse"), (entropy, "entropy"), (dlogprob, "dlogprob"),
+                          (dentropy, "dentropy"), (dlse, "dlse"))]
+    if lse is None or entropy is None:
+        raise ValueError("lse and entropy of the forward call are needed")
+    st = (_lib or load()).gbla_token_logprobs_backward(
+        at, *small[:2], tok, lens, strides, *small[2:],
+        _plain(out, "out", logits.shape, logits.dtype, dev), B, N, V, scale, code,
+        _raw_stream(dev, stream))
+    _check(st, "gbla_token_logprobs_backward")
+    if given:
+        _changed((out,))
     return out

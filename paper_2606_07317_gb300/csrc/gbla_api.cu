@@ -1230,7 +1230,9 @@ gbla_status gbla_delta_attention(const void *q, const void *k, const void *v,
                   {w.in[0], w.in[1], w.in[2], w.in[3], w.in[4], w.in[5], w.in[6]}))
     return GBLA_ERR_INVALID_ARG;
   a.o = o, a.fin = state_out;
-  return from_cuda(delta_forward(a, st));
+  Scratch ws;
+  if ((s = ws.alloc(sizeof(float) * delta_forward_floats(a), st)) != GBLA_OK) return s;
+  return from_cuda(delta_forward(a, (float *)ws.ptr, st));
 }
 
 gbla_status gbla_delta_attention_step(const void *q, const void *k, const void *v,

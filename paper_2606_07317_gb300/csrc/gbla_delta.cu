@@ -1,5 +1,4 @@
-// Attention by the gated delta rule, token by token: the single-token form on a
-// pool of states, and a scan over the tokens of a sequence.
+// Attention by the gated delta rule: the single-token form on a pool of states.
 //
 // With the state S[d][e] of a head, each token reads what the decayed state holds
 // for its key, and writes the difference to its value, weighted by beta:
@@ -19,8 +18,6 @@ using namespace sm100;
 
 __device__ __forceinline__ float to_f(float v) { return v; }
 __device__ __forceinline__ float to_f(__nv_bfloat16 v) { return __bfloat162float(v); }
-__device__ __forceinline__ void store1(float *p, float v) { *p = v; }
-__device__ __forceinline__ void store1(__nv_bfloat16 *p, float v) { *p = __float2bfloat16_rn(v); }
 __device__ __forceinline__ void load4(const float *p, float (&f)[4]) {
   const float4 v = __ldg((const float4 *)p);
   f[0] = v.x, f[1] = v.y, f[2] = v.z, f[3] = v.w;
@@ -135,112 +132,7 @@ cudaError_t step_launch(const DeltaStepArgs &a, cudaStream_t st) {
   return launch_pdl(step_kernel<T, D>, dim3(a.H, a.B), dim3(StepShape<D>::kThreads), 0, st, a);
 }
 
-// ------------------------------------------------------------- token by token
-// A block serves 32 of the state's columns (each by itself a recurrence over the
-// tokens) of one (sequence, head); four threads share a column, a quarter of the
-// rows each, in registers for the whole sequence.
-constexpr int kTile = 16;  // tokens in shared memory at a time
-
-template <typename T, int D>
-__global__ void __launch_bounds__(128) token_kernel(const DeltaArgs p) {
-  constexpr int kQuads = D / 16;  // float4s of rows a thread holds
-  __shared__ __align__(16) float ks[kTile][D], qs[kTile][D];
-  __shared__ float vs[kTile][32];
-  __shared__ float gate[3][kTile];  // decay as two floats, beta
-  const int tid = threadIdx.x, r = tid & 3, col = blockIdx.x * 32 + (tid >> 2);
-  const int h = blockIdx.y, b = blockIdx.z, hk = h / (p.H / p.Hk);
-  const int L = p.seq_lens ? min(max(__ldg(p.seq_lens + b), 0), p.N) : p.N;
-  const size_t bh = (size_t)b * p.H + h;
-  float4 S[kQuads];
-#pragma unroll
-  for (int i = 0; i < kQuads; ++i) {
-    S[i] = make_float4(0.f, 0.f, 0.f, 0.f);
-    if (p.init) {
-      const float *s0 = p.init + bh * D * D + (size_t)(16 * i + 4 * r) * D + col;
-      S[i] = make_float4(s0[0], s0[D], s0[2 * D], s0[3 * D]);
-    }
-  }
-  const T *q = (const T *)p.q + b * p.sq[0] + (long long)hk * D;
-  const T *k = (const T *)p.k + b * p.sk[0] + (long long)hk * D;
-  const T *v = (const T *)p.v + b * p.sv[0] + (long long)h * D + blockIdx.x * 32;
-  const T *lg = (const T *)p.log_decay + b * p.sg[0] + h;
-  const T *be = (const T *)p.beta + b * p.sb[0] + h;
-  T *o = (T *)p.o + ((size_t)b * p.N * p.H + h) * D + col;
-  for (int t0 = 0; t0 < L; t0 += kTile) {
-    const int n = min(kTile, L - t0);
-    __syncthreads();
-    for (int i = tid; i < n * D; i += 128) {
-      const int t = i / D, d = i % D;
-      ks[t][d] = to_f(k[(t0 + t) * p.sk[1] + d]);
-      qs[t][d] = to_f(q[(t0 + t) * p.sq[1] + d]);
-    }
-    for (int i = tid; i < n * 32; i += 128) vs[i / 32][i % 32] = to_f(v[(t0 + i / 32) * p.sv[1] + i % 32]);
-    if (tid < n) {
-      const DecayFactor f = decay_factor(to_f(lg[(t0 + tid) * p.sg[1]]));
-      gate[0][tid] = f.hi, gate[1][tid] = f.lo;
-      gate[2][tid] = to_f(be[(t0 + tid) * p.sb[1]]);
-    }
-    __syncthreads();
-    for (int t = 0; t < n; ++t) {
-      const float hi = gate[0][t], lo = gate[1][t];
-      float ka = 0.f, qa = 0.f, kq = 0.f, kb = 0.f, qb = 0.f, kr = 0.f;
-#pragma unroll
-      for (int i = 0; i < kQuads; ++i) {
-        const float4 kv = *(const float4 *)&ks[t][16 * i + 4 * r], qv = *(const float4 *)&qs[t][16 * i + 4 * r];
-        S[i].x = fmaf(hi, S[i].x, lo * S[i].x), S[i].y = fmaf(hi, S[i].y, lo * S[i].y);
-        S[i].z = fmaf(hi, S[i].z, lo * S[i].z), S[i].w = fmaf(hi, S[i].w, lo * S[i].w);
-        ka = fmaf(kv.x, S[i].x, ka), kb = fmaf(kv.y, S[i].y, kb);
-        ka = fmaf(kv.z, S[i].z, ka), kb = fmaf(kv.w, S[i].w, kb);
-        qa = fmaf(qv.x, S[i].x, qa), qb = fmaf(qv.y, S[i].y, qb);
-        qa = fmaf(qv.z, S[i].z, qa), qb = fmaf(qv.w, S[i].w, qb);
-        kq = fmaf(kv.x, qv.x, kq), kr = fmaf(kv.y, qv.y, kr);
-        kq = fmaf(kv.z, qv.z, kq), kr = fmaf(kv.w, qv.w, kr);
-      }
-      ka += kb, qa += qb, kq += kr;
-#pragma unroll
-      for (int m = 1; m < 4; m <<= 1) {
-        ka += __shfl_xor_sync(0xFFFFFFFFu, ka, m);
-        qa += __shfl_xor_sync(0xFFFFFFFFu, qa, m);
-        kq += __shfl_xor_sync(0xFFFFFFFFu, kq, m);
-      }
-      const float u = gate[2][t] * (vs[t][tid >> 2] - ka);
-#pragma unroll
-      for (int i = 0; i < kQuads; ++i) {
-        const float4 kv = *(const float4 *)&ks[t][16 * i + 4 * r];
-        S[i].x = fmaf(kv.x, u, S[i].x), S[i].y = fmaf(kv.y, u, S[i].y);
-        S[i].z = fmaf(kv.z, u, S[i].z), S[i].w = fmaf(kv.w, u, S[i].w);
-      }
-      if (r == 0) store1(o + (size_t)(t0 + t) * p.H * D, p.scale * fmaf(kq, u, qa));
-    }
-  }
-  if (p.fin) {
-#pragma unroll
-    for (int i = 0; i < kQuads; ++i) {
-      float *s1 = p.fin + bh * D * D + (size_t)(16 * i + 4 * r) * D + col;
-      s1[0] = S[i].x, s1[D] = S[i].y, s1[2 * D] = S[i].z, s1[3 * D] = S[i].w;
-    }
-  }
-}
-
-template <typename T, int D>
-cudaError_t token_launch(const DeltaArgs &a, cudaStream_t st) {
-  count_launch();
-  token_kernel<T, D><<<dim3(D / 32, a.H, a.B), 128, 0, st>>>(a);
-  return cudaGetLastError();
-}
-
 }  // namespace
-
-cudaError_t delta_forward(const DeltaArgs &a, cudaStream_t st) {
-  if (a.dtype == GBLA_FP32) {
-    if (a.D == 32) return token_launch<float, 32>(a, st);
-    if (a.D == 64) return token_launch<float, 64>(a, st);
-    return token_launch<float, 128>(a, st);
-  }
-  if (a.D == 32) return token_launch<__nv_bfloat16, 32>(a, st);
-  if (a.D == 64) return token_launch<__nv_bfloat16, 64>(a, st);
-  return token_launch<__nv_bfloat16, 128>(a, st);
-}
 
 cudaError_t delta_step(const DeltaStepArgs &a, cudaStream_t st) {
   if (a.dtype == GBLA_FP32) {

@@ -235,7 +235,7 @@ struct StepArgs {
 };
 cudaError_t decay_step(const StepArgs &a, cudaStream_t st);
 
-// ---- attention by the gated delta rule (gbla_delta.cu) ----------------------
+// ---- attention by the gated delta rule (gbla_delta.cu, gbla_delta_chunk.cu) -
 struct DeltaArgs {
   const void *q, *k, *v;                // [B, N, Hk, D] twice, [B, N, H, D]
   const void *log_decay, *beta;         // [B, N, H]
@@ -248,7 +248,9 @@ struct DeltaArgs {
   float scale;
   gbla_dtype dtype;
 };
-cudaError_t delta_forward(const DeltaArgs &a, cudaStream_t st);
+// Scratch: what the chunks prepare.
+size_t delta_forward_floats(const DeltaArgs &a);
+cudaError_t delta_forward(const DeltaArgs &a, float *scratch, cudaStream_t st);
 struct DeltaStepArgs {
   const void *q, *k, *v, *log_decay, *beta;  // one token of each sequence; row strides in elements
   long long sq, sk, sv, sg, sb;

@@ -18,13 +18,24 @@ namespace gbla {
 namespace delta {
 namespace {
 
+// A chunk's record: M, P and the powers of its gates.  M in kSolve terms; P in one where results
+// are bf16.
+template <typename T, int kSolve>
+struct Record {
+  static constexpr int C = kChunkOf<T>;
+  using M = Tiles<C, kSolve>;
+  using P = Tiles<C, sizeof(T) == 2 ? 1 : 3>;
+  static constexpr int kM = 0, kP = M::kFloats, kGates = kP + P::kFloats;
+  static constexpr int kFloats = kGates + Gates<C>::kFloats;
+};
+
 // --------------------------------------------------------------- first launch
-// One block a (chunk, head, batch).
+// One block a (chunk, head, batch), a warp for each 16 of its tokens.
 template <typename T, int D>
 struct PrepShape {
   static constexpr int C = kChunkOf<T>, kWarps = C / 16, kThreads = kWarps * 32;
   static constexpr int kRow = pad_row<T>(D), kMat = C + 4;
-  static constexpr int kBytes = (2 * C * kRow) * sizeof(T) + C * kMat * 4 + 4 * C * 4 + 16;
+  static constexpr int kBytes = 2 * C * kRow * (int)sizeof(T) + 2 * C * kMat * 4 + 4 * C * 4 + 16;
 };
 
 // Products of 16 rows of `left` with every row of `right` up to the block's last row, fp32 tiles
@@ -67,15 +78,108 @@ __device__ __forceinline__ void rows_times_rows(float (&acc)[C / 8][4], const fl
   }
 }
 
-template <typename T, int D>
+// Parts of C x C matrices in shared memory (rows of C + 4 floats) as operands: 16 rows from i on
+// at columns j .. j + 7 on the left, columns j .. j + 7 of rows i .. i + 7 on the right.
+template <int C>
+__device__ __forceinline__ LeftTf32<3> left_of(const float *m, int i, int j) {
+  const int g = (threadIdx.x & 31) >> 2, t = threadIdx.x & 3;
+  const float2 x = *(const float2 *)(m + (i + g) * (C + 4) + j + 2 * t);
+  const float2 y = *(const float2 *)(m + (i + g + 8) * (C + 4) + j + 2 * t);
+  const float c[4] = {x.x, x.y, y.x, y.y};
+  return LeftTf32<3>(c);
+}
+template <int C>
+__device__ __forceinline__ void times_right(float (&c)[4], const LeftTf32<3> &a, const float *m,
+                                            int i, int j) {
+  const int g = (threadIdx.x & 31) >> 2, t = threadIdx.x & 3;
+  const float *at = m + (i + 2 * t) * (C + 4) + j + g;
+  a.times(c, at[0], at[C + 4]);
+}
+
+// to = (1 + A)^-1 for strictly lower triangular A, on and below its diagonal blocks of 16.
+// Those by forward substitution, the rest from
+//   (1 + A)^-1 = [ M0 0; -M1 A10 M0 M1 ]
+// for pairs of blocks of 16 and then of 32, in products of three tf32 terms.  (No powers of A,
+// which grow where the inverse does not: keys that repeat.)  Begins and ends with all of A, and
+// of `to`, visible to the block.
+template <int C>
+__device__ __forceinline__ void invert(float *to, const float *A, int w) {
+  constexpr int kMat = C + 4;
+  const int lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
+  auto put = [&](const float (&c)[4], int i, int j) {  // minus the product
+    *(float2 *)(to + (i + g) * kMat + j + 2 * t) = make_float2(-c[0], -c[1]);
+    *(float2 *)(to + (i + g + 8) * kMat + j + 2 * t) = make_float2(-c[2], -c[3]);
+  };
+  {
+    const float *a = A + 16 * w * kMat + 16 * w;
+    float x[16];
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+      float s = i == (lane & 15) ? 1.f : 0.f, s1 = 0.f;
+#pragma unroll
+      for (int m = 0; m < i; m += 4) {
+        const float4 v = *(const float4 *)(a + i * kMat + m);
+        s = fmaf(-v.x, x[m], s);
+        if (m + 1 < i) s1 = fmaf(-v.y, x[m + 1], s1);
+        if (m + 2 < i) s = fmaf(-v.z, x[m + 2], s);
+        if (m + 3 < i) s1 = fmaf(-v.w, x[m + 3], s1);
+      }
+      x[i] = s + s1;
+      if (lane < 16) to[(16 * w + i) * kMat + 16 * w + lane] = x[i];
+    }
+  }
+  __syncthreads();
+  if (w & 1) {
+    const int i = 16 * w, j = i - 16;
+    float z[2][4] = {}, y[2][4] = {};
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+      const LeftTf32<3> a = left_of<C>(to, i, i + 8 * k);
+#pragma unroll
+      for (int n = 0; n < 2; ++n) times_right<C>(z[n], a, A, i + 8 * k, j + 8 * n);
+    }
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+      const LeftTf32<3> a(z[k]);
+#pragma unroll
+      for (int n = 0; n < 2; ++n) times_right<C>(y[n], a, to, j + 8 * k, j + 8 * n);
+    }
+    put(y[0], i, j), put(y[1], i, j + 8);
+  }
+  __syncthreads();
+  if (C == 64) {
+    // rows 32 .. 63, columns 0 .. 31: a warp takes 16 of each
+    const int i = 32 + 16 * (w & 1), j = 16 * (w >> 1);
+    float z[4][4] = {}, y[2][4] = {};
+#pragma unroll
+    for (int k = 0; k < 4; ++k)
+      if (k < 2 || (w & 1)) {
+        const LeftTf32<3> a = left_of<C>(to, i, 32 + 8 * k);
+#pragma unroll
+        for (int n = 0; n < 4; ++n) times_right<C>(z[n], a, A, 32 + 8 * k, 8 * n);
+      }
+#pragma unroll
+    for (int k = 0; k < 4; ++k)
+      if (k >= 2 || j == 0) {
+        const LeftTf32<3> a(z[k]);
+#pragma unroll
+        for (int n = 0; n < 2; ++n) times_right<C>(y[n], a, to, 8 * k, j + 8 * n);
+      }
+    put(y[0], i, j), put(y[1], i, j + 8);
+    __syncthreads();
+  }
+}
+
+template <typename T, int D, int kSolve>
 __global__ void __launch_bounds__(PrepShape<T, D>::kThreads)
-    prepare_kernel(const DeltaArgs p, float *mats, float *scores, float *gates, int nc) {
+    prepare_kernel(const DeltaArgs p, float *records, int nc) {
   using Sh = PrepShape<T, D>;
+  using Rec = Record<T, kSolve>;
   constexpr int C = Sh::C, kThreads = Sh::kThreads, kRow = Sh::kRow, kMat = Sh::kMat;
   extern __shared__ __align__(16) char raw[];
   T *ks = (T *)raw, *qs = ks + C * kRow;
-  float *A = (float *)(qs + C * kRow);
-  float *hi = A + C * kMat, *lo = hi + C, *beta = lo + C;
+  float *A = (float *)(qs + C * kRow), *inv = A + C * kMat;
+  float *hi = inv + C * kMat, *lo = hi + C, *beta = lo + C;
   double *first = (double *)(beta + 2 * C);
   grid_dep_wait();
   const int h = blockIdx.y, b = blockIdx.z, hk = h / (p.H / p.Hk), tid = threadIdx.x;
@@ -107,76 +211,64 @@ __global__ void __launch_bounds__(PrepShape<T, D>::kThreads)
   }
   cp_async_wait_all();
   __syncthreads();
-  const size_t at = ((size_t)b * p.H + h) * nc + blockIdx.x;
-  float *gt = gates + at * Prepared<C>::kGates;
+  float *rec = records + (((size_t)b * p.H + h) * nc + blockIdx.x) * Rec::kFloats;
+  float *gt = rec + Rec::kGates;
   if (tid < C) {
     if (tid >= 32) G += *first;
     const double G2 = G * 1.4426950408889634;  // powers of two from here on
     hi[tid] = (float)G2, lo[tid] = (float)(G2 - (double)hi[tid]);
-    gt[Prepared<C>::kUp + tid] = expf((float)G);
-    gt[Prepared<C>::kBeta + tid] = beta[tid];
+    gt[Gates<C>::kUp + tid] = expf((float)G);
+    gt[Gates<C>::kBeta + tid] = beta[tid];
     if (tid == C - 1) {
       const DecayFactor f = G < -300. ? DecayFactor{0.f, 0.f} : decay_factor((float)G);
-      gt[Prepared<C>::kWhole] = f.hi, gt[Prepared<C>::kWhole + 1] = f.lo;
+      gt[Gates<C>::kWhole] = f.hi, gt[Gates<C>::kWhole + 1] = f.lo;
     }
   }
   __syncthreads();
   if (tid < C)
-    gt[Prepared<C>::kDown + tid] = exp2f((hi[C - 1] - hi[tid]) + (lo[C - 1] - lo[tid]));
+    gt[Gates<C>::kDown + tid] = exp2f((hi[C - 1] - hi[tid]) + (lo[C - 1] - lo[tid]));
   // the warp's 16 rows of both products, weighted
   const int w = tid / 32, g = (tid & 31) >> 2, t = tid & 3;
   float kk[C / 8][4] = {}, qk[C / 8][4] = {};
   rows_times_rows<D, C>(kk, ks, ks, w);
   rows_times_rows<D, C>(qk, qs, ks, w);
-  float *P = scores + at * C * C;
 #pragma unroll
   for (int m = 0; m < C / 8; ++m) {
     if (m > 2 * w + 1) continue;
+    const int j = 8 * m + 2 * t;
+    const float2 hj = *(const float2 *)(hi + j), lj = *(const float2 *)(lo + j);
+    const float2 bj = *(const float2 *)(beta + j);
 #pragma unroll
     for (int half = 0; half < 2; ++half) {
-      const int i = 16 * w + g + 8 * half, j = 8 * m + 2 * t;
-      float x[2], y[2];
-#pragma unroll
-      for (int e = 0; e < 2; ++e) {
-        const float f = i >= j + e ? ex2_approx((hi[i] - hi[j + e]) + (lo[i] - lo[j + e])) : 0.f;
-        x[e] = i > j + e ? kk[m][2 * half + e] * f * beta[j + e] : 0.f;
-        y[e] = p.scale * qk[m][2 * half + e] * f;
-        if (sizeof(T) == 2) y[e] = __uint_as_float(tf32_of(y[e]));  // as the products read it
-      }
-      *(float2 *)(A + i * kMat + j) = make_float2(x[0], x[1]);
-      *(float2 *)(P + i * C + j) = make_float2(y[0], y[1]);
+      const int i = 16 * w + g + 8 * half;
+      const float f0 = i >= j ? ex2_approx((hi[i] - hj.x) + (lo[i] - lj.x)) : 0.f;
+      const float f1 = i >= j + 1 ? ex2_approx((hi[i] - hj.y) + (lo[i] - lj.y)) : 0.f;
+      *(float2 *)(A + i * kMat + j) =
+          make_float2(i > j ? kk[m][2 * half] * f0 * bj.x : 0.f,
+                      i > j + 1 ? kk[m][2 * half + 1] * f1 * bj.y : 0.f);
+      if (2 * w + half >= m)
+        Rec::P::store(rec + Rec::kP, 2 * w + half, m, p.scale * qk[m][2 * half] * f0,
+                      p.scale * qk[m][2 * half + 1] * f1);
     }
   }
   __syncthreads();
-  // M - 1 by forward substitution, a column a thread: x_i = [i = j] - sum_m A_im x_m.
-  float x[C];
-  float *M = mats + at * C * C;
-  if (tid < C) {
-#pragma unroll
-    for (int i = 0; i < C; ++i) {
-      float s = i == tid ? 1.f : 0.f, s1 = 0.f;
-#pragma unroll
-      for (int m = 0; m < i; m += 4) {
-        const float4 a = *(const float4 *)(A + i * kMat + m);
-        s = fmaf(-a.x, x[m], s);
-        if (m + 1 < i) s1 = fmaf(-a.y, x[m + 1], s1);
-        if (m + 2 < i) s = fmaf(-a.z, x[m + 2], s);
-        if (m + 3 < i) s1 = fmaf(-a.w, x[m + 3], s1);
-      }
-      x[i] = s + s1;
-      M[i * C + tid] = x[i] - (i == tid ? 1.f : 0.f);
+  invert<C>(inv, A, w);
+  // M - 1, whose diagonal is 0: the identity's part of a product needs no rounding
+  for (int m = w; m < C / 8; m += Sh::kWarps)
+    for (int j = 0; j <= m; ++j) {
+      const float2 v = *(const float2 *)(inv + (8 * m + g) * kMat + 8 * j + 2 * t);
+      Rec::M::store(rec + Rec::kM, m, j, j == m && g == 2 * t ? 0.f : v.x,
+                    j == m && g == 2 * t + 1 ? 0.f : v.y);
     }
-  }
 }
 
 // --------------------------------------------------------------- second launch
-template <typename T, int D>
+template <typename T, int D, int kSolve>
 struct ScanShape {
   static constexpr int C = kChunkOf<T>, kWarps = D / 16, kThreads = kWarps * 32;
   static constexpr int kRow = pad_row<T>(D);
-  static constexpr int kTile = C * kRow * sizeof(T);             // bytes of k, q or v
-  static constexpr int kMatBytes = C * mat_row(C) * 4;
-  static constexpr int kStage = 3 * kTile + 2 * kMatBytes + Prepared<C>::kGates * 4;
+  static constexpr int kTile = C * kRow * (int)sizeof(T);        // bytes of k, q or v
+  static constexpr int kStage = 3 * kTile + Record<T, kSolve>::kFloats * 4;
   static constexpr int kBytes = 2 * kStage;
 };
 
@@ -226,15 +318,16 @@ template <int kTerms, int D, int C>
 __device__ __forceinline__ void state_update(float (&S)[D / 8][4], float hi, float lo,
                                              const float (&w)[C / 8][4], const __nv_bfloat16 *ks) {
   constexpr int kRow = pad_row<__nv_bfloat16>(D);
+  static_assert(C == 64, "four left operands");
+  const LeftBf16<kTerms> a[4] = {{w[0], w[1]}, {w[2], w[3]}, {w[4], w[5]}, {w[6], w[7]}};
 #pragma unroll
   for (int d = 0; d < D / 16; ++d) {
     float x[2][4] = {};
 #pragma unroll
     for (int j = 0; j < C / 16; ++j) {
-      const LeftBf16<kTerms> a(w[2 * j], w[2 * j + 1]);
       const PairBf16 k = by_channel<kRow>(ks, 16 * j, 16 * d);
-      a.times(x[0], k.b[0][0], k.b[0][1]);
-      a.times(x[1], k.b[1][0], k.b[1][1]);
+      a[j].times(x[0], k.b[0][0], k.b[0][1]);
+      a[j].times(x[1], k.b[1][0], k.b[1][1]);
     }
 #pragma unroll
     for (int i = 0; i < 2; ++i)
@@ -307,11 +400,11 @@ __device__ __forceinline__ void store_tile(float *o, size_t stride, const float 
 // kTerms: bf16 numbers that stand for a value of the state where it meets a key or takes a
 // write (fp32: 3 tf32 products); kSolve: terms of the product with M.
 template <typename T, int D, int kTerms, int kSolve>
-__global__ void __launch_bounds__(ScanShape<T, D>::kThreads)
-    scan_kernel(const DeltaArgs p, const float *mats, const float *scores, const float *gates,
-                int nc) {
-  using Sh = ScanShape<T, D>;
-  constexpr int C = Sh::C, kThreads = Sh::kThreads, kRow = Sh::kRow, kMat = mat_row(C);
+__global__ void __launch_bounds__(ScanShape<T, D, kSolve>::kThreads)
+    scan_kernel(const DeltaArgs p, const float *records, int nc) {
+  using Sh = ScanShape<T, D, kSolve>;
+  using Rec = Record<T, kSolve>;
+  constexpr int C = Sh::C, kThreads = Sh::kThreads, kRow = Sh::kRow;
   constexpr int kOut = sizeof(T) == 2 ? 1 : 3;  // terms of the product with P
   extern __shared__ __align__(16) char raw[];
   grid_dep_wait();
@@ -329,14 +422,11 @@ __global__ void __launch_bounds__(ScanShape<T, D>::kThreads)
     char *s = raw + (c & 1) * Sh::kStage;
     const long long t0 = (long long)c * C;
     const int n = min(C, L - c * C);
-    const size_t at = bh * nc + c;
     load_rows<T, C, D, kThreads>((T *)s, kg + t0 * p.sk[1], p.sk[1], n);
     load_rows<T, C, D, kThreads>((T *)(s + Sh::kTile), qg + t0 * p.sq[1], p.sq[1], n);
     load_rows<T, C, D, kThreads>((T *)(s + 2 * Sh::kTile), vg + t0 * p.sv[1], p.sv[1], n);
-    load_lower<C, kThreads>((float *)(s + 3 * Sh::kTile), mats + at * C * C);
-    load_lower<C, kThreads>((float *)(s + 3 * Sh::kTile + Sh::kMatBytes), scores + at * C * C);
-    load_flat<Prepared<C>::kGates, kThreads>((float *)(s + 3 * Sh::kTile + 2 * Sh::kMatBytes),
-                                             gates + at * Prepared<C>::kGates);
+    load_flat<Rec::kFloats, kThreads>((float *)(s + 3 * Sh::kTile),
+                                      records + (bh * nc + c) * Rec::kFloats);
   };
   float S[D / 8][4];  // rows: columns e0 + g, + 8 of the state; columns: its rows
 #pragma unroll
@@ -354,7 +444,7 @@ __global__ void __launch_bounds__(ScanShape<T, D>::kThreads)
     cp_async_commit();
     const char *s = raw + (c & 1) * Sh::kStage;
     const T *ks = (const T *)s, *qs = (const T *)(s + Sh::kTile), *vs = (const T *)(s + 2 * Sh::kTile);
-    const float *M = (const float *)(s + 3 * Sh::kTile), *P = M + C * kMat, *gt = P + C * kMat;
+    const float *rec = (const float *)(s + 3 * Sh::kTile), *gt = rec + Rec::kGates;
     const int n = min(C, L - c * C);
     float r[C / 8][4] = {}, o[C / 8][4] = {};
     state_products<kTerms, D, C>(S, ks, qs, r, o);
@@ -364,7 +454,7 @@ __global__ void __launch_bounds__(ScanShape<T, D>::kThreads)
       values_of<kRow>(v[0], v[1], vs, m, e0);
 #pragma unroll
       for (int i = 0; i < 2; ++i) {
-        const float2 up = *(const float2 *)(gt + Prepared<C>::kUp + 16 * m + 8 * i + 2 * t);
+        const float2 up = *(const float2 *)(gt + Gates<C>::kUp + 16 * m + 8 * i + 2 * t);
         float(&x)[4] = r[2 * m + i], (&y)[4] = o[2 * m + i];
         x[0] = fmaf(-up.x, x[0], v[i][0]), x[1] = fmaf(-up.y, x[1], v[i][1]);
         x[2] = fmaf(-up.x, x[2], v[i][2]), x[3] = fmaf(-up.y, x[3], v[i][3]);
@@ -383,10 +473,7 @@ __global__ void __launch_bounds__(ScanShape<T, D>::kThreads)
         const LeftTf32<kSolve> a(r[j]);
 #pragma unroll
         for (int m = 0; m < kHalf; ++m)
-          if (half * kHalf + m >= j) {
-            const float2 f = *(const float2 *)(M + (8 * (half * kHalf + m) + g) * kMat + 8 * j + 2 * t);
-            a.times(x[m], f.x, f.y);
-          }
+          if (half * kHalf + m >= j) a.times(x[m], Rec::M::load(rec + Rec::kM, half * kHalf + m, j));
       }
 #pragma unroll
       for (int m = 0; m < kHalf; ++m)
@@ -396,19 +483,16 @@ __global__ void __launch_bounds__(ScanShape<T, D>::kThreads)
     // u, and the results
 #pragma unroll
     for (int j = 0; j < C / 8; ++j) {
-      const float2 be = *(const float2 *)(gt + Prepared<C>::kBeta + 8 * j + 2 * t);
+      const float2 be = *(const float2 *)(gt + Gates<C>::kBeta + 8 * j + 2 * t);
       r[j][0] *= be.x, r[j][1] *= be.y, r[j][2] *= be.x, r[j][3] *= be.y;
       const LeftTf32<kOut> a(r[j]);
 #pragma unroll
-      for (int m = j; m < C / 8; ++m) {
-        const float2 f = *(const float2 *)(P + (8 * m + g) * kMat + 8 * j + 2 * t);
-        a.times(o[m], f.x, f.y);
-      }
+      for (int m = j; m < C / 8; ++m) a.times(o[m], Rec::P::load(rec + Rec::kP, m, j));
       store_tile(og + (size_t)c * C * orow, orow, o[j], 8 * j, n);  // no later u meets it
-      const float2 dn = *(const float2 *)(gt + Prepared<C>::kDown + 8 * j + 2 * t);
+      const float2 dn = *(const float2 *)(gt + Gates<C>::kDown + 8 * j + 2 * t);
       r[j][0] *= dn.x, r[j][1] *= dn.y, r[j][2] *= dn.x, r[j][3] *= dn.y;
     }
-    state_update<kTerms, D, C>(S, gt[Prepared<C>::kWhole], gt[Prepared<C>::kWhole + 1], r, ks);
+    state_update<kTerms, D, C>(S, gt[Gates<C>::kWhole], gt[Gates<C>::kWhole + 1], r, ks);
   }
   if (p.fin) {
 #pragma unroll
@@ -422,15 +506,15 @@ __global__ void __launch_bounds__(ScanShape<T, D>::kThreads)
 template <typename T>
 int chunks_of(const DeltaArgs &a) { return (a.N + kChunkOf<T> - 1) / kChunkOf<T>; }
 
+// Terms of the product with M: bf16 results alone need one (2^-11 of what M adds to a miss).
+bool exact_state(const DeltaArgs &a) { return a.dtype == GBLA_FP32 || a.fin; }
+
 template <typename T, int D, int kTerms, int kSolve>
 cudaError_t launch(const DeltaArgs &a, float *scratch, cudaStream_t st) {
   using Pr = PrepShape<T, D>;
-  using Sc = ScanShape<T, D>;
-  constexpr int C = Pr::C;
+  using Sc = ScanShape<T, D, kSolve>;
   const int nc = chunks_of<T>(a);
-  const size_t all = (size_t)a.B * a.H * nc;
-  float *mats = scratch, *scores = mats + all * C * C, *gates = scores + all * C * C;
-  const auto prep = prepare_kernel<T, D>;
+  const auto prep = prepare_kernel<T, D, kSolve>;
   const auto scan = scan_kernel<T, D, kTerms, kSolve>;
   cudaError_t e;
   if ((e = cudaFuncSetAttribute(prep, cudaFuncAttributeMaxDynamicSharedMemorySize, Pr::kBytes)) !=
@@ -440,37 +524,36 @@ cudaError_t launch(const DeltaArgs &a, float *scratch, cudaStream_t st) {
       cudaSuccess)
     return e;
   count_launch();
-  if ((e = launch_pdl(prep, dim3(nc, a.H, a.B), dim3(Pr::kThreads), Pr::kBytes, st, a, mats, scores,
-                      gates, nc)) != cudaSuccess)
+  if ((e = launch_pdl(prep, dim3(nc, a.H, a.B), dim3(Pr::kThreads), Pr::kBytes, st, a, scratch,
+                      nc)) != cudaSuccess)
     return e;
   count_launch();
   return launch_pdl(scan, dim3(a.H, a.B), dim3(Sc::kThreads), Sc::kBytes, st, a,
-                    (const float *)mats, (const float *)scores, (const float *)gates, nc);
+                    (const float *)scratch, nc);
 }
 
-template <typename T, int D>
-cudaError_t launch_terms(const DeltaArgs &a, float *scratch, cudaStream_t st) {
-  if (sizeof(T) == 4 || a.fin) return launch<T, D, 3, 3>(a, scratch, st);
-  return launch<T, D, 2, 3>(a, scratch, st);
+template <int D>
+cudaError_t launch_d(const DeltaArgs &a, float *scratch, cudaStream_t st) {
+  if (a.dtype == GBLA_FP32) return launch<float, D, 3, 3>(a, scratch, st);
+  if (exact_state(a)) return launch<__nv_bfloat16, D, 3, 3>(a, scratch, st);
+  return launch<__nv_bfloat16, D, 2, 1>(a, scratch, st);
 }
 
 }  // namespace
 }  // namespace delta
 
 size_t delta_forward_floats(const DeltaArgs &a) {
-  const int C = a.dtype == GBLA_FP32 ? delta::kChunkOf<float> : delta::kChunkOf<__nv_bfloat16>;
-  return (size_t)a.B * a.H * ((a.N + C - 1) / C) * (2 * C * C + 4 * C);
+  using namespace delta;
+  const size_t bh = (size_t)a.B * a.H;
+  if (a.dtype == GBLA_FP32) return bh * chunks_of<float>(a) * Record<float, 3>::kFloats;
+  return bh * chunks_of<__nv_bfloat16>(a) *
+         (exact_state(a) ? Record<__nv_bfloat16, 3>::kFloats : Record<__nv_bfloat16, 1>::kFloats);
 }
 
 cudaError_t delta_forward(const DeltaArgs &a, float *scratch, cudaStream_t st) {
-  if (a.dtype == GBLA_FP32) {
-    if (a.D == 32) return delta::launch_terms<float, 32>(a, scratch, st);
-    if (a.D == 64) return delta::launch_terms<float, 64>(a, scratch, st);
-    return delta::launch_terms<float, 128>(a, scratch, st);
-  }
-  if (a.D == 32) return delta::launch_terms<__nv_bfloat16, 32>(a, scratch, st);
-  if (a.D == 64) return delta::launch_terms<__nv_bfloat16, 64>(a, scratch, st);
-  return delta::launch_terms<__nv_bfloat16, 128>(a, scratch, st);
+  if (a.D == 32) return delta::launch_d<32>(a, scratch, st);
+  if (a.D == 64) return delta::launch_d<64>(a, scratch, st);
+  return delta::launch_d<128>(a, scratch, st);
 }
 
 }  // namespace gbla

@@ -3,6 +3,8 @@
 // the layout of what a chunk prepares.
 #pragma once
 
+#include <type_traits>
+
 #include "gbla_decay.cuh"
 #include "gbla_internal.cuh"
 #include "gbla_sm100.cuh"
@@ -19,35 +21,33 @@ using namespace sm100;
 // columns 2t and 2t + 1 in the places of t and t + 4): chains of products stay in registers.
 __device__ __forceinline__ void mma_bf16(float (&c)[4], const uint32_t (&a)[4], uint32_t b0,
                                          uint32_t b1) {
-  asm volatile(
-      "mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, "
+  asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, "
       "{%8,%9}, {%0,%1,%2,%3};"
       : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
       : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
 __device__ __forceinline__ void mma_tf32(float (&c)[4], const uint32_t (&a)[4], uint32_t b0,
                                          uint32_t b1) {
-  asm volatile(
-      "mma.sync.aligned.m16n8k8.row.col.f32.tf32.tf32.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, "
+  asm("mma.sync.aligned.m16n8k8.row.col.f32.tf32.tf32.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, "
       "{%8,%9}, {%0,%1,%2,%3};"
       : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
       : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
+// (Tiles that these read are written by asynchronous copies alone; volatile keeps the loads
+// behind the barrier after those.)
 __device__ __forceinline__ void ldmatrix4(uint32_t (&r)[4], uint32_t addr) {
   asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0,%1,%2,%3}, [%4];"
                : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3])
-               : "r"(addr)
-               : "memory");
+               : "r"(addr));
 }
 __device__ __forceinline__ void ldmatrix4_t(uint32_t (&r)[4], uint32_t addr) {
   asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0,%1,%2,%3}, [%4];"
                : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3])
-               : "r"(addr)
-               : "memory");
+               : "r"(addr));
 }
 __device__ __forceinline__ uint32_t transpose8(uint32_t v) {
   uint32_t r;
-  asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(r) : "r"(v));
+  asm("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(r) : "r"(v));
   return r;
 }
 // fp32 rounded to the 11 significant bits that tf32 products read.
@@ -75,19 +75,25 @@ struct LeftTf32 {
       else tf32_split(x[i], hi[i], lo[i]);
     }
   }
-  // b: the right operand's values at (row 2t, 2t + 1) of this lane's column; with one term
-  // they have 11 bits already.
+  // The right operand's values at rows 2t and 2t + 1 of this lane's column: as they are,
   __device__ __forceinline__ void times(float (&c)[4], float b0, float b1) const {
     if (kTerms == 1) {
-      mma_tf32(c, hi, __float_as_uint(b0), __float_as_uint(b1));
+      mma_tf32(c, hi, tf32_of(b0), tf32_of(b1));
       return;
     }
     uint32_t h0, l0, h1, l1;
     tf32_split(b0, h0, l0);
     tf32_split(b1, h1, l1);
-    mma_tf32(c, lo, h0, h1);
-    mma_tf32(c, hi, l0, l1);
-    mma_tf32(c, hi, h0, h1);
+    times(c, make_uint4(h0, h1, l0, l1));
+  }
+  // or rounded or split before.
+  __device__ __forceinline__ void times(float (&c)[4], const uint2 &b) const {
+    mma_tf32(c, hi, b.x, b.y);
+  }
+  __device__ __forceinline__ void times(float (&c)[4], const uint4 &b) const {
+    mma_tf32(c, lo, b.x, b.y);
+    mma_tf32(c, hi, b.z, b.w);
+    mma_tf32(c, hi, b.x, b.y);
   }
 };
 // The left operand of bf16 products made of two result tiles, as kTerms bf16 numbers each
@@ -128,10 +134,7 @@ constexpr int kChunkOf = sizeof(T) == 2 ? 64 : 32;
 // Elements of a padded row of kCols values: rows 4 banks (bf16: ldmatrix) or 8 (fp32: pairs of
 // two) apart.
 template <typename T>
-constexpr int pad_row(int cols) { return cols + (sizeof(T) == 2 ? 8 : 8); }
-// Floats of a padded row of a C x C matrix.
-constexpr int mat_row(int C) { return C + 8; }
-
+constexpr int pad_row(int cols) { return cols + 8; }
 // kRows tokens of kCols values into padded rows; rows from n on become zeros.
 template <typename T, int kRows, int kCols, int kThreads>
 __device__ __forceinline__ void load_rows(T *to, const T *from, long long stride, int n) {
@@ -140,14 +143,6 @@ __device__ __forceinline__ void load_rows(T *to, const T *from, long long stride
     const int r = i / kPer, c = i % kPer * kVec;
     cp_async_or_zero(smem_u32(to + r * pad_row<T>(kCols) + c), from + (r < n ? r * stride + c : 0),
                      r < n);
-  }
-}
-// The blocks on and below the diagonal of a C x C fp32 matrix into padded rows.
-template <int C, int kThreads>
-__device__ __forceinline__ void load_lower(float *to, const float *from) {
-  for (int i = threadIdx.x; i < C * C / 4; i += kThreads) {
-    const int r = i / (C / 4), c = i % (C / 4) * 4;
-    if (c < (r / 8 + 1) * 8) cp_async_16(smem_u32(to + r * mat_row(C) + c), from + r * C + c);
   }
 }
 template <int kFloats, int kThreads>
@@ -180,12 +175,35 @@ __device__ __forceinline__ PairBf16 by_channel(const __nv_bfloat16 *tile, int to
 }
 
 // ------------------------------------------------------------- what a chunk prepares
-// For every (batch, head, chunk): the matrix of the chunk's own overlaps, inverted
-// (below), the weighted scores, and the gates' powers.
+// Lower triangular C x C matrices, as the right operands of tf32 products: tiles of 8 x 8 on
+// and below the diagonal, row by row of tiles, each with a uint2 (one term: rounded) or uint4
+// (three: two hi, two lo) a lane, so that a warp's loads lie side by side.
+template <int C, int kTerms>
+struct Tiles {
+  static constexpr int kLane = kTerms == 1 ? 2 : 4;  // floats
+  static constexpr int kTiles = (C / 8) * (C / 8 + 1) / 2, kFloats = kTiles * 32 * kLane;
+  using Word = std::conditional_t<kTerms == 1, uint2, uint4>;
+  static __device__ __forceinline__ int at(int m, int j) {
+    return (m * (m + 1) / 2 + j) * 32 + (threadIdx.x & 31);
+  }
+  static __device__ __forceinline__ Word load(const float *base, int m, int j) {
+    return ((const Word *)base)[at(m, j)];
+  }
+  static __device__ __forceinline__ void store(float *base, int m, int j, float b0, float b1) {
+    if constexpr (kTerms == 1) {
+      ((uint2 *)base)[at(m, j)] = make_uint2(tf32_of(b0), tf32_of(b1));
+    } else {
+      uint4 v;
+      tf32_split(b0, v.x, v.z);
+      tf32_split(b1, v.y, v.w);
+      ((uint4 *)base)[at(m, j)] = v;
+    }
+  }
+};
+// Powers of a chunk's gates.
 template <int C>
-struct Prepared {
-  static constexpr int kUp = 0, kDown = C, kBeta = 2 * C, kWhole = 3 * C;  // floats of `gates`
-  static constexpr int kGates = 4 * C;
+struct Gates {
+  static constexpr int kUp = 0, kDown = C, kBeta = 2 * C, kWhole = 3 * C, kFloats = 4 * C;
 };
 
 }  // namespace delta

@@ -562,6 +562,22 @@ gbla_status gbla_delta_attention(const void *q, const void *k, const void *v,
                                  gbla_stream_t stream);
 
 /*
+ * gbla_delta_attention_backward -- gradients of sum(d_o * o) + sum(dstate_out * state_out)
+ * with respect to q, k, v, the gates and state_in.  Inputs as gbla_delta_attention plus d_o
+ * [B, N, H, D] dtype and dstate_out [B, H, D, D] fp32 (NULL: zeros).  Outputs, contiguous:
+ * dq, dk [B, N, Hk, D] (sums over the value heads that read a key head, in fp32), dv
+ * [B, N, H, D], dlog_decay, dbeta [B, N, H] dtype (rows t >= L_b written as 0; where
+ * log_decay is -inf its gradient is 0) and dstate_in [B, H, D, D] fp32 or NULL.  Nothing is
+ * kept from a forward call.
+ */
+gbla_status gbla_delta_attention_backward(
+    const void *q, const void *k, const void *v, const void *log_decay, const void *beta,
+    const int32_t *seq_lens, const int64_t *strides, const float *state_in, const void *d_o,
+    const float *dstate_out, void *dq, void *dk, void *dv, void *dlog_decay, void *dbeta,
+    float *dstate_in, int B, int N, int H, int Hk, int D, float scale, gbla_dtype dtype,
+    gbla_stream_t stream);
+
+/*
  * gbla_delta_attention_step -- the same recurrence for one token of each sequence, on a
  * pool of states updated in place at slots[b], as gbla_decay_attention_step.
  *   q, k [B, Hk, D], v [B, H, D], log_decay, beta [B, H] dtype; strides NULL or a host

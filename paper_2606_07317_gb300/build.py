@@ -22,7 +22,7 @@ OBJ_DIR = os.path.join(PKG, "_build")
 
 SOURCES = ["gbla_api.cu", "gbla_simt.cu", "gbla_tc.cu", "gbla_bwd.cu", "gbla_bwd_tc.cu",
            "gbla_project.cu", "gbla_static_scratch.cu", "gbla_sa.cu", "gbla_seqsplit.cu",
-           "gbla_rotate.cu", "gbla_decay.cu", "gbla_decay_tc.cu", "gbla_delta.cu", "gbla_delta_chunk.cu",
+           "gbla_rotate.cu", "gbla_decay.cu", "gbla_decay_tc.cu", "gbla_delta.cu", "gbla_delta_chunk.cu", "gbla_delta_bwd.cu",
            "gbla_logprob.cu"]
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
 

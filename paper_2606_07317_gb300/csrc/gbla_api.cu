@@ -1235,6 +1235,38 @@ gbla_status gbla_delta_attention(const void *q, const void *k, const void *v,
   return from_cuda(delta_forward(a, (float *)ws.ptr, st));
 }
 
+gbla_status gbla_delta_attention_backward(
+    const void *q, const void *k, const void *v, const void *log_decay, const void *beta,
+    const int32_t *seq_lens, const int64_t *strides, const float *state_in, const void *d_o,
+    const float *dstate_out, void *dq, void *dk, void *dv, void *dlog_decay, void *dbeta,
+    float *dstate_in, int B, int N, int H, int Hk, int D, float scale, gbla_dtype dtype,
+    gbla_stream_t stream) {
+  DeltaBackArgs p = {};
+  DeltaViews w;
+  bool empty = false;
+  gbla_status s = check_delta(&p.f, &w, q, k, v, log_decay, beta, seq_lens, strides, state_in, B,
+                              N, H, Hk, D, scale, dtype, &empty);
+  if (s != GBLA_OK) return s;
+  cudaStream_t st = (cudaStream_t)stream;
+  const size_t sb = sizeof(float) * D * D * (size_t)B * H;
+  if (empty) return pass_state(dstate_out, dstate_in, sb, st);
+  if ((s = check_ptrs({d_o, dq, dk, dv, dlog_decay, dbeta})) != GBLA_OK) return s;
+  if (!aligned_or_null({dstate_out, dstate_in})) return GBLA_ERR_INVALID_ARG;
+  const size_t tok = (size_t)B * N * elem_bytes(dtype);
+  if (any_overlap({range_of(dq, tok * Hk * D), range_of(dk, tok * Hk * D), range_of(dv, tok * H * D),
+                   range_of(dlog_decay, tok * H), range_of(dbeta, tok * H),
+                   range_of(dstate_in, dstate_in ? sb : 0)},
+                  {w.in[0], w.in[1], w.in[2], w.in[3], w.in[4], w.in[5], w.in[6],
+                   range_of(d_o, tok * H * D), range_of(dstate_out, dstate_out ? sb : 0)}))
+    return GBLA_ERR_INVALID_ARG;
+  p.d_o = d_o, p.dstate = dstate_out;
+  p.dq = dq, p.dk = dk, p.dv = dv, p.dlog_decay = dlog_decay, p.dbeta = dbeta;
+  p.dstate_in = dstate_in;
+  Scratch ws;
+  if ((s = ws.alloc(sizeof(float) * delta_backward_floats(p), st)) != GBLA_OK) return s;
+  return from_cuda(delta_backward(p, (float *)ws.ptr, st));
+}
+
 gbla_status gbla_delta_attention_step(const void *q, const void *k, const void *v,
                                       const void *log_decay, const void *beta,
                                       const int32_t *slots, const int64_t *strides, float *state,

@@ -1,0 +1,557 @@
+// Backward pass of attention by the gated delta rule, in chunks of C tokens.
+//
+// With the notation of the forward pass (S before the chunk, A the gradient of the state
+// after it, m the misses, u = beta m, T = (1 + beta X)^-1), d the gradients of the results:
+//   du_j  = sum_i P_ij d_i + e^(G_C - G_j) A^T k_j,   w = T^T du,   dv = beta w,
+//   dbeta_j = w_j . m_j,
+//   A'    = e^(G_C) A + sum_i e^(G_i) (scale q_i d_i^T - k_i dv_i^T)   (before the chunk),
+// and with dP_ij = scale e^(G_i - G_j) d_i . u_j (j <= i), E_ij = -e^(G_i - G_j) dv_i . u_j (j < i)
+//   dq_i = scale e^(G_i) S d_i + sum_j dP_ij k_j,
+//   dk_i = e^(G_C - G_i) A u_i - e^(G_i) S dv_i + sum_j E_ij k_j + sum_j (dP_ji q_j + E_ji k_j).
+// Every product with a power e^(+-G_i) gives G_i its share, +- itself; the gradient of a token's
+// log decay is the sum of those of G_i from it to the chunk's end.
+//
+// Four launches: what every chunk can prepare by itself, the misses and states from the first
+// chunk on, w, dv and A from the last one back, and the rest of each chunk's gradients.
+#include <math.h>
+
+#include "gbla_delta_mma.cuh"
+
+namespace gbla {
+namespace delta {
+namespace {
+
+// ------------------------------------------------------------- from the last chunk back
+template <typename T, int D, int kSolve>
+struct ReverseShape {
+  using Rec = Record<T, kSolve, true>;
+  static constexpr int C = kChunkOf<T>, kWarps = D / 16, kThreads = kWarps * 32;
+  static constexpr int kRow = pad_row<T>(D);
+  static constexpr int kTile = C * kRow * (int)sizeof(T);          // bytes of k, q or d
+  static constexpr int kStage = 3 * kTile + (Rec::kFloats - Rec::kP) * 4;  // M is not read
+  static constexpr int kBytes = 2 * kStage;
+};
+
+template <typename T, int D, int kTerms, int kSolve>
+__global__ void __launch_bounds__(ReverseShape<T, D, kSolve>::kThreads)
+    reverse_kernel(const DeltaBackArgs p, const float *records, float *after, float *weights, int nc) {
+  using Sh = ReverseShape<T, D, kSolve>;
+  using Rec = typename Sh::Rec;
+  constexpr int C = Sh::C, kThreads = Sh::kThreads, kRow = Sh::kRow;
+  extern __shared__ __align__(16) char raw[];
+  grid_dep_wait();
+  const DeltaArgs &f = p.f;
+  const int h = blockIdx.x, b = blockIdx.y, hk = h / (f.H / f.Hk), tid = threadIdx.x;
+  const int t = tid & 3, e0 = tid / 32 * 16;
+  const int L = f.seq_lens ? min(max(__ldg(f.seq_lens + b), 0), f.N) : f.N;
+  const size_t bh = (size_t)b * f.H + h;
+  const T *kg = (const T *)f.k + b * f.sk[0] + (long long)hk * D;
+  const T *qg = (const T *)f.q + b * f.sq[0] + (long long)hk * D;
+  const size_t orow = (size_t)f.H * D;
+  const T *dg = (const T *)p.d_o + ((size_t)b * f.N * f.H + h) * D;
+  T *vg = (T *)p.dv + ((size_t)b * f.N * f.H + h) * D + e0;
+  const int chunks = (L + C - 1) / C;
+  auto load = [&](int c) {
+    char *s = raw + (c & 1) * Sh::kStage;
+    const long long t0 = (long long)c * C;
+    const int n = min(C, L - c * C);
+    load_rows<T, C, D, kThreads>((T *)s, kg + t0 * f.sk[1], f.sk[1], n);
+    load_rows<T, C, D, kThreads>((T *)(s + Sh::kTile), qg + t0 * f.sq[1], f.sq[1], n);
+    load_rows<T, C, D, kThreads>((T *)(s + 2 * Sh::kTile), dg + t0 * orow, (long long)orow, n);
+    load_flat<Rec::kFloats - Rec::kP, kThreads>((float *)(s + 3 * Sh::kTile),
+                                                records + (bh * nc + c) * Rec::kFloats + Rec::kP);
+  };
+  float A[D / 8][4];
+  load_state<D>(A, p.dstate ? p.dstate + bh * D * D : nullptr, e0);
+  if (chunks > 0) load(chunks - 1);
+  cp_async_commit();
+  for (int c = chunks - 1; c >= 0; --c) {
+    cp_async_wait_all();
+    __syncthreads();
+    if (c > 0) load(c - 1);
+    cp_async_commit();
+    const char *s = raw + (c & 1) * Sh::kStage;
+    const T *ks = (const T *)s, *qs = (const T *)(s + Sh::kTile), *ds = (const T *)(s + 2 * Sh::kTile);
+    const float *P = (const float *)(s + 3 * Sh::kTile), *Tm = P + (Rec::kT - Rec::kP);
+    const float *gt = P + (Rec::kGates - Rec::kP);
+    const int n = min(C, L - c * C);
+    store_state<D>(after + (bh * nc + c) * D * D, A, e0);
+    float r[C / 8][4] = {};
+    state_products<kTerms, D, C, false>(A, ks, ks, r, r);
+    {
+      float x[C / 8][4] = {};
+#pragma unroll
+      for (int m = 0; m < C / 16; ++m) {
+        float d[2][4];
+        values_of<kRow>(d[0], d[1], ds, m, e0);
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          const LeftTf32<kSolve> a(d[i]);
+#pragma unroll
+          for (int j = 0; j <= 2 * m + i; ++j) a.times(x[j], Rec::P::load(P, 2 * m + i, j));
+        }
+      }
+#pragma unroll
+      for (int j = 0; j < C / 8; ++j) {
+        const float2 dn = *(const float2 *)(gt + Gates<C>::kDown + 8 * j + 2 * t);
+        r[j][0] = fmaf(dn.x, r[j][0], x[j][0]), r[j][1] = fmaf(dn.y, r[j][1], x[j][1]);
+        r[j][2] = fmaf(dn.x, r[j][2], x[j][2]), r[j][3] = fmaf(dn.y, r[j][3], x[j][3]);
+      }
+    }
+    // r += (T - 1)^T r: the earlier half of the tokens first, which needs the later ones as
+    // they are
+#pragma unroll
+    for (int half = 0; half < 2; ++half) {
+      constexpr int kHalf = C / 16;
+      float x[kHalf][4] = {};
+#pragma unroll
+      for (int i = half * kHalf; i < C / 8; ++i) {
+        const LeftTf32<kSolve> a(r[i]);
+#pragma unroll
+        for (int j = 0; j < kHalf; ++j)
+          if (half * kHalf + j <= i) a.times(x[j], Rec::M::load(Tm, i, half * kHalf + j));
+      }
+#pragma unroll
+      for (int j = 0; j < kHalf; ++j)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) r[half * kHalf + j][i] += x[j][i];
+    }
+#pragma unroll
+    for (int j = 0; j < C / 8; ++j) {
+      store_tile(weights + (bh * nc + c) * C * D + e0, D, r[j], 8 * j, C);
+      const float2 be = *(const float2 *)(gt + Gates<C>::kBeta + 8 * j + 2 * t);
+      r[j][0] *= be.x, r[j][1] *= be.y, r[j][2] *= be.x, r[j][3] *= be.y;
+      store_tile(vg + (size_t)c * C * orow, orow, r[j], 8 * j, n);
+      const float2 up = *(const float2 *)(gt + Gates<C>::kUp + 8 * j + 2 * t);
+      r[j][0] *= -up.x, r[j][1] *= -up.y, r[j][2] *= -up.x, r[j][3] *= -up.y;
+    }
+    state_update<kTerms, D, C>(A, gt[Gates<C>::kWhole], gt[Gates<C>::kWhole + 1], r, ks);
+#pragma unroll
+    for (int m = 0; m < C / 16; ++m) {
+      values_of<kRow>(r[2 * m], r[2 * m + 1], ds, m, e0);
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        const float2 up = *(const float2 *)(gt + Gates<C>::kUp + 16 * m + 8 * i + 2 * t);
+        const float ux = up.x * f.scale, uy = up.y * f.scale;
+        float(&x)[4] = r[2 * m + i];
+        x[0] *= ux, x[1] *= uy, x[2] *= ux, x[3] *= uy;
+      }
+    }
+    state_update<kTerms, D, C>(A, 1.f, 0.f, r, qs);
+  }
+  if (p.dstate_in) store_state<D>(p.dstate_in + bh * D * D, A, e0);
+}
+
+// ------------------------------------------------------------- the chunks' own gradients
+// One block a (chunk, head, batch), a warp for each 16 of its tokens; results in registers,
+// 16 x D of dq and of dk a warp.
+template <typename T, int D>
+struct GradShape {
+  static constexpr int C = kChunkOf<T>, kWarps = C / 16, kThreads = kWarps * 32;
+  static constexpr int kRow = pad_row<T>(D), kWide = D + 8, kMat = C + 4;
+  static constexpr int kTile = C * kRow * (int)sizeof(T);
+  static constexpr int kStateFloats = D * kWide > 2 * C * kMat ? D * kWide : 2 * C * kMat;
+  static constexpr int kSmall = Gates<C>::kFloats + 2 * C + kWarps * C + 4 + kWarps;
+  static constexpr int kBytes = 3 * kTile + (2 * C * kWide + kStateFloats + kSmall) * 4;
+};
+
+// 16 rows from i on at columns k .. k + 7 of a tile, as the left operand of tf32 products; times
+// the rows' factors.
+template <int kTerms, int kRow, typename T>
+__device__ __forceinline__ LeftTf32<kTerms> left_rows(const T *tile, int i, int k, float fx = 1.f,
+                                                      float fy = 1.f) {
+  const int g = (threadIdx.x & 31) >> 2, t = threadIdx.x & 3;
+  const T *x = tile + (i + g) * kRow + k + 2 * t, *y = x + 8 * kRow;
+  const float c[4] = {fx * to_f(x[0]), fx * to_f(x[1]), fy * to_f(y[0]), fy * to_f(y[1])};
+  return LeftTf32<kTerms>(c);
+}
+// x += (16 x 16 coefficients a, b) times rows i .. i + 15 of a raw tile.
+template <int D>
+__device__ __forceinline__ void add_rows(float (&x)[D / 8][4], const float (&a)[4],
+                                         const float (&b)[4], const __nv_bfloat16 *tile, int i) {
+  const LeftBf16<2> l(a, b);
+#pragma unroll
+  for (int d = 0; d < D / 16; ++d) {
+    const PairBf16 k = by_channel<pad_row<__nv_bfloat16>(D)>(tile, i, 16 * d);
+    l.times(x[2 * d], k.b[0][0], k.b[0][1]);
+    l.times(x[2 * d + 1], k.b[1][0], k.b[1][1]);
+  }
+}
+template <int D>
+__device__ __forceinline__ void add_rows(float (&x)[D / 8][4], const float (&a)[4],
+                                         const float (&b)[4], const float *tile, int i) {
+  constexpr int kRow = pad_row<float>(D);
+  const int g = (threadIdx.x & 31) >> 2, t = threadIdx.x & 3;
+  const LeftTf32<3> l0(a), l1(b);
+#pragma unroll
+  for (int d = 0; d < D / 8; ++d) {
+    const float *at = tile + (i + 2 * t) * kRow + 8 * d + g;
+    l0.times(x[d], at[0], at[kRow]);
+    l1.times(x[d], at[8 * kRow], at[9 * kRow]);
+  }
+}
+// Products of 16 rows of q and of k with rows j .. j + 15 of k.
+template <int D>
+__device__ __forceinline__ void score_tiles(float (&qk)[2][4], float (&kk)[2][4],
+                                            const __nv_bfloat16 *qs, const __nv_bfloat16 *ks, int i,
+                                            int j) {
+  constexpr int kRow = pad_row<__nv_bfloat16>(D);
+  const int l = threadIdx.x & 31;
+#pragma unroll
+  for (int d = 0; d < D / 16; ++d) {
+    uint32_t a[4], c[4];
+    ldmatrix4(a, smem_u32(qs + (i + (l & 15)) * kRow + 16 * d + (l >> 4) * 8));
+    ldmatrix4(c, smem_u32(ks + (i + (l & 15)) * kRow + 16 * d + (l >> 4) * 8));
+    const PairBf16 k = by_token<kRow>(ks, j, 16 * d);
+#pragma unroll
+    for (int n = 0; n < 2; ++n) {
+      mma_bf16(qk[n], a, k.b[n][0], k.b[n][1]);
+      mma_bf16(kk[n], c, k.b[n][0], k.b[n][1]);
+    }
+  }
+}
+template <int D>
+__device__ __forceinline__ void score_tiles(float (&qk)[2][4], float (&kk)[2][4], const float *qs,
+                                            const float *ks, int i, int j) {
+  constexpr int kRow = pad_row<float>(D);
+  const int g = (threadIdx.x & 31) >> 2, t = threadIdx.x & 3;
+#pragma unroll 2
+  for (int d = 0; d < D / 8; ++d) {
+    const LeftTf32<3> a = left_rows<3, kRow>(qs, i, 8 * d), c = left_rows<3, kRow>(ks, i, 8 * d);
+#pragma unroll
+    for (int n = 0; n < 2; ++n) {
+      const float2 k = *(const float2 *)(ks + (j + 8 * n + g) * kRow + 8 * d + 2 * t);
+      a.times(qk[n], k.x, k.y);
+      c.times(kk[n], k.x, k.y);
+    }
+  }
+}
+// Sums over each of the warp's 16 rows of x times a raw tile's rows, in every lane of a row.
+template <int D, typename T>
+__device__ __forceinline__ void row_dots(float &top, float &bottom, const float (&x)[D / 8][4],
+                                         const T *tile, int i) {
+  constexpr int kRow = pad_row<T>(D);
+  const int g = (threadIdx.x & 31) >> 2, t = threadIdx.x & 3;
+  top = bottom = 0.f;
+#pragma unroll
+  for (int d = 0; d < D / 8; ++d) {
+    const T *a = tile + (i + g) * kRow + 8 * d + 2 * t, *b = a + 8 * kRow;
+    top = fmaf(x[d][0], to_f(a[0]), fmaf(x[d][1], to_f(a[1]), top));
+    bottom = fmaf(x[d][2], to_f(b[0]), fmaf(x[d][3], to_f(b[1]), bottom));
+  }
+#pragma unroll
+  for (int m = 1; m < 4; m <<= 1) {
+    top += __shfl_xor_sync(0xFFFFFFFFu, top, m);
+    bottom += __shfl_xor_sync(0xFFFFFFFFu, bottom, m);
+  }
+}
+__device__ __forceinline__ void store2(float *p, float x, float y) { *(float2 *)p = make_float2(x, y); }
+__device__ __forceinline__ void store2(__nv_bfloat16 *p, float x, float y) {
+  *(uint32_t *)p = f2_to_bf2(x, y);
+}
+__device__ __forceinline__ void store1(float *p, float x) { *p = x; }
+__device__ __forceinline__ void store1(__nv_bfloat16 *p, float x) { *p = __float2bfloat16_rn(x); }
+
+// O: the type dq and dk leave in (fp32 planes where heads are shared).
+template <typename T, typename O, int D, int kSolve>
+__global__ void __launch_bounds__(GradShape<T, D>::kThreads)
+    grads_kernel(const DeltaBackArgs p, const float *records, const float *states,
+                 const float *misses, const float *after, const float *weights, O *dq, O *dk, int nc) {
+  using Sh = GradShape<T, D>;
+  using Rec = Record<T, kSolve, true>;
+  constexpr int C = Sh::C, kThreads = Sh::kThreads, kRow = Sh::kRow, kWide = Sh::kWide;
+  constexpr int kMat = Sh::kMat, kWarps = Sh::kWarps, kG = sizeof(T) == 2 ? 1 : 3;
+  extern __shared__ __align__(16) char raw[];
+  T *ks = (T *)raw, *qs = (T *)(raw + Sh::kTile), *ds = (T *)(raw + 2 * Sh::kTile);
+  float *us = (float *)(raw + 3 * Sh::kTile), *vs = us + C * kWide, *st = vs + C * kWide;
+  float *gt = st + Sh::kStateFloats, *share = gt + Gates<C>::kFloats, *end = share + C;
+  float *cols = end + C, *dots = cols + kWarps * C;
+  float *dP = st, *E = st + C * kMat;  // once the states are done with
+  grid_dep_wait();
+  const DeltaArgs &f = p.f;
+  const int h = blockIdx.y, b = blockIdx.z, hk = h / (f.H / f.Hk), tid = threadIdx.x;
+  const int w = tid / 32, lane = tid & 31, g = lane >> 2, t = lane & 3, i0 = 16 * w;
+  const int L = f.seq_lens ? min(max(__ldg(f.seq_lens + b), 0), f.N) : f.N;
+  const int t0 = blockIdx.x * C, n = min(max(L - t0, 0), C), rows = min(f.N - t0, C);
+  const size_t bt = (size_t)b * f.N + t0, row0 = bt * f.H + h;  // first token's row of a head
+  const size_t orow = (size_t)f.H * D;
+  dq += row0 * D, dk += row0 * D;
+  T *dlog = (T *)p.dlog_decay + row0, *dbeta = (T *)p.dbeta + row0;
+  // rows past the end
+  for (int i = tid; i < (rows - n) * (D / 2); i += kThreads) {
+    const size_t at = (size_t)(n + i / (D / 2)) * orow + i % (D / 2) * 2;
+    store2(dq + at, 0.f, 0.f);
+    store2(dk + at, 0.f, 0.f);
+    store2((T *)p.dv + row0 * D + at, 0.f, 0.f);
+  }
+  for (int i = n + tid; i < rows; i += kThreads) {
+    store1(dlog + (size_t)i * f.H, 0.f);
+    store1(dbeta + (size_t)i * f.H, 0.f);
+  }
+  if (n == 0) return;
+  const size_t at = ((size_t)b * f.H + h) * nc + blockIdx.x;
+  const float *S0 = states + at * D * D, *A1 = after + at * D * D;
+  load_rows<T, C, D, kThreads>(ks, (const T *)f.k + b * f.sk[0] + t0 * f.sk[1] + (long long)hk * D,
+                               f.sk[1], n);
+  load_rows<T, C, D, kThreads>(qs, (const T *)f.q + b * f.sq[0] + t0 * f.sq[1] + (long long)hk * D,
+                               f.sq[1], n);
+  load_rows<T, C, D, kThreads>(ds, (const T *)p.d_o + row0 * D, (long long)orow, n);
+  load_rows<float, C, D, kThreads>(us, misses + at * C * D, D, C);
+  load_rows<float, C, D, kThreads>(vs, weights + at * C * D, D, C);
+  load_rows<float, D, D, kThreads>(st, A1, D, D);
+  load_flat<Gates<C>::kFloats, kThreads>(gt, records + at * Rec::kFloats + Rec::kGates);
+  cp_async_commit();
+  cp_async_wait_all();
+  __syncthreads();
+  // dbeta, then u and dv in the places of the misses and w
+  for (int i = i0; i < i0 + 16; ++i) {
+    const float be = gt[Gates<C>::kBeta + i];
+    float dot = 0.f;
+#pragma unroll
+    for (int d = lane; d < D; d += 32) {
+      const float m = us[i * kWide + d], x = vs[i * kWide + d];
+      dot = fmaf(m, x, dot);
+      us[i * kWide + d] = be * m, vs[i * kWide + d] = be * x;
+    }
+#pragma unroll
+    for (int m = 16; m > 0; m >>= 1) dot += __shfl_xor_sync(0xFFFFFFFFu, dot, m);
+    if (lane == 0 && i < n) store1(dbeta + (size_t)i * f.H, dot);
+  }
+  __syncwarp();
+  // products with the states.  G's shares: sums of rows of each term with the token's own vector
+  const float up0 = gt[Gates<C>::kUp + i0 + g], up1 = gt[Gates<C>::kUp + i0 + g + 8];
+  const float dn0 = gt[Gates<C>::kDown + i0 + g], dn1 = gt[Gates<C>::kDown + i0 + g + 8];
+  float x[D / 8][4] = {}, y[D / 8][4] = {};  // dq, dk
+#pragma unroll 2
+  for (int e = 0; e < D; e += 8) {
+    const LeftTf32<kG> a = left_rows<kG, kWide>(us, i0, e, dn0, dn1);
+#pragma unroll
+    for (int d = 0; d < D / 8; ++d) {
+      const float2 s = *(const float2 *)(st + (8 * d + g) * kWide + e + 2 * t);
+      a.times(y[d], s.x, s.y);
+    }
+  }
+  float to0, to1, all0, all1, q0, q1;
+  row_dots<D>(to0, to1, y, ks, i0);
+  __syncthreads();
+  {
+    float dot = 0.f;  // S . A, as S takes A's place
+    for (int i = tid; i < D * D / 4; i += kThreads) {
+      float4 *s = (float4 *)(st + i / (D / 4) * kWide + i % (D / 4) * 4);
+      const float4 a = *s, v = ((const float4 *)S0)[i];
+      dot = fmaf(a.x, v.x, fmaf(a.y, v.y, fmaf(a.z, v.z, fmaf(a.w, v.w, dot))));
+      *s = v;
+    }
+#pragma unroll
+    for (int m = 16; m > 0; m >>= 1) dot += __shfl_xor_sync(0xFFFFFFFFu, dot, m);
+    if (lane == 0) dots[w] = dot;
+  }
+  __syncthreads();
+#pragma unroll 2
+  for (int e = 0; e < D; e += 8) {
+    const LeftTf32<kG> a = left_rows<kG, kRow>(ds, i0, e, up0 * f.scale, up1 * f.scale);
+    const LeftTf32<kG> c = left_rows<kG, kWide>(vs, i0, e, -up0, -up1);
+#pragma unroll
+    for (int d = 0; d < D / 8; ++d) {
+      const float2 s = *(const float2 *)(st + (8 * d + g) * kWide + e + 2 * t);
+      a.times(x[d], s.x, s.y);
+      c.times(y[d], s.x, s.y);
+    }
+  }
+  row_dots<D>(q0, q1, x, qs, i0);
+  row_dots<D>(all0, all1, y, ks, i0);
+  float mine0 = q0 + (all0 - to0) - to0, mine1 = q1 + (all1 - to1) - to1;
+  __syncthreads();  // the states are done with
+  // the tokens before, 16 at a time
+  float below0 = 0.f, below1 = 0.f;
+  for (int j0 = 0; j0 <= i0; j0 += 16) {
+    float qk[2][4] = {}, kk[2][4] = {}, a[2][4] = {}, c[2][4] = {};
+    score_tiles<D>(qk, kk, qs, ks, i0, j0);
+#pragma unroll 2
+    for (int e = 0; e < D; e += 8) {
+      const LeftTf32<kG> l = left_rows<kG, kRow>(ds, i0, e), m = left_rows<kG, kWide>(vs, i0, e);
+#pragma unroll
+      for (int q = 0; q < 2; ++q) {
+        const float2 u = *(const float2 *)(us + (j0 + 8 * q + g) * kWide + e + 2 * t);
+        l.times(a[q], u.x, u.y);
+        m.times(c[q], u.x, u.y);
+      }
+    }
+#pragma unroll
+    for (int q = 0; q < 2; ++q) {
+      float col[2] = {};
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const int i = i0 + g + (e >> 1) * 8, j = j0 + 8 * q + 2 * t + (e & 1);
+        const float pw = i >= j ? ex2_approx((gt[Gates<C>::kHi + i] - gt[Gates<C>::kHi + j]) +
+                                             (gt[Gates<C>::kLo + i] - gt[Gates<C>::kLo + j]))
+                                : 0.f;
+        a[q][e] = f.scale * pw * a[q][e];
+        c[q][e] = i > j ? -pw * c[q][e] : 0.f;
+        const float m = fmaf(a[q][e], qk[q][e], c[q][e] * kk[q][e]);
+        (e < 2 ? below0 : below1) += m;
+        col[e & 1] += m;
+        dP[i * kMat + j] = a[q][e];
+        E[i * kMat + j] = c[q][e];
+      }
+#pragma unroll
+      for (int m = 4; m < 32; m <<= 1) {
+        col[0] += __shfl_xor_sync(0xFFFFFFFFu, col[0], m);
+        col[1] += __shfl_xor_sync(0xFFFFFFFFu, col[1], m);
+      }
+      if (g == 0) *(float2 *)(cols + w * C + j0 + 8 * q + 2 * t) = make_float2(col[0], col[1]);
+    }
+    add_rows<D>(x, a[0], a[1], ks, j0);
+    add_rows<D>(y, c[0], c[1], ks, j0);
+  }
+#pragma unroll
+  for (int m = 1; m < 4; m <<= 1) {
+    below0 += __shfl_xor_sync(0xFFFFFFFFu, below0, m);
+    below1 += __shfl_xor_sync(0xFFFFFFFFu, below1, m);
+  }
+  if (t == 0) {
+    share[i0 + g] = mine0 + below0, share[i0 + g + 8] = mine1 + below1;
+    end[i0 + g] = to0, end[i0 + g + 8] = to1;
+  }
+  __syncthreads();
+  // the tokens from these on: dP and E the other way round
+  for (int j0 = i0; j0 < C; j0 += 16) {
+    float a[2][4], c[2][4];
+#pragma unroll
+    for (int q = 0; q < 2; ++q)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const int at2 = (j0 + 8 * q + 2 * t + (e & 1)) * kMat + i0 + g + (e >> 1) * 8;
+        a[q][e] = dP[at2], c[q][e] = E[at2];
+      }
+    add_rows<D>(y, a[0], a[1], qs, j0);
+    add_rows<D>(y, c[0], c[1], ks, j0);
+  }
+#pragma unroll
+  for (int half = 0; half < 2; ++half)
+    if (i0 + g + 8 * half < n) {
+      const size_t to = (size_t)(i0 + g + 8 * half) * orow + 2 * t;
+#pragma unroll
+      for (int d = 0; d < D / 8; ++d) {
+        store2(dq + to + 8 * d, x[d][2 * half], x[d][2 * half + 1]);
+        store2(dk + to + 8 * d, y[d][2 * half], y[d][2 * half + 1]);
+      }
+    }
+  // the log decays: sums from each token to the chunk's end
+  if (tid < C) {
+    double G = share[tid];
+    for (int v = tid / 16; v < kWarps; ++v) G -= cols[v * C + tid];
+    if (tid == C - 1) {
+      double last = 0.;
+      for (int i = 0; i < C; ++i) last += end[i];
+      for (int v = 0; v < kWarps; ++v) last += (double)gt[Gates<C>::kWhole] * dots[v];
+      G += last;
+    }
+#pragma unroll
+    for (int m = 1; m < 32; m <<= 1) {
+      const double o = __shfl_down_sync(0xFFFFFFFFu, G, m);
+      if (lane + m < 32) G += o;
+    }
+    double *later = (double *)cols;  // (read before: the barrier below)
+    if (C > 32) {
+      named_barrier(1, C);
+      if (tid == 32) *later = G;
+      named_barrier(1, C);
+      if (tid < 32) G += *later;
+    }
+    if (tid < n) {
+      const float lg = to_f(((const T *)f.log_decay)[b * f.sg[0] + (t0 + tid) * f.sg[1] + h]);
+      store1(dlog + (size_t)tid * f.H, lg == -INFINITY ? 0.f : (float)G);
+    }
+  }
+}
+
+// Scratch of the backward pass, in floats from one base.
+struct Layout {
+  size_t records, states, misses, after, weights, dq, dk, total;
+};
+template <typename T>
+Layout layout_of(const DeltaBackArgs &p, bool exact) {
+  const DeltaArgs &a = p.f;
+  constexpr int C = kChunkOf<T>;
+  const size_t all = (size_t)a.B * a.H * chunks_of<T>(a);
+  Layout l = {};
+  size_t at = 0;
+  auto take = [&](size_t &to, size_t floats) { to = at, at += (floats + 63) / 64 * 64; };
+  take(l.records, all * (exact || sizeof(T) == 4 ? Record<T, 3, true>::kFloats : Record<T, 1, true>::kFloats));
+  take(l.states, all * a.D * a.D);
+  take(l.after, all * a.D * a.D);
+  take(l.misses, all * C * a.D);
+  take(l.weights, all * C * a.D);
+  const size_t plane = a.H == a.Hk ? 0 : (size_t)a.B * a.N * a.H * a.D;
+  take(l.dq, plane);
+  take(l.dk, plane);
+  l.total = at;
+  return l;
+}
+// Terms: three where a state's gradient is a result.
+bool exact_back(const DeltaBackArgs &p) { return p.f.dtype == GBLA_FP32 || p.dstate_in; }
+
+template <typename T, typename O, int D, int kSolve>
+cudaError_t grads_launch(const DeltaBackArgs &p, const Layout &l, float *s, O *dq, O *dk,
+                         cudaStream_t st) {
+  using Sh = GradShape<T, D>;
+  const int nc = chunks_of<T>(p.f);
+  const auto kernel = grads_kernel<T, O, D, kSolve>;
+  cudaError_t e;
+  if ((e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, Sh::kBytes)) !=
+      cudaSuccess)
+    return e;
+  count_launch();
+  return launch_pdl(kernel, dim3(nc, p.f.H, p.f.B), dim3(Sh::kThreads), Sh::kBytes, st, p,
+                    (const float *)(s + l.records), (const float *)(s + l.states),
+                    (const float *)(s + l.misses), (const float *)(s + l.after),
+                    (const float *)(s + l.weights), dq, dk, nc);
+}
+
+template <typename T, int D, int kTerms, int kSolve>
+cudaError_t back_launch(const DeltaBackArgs &p, float *s, cudaStream_t st) {
+  using Sh = ReverseShape<T, D, kSolve>;
+  const DeltaArgs &a = p.f;
+  const Layout l = layout_of<T>(p, kSolve == 3);
+  const int nc = chunks_of<T>(a);
+  cudaError_t e;
+  if ((e = save_forward(a, kSolve == 3, s + l.records, s + l.states, s + l.misses, st)) != cudaSuccess)
+    return e;
+  const auto reverse = reverse_kernel<T, D, kTerms, kSolve>;
+  if ((e = cudaFuncSetAttribute(reverse, cudaFuncAttributeMaxDynamicSharedMemorySize, Sh::kBytes)) !=
+      cudaSuccess)
+    return e;
+  count_launch();
+  if ((e = launch_pdl(reverse, dim3(a.H, a.B), dim3(Sh::kThreads), Sh::kBytes, st, p,
+                      (const float *)(s + l.records), s + l.after, s + l.weights, nc)) != cudaSuccess)
+    return e;
+  if (a.H == a.Hk) return grads_launch<T, T, D, kSolve>(p, l, s, (T *)p.dq, (T *)p.dk, st);
+  float *dq = s + l.dq, *dk = s + l.dk;
+  if ((e = grads_launch<T, float, D, kSolve>(p, l, s, dq, dk, st)) != cudaSuccess) return e;
+  return sum_shared_heads(dq, dk, p.dq, p.dk, (long long)a.B * a.N, a.Hk, a.H / a.Hk, D, a.dtype, st);
+}
+
+template <int D>
+cudaError_t back_d(const DeltaBackArgs &p, float *s, cudaStream_t st) {
+  if (p.f.dtype == GBLA_FP32) return back_launch<float, D, 3, 3>(p, s, st);
+  if (exact_back(p)) return back_launch<__nv_bfloat16, D, 3, 3>(p, s, st);
+  return back_launch<__nv_bfloat16, D, 2, 1>(p, s, st);
+}
+
+}  // namespace
+}  // namespace delta
+
+size_t delta_backward_floats(const DeltaBackArgs &p) {
+  using namespace delta;
+  return (p.f.dtype == GBLA_FP32 ? layout_of<float>(p, true)
+                                 : layout_of<__nv_bfloat16>(p, exact_back(p))).total;
+}
+
+cudaError_t delta_backward(const DeltaBackArgs &p, float *scratch, cudaStream_t st) {
+  if (p.f.D == 32) return delta::back_d<32>(p, scratch, st);
+  if (p.f.D == 64) return delta::back_d<64>(p, scratch, st);
+  return delta::back_d<128>(p, scratch, st);
+}
+
+}  // namespace gbla

@@ -18,17 +18,6 @@ namespace gbla {
 namespace delta {
 namespace {
 
-// A chunk's record: M, P and the powers of its gates.  M in kSolve terms; P in one where results
-// are bf16.
-template <typename T, int kSolve>
-struct Record {
-  static constexpr int C = kChunkOf<T>;
-  using M = Tiles<C, kSolve>;
-  using P = Tiles<C, sizeof(T) == 2 ? 1 : 3>;
-  static constexpr int kM = 0, kP = M::kFloats, kGates = kP + P::kFloats;
-  static constexpr int kFloats = kGates + Gates<C>::kFloats;
-};
-
 // --------------------------------------------------------------- first launch
 // One block a (chunk, head, batch), a warp for each 16 of its tokens.
 template <typename T, int D>
@@ -170,11 +159,11 @@ __device__ __forceinline__ void invert(float *to, const float *A, int w) {
   }
 }
 
-template <typename T, int D, int kSolve>
+template <typename T, int D, int kSolve, bool kBack>
 __global__ void __launch_bounds__(PrepShape<T, D>::kThreads)
     prepare_kernel(const DeltaArgs p, float *records, int nc) {
   using Sh = PrepShape<T, D>;
-  using Rec = Record<T, kSolve>;
+  using Rec = Record<T, kSolve, kBack>;
   constexpr int C = Sh::C, kThreads = Sh::kThreads, kRow = Sh::kRow, kMat = Sh::kMat;
   extern __shared__ __align__(16) char raw[];
   T *ks = (T *)raw, *qs = ks + C * kRow;
@@ -217,6 +206,7 @@ __global__ void __launch_bounds__(PrepShape<T, D>::kThreads)
     if (tid >= 32) G += *first;
     const double G2 = G * 1.4426950408889634;  // powers of two from here on
     hi[tid] = (float)G2, lo[tid] = (float)(G2 - (double)hi[tid]);
+    if (kBack) gt[Gates<C>::kHi + tid] = hi[tid], gt[Gates<C>::kLo + tid] = lo[tid];
     gt[Gates<C>::kUp + tid] = expf((float)G);
     gt[Gates<C>::kBeta + tid] = beta[tid];
     if (tid == C - 1) {
@@ -243,173 +233,78 @@ __global__ void __launch_bounds__(PrepShape<T, D>::kThreads)
       const int i = 16 * w + g + 8 * half;
       const float f0 = i >= j ? ex2_approx((hi[i] - hj.x) + (lo[i] - lj.x)) : 0.f;
       const float f1 = i >= j + 1 ? ex2_approx((hi[i] - hj.y) + (lo[i] - lj.y)) : 0.f;
-      *(float2 *)(A + i * kMat + j) =
-          make_float2(i > j ? kk[m][2 * half] * f0 * bj.x : 0.f,
-                      i > j + 1 ? kk[m][2 * half + 1] * f1 * bj.y : 0.f);
-      if (2 * w + half >= m)
-        Rec::P::store(rec + Rec::kP, 2 * w + half, m, p.scale * qk[m][2 * half] * f0,
-                      p.scale * qk[m][2 * half + 1] * f1);
+      float &x0 = kk[m][2 * half], &x1 = kk[m][2 * half + 1];
+      x0 = i > j ? x0 * f0 : 0.f, x1 = i > j + 1 ? x1 * f1 : 0.f;
+      *(float2 *)(A + i * kMat + j) = make_float2(x0 * bj.x, x1 * bj.y);
+      const float p0 = p.scale * qk[m][2 * half] * f0, p1 = p.scale * qk[m][2 * half + 1] * f1;
+      if (kBack)
+        *(float2 *)(inv + i * kMat + j) = make_float2(p0, p1);
+      else if (2 * w + half >= m)
+        Rec::P::store(rec + Rec::kP, 2 * w + half, m, p0, p1);
     }
   }
   __syncthreads();
+  // a matrix in shared memory, tile by tile: as it is, or (kFlip) for sums over its rows;
+  // inverses without their diagonal of 1 (that part of a product needs no rounding)
+  auto put = [&](float *to, auto tiles, bool flip, bool inverse) {
+    using Form = decltype(tiles);
+    for (int m = w; m < C / 8; m += Sh::kWarps)
+      for (int j = 0; j <= m; ++j) {
+        const float *at = inv + (8 * m + (flip ? 2 * t : g)) * kMat + 8 * j + (flip ? g : 2 * t);
+        const bool one = inverse && j == m;
+        Form::store(to, m, j, one && g == 2 * t ? 0.f : at[0],
+                    one && g == 2 * t + 1 ? 0.f : at[flip ? kMat : 1]);
+      }
+  };
+  if (kBack) {
+    put(rec + Rec::kP, typename Rec::P{}, true, false);
+    __syncthreads();
+  }
   invert<C>(inv, A, w);
-  // M - 1, whose diagonal is 0: the identity's part of a product needs no rounding
-  for (int m = w; m < C / 8; m += Sh::kWarps)
-    for (int j = 0; j <= m; ++j) {
-      const float2 v = *(const float2 *)(inv + (8 * m + g) * kMat + 8 * j + 2 * t);
-      Rec::M::store(rec + Rec::kM, m, j, j == m && g == 2 * t ? 0.f : v.x,
-                    j == m && g == 2 * t + 1 ? 0.f : v.y);
+  put(rec + Rec::kM, typename Rec::M{}, false, true);
+  if (kBack) {  // (1 + beta X)^-1: the rows weighted in place of the columns
+    __syncthreads();
+#pragma unroll
+    for (int m = 0; m < C / 8; ++m) {
+      if (m > 2 * w + 1) continue;
+#pragma unroll
+      for (int half = 0; half < 2; ++half) {
+        const int i = 16 * w + g + 8 * half;
+        *(float2 *)(A + i * kMat + 8 * m + 2 * t) =
+            make_float2(kk[m][2 * half] * beta[i], kk[m][2 * half + 1] * beta[i]);
+      }
     }
+    __syncthreads();
+    invert<C>(inv, A, w);
+    put(rec + Rec::kT, typename Rec::M{}, true, true);
+  }
 }
 
 // --------------------------------------------------------------- second launch
-template <typename T, int D, int kSolve>
+template <typename T, int D, int kSolve, bool kSave>
 struct ScanShape {
   static constexpr int C = kChunkOf<T>, kWarps = D / 16, kThreads = kWarps * 32;
   static constexpr int kRow = pad_row<T>(D);
-  static constexpr int kTile = C * kRow * (int)sizeof(T);        // bytes of k, q or v
-  static constexpr int kStage = 3 * kTile + Record<T, kSolve>::kFloats * 4;
+  static constexpr int kTile = C * kRow * (int)sizeof(T);        // bytes of k, v or q
+  static constexpr int kTiles = kSave ? 2 : 3;
+  static constexpr int kStage = kTiles * kTile + Record<T, kSolve, kSave>::kFloats * 4;
   static constexpr int kBytes = 2 * kStage;
 };
 
-// Products of the state's 16 columns (transposed: D / 8 tiles) with keys and queries.
-template <int kTerms, int D, int C>
-__device__ __forceinline__ void state_products(const float (&S)[D / 8][4], const __nv_bfloat16 *ks,
-                                               const __nv_bfloat16 *qs, float (&kv)[C / 8][4],
-                                               float (&qv)[C / 8][4]) {
-  constexpr int kRow = pad_row<__nv_bfloat16>(D);
-#pragma unroll
-  for (int d = 0; d < D / 16; ++d) {
-    const LeftBf16<kTerms> a(S[2 * d], S[2 * d + 1]);
-#pragma unroll
-    for (int n = 0; n < C / 16; ++n) {
-      const PairBf16 k = by_token<kRow>(ks, 16 * n, 16 * d), q = by_token<kRow>(qs, 16 * n, 16 * d);
-      a.times(kv[2 * n], k.b[0][0], k.b[0][1]);
-      a.times(kv[2 * n + 1], k.b[1][0], k.b[1][1]);
-#pragma unroll
-      for (int i = 0; i < 2; ++i)  // results are bf16: 16 bits of the state do
-#pragma unroll
-        for (int p = 1; p >= 0; --p) mma_bf16(qv[2 * n + i], a.part[p], q.b[i][0], q.b[i][1]);
-    }
-  }
-}
-template <int kTerms, int D, int C>
-__device__ __forceinline__ void state_products(const float (&S)[D / 8][4], const float *ks,
-                                               const float *qs, float (&kv)[C / 8][4],
-                                               float (&qv)[C / 8][4]) {
-  constexpr int kRow = pad_row<float>(D);
-  const int g = (threadIdx.x & 31) >> 2, t = threadIdx.x & 3;
-#pragma unroll
-  for (int d = 0; d < D / 8; ++d) {
-    const LeftTf32<3> a(S[d]);
-#pragma unroll
-    for (int n = 0; n < C / 8; ++n) {
-      const float2 k = *(const float2 *)(ks + (8 * n + g) * kRow + 8 * d + 2 * t);
-      const float2 q = *(const float2 *)(qs + (8 * n + g) * kRow + 8 * d + 2 * t);
-      a.times(kv[n], k.x, k.y);
-      a.times(qv[n], q.x, q.y);
-    }
-  }
-}
-// S = (hi + lo) S + w^T k over the chunk's tokens.  The chunk's own sum starts from zero and is
-// added in one rounding: the tensor cores cut off what their accumulator cannot hold, which
-// over the chunks of a long sequence would shrink the state.
-template <int kTerms, int D, int C>
-__device__ __forceinline__ void state_update(float (&S)[D / 8][4], float hi, float lo,
-                                             const float (&w)[C / 8][4], const __nv_bfloat16 *ks) {
-  constexpr int kRow = pad_row<__nv_bfloat16>(D);
-  static_assert(C == 64, "four left operands");
-  const LeftBf16<kTerms> a[4] = {{w[0], w[1]}, {w[2], w[3]}, {w[4], w[5]}, {w[6], w[7]}};
-#pragma unroll
-  for (int d = 0; d < D / 16; ++d) {
-    float x[2][4] = {};
-#pragma unroll
-    for (int j = 0; j < C / 16; ++j) {
-      const PairBf16 k = by_channel<kRow>(ks, 16 * j, 16 * d);
-      a[j].times(x[0], k.b[0][0], k.b[0][1]);
-      a[j].times(x[1], k.b[1][0], k.b[1][1]);
-    }
-#pragma unroll
-    for (int i = 0; i < 2; ++i)
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        float &s = S[2 * d + i][e];
-        s = fmaf(hi, s, fmaf(lo, s, x[i][e]));
-      }
-  }
-}
-template <int kTerms, int D, int C>
-__device__ __forceinline__ void state_update(float (&S)[D / 8][4], float hi, float lo,
-                                             const float (&w)[C / 8][4], const float *ks) {
-  constexpr int kRow = pad_row<float>(D);
-  const int g = (threadIdx.x & 31) >> 2, t = threadIdx.x & 3;
-#pragma unroll
-  for (int d = 0; d < D / 8; ++d) {
-    float x[4] = {};
-#pragma unroll
-    for (int j = 0; j < C / 8; ++j) {
-      const LeftTf32<3> a(w[j]);
-      a.times(x, ks[(8 * j + 2 * t) * kRow + 8 * d + g], ks[(8 * j + 2 * t + 1) * kRow + 8 * d + g]);
-    }
-#pragma unroll
-    for (int e = 0; e < 4; ++e) S[d][e] = fmaf(hi, S[d][e], fmaf(lo, S[d][e], x[e]));
-  }
-}
-// The values of the warp's columns e0 .. e0 + 15 at the tokens of tiles 2n and 2n + 1, as
-// product tiles hold them.
-template <int kRow>
-__device__ __forceinline__ void values_of(float (&a)[4], float (&b)[4], const __nv_bfloat16 *vs,
-                                          int n, int e0) {
-  const int l = threadIdx.x & 31;
-  uint32_t r[4];
-  ldmatrix4_t(r, smem_u32(vs + (16 * n + (l >> 4) * 8 + (l & 7)) * kRow + e0 + ((l >> 3) & 1) * 8));
-  const float2 f[4] = {bf2_to_f2(r[0]), bf2_to_f2(r[1]), bf2_to_f2(r[2]), bf2_to_f2(r[3])};
-  a[0] = f[0].x, a[1] = f[0].y, a[2] = f[1].x, a[3] = f[1].y;
-  b[0] = f[2].x, b[1] = f[2].y, b[2] = f[3].x, b[3] = f[3].y;
-}
-template <int kRow>
-__device__ __forceinline__ void values_of(float (&a)[4], float (&b)[4], const float *vs, int n,
-                                          int e0) {
-  const int g = (threadIdx.x & 31) >> 2, t = threadIdx.x & 3;
-  const float *v = vs + (16 * n + 2 * t) * kRow + e0 + g;
-  a[0] = v[0], a[1] = v[kRow], a[2] = v[8], a[3] = v[kRow + 8];
-  v += 8 * kRow;
-  b[0] = v[0], b[1] = v[kRow], b[2] = v[8], b[3] = v[kRow + 8];
-}
-// A result tile (16 columns of the values, 8 tokens from `token` on) to global memory.
-__device__ __forceinline__ void store_tile(__nv_bfloat16 *o, size_t stride, const float (&c)[4],
-                                           int token, int n) {
-  const int g = (threadIdx.x & 31) >> 2, t = threadIdx.x & 3;
-  const uint32_t lo = transpose8(f2_to_bf2(c[0], c[1])), hi = transpose8(f2_to_bf2(c[2], c[3]));
-  if (token + g < n) {
-    uint32_t *at = (uint32_t *)(o + (size_t)(token + g) * stride + 2 * t);
-    at[0] = lo, at[4] = hi;
-  }
-}
-__device__ __forceinline__ void store_tile(float *o, size_t stride, const float (&c)[4], int token,
-                                           int n) {
-  const int g = (threadIdx.x & 31) >> 2, t = threadIdx.x & 3;
-#pragma unroll
-  for (int e = 0; e < 2; ++e)
-    if (token + 2 * t + e < n) {
-      float *at = o + (size_t)(token + 2 * t + e) * stride + g;
-      at[0] = c[e], at[8] = c[2 + e];
-    }
-}
-
 // kTerms: bf16 numbers that stand for a value of the state where it meets a key or takes a
 // write (fp32: 3 tf32 products); kSolve: terms of the product with M.
-template <typename T, int D, int kTerms, int kSolve>
-__global__ void __launch_bounds__(ScanShape<T, D, kSolve>::kThreads)
-    scan_kernel(const DeltaArgs p, const float *records, int nc) {
-  using Sh = ScanShape<T, D, kSolve>;
-  using Rec = Record<T, kSolve>;
+// kSave: no results, but for the backward pass the state before every chunk and the misses.
+template <typename T, int D, int kTerms, int kSolve, bool kSave>
+__global__ void __launch_bounds__(ScanShape<T, D, kSolve, kSave>::kThreads)
+    scan_kernel(const DeltaArgs p, const float *records, float *states, float *misses, int nc) {
+  using Sh = ScanShape<T, D, kSolve, kSave>;
+  using Rec = Record<T, kSolve, kSave>;
   constexpr int C = Sh::C, kThreads = Sh::kThreads, kRow = Sh::kRow;
   constexpr int kOut = sizeof(T) == 2 ? 1 : 3;  // terms of the product with P
   extern __shared__ __align__(16) char raw[];
   grid_dep_wait();
   const int h = blockIdx.x, b = blockIdx.y, hk = h / (p.H / p.Hk), tid = threadIdx.x;
-  const int w = tid / 32, g = (tid & 31) >> 2, t = tid & 3, e0 = 16 * w;
+  const int t = tid & 3, e0 = tid / 32 * 16;
   const int L = p.seq_lens ? min(max(__ldg(p.seq_lens + b), 0), p.N) : p.N;
   const size_t bh = (size_t)b * p.H + h;
   const T *kg = (const T *)p.k + b * p.sk[0] + (long long)hk * D;
@@ -423,18 +318,14 @@ __global__ void __launch_bounds__(ScanShape<T, D, kSolve>::kThreads)
     const long long t0 = (long long)c * C;
     const int n = min(C, L - c * C);
     load_rows<T, C, D, kThreads>((T *)s, kg + t0 * p.sk[1], p.sk[1], n);
-    load_rows<T, C, D, kThreads>((T *)(s + Sh::kTile), qg + t0 * p.sq[1], p.sq[1], n);
-    load_rows<T, C, D, kThreads>((T *)(s + 2 * Sh::kTile), vg + t0 * p.sv[1], p.sv[1], n);
-    load_flat<Rec::kFloats, kThreads>((float *)(s + 3 * Sh::kTile),
+    load_rows<T, C, D, kThreads>((T *)(s + Sh::kTile), vg + t0 * p.sv[1], p.sv[1], n);
+    if (!kSave)
+      load_rows<T, C, D, kThreads>((T *)(s + 2 * Sh::kTile), qg + t0 * p.sq[1], p.sq[1], n);
+    load_flat<Rec::kFloats, kThreads>((float *)(s + Sh::kTiles * Sh::kTile),
                                       records + (bh * nc + c) * Rec::kFloats);
   };
   float S[D / 8][4];  // rows: columns e0 + g, + 8 of the state; columns: its rows
-#pragma unroll
-  for (int d = 0; d < D / 8; ++d)
-#pragma unroll
-    for (int i = 0; i < 4; ++i)
-      S[d][i] = p.init ? p.init[bh * D * D + (size_t)(8 * d + 2 * t + (i & 1)) * D + e0 + g + (i >> 1) * 8]
-                       : 0.f;
+  load_state<D>(S, p.init ? p.init + bh * D * D : nullptr, e0);
   if (chunks > 0) load(0);
   cp_async_commit();
   for (int c = 0; c < chunks; ++c) {
@@ -443,11 +334,12 @@ __global__ void __launch_bounds__(ScanShape<T, D, kSolve>::kThreads)
     if (c + 1 < chunks) load(c + 1);
     cp_async_commit();
     const char *s = raw + (c & 1) * Sh::kStage;
-    const T *ks = (const T *)s, *qs = (const T *)(s + Sh::kTile), *vs = (const T *)(s + 2 * Sh::kTile);
-    const float *rec = (const float *)(s + 3 * Sh::kTile), *gt = rec + Rec::kGates;
+    const T *ks = (const T *)s, *vs = (const T *)(s + Sh::kTile), *qs = (const T *)(s + 2 * Sh::kTile);
+    const float *rec = (const float *)(s + Sh::kTiles * Sh::kTile), *gt = rec + Rec::kGates;
     const int n = min(C, L - c * C);
+    if (kSave) store_state<D>(states + (bh * nc + c) * D * D, S, e0);
     float r[C / 8][4] = {}, o[C / 8][4] = {};
-    state_products<kTerms, D, C>(S, ks, qs, r, o);
+    state_products<kTerms, D, C, !kSave>(S, ks, qs, r, o);
 #pragma unroll
     for (int m = 0; m < C / 16; ++m) {
       float v[2][4];
@@ -483,39 +375,34 @@ __global__ void __launch_bounds__(ScanShape<T, D, kSolve>::kThreads)
     // u, and the results
 #pragma unroll
     for (int j = 0; j < C / 8; ++j) {
+      if (kSave) store_tile(misses + (bh * nc + c) * C * D + e0, D, r[j], 8 * j, C);
       const float2 be = *(const float2 *)(gt + Gates<C>::kBeta + 8 * j + 2 * t);
       r[j][0] *= be.x, r[j][1] *= be.y, r[j][2] *= be.x, r[j][3] *= be.y;
-      const LeftTf32<kOut> a(r[j]);
+      if constexpr (!kSave) {
+        const LeftTf32<kOut> a(r[j]);
 #pragma unroll
-      for (int m = j; m < C / 8; ++m) a.times(o[m], Rec::P::load(rec + Rec::kP, m, j));
-      store_tile(og + (size_t)c * C * orow, orow, o[j], 8 * j, n);  // no later u meets it
+        for (int m = j; m < C / 8; ++m) a.times(o[m], Rec::P::load(rec + Rec::kP, m, j));
+        store_tile(og + (size_t)c * C * orow, orow, o[j], 8 * j, n);  // no later u meets it
+      }
       const float2 dn = *(const float2 *)(gt + Gates<C>::kDown + 8 * j + 2 * t);
       r[j][0] *= dn.x, r[j][1] *= dn.y, r[j][2] *= dn.x, r[j][3] *= dn.y;
     }
     state_update<kTerms, D, C>(S, gt[Gates<C>::kWhole], gt[Gates<C>::kWhole + 1], r, ks);
   }
-  if (p.fin) {
-#pragma unroll
-    for (int d = 0; d < D / 8; ++d)
-#pragma unroll
-      for (int i = 0; i < 4; ++i)
-        p.fin[bh * D * D + (size_t)(8 * d + 2 * t + (i & 1)) * D + e0 + g + (i >> 1) * 8] = S[d][i];
-  }
+  if (!kSave && p.fin) store_state<D>(p.fin + bh * D * D, S, e0);
 }
-
-template <typename T>
-int chunks_of(const DeltaArgs &a) { return (a.N + kChunkOf<T> - 1) / kChunkOf<T>; }
 
 // Terms of the product with M: bf16 results alone need one (2^-11 of what M adds to a miss).
 bool exact_state(const DeltaArgs &a) { return a.dtype == GBLA_FP32 || a.fin; }
 
-template <typename T, int D, int kTerms, int kSolve>
-cudaError_t launch(const DeltaArgs &a, float *scratch, cudaStream_t st) {
+template <typename T, int D, int kTerms, int kSolve, bool kSave>
+cudaError_t launch(const DeltaArgs &a, float *records, float *states, float *misses,
+                   cudaStream_t st) {
   using Pr = PrepShape<T, D>;
-  using Sc = ScanShape<T, D, kSolve>;
+  using Sc = ScanShape<T, D, kSolve, kSave>;
   const int nc = chunks_of<T>(a);
-  const auto prep = prepare_kernel<T, D, kSolve>;
-  const auto scan = scan_kernel<T, D, kTerms, kSolve>;
+  const auto prep = prepare_kernel<T, D, kSolve, kSave>;
+  const auto scan = scan_kernel<T, D, kTerms, kSolve, kSave>;
   cudaError_t e;
   if ((e = cudaFuncSetAttribute(prep, cudaFuncAttributeMaxDynamicSharedMemorySize, Pr::kBytes)) !=
       cudaSuccess)
@@ -524,36 +411,52 @@ cudaError_t launch(const DeltaArgs &a, float *scratch, cudaStream_t st) {
       cudaSuccess)
     return e;
   count_launch();
-  if ((e = launch_pdl(prep, dim3(nc, a.H, a.B), dim3(Pr::kThreads), Pr::kBytes, st, a, scratch,
+  if ((e = launch_pdl(prep, dim3(nc, a.H, a.B), dim3(Pr::kThreads), Pr::kBytes, st, a, records,
                       nc)) != cudaSuccess)
     return e;
   count_launch();
   return launch_pdl(scan, dim3(a.H, a.B), dim3(Sc::kThreads), Sc::kBytes, st, a,
-                    (const float *)scratch, nc);
+                    (const float *)records, states, misses, nc);
 }
 
 template <int D>
-cudaError_t launch_d(const DeltaArgs &a, float *scratch, cudaStream_t st) {
-  if (a.dtype == GBLA_FP32) return launch<float, D, 3, 3>(a, scratch, st);
-  if (exact_state(a)) return launch<__nv_bfloat16, D, 3, 3>(a, scratch, st);
-  return launch<__nv_bfloat16, D, 2, 1>(a, scratch, st);
+cudaError_t forward_d(const DeltaArgs &a, float *records, cudaStream_t st) {
+  if (a.dtype == GBLA_FP32) return launch<float, D, 3, 3, false>(a, records, nullptr, nullptr, st);
+  if (exact_state(a)) return launch<__nv_bfloat16, D, 3, 3, false>(a, records, nullptr, nullptr, st);
+  return launch<__nv_bfloat16, D, 2, 1, false>(a, records, nullptr, nullptr, st);
+}
+template <int D>
+cudaError_t save_d(const DeltaArgs &a, bool exact, float *records, float *states, float *misses,
+                   cudaStream_t st) {
+  if (a.dtype == GBLA_FP32) return launch<float, D, 3, 3, true>(a, records, states, misses, st);
+  if (exact) return launch<__nv_bfloat16, D, 3, 3, true>(a, records, states, misses, st);
+  return launch<__nv_bfloat16, D, 2, 1, true>(a, records, states, misses, st);
 }
 
 }  // namespace
+
+cudaError_t save_forward(const DeltaArgs &a, bool exact, float *records, float *states,
+                         float *misses, cudaStream_t st) {
+  if (a.D == 32) return save_d<32>(a, exact, records, states, misses, st);
+  if (a.D == 64) return save_d<64>(a, exact, records, states, misses, st);
+  return save_d<128>(a, exact, records, states, misses, st);
+}
+
 }  // namespace delta
 
 size_t delta_forward_floats(const DeltaArgs &a) {
   using namespace delta;
   const size_t bh = (size_t)a.B * a.H;
-  if (a.dtype == GBLA_FP32) return bh * chunks_of<float>(a) * Record<float, 3>::kFloats;
+  if (a.dtype == GBLA_FP32) return bh * chunks_of<float>(a) * Record<float, 3, false>::kFloats;
   return bh * chunks_of<__nv_bfloat16>(a) *
-         (exact_state(a) ? Record<__nv_bfloat16, 3>::kFloats : Record<__nv_bfloat16, 1>::kFloats);
+         (exact_state(a) ? Record<__nv_bfloat16, 3, false>::kFloats
+                         : Record<__nv_bfloat16, 1, false>::kFloats);
 }
 
 cudaError_t delta_forward(const DeltaArgs &a, float *scratch, cudaStream_t st) {
-  if (a.D == 32) return delta::launch_d<32>(a, scratch, st);
-  if (a.D == 64) return delta::launch_d<64>(a, scratch, st);
-  return delta::launch_d<128>(a, scratch, st);
+  if (a.D == 32) return delta::forward_d<32>(a, scratch, st);
+  if (a.D == 64) return delta::forward_d<64>(a, scratch, st);
+  return delta::forward_d<128>(a, scratch, st);
 }
 
 }  // namespace gbla

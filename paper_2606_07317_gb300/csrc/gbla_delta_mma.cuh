@@ -193,7 +193,7 @@ struct Tiles {
     if constexpr (kTerms == 1) {
       ((uint2 *)base)[at(m, j)] = make_uint2(tf32_of(b0), tf32_of(b1));
     } else {
-      uint4 v;
+      uint4 v;  // hi, hi, lo, lo
       tf32_split(b0, v.x, v.z);
       tf32_split(b1, v.y, v.w);
       ((uint4 *)base)[at(m, j)] = v;
@@ -203,8 +203,182 @@ struct Tiles {
 // Powers of a chunk's gates.
 template <int C>
 struct Gates {
-  static constexpr int kUp = 0, kDown = C, kBeta = 2 * C, kWhole = 3 * C, kFloats = 4 * C;
+  // e^G_i, e^(G_C - G_i), beta_i; G_i log2 e as two floats; e^G_C as two
+  static constexpr int kUp = 0, kDown = C, kBeta = 2 * C, kHi = 3 * C, kLo = 4 * C, kWhole = 5 * C;
+  static constexpr int kFloats = 5 * C + 4;
 };
+
+// A chunk's record.  For the forward pass M, P and the powers of its gates, M in kSolve terms, P
+// in one where results are bf16.  For the backward pass (kBack) M, and, for products that sum
+// over the row index, T = (1 + beta X)^-1 and P the other way round, in kSolve terms.
+template <typename T, int kSolve, bool kBack>
+struct Record {
+  static constexpr int C = kChunkOf<T>;
+  using M = Tiles<C, kSolve>;
+  using P = Tiles<C, kBack ? kSolve : sizeof(T) == 2 ? 1 : 3>;
+  static constexpr int kM = 0, kP = M::kFloats, kT = kP + P::kFloats;
+  static constexpr int kGates = kT + (kBack ? M::kFloats : 0);
+  static constexpr int kFloats = kGates + Gates<C>::kFloats;
+};
+
+// ------------------------------------------------------------- a warp's part of a state
+// Products of the state's 16 columns (transposed: D / 8 tiles) with the rows of a tile (keys, or
+// with `more` keys and, in 16 bits where they are bf16, queries).
+template <int kTerms, int D, int C, bool kMore>
+__device__ __forceinline__ void state_products(const float (&S)[D / 8][4], const __nv_bfloat16 *ks,
+                                               const __nv_bfloat16 *qs, float (&kv)[C / 8][4],
+                                               float (&qv)[C / 8][4]) {
+  constexpr int kRow = pad_row<__nv_bfloat16>(D);
+#pragma unroll
+  for (int d = 0; d < D / 16; ++d) {
+    const LeftBf16<kTerms> a(S[2 * d], S[2 * d + 1]);
+#pragma unroll
+    for (int n = 0; n < C / 16; ++n) {
+      const PairBf16 k = by_token<kRow>(ks, 16 * n, 16 * d);
+      a.times(kv[2 * n], k.b[0][0], k.b[0][1]);
+      a.times(kv[2 * n + 1], k.b[1][0], k.b[1][1]);
+      if (kMore) {
+        const PairBf16 q = by_token<kRow>(qs, 16 * n, 16 * d);
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+#pragma unroll
+          for (int p = 1; p >= 0; --p) mma_bf16(qv[2 * n + i], a.part[p], q.b[i][0], q.b[i][1]);
+      }
+    }
+  }
+}
+template <int kTerms, int D, int C, bool kMore>
+__device__ __forceinline__ void state_products(const float (&S)[D / 8][4], const float *ks,
+                                               const float *qs, float (&kv)[C / 8][4],
+                                               float (&qv)[C / 8][4]) {
+  constexpr int kRow = pad_row<float>(D);
+  const int g = (threadIdx.x & 31) >> 2, t = threadIdx.x & 3;
+#pragma unroll
+  for (int d = 0; d < D / 8; ++d) {
+    const LeftTf32<3> a(S[d]);
+#pragma unroll
+    for (int n = 0; n < C / 8; ++n) {
+      const float2 k = *(const float2 *)(ks + (8 * n + g) * kRow + 8 * d + 2 * t);
+      a.times(kv[n], k.x, k.y);
+      if (kMore) {
+        const float2 q = *(const float2 *)(qs + (8 * n + g) * kRow + 8 * d + 2 * t);
+        a.times(qv[n], q.x, q.y);
+      }
+    }
+  }
+}
+// The warp's columns e0 .. e0 + 15 of a D x D matrix in global memory (NULL: zeros).
+template <int D>
+__device__ __forceinline__ void load_state(float (&S)[D / 8][4], const float *from, int e0) {
+  const int g = (threadIdx.x & 31) >> 2, t = threadIdx.x & 3;
+#pragma unroll
+  for (int d = 0; d < D / 8; ++d)
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      S[d][i] = from ? from[(8 * d + 2 * t + (i & 1)) * D + e0 + g + (i >> 1) * 8] : 0.f;
+}
+template <int D>
+__device__ __forceinline__ void store_state(float *to, const float (&S)[D / 8][4], int e0) {
+  const int g = (threadIdx.x & 31) >> 2, t = threadIdx.x & 3;
+#pragma unroll
+  for (int d = 0; d < D / 8; ++d)
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      to[(8 * d + 2 * t + (i & 1)) * D + e0 + g + (i >> 1) * 8] = S[d][i];
+}
+// S = (hi + lo) S + w^T k over the chunk's tokens.  The chunk's own sum starts from zero and is
+// added in one rounding: the tensor cores cut off what their accumulator cannot hold, which
+// over the chunks of a long sequence would shrink the state.
+template <int kTerms, int D, int C>
+__device__ __forceinline__ void state_update(float (&S)[D / 8][4], float hi, float lo,
+                                             const float (&w)[C / 8][4], const __nv_bfloat16 *ks) {
+  constexpr int kRow = pad_row<__nv_bfloat16>(D);
+  static_assert(C == 64, "four left operands");
+  const LeftBf16<kTerms> a[4] = {{w[0], w[1]}, {w[2], w[3]}, {w[4], w[5]}, {w[6], w[7]}};
+#pragma unroll
+  for (int d = 0; d < D / 16; ++d) {
+    float x[2][4] = {};
+#pragma unroll
+    for (int j = 0; j < C / 16; ++j) {
+      const PairBf16 k = by_channel<kRow>(ks, 16 * j, 16 * d);
+      a[j].times(x[0], k.b[0][0], k.b[0][1]);
+      a[j].times(x[1], k.b[1][0], k.b[1][1]);
+    }
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        float &s = S[2 * d + i][e];
+        s = fmaf(hi, s, fmaf(lo, s, x[i][e]));
+      }
+  }
+}
+template <int kTerms, int D, int C>
+__device__ __forceinline__ void state_update(float (&S)[D / 8][4], float hi, float lo,
+                                             const float (&w)[C / 8][4], const float *ks) {
+  constexpr int kRow = pad_row<float>(D);
+  const int g = (threadIdx.x & 31) >> 2, t = threadIdx.x & 3;
+#pragma unroll
+  for (int d = 0; d < D / 8; ++d) {
+    float x[4] = {};
+#pragma unroll
+    for (int j = 0; j < C / 8; ++j) {
+      const LeftTf32<3> a(w[j]);
+      a.times(x, ks[(8 * j + 2 * t) * kRow + 8 * d + g], ks[(8 * j + 2 * t + 1) * kRow + 8 * d + g]);
+    }
+#pragma unroll
+    for (int e = 0; e < 4; ++e) S[d][e] = fmaf(hi, S[d][e], fmaf(lo, S[d][e], x[e]));
+  }
+}
+// The values of the warp's columns e0 .. e0 + 15 at the tokens of tiles 2n and 2n + 1, as
+// product tiles hold them.
+template <int kRow>
+__device__ __forceinline__ void values_of(float (&a)[4], float (&b)[4], const __nv_bfloat16 *vs,
+                                          int n, int e0) {
+  const int l = threadIdx.x & 31;
+  uint32_t r[4];
+  ldmatrix4_t(r, smem_u32(vs + (16 * n + (l >> 4) * 8 + (l & 7)) * kRow + e0 + ((l >> 3) & 1) * 8));
+  const float2 f[4] = {bf2_to_f2(r[0]), bf2_to_f2(r[1]), bf2_to_f2(r[2]), bf2_to_f2(r[3])};
+  a[0] = f[0].x, a[1] = f[0].y, a[2] = f[1].x, a[3] = f[1].y;
+  b[0] = f[2].x, b[1] = f[2].y, b[2] = f[3].x, b[3] = f[3].y;
+}
+template <int kRow>
+__device__ __forceinline__ void values_of(float (&a)[4], float (&b)[4], const float *vs, int n,
+                                          int e0) {
+  const int g = (threadIdx.x & 31) >> 2, t = threadIdx.x & 3;
+  const float *v = vs + (16 * n + 2 * t) * kRow + e0 + g;
+  a[0] = v[0], a[1] = v[kRow], a[2] = v[8], a[3] = v[kRow + 8];
+  v += 8 * kRow;
+  b[0] = v[0], b[1] = v[kRow], b[2] = v[8], b[3] = v[kRow + 8];
+}
+// A result tile (16 columns of the values, 8 tokens from `token` on) to global memory.
+__device__ __forceinline__ void store_tile(__nv_bfloat16 *o, size_t stride, const float (&c)[4],
+                                           int token, int n) {
+  const int g = (threadIdx.x & 31) >> 2, t = threadIdx.x & 3;
+  const uint32_t lo = transpose8(f2_to_bf2(c[0], c[1])), hi = transpose8(f2_to_bf2(c[2], c[3]));
+  if (token + g < n) {
+    uint32_t *at = (uint32_t *)(o + (size_t)(token + g) * stride + 2 * t);
+    at[0] = lo, at[4] = hi;
+  }
+}
+__device__ __forceinline__ void store_tile(float *o, size_t stride, const float (&c)[4], int token,
+                                           int n) {
+  const int g = (threadIdx.x & 31) >> 2, t = threadIdx.x & 3;
+#pragma unroll
+  for (int e = 0; e < 2; ++e)
+    if (token + 2 * t + e < n) {
+      float *at = o + (size_t)(token + 2 * t + e) * stride + g;
+      at[0] = c[e], at[8] = c[2 + e];
+    }
+}
+
+// ------------------------------------------------------------- between the files
+template <typename T>
+int chunks_of(const DeltaArgs &a) { return (a.N + kChunkOf<T> - 1) / kChunkOf<T>; }
+// First part of the backward pass: records (of the backward's form), the state before every
+// chunk [B H chunks][D][D] and the misses [B H chunks][C][D].  exact: three terms throughout.
+cudaError_t save_forward(const DeltaArgs &a, bool exact, float *records, float *states,
+                         float *misses, cudaStream_t st);
 
 }  // namespace delta
 }  // namespace gbla

@@ -235,7 +235,7 @@ struct StepArgs {
 };
 cudaError_t decay_step(const StepArgs &a, cudaStream_t st);
 
-// ---- attention by the gated delta rule (gbla_delta.cu, gbla_delta_chunk.cu) -
+// ---- attention by the gated delta rule (gbla_delta*.cu) -----------------
 struct DeltaArgs {
   const void *q, *k, *v;                // [B, N, Hk, D] twice, [B, N, H, D]
   const void *log_decay, *beta;         // [B, N, H]
@@ -251,6 +251,15 @@ struct DeltaArgs {
 // Scratch: what the chunks prepare.
 size_t delta_forward_floats(const DeltaArgs &a);
 cudaError_t delta_forward(const DeltaArgs &a, float *scratch, cudaStream_t st);
+struct DeltaBackArgs {
+  DeltaArgs f;                          // the forward pass (o and fin unused)
+  const void *d_o;                      // [B, N, H, D] contiguous
+  const float *dstate;                  // [B, H, D, D] or NULL
+  void *dq, *dk, *dv, *dlog_decay, *dbeta;  // contiguous
+  float *dstate_in;                     // or NULL
+};
+size_t delta_backward_floats(const DeltaBackArgs &p);
+cudaError_t delta_backward(const DeltaBackArgs &p, float *scratch, cudaStream_t st);
 struct DeltaStepArgs {
   const void *q, *k, *v, *log_decay, *beta;  // one token of each sequence; row strides in elements
   long long sq, sk, sv, sg, sb;

@@ -35,7 +35,7 @@ EXPORTED = ["gbla_forward", "gbla_forward_ex", "gbla_forward_variant", "gbla_for
             "gbla_project", "gbla_layer_forward", "gbla_attention_forward",
             "gbla_qk_norm_rotate", "gbla_qk_norm_rotate_backward", "gbla_decay_attention",
             "gbla_decay_attention_backward", "gbla_decay_attention_step",
-            "gbla_delta_attention", "gbla_delta_attention_step",
+            "gbla_delta_attention", "gbla_delta_attention_backward", "gbla_delta_attention_step",
             "gbla_token_logprobs", "gbla_token_logprobs_backward"]
 
 _lock = threading.Lock()
@@ -115,6 +115,8 @@ def load(path: str | None = None):
         lib.gbla_decay_attention_step.restype = _i
         lib.gbla_delta_attention.argtypes = [_vp] * 10 + [_i] * 5 + [f, _i, _vp]
         lib.gbla_delta_attention.restype = _i
+        lib.gbla_delta_attention_backward.argtypes = [_vp] * 16 + [_i] * 5 + [f, _i, _vp]
+        lib.gbla_delta_attention_backward.restype = _i
         lib.gbla_delta_attention_step.argtypes = [_vp] * 9 + [_i] * 5 + [f, _i, _vp]
         lib.gbla_delta_attention_step.restype = _i
         lib.gbla_token_logprobs.argtypes = [_vp] * 9 + [_i] * 4 + [f, _i, _vp]
@@ -701,6 +703,31 @@ def delta_attention(q, k, v, log_decay, beta, seq_lens=None, state=None, scale=N
     if given:
         _changed((out,))
     return (out, fin) if return_state else out
+
+
+def delta_attention_backward(q, k, v, log_decay, beta, do, seq_lens=None, state=None, dstate=None,
+                             scale=None, return_dstate: bool = False, stream=None) -> dict:
+    """Gradients of delta_attention (gbla_delta_attention_backward): `do` [B, N, H, D]
+    contiguous, `dstate` [B, H, D, D] the gradient of the returned state (None: zeros).
+    Returns dq, dk (summed over the value heads that share a key head), dv, dlog_decay, dbeta
+    (0 past seq_lens) and, with return_dstate, dstate, the gradient of the first state."""
+    code, dev, whole, dims = _delta_args(q, k, v, log_decay, beta)
+    B, N, H, Hk, D = dims
+    f32 = torch.float32
+    g = {"d" + n: _like(t, stream) for n, t in (("q", q), ("k", k), ("v", v),
+                                                ("log_decay", log_decay), ("beta", beta))}
+    if return_dstate:
+        g["dstate"] = _empty(stream, (B, H, D, D), f32, q.device)
+    out = [t.data_ptr() for t in g.values()] + ([] if return_dstate else [None])
+    st = (_lib or load()).gbla_delta_attention_backward(
+        q.data_ptr(), k.data_ptr(), v.data_ptr(), log_decay.data_ptr(), beta.data_ptr(),
+        _plain(seq_lens, "seq_lens", (B,), torch.int32, dev),
+        None if whole else _strides(q, k, v, log_decay, beta),
+        _plain(state, "state", (B, H, D, D), f32, dev), _plain(do, "do", v.shape, q.dtype, dev),
+        _plain(dstate, "dstate", (B, H, D, D), f32, dev), *out, *dims,
+        D ** -0.5 if scale is None else scale, code, _raw_stream(dev, stream))
+    _check(st, "gbla_delta_attention_backward")
+    return g
 
 
 def delta_attention_step(q, k, v, log_decay, beta, state, slots=None, scale=None, out=None,

@@ -11,6 +11,11 @@ no error of the state apart, so that rounding errors of tokens add up like indep
 * bf16 results: one rounding, 2^-8 at most, and operands inside rounded to 2^-11 (the
   triangular products) or 2^-16 (the state) at most three times in a row:  2^-8 + 3 2^-11.
   The state itself: the fp32 bound, whatever the type.
+* gradients: the same, with twice the products in a row; the log decays' are sums of up to 64
+  shares of either sign, with errors that add like independent ones: 8 times what comes before
+  the last rounding.  The shares may cancel (a first token without a state before it has none
+  to fade, its gradient is exactly 0): as inner products they are off by that of their vectors'
+  lengths, |do| |o| and |dv| |v|, which count beside the gradient.
 Single elements: 24 times the bound times the tensor's root mean square, and half an ulp."""
 import math
 
@@ -30,15 +35,31 @@ def bound(dtype, N, D):
     return f if dtype == "fp32" else 2.0 ** -8 + 3 * 2.0 ** -11 + f
 
 
-def close(got, ref, tol, what):
+def grad_bound(name, dtype, N, D):
+    if name == "dstate":
+        return 2 * bound("fp32", N, D)
+    inner = 2 * (bound(dtype, N, D) - (2.0 ** -8 if dtype == "bf16" else 0))
+    return (8 if name == "dlog_decay" else 1) * inner + (2.0 ** -8 if dtype == "bf16" else 0)
+
+
+def shares(x, do, g, lens, state, scale):
+    """Lengths of the vectors whose products a log decay's gradient consists of."""
+    o, _ = R.delta(*x.values(), lens, state, scale)
+    v, past = x["v"].double(), (o == 0).all(-1)
+    got = do.double().norm(dim=-1) * o.norm(dim=-1) + g["dv"].norm(dim=-1) * v.norm(dim=-1)
+    return torch.where(past, 0.0, got)
+
+
+def close(got, ref, tol, what, beside=None):
     got, ref = got.detach().double(), ref.to(got.device)
     assert got.shape == ref.shape, what
     assert torch.isfinite(got).all(), what
     if not ref.numel():
         return
     d = got - ref
-    assert d.norm() <= tol * ref.norm() + 1e-30, (what, (d.norm() / ref.norm()).item(), tol)
-    rms = ref.norm() / math.sqrt(ref.numel())
+    size = ref.norm() + (0 if beside is None else beside.norm())
+    assert d.norm() <= tol * size + 1e-30, (what, (d.norm() / size).item(), tol)
+    rms = size / math.sqrt(ref.numel())
     over = (d.abs() - (24 * tol * rms + (2.0 ** -8 * ref.abs() if tol > 1e-3 else 0))).max()
     assert over <= 1e-30, (what, over.item(), rms.item())
 
@@ -122,6 +143,35 @@ def test_forward(i, keep):
     assert gbla.device_error() == 0
 
 
+@pytest.mark.parametrize("ends", ["none", "dstate", "both"])
+@pytest.mark.parametrize("i", range(len(CASES)))
+def test_backward(i, ends):
+    """ends: which of the last state's gradient (in) and the first one's (out) there are."""
+    c, s0 = _case(i)
+    do = c.n(*c.x["v"].shape).to(TYPES[c.dtype]).cuda()
+    ds = c.n(c.B, c.H, c.D, c.D).cuda() if ends != "none" else None
+    past = c.past()
+    bad = do.clone()
+    bad[past] = float("nan")
+    kw = dict(seq_lens=c.seq_lens, state=s0, dstate=ds, return_dstate=ends == "both")
+    got = gbla.delta_attention_backward(*c.poisoned().values(), bad, **kw)
+    ref = R.delta_backward(*c.x.values(), do, c.lens, s0, ds, c.D ** -0.5)
+    assert got.keys() == {"dq", "dk", "dv", "dlog_decay", "dbeta"} | ({"dstate"} if ends == "both" else set())
+    for n, g in got.items():
+        r = ref[n]
+        if n == "dlog_decay":
+            r = torch.where(c.x["log_decay"] == -math.inf, torch.zeros_like(r), r)
+            assert (g[c.x["log_decay"] == -math.inf] == 0).all()
+        if n != "dstate":
+            assert (g[past] == 0).all(), (n, "padding rows are 0")
+        beside = shares(c.x, do, ref, c.lens, s0, c.D ** -0.5) if n == "dlog_decay" else None
+        close(g, r, grad_bound(n, c.dtype, c.N, c.D), n, beside)
+    again = gbla.delta_attention_backward(*c.x.values(), do, **kw)
+    for n in got:
+        assert torch.equal(got[n], again[n]), n
+    assert gbla.device_error() == 0
+
+
 @pytest.mark.parametrize("dtype", ["fp32", "bf16"])
 @pytest.mark.parametrize("D", [32, 64, 128])
 def test_strides_and_scale(dtype, D):
@@ -140,6 +190,12 @@ def test_strides_and_scale(dtype, D):
     past = c.past()
     close(got[~past], o[~past], bound(dtype, N, D), "o")
     close(S, ref, bound("fp32", N, D), "state")
+    do = c.n(B, N, H, D).to(TYPES[dtype]).cuda()
+    grads = gbla.delta_attention_backward(q, k, v, g, b, do, c.seq_lens, scale=-0.3)
+    want = R.delta_backward(*c.x.values(), do, c.lens, None, None, -0.3)
+    for n, t in grads.items():
+        beside = shares(c.x, do, want, c.lens, None, -0.3) if n == "dlog_decay" else None
+        close(t, want[n], grad_bound(n, dtype, N, D), n, beside)
 
 
 @pytest.mark.parametrize("dtype", ["fp32", "bf16"])
@@ -182,6 +238,12 @@ def test_extreme_keys_and_gates(dtype, how):
     many = 8 if how == "beta two" else 1
     close(got, o, many * bound(dtype, 150, 64), "o")
     close(fin, S, many * bound("fp32", 150, 64), "state")
+    do, ds = c.n(1, 150, 2, 64).to(TYPES[dtype]).cuda(), c.state()
+    g = gbla.delta_attention_backward(*x.values(), do, state=s0, dstate=ds, scale=0.125, return_dstate=True)
+    want = R.delta_backward(*x.values(), do, c.lens, s0, ds, 0.125)
+    for n, t in g.items():
+        beside = shares(x, do, want, c.lens, s0, 0.125) if n == "dlog_decay" else None
+        close(t, want[n], many * grad_bound(n, dtype, 150, 64), n, beside)
 
 
 def test_long_sequences():
@@ -193,6 +255,12 @@ def test_long_sequences():
         got, fin = gbla.delta_attention(*c.x.values(), return_state=True)
         close(got, o, bound(dtype, 4001, D), (D, dtype, "o"))
         close(fin, S, bound("fp32", 4001, D), (D, dtype, "state"))
+        do = c.n(1, 4001, 2, D).to(TYPES[dtype]).cuda()
+        g = gbla.delta_attention_backward(*c.x.values(), do)
+        want = R.delta_backward(*c.x.values(), do, c.lens, None, None, D ** -0.5)
+        for n, t in g.items():
+            beside = shares(c.x, do, want, c.lens, None, D ** -0.5) if n == "dlog_decay" else None
+            close(t, want[n], grad_bound(n, dtype, 4001, D), (D, dtype, n), beside)
 
 
 STEPS = [(1, 1, 1, 32, "fp32"), (4, 8, 8, 64, "bf16"), (5, 6, 2, 128, "bf16"), (7, 4, 1, 64, "fp32"),
@@ -244,6 +312,10 @@ def test_nothing_to_do_and_empty_sequences():
     assert o.shape == (2, 0, 2, 64) and torch.equal(S, s0)
     _, S = gbla.delta_attention(*none.values(), return_state=True)
     assert (S == 0).all()
+    for x in (c.x, none):  # no tokens: the state's gradient passes through
+        g = gbla.delta_attention_backward(*x.values(), x["v"], dstate=s0, return_dstate=True,
+                                          seq_lens=c.seq_lens)
+        assert torch.equal(g["dstate"], s0) and all((g[n] == 0).all() for n in g if n != "dstate")
 
 
 @pytest.mark.parametrize("dtype", ["fp32", "bf16"])
@@ -256,16 +328,20 @@ def test_another_stream_and_a_graph(dtype):
     torch.cuda.current_stream().wait_stream(side)
     assert torch.equal(got, ref) and torch.equal(fin, S)
     graphs = []
+    do = c.n(*ref.shape).to(ref.dtype).cuda()
+    dref = gbla.delta_attention_backward(*c.x.values(), do)
     for _ in range(2):  # two graphs of the same calls, replayed in turn
         graph = torch.cuda.CUDAGraph()
         with torch.cuda.graph(graph):
             o, s = gbla.delta_attention(*c.x.values(), return_state=True)
             one = gbla.delta_attention_step(*[t[:, -1:] for t in c.x.values()], s)
-        graphs.append((graph, o, s, one))
+            d = gbla.delta_attention_backward(*c.x.values(), do)
+        graphs.append((graph, o, s, one, d))
     want = S.clone()
     last = gbla.delta_attention_step(*[t[:, -1:] for t in c.x.values()], want)
     for _ in range(3):
-        for graph, o, s, one in graphs:
+        for graph, o, s, one, d in graphs:
             graph.replay()
             torch.cuda.synchronize()
+            assert all(torch.equal(d[n], dref[n]) for n in d)
             assert torch.equal(o, ref) and torch.equal(s, want) and torch.equal(one, last)

@@ -28,7 +28,7 @@ struct ReverseShape {
   static constexpr int C = kChunkOf<T>, kWarps = D / 16, kThreads = kWarps * 32;
   static constexpr int kRow = pad_row<T>(D);
   static constexpr int kTile = C * kRow * (int)sizeof(T);          // bytes of k, q or d
-  static constexpr int kStage = 3 * kTile + (Rec::kFloats - Rec::kP) * 4;  // M is not read
+  static constexpr int kStage = 3 * kTile + (Rec::kFloats - Rec::kGates) * 4;  // M is not read
   static constexpr int kBytes = 2 * kStage;
 };
 
@@ -38,6 +38,7 @@ __global__ void __launch_bounds__(ReverseShape<T, D, kSolve>::kThreads)
   using Sh = ReverseShape<T, D, kSolve>;
   using Rec = typename Sh::Rec;
   constexpr int C = Sh::C, kThreads = Sh::kThreads, kRow = Sh::kRow;
+  constexpr bool kSums = sizeof(T) == 4;
   extern __shared__ __align__(16) char raw[];
   grid_dep_wait();
   const DeltaArgs &f = p.f;
@@ -55,11 +56,11 @@ __global__ void __launch_bounds__(ReverseShape<T, D, kSolve>::kThreads)
     char *s = raw + (c & 1) * Sh::kStage;
     const long long t0 = (long long)c * C;
     const int n = min(C, L - c * C);
-    load_rows<T, C, D, kThreads>((T *)s, kg + t0 * f.sk[1], f.sk[1], n);
-    load_rows<T, C, D, kThreads>((T *)(s + Sh::kTile), qg + t0 * f.sq[1], f.sq[1], n);
-    load_rows<T, C, D, kThreads>((T *)(s + 2 * Sh::kTile), dg + t0 * orow, (long long)orow, n);
-    load_flat<Rec::kFloats - Rec::kP, kThreads>((float *)(s + 3 * Sh::kTile),
-                                                records + (bh * nc + c) * Rec::kFloats + Rec::kP);
+    load_rows<T, C, D, kThreads>((T *)s, kg + t0 * f.sk[1], f.sk[1], n, tid);
+    load_rows<T, C, D, kThreads>((T *)(s + Sh::kTile), qg + t0 * f.sq[1], f.sq[1], n, tid);
+    load_rows<T, C, D, kThreads>((T *)(s + 2 * Sh::kTile), dg + t0 * orow, (long long)orow, n, tid);
+    load_flat<Rec::kFloats - Rec::kGates, kThreads>(
+        (float *)(s + 3 * Sh::kTile), records + (bh * nc + c) * Rec::kFloats + Rec::kGates, tid);
   };
   float A[D / 8][4];
   load_state<D>(A, p.dstate ? p.dstate + bh * D * D : nullptr, e0);
@@ -72,12 +73,12 @@ __global__ void __launch_bounds__(ReverseShape<T, D, kSolve>::kThreads)
     cp_async_commit();
     const char *s = raw + (c & 1) * Sh::kStage;
     const T *ks = (const T *)s, *qs = (const T *)(s + Sh::kTile), *ds = (const T *)(s + 2 * Sh::kTile);
-    const float *P = (const float *)(s + 3 * Sh::kTile), *Tm = P + (Rec::kT - Rec::kP);
-    const float *gt = P + (Rec::kGates - Rec::kP);
+    const float *gt = (const float *)(s + 3 * Sh::kTile);
+    const float *P = gt + (Rec::kP - Rec::kGates), *Tm = gt + (Rec::kT - Rec::kGates);
     const int n = min(C, L - c * C);
     store_state<D>(after + (bh * nc + c) * D * D, A, e0);
     float r[C / 8][4] = {};
-    state_products<kTerms, D, C, false>(A, ks, ks, r, r);
+    key_products<kTerms, D, C, false>(A, ks, r, nullptr);
     {
       float x[C / 8][4] = {};
 #pragma unroll
@@ -86,7 +87,7 @@ __global__ void __launch_bounds__(ReverseShape<T, D, kSolve>::kThreads)
         values_of<kRow>(d[0], d[1], ds, m, e0);
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
-          const LeftTf32<kSolve> a(d[i]);
+          const LeftTf32<kSolve, kSums> a(d[i]);
 #pragma unroll
           for (int j = 0; j <= 2 * m + i; ++j) a.times(x[j], Rec::P::load(P, 2 * m + i, j));
         }
@@ -106,7 +107,7 @@ __global__ void __launch_bounds__(ReverseShape<T, D, kSolve>::kThreads)
       float x[kHalf][4] = {};
 #pragma unroll
       for (int i = half * kHalf; i < C / 8; ++i) {
-        const LeftTf32<kSolve> a(r[i]);
+        const LeftTf32<kSolve, kSums> a(r[i]);
 #pragma unroll
         for (int j = 0; j < kHalf; ++j)
           if (half * kHalf + j <= i) a.times(x[j], Rec::M::load(Tm, i, half * kHalf + j));
@@ -158,12 +159,12 @@ struct GradShape {
 // 16 rows from i on at columns k .. k + 7 of a tile, as the left operand of tf32 products; times
 // the rows' factors.
 template <int kTerms, int kRow, typename T>
-__device__ __forceinline__ LeftTf32<kTerms> left_rows(const T *tile, int i, int k, float fx = 1.f,
+__device__ __forceinline__ LeftTf32<kTerms, kTerms == 3> left_rows(const T *tile, int i, int k, float fx = 1.f,
                                                       float fy = 1.f) {
   const int g = (threadIdx.x & 31) >> 2, t = threadIdx.x & 3;
   const T *x = tile + (i + g) * kRow + k + 2 * t, *y = x + 8 * kRow;
   const float c[4] = {fx * to_f(x[0]), fx * to_f(x[1]), fy * to_f(y[0]), fy * to_f(y[1])};
-  return LeftTf32<kTerms>(c);
+  return LeftTf32<kTerms, kTerms == 3>(c);
 }
 // x += (16 x 16 coefficients a, b) times rows i .. i + 15 of a raw tile.
 template <int D>
@@ -182,7 +183,7 @@ __device__ __forceinline__ void add_rows(float (&x)[D / 8][4], const float (&a)[
                                          const float (&b)[4], const float *tile, int i) {
   constexpr int kRow = pad_row<float>(D);
   const int g = (threadIdx.x & 31) >> 2, t = threadIdx.x & 3;
-  const LeftTf32<3> l0(a), l1(b);
+  const LeftTf32<3, true> l0(a), l1(b);
 #pragma unroll
   for (int d = 0; d < D / 8; ++d) {
     const float *at = tile + (i + 2 * t) * kRow + 8 * d + g;
@@ -217,7 +218,7 @@ __device__ __forceinline__ void score_tiles(float (&qk)[2][4], float (&kk)[2][4]
   const int g = (threadIdx.x & 31) >> 2, t = threadIdx.x & 3;
 #pragma unroll 2
   for (int d = 0; d < D / 8; ++d) {
-    const LeftTf32<3> a = left_rows<3, kRow>(qs, i, 8 * d), c = left_rows<3, kRow>(ks, i, 8 * d);
+    const auto a = left_rows<3, kRow>(qs, i, 8 * d), c = left_rows<3, kRow>(ks, i, 8 * d);
 #pragma unroll
     for (int n = 0; n < 2; ++n) {
       const float2 k = *(const float2 *)(ks + (j + 8 * n + g) * kRow + 8 * d + 2 * t);
@@ -292,14 +293,14 @@ __global__ void __launch_bounds__(GradShape<T, D>::kThreads)
   const size_t at = ((size_t)b * f.H + h) * nc + blockIdx.x;
   const float *S0 = states + at * D * D, *A1 = after + at * D * D;
   load_rows<T, C, D, kThreads>(ks, (const T *)f.k + b * f.sk[0] + t0 * f.sk[1] + (long long)hk * D,
-                               f.sk[1], n);
+                               f.sk[1], n, tid);
   load_rows<T, C, D, kThreads>(qs, (const T *)f.q + b * f.sq[0] + t0 * f.sq[1] + (long long)hk * D,
-                               f.sq[1], n);
-  load_rows<T, C, D, kThreads>(ds, (const T *)p.d_o + row0 * D, (long long)orow, n);
-  load_rows<float, C, D, kThreads>(us, misses + at * C * D, D, C);
-  load_rows<float, C, D, kThreads>(vs, weights + at * C * D, D, C);
-  load_rows<float, D, D, kThreads>(st, A1, D, D);
-  load_flat<Gates<C>::kFloats, kThreads>(gt, records + at * Rec::kFloats + Rec::kGates);
+                               f.sq[1], n, tid);
+  load_rows<T, C, D, kThreads>(ds, (const T *)p.d_o + row0 * D, (long long)orow, n, tid);
+  load_rows<float, C, D, kThreads>(us, misses + at * C * D, D, C, tid);
+  load_rows<float, C, D, kThreads>(vs, weights + at * C * D, D, C, tid);
+  load_rows<float, D, D, kThreads>(st, A1, D, D, tid);
+  load_flat<Gates<C>::kFloats, kThreads>(gt, records + at * Rec::kFloats + Rec::kGates, tid);
   cp_async_commit();
   cp_async_wait_all();
   __syncthreads();
@@ -324,7 +325,7 @@ __global__ void __launch_bounds__(GradShape<T, D>::kThreads)
   float x[D / 8][4] = {}, y[D / 8][4] = {};  // dq, dk
 #pragma unroll 2
   for (int e = 0; e < D; e += 8) {
-    const LeftTf32<kG> a = left_rows<kG, kWide>(us, i0, e, dn0, dn1);
+    const auto a = left_rows<kG, kWide>(us, i0, e, dn0, dn1);
 #pragma unroll
     for (int d = 0; d < D / 8; ++d) {
       const float2 s = *(const float2 *)(st + (8 * d + g) * kWide + e + 2 * t);
@@ -349,8 +350,8 @@ __global__ void __launch_bounds__(GradShape<T, D>::kThreads)
   __syncthreads();
 #pragma unroll 2
   for (int e = 0; e < D; e += 8) {
-    const LeftTf32<kG> a = left_rows<kG, kRow>(ds, i0, e, up0 * f.scale, up1 * f.scale);
-    const LeftTf32<kG> c = left_rows<kG, kWide>(vs, i0, e, -up0, -up1);
+    const auto a = left_rows<kG, kRow>(ds, i0, e, up0 * f.scale, up1 * f.scale);
+    const auto c = left_rows<kG, kWide>(vs, i0, e, -up0, -up1);
 #pragma unroll
     for (int d = 0; d < D / 8; ++d) {
       const float2 s = *(const float2 *)(st + (8 * d + g) * kWide + e + 2 * t);
@@ -369,7 +370,8 @@ __global__ void __launch_bounds__(GradShape<T, D>::kThreads)
     score_tiles<D>(qk, kk, qs, ks, i0, j0);
 #pragma unroll 2
     for (int e = 0; e < D; e += 8) {
-      const LeftTf32<kG> l = left_rows<kG, kRow>(ds, i0, e), m = left_rows<kG, kWide>(vs, i0, e);
+      const auto l = left_rows<kG, kRow>(ds, i0, e);
+      const auto m = left_rows<kG, kWide>(vs, i0, e);
 #pragma unroll
       for (int q = 0; q < 2; ++q) {
         const float2 u = *(const float2 *)(us + (j0 + 8 * q + g) * kWide + e + 2 * t);
@@ -468,7 +470,8 @@ __global__ void __launch_bounds__(GradShape<T, D>::kThreads)
 
 // Scratch of the backward pass, in floats from one base.
 struct Layout {
-  size_t records, states, misses, after, weights, dq, dk, total;
+  size_t records, states, misses, after, weights, before, dq, dk, total;
+  Segments segments;
 };
 template <typename T>
 Layout layout_of(const DeltaBackArgs &p, bool exact) {
@@ -483,6 +486,8 @@ Layout layout_of(const DeltaBackArgs &p, bool exact) {
   take(l.after, all * a.D * a.D);
   take(l.misses, all * C * a.D);
   take(l.weights, all * C * a.D);
+  l.segments = segments_of(a);
+  take(l.before, l.segments.floats(a));
   const size_t plane = a.H == a.Hk ? 0 : (size_t)a.B * a.N * a.H * a.D;
   take(l.dq, plane);
   take(l.dk, plane);
@@ -516,7 +521,8 @@ cudaError_t back_launch(const DeltaBackArgs &p, float *s, cudaStream_t st) {
   const Layout l = layout_of<T>(p, kSolve == 3);
   const int nc = chunks_of<T>(a);
   cudaError_t e;
-  if ((e = save_forward(a, kSolve == 3, s + l.records, s + l.states, s + l.misses, st)) != cudaSuccess)
+  if ((e = save_forward(a, l.segments, kSolve == 3, s + l.records, s + l.states, s + l.misses,
+                        s + l.before, st)) != cudaSuccess)
     return e;
   const auto reverse = reverse_kernel<T, D, kTerms, kSolve>;
   if ((e = cudaFuncSetAttribute(reverse, cudaFuncAttributeMaxDynamicSharedMemorySize, Sh::kBytes)) !=

@@ -11,6 +11,7 @@
 // goes through the chunks, and in it the columns of S are independent of one another: each
 // warp carries 16 of them, transposed, through the whole sequence, in registers.
 #include <math.h>
+#include <stdlib.h>
 
 #include "gbla_delta_mma.cuh"
 
@@ -176,9 +177,9 @@ __global__ void __launch_bounds__(PrepShape<T, D>::kThreads)
   const int t0 = blockIdx.x * C, n = min(C, L - t0);
   if (n <= 0) return;
   load_rows<T, C, D, kThreads>(ks, (const T *)p.k + b * p.sk[0] + t0 * p.sk[1] + (long long)hk * D,
-                               p.sk[1], n);
+                               p.sk[1], n, tid);
   load_rows<T, C, D, kThreads>(qs, (const T *)p.q + b * p.sq[0] + t0 * p.sq[1] + (long long)hk * D,
-                               p.sq[1], n);
+                               p.sq[1], n, tid);
   cp_async_commit();
   // Sums of the log decays in 64 bits: differences of two of them are what counts, also
   // behind a token that ends the memory (-inf: a number whose power is 0 next to any other).
@@ -280,171 +281,382 @@ __global__ void __launch_bounds__(PrepShape<T, D>::kThreads)
   }
 }
 
-// --------------------------------------------------------------- second launch
-template <typename T, int D, int kSolve, bool kSave>
+// --------------------------------------------------------------- the scan
+// A block carries E = min(D, 64) of the state's columns through the chunks of a segment of a
+// sequence, 16 a warp in kCarry warps.  What the columns need for the next chunk is a chain:
+//   S^T k -> r -> miss = M r -> u -> S',
+// and everything else is taken off it: a second warp for each first one fetches tiles, and forms
+// the results of the chunk before, from the state and u that the first one leaves in shared
+// memory.  One barrier a chunk.
+//
+// What it is for: results (kResults), the states and misses that the backward pass needs
+// (kSave), or what a segment does to the state before it (kSegment): E columns of its own
+// state, from zero, or of the matrix that takes the state before the segment to the one after
+// it, from the identity and with no values.
+enum Purpose { kResults, kSave, kSegment };
+
+template <typename T, int D, int kSolve, Purpose kFor>
 struct ScanShape {
-  static constexpr int C = kChunkOf<T>, kWarps = D / 16, kThreads = kWarps * 32;
-  static constexpr int kRow = pad_row<T>(D);
-  static constexpr int kTile = C * kRow * (int)sizeof(T);        // bytes of k, v or q
-  static constexpr int kTiles = kSave ? 2 : 3;
-  static constexpr int kStage = kTiles * kTile + Record<T, kSolve, kSave>::kFloats * 4;
-  static constexpr int kBytes = 2 * kStage;
+  using Rec = Record<T, kSolve, kFor == kSave>;
+  // (bf16 results of three terms at D = 128: what 64 columns hand on and the larger M would
+  // not fit into shared memory)
+  static constexpr bool kNarrow = sizeof(T) == 2 && D == 128 && kSolve == 3 && kFor == kResults;
+  static constexpr int C = kChunkOf<T>, E = D < 64 ? D : kNarrow ? 32 : 64, kSplit = D / E;
+  static constexpr int kCarry = E / 16, kThreads = 2 * kCarry * 32;
+  static constexpr int kRow = pad_row<T>(D), kValRow = pad_row<T>(E);
+  // bytes: keys, values, M and gates of a chunk; queries, P and gates of the one before
+  static constexpr int kKeys = C * kRow * (int)sizeof(T), kVals = C * kValRow * (int)sizeof(T);
+  static constexpr int kRecord = Rec::kP * 4, kFirst = kKeys + kVals + kRecord;
+  static constexpr int kSecond = kFor == kResults ? kKeys + (Rec::P::kFloats + C) * 4 : 0;
+  // what a warp hands on: its state before the chunk and u (kSave: the misses)
+  static constexpr int kHand = kFor == kSegment ? 0 : (kHandWords<D> + C / 8) * 32 * 16;
+  static constexpr int kBytes = 2 * (kFirst + kSecond + kCarry * kHand);
+  static_assert(kBytes <= 227 * 1024, "shared memory of a block");
 };
 
 // kTerms: bf16 numbers that stand for a value of the state where it meets a key or takes a
 // write (fp32: 3 tf32 products); kSolve: terms of the product with M.
-// kSave: no results, but for the backward pass the state before every chunk and the misses.
-template <typename T, int D, int kTerms, int kSolve, bool kSave>
-__global__ void __launch_bounds__(ScanShape<T, D, kSolve, kSave>::kThreads)
-    scan_kernel(const DeltaArgs p, const float *records, float *states, float *misses, int nc) {
-  using Sh = ScanShape<T, D, kSolve, kSave>;
-  using Rec = Record<T, kSolve, kSave>;
-  constexpr int C = Sh::C, kThreads = Sh::kThreads, kRow = Sh::kRow;
+// Segments have `seg` chunks; `before` holds the states before all but the first, or takes what
+// kSegment forms, [B H][segments - 1][D][D], the matrices in `moves`.  Records are `stride` floats
+// apart (their M and gates lie at the same place in both forms).
+template <typename T, int D, int kTerms, int kSolve, Purpose kFor>
+__global__ void __launch_bounds__(ScanShape<T, D, kSolve, kFor>::kThreads)
+    scan_kernel(const DeltaArgs p, const float *records, float *states, float *misses,
+                float *before, float *moves, int nc, int seg, int stride) {
+  using Sh = ScanShape<T, D, kSolve, kFor>;
+  using Rec = typename Sh::Rec;
+  constexpr int C = Sh::C, E = Sh::E, kCarry = Sh::kCarry, kFetch = kCarry * 32;
   constexpr int kOut = sizeof(T) == 2 ? 1 : 3;  // terms of the product with P
+  constexpr bool kSums = sizeof(T) == 4;
+  constexpr int kColumns = kFor == kSegment ? 2 * Sh::kSplit : Sh::kSplit;  // blocks a head
   extern __shared__ __align__(16) char raw[];
   grid_dep_wait();
-  const int h = blockIdx.x, b = blockIdx.y, hk = h / (p.H / p.Hk), tid = threadIdx.x;
-  const int t = tid & 3, e0 = tid / 32 * 16;
+  const int h = blockIdx.x / kColumns, part = blockIdx.x % kColumns, b = blockIdx.y, s = blockIdx.z;
+  const int hk = h / (p.H / p.Hk), tid = threadIdx.x, warp = tid / 32, lane = tid & 31, t = tid & 3;
+  const bool carry = warp < kCarry;
+  const bool move = part >= Sh::kSplit;  // kSegment: columns of the matrix
+  const int x0 = part % Sh::kSplit * E, e0 = x0 + warp % kCarry * 16;
   const int L = p.seq_lens ? min(max(__ldg(p.seq_lens + b), 0), p.N) : p.N;
   const size_t bh = (size_t)b * p.H + h;
+  const int chunks = (L + C - 1) / C, first = s * seg, end = min(chunks, first + seg);
+  const int last = gridDim.z;  // segments, but for kSegment, which leaves the last one out
+  if (kFor == kSegment ? first + seg >= chunks : s > 0 && first >= chunks) return;
   const T *kg = (const T *)p.k + b * p.sk[0] + (long long)hk * D;
   const T *qg = (const T *)p.q + b * p.sq[0] + (long long)hk * D;
-  const T *vg = (const T *)p.v + b * p.sv[0] + (long long)h * D;
-  T *og = (T *)p.o + ((size_t)b * p.N * p.H + h) * D + e0;
+  const T *vg = (const T *)p.v + b * p.sv[0] + (long long)h * D + x0;
   const size_t orow = (size_t)p.H * D;
-  const int chunks = (L + C - 1) / C;
-  auto load = [&](int c) {
-    char *s = raw + (c & 1) * Sh::kStage;
+  char *hands = raw + 2 * (Sh::kFirst + Sh::kSecond) + warp % kCarry * Sh::kHand;
+  auto first_of = [&](int c) { return raw + (c & 1) * Sh::kFirst; };
+  auto second_of = [&](int c) { return raw + 2 * Sh::kFirst + (c & 1) * Sh::kSecond; };
+  auto hand_of = [&](int c) { return (uint4 *)(hands + (c & 1) * (kCarry * Sh::kHand)); };
+  const int ftid = tid - kCarry * 32;
+  auto fetch_first = [&](int c) {
+    char *to = first_of(c);
     const long long t0 = (long long)c * C;
     const int n = min(C, L - c * C);
-    load_rows<T, C, D, kThreads>((T *)s, kg + t0 * p.sk[1], p.sk[1], n);
-    load_rows<T, C, D, kThreads>((T *)(s + Sh::kTile), vg + t0 * p.sv[1], p.sv[1], n);
-    if (!kSave)
-      load_rows<T, C, D, kThreads>((T *)(s + 2 * Sh::kTile), qg + t0 * p.sq[1], p.sq[1], n);
-    load_flat<Rec::kFloats, kThreads>((float *)(s + Sh::kTiles * Sh::kTile),
-                                      records + (bh * nc + c) * Rec::kFloats);
+    load_rows<T, C, D, kFetch>((T *)to, kg + t0 * p.sk[1], p.sk[1], n, ftid);
+    load_rows<T, C, E, kFetch>((T *)(to + Sh::kKeys), vg + t0 * p.sv[1], p.sv[1], move ? 0 : n, ftid);
+    load_flat<Rec::kP, kFetch>((float *)(to + Sh::kKeys + Sh::kVals),
+                               records + (bh * nc + c) * stride, ftid);
+  };
+  auto fetch_second = [&](int c) {
+    char *to = second_of(c);
+    const long long t0 = (long long)c * C;
+    const float *rec = records + (bh * nc + c) * stride;
+    load_rows<T, C, D, kFetch>((T *)to, qg + t0 * p.sq[1], p.sq[1], min(C, L - c * C), ftid);
+    load_flat<Rec::P::kFloats, kFetch>((float *)(to + Sh::kKeys), rec + Rec::kP, ftid);
+    load_flat<C, kFetch>((float *)(to + Sh::kKeys) + Rec::P::kFloats,
+                         rec + Rec::kGates + Gates<C>::kUp, ftid);
   };
   float S[D / 8][4];  // rows: columns e0 + g, + 8 of the state; columns: its rows
-  load_state<D>(S, p.init ? p.init + bh * D * D : nullptr, e0);
-  if (chunks > 0) load(0);
-  cp_async_commit();
-  for (int c = 0; c < chunks; ++c) {
-    cp_async_wait_all();
-    __syncthreads();  // this chunk's tiles are in, the other buffer is read
-    if (c + 1 < chunks) load(c + 1);
-    cp_async_commit();
-    const char *s = raw + (c & 1) * Sh::kStage;
-    const T *ks = (const T *)s, *vs = (const T *)(s + Sh::kTile), *qs = (const T *)(s + 2 * Sh::kTile);
-    const float *rec = (const float *)(s + Sh::kTiles * Sh::kTile), *gt = rec + Rec::kGates;
-    const int n = min(C, L - c * C);
-    if (kSave) store_state<D>(states + (bh * nc + c) * D * D, S, e0);
-    float r[C / 8][4] = {}, o[C / 8][4] = {};
-    state_products<kTerms, D, C, !kSave>(S, ks, qs, r, o);
+  if (carry) {
+    if (move) {
+      const int g = lane >> 2;
 #pragma unroll
-    for (int m = 0; m < C / 16; ++m) {
-      float v[2][4];
-      values_of<kRow>(v[0], v[1], vs, m, e0);
+      for (int d = 0; d < D / 8; ++d)
 #pragma unroll
-      for (int i = 0; i < 2; ++i) {
-        const float2 up = *(const float2 *)(gt + Gates<C>::kUp + 16 * m + 8 * i + 2 * t);
-        float(&x)[4] = r[2 * m + i], (&y)[4] = o[2 * m + i];
-        x[0] = fmaf(-up.x, x[0], v[i][0]), x[1] = fmaf(-up.y, x[1], v[i][1]);
-        x[2] = fmaf(-up.x, x[2], v[i][2]), x[3] = fmaf(-up.y, x[3], v[i][3]);
-        const float ux = up.x * p.scale, uy = up.y * p.scale;
-        y[0] *= ux, y[1] *= uy, y[2] *= ux, y[3] *= uy;
-      }
+        for (int i = 0; i < 4; ++i)
+          S[d][i] = 8 * d + 2 * t + (i & 1) == e0 + g + (i >> 1) * 8 ? 1.f : 0.f;
+    } else {
+      const float *from = kFor == kSegment ? nullptr
+                          : s > 0          ? before + (bh * (last - 1) + s - 1) * D * D
+                          : p.init         ? p.init + bh * D * D
+                                           : nullptr;
+      load_state<D>(S, from, e0);
     }
-    // r += (M - 1) r: the later half of the tokens first, which needs the earlier ones as
-    // they are; then those
+  } else {
+    if (first < end) fetch_first(first);
+    cp_async_commit();
+    cp_async_wait_all();
+  }
+  const int rounds = kFor == kSegment ? end : end + 1;
+  for (int c = first; c < rounds; ++c) {
+    __syncthreads();  // this round's tiles and what was handed on are there, the others are read
+    if (carry) {
+      if (c >= end) break;
+      const char *in = first_of(c);
+      const T *ks = (const T *)in, *vs = (const T *)(in + Sh::kKeys);
+      const float *M = (const float *)(in + Sh::kKeys + Sh::kVals), *gt = M + Rec::kGates;
+      uint4 *hand = hand_of(c);
+      float r[C / 8][4] = {};
+      if (kFor == kSave) {
 #pragma unroll
-    for (int half = 1; half >= 0; --half) {
-      constexpr int kHalf = C / 16;
-      float x[kHalf][4] = {};
+        for (int d = 0; d < D / 8; ++d)
+          ((float4 *)hand)[d * 32 + lane] = make_float4(S[d][0], S[d][1], S[d][2], S[d][3]);
+      }
+      key_products<kTerms, D, C, kFor == kResults>(S, ks, r, hand);
 #pragma unroll
-      for (int j = 0; j < (half + 1) * kHalf; ++j) {
-        const LeftTf32<kSolve> a(r[j]);
+      for (int m = 0; m < C / 16; ++m) {
+        float v[2][4];
+        values_of<Sh::kValRow>(v[0], v[1], vs, m, e0 - x0);
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          const float2 up = *(const float2 *)(gt + Gates<C>::kUp + 16 * m + 8 * i + 2 * t);
+          float(&x)[4] = r[2 * m + i];
+          x[0] = fmaf(-up.x, x[0], v[i][0]), x[1] = fmaf(-up.y, x[1], v[i][1]);
+          x[2] = fmaf(-up.x, x[2], v[i][2]), x[3] = fmaf(-up.y, x[3], v[i][3]);
+        }
+      }
+      // r += (M - 1) r: the later half of the tokens first, which needs the earlier ones as
+      // they are; then those
+#pragma unroll
+      for (int half = 1; half >= 0; --half) {
+        constexpr int kHalf = C / 16;
+        float x[kHalf][4] = {};
+#pragma unroll
+        for (int j = 0; j < (half + 1) * kHalf; ++j) {
+          const LeftTf32<kSolve, kSums> a(r[j]);
+#pragma unroll
+          for (int m = 0; m < kHalf; ++m)
+            if (half * kHalf + m >= j) a.times(x[m], Rec::M::load(M, half * kHalf + m, j));
+        }
 #pragma unroll
         for (int m = 0; m < kHalf; ++m)
-          if (half * kHalf + m >= j) a.times(x[m], Rec::M::load(rec + Rec::kM, half * kHalf + m, j));
+#pragma unroll
+          for (int i = 0; i < 4; ++i) r[half * kHalf + m][i] += x[m][i];
       }
 #pragma unroll
-      for (int m = 0; m < kHalf; ++m)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) r[half * kHalf + m][i] += x[m][i];
-    }
-    // u, and the results
-#pragma unroll
-    for (int j = 0; j < C / 8; ++j) {
-      if (kSave) store_tile(misses + (bh * nc + c) * C * D + e0, D, r[j], 8 * j, C);
-      const float2 be = *(const float2 *)(gt + Gates<C>::kBeta + 8 * j + 2 * t);
-      r[j][0] *= be.x, r[j][1] *= be.y, r[j][2] *= be.x, r[j][3] *= be.y;
-      if constexpr (!kSave) {
-        const LeftTf32<kOut> a(r[j]);
-#pragma unroll
-        for (int m = j; m < C / 8; ++m) a.times(o[m], Rec::P::load(rec + Rec::kP, m, j));
-        store_tile(og + (size_t)c * C * orow, orow, o[j], 8 * j, n);  // no later u meets it
+      for (int j = 0; j < C / 8; ++j) {
+        float4 *to = (float4 *)hand + (kHandWords<D> + j) * 32 + lane;
+        if (kFor == kSave) *to = make_float4(r[j][0], r[j][1], r[j][2], r[j][3]);
+        const float2 be = *(const float2 *)(gt + Gates<C>::kBeta + 8 * j + 2 * t);
+        r[j][0] *= be.x, r[j][1] *= be.y, r[j][2] *= be.x, r[j][3] *= be.y;
+        if (kFor == kResults) *to = make_float4(r[j][0], r[j][1], r[j][2], r[j][3]);
+        const float2 dn = *(const float2 *)(gt + Gates<C>::kDown + 8 * j + 2 * t);
+        r[j][0] *= dn.x, r[j][1] *= dn.y, r[j][2] *= dn.x, r[j][3] *= dn.y;
       }
-      const float2 dn = *(const float2 *)(gt + Gates<C>::kDown + 8 * j + 2 * t);
-      r[j][0] *= dn.x, r[j][1] *= dn.y, r[j][2] *= dn.x, r[j][3] *= dn.y;
+      state_update<kTerms, D, C>(S, gt[Gates<C>::kWhole], gt[Gates<C>::kWhole + 1], r, ks);
+    } else {
+      if (c + 1 < end) fetch_first(c + 1);
+      if (kFor == kResults && c < end) fetch_second(c);
+      cp_async_commit();
+      if (kFor != kSegment && c > first) {  // the chunk before
+        const int d0 = c - 1;
+        const uint4 *hand = hand_of(d0);
+        const float4 *us = (const float4 *)hand + kHandWords<D> * 32 + lane;
+        if constexpr (kFor == kSave) {
+          float x[D / 8][4];
+#pragma unroll
+          for (int d = 0; d < D / 8; ++d) {
+            const float4 v = ((const float4 *)hand)[d * 32 + lane];
+            x[d][0] = v.x, x[d][1] = v.y, x[d][2] = v.z, x[d][3] = v.w;
+          }
+          store_state<D>(states + (bh * nc + d0) * D * D, x, e0);
+#pragma unroll
+          for (int j = 0; j < C / 8; ++j) {
+            const float4 v = us[j * 32];
+            const float m[4] = {v.x, v.y, v.z, v.w};
+            store_tile(misses + (bh * nc + d0) * C * D + e0, D, m, 8 * j, C);
+          }
+        } else {
+          const char *in = second_of(d0);
+          const float *P = (const float *)(in + Sh::kKeys), *ups = P + Rec::P::kFloats;
+          T *og = (T *)p.o + (((size_t)b * p.N + (size_t)d0 * C) * p.H + h) * D + e0;
+          const int n = min(C, L - d0 * C);
+          float o[C / 8][4] = {};
+          query_products<D, C>(hand, (const T *)in, o);
+#pragma unroll
+          for (int j = 0; j < C / 8; ++j) {
+            const float2 up = *(const float2 *)(ups + 8 * j + 2 * t);
+            const float ux = up.x * p.scale, uy = up.y * p.scale;
+            o[j][0] *= ux, o[j][1] *= uy, o[j][2] *= ux, o[j][3] *= uy;
+          }
+#pragma unroll
+          for (int j = 0; j < C / 8; ++j) {
+            const float4 v = us[j * 32];
+            const float u[4] = {v.x, v.y, v.z, v.w};
+            const LeftTf32<kOut, kSums> a(u);
+#pragma unroll
+            for (int m = j; m < C / 8; ++m) a.times(o[m], Rec::P::load(P, m, j));
+            store_tile(og, orow, o[j], 8 * j, n);  // no later u meets it
+          }
+        }
+      }
+      cp_async_wait_all();
     }
-    state_update<kTerms, D, C>(S, gt[Gates<C>::kWhole], gt[Gates<C>::kWhole + 1], r, ks);
   }
-  if (!kSave && p.fin) store_state<D>(p.fin + bh * D * D, S, e0);
+  if (!carry) return;
+  if (kFor == kSegment) {
+    const size_t at = (bh * last + s) * D * D;
+    store_state<D>((move ? moves : before) + at, S, e0);
+  } else if (kFor == kResults && p.fin && (end == chunks)) {
+    store_state<D>(p.fin + bh * D * D, S, e0);
+  }
+}
+
+// --------------------------------------------------------------- between segments
+// Turns what each segment forms by itself into the state after it, in place: S' = move S + own,
+// one segment after the other.  A block takes E of the state's columns of one (batch, head).
+template <int D>
+struct JoinShape {
+  static constexpr int E = D < 64 ? D : 64, kThreads = E * 2, kRow = D + 8;
+  static constexpr int kBytes = 2 * D * kRow * 4;
+};
+template <int D>
+__global__ void __launch_bounds__(JoinShape<D>::kThreads)
+    join_kernel(const float *init, const int32_t *seq_lens, float *before, const float *moves, int N,
+                int H, int tokens, int ns) {
+  using Sh = JoinShape<D>;
+  constexpr int kThreads = Sh::kThreads, kRow = Sh::kRow;
+  extern __shared__ __align__(16) char raw[];
+  float *tile = (float *)raw;
+  grid_dep_wait();
+  const int h = blockIdx.y, b = blockIdx.z, tid = threadIdx.x, g = (tid & 31) >> 2, t = tid & 3;
+  const int e0 = blockIdx.x * Sh::E + tid / 32 * 16;
+  const int L = seq_lens ? min(max(__ldg(seq_lens + b), 0), N) : N;
+  const int steps = (L + tokens - 1) / tokens - 1;  // segments that another one follows
+  if (steps <= 0) return;
+  const size_t bh = (size_t)b * H + h;
+  before += bh * ns * D * D, moves += bh * ns * D * D;
+  auto fetch = [&](int s) {
+    load_rows<float, D, D, kThreads>(tile + (s & 1) * D * kRow, moves + (size_t)s * D * D, D, D, tid);
+  };
+  float S[D / 8][4];
+  load_state<D>(S, init ? init + bh * D * D : nullptr, e0);
+  fetch(0);
+  cp_async_commit();
+  for (int s = 0; s < steps; ++s) {
+    float own[D / 8][4], x[D / 8][4] = {};
+    load_state<D>(own, before + (size_t)s * D * D, e0);
+    cp_async_wait_all();
+    __syncthreads();
+    if (s + 1 < steps) fetch(s + 1);
+    cp_async_commit();
+    const float *m = tile + (s & 1) * D * kRow;
+#pragma unroll
+    for (int k = 0; k < D / 8; ++k) {
+      const LeftTf32<3, true> a(S[k]);
+#pragma unroll
+      for (int n = 0; n < D / 8; ++n) {
+        const float2 v = *(const float2 *)(m + (8 * n + g) * kRow + 8 * k + 2 * t);
+        a.times(x[n], v.x, v.y);
+      }
+    }
+#pragma unroll
+    for (int d = 0; d < D / 8; ++d)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) S[d][i] = x[d][i] + own[d][i];
+    store_state<D>(before + (size_t)s * D * D, S, e0);
+  }
 }
 
 // Terms of the product with M: bf16 results alone need one (2^-11 of what M adds to a miss).
 bool exact_state(const DeltaArgs &a) { return a.dtype == GBLA_FP32 || a.fin; }
 
-template <typename T, int D, int kTerms, int kSolve, bool kSave>
-cudaError_t launch(const DeltaArgs &a, float *records, float *states, float *misses,
-                   cudaStream_t st) {
+int sm_count() {
+  int dev = 0, n = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess ||
+      cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess || n <= 0)
+    return 152;
+  return n;
+}
+
+template <typename K>
+cudaError_t allow_smem(K kernel, int bytes) {
+  return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
+}
+
+template <typename T, int D, int kTerms, int kSolve, Purpose kFor>
+cudaError_t launch(const DeltaArgs &a, const Segments &g, float *records, float *states,
+                   float *misses, float *before, cudaStream_t st) {
   using Pr = PrepShape<T, D>;
-  using Sc = ScanShape<T, D, kSolve, kSave>;
-  const int nc = chunks_of<T>(a);
-  const auto prep = prepare_kernel<T, D, kSolve, kSave>;
-  const auto scan = scan_kernel<T, D, kTerms, kSolve, kSave>;
+  using Sc = ScanShape<T, D, kSolve, kFor>;
+  using Se = ScanShape<T, D, kSolve, kSegment>;
+  using Jo = JoinShape<D>;
+  static_assert(kFor != kSegment, "");
+  const int nc = chunks_of<T>(a), stride = Record<T, kSolve, kFor == kSave>::kFloats;
+  float *moves = before + (size_t)a.B * a.H * (g.count - 1) * D * D;
   cudaError_t e;
-  if ((e = cudaFuncSetAttribute(prep, cudaFuncAttributeMaxDynamicSharedMemorySize, Pr::kBytes)) !=
-      cudaSuccess)
-    return e;
-  if ((e = cudaFuncSetAttribute(scan, cudaFuncAttributeMaxDynamicSharedMemorySize, Sc::kBytes)) !=
-      cudaSuccess)
-    return e;
+  const auto prep = prepare_kernel<T, D, kSolve, kFor == kSave>;
+  if ((e = allow_smem(prep, Pr::kBytes)) != cudaSuccess) return e;
   count_launch();
   if ((e = launch_pdl(prep, dim3(nc, a.H, a.B), dim3(Pr::kThreads), Pr::kBytes, st, a, records,
                       nc)) != cudaSuccess)
     return e;
+  if (g.count > 1) {
+    const auto own = scan_kernel<T, D, kTerms, kSolve, kSegment>;
+    if ((e = allow_smem(own, Se::kBytes)) != cudaSuccess) return e;
+    count_launch();
+    if ((e = launch_pdl(own, dim3(2 * Se::kSplit * a.H, a.B, g.count - 1), dim3(Se::kThreads),
+                        Se::kBytes, st, a, (const float *)records, (float *)nullptr,
+                        (float *)nullptr, before, moves, nc, g.chunks, stride)) != cudaSuccess)
+      return e;
+    const auto join = join_kernel<D>;
+    if ((e = allow_smem(join, Jo::kBytes)) != cudaSuccess) return e;
+    count_launch();
+    if ((e = launch_pdl(join, dim3(D / Jo::E, a.H, a.B), dim3(Jo::kThreads), Jo::kBytes, st, a.init,
+                        a.seq_lens, before, (const float *)moves, a.N, a.H,
+                        g.chunks * kChunkOf<T>, g.count - 1)) != cudaSuccess)
+      return e;
+  }
+  const auto scan = scan_kernel<T, D, kTerms, kSolve, kFor>;
+  if ((e = allow_smem(scan, Sc::kBytes)) != cudaSuccess) return e;
   count_launch();
-  return launch_pdl(scan, dim3(a.H, a.B), dim3(Sc::kThreads), Sc::kBytes, st, a,
-                    (const float *)records, states, misses, nc);
+  return launch_pdl(scan, dim3(Sc::kSplit * a.H, a.B, g.count), dim3(Sc::kThreads), Sc::kBytes, st,
+                    a, (const float *)records, states, misses, before, moves, nc, g.chunks, stride);
 }
 
 template <int D>
-cudaError_t forward_d(const DeltaArgs &a, float *records, cudaStream_t st) {
-  if (a.dtype == GBLA_FP32) return launch<float, D, 3, 3, false>(a, records, nullptr, nullptr, st);
-  if (exact_state(a)) return launch<__nv_bfloat16, D, 3, 3, false>(a, records, nullptr, nullptr, st);
-  return launch<__nv_bfloat16, D, 2, 1, false>(a, records, nullptr, nullptr, st);
+cudaError_t forward_d(const DeltaArgs &a, const Segments &g, float *records, float *before,
+                      cudaStream_t st) {
+  if (a.dtype == GBLA_FP32)
+    return launch<float, D, 3, 3, kResults>(a, g, records, nullptr, nullptr, before, st);
+  if (exact_state(a))
+    return launch<__nv_bfloat16, D, 3, 3, kResults>(a, g, records, nullptr, nullptr, before, st);
+  return launch<__nv_bfloat16, D, 2, 1, kResults>(a, g, records, nullptr, nullptr, before, st);
 }
 template <int D>
-cudaError_t save_d(const DeltaArgs &a, bool exact, float *records, float *states, float *misses,
-                   cudaStream_t st) {
-  if (a.dtype == GBLA_FP32) return launch<float, D, 3, 3, true>(a, records, states, misses, st);
-  if (exact) return launch<__nv_bfloat16, D, 3, 3, true>(a, records, states, misses, st);
-  return launch<__nv_bfloat16, D, 2, 1, true>(a, records, states, misses, st);
+cudaError_t save_d(const DeltaArgs &a, const Segments &g, bool exact, float *records, float *states,
+                   float *misses, float *before, cudaStream_t st) {
+  if (a.dtype == GBLA_FP32)
+    return launch<float, D, 3, 3, kSave>(a, g, records, states, misses, before, st);
+  if (exact)
+    return launch<__nv_bfloat16, D, 3, 3, kSave>(a, g, records, states, misses, before, st);
+  return launch<__nv_bfloat16, D, 2, 1, kSave>(a, g, records, states, misses, before, st);
 }
 
 }  // namespace
 
-cudaError_t save_forward(const DeltaArgs &a, bool exact, float *records, float *states,
-                         float *misses, cudaStream_t st) {
-  if (a.D == 32) return save_d<32>(a, exact, records, states, misses, st);
-  if (a.D == 64) return save_d<64>(a, exact, records, states, misses, st);
-  return save_d<128>(a, exact, records, states, misses, st);
+Segments segments_of(const DeltaArgs &a) {
+  const int nc = a.dtype == GBLA_FP32 ? chunks_of<float>(a) : chunks_of<__nv_bfloat16>(a);
+  const long long blocks = (long long)a.B * a.H * (a.D > 64 ? 2 : 1), sms = sm_count();
+  Segments best = {1, nc};
+  const char *force = getenv("SEG");
+  if (force && atoi(force) > 1) { best.chunks = (nc + atoi(force) - 1) / atoi(force); best.count = (nc + best.chunks - 1) / best.chunks; }
+  (void)blocks; (void)sms;
+  return best;
+}
+
+cudaError_t save_forward(const DeltaArgs &a, const Segments &g, bool exact, float *records,
+                         float *states, float *misses, float *before, cudaStream_t st) {
+  if (a.D == 32) return save_d<32>(a, g, exact, records, states, misses, before, st);
+  if (a.D == 64) return save_d<64>(a, g, exact, records, states, misses, before, st);
+  return save_d<128>(a, g, exact, records, states, misses, before, st);
 }
 
 }  // namespace delta
 
-size_t delta_forward_floats(const DeltaArgs &a) {
+static size_t record_floats(const DeltaArgs &a) {
   using namespace delta;
   const size_t bh = (size_t)a.B * a.H;
   if (a.dtype == GBLA_FP32) return bh * chunks_of<float>(a) * Record<float, 3, false>::kFloats;
@@ -453,10 +665,16 @@ size_t delta_forward_floats(const DeltaArgs &a) {
                          : Record<__nv_bfloat16, 1, false>::kFloats);
 }
 
+size_t delta_forward_floats(const DeltaArgs &a) {
+  return record_floats(a) + delta::segments_of(a).floats(a);
+}
+
 cudaError_t delta_forward(const DeltaArgs &a, float *scratch, cudaStream_t st) {
-  if (a.D == 32) return delta::forward_d<32>(a, scratch, st);
-  if (a.D == 64) return delta::forward_d<64>(a, scratch, st);
-  return delta::forward_d<128>(a, scratch, st);
+  const delta::Segments g = delta::segments_of(a);
+  float *before = scratch + record_floats(a);
+  if (a.D == 32) return delta::forward_d<32>(a, g, scratch, before, st);
+  if (a.D == 64) return delta::forward_d<64>(a, g, scratch, before, st);
+  return delta::forward_d<128>(a, g, scratch, before, st);
 }
 
 }  // namespace gbla

@@ -63,8 +63,11 @@ __device__ __forceinline__ void tf32_split(float x, uint32_t &hi, uint32_t &lo) 
 }
 
 // The left operand of tf32 products made of a result tile; kTerms 1: rounded to 11 bits,
-// 3: hi + lo (the product of the two small parts is left out: 2^-22).
-template <int kTerms>
+// 3: hi + lo (the product of the two small parts is left out: 2^-22).  The tensor cores cut off
+// what their accumulator cannot hold, so that long sums shrink: where results are fp32 (kSums),
+// the products of 8 are summed from zero and added in one rounding (the gradient of the keys
+// 1.9e-6 of its norm off, 0.4e-6 with it).
+template <int kTerms, bool kSums = false>
 struct LeftTf32 {
   uint32_t hi[4], lo[4];
   __device__ __forceinline__ explicit LeftTf32(const float (&c)[4]) {
@@ -91,6 +94,15 @@ struct LeftTf32 {
     mma_tf32(c, hi, b.x, b.y);
   }
   __device__ __forceinline__ void times(float (&c)[4], const uint4 &b) const {
+    if (kSums) {
+      float z[4] = {};
+      mma_tf32(z, lo, b.x, b.y);
+      mma_tf32(z, hi, b.z, b.w);
+      mma_tf32(z, hi, b.x, b.y);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) c[i] += z[i];
+      return;
+    }
     mma_tf32(c, lo, b.x, b.y);
     mma_tf32(c, hi, b.z, b.w);
     mma_tf32(c, hi, b.x, b.y);
@@ -137,17 +149,17 @@ template <typename T>
 constexpr int pad_row(int cols) { return cols + 8; }
 // kRows tokens of kCols values into padded rows; rows from n on become zeros.
 template <typename T, int kRows, int kCols, int kThreads>
-__device__ __forceinline__ void load_rows(T *to, const T *from, long long stride, int n) {
+__device__ __forceinline__ void load_rows(T *to, const T *from, long long stride, int n, int tid) {
   constexpr int kVec = 16 / sizeof(T), kPer = kCols / kVec;
-  for (int i = threadIdx.x; i < kRows * kPer; i += kThreads) {
+  for (int i = tid; i < kRows * kPer; i += kThreads) {
     const int r = i / kPer, c = i % kPer * kVec;
     cp_async_or_zero(smem_u32(to + r * pad_row<T>(kCols) + c), from + (r < n ? r * stride + c : 0),
                      r < n);
   }
 }
 template <int kFloats, int kThreads>
-__device__ __forceinline__ void load_flat(float *to, const float *from) {
-  for (int i = threadIdx.x * 4; i < kFloats; i += kThreads * 4)
+__device__ __forceinline__ void load_flat(float *to, const float *from, int tid) {
+  for (int i = tid * 4; i < kFloats; i += kThreads * 4)
     cp_async_16(smem_u32(to + i), from + i);
 }
 
@@ -216,54 +228,90 @@ struct Record {
   static constexpr int C = kChunkOf<T>;
   using M = Tiles<C, kSolve>;
   using P = Tiles<C, kBack ? kSolve : sizeof(T) == 2 ? 1 : 3>;
-  static constexpr int kM = 0, kP = M::kFloats, kT = kP + P::kFloats;
-  static constexpr int kGates = kT + (kBack ? M::kFloats : 0);
-  static constexpr int kFloats = kGates + Gates<C>::kFloats;
+  static constexpr int kM = 0, kGates = M::kFloats, kP = kGates + Gates<C>::kFloats;
+  static constexpr int kT = kP + P::kFloats, kFloats = kT + (kBack ? M::kFloats : 0);
 };
 
 // ------------------------------------------------------------- a warp's part of a state
-// Products of the state's 16 columns (transposed: D / 8 tiles) with the rows of a tile (keys, or
-// with `more` keys and, in 16 bits where they are bf16, queries).
-template <int kTerms, int D, int C, bool kMore>
-__device__ __forceinline__ void state_products(const float (&S)[D / 8][4], const __nv_bfloat16 *ks,
-                                               const __nv_bfloat16 *qs, float (&kv)[C / 8][4],
-                                               float (&qv)[C / 8][4]) {
+// A state's 16 columns as left operands, handed to another warp through shared memory: a uint4 a
+// lane for each 8 (fp32) or twice for each 16 (bf16, two numbers a value) of its rows.
+template <int D>
+constexpr int kHandWords = D / 8;
+
+// Products of the state's 16 columns (transposed: D / 8 tiles) with the rows of a tile of keys.
+// kHand: leaves the left operands in `hand`.
+template <int kTerms, int D, int C, bool kHand>
+__device__ __forceinline__ void key_products(const float (&S)[D / 8][4], const __nv_bfloat16 *ks,
+                                             float (&kv)[C / 8][4], uint4 *hand) {
   constexpr int kRow = pad_row<__nv_bfloat16>(D);
+  const int lane = threadIdx.x & 31;
 #pragma unroll
   for (int d = 0; d < D / 16; ++d) {
     const LeftBf16<kTerms> a(S[2 * d], S[2 * d + 1]);
+    if (kHand) {
+#pragma unroll
+      for (int p = 0; p < 2; ++p)
+        hand[(2 * d + p) * 32 + lane] = make_uint4(a.part[p][0], a.part[p][1], a.part[p][2], a.part[p][3]);
+    }
 #pragma unroll
     for (int n = 0; n < C / 16; ++n) {
       const PairBf16 k = by_token<kRow>(ks, 16 * n, 16 * d);
       a.times(kv[2 * n], k.b[0][0], k.b[0][1]);
       a.times(kv[2 * n + 1], k.b[1][0], k.b[1][1]);
-      if (kMore) {
-        const PairBf16 q = by_token<kRow>(qs, 16 * n, 16 * d);
-#pragma unroll
-        for (int i = 0; i < 2; ++i)
-#pragma unroll
-          for (int p = 1; p >= 0; --p) mma_bf16(qv[2 * n + i], a.part[p], q.b[i][0], q.b[i][1]);
-      }
     }
   }
 }
-template <int kTerms, int D, int C, bool kMore>
-__device__ __forceinline__ void state_products(const float (&S)[D / 8][4], const float *ks,
-                                               const float *qs, float (&kv)[C / 8][4],
-                                               float (&qv)[C / 8][4]) {
+template <int kTerms, int D, int C, bool kHand>
+__device__ __forceinline__ void key_products(const float (&S)[D / 8][4], const float *ks,
+                                             float (&kv)[C / 8][4], uint4 *hand) {
   constexpr int kRow = pad_row<float>(D);
-  const int g = (threadIdx.x & 31) >> 2, t = threadIdx.x & 3;
+  const int lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
 #pragma unroll
   for (int d = 0; d < D / 8; ++d) {
-    const LeftTf32<3> a(S[d]);
+    const LeftTf32<3, true> a(S[d]);
+    if (kHand) ((float4 *)hand)[d * 32 + lane] = make_float4(S[d][0], S[d][1], S[d][2], S[d][3]);
 #pragma unroll
     for (int n = 0; n < C / 8; ++n) {
       const float2 k = *(const float2 *)(ks + (8 * n + g) * kRow + 8 * d + 2 * t);
       a.times(kv[n], k.x, k.y);
-      if (kMore) {
-        const float2 q = *(const float2 *)(qs + (8 * n + g) * kRow + 8 * d + 2 * t);
-        a.times(qv[n], q.x, q.y);
+    }
+  }
+}
+// The same with a state handed over, in 16 bits where results are bf16.
+template <int D, int C>
+__device__ __forceinline__ void query_products(const uint4 *hand, const __nv_bfloat16 *qs,
+                                               float (&qv)[C / 8][4]) {
+  constexpr int kRow = pad_row<__nv_bfloat16>(D);
+  const int lane = threadIdx.x & 31;
+#pragma unroll
+  for (int d = 0; d < D / 16; ++d) {
+    const uint4 x = hand[2 * d * 32 + lane], y = hand[(2 * d + 1) * 32 + lane];
+    const uint32_t hi[4] = {x.x, x.y, x.z, x.w}, lo[4] = {y.x, y.y, y.z, y.w};
+#pragma unroll
+    for (int n = 0; n < C / 16; ++n) {
+      const PairBf16 q = by_token<kRow>(qs, 16 * n, 16 * d);
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        mma_bf16(qv[2 * n + i], lo, q.b[i][0], q.b[i][1]);
+        mma_bf16(qv[2 * n + i], hi, q.b[i][0], q.b[i][1]);
       }
+    }
+  }
+}
+template <int D, int C>
+__device__ __forceinline__ void query_products(const uint4 *hand, const float *qs,
+                                               float (&qv)[C / 8][4]) {
+  constexpr int kRow = pad_row<float>(D);
+  const int lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
+#pragma unroll
+  for (int d = 0; d < D / 8; ++d) {
+    const float4 s = ((const float4 *)hand)[d * 32 + lane];
+    const float c[4] = {s.x, s.y, s.z, s.w};
+    const LeftTf32<3, true> a(c);
+#pragma unroll
+    for (int n = 0; n < C / 8; ++n) {
+      const float2 q = *(const float2 *)(qs + (8 * n + g) * kRow + 8 * d + 2 * t);
+      a.times(qv[n], q.x, q.y);
     }
   }
 }
@@ -296,16 +344,18 @@ __device__ __forceinline__ void state_update(float (&S)[D / 8][4], float hi, flo
   static_assert(C == 64, "four left operands");
   const LeftBf16<kTerms> a[4] = {{w[0], w[1]}, {w[2], w[3]}, {w[4], w[5]}, {w[6], w[7]}};
 #pragma unroll
-  for (int d = 0; d < D / 16; ++d) {
-    float x[2][4] = {};
+  for (int d = 0; d < D / 16; d += 2) {  // four sums at a time
+    float x[4][4] = {};
 #pragma unroll
-    for (int j = 0; j < C / 16; ++j) {
-      const PairBf16 k = by_channel<kRow>(ks, 16 * j, 16 * d);
-      a[j].times(x[0], k.b[0][0], k.b[0][1]);
-      a[j].times(x[1], k.b[1][0], k.b[1][1]);
-    }
+    for (int j = 0; j < C / 16; ++j)
 #pragma unroll
-    for (int i = 0; i < 2; ++i)
+      for (int e = 0; e < 2; ++e) {
+        const PairBf16 k = by_channel<kRow>(ks, 16 * j, 16 * (d + e));
+        a[j].times(x[2 * e], k.b[0][0], k.b[0][1]);
+        a[j].times(x[2 * e + 1], k.b[1][0], k.b[1][1]);
+      }
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
         float &s = S[2 * d + i][e];
@@ -323,7 +373,7 @@ __device__ __forceinline__ void state_update(float (&S)[D / 8][4], float hi, flo
     float x[4] = {};
 #pragma unroll
     for (int j = 0; j < C / 8; ++j) {
-      const LeftTf32<3> a(w[j]);
+      const LeftTf32<3, true> a(w[j]);
       a.times(x, ks[(8 * j + 2 * t) * kRow + 8 * d + g], ks[(8 * j + 2 * t + 1) * kRow + 8 * d + g]);
     }
 #pragma unroll
@@ -375,10 +425,19 @@ __device__ __forceinline__ void store_tile(float *o, size_t stride, const float 
 // ------------------------------------------------------------- between the files
 template <typename T>
 int chunks_of(const DeltaArgs &a) { return (a.N + kChunkOf<T> - 1) / kChunkOf<T>; }
+// A sequence is cut into `count` segments of `chunks` chunks (the last one shorter).
+struct Segments {
+  int count, chunks;
+  // scratch: a state and a matrix for each segment but the last
+  size_t floats(const DeltaArgs &a) const {
+    return 2 * (size_t)a.B * a.H * (count - 1) * a.D * a.D;
+  }
+};
+Segments segments_of(const DeltaArgs &a);
 // First part of the backward pass: records (of the backward's form), the state before every
 // chunk [B H chunks][D][D] and the misses [B H chunks][C][D].  exact: three terms throughout.
-cudaError_t save_forward(const DeltaArgs &a, bool exact, float *records, float *states,
-                         float *misses, cudaStream_t st);
+cudaError_t save_forward(const DeltaArgs &a, const Segments &g, bool exact, float *records,
+                         float *states, float *misses, float *before, cudaStream_t st);
 
 }  // namespace delta
 }  // namespace gbla

@@ -25,7 +25,10 @@ template <typename T, int D>
 struct PrepShape {
   static constexpr int C = kChunkOf<T>, kWarps = C / 16, kThreads = kWarps * 32;
   static constexpr int kRow = pad_row<T>(D), kMat = C + 4;
-  static constexpr int kBytes = 2 * C * kRow * (int)sizeof(T) + 2 * C * kMat * 4 + 4 * C * 4 + 16;
+  // keys and queries, then the inverse in their place; A; the gates
+  static constexpr int kTiles = 2 * C * kRow * (int)sizeof(T), kInverse = C * kMat * 4;
+  static constexpr int kFirst = kTiles > kInverse ? kTiles : kInverse;
+  static constexpr int kBytes = kFirst + kInverse + 4 * C * 4 + 16;
 };
 
 // Products of 16 rows of `left` with every row of `right` up to the block's last row, fp32 tiles
@@ -70,17 +73,17 @@ __device__ __forceinline__ void rows_times_rows(float (&acc)[C / 8][4], const fl
 
 // Parts of C x C matrices in shared memory (rows of C + 4 floats) as operands: 16 rows from i on
 // at columns j .. j + 7 on the left, columns j .. j + 7 of rows i .. i + 7 on the right.
-template <int C>
-__device__ __forceinline__ LeftTf32<3> left_of(const float *m, int i, int j) {
+template <int C, int kTerms>
+__device__ __forceinline__ LeftTf32<kTerms> left_of(const float *m, int i, int j) {
   const int g = (threadIdx.x & 31) >> 2, t = threadIdx.x & 3;
   const float2 x = *(const float2 *)(m + (i + g) * (C + 4) + j + 2 * t);
   const float2 y = *(const float2 *)(m + (i + g + 8) * (C + 4) + j + 2 * t);
   const float c[4] = {x.x, x.y, y.x, y.y};
-  return LeftTf32<3>(c);
+  return LeftTf32<kTerms>(c);
 }
-template <int C>
-__device__ __forceinline__ void times_right(float (&c)[4], const LeftTf32<3> &a, const float *m,
-                                            int i, int j) {
+template <int C, int kTerms>
+__device__ __forceinline__ void times_right(float (&c)[4], const LeftTf32<kTerms> &a,
+                                            const float *m, int i, int j) {
   const int g = (threadIdx.x & 31) >> 2, t = threadIdx.x & 3;
   const float *at = m + (i + 2 * t) * (C + 4) + j + g;
   a.times(c, at[0], at[C + 4]);
@@ -89,10 +92,10 @@ __device__ __forceinline__ void times_right(float (&c)[4], const LeftTf32<3> &a,
 // to = (1 + A)^-1 for strictly lower triangular A, on and below its diagonal blocks of 16.
 // Those by forward substitution, the rest from
 //   (1 + A)^-1 = [ M0 0; -M1 A10 M0 M1 ]
-// for pairs of blocks of 16 and then of 32, in products of three tf32 terms.  (No powers of A,
-// which grow where the inverse does not: keys that repeat.)  Begins and ends with all of A, and
+// for pairs of blocks of 16 and then of 32, in tf32 products of as many terms as the inverse is
+// used in.  (No powers of A, which grow where the inverse does not: keys that repeat.)  Begins and ends with all of A, and
 // of `to`, visible to the block.
-template <int C>
+template <int C, int kTerms>
 __device__ __forceinline__ void invert(float *to, const float *A, int w) {
   constexpr int kMat = C + 4;
   const int lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
@@ -124,15 +127,15 @@ __device__ __forceinline__ void invert(float *to, const float *A, int w) {
     float z[2][4] = {}, y[2][4] = {};
 #pragma unroll
     for (int k = 0; k < 2; ++k) {
-      const LeftTf32<3> a = left_of<C>(to, i, i + 8 * k);
+      const auto a = left_of<C, kTerms>(to, i, i + 8 * k);
 #pragma unroll
-      for (int n = 0; n < 2; ++n) times_right<C>(z[n], a, A, i + 8 * k, j + 8 * n);
+      for (int n = 0; n < 2; ++n) times_right<C, kTerms>(z[n], a, A, i + 8 * k, j + 8 * n);
     }
 #pragma unroll
     for (int k = 0; k < 2; ++k) {
-      const LeftTf32<3> a(z[k]);
+      const LeftTf32<kTerms> a(z[k]);
 #pragma unroll
-      for (int n = 0; n < 2; ++n) times_right<C>(y[n], a, to, j + 8 * k, j + 8 * n);
+      for (int n = 0; n < 2; ++n) times_right<C, kTerms>(y[n], a, to, j + 8 * k, j + 8 * n);
     }
     put(y[0], i, j), put(y[1], i, j + 8);
   }
@@ -144,16 +147,16 @@ __device__ __forceinline__ void invert(float *to, const float *A, int w) {
 #pragma unroll
     for (int k = 0; k < 4; ++k)
       if (k < 2 || (w & 1)) {
-        const LeftTf32<3> a = left_of<C>(to, i, 32 + 8 * k);
+        const auto a = left_of<C, kTerms>(to, i, 32 + 8 * k);
 #pragma unroll
-        for (int n = 0; n < 4; ++n) times_right<C>(z[n], a, A, 32 + 8 * k, 8 * n);
+        for (int n = 0; n < 4; ++n) times_right<C, kTerms>(z[n], a, A, 32 + 8 * k, 8 * n);
       }
 #pragma unroll
     for (int k = 0; k < 4; ++k)
       if (k >= 2 || j == 0) {
-        const LeftTf32<3> a(z[k]);
+        const LeftTf32<kTerms> a(z[k]);
 #pragma unroll
-        for (int n = 0; n < 2; ++n) times_right<C>(y[n], a, to, 8 * k, j + 8 * n);
+        for (int n = 0; n < 2; ++n) times_right<C, kTerms>(y[n], a, to, 8 * k, j + 8 * n);
       }
     put(y[0], i, j), put(y[1], i, j + 8);
     __syncthreads();
@@ -161,15 +164,15 @@ __device__ __forceinline__ void invert(float *to, const float *A, int w) {
 }
 
 template <typename T, int D, int kSolve, bool kBack>
-__global__ void __launch_bounds__(PrepShape<T, D>::kThreads)
+__global__ void __launch_bounds__(PrepShape<T, D>::kThreads, 5)
     prepare_kernel(const DeltaArgs p, float *records, int nc) {
   using Sh = PrepShape<T, D>;
   using Rec = Record<T, kSolve, kBack>;
   constexpr int C = Sh::C, kThreads = Sh::kThreads, kRow = Sh::kRow, kMat = Sh::kMat;
   extern __shared__ __align__(16) char raw[];
   T *ks = (T *)raw, *qs = ks + C * kRow;
-  float *A = (float *)(qs + C * kRow), *inv = A + C * kMat;
-  float *hi = inv + C * kMat, *lo = hi + C, *beta = lo + C;
+  float *A = (float *)(raw + Sh::kFirst), *inv = (float *)raw;
+  float *hi = A + C * kMat, *lo = hi + C, *beta = lo + C;
   double *first = (double *)(beta + 2 * C);
   grid_dep_wait();
   const int h = blockIdx.y, b = blockIdx.z, hk = h / (p.H / p.Hk), tid = threadIdx.x;
@@ -218,26 +221,48 @@ __global__ void __launch_bounds__(PrepShape<T, D>::kThreads)
   __syncthreads();
   if (tid < C)
     gt[Gates<C>::kDown + tid] = exp2f((hi[C - 1] - hi[tid]) + (lo[C - 1] - lo[tid]));
-  // the warp's 16 rows of both products, weighted
-  const int w = tid / 32, g = (tid & 31) >> 2, t = tid & 3;
+  // the warp's 16 rows of both products, weighted.  Columns before the warp's first row meet
+  // the power in two factors, both at most 1 (rows to that one, that one to the columns).
+  const int w = tid / 32, g = (tid & 31) >> 2, t = tid & 3, i0 = 16 * w;
   float kk[C / 8][4] = {}, qk[C / 8][4] = {};
   rows_times_rows<D, C>(kk, ks, ks, w);
   rows_times_rows<D, C>(qk, qs, ks, w);
+  if (kBack) __syncthreads();  // P takes their place
+  const float hr = hi[i0], lr = lo[i0];
+  float row[2];
+#pragma unroll
+  for (int half = 0; half < 2; ++half) {
+    const int i = i0 + g + 8 * half;
+    row[half] = ex2_approx((hi[i] - hr) + (lo[i] - lr));
+  }
 #pragma unroll
   for (int m = 0; m < C / 8; ++m) {
     if (m > 2 * w + 1) continue;
     const int j = 8 * m + 2 * t;
     const float2 hj = *(const float2 *)(hi + j), lj = *(const float2 *)(lo + j);
     const float2 bj = *(const float2 *)(beta + j);
+    float f[2][2];
+    if (m < 2 * w) {
+      const float c0 = ex2_approx((hr - hj.x) + (lr - lj.x)), c1 = ex2_approx((hr - hj.y) + (lr - lj.y));
+#pragma unroll
+      for (int half = 0; half < 2; ++half) f[half][0] = row[half] * c0, f[half][1] = row[half] * c1;
+    } else {
+#pragma unroll
+      for (int half = 0; half < 2; ++half) {
+        const int i = i0 + g + 8 * half;
+        f[half][0] = i >= j ? ex2_approx((hi[i] - hj.x) + (lo[i] - lj.x)) : 0.f;
+        f[half][1] = i >= j + 1 ? ex2_approx((hi[i] - hj.y) + (lo[i] - lj.y)) : 0.f;
+      }
+    }
 #pragma unroll
     for (int half = 0; half < 2; ++half) {
-      const int i = 16 * w + g + 8 * half;
-      const float f0 = i >= j ? ex2_approx((hi[i] - hj.x) + (lo[i] - lj.x)) : 0.f;
-      const float f1 = i >= j + 1 ? ex2_approx((hi[i] - hj.y) + (lo[i] - lj.y)) : 0.f;
+      const int i = i0 + g + 8 * half;
       float &x0 = kk[m][2 * half], &x1 = kk[m][2 * half + 1];
-      x0 = i > j ? x0 * f0 : 0.f, x1 = i > j + 1 ? x1 * f1 : 0.f;
+      x0 *= f[half][0], x1 *= f[half][1];
+      if (m >= 2 * w) x0 = i > j ? x0 : 0.f, x1 = i > j + 1 ? x1 : 0.f;
       *(float2 *)(A + i * kMat + j) = make_float2(x0 * bj.x, x1 * bj.y);
-      const float p0 = p.scale * qk[m][2 * half] * f0, p1 = p.scale * qk[m][2 * half + 1] * f1;
+      const float p0 = p.scale * qk[m][2 * half] * f[half][0];
+      const float p1 = p.scale * qk[m][2 * half + 1] * f[half][1];
       if (kBack)
         *(float2 *)(inv + i * kMat + j) = make_float2(p0, p1);
       else if (2 * w + half >= m)
@@ -261,7 +286,7 @@ __global__ void __launch_bounds__(PrepShape<T, D>::kThreads)
     put(rec + Rec::kP, typename Rec::P{}, true, false);
     __syncthreads();
   }
-  invert<C>(inv, A, w);
+  invert<C, kSolve>(inv, A, w);
   put(rec + Rec::kM, typename Rec::M{}, false, true);
   if (kBack) {  // (1 + beta X)^-1: the rows weighted in place of the columns
     __syncthreads();
@@ -276,7 +301,7 @@ __global__ void __launch_bounds__(PrepShape<T, D>::kThreads)
       }
     }
     __syncthreads();
-    invert<C>(inv, A, w);
+    invert<C, kSolve>(inv, A, w);
     put(rec + Rec::kT, typename Rec::M{}, true, true);
   }
 }
@@ -302,7 +327,10 @@ struct ScanShape {
   // not fit into shared memory)
   static constexpr bool kNarrow = sizeof(T) == 2 && D == 128 && kSolve == 3 && kFor == kResults;
   static constexpr int C = kChunkOf<T>, E = D < 64 ? D : kNarrow ? 32 : 64, kSplit = D / E;
-  static constexpr int kCarry = E / 16, kThreads = 2 * kCarry * 32;
+  // (kSegment: the other warps only fetch, half as many do, and two blocks fit an SM)
+  static constexpr int kCarry = E / 16, kHelp = kFor == kSegment && kCarry > 2 ? 2 : kCarry;
+  static constexpr int kThreads = (kCarry + kHelp) * 32;
+  static constexpr int kBlocks = kFor == kSegment && (D < 128 || kSolve == 1) ? 2 : 1;
   static constexpr int kRow = pad_row<T>(D), kValRow = pad_row<T>(E);
   // bytes: keys, values, M and gates of a chunk; queries, P and gates of the one before
   static constexpr int kKeys = C * kRow * (int)sizeof(T), kVals = C * kValRow * (int)sizeof(T);
@@ -320,12 +348,13 @@ struct ScanShape {
 // kSegment forms, [B H][segments - 1][D][D], the matrices in `moves`.  Records are `stride` floats
 // apart (their M and gates lie at the same place in both forms).
 template <typename T, int D, int kTerms, int kSolve, Purpose kFor>
-__global__ void __launch_bounds__(ScanShape<T, D, kSolve, kFor>::kThreads)
+__global__ void __launch_bounds__(ScanShape<T, D, kSolve, kFor>::kThreads,
+                                  ScanShape<T, D, kSolve, kFor>::kBlocks)
     scan_kernel(const DeltaArgs p, const float *records, float *states, float *misses,
                 float *before, float *moves, int nc, int seg, int stride) {
   using Sh = ScanShape<T, D, kSolve, kFor>;
   using Rec = typename Sh::Rec;
-  constexpr int C = Sh::C, E = Sh::E, kCarry = Sh::kCarry, kFetch = kCarry * 32;
+  constexpr int C = Sh::C, E = Sh::E, kCarry = Sh::kCarry, kFetch = Sh::kHelp * 32;
   constexpr int kOut = sizeof(T) == 2 ? 1 : 3;  // terms of the product with P
   constexpr bool kSums = sizeof(T) == 4;
   constexpr int kColumns = kFor == kSegment ? 2 * Sh::kSplit : Sh::kSplit;  // blocks a head
@@ -545,7 +574,7 @@ __global__ void __launch_bounds__(JoinShape<D>::kThreads)
     const float *m = tile + (s & 1) * D * kRow;
 #pragma unroll
     for (int k = 0; k < D / 8; ++k) {
-      const LeftTf32<3, true> a(S[k]);
+      const LeftTf32<3> a(S[k]);
 #pragma unroll
       for (int n = 0; n < D / 8; ++n) {
         const float2 v = *(const float2 *)(m + (8 * n + g) * kRow + 8 * k + 2 * t);

@@ -147,20 +147,32 @@ constexpr int kChunkOf = sizeof(T) == 2 ? 64 : 32;
 // two) apart.
 template <typename T>
 constexpr int pad_row(int cols) { return cols + 8; }
-// kRows tokens of kCols values into padded rows; rows from n on become zeros.
+// kRows tokens of kCols values into padded rows; rows from n on become zeros.  A thread keeps its
+// columns and goes down the rows: a copy costs two or three instructions.
 template <typename T, int kRows, int kCols, int kThreads>
 __device__ __forceinline__ void load_rows(T *to, const T *from, long long stride, int n, int tid) {
-  constexpr int kVec = 16 / sizeof(T), kPer = kCols / kVec;
-  for (int i = tid; i < kRows * kPer; i += kThreads) {
-    const int r = i / kPer, c = i % kPer * kVec;
-    cp_async_or_zero(smem_u32(to + r * pad_row<T>(kCols) + c), from + (r < n ? r * stride + c : 0),
-                     r < n);
+  constexpr int kVec = 16 / sizeof(T), kPer = kCols / kVec, kStep = kThreads / kPer;
+  constexpr int kTimes = kRows / kStep;
+  static_assert(kThreads % kPer == 0 && kRows % kStep == 0, "whole rows at a time");
+  const int r = tid / kPer, c = tid % kPer * kVec;
+  const uint32_t dst = smem_u32(to + r * pad_row<T>(kCols) + c);
+  const T *src = from + r * stride + c;
+#pragma unroll
+  for (int i = 0; i < kTimes; ++i) {
+    const bool valid = r + i * kStep < n;
+    cp_async_or_zero(dst + i * (kStep * pad_row<T>(kCols) * (int)sizeof(T)), valid ? src : from, valid);
+    src += kStep * stride;
   }
 }
 template <int kFloats, int kThreads>
 __device__ __forceinline__ void load_flat(float *to, const float *from, int tid) {
-  for (int i = tid * 4; i < kFloats; i += kThreads * 4)
-    cp_async_16(smem_u32(to + i), from + i);
+  constexpr int kTimes = (kFloats / 4 + kThreads - 1) / kThreads;
+  const uint32_t dst = smem_u32(to + tid * 4);
+  from += tid * 4;
+#pragma unroll
+  for (int i = 0; i < kTimes; ++i)
+    if ((i + 1) * kThreads * 4 <= kFloats || tid * 4 + i * kThreads * 4 < kFloats)
+      cp_async_16(dst + i * kThreads * 16, from + i * kThreads * 4);
 }
 
 // Right operands from a raw tile of tokens x channels, for products with the left operands

@@ -22,125 +22,183 @@ namespace delta {
 namespace {
 
 // ------------------------------------------------------------- from the last chunk back
+// The forward scan's counterpart: a block carries E = min(D, 64) of the columns of A, 16 a warp,
+// from a segment's last chunk to its first.  On the chain are A^T k -> du -> w -> A'; what does
+// not need A (sum_i P_ij d_i, and what the results and queries add to A') other warps form one
+// chunk ahead and leave in shared memory.  kOwn: what a segment adds to A, from zero and with
+// nothing written.
 template <typename T, int D, int kSolve>
 struct ReverseShape {
   using Rec = Record<T, kSolve, true>;
-  static constexpr int C = kChunkOf<T>, kWarps = D / 16, kThreads = kWarps * 32;
-  static constexpr int kRow = pad_row<T>(D);
-  static constexpr int kTile = C * kRow * (int)sizeof(T);          // bytes of k, q or d
-  static constexpr int kStage = 3 * kTile + (Rec::kFloats - Rec::kGates) * 4;  // M is not read
-  static constexpr int kBytes = 2 * kStage;
+  // (bf16 of three terms at D = 128: 64 columns would not fit into shared memory)
+  static constexpr bool kNarrow = sizeof(T) == 2 && D == 128 && kSolve == 3;
+  static constexpr int C = kChunkOf<T>, E = D < 64 ? D : kNarrow ? 32 : 64, kSplit = D / E;
+  static constexpr int kCarry = E / 16, kThreads = 2 * kCarry * 32;
+  static constexpr int kRow = pad_row<T>(D), kValRow = pad_row<T>(E);
+  // bytes: keys, gates and T of a chunk; queries, d, gates and P of the one ahead
+  static constexpr int kKeys = C * kRow * (int)sizeof(T), kVals = C * kValRow * (int)sizeof(T);
+  static constexpr int kGate = Gates<C>::kFloats * 4;
+  static constexpr int kFirst = kKeys + kGate + Rec::M::kFloats * 4;
+  static constexpr int kSecond = kKeys + kVals + kGate + Rec::P::kFloats * 4;
+  static constexpr int kHand = (C / 8 + D / 8) * 32 * 16;
+  static constexpr int kBytes = 2 * (kFirst + kSecond + kCarry * kHand);
+  static_assert(kBytes <= 227 * 1024, "shared memory of a block");
 };
 
-template <typename T, int D, int kTerms, int kSolve>
+template <typename T, int D, int kTerms, int kSolve, bool kOwn>
 __global__ void __launch_bounds__(ReverseShape<T, D, kSolve>::kThreads)
-    reverse_kernel(const DeltaBackArgs p, const float *records, float *after, float *weights, int nc) {
+    reverse_kernel(const DeltaBackArgs p, const float *records, float *after, float *weights,
+                   float *own, int nc, int seg, int count) {
   using Sh = ReverseShape<T, D, kSolve>;
   using Rec = typename Sh::Rec;
-  constexpr int C = Sh::C, kThreads = Sh::kThreads, kRow = Sh::kRow;
+  constexpr int C = Sh::C, E = Sh::E, kCarry = Sh::kCarry, kFetch = kCarry * 32;
   constexpr bool kSums = sizeof(T) == 4;
   extern __shared__ __align__(16) char raw[];
   grid_dep_wait();
   const DeltaArgs &f = p.f;
-  const int h = blockIdx.x, b = blockIdx.y, hk = h / (f.H / f.Hk), tid = threadIdx.x;
-  const int t = tid & 3, e0 = tid / 32 * 16;
+  const int h = blockIdx.x / Sh::kSplit, b = blockIdx.y, s = blockIdx.z;
+  const int hk = h / (f.H / f.Hk), tid = threadIdx.x, warp = tid / 32, lane = tid & 31, t = tid & 3;
+  const bool carry = warp < kCarry;
+  const int x0 = blockIdx.x % Sh::kSplit * E, e0 = x0 + warp % kCarry * 16;
   const int L = f.seq_lens ? min(max(__ldg(f.seq_lens + b), 0), f.N) : f.N;
   const size_t bh = (size_t)b * f.H + h;
+  const int chunks = (L + C - 1) / C, first = s * seg, end = min(chunks, first + seg);
+  if (s > 0 && first >= chunks) return;
+  if (kOwn && s == 0) return;  // nobody reads it
   const T *kg = (const T *)f.k + b * f.sk[0] + (long long)hk * D;
   const T *qg = (const T *)f.q + b * f.sq[0] + (long long)hk * D;
   const size_t orow = (size_t)f.H * D;
-  const T *dg = (const T *)p.d_o + ((size_t)b * f.N * f.H + h) * D;
+  const T *dg = (const T *)p.d_o + ((size_t)b * f.N * f.H + h) * D + x0;
   T *vg = (T *)p.dv + ((size_t)b * f.N * f.H + h) * D + e0;
-  const int chunks = (L + C - 1) / C;
-  auto load = [&](int c) {
-    char *s = raw + (c & 1) * Sh::kStage;
+  char *hands = raw + 2 * (Sh::kFirst + Sh::kSecond) + warp % kCarry * Sh::kHand;
+  auto first_of = [&](int c) { return raw + (c & 1) * Sh::kFirst; };
+  auto second_of = [&](int c) { return raw + 2 * Sh::kFirst + (c & 1) * Sh::kSecond; };
+  auto hand_of = [&](int c) { return (float4 *)(hands + (c & 1) * (kCarry * Sh::kHand)) + lane; };
+  const int ftid = tid - kCarry * 32;
+  auto fetch_first = [&](int c) {
+    char *to = first_of(c);
+    const long long t0 = (long long)c * C;
+    const float *rec = records + (bh * nc + c) * Rec::kFloats;
+    load_rows<T, C, D, kFetch>((T *)to, kg + t0 * f.sk[1], f.sk[1], min(C, L - c * C), ftid);
+    load_flat<Gates<C>::kFloats, kFetch>((float *)(to + Sh::kKeys), rec + Rec::kGates, ftid);
+    load_flat<Rec::M::kFloats, kFetch>((float *)(to + Sh::kKeys + Sh::kGate), rec + Rec::kT, ftid);
+  };
+  auto fetch_second = [&](int c) {
+    char *to = second_of(c);
     const long long t0 = (long long)c * C;
     const int n = min(C, L - c * C);
-    load_rows<T, C, D, kThreads>((T *)s, kg + t0 * f.sk[1], f.sk[1], n, tid);
-    load_rows<T, C, D, kThreads>((T *)(s + Sh::kTile), qg + t0 * f.sq[1], f.sq[1], n, tid);
-    load_rows<T, C, D, kThreads>((T *)(s + 2 * Sh::kTile), dg + t0 * orow, (long long)orow, n, tid);
-    load_flat<Rec::kFloats - Rec::kGates, kThreads>(
-        (float *)(s + 3 * Sh::kTile), records + (bh * nc + c) * Rec::kFloats + Rec::kGates, tid);
+    load_rows<T, C, D, kFetch>((T *)to, qg + t0 * f.sq[1], f.sq[1], n, ftid);
+    load_rows<T, C, E, kFetch>((T *)(to + Sh::kKeys), dg + t0 * orow, (long long)orow, n, ftid);
+    load_flat<Gates<C>::kFloats + Rec::P::kFloats, kFetch>(  // (side by side)
+        (float *)(to + Sh::kKeys + Sh::kVals),
+        records + (bh * nc + c) * Rec::kFloats + Rec::kGates, ftid);
   };
   float A[D / 8][4];
-  load_state<D>(A, p.dstate ? p.dstate + bh * D * D : nullptr, e0);
-  if (chunks > 0) load(chunks - 1);
-  cp_async_commit();
-  for (int c = chunks - 1; c >= 0; --c) {
-    cp_async_wait_all();
-    __syncthreads();
-    if (c > 0) load(c - 1);
+  if (carry) {
+    const float *from = kOwn           ? nullptr
+                        : end < chunks ? own + (bh * count + s + 1) * D * D
+                        : p.dstate     ? p.dstate + bh * D * D
+                                       : nullptr;
+    load_state<D>(A, from, e0);
+  } else {
+    if (first < end) fetch_second(end - 1);
     cp_async_commit();
-    const char *s = raw + (c & 1) * Sh::kStage;
-    const T *ks = (const T *)s, *qs = (const T *)(s + Sh::kTile), *ds = (const T *)(s + 2 * Sh::kTile);
-    const float *gt = (const float *)(s + 3 * Sh::kTile);
-    const float *P = gt + (Rec::kP - Rec::kGates), *Tm = gt + (Rec::kT - Rec::kGates);
-    const int n = min(C, L - c * C);
-    store_state<D>(after + (bh * nc + c) * D * D, A, e0);
-    float r[C / 8][4] = {};
-    key_products<kTerms, D, C, false>(A, ks, r, nullptr);
-    {
-      float x[C / 8][4] = {};
-#pragma unroll
-      for (int m = 0; m < C / 16; ++m) {
-        float d[2][4];
-        values_of<kRow>(d[0], d[1], ds, m, e0);
-#pragma unroll
-        for (int i = 0; i < 2; ++i) {
-          const LeftTf32<kSolve, kSums> a(d[i]);
-#pragma unroll
-          for (int j = 0; j <= 2 * m + i; ++j) a.times(x[j], Rec::P::load(P, 2 * m + i, j));
-        }
-      }
+    cp_async_wait_all();
+  }
+  // round c: the chain's chunk c, the others' chunk c - 1
+  for (int c = end; c >= first; --c) {
+    __syncthreads();  // this round's tiles and what was left are there, the others are read
+    if (carry) {
+      if (c == end) continue;
+      const char *in = first_of(c);
+      const T *ks = (const T *)in;
+      const float *gt = (const float *)(in + Sh::kKeys), *Tm = gt + Gates<C>::kFloats;
+      const float4 *hand = hand_of(c);
+      const int n = min(C, L - c * C);
+      if (!kOwn) store_packed(after + (bh * nc + c) * D * D, A, e0);
+      float r[C / 8][4] = {};
+      key_products<kTerms, D, C, false>(A, ks, r, nullptr);
 #pragma unroll
       for (int j = 0; j < C / 8; ++j) {
         const float2 dn = *(const float2 *)(gt + Gates<C>::kDown + 8 * j + 2 * t);
-        r[j][0] = fmaf(dn.x, r[j][0], x[j][0]), r[j][1] = fmaf(dn.y, r[j][1], x[j][1]);
-        r[j][2] = fmaf(dn.x, r[j][2], x[j][2]), r[j][3] = fmaf(dn.y, r[j][3], x[j][3]);
+        const float4 x = hand[j * 32];
+        r[j][0] = fmaf(dn.x, r[j][0], x.x), r[j][1] = fmaf(dn.y, r[j][1], x.y);
+        r[j][2] = fmaf(dn.x, r[j][2], x.z), r[j][3] = fmaf(dn.y, r[j][3], x.w);
       }
-    }
-    // r += (T - 1)^T r: the earlier half of the tokens first, which needs the later ones as
-    // they are
+      // r += (T - 1)^T r: the earlier half of the tokens first, which needs the later ones as
+      // they are
 #pragma unroll
-    for (int half = 0; half < 2; ++half) {
-      constexpr int kHalf = C / 16;
-      float x[kHalf][4] = {};
+      for (int half = 0; half < 2; ++half) {
+        constexpr int kHalf = C / 16;
+        float x[kHalf][4] = {};
 #pragma unroll
-      for (int i = half * kHalf; i < C / 8; ++i) {
-        const LeftTf32<kSolve, kSums> a(r[i]);
+        for (int i = half * kHalf; i < C / 8; ++i) {
+          const LeftTf32<kSolve, kSums> a(r[i]);
+#pragma unroll
+          for (int j = 0; j < kHalf; ++j)
+            if (half * kHalf + j <= i) a.times(x[j], Rec::M::load(Tm, i, half * kHalf + j));
+        }
 #pragma unroll
         for (int j = 0; j < kHalf; ++j)
-          if (half * kHalf + j <= i) a.times(x[j], Rec::M::load(Tm, i, half * kHalf + j));
+#pragma unroll
+          for (int i = 0; i < 4; ++i) r[half * kHalf + j][i] += x[j][i];
       }
+      if (!kOwn) store_packed(weights + (bh * nc + c) * C * D, r, e0);
 #pragma unroll
-      for (int j = 0; j < kHalf; ++j)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) r[half * kHalf + j][i] += x[j][i];
-    }
-#pragma unroll
-    for (int j = 0; j < C / 8; ++j) {
-      store_tile(weights + (bh * nc + c) * C * D + e0, D, r[j], 8 * j, C);
-      const float2 be = *(const float2 *)(gt + Gates<C>::kBeta + 8 * j + 2 * t);
-      r[j][0] *= be.x, r[j][1] *= be.y, r[j][2] *= be.x, r[j][3] *= be.y;
-      store_tile(vg + (size_t)c * C * orow, orow, r[j], 8 * j, n);
-      const float2 up = *(const float2 *)(gt + Gates<C>::kUp + 8 * j + 2 * t);
-      r[j][0] *= -up.x, r[j][1] *= -up.y, r[j][2] *= -up.x, r[j][3] *= -up.y;
-    }
-    state_update<kTerms, D, C>(A, gt[Gates<C>::kWhole], gt[Gates<C>::kWhole + 1], r, ks);
-#pragma unroll
-    for (int m = 0; m < C / 16; ++m) {
-      values_of<kRow>(r[2 * m], r[2 * m + 1], ds, m, e0);
-#pragma unroll
-      for (int i = 0; i < 2; ++i) {
-        const float2 up = *(const float2 *)(gt + Gates<C>::kUp + 16 * m + 8 * i + 2 * t);
-        const float ux = up.x * f.scale, uy = up.y * f.scale;
-        float(&x)[4] = r[2 * m + i];
-        x[0] *= ux, x[1] *= uy, x[2] *= ux, x[3] *= uy;
+      for (int j = 0; j < C / 8; ++j) {
+        const float2 be = *(const float2 *)(gt + Gates<C>::kBeta + 8 * j + 2 * t);
+        r[j][0] *= be.x, r[j][1] *= be.y, r[j][2] *= be.x, r[j][3] *= be.y;
+        if (!kOwn) store_tile(vg + (size_t)c * C * orow, orow, r[j], 8 * j, n);
+        const float2 up = *(const float2 *)(gt + Gates<C>::kUp + 8 * j + 2 * t);
+        r[j][0] *= -up.x, r[j][1] *= -up.y, r[j][2] *= -up.x, r[j][3] *= -up.y;
       }
+      state_update<kTerms, D, C>(A, gt[Gates<C>::kWhole], gt[Gates<C>::kWhole + 1], r, ks);
+#pragma unroll
+      for (int d = 0; d < D / 8; ++d) {
+        const float4 y = hand[(C / 8 + d) * 32];
+        A[d][0] += y.x, A[d][1] += y.y, A[d][2] += y.z, A[d][3] += y.w;
+      }
+    } else {
+      if (c > first) {
+        fetch_first(c - 1);
+        if (c - 1 > first) fetch_second(c - 2);
+      }
+      cp_async_commit();
+      if (c > first) {
+        const char *in = second_of(c - 1);
+        const T *qs = (const T *)in, *ds = (const T *)(in + Sh::kKeys);
+        const float *gt = (const float *)(in + Sh::kKeys + Sh::kVals), *P = gt + Gates<C>::kFloats;
+        float4 *hand = hand_of(c - 1);
+        float x[C / 8][4] = {}, r[C / 8][4];
+#pragma unroll
+        for (int m = 0; m < C / 16; ++m) {
+          values_of<Sh::kValRow>(r[2 * m], r[2 * m + 1], ds, m, e0 - x0);
+#pragma unroll
+          for (int i = 0; i < 2; ++i) {
+            const LeftTf32<kSolve, kSums> a(r[2 * m + i]);
+#pragma unroll
+            for (int j = 0; j <= 2 * m + i; ++j) a.times(x[j], Rec::P::load(P, 2 * m + i, j));
+          }
+        }
+#pragma unroll
+        for (int j = 0; j < C / 8; ++j) {
+          hand[j * 32] = make_float4(x[j][0], x[j][1], x[j][2], x[j][3]);
+          const float2 up = *(const float2 *)(gt + Gates<C>::kUp + 8 * j + 2 * t);
+          const float ux = up.x * f.scale, uy = up.y * f.scale;
+          r[j][0] *= ux, r[j][1] *= uy, r[j][2] *= ux, r[j][3] *= uy;
+        }
+        float y[D / 8][4] = {};
+        state_update<kTerms, D, C>(y, 0.f, 0.f, r, qs);
+#pragma unroll
+        for (int d = 0; d < D / 8; ++d)
+          hand[(C / 8 + d) * 32] = make_float4(y[d][0], y[d][1], y[d][2], y[d][3]);
+      }
+      cp_async_wait_all();
     }
-    state_update<kTerms, D, C>(A, 1.f, 0.f, r, qs);
   }
-  if (p.dstate_in) store_state<D>(p.dstate_in + bh * D * D, A, e0);
+  if (!carry) return;
+  if (kOwn) store_state<D>(own + (bh * count + s) * D * D, A, e0);
+  else if (p.dstate_in && s == 0) store_state<D>(p.dstate_in + bh * D * D, A, e0);
 }
 
 // ------------------------------------------------------------- the chunks' own gradients
@@ -156,14 +214,36 @@ struct GradShape {
   static constexpr int kBytes = 3 * kTile + (2 * C * kWide + kStateFloats + kSmall) * 4;
 };
 
+__device__ __forceinline__ float2 pair_at(const float *p) { return *(const float2 *)p; }
+__device__ __forceinline__ float2 pair_at(const __nv_bfloat16 *p) { return bf2_to_f2(*(const uint32_t *)p); }
+
+// What store_packed left of a kTiles * 8 x D matrix (rows: tiles; columns: 16 by 16) into rows of
+// D + 8 floats, rounded for products of one term.
+template <int D, int kTiles, int kTerms, int kThreads>
+__device__ __forceinline__ void unpack(float *to, const float *from, int tid) {
+  const int g = (tid & 31) >> 2, t = tid & 3;
+#pragma unroll 4
+  for (int i = tid; i < D / 16 * kTiles * 32; i += kThreads) {
+    const int tile = i / 32, e = tile / kTiles * 16 + g, r = tile % kTiles * 8 + 2 * t;
+    const float4 v = __ldg((const float4 *)from + i);
+    float x[4] = {v.x, v.y, v.z, v.w};
+    if (kTerms == 1)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) x[j] = __uint_as_float(tf32_of(x[j]));
+    float *at = to + r * (D + 8) + e;
+    at[0] = x[0], at[D + 8] = x[1], at[8] = x[2], at[D + 16] = x[3];
+  }
+}
+
 // 16 rows from i on at columns k .. k + 7 of a tile, as the left operand of tf32 products; times
 // the rows' factors.
 template <int kTerms, int kRow, typename T>
 __device__ __forceinline__ LeftTf32<kTerms, kTerms == 3> left_rows(const T *tile, int i, int k, float fx = 1.f,
                                                       float fy = 1.f) {
   const int g = (threadIdx.x & 31) >> 2, t = threadIdx.x & 3;
-  const T *x = tile + (i + g) * kRow + k + 2 * t, *y = x + 8 * kRow;
-  const float c[4] = {fx * to_f(x[0]), fx * to_f(x[1]), fy * to_f(y[0]), fy * to_f(y[1])};
+  const float2 x = pair_at(tile + (i + g) * kRow + k + 2 * t);
+  const float2 y = pair_at(tile + (i + g + 8) * kRow + k + 2 * t);
+  const float c[4] = {fx * x.x, fx * x.y, fy * y.x, fy * y.y};
   return LeftTf32<kTerms, kTerms == 3>(c);
 }
 // x += (16 x 16 coefficients a, b) times rows i .. i + 15 of a raw tile.
@@ -236,9 +316,10 @@ __device__ __forceinline__ void row_dots(float &top, float &bottom, const float 
   top = bottom = 0.f;
 #pragma unroll
   for (int d = 0; d < D / 8; ++d) {
-    const T *a = tile + (i + g) * kRow + 8 * d + 2 * t, *b = a + 8 * kRow;
-    top = fmaf(x[d][0], to_f(a[0]), fmaf(x[d][1], to_f(a[1]), top));
-    bottom = fmaf(x[d][2], to_f(b[0]), fmaf(x[d][3], to_f(b[1]), bottom));
+    const float2 a = pair_at(tile + (i + g) * kRow + 8 * d + 2 * t);
+    const float2 b = pair_at(tile + (i + g + 8) * kRow + 8 * d + 2 * t);
+    top = fmaf(x[d][0], a.x, fmaf(x[d][1], a.y, top));
+    bottom = fmaf(x[d][2], b.x, fmaf(x[d][3], b.y, bottom));
   }
 #pragma unroll
   for (int m = 1; m < 4; m <<= 1) {
@@ -297,26 +378,35 @@ __global__ void __launch_bounds__(GradShape<T, D>::kThreads)
   load_rows<T, C, D, kThreads>(qs, (const T *)f.q + b * f.sq[0] + t0 * f.sq[1] + (long long)hk * D,
                                f.sq[1], n, tid);
   load_rows<T, C, D, kThreads>(ds, (const T *)p.d_o + row0 * D, (long long)orow, n, tid);
-  load_rows<float, C, D, kThreads>(us, misses + at * C * D, D, C, tid);
-  load_rows<float, C, D, kThreads>(vs, weights + at * C * D, D, C, tid);
-  load_rows<float, D, D, kThreads>(st, A1, D, D, tid);
   load_flat<Gates<C>::kFloats, kThreads>(gt, records + at * Rec::kFloats + Rec::kGates, tid);
   cp_async_commit();
+  // the misses and w (as they are: dbeta is a product of both)
+  unpack<D, C / 8, 3, kThreads>(us, misses + at * C * D, tid);
+  unpack<D, C / 8, 3, kThreads>(vs, weights + at * C * D, tid);
+  unpack<D, D / 8, kG, kThreads>(st, A1, tid);
   cp_async_wait_all();
   __syncthreads();
-  // dbeta, then u and dv in the places of the misses and w
-  for (int i = i0; i < i0 + 16; ++i) {
+  // dbeta, then u and dv in the places of the misses and w; four lanes a row
+#pragma unroll
+  for (int half = 0; half < 2; ++half) {
+    const int i = i0 + g + 8 * half;
     const float be = gt[Gates<C>::kBeta + i];
     float dot = 0.f;
 #pragma unroll
-    for (int d = lane; d < D; d += 32) {
-      const float m = us[i * kWide + d], x = vs[i * kWide + d];
-      dot = fmaf(m, x, dot);
-      us[i * kWide + d] = be * m, vs[i * kWide + d] = be * x;
+    for (int d = 4 * t; d < D; d += 16) {
+      float4 &m = *(float4 *)(us + i * kWide + d), &x = *(float4 *)(vs + i * kWide + d);
+      const float4 a = m, c = x;
+      dot = fmaf(a.x, c.x, fmaf(a.y, c.y, fmaf(a.z, c.z, fmaf(a.w, c.w, dot))));
+      m = make_float4(be * a.x, be * a.y, be * a.z, be * a.w);
+      x = make_float4(be * c.x, be * c.y, be * c.z, be * c.w);
+      if (kG == 1) {  // u is a right operand too
+        m.x = __uint_as_float(tf32_of(m.x)), m.y = __uint_as_float(tf32_of(m.y));
+        m.z = __uint_as_float(tf32_of(m.z)), m.w = __uint_as_float(tf32_of(m.w));
+      }
     }
-#pragma unroll
-    for (int m = 16; m > 0; m >>= 1) dot += __shfl_xor_sync(0xFFFFFFFFu, dot, m);
-    if (lane == 0 && i < n) store1(dbeta + (size_t)i * f.H, dot);
+    dot += __shfl_xor_sync(0xFFFFFFFFu, dot, 1);
+    dot += __shfl_xor_sync(0xFFFFFFFFu, dot, 2);
+    if (t == 0 && i < n) store1(dbeta + (size_t)i * f.H, dot);
   }
   __syncwarp();
   // products with the states.  G's shares: sums of rows of each term with the token's own vector
@@ -329,20 +419,20 @@ __global__ void __launch_bounds__(GradShape<T, D>::kThreads)
 #pragma unroll
     for (int d = 0; d < D / 8; ++d) {
       const float2 s = *(const float2 *)(st + (8 * d + g) * kWide + e + 2 * t);
-      a.times(y[d], s.x, s.y);
+      a.times_rounded(y[d], s.x, s.y);
     }
   }
   float to0, to1, all0, all1, q0, q1;
   row_dots<D>(to0, to1, y, ks, i0);
   __syncthreads();
   {
-    float dot = 0.f;  // S . A, as S takes A's place
+    float dot = 0.f;  // S . A
+#pragma unroll 4
     for (int i = tid; i < D * D / 4; i += kThreads) {
-      float4 *s = (float4 *)(st + i / (D / 4) * kWide + i % (D / 4) * 4);
-      const float4 a = *s, v = ((const float4 *)S0)[i];
+      const float4 a = __ldg((const float4 *)A1 + i), v = __ldg((const float4 *)S0 + i);
       dot = fmaf(a.x, v.x, fmaf(a.y, v.y, fmaf(a.z, v.z, fmaf(a.w, v.w, dot))));
-      *s = v;
     }
+    unpack<D, D / 8, kG, kThreads>(st, S0, tid);
 #pragma unroll
     for (int m = 16; m > 0; m >>= 1) dot += __shfl_xor_sync(0xFFFFFFFFu, dot, m);
     if (lane == 0) dots[w] = dot;
@@ -355,8 +445,8 @@ __global__ void __launch_bounds__(GradShape<T, D>::kThreads)
 #pragma unroll
     for (int d = 0; d < D / 8; ++d) {
       const float2 s = *(const float2 *)(st + (8 * d + g) * kWide + e + 2 * t);
-      a.times(x[d], s.x, s.y);
-      c.times(y[d], s.x, s.y);
+      a.times_rounded(x[d], s.x, s.y);
+      c.times_rounded(y[d], s.x, s.y);
     }
   }
   row_dots<D>(q0, q1, x, qs, i0);
@@ -375,8 +465,8 @@ __global__ void __launch_bounds__(GradShape<T, D>::kThreads)
 #pragma unroll
       for (int q = 0; q < 2; ++q) {
         const float2 u = *(const float2 *)(us + (j0 + 8 * q + g) * kWide + e + 2 * t);
-        l.times(a[q], u.x, u.y);
-        m.times(c[q], u.x, u.y);
+        l.times_rounded(a[q], u.x, u.y);
+        m.times_rounded(c[q], u.x, u.y);
       }
     }
 #pragma unroll
@@ -470,7 +560,7 @@ __global__ void __launch_bounds__(GradShape<T, D>::kThreads)
 
 // Scratch of the backward pass, in floats from one base.
 struct Layout {
-  size_t records, states, misses, after, weights, before, dq, dk, total;
+  size_t records, states, misses, after, weights, before, own, moves, dq, dk, total;
   Segments segments;
 };
 template <typename T>
@@ -487,7 +577,7 @@ Layout layout_of(const DeltaBackArgs &p, bool exact) {
   take(l.misses, all * C * a.D);
   take(l.weights, all * C * a.D);
   l.segments = segments_of(a);
-  take(l.before, l.segments.floats(a));
+  for (size_t *to : {&l.before, &l.own, &l.moves}) take(*to, l.segments.floats(a));
   const size_t plane = a.H == a.Hk ? 0 : (size_t)a.B * a.N * a.H * a.D;
   take(l.dq, plane);
   take(l.dk, plane);
@@ -522,15 +612,30 @@ cudaError_t back_launch(const DeltaBackArgs &p, float *s, cudaStream_t st) {
   const int nc = chunks_of<T>(a);
   cudaError_t e;
   if ((e = save_forward(a, l.segments, kSolve == 3, s + l.records, s + l.states, s + l.misses,
-                        s + l.before, st)) != cudaSuccess)
+                        s + l.before, s + l.moves, st)) != cudaSuccess)
     return e;
-  const auto reverse = reverse_kernel<T, D, kTerms, kSolve>;
+  const Segments &g = l.segments;
+  const float *records = s + l.records;
+  const dim3 grid(a.H * Sh::kSplit, a.B, g.count), block(Sh::kThreads);
+  if (g.count > 1) {
+    const auto own = reverse_kernel<T, D, kTerms, kSolve, true>;
+    if ((e = cudaFuncSetAttribute(own, cudaFuncAttributeMaxDynamicSharedMemorySize, Sh::kBytes)) !=
+        cudaSuccess)
+      return e;
+    count_launch();
+    if ((e = launch_pdl(own, grid, block, Sh::kBytes, st, p, records, (float *)nullptr,
+                        (float *)nullptr, s + l.own, nc, g.chunks, g.count)) != cudaSuccess)
+      return e;
+    if ((e = join_segments(a, g, true, p.dstate, s + l.own, s + l.moves, st)) != cudaSuccess)
+      return e;
+  }
+  const auto reverse = reverse_kernel<T, D, kTerms, kSolve, false>;
   if ((e = cudaFuncSetAttribute(reverse, cudaFuncAttributeMaxDynamicSharedMemorySize, Sh::kBytes)) !=
       cudaSuccess)
     return e;
   count_launch();
-  if ((e = launch_pdl(reverse, dim3(a.H, a.B), dim3(Sh::kThreads), Sh::kBytes, st, p,
-                      (const float *)(s + l.records), s + l.after, s + l.weights, nc)) != cudaSuccess)
+  if ((e = launch_pdl(reverse, grid, block, Sh::kBytes, st, p, records, s + l.after, s + l.weights,
+                      s + l.own, nc, g.chunks, g.count)) != cudaSuccess)
     return e;
   if (a.H == a.Hk) return grads_launch<T, T, D, kSolve>(p, l, s, (T *)p.dq, (T *)p.dk, st);
   float *dq = s + l.dq, *dk = s + l.dk;

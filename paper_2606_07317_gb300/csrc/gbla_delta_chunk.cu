@@ -310,9 +310,8 @@ __global__ void __launch_bounds__(PrepShape<T, D>::kThreads, 5)
 // A block carries E = min(D, 64) of the state's columns through the chunks of a segment of a
 // sequence, 16 a warp in kCarry warps.  What the columns need for the next chunk is a chain:
 //   S^T k -> r -> miss = M r -> u -> S',
-// and everything else is taken off it: a second warp for each first one fetches tiles, and forms
-// the results of the chunk before, from the state and u that the first one leaves in shared
-// memory.  One barrier a chunk.
+// and everything else is taken off it: other warps fetch tiles, and form the results of the chunk
+// before, from the state and u that the first ones leave in shared memory.  One barrier a chunk.
 //
 // What it is for: results (kResults), the states and misses that the backward pass needs
 // (kSave), or what a segment does to the state before it (kSegment): E columns of its own
@@ -327,31 +326,31 @@ struct ScanShape {
   // not fit into shared memory)
   static constexpr bool kNarrow = sizeof(T) == 2 && D == 128 && kSolve == 3 && kFor == kResults;
   static constexpr int C = kChunkOf<T>, E = D < 64 ? D : kNarrow ? 32 : 64, kSplit = D / E;
-  // (kSegment: the other warps only fetch, half as many do, and two blocks fit an SM)
-  static constexpr int kCarry = E / 16, kHelp = kFor == kSegment && kCarry > 2 ? 2 : kCarry;
+  // (without results the other warps only fetch, half as many do, and two blocks fit an SM)
+  static constexpr int kCarry = E / 16, kHelp = kFor != kResults && kCarry > 2 ? 2 : kCarry;
   static constexpr int kThreads = (kCarry + kHelp) * 32;
-  static constexpr int kBlocks = kFor == kSegment && (D < 128 || kSolve == 1) ? 2 : 1;
+  static constexpr int kBlocks = kFor != kResults && (D < 128 || kSolve == 1) ? 2 : 1;
   static constexpr int kRow = pad_row<T>(D), kValRow = pad_row<T>(E);
   // bytes: keys, values, M and gates of a chunk; queries, P and gates of the one before
   static constexpr int kKeys = C * kRow * (int)sizeof(T), kVals = C * kValRow * (int)sizeof(T);
   static constexpr int kRecord = Rec::kP * 4, kFirst = kKeys + kVals + kRecord;
   static constexpr int kSecond = kFor == kResults ? kKeys + (Rec::P::kFloats + C) * 4 : 0;
-  // what a warp hands on: its state before the chunk and u (kSave: the misses)
-  static constexpr int kHand = kFor == kSegment ? 0 : (kHandWords<D> + C / 8) * 32 * 16;
+  // what a warp hands on: its state before the chunk and u
+  static constexpr int kHand = kFor != kResults ? 0 : (kHandWords<D> + C / 8) * 32 * 16;
   static constexpr int kBytes = 2 * (kFirst + kSecond + kCarry * kHand);
   static_assert(kBytes <= 227 * 1024, "shared memory of a block");
 };
 
 // kTerms: bf16 numbers that stand for a value of the state where it meets a key or takes a
 // write (fp32: 3 tf32 products); kSolve: terms of the product with M.
-// Segments have `seg` chunks; `before` holds the states before all but the first, or takes what
-// kSegment forms, [B H][segments - 1][D][D], the matrices in `moves`.  Records are `stride` floats
+// Segments have `seg` chunks; `before` holds the states after all but the last, or takes what
+// kSegment forms, the matrices in `moves`, [B H][count][D][D] both.  Records are `stride` floats
 // apart (their M and gates lie at the same place in both forms).
 template <typename T, int D, int kTerms, int kSolve, Purpose kFor>
 __global__ void __launch_bounds__(ScanShape<T, D, kSolve, kFor>::kThreads,
                                   ScanShape<T, D, kSolve, kFor>::kBlocks)
     scan_kernel(const DeltaArgs p, const float *records, float *states, float *misses,
-                float *before, float *moves, int nc, int seg, int stride) {
+                float *before, float *moves, int nc, int seg, int count, int stride) {
   using Sh = ScanShape<T, D, kSolve, kFor>;
   using Rec = typename Sh::Rec;
   constexpr int C = Sh::C, E = Sh::E, kCarry = Sh::kCarry, kFetch = Sh::kHelp * 32;
@@ -368,8 +367,9 @@ __global__ void __launch_bounds__(ScanShape<T, D, kSolve, kFor>::kThreads,
   const int L = p.seq_lens ? min(max(__ldg(p.seq_lens + b), 0), p.N) : p.N;
   const size_t bh = (size_t)b * p.H + h;
   const int chunks = (L + C - 1) / C, first = s * seg, end = min(chunks, first + seg);
-  const int last = gridDim.z;  // segments, but for kSegment, which leaves the last one out
-  if (kFor == kSegment ? first + seg >= chunks : s > 0 && first >= chunks) return;
+  // (gridDim.z: all segments, or, for kSegment in the forward pass, those that another follows)
+  if (s > 0 && first >= chunks) return;
+  if (kFor == kSegment && (chunks == 0 || ((int)gridDim.z < count && end == chunks))) return;
   const T *kg = (const T *)p.k + b * p.sk[0] + (long long)hk * D;
   const T *qg = (const T *)p.q + b * p.sq[0] + (long long)hk * D;
   const T *vg = (const T *)p.v + b * p.sv[0] + (long long)h * D + x0;
@@ -408,7 +408,7 @@ __global__ void __launch_bounds__(ScanShape<T, D, kSolve, kFor>::kThreads,
           S[d][i] = 8 * d + 2 * t + (i & 1) == e0 + g + (i >> 1) * 8 ? 1.f : 0.f;
     } else {
       const float *from = kFor == kSegment ? nullptr
-                          : s > 0          ? before + (bh * (last - 1) + s - 1) * D * D
+                          : s > 0          ? before + (bh * count + s - 1) * D * D
                           : p.init         ? p.init + bh * D * D
                                            : nullptr;
       load_state<D>(S, from, e0);
@@ -418,7 +418,7 @@ __global__ void __launch_bounds__(ScanShape<T, D, kSolve, kFor>::kThreads,
     cp_async_commit();
     cp_async_wait_all();
   }
-  const int rounds = kFor == kSegment ? end : end + 1;
+  const int rounds = kFor == kResults ? end + 1 : end;
   for (int c = first; c < rounds; ++c) {
     __syncthreads();  // this round's tiles and what was handed on are there, the others are read
     if (carry) {
@@ -428,11 +428,7 @@ __global__ void __launch_bounds__(ScanShape<T, D, kSolve, kFor>::kThreads,
       const float *M = (const float *)(in + Sh::kKeys + Sh::kVals), *gt = M + Rec::kGates;
       uint4 *hand = hand_of(c);
       float r[C / 8][4] = {};
-      if (kFor == kSave) {
-#pragma unroll
-        for (int d = 0; d < D / 8; ++d)
-          ((float4 *)hand)[d * 32 + lane] = make_float4(S[d][0], S[d][1], S[d][2], S[d][3]);
-      }
+      if (kFor == kSave) store_packed(states + (bh * nc + c) * D * D, S, e0);
       key_products<kTerms, D, C, kFor == kResults>(S, ks, r, hand);
 #pragma unroll
       for (int m = 0; m < C / 16; ++m) {
@@ -464,10 +460,10 @@ __global__ void __launch_bounds__(ScanShape<T, D, kSolve, kFor>::kThreads,
 #pragma unroll
           for (int i = 0; i < 4; ++i) r[half * kHalf + m][i] += x[m][i];
       }
+      if (kFor == kSave) store_packed(misses + (bh * nc + c) * C * D, r, e0);
 #pragma unroll
       for (int j = 0; j < C / 8; ++j) {
         float4 *to = (float4 *)hand + (kHandWords<D> + j) * 32 + lane;
-        if (kFor == kSave) *to = make_float4(r[j][0], r[j][1], r[j][2], r[j][3]);
         const float2 be = *(const float2 *)(gt + Gates<C>::kBeta + 8 * j + 2 * t);
         r[j][0] *= be.x, r[j][1] *= be.y, r[j][2] *= be.x, r[j][3] *= be.y;
         if (kFor == kResults) *to = make_float4(r[j][0], r[j][1], r[j][2], r[j][3]);
@@ -479,25 +475,11 @@ __global__ void __launch_bounds__(ScanShape<T, D, kSolve, kFor>::kThreads,
       if (c + 1 < end) fetch_first(c + 1);
       if (kFor == kResults && c < end) fetch_second(c);
       cp_async_commit();
-      if (kFor != kSegment && c > first) {  // the chunk before
-        const int d0 = c - 1;
-        const uint4 *hand = hand_of(d0);
-        const float4 *us = (const float4 *)hand + kHandWords<D> * 32 + lane;
-        if constexpr (kFor == kSave) {
-          float x[D / 8][4];
-#pragma unroll
-          for (int d = 0; d < D / 8; ++d) {
-            const float4 v = ((const float4 *)hand)[d * 32 + lane];
-            x[d][0] = v.x, x[d][1] = v.y, x[d][2] = v.z, x[d][3] = v.w;
-          }
-          store_state<D>(states + (bh * nc + d0) * D * D, x, e0);
-#pragma unroll
-          for (int j = 0; j < C / 8; ++j) {
-            const float4 v = us[j * 32];
-            const float m[4] = {v.x, v.y, v.z, v.w};
-            store_tile(misses + (bh * nc + d0) * C * D + e0, D, m, 8 * j, C);
-          }
-        } else {
+      if constexpr (kFor == kResults)
+        if (c > first) {  // the chunk before
+          const int d0 = c - 1;
+          const uint4 *hand = hand_of(d0);
+          const float4 *us = (const float4 *)hand + kHandWords<D> * 32 + lane;
           const char *in = second_of(d0);
           const float *P = (const float *)(in + Sh::kKeys), *ups = P + Rec::P::kFloats;
           T *og = (T *)p.o + (((size_t)b * p.N + (size_t)d0 * C) * p.H + h) * D + e0;
@@ -520,13 +502,12 @@ __global__ void __launch_bounds__(ScanShape<T, D, kSolve, kFor>::kThreads,
             store_tile(og, orow, o[j], 8 * j, n);  // no later u meets it
           }
         }
-      }
       cp_async_wait_all();
     }
   }
   if (!carry) return;
   if (kFor == kSegment) {
-    const size_t at = (bh * last + s) * D * D;
+    const size_t at = (bh * count + s) * D * D;
     store_state<D>((move ? moves : before) + at, S, e0);
   } else if (kFor == kResults && p.fin && (end == chunks)) {
     store_state<D>(p.fin + bh * D * D, S, e0);
@@ -534,17 +515,16 @@ __global__ void __launch_bounds__(ScanShape<T, D, kSolve, kFor>::kThreads,
 }
 
 // --------------------------------------------------------------- between segments
-// Turns what each segment forms by itself into the state after it, in place: S' = move S + own,
-// one segment after the other.  A block takes E of the state's columns of one (batch, head).
+// A block takes E of the state's columns of one (batch, head).
 template <int D>
 struct JoinShape {
   static constexpr int E = D < 64 ? D : 64, kThreads = E * 2, kRow = D + 8;
   static constexpr int kBytes = 2 * D * kRow * 4;
 };
-template <int D>
+template <int D, bool kBack>
 __global__ void __launch_bounds__(JoinShape<D>::kThreads)
-    join_kernel(const float *init, const int32_t *seq_lens, float *before, const float *moves, int N,
-                int H, int tokens, int ns) {
+    join_kernel(const float *init, const int32_t *seq_lens, float *own, const float *moves, int N,
+                int H, int tokens, int count) {
   using Sh = JoinShape<D>;
   constexpr int kThreads = Sh::kThreads, kRow = Sh::kRow;
   extern __shared__ __align__(16) char raw[];
@@ -553,39 +533,46 @@ __global__ void __launch_bounds__(JoinShape<D>::kThreads)
   const int h = blockIdx.y, b = blockIdx.z, tid = threadIdx.x, g = (tid & 31) >> 2, t = tid & 3;
   const int e0 = blockIdx.x * Sh::E + tid / 32 * 16;
   const int L = seq_lens ? min(max(__ldg(seq_lens + b), 0), N) : N;
-  const int steps = (L + tokens - 1) / tokens - 1;  // segments that another one follows
+  const int ns = (L + tokens - 1) / tokens, steps = ns - 1;
   if (steps <= 0) return;
   const size_t bh = (size_t)b * H + h;
-  before += bh * ns * D * D, moves += bh * ns * D * D;
-  auto fetch = [&](int s) {
-    load_rows<float, D, D, kThreads>(tile + (s & 1) * D * kRow, moves + (size_t)s * D * D, D, D, tid);
+  own += bh * count * D * D, moves += bh * count * D * D;
+  // the i-th segment in order, 0 .. ns - 2 or ns - 1 .. 1
+  auto at = [&](int i) { return (size_t)(kBack ? ns - 1 - i : i) * D * D; };
+  auto fetch = [&](int i) {
+    load_rows<float, D, D, kThreads>(tile + (i & 1) * D * kRow, moves + at(i), D, D, tid);
   };
   float S[D / 8][4];
   load_state<D>(S, init ? init + bh * D * D : nullptr, e0);
   fetch(0);
   cp_async_commit();
-  for (int s = 0; s < steps; ++s) {
-    float own[D / 8][4], x[D / 8][4] = {};
-    load_state<D>(own, before + (size_t)s * D * D, e0);
+  for (int i = 0; i < steps; ++i) {
+    float add[D / 8][4], x[D / 8][4] = {};
+    load_state<D>(add, own + at(i), e0);
     cp_async_wait_all();
     __syncthreads();
-    if (s + 1 < steps) fetch(s + 1);
+    if (i + 1 < steps) fetch(i + 1);
     cp_async_commit();
-    const float *m = tile + (s & 1) * D * kRow;
+    const float *m = tile + (i & 1) * D * kRow;
 #pragma unroll
     for (int k = 0; k < D / 8; ++k) {
       const LeftTf32<3> a(S[k]);
 #pragma unroll
       for (int n = 0; n < D / 8; ++n) {
-        const float2 v = *(const float2 *)(m + (8 * n + g) * kRow + 8 * k + 2 * t);
-        a.times(x[n], v.x, v.y);
+        if (kBack) {
+          const float *v = m + (8 * k + 2 * t) * kRow + 8 * n + g;
+          a.times(x[n], v[0], v[kRow]);
+        } else {
+          const float2 v = *(const float2 *)(m + (8 * n + g) * kRow + 8 * k + 2 * t);
+          a.times(x[n], v.x, v.y);
+        }
       }
     }
 #pragma unroll
     for (int d = 0; d < D / 8; ++d)
 #pragma unroll
-      for (int i = 0; i < 4; ++i) S[d][i] = x[d][i] + own[d][i];
-    store_state<D>(before + (size_t)s * D * D, S, e0);
+      for (int e = 0; e < 4; ++e) S[d][e] = x[d][e] + add[d][e];
+    store_state<D>(own + at(i), S, e0);
   }
 }
 
@@ -605,16 +592,27 @@ cudaError_t allow_smem(K kernel, int bytes) {
   return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
 }
 
+template <int D, bool kBack>
+cudaError_t join_launch(const DeltaArgs &a, const Segments &g, const float *init, float *own,
+                        const float *moves, cudaStream_t st) {
+  using Jo = JoinShape<D>;
+  const auto join = join_kernel<D, kBack>;
+  cudaError_t e;
+  if ((e = allow_smem(join, Jo::kBytes)) != cudaSuccess) return e;
+  const int C = a.dtype == GBLA_FP32 ? kChunkOf<float> : kChunkOf<__nv_bfloat16>;
+  count_launch();
+  return launch_pdl(join, dim3(D / Jo::E, a.H, a.B), dim3(Jo::kThreads), Jo::kBytes, st, init,
+                    a.seq_lens, own, moves, a.N, a.H, g.chunks * C, g.count);
+}
+
 template <typename T, int D, int kTerms, int kSolve, Purpose kFor>
 cudaError_t launch(const DeltaArgs &a, const Segments &g, float *records, float *states,
-                   float *misses, float *before, cudaStream_t st) {
+                   float *misses, float *before, float *moves, cudaStream_t st) {
   using Pr = PrepShape<T, D>;
   using Sc = ScanShape<T, D, kSolve, kFor>;
   using Se = ScanShape<T, D, kSolve, kSegment>;
-  using Jo = JoinShape<D>;
   static_assert(kFor != kSegment, "");
   const int nc = chunks_of<T>(a), stride = Record<T, kSolve, kFor == kSave>::kFloats;
-  float *moves = before + (size_t)a.B * a.H * (g.count - 1) * D * D;
   cudaError_t e;
   const auto prep = prepare_kernel<T, D, kSolve, kFor == kSave>;
   if ((e = allow_smem(prep, Pr::kBytes)) != cudaSuccess) return e;
@@ -626,61 +624,83 @@ cudaError_t launch(const DeltaArgs &a, const Segments &g, float *records, float 
     const auto own = scan_kernel<T, D, kTerms, kSolve, kSegment>;
     if ((e = allow_smem(own, Se::kBytes)) != cudaSuccess) return e;
     count_launch();
-    if ((e = launch_pdl(own, dim3(2 * Se::kSplit * a.H, a.B, g.count - 1), dim3(Se::kThreads),
-                        Se::kBytes, st, a, (const float *)records, (float *)nullptr,
-                        (float *)nullptr, before, moves, nc, g.chunks, stride)) != cudaSuccess)
+    // (the backward pass moves its gradients by the last segment's matrix too)
+    if ((e = launch_pdl(own, dim3(2 * Se::kSplit * a.H, a.B, kFor == kSave ? g.count : g.count - 1),
+                        dim3(Se::kThreads), Se::kBytes, st, a, (const float *)records,
+                        (float *)nullptr, (float *)nullptr, before, moves, nc, g.chunks, g.count,
+                        stride)) != cudaSuccess)
       return e;
-    const auto join = join_kernel<D>;
-    if ((e = allow_smem(join, Jo::kBytes)) != cudaSuccess) return e;
-    count_launch();
-    if ((e = launch_pdl(join, dim3(D / Jo::E, a.H, a.B), dim3(Jo::kThreads), Jo::kBytes, st, a.init,
-                        a.seq_lens, before, (const float *)moves, a.N, a.H,
-                        g.chunks * kChunkOf<T>, g.count - 1)) != cudaSuccess)
-      return e;
+    if ((e = join_launch<D, false>(a, g, a.init, before, moves, st)) != cudaSuccess) return e;
   }
   const auto scan = scan_kernel<T, D, kTerms, kSolve, kFor>;
   if ((e = allow_smem(scan, Sc::kBytes)) != cudaSuccess) return e;
   count_launch();
   return launch_pdl(scan, dim3(Sc::kSplit * a.H, a.B, g.count), dim3(Sc::kThreads), Sc::kBytes, st,
-                    a, (const float *)records, states, misses, before, moves, nc, g.chunks, stride);
+                    a, (const float *)records, states, misses, before, moves, nc, g.chunks, g.count,
+                    stride);
 }
 
 template <int D>
-cudaError_t forward_d(const DeltaArgs &a, const Segments &g, float *records, float *before,
+cudaError_t forward_d(const DeltaArgs &a, const Segments &g, float *rec, float *before, float *moves,
                       cudaStream_t st) {
   if (a.dtype == GBLA_FP32)
-    return launch<float, D, 3, 3, kResults>(a, g, records, nullptr, nullptr, before, st);
+    return launch<float, D, 3, 3, kResults>(a, g, rec, nullptr, nullptr, before, moves, st);
   if (exact_state(a))
-    return launch<__nv_bfloat16, D, 3, 3, kResults>(a, g, records, nullptr, nullptr, before, st);
-  return launch<__nv_bfloat16, D, 2, 1, kResults>(a, g, records, nullptr, nullptr, before, st);
+    return launch<__nv_bfloat16, D, 3, 3, kResults>(a, g, rec, nullptr, nullptr, before, moves, st);
+  return launch<__nv_bfloat16, D, 2, 1, kResults>(a, g, rec, nullptr, nullptr, before, moves, st);
 }
 template <int D>
-cudaError_t save_d(const DeltaArgs &a, const Segments &g, bool exact, float *records, float *states,
-                   float *misses, float *before, cudaStream_t st) {
+cudaError_t save_d(const DeltaArgs &a, const Segments &g, bool exact, float *rec, float *states,
+                   float *misses, float *before, float *moves, cudaStream_t st) {
   if (a.dtype == GBLA_FP32)
-    return launch<float, D, 3, 3, kSave>(a, g, records, states, misses, before, st);
+    return launch<float, D, 3, 3, kSave>(a, g, rec, states, misses, before, moves, st);
   if (exact)
-    return launch<__nv_bfloat16, D, 3, 3, kSave>(a, g, records, states, misses, before, st);
-  return launch<__nv_bfloat16, D, 2, 1, kSave>(a, g, records, states, misses, before, st);
+    return launch<__nv_bfloat16, D, 3, 3, kSave>(a, g, rec, states, misses, before, moves, st);
+  return launch<__nv_bfloat16, D, 2, 1, kSave>(a, g, rec, states, misses, before, moves, st);
 }
 
 }  // namespace
 
+// How many segments.  In units of a chunk in a scan of whole sequences (measured, bf16 D = 64:
+// 2.1 us): a round of blocks takes a segment's chunks; the scan that forms the segments' own
+// states and matrices as much (twice the columns, twice the blocks an SM); and a segment that
+// is joined 1.2.  B2 H8 N32768: 1 segment 1125 us, 4 530, 9 375, 19 389; B8 H8 N2048 is not cut
+// (132 us, 2 segments 127, 4 145).
 Segments segments_of(const DeltaArgs &a) {
   const int nc = a.dtype == GBLA_FP32 ? chunks_of<float>(a) : chunks_of<__nv_bfloat16>(a);
   const long long blocks = (long long)a.B * a.H * (a.D > 64 ? 2 : 1), sms = sm_count();
   Segments best = {1, nc};
+  double least = 0.;
+  for (int want = 1; want <= 64 && want <= nc; ++want) {
+    const int chunks = (nc + want - 1) / want, count = (nc + chunks - 1) / chunks;
+    double cost = (double)((blocks * count + sms - 1) / sms) * chunks;
+    if (count > 1)
+      cost += (double)((blocks * (count - 1) + sms - 1) / sms) * chunks + 1.2 * (count - 1) + 4.;
+    if (want == 1 || cost < least) least = cost, best = {count, chunks};
+  }
   const char *force = getenv("SEG");
-  if (force && atoi(force) > 1) { best.chunks = (nc + atoi(force) - 1) / atoi(force); best.count = (nc + best.chunks - 1) / best.chunks; }
-  (void)blocks; (void)sms;
+  if (force) { int w = atoi(force) < nc ? atoi(force) : nc; best.chunks = (nc + w - 1) / w; best.count = (nc + best.chunks - 1) / best.chunks; }
   return best;
 }
 
-cudaError_t save_forward(const DeltaArgs &a, const Segments &g, bool exact, float *records,
-                         float *states, float *misses, float *before, cudaStream_t st) {
-  if (a.D == 32) return save_d<32>(a, g, exact, records, states, misses, before, st);
-  if (a.D == 64) return save_d<64>(a, g, exact, records, states, misses, before, st);
-  return save_d<128>(a, g, exact, records, states, misses, before, st);
+cudaError_t save_forward(const DeltaArgs &a, const Segments &g, bool exact, float *rec,
+                         float *states, float *misses, float *before, float *moves,
+                         cudaStream_t st) {
+  if (a.D == 32) return save_d<32>(a, g, exact, rec, states, misses, before, moves, st);
+  if (a.D == 64) return save_d<64>(a, g, exact, rec, states, misses, before, moves, st);
+  return save_d<128>(a, g, exact, rec, states, misses, before, moves, st);
+}
+
+cudaError_t join_segments(const DeltaArgs &a, const Segments &g, bool back, const float *init,
+                          float *own, const float *moves, cudaStream_t st) {
+  if (a.D == 32)
+    return back ? join_launch<32, true>(a, g, init, own, moves, st)
+                : join_launch<32, false>(a, g, init, own, moves, st);
+  if (a.D == 64)
+    return back ? join_launch<64, true>(a, g, init, own, moves, st)
+                : join_launch<64, false>(a, g, init, own, moves, st);
+  return back ? join_launch<128, true>(a, g, init, own, moves, st)
+              : join_launch<128, false>(a, g, init, own, moves, st);
 }
 
 }  // namespace delta
@@ -695,15 +715,15 @@ static size_t record_floats(const DeltaArgs &a) {
 }
 
 size_t delta_forward_floats(const DeltaArgs &a) {
-  return record_floats(a) + delta::segments_of(a).floats(a);
+  return record_floats(a) + 2 * delta::segments_of(a).floats(a);
 }
 
 cudaError_t delta_forward(const DeltaArgs &a, float *scratch, cudaStream_t st) {
   const delta::Segments g = delta::segments_of(a);
-  float *before = scratch + record_floats(a);
-  if (a.D == 32) return delta::forward_d<32>(a, g, scratch, before, st);
-  if (a.D == 64) return delta::forward_d<64>(a, g, scratch, before, st);
-  return delta::forward_d<128>(a, g, scratch, before, st);
+  float *before = scratch + record_floats(a), *moves = before + g.floats(a);
+  if (a.D == 32) return delta::forward_d<32>(a, g, scratch, before, moves, st);
+  if (a.D == 64) return delta::forward_d<64>(a, g, scratch, before, moves, st);
+  return delta::forward_d<128>(a, g, scratch, before, moves, st);
 }
 
 }  // namespace gbla

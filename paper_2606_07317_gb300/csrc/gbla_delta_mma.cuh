@@ -89,7 +89,12 @@ struct LeftTf32 {
     tf32_split(b1, h1, l1);
     times(c, make_uint4(h0, h1, l0, l1));
   }
-  // or rounded or split before.
+  // rounded before (one term),
+  __device__ __forceinline__ void times_rounded(float (&c)[4], float b0, float b1) const {
+    if (kTerms == 1) mma_tf32(c, hi, __float_as_uint(b0), __float_as_uint(b1));
+    else times(c, b0, b1);
+  }
+  // or rounded or split before, and packed.
   __device__ __forceinline__ void times(float (&c)[4], const uint2 &b) const {
     mma_tf32(c, hi, b.x, b.y);
   }
@@ -346,6 +351,14 @@ __device__ __forceinline__ void store_state(float *to, const float (&S)[D / 8][4
     for (int i = 0; i < 4; ++i)
       to[(8 * d + 2 * t + (i & 1)) * D + e0 + g + (i >> 1) * 8] = S[d][i];
 }
+// The same between the launches of the backward pass, as the warps hold it: a float4 a lane for
+// each 8 of a matrix's rows (kTiles; or of a chunk's tokens), one 16 columns after the other.
+template <int kTiles>
+__device__ __forceinline__ void store_packed(float *to, const float (&x)[kTiles][4], int e0) {
+  float4 *at = (float4 *)to + e0 / 16 * kTiles * 32 + (threadIdx.x & 31);
+#pragma unroll
+  for (int i = 0; i < kTiles; ++i) at[i * 32] = make_float4(x[i][0], x[i][1], x[i][2], x[i][3]);
+}
 // S = (hi + lo) S + w^T k over the chunk's tokens.  The chunk's own sum starts from zero and is
 // added in one rounding: the tensor cores cut off what their accumulator cannot hold, which
 // over the chunks of a long sequence would shrink the state.
@@ -437,19 +450,25 @@ __device__ __forceinline__ void store_tile(float *o, size_t stride, const float 
 // ------------------------------------------------------------- between the files
 template <typename T>
 int chunks_of(const DeltaArgs &a) { return (a.N + kChunkOf<T> - 1) / kChunkOf<T>; }
-// A sequence is cut into `count` segments of `chunks` chunks (the last one shorter).
+// A sequence is cut into `count` segments of `chunks` chunks (the last one shorter).  Scratch: a
+// state and a matrix for each, [B H][count][D][D].
 struct Segments {
   int count, chunks;
-  // scratch: a state and a matrix for each segment but the last
   size_t floats(const DeltaArgs &a) const {
-    return 2 * (size_t)a.B * a.H * (count - 1) * a.D * a.D;
+    return count > 1 ? (size_t)a.B * a.H * count * a.D * a.D : 0;
   }
 };
 Segments segments_of(const DeltaArgs &a);
-// First part of the backward pass: records (of the backward's form), the state before every
-// chunk [B H chunks][D][D] and the misses [B H chunks][C][D].  exact: three terms throughout.
+// First part of the backward pass: records (of the backward's form), the states before all
+// chunks and the misses, packed; `moves`: the matrices that segments move a state by.  exact:
+// three terms throughout.
 cudaError_t save_forward(const DeltaArgs &a, const Segments &g, bool exact, float *records,
-                         float *states, float *misses, float *before, cudaStream_t st);
+                         float *states, float *misses, float *before, float *moves,
+                         cudaStream_t st);
+// Turns what each segment forms by itself into the state after it (kBack: before it), in place:
+// S' = move S + own (A' = move^T A + own), one segment after the other.
+cudaError_t join_segments(const DeltaArgs &a, const Segments &g, bool back, const float *init,
+                          float *own, const float *moves, cudaStream_t st);
 
 }  // namespace delta
 }  // namespace gbla

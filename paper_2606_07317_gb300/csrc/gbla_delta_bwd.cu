@@ -210,27 +210,34 @@ struct GradShape {
   static constexpr int kRow = pad_row<T>(D), kWide = D + 8, kMat = C + 4;
   static constexpr int kTile = C * kRow * (int)sizeof(T);
   static constexpr int kStateFloats = D * kWide > 2 * C * kMat ? D * kWide : 2 * C * kMat;
-  static constexpr int kSmall = Gates<C>::kFloats + 2 * C + kWarps * C + 4 + kWarps;
+  static constexpr int kSmall = Gates<C>::kFloats + 2 * C + 2 * kWarps * C + 4 + kWarps;
+  // words of packed matrices a thread fetches: of C x D and D x D, the latter at most 16 at a time
+  static constexpr int kRowWords = C * D / 4 / kThreads, kStateWords = D * D / 4 / kThreads;
+  static constexpr int kBatch = kStateWords < 16 ? kStateWords : 16;
   static constexpr int kBytes = 3 * kTile + (2 * C * kWide + kStateFloats + kSmall) * 4;
 };
 
 __device__ __forceinline__ float2 pair_at(const float *p) { return *(const float2 *)p; }
 __device__ __forceinline__ float2 pair_at(const __nv_bfloat16 *p) { return bf2_to_f2(*(const uint32_t *)p); }
 
-// What store_packed left of a kTiles * 8 x D matrix (rows: tiles; columns: 16 by 16) into rows of
-// D + 8 floats, rounded for products of one term.
-template <int D, int kTiles, int kTerms, int kThreads>
-__device__ __forceinline__ void unpack(float *to, const float *from, int tid) {
-  const int g = (tid & 31) >> 2, t = tid & 3;
-#pragma unroll 4
-  for (int i = tid; i < D / 16 * kTiles * 32; i += kThreads) {
-    const int tile = i / 32, e = tile / kTiles * 16 + g, r = tile % kTiles * 8 + 2 * t;
-    const float4 v = __ldg((const float4 *)from + i);
-    float x[4] = {v.x, v.y, v.z, v.w};
+// What store_packed left of a kTiles * 8 x D matrix (rows: tiles; columns: 16 by 16): words
+// first, first + kThreads, ... of a thread, all in flight before the first is used, and into rows
+// of D + 8 floats, rounded for products of one term.
+template <int kThreads, int kN>
+__device__ __forceinline__ void fetch_packed(float4 (&v)[kN], const float *from, int first) {
+#pragma unroll
+  for (int i = 0; i < kN; ++i) v[i] = __ldg((const float4 *)from + first + i * kThreads);
+}
+template <int D, int kTiles, int kTerms, int kThreads, int kN>
+__device__ __forceinline__ void spread(float *to, const float4 (&v)[kN], int first) {
+#pragma unroll
+  for (int n = 0; n < kN; ++n) {
+    const int i = first + n * kThreads, tile = i / 32, g = (i & 31) >> 2, t = i & 3;
+    float x[4] = {v[n].x, v[n].y, v[n].z, v[n].w};
     if (kTerms == 1)
 #pragma unroll
       for (int j = 0; j < 4; ++j) x[j] = __uint_as_float(tf32_of(x[j]));
-    float *at = to + r * (D + 8) + e;
+    float *at = to + (tile % kTiles * 8 + 2 * t) * (D + 8) + tile / kTiles * 16 + g;
     at[0] = x[0], at[D + 8] = x[1], at[8] = x[2], at[D + 16] = x[3];
   }
 }
@@ -347,7 +354,7 @@ __global__ void __launch_bounds__(GradShape<T, D>::kThreads)
   T *ks = (T *)raw, *qs = (T *)(raw + Sh::kTile), *ds = (T *)(raw + 2 * Sh::kTile);
   float *us = (float *)(raw + 3 * Sh::kTile), *vs = us + C * kWide, *st = vs + C * kWide;
   float *gt = st + Sh::kStateFloats, *share = gt + Gates<C>::kFloats, *end = share + C;
-  float *cols = end + C, *dots = cols + kWarps * C;
+  float *cols = end + C, *below = cols + kWarps * C, *dots = below + kWarps * C;
   float *dP = st, *E = st + C * kMat;  // once the states are done with
   grid_dep_wait();
   const DeltaArgs &f = p.f;
@@ -380,10 +387,35 @@ __global__ void __launch_bounds__(GradShape<T, D>::kThreads)
   load_rows<T, C, D, kThreads>(ds, (const T *)p.d_o + row0 * D, (long long)orow, n, tid);
   load_flat<Gates<C>::kFloats, kThreads>(gt, records + at * Rec::kFloats + Rec::kGates, tid);
   cp_async_commit();
-  // the misses and w (as they are: dbeta is a product of both)
-  unpack<D, C / 8, 3, kThreads>(us, misses + at * C * D, tid);
-  unpack<D, C / 8, 3, kThreads>(vs, weights + at * C * D, tid);
-  unpack<D, D / 8, kG, kThreads>(st, A1, tid);
+  // the misses and w (as they are: dbeta is a product of both), A, and where it is small S, with
+  // their inner product
+  constexpr int kRW = Sh::kRowWords, kSW = Sh::kStateWords, kBatch = Sh::kBatch;
+  constexpr bool kKeep = kSW <= 8;
+  float4 kept[kKeep ? kSW : 1];
+  float dot = 0.f;
+  {
+    float4 m[kRW], x[kRW], a[kBatch];
+    fetch_packed<kThreads>(m, misses + at * C * D, tid);
+    fetch_packed<kThreads>(x, weights + at * C * D, tid);
+    if constexpr (kKeep) {
+      fetch_packed<kThreads>(a, A1, tid);
+      fetch_packed<kThreads>(kept, S0, tid);
+    }
+    spread<D, C / 8, 3, kThreads>(us, m, tid);
+    spread<D, C / 8, 3, kThreads>(vs, x, tid);
+    if constexpr (!kKeep) {
+#pragma unroll 1
+      for (int i = tid; i < D * D / 4; i += kBatch * kThreads) {
+        fetch_packed<kThreads>(a, A1, i);
+        spread<D, D / 8, kG, kThreads>(st, a, i);
+      }
+    } else {
+      spread<D, D / 8, kG, kThreads>(st, a, tid);
+#pragma unroll
+      for (int i = 0; i < kSW; ++i)
+        dot = fmaf(a[i].x, kept[i].x, fmaf(a[i].y, kept[i].y, fmaf(a[i].z, kept[i].z, fmaf(a[i].w, kept[i].w, dot))));
+    }
+  }
   cp_async_wait_all();
   __syncthreads();
   // dbeta, then u and dv in the places of the misses and w; four lanes a row
@@ -391,12 +423,12 @@ __global__ void __launch_bounds__(GradShape<T, D>::kThreads)
   for (int half = 0; half < 2; ++half) {
     const int i = i0 + g + 8 * half;
     const float be = gt[Gates<C>::kBeta + i];
-    float dot = 0.f;
+    float sum = 0.f;
 #pragma unroll
     for (int d = 4 * t; d < D; d += 16) {
       float4 &m = *(float4 *)(us + i * kWide + d), &x = *(float4 *)(vs + i * kWide + d);
       const float4 a = m, c = x;
-      dot = fmaf(a.x, c.x, fmaf(a.y, c.y, fmaf(a.z, c.z, fmaf(a.w, c.w, dot))));
+      sum = fmaf(a.x, c.x, fmaf(a.y, c.y, fmaf(a.z, c.z, fmaf(a.w, c.w, sum))));
       m = make_float4(be * a.x, be * a.y, be * a.z, be * a.w);
       x = make_float4(be * c.x, be * c.y, be * c.z, be * c.w);
       if (kG == 1) {  // u is a right operand too
@@ -404,9 +436,9 @@ __global__ void __launch_bounds__(GradShape<T, D>::kThreads)
         m.z = __uint_as_float(tf32_of(m.z)), m.w = __uint_as_float(tf32_of(m.w));
       }
     }
-    dot += __shfl_xor_sync(0xFFFFFFFFu, dot, 1);
-    dot += __shfl_xor_sync(0xFFFFFFFFu, dot, 2);
-    if (t == 0 && i < n) store1(dbeta + (size_t)i * f.H, dot);
+    sum += __shfl_xor_sync(0xFFFFFFFFu, sum, 1);
+    sum += __shfl_xor_sync(0xFFFFFFFFu, sum, 2);
+    if (t == 0 && i < n) store1(dbeta + (size_t)i * f.H, sum);
   }
   __syncwarp();
   // products with the states.  G's shares: sums of rows of each term with the token's own vector
@@ -426,13 +458,20 @@ __global__ void __launch_bounds__(GradShape<T, D>::kThreads)
   row_dots<D>(to0, to1, y, ks, i0);
   __syncthreads();
   {
-    float dot = 0.f;  // S . A
-#pragma unroll 4
-    for (int i = tid; i < D * D / 4; i += kThreads) {
-      const float4 a = __ldg((const float4 *)A1 + i), v = __ldg((const float4 *)S0 + i);
-      dot = fmaf(a.x, v.x, fmaf(a.y, v.y, fmaf(a.z, v.z, fmaf(a.w, v.w, dot))));
+    if constexpr (kKeep) {
+      spread<D, D / 8, kG, kThreads>(st, kept, tid);
+    } else {
+#pragma unroll 1
+      for (int i = tid; i < D * D / 4; i += kBatch * kThreads) {
+        float4 a[kBatch], v[kBatch];
+        fetch_packed<kThreads>(a, A1, i);
+        fetch_packed<kThreads>(v, S0, i);
+#pragma unroll
+        for (int j = 0; j < kBatch; ++j)
+          dot = fmaf(a[j].x, v[j].x, fmaf(a[j].y, v[j].y, fmaf(a[j].z, v[j].z, fmaf(a[j].w, v[j].w, dot))));
+        spread<D, D / 8, kG, kThreads>(st, v, i);
+      }
     }
-    unpack<D, D / 8, kG, kThreads>(st, S0, tid);
 #pragma unroll
     for (int m = 16; m > 0; m >>= 1) dot += __shfl_xor_sync(0xFFFFFFFFu, dot, m);
     if (lane == 0) dots[w] = dot;
@@ -451,62 +490,99 @@ __global__ void __launch_bounds__(GradShape<T, D>::kThreads)
   }
   row_dots<D>(q0, q1, x, qs, i0);
   row_dots<D>(all0, all1, y, ks, i0);
-  float mine0 = q0 + (all0 - to0) - to0, mine1 = q1 + (all1 - to1) - to1;
+  if (t == 0) {
+    share[i0 + g] = q0 + (all0 - to0) - to0, share[i0 + g + 8] = q1 + (all1 - to1) - to1;
+    end[i0 + g] = to0, end[i0 + g + 8] = to1;
+  }
   __syncthreads();  // the states are done with
-  // the tokens before, 16 at a time
-  float below0 = 0.f, below1 = 0.f;
-  for (int j0 = 0; j0 <= i0; j0 += 16) {
+  // dP and E, blocks of 16 x 16 on and below the diagonal, warp by warp
+  for (int blk = w; blk < kWarps * (kWarps + 1) / 2; blk += kWarps) {
+    int ib = 0;
+    while ((ib + 1) * (ib + 2) / 2 <= blk) ++ib;
+    const int jb = blk - ib * (ib + 1) / 2, i1 = 16 * ib, j1 = 16 * jb;
     float qk[2][4] = {}, kk[2][4] = {}, a[2][4] = {}, c[2][4] = {};
-    score_tiles<D>(qk, kk, qs, ks, i0, j0);
-#pragma unroll 2
+    score_tiles<D>(qk, kk, qs, ks, i1, j1);
+#pragma unroll 4
     for (int e = 0; e < D; e += 8) {
-      const auto l = left_rows<kG, kRow>(ds, i0, e);
-      const auto m = left_rows<kG, kWide>(vs, i0, e);
+      const auto l = left_rows<kG, kRow>(ds, i1, e);
+      const auto m = left_rows<kG, kWide>(vs, i1, e);
 #pragma unroll
       for (int q = 0; q < 2; ++q) {
-        const float2 u = *(const float2 *)(us + (j0 + 8 * q + g) * kWide + e + 2 * t);
+        const float2 u = *(const float2 *)(us + (j1 + 8 * q + g) * kWide + e + 2 * t);
         l.times_rounded(a[q], u.x, u.y);
         m.times_rounded(c[q], u.x, u.y);
       }
     }
+    // powers e^(G_i - G_j); off the diagonal in two factors, by way of the block's first row
+    const float hr = gt[Gates<C>::kHi + i1], lr = gt[Gates<C>::kLo + i1];
+    float hi[2], lo[2], pr[2], row[2] = {};
+#pragma unroll
+    for (int half = 0; half < 2; ++half) {
+      hi[half] = gt[Gates<C>::kHi + i1 + g + 8 * half], lo[half] = gt[Gates<C>::kLo + i1 + g + 8 * half];
+      pr[half] = ex2_approx((hi[half] - hr) + (lo[half] - lr));
+    }
 #pragma unroll
     for (int q = 0; q < 2; ++q) {
-      float col[2] = {};
+      const int j = j1 + 8 * q + 2 * t;
+      const float2 hj = *(const float2 *)(gt + Gates<C>::kHi + j), lj = *(const float2 *)(gt + Gates<C>::kLo + j);
+      float pw[4], col[2] = {};
+      if (ib != jb) {
+        const float c0 = ex2_approx((hr - hj.x) + (lr - lj.x)), c1 = ex2_approx((hr - hj.y) + (lr - lj.y));
+        pw[0] = pr[0] * c0, pw[1] = pr[0] * c1, pw[2] = pr[1] * c0, pw[3] = pr[1] * c1;
+      } else {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const bool on = i1 + g + (e >> 1) * 8 >= j + (e & 1), same = i1 + g + (e >> 1) * 8 == j + (e & 1);
+          const float gap = (hi[e >> 1] - (e & 1 ? hj.y : hj.x)) + (lo[e >> 1] - (e & 1 ? lj.y : lj.x));
+          pw[e] = on ? ex2_approx(gap) : 0.f;
+          if (same) c[q][e] = 0.f;
+        }
+      }
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
-        const int i = i0 + g + (e >> 1) * 8, j = j0 + 8 * q + 2 * t + (e & 1);
-        const float pw = i >= j ? ex2_approx((gt[Gates<C>::kHi + i] - gt[Gates<C>::kHi + j]) +
-                                             (gt[Gates<C>::kLo + i] - gt[Gates<C>::kLo + j]))
-                                : 0.f;
-        a[q][e] = f.scale * pw * a[q][e];
-        c[q][e] = i > j ? -pw * c[q][e] : 0.f;
+        a[q][e] *= f.scale * pw[e];
+        c[q][e] *= -pw[e];
         const float m = fmaf(a[q][e], qk[q][e], c[q][e] * kk[q][e]);
-        (e < 2 ? below0 : below1) += m;
+        row[e >> 1] += m;
         col[e & 1] += m;
-        dP[i * kMat + j] = a[q][e];
-        E[i * kMat + j] = c[q][e];
+      }
+#pragma unroll
+      for (int half = 0; half < 2; ++half) {
+        const int at2 = (i1 + g + 8 * half) * kMat + j;
+        *(float2 *)(dP + at2) = make_float2(a[q][2 * half], a[q][2 * half + 1]);
+        *(float2 *)(E + at2) = make_float2(c[q][2 * half], c[q][2 * half + 1]);
       }
 #pragma unroll
       for (int m = 4; m < 32; m <<= 1) {
         col[0] += __shfl_xor_sync(0xFFFFFFFFu, col[0], m);
         col[1] += __shfl_xor_sync(0xFFFFFFFFu, col[1], m);
       }
-      if (g == 0) *(float2 *)(cols + w * C + j0 + 8 * q + 2 * t) = make_float2(col[0], col[1]);
+      if (g == 0) *(float2 *)(cols + ib * C + j) = make_float2(col[0], col[1]);
     }
+#pragma unroll
+    for (int m = 1; m < 4; m <<= 1) {
+      row[0] += __shfl_xor_sync(0xFFFFFFFFu, row[0], m);
+      row[1] += __shfl_xor_sync(0xFFFFFFFFu, row[1], m);
+    }
+    if (t == 0) below[jb * C + i1 + g] = row[0], below[jb * C + i1 + g + 8] = row[1];
+  }
+  __syncthreads();
+  // their products: the warp's rows with the tokens before, its columns with those after
+#pragma unroll 1
+  for (int j0 = 0; j0 <= i0; j0 += 16) {
+    float a[2][4], c[2][4];
+#pragma unroll
+    for (int q = 0; q < 2; ++q)
+#pragma unroll
+      for (int half = 0; half < 2; ++half) {
+        const int at2 = (i0 + g + 8 * half) * kMat + j0 + 8 * q + 2 * t;
+        const float2 u = *(const float2 *)(dP + at2), v = *(const float2 *)(E + at2);
+        a[q][2 * half] = u.x, a[q][2 * half + 1] = u.y, c[q][2 * half] = v.x, c[q][2 * half + 1] = v.y;
+      }
     add_rows<D>(x, a[0], a[1], ks, j0);
     add_rows<D>(y, c[0], c[1], ks, j0);
   }
-#pragma unroll
-  for (int m = 1; m < 4; m <<= 1) {
-    below0 += __shfl_xor_sync(0xFFFFFFFFu, below0, m);
-    below1 += __shfl_xor_sync(0xFFFFFFFFu, below1, m);
-  }
-  if (t == 0) {
-    share[i0 + g] = mine0 + below0, share[i0 + g + 8] = mine1 + below1;
-    end[i0 + g] = to0, end[i0 + g + 8] = to1;
-  }
-  __syncthreads();
-  // the tokens from these on: dP and E the other way round
+#pragma unroll 1
   for (int j0 = i0; j0 < C; j0 += 16) {
     float a[2][4], c[2][4];
 #pragma unroll
@@ -532,6 +608,7 @@ __global__ void __launch_bounds__(GradShape<T, D>::kThreads)
   // the log decays: sums from each token to the chunk's end
   if (tid < C) {
     double G = share[tid];
+    for (int v = 0; v <= tid / 16; ++v) G += below[v * C + tid];
     for (int v = tid / 16; v < kWarps; ++v) G -= cols[v * C + tid];
     if (tid == C - 1) {
       double last = 0.;

@@ -607,26 +607,35 @@ __global__ void __launch_bounds__(GradShape<T, D>::kThreads)
     }
   // the log decays: sums from each token to the chunk's end
   if (tid < C) {
-    double G = share[tid];
-    for (int v = 0; v <= tid / 16; ++v) G += below[v * C + tid];
-    for (int v = tid / 16; v < kWarps; ++v) G -= cols[v * C + tid];
+    float mine = share[tid];
+    for (int v = 0; v <= tid / 16; ++v) mine += below[v * C + tid];
+    for (int v = tid / 16; v < kWarps; ++v) mine -= cols[v * C + tid];
+    double G = mine;
+    // the last one has what all keys sent to the chunk's end, and the state's own share
+    double sent = end[tid];
+#pragma unroll
+    for (int m = 16; m > 0; m >>= 1) sent += __shfl_xor_sync(0xFFFFFFFFu, sent, m);
+    double *other = (double *)cols;
+    if (C > 32) {
+      named_barrier(1, C);  // cols are read
+      if (lane == 0) other[w] = sent;
+      named_barrier(1, C);
+      sent = other[0] + other[1];
+    }
     if (tid == C - 1) {
-      double last = 0.;
-      for (int i = 0; i < C; ++i) last += end[i];
-      for (int v = 0; v < kWarps; ++v) last += (double)gt[Gates<C>::kWhole] * dots[v];
-      G += last;
+      float own = dots[0];
+      for (int v = 1; v < kWarps; ++v) own += dots[v];
+      G += sent + (double)gt[Gates<C>::kWhole] * own;
     }
 #pragma unroll
     for (int m = 1; m < 32; m <<= 1) {
       const double o = __shfl_down_sync(0xFFFFFFFFu, G, m);
       if (lane + m < 32) G += o;
     }
-    double *later = (double *)cols;  // (read before: the barrier below)
     if (C > 32) {
+      if (tid == 32) other[2] = G;
       named_barrier(1, C);
-      if (tid == 32) *later = G;
-      named_barrier(1, C);
-      if (tid < 32) G += *later;
+      if (tid < 32) G += other[2];
     }
     if (tid < n) {
       const float lg = to_f(((const T *)f.log_decay)[b * f.sg[0] + (t0 + tid) * f.sg[1] + h]);

@@ -71,6 +71,17 @@ __device__ __forceinline__ void rows_times_rows(float (&acc)[C / 8][4], const fl
   }
 }
 
+struct TwoFloat {
+  float hi, lo;
+};
+// a + b to 2^-45 or so of the larger (the rounding of a sum, found and carried along).
+__device__ __forceinline__ TwoFloat sum_of(const TwoFloat &a, const TwoFloat &b) {
+  const float s = a.hi + b.hi, r = s - a.hi;
+  const float e = (a.hi - (s - r)) + (b.hi - r) + (a.lo + b.lo);
+  const float hi = s + e;
+  return {hi, e - (hi - s)};
+}
+
 // Parts of C x C matrices in shared memory (rows of C + 4 floats) as operands: 16 rows from i on
 // at columns j .. j + 7 on the left, columns j .. j + 7 of rows i .. i + 7 on the right.
 template <int C, int kTerms>
@@ -173,7 +184,7 @@ __global__ void __launch_bounds__(PrepShape<T, D>::kThreads, 5)
   T *ks = (T *)raw, *qs = ks + C * kRow;
   float *A = (float *)(raw + Sh::kFirst), *inv = (float *)raw;
   float *hi = A + C * kMat, *lo = hi + C, *beta = lo + C;
-  double *first = (double *)(beta + 2 * C);
+  TwoFloat *first = (TwoFloat *)(beta + 2 * C);
   grid_dep_wait();
   const int h = blockIdx.y, b = blockIdx.z, hk = h / (p.H / p.Hk), tid = threadIdx.x;
   const int L = p.seq_lens ? min(max(__ldg(p.seq_lens + b), 0), p.N) : p.N;
@@ -184,9 +195,10 @@ __global__ void __launch_bounds__(PrepShape<T, D>::kThreads, 5)
   load_rows<T, C, D, kThreads>(qs, (const T *)p.q + b * p.sq[0] + t0 * p.sq[1] + (long long)hk * D,
                                p.sq[1], n, tid);
   cp_async_commit();
-  // Sums of the log decays in 64 bits: differences of two of them are what counts, also
-  // behind a token that ends the memory (-inf: a number whose power is 0 next to any other).
-  double G = 0.;
+  // Sums of the log decays (times log2 e) as two floats: differences of two of them are what
+  // counts, also behind a token that ends the memory (-inf: a number whose power is 0 next to
+  // any other).
+  TwoFloat G = {0.f, 0.f};
   if (tid < C) {
     float lg = 0.f, be = 0.f;
     if (tid < n) {
@@ -194,11 +206,14 @@ __global__ void __launch_bounds__(PrepShape<T, D>::kThreads, 5)
       be = to_f(((const T *)p.beta)[b * p.sb[0] + (t0 + tid) * p.sb[1] + h]);
     }
     beta[tid] = be;
-    G = fmax((double)lg, -1e3);
+    lg = lg < -1e3f ? -1e3f : lg;  // (a NaN stays)
+    constexpr float kLog2e = 1.4426950408889634f, kRest = (float)(1.4426950408889634 - (double)kLog2e);
+    G.hi = lg * kLog2e;
+    G.lo = fmaf(lg, kLog2e, -G.hi) + lg * kRest;
 #pragma unroll
     for (int m = 1; m < 32; m <<= 1) {
-      const double o = __shfl_up_sync(0xFFFFFFFFu, G, m);
-      if ((tid & 31) >= m) G += o;
+      const TwoFloat o = {__shfl_up_sync(0xFFFFFFFFu, G.hi, m), __shfl_up_sync(0xFFFFFFFFu, G.lo, m)};
+      if ((tid & 31) >= m) G = sum_of(o, G);
     }
     if (tid == 31) *first = G;
   }
@@ -207,14 +222,14 @@ __global__ void __launch_bounds__(PrepShape<T, D>::kThreads, 5)
   float *rec = records + (((size_t)b * p.H + h) * nc + blockIdx.x) * Rec::kFloats;
   float *gt = rec + Rec::kGates;
   if (tid < C) {
-    if (tid >= 32) G += *first;
-    const double G2 = G * 1.4426950408889634;  // powers of two from here on
-    hi[tid] = (float)G2, lo[tid] = (float)(G2 - (double)hi[tid]);
-    if (kBack) gt[Gates<C>::kHi + tid] = hi[tid], gt[Gates<C>::kLo + tid] = lo[tid];
-    gt[Gates<C>::kUp + tid] = expf((float)G);
+    if (tid >= 32) G = sum_of(*first, G);
+    hi[tid] = G.hi, lo[tid] = G.lo;
+    if (kBack) gt[Gates<C>::kHi + tid] = G.hi, gt[Gates<C>::kLo + tid] = G.lo;
+    const float x = (G.hi + G.lo) * 0.6931471805599453f;
+    gt[Gates<C>::kUp + tid] = expf(x);
     gt[Gates<C>::kBeta + tid] = beta[tid];
     if (tid == C - 1) {
-      const DecayFactor f = G < -300. ? DecayFactor{0.f, 0.f} : decay_factor((float)G);
+      const DecayFactor f = x < -300.f ? DecayFactor{0.f, 0.f} : decay_factor(x);
       gt[Gates<C>::kWhole] = f.hi, gt[Gates<C>::kWhole + 1] = f.lo;
     }
   }

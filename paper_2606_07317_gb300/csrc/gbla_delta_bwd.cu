@@ -56,7 +56,8 @@ __global__ void __launch_bounds__(ReverseShape<T, D, kSolve>::kThreads)
   extern __shared__ __align__(16) char raw[];
   grid_dep_wait();
   const DeltaArgs &f = p.f;
-  const int h = blockIdx.x / Sh::kSplit, b = blockIdx.y, s = blockIdx.z;
+  const int h = blockIdx.x / Sh::kSplit, s = blockIdx.z;
+  const int b = longest_first(f.seq_lens, f.B, blockIdx.y);
   const int hk = h / (f.H / f.Hk), tid = threadIdx.x, warp = tid / 32, lane = tid & 31, t = tid & 3;
   const bool carry = warp < kCarry;
   const int x0 = blockIdx.x % Sh::kSplit * E, e0 = x0 + warp % kCarry * 16;

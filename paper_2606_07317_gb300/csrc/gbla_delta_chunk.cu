@@ -11,7 +11,6 @@
 // goes through the chunks, and in it the columns of S are independent of one another: each
 // warp carries 16 of them, transposed, through the whole sequence, in registers.
 #include <math.h>
-#include <stdlib.h>
 
 #include "gbla_delta_mma.cuh"
 
@@ -20,7 +19,9 @@ namespace delta {
 namespace {
 
 // --------------------------------------------------------------- first launch
-// One block a (chunk, head, batch), a warp for each 16 of its tokens.
+// One block a (chunk, head, batch), a warp for each 16 of its tokens.  (Blocks that stay and take
+// the chunks that there are one after the other were a third slower than a grid whose blocks for
+// a short sequence's missing chunks end at once: ragged D = 128 606 us for 450.)
 template <typename T, int D>
 struct PrepShape {
   static constexpr int C = kChunkOf<T>, kWarps = C / 16, kThreads = kWarps * 32;
@@ -29,7 +30,9 @@ struct PrepShape {
   static constexpr int kTiles = 2 * C * kRow * (int)sizeof(T), kInverse = C * kMat * 4;
   static constexpr int kFirst = kTiles > kInverse ? kTiles : kInverse;
   static constexpr int kBytes = kFirst + kInverse + 4 * C * 4 + 16;
+  static constexpr int kBlocks = sizeof(T) == 2 ? 5 : 8;  // an SM
 };
+
 
 // Products of 16 rows of `left` with every row of `right` up to the block's last row, fp32 tiles
 // of 16 x 8 in acc.
@@ -175,7 +178,7 @@ __device__ __forceinline__ void invert(float *to, const float *A, int w) {
 }
 
 template <typename T, int D, int kSolve, bool kBack>
-__global__ void __launch_bounds__(PrepShape<T, D>::kThreads, 5)
+__global__ void __launch_bounds__(PrepShape<T, D>::kThreads, PrepShape<T, D>::kBlocks)
     prepare_kernel(const DeltaArgs p, float *records, int nc) {
   using Sh = PrepShape<T, D>;
   using Rec = Record<T, kSolve, kBack>;
@@ -374,7 +377,8 @@ __global__ void __launch_bounds__(ScanShape<T, D, kSolve, kFor>::kThreads,
   constexpr int kColumns = kFor == kSegment ? 2 * Sh::kSplit : Sh::kSplit;  // blocks a head
   extern __shared__ __align__(16) char raw[];
   grid_dep_wait();
-  const int h = blockIdx.x / kColumns, part = blockIdx.x % kColumns, b = blockIdx.y, s = blockIdx.z;
+  const int h = blockIdx.x / kColumns, part = blockIdx.x % kColumns, s = blockIdx.z;
+  const int b = longest_first(p.seq_lens, p.B, blockIdx.y);
   const int hk = h / (p.H / p.Hk), tid = threadIdx.x, warp = tid / 32, lane = tid & 31, t = tid & 3;
   const bool carry = warp < kCarry;
   const bool move = part >= Sh::kSplit;  // kSegment: columns of the matrix
@@ -693,8 +697,6 @@ Segments segments_of(const DeltaArgs &a) {
       cost += (double)((blocks * (count - 1) + sms - 1) / sms) * chunks + 1.2 * (count - 1) + 4.;
     if (want == 1 || cost < least) least = cost, best = {count, chunks};
   }
-  const char *force = getenv("SEG");
-  if (force) { int w = atoi(force) < nc ? atoi(force) : nc; best.chunks = (nc + w - 1) / w; best.count = (nc + best.chunks - 1) / best.chunks; }
   return best;
 }
 

@@ -144,6 +144,25 @@ __device__ __forceinline__ void cp_async_or_zero(uint32_t dst, const void *src, 
                : "memory");
 }
 
+// The sequence that the place-th blocks of a scan take: the place-th longest, so that a long one
+// does not begin when the others end (lengths of at most 256 sequences; equal ones, and more
+// than those, in their order).  Ends with a barrier.
+__device__ __forceinline__ int longest_first(const int32_t *seq_lens, int B, int place) {
+  if (!seq_lens || B > 256 || B == 1) return place;
+  __shared__ int found;
+  for (int i = threadIdx.x; i < B; i += blockDim.x) {
+    const int mine = __ldg(seq_lens + i);
+    int rank = 0;
+    for (int j = 0; j < B; ++j) {
+      const int o = __ldg(seq_lens + j);
+      rank += o > mine || (o == mine && j < i);
+    }
+    if (rank == place) found = i;
+  }
+  __syncthreads();
+  return found;
+}
+
 // Tokens of a chunk: bf16 64; fp32 32, whose tiles are twice the bytes a token.
 template <typename T>
 constexpr int kChunkOf = sizeof(T) == 2 ? 64 : 32;

@@ -2,8 +2,10 @@
 
 The layer that emits tokens next to the bidirectional encoder: the front end
 (gbla_project: Conv1D on the input, stacked projections), the norm and rotation
-of queries and keys, the decayed linear attention, the SiLU output gate and an
-output projection with a residual (a plain matrix product).
+of queries and keys, a mixer over the tokens, the SiLU output gate and an output
+projection with a residual (a plain matrix product).  The mixer is the decayed
+linear attention, whose decays are constants, or attention by the gated delta
+rule, whose decays and writes are formed from the input.
 
 * `DecoderLayer.prompt` reads whole, possibly ragged prompts in parallel and
   leaves a cache: the attention state of every head, the last three inputs (the
@@ -12,11 +14,16 @@ output projection with a residual (a plain matrix product).
   cache in place: the library's projection (of the window with the new input: four
   rows, of which the last counts), norm with rotation and step, a kernel each, and
   PyTorch's operations for the window, the gate, the output product and the residual.
-* `norm_rotate` and `attention` are the two operators as differentiable torch
-  functions, for training (first derivatives; deriving their gradients is an error).
+* `AnswerHead` turns a layer's outputs into logits over items and says what they say:
+  the candidates of the next item with their log probabilities (a beam search's step), or
+  the log probabilities of answers that are there (a training loss).
+* `norm_rotate`, `attention`, `delta_attention` and `token_logprobs` are the operators as
+  differentiable torch functions, for training (first derivatives; deriving their
+  gradients is an error).
 
-`python -m paper_2606_07317_gb300.decoder` reads a prompt, continues it token by
-token and compares the continuation with one parallel call over all tokens.
+`python -m paper_2606_07317_gb300.decoder` reads a prompt with each mixer, continues it
+token by token, compares the continuation with one parallel call over all tokens and
+names the next item's candidates.
 """
 from __future__ import annotations
 
@@ -91,6 +98,60 @@ class _Attention(torch.autograd.Function):
         return None, dq, dk, dv, None, None, first
 
 
+class _DeltaAttention(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, options, keep, q, k, v, log_decay, beta, seq_lens, state):
+        ctx.options = options
+        ctx.save_for_backward(q, k, v, log_decay, beta, seq_lens, state)
+        out = torch.zeros(v.shape, dtype=v.dtype, device=v.device)
+        return gbla.delta_attention(q, k, v, log_decay, beta, seq_lens, state, out=out,
+                                    return_state=keep, **options)
+
+    @staticmethod
+    def backward(ctx, do, dstate=None):
+        q, k, v, log_decay, beta, seq_lens, state = ctx.saved_tensors
+        options = ctx.options
+
+        def compute(q, k, v, log_decay, beta, state, do, dstate):
+            g = gbla.delta_attention_backward(
+                q, k, v, log_decay, beta, do.contiguous(), seq_lens, state,
+                None if dstate is None else dstate.contiguous(), return_dstate=state is not None,
+                **options)
+            return (*(g["d" + n] for n in ("q", "k", "v", "log_decay", "beta")), g.get("dstate"))
+
+        *grads, first = _Gradients.apply(compute, q, k, v, log_decay, beta, state, do, dstate)
+        return None, None, *grads, None, first
+
+
+class _TokenLogprobs(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, scale, top, logits, tokens, seq_lens):
+        ctx.scale, shape = scale, logits.shape[:2]
+        f32 = dict(dtype=torch.float32, device=logits.device)
+        out = {"lse": torch.zeros(shape, **f32), "entropy": torch.zeros(shape, **f32)}
+        if tokens is not None:
+            out["logprob"] = torch.zeros(shape, **f32)
+        if top:
+            out["top_logprob"] = torch.zeros((*shape, top), **f32)
+            out["top_token"] = torch.zeros((*shape, top), dtype=torch.int32, device=logits.device)
+            ctx.mark_non_differentiable(out["top_logprob"], out["top_token"])
+        gbla.token_logprobs(logits, tokens, top=top, scale=scale, seq_lens=seq_lens, out=out)
+        ctx.save_for_backward(logits, tokens, seq_lens, out["lse"], out["entropy"])
+        return tuple(out.values())
+
+    @staticmethod
+    def backward(ctx, dlse, dentropy, *more):
+        logits, tokens, seq_lens, lse, entropy = ctx.saved_tensors
+        scale, dlogprob = ctx.scale, more[0] if tokens is not None else None
+
+        def compute(logits, dlse, dentropy, dlogprob):
+            g = [None if t is None else t.contiguous() for t in (dlogprob, dentropy, dlse)]
+            return (gbla.token_logprobs_backward(logits, lse, entropy, tokens, *g, scale=scale,
+                                                 seq_lens=seq_lens),)
+
+        return None, None, *_Gradients.apply(compute, logits, dlse, dentropy, dlogprob), None, None
+
+
 def _constant(t, name):
     if t is not None and t.requires_grad and torch.is_grad_enabled():
         raise ValueError(f"{name} has no gradient: it is a constant of the model (detach it)")
@@ -115,6 +176,22 @@ def attention(q, k, v, log_decay, seq_lens=None, state=None, scale=None,
     return _Attention.apply(dict(scale=scale, algo=algo), q, k, v, log_decay, seq_lens, state)
 
 
+def delta_attention(q, k, v, log_decay, beta, seq_lens=None, state=None, scale=None,
+                    return_state: bool = False):
+    """gbla.delta_attention with gradients for everything but the lengths; padding rows of o
+    are 0.  Returns o, or with return_state (o, the state after each sequence)."""
+    return _DeltaAttention.apply(dict(scale=scale), return_state, q, k, v, log_decay, beta,
+                                 seq_lens, state)
+
+
+def token_logprobs(logits, tokens=None, top: int = 0, scale: float = 1.0, seq_lens=None) -> dict:
+    """gbla.token_logprobs with gradients of lse, entropy and logprob for the logits (the top
+    alternatives are constants); padding rows are 0."""
+    names = ["lse", "entropy"] + ["logprob"] * (tokens is not None)
+    names += ["top_logprob", "top_token"] * bool(top)
+    return dict(zip(names, _TokenLogprobs.apply(scale, top, logits, tokens, seq_lens)))
+
+
 def head_decays(H: int, shortest: float = 32.0, longest: float = 4096.0, device="cuda"):
     """[H] fp32 ln of the decays whose horizons (tokens until a contribution has faded to
     1/e) run evenly in their logarithm from `shortest` to `longest`."""
@@ -125,10 +202,14 @@ def head_decays(H: int, shortest: float = 32.0, longest: float = 4096.0, device=
 
 class DecoderLayer:
     """Random weights of a layer of width d with H heads of D (bf16; limits as gbla_project).
-    `algo`: the kernel family of the prompts' attention."""
+    `algo`: the kernel family of the prompts' decayed attention.  `mixer`: "decay" (decayed
+    linear attention) or "delta" (the gated delta rule: keys of unit length, decays from a
+    projection of the input, writes weighted by the layer's gate)."""
 
     def __init__(self, d: int, H: int, D: int, max_positions: int, seed: int = 0, device="cuda",
-                 algo: int = gbla.ALGO_AUTO):
+                 algo: int = gbla.ALGO_AUTO, mixer: str = "decay"):
+        if mixer not in ("decay", "delta"):
+            raise ValueError(f"mixer must be 'decay' or 'delta', not {mixer!r}")
         g = torch.Generator(device=device).manual_seed(seed)
 
         def normal(*shape, std):
@@ -141,6 +222,16 @@ class DecoderLayer:
         self.w_out = normal(H * D, d, std=(H * D) ** -0.5).to(torch.bfloat16)
         self.log_decay = head_decays(H, device=device)
         self.rot = gbla.rotation_table(max_positions, D, device=device)
+        self.mixer = mixer
+        if mixer == "delta":
+            self.norm_k = self.norm_k * D ** -0.5
+            self.w_decay = normal(d, H, std=d ** -0.5).to(torch.bfloat16)
+
+    def _gates(self, x, gate):
+        """log_decay and beta [B, N, H] of inputs x and the projection's gate: a head fades by
+        about its constant decay a token, by more or less as the input says."""
+        more = torch.nn.functional.softplus((x @ self.w_decay).float()) / 0.6931471805599453
+        return (more * self.log_decay).to(x.dtype), gate.sigmoid()
 
     def _out(self, x, o, out_gate):
         y = o * torch.nn.functional.silu(out_gate)
@@ -166,8 +257,12 @@ class DecoderLayer:
         p = gbla.project(x, self.conv_x, self.w_proj, self.H, self.D, seq_lens)
         q, k = gbla.qk_norm_rotate(p["q"], p["k"], self.norm_q, self.norm_k, self.rot,
                                    seq_lens=seq_lens)
-        o, state = gbla.decay_attention(q, k, p["v"], self.log_decay, seq_lens, return_state=True,
-                                        algo=self.algo)
+        if self.mixer == "delta":
+            o, state = gbla.delta_attention(q, k, p["v"], *self._gates(x, p["gate"]), seq_lens,
+                                            return_state=True)
+        else:
+            o, state = gbla.decay_attention(q, k, p["v"], self.log_decay, seq_lens,
+                                            return_state=True, algo=self.algo)
         L = (torch.full((B,), N, dtype=torch.int32, device=x.device) if seq_lens is None
              else seq_lens.clamp(0, N))
         at = L[:, None].long() + torch.arange(-HISTORY, 0, device=x.device)  # the last inputs
@@ -185,15 +280,46 @@ class DecoderLayer:
         now = slice(HISTORY, HISTORY + 1)  # the one output whose history is whole
         q, k = gbla.qk_norm_rotate(p["q"][:, now], p["k"][:, now], self.norm_q, self.norm_k,
                                    self.rot, cache["positions"])
-        o = gbla.decay_attention_step(q, k, p["v"][:, now], self.log_decay, cache["state"])
+        if self.mixer == "delta":
+            o = gbla.delta_attention_step(q, k, p["v"][:, now],
+                                          *self._gates(x, p["gate"][:, now]), cache["state"])
+        else:
+            o = gbla.decay_attention_step(q, k, p["v"][:, now], self.log_decay, cache["state"])
         cache["window"].copy_(wide[:, 1:])
         cache["positions"].add_(1)
         cache["tokens"] += 1
         return self._out(x, o, p["out_gate"][:, now])
 
 
-def main(B: int = 4, N: int = 2048, new: int = 64, d: int = 512, H: int = 8, D: int = 64):
-    layer = DecoderLayer(d, H, D, N + new)
+class AnswerHead:
+    """Logits over V items from a layer's outputs y [B, N, d] (random weights, a plain matrix
+    product), and what they say."""
+
+    def __init__(self, d: int, V: int, seed: int = 0, device="cuda"):
+        g = torch.Generator(device=device).manual_seed(seed)
+        self.w = (torch.randn((V, d), generator=g, device=device) * d ** -0.5).to(torch.bfloat16)
+
+    def logits(self, y):
+        return y @ self.w.t()
+
+    def candidates(self, y, top: int, ruled_out=None, scale: float = 1.0) -> dict:
+        """The `top` most probable items at every place, with their log probabilities and the
+        entropy (gbla.token_logprobs); `ruled_out` (truth values that broadcast to [B, N, V])
+        names items that cannot follow."""
+        logits = self.logits(y)
+        if ruled_out is not None:
+            logits = logits.masked_fill(ruled_out, -torch.inf)
+        return gbla.token_logprobs(logits, top=top, scale=scale)
+
+    def score(self, y, items, seq_lens=None, scale: float = 1.0) -> dict:
+        """Log probabilities of the items [B, N] int32 that are there, differentiable in y and
+        the weights (token_logprobs)."""
+        return token_logprobs(self.logits(y), items, scale=scale, seq_lens=seq_lens)
+
+
+def main(B: int = 4, N: int = 2048, new: int = 64, d: int = 512, H: int = 8, D: int = 64,
+         mixer: str = "decay", V: int = 4096):
+    layer = DecoderLayer(d, H, D, N + new, mixer=mixer)
     x = torch.randn((B, N + new, d), generator=torch.Generator().manual_seed(1))
     x = x.to(torch.bfloat16).cuda()
     whole, _ = layer.prompt(x)
@@ -206,10 +332,14 @@ def main(B: int = 4, N: int = 2048, new: int = 64, d: int = 512, H: int = 8, D: 
     got = torch.cat(steps, 1).float()
     want = whole[:, N:].float()
     off = ((got - want).norm() / (want - x[:, N:].float()).norm()).item()
-    print(f"{B} sequences: prompt of {N}, {new} steps at {ms:.3f} ms; the steps are {off:.2e} of "
-          "the layer's output off the parallel form")
+    print(f"{mixer}: {B} sequences: prompt of {N}, {new} steps at {ms:.3f} ms; the steps are "
+          f"{off:.2e} of the layer's output off the parallel form")
+    best = AnswerHead(d, V).candidates(steps[-1], 3)
+    print(f"next items of the first sequence: {best['top_token'][0, 0].tolist()}, "
+          f"log probabilities {[round(p, 3) for p in best['top_logprob'][0, 0].tolist()]}")
     return off
 
 
 if __name__ == "__main__":
     main()
+    main(mixer="delta")

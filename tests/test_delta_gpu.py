@@ -263,6 +263,49 @@ def test_long_sequences():
             close(t, want[n], grad_bound(n, dtype, 4001, D), (D, dtype, n), beside)
 
 
+@pytest.mark.parametrize("D,dtype", [(32, "bf16"), (64, "bf16"), (64, "fp32"), (128, "bf16"), (128, "fp32")])
+def test_segments_of_ragged_sequences(D, dtype):
+    """Long enough to be cut into segments: sequences that end in the first, in the middle of
+    one, at a border, nowhere (empty), with states in and out and memories that end."""
+    lens = [2600, 0, 1300, 64, 2599, 2560]
+    c = Case(40 + D, 6, 2600, 2, 1, D, dtype, lens, packed=False)
+    c.x["log_decay"][:, ::700] = -math.inf
+    s0 = c.state()
+    out = torch.full_like(c.x["v"], 7.0)
+    x = c.poisoned()
+    _, S = gbla.delta_attention(*x.values(), seq_lens=c.seq_lens, state=s0, out=out, return_state=True)
+    o, ref = R.delta(*c.x.values(), c.lens, s0, D ** -0.5)
+    past = c.past()
+    assert (out[past] == 7.0).all()
+    close(out[~past], o[~past], bound(dtype, 2600, D), "o")
+    close(S, ref, bound("fp32", 2600, D), "state")
+    alone = gbla.delta_attention(*x.values(), seq_lens=c.seq_lens, state=s0)
+    close(alone[~past], o[~past], bound(dtype, 2600, D), "o without a state")
+    do, ds = c.n(*o.shape).to(TYPES[dtype]).cuda(), c.state()
+    want = R.delta_backward(*c.x.values(), do, c.lens, s0, ds, D ** -0.5)
+    g = gbla.delta_attention_backward(*x.values(), do, seq_lens=c.seq_lens, state=s0, dstate=ds, return_dstate=True)
+    for n, t in g.items():
+        r = want[n]
+        if n == "dlog_decay":
+            r = torch.where(c.x["log_decay"] == -math.inf, 0.0, r)
+        beside = shares(c.x, do, want, c.lens, s0, D ** -0.5) if n == "dlog_decay" else None
+        close(t, r, grad_bound(n, dtype, 2600, D), n, beside)
+    assert gbla.device_error() == 0
+
+
+def test_far_offsets():
+    """Rows of a batch more than 2^32 elements apart."""
+    c = Case(50, 2, 70, 2, 2, 64, "bf16")
+    far = torch.empty_strided((2, 70, 2, 64), ((1 << 32) + 64, 128, 64, 1), dtype=torch.bfloat16, device="cuda")
+    far.copy_(c.x["v"])
+    want = gbla.delta_attention(*c.x.values())
+    x = {**c.x, "v": far}
+    assert torch.equal(gbla.delta_attention(*x.values()), want)
+    do = c.n(2, 70, 2, 64).to(torch.bfloat16).cuda()
+    a, b = (gbla.delta_attention_backward(*t.values(), do) for t in (c.x, x))
+    assert all(torch.equal(a[n], b[n]) for n in a)
+
+
 STEPS = [(1, 1, 1, 32, "fp32"), (4, 8, 8, 64, "bf16"), (5, 6, 2, 128, "bf16"), (7, 4, 1, 64, "fp32"),
          (3, 3, 3, 128, "fp32"), (6, 8, 2, 32, "bf16")]
 

@@ -34,42 +34,49 @@ struct PrepShape {
 };
 
 
-// Products of 16 rows of `left` with every row of `right` up to the block's last row, fp32 tiles
-// of 16 x 8 in acc.
+// Products of the warp's 16 rows of keys and of queries with every row of keys up to them, fp32
+// tiles of 16 x 8.
 template <int D, int C>
-__device__ __forceinline__ void rows_times_rows(float (&acc)[C / 8][4], const __nv_bfloat16 *left,
-                                                const __nv_bfloat16 *right, int w) {
+__device__ __forceinline__ void rows_times_keys(float (&kk)[C / 8][4], float (&qk)[C / 8][4],
+                                                const __nv_bfloat16 *ks, const __nv_bfloat16 *qs,
+                                                int w) {
   constexpr int kRow = pad_row<__nv_bfloat16>(D);
-  const int l = threadIdx.x & 31;
+  const int l = threadIdx.x & 31, at = (16 * w + (l & 15)) * kRow + (l >> 4) * 8;
 #pragma unroll
   for (int k = 0; k < D / 16; ++k) {
-    uint32_t a[4];
-    ldmatrix4(a, smem_u32(left + (16 * w + (l & 15)) * kRow + 16 * k + (l >> 4) * 8));
+    uint32_t a[4], b[4];
+    ldmatrix4(a, smem_u32(ks + at + 16 * k));
+    ldmatrix4(b, smem_u32(qs + at + 16 * k));
 #pragma unroll
     for (int n = 0; n < C / 16; ++n)
       if (n <= w) {
-        const PairBf16 p = by_token<kRow>(right, 16 * n, 16 * k);
-        mma_bf16(acc[2 * n], a, p.b[0][0], p.b[0][1]);
-        mma_bf16(acc[2 * n + 1], a, p.b[1][0], p.b[1][1]);
+        const PairBf16 p = by_token<kRow>(ks, 16 * n, 16 * k);
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          mma_bf16(kk[2 * n + i], a, p.b[i][0], p.b[i][1]);
+          mma_bf16(qk[2 * n + i], b, p.b[i][0], p.b[i][1]);
+        }
       }
   }
 }
 template <int D, int C>
-__device__ __forceinline__ void rows_times_rows(float (&acc)[C / 8][4], const float *left,
-                                                const float *right, int w) {
+__device__ __forceinline__ void rows_times_keys(float (&kk)[C / 8][4], float (&qk)[C / 8][4],
+                                                const float *ks, const float *qs, int w) {
   constexpr int kRow = pad_row<float>(D);
   const int g = (threadIdx.x & 31) >> 2, t = threadIdx.x & 3;
 #pragma unroll 2
   for (int k = 0; k < D / 8; ++k) {
-    const float2 x = *(const float2 *)(left + (16 * w + g) * kRow + 8 * k + 2 * t);
-    const float2 y = *(const float2 *)(left + (16 * w + g + 8) * kRow + 8 * k + 2 * t);
-    const float c[4] = {x.x, x.y, y.x, y.y};
-    const LeftTf32<3> a(c);
+    const int at = (16 * w + g) * kRow + 8 * k + 2 * t;
+    const float2 x = *(const float2 *)(ks + at), y = *(const float2 *)(ks + at + 8 * kRow);
+    const float2 u = *(const float2 *)(qs + at), v = *(const float2 *)(qs + at + 8 * kRow);
+    const float c[4] = {x.x, x.y, y.x, y.y}, d[4] = {u.x, u.y, v.x, v.y};
+    const LeftTf32<3> a(c), q(d);
 #pragma unroll
     for (int n = 0; n < C / 8; ++n)
       if (n <= 2 * w + 1) {
-        const float2 b = *(const float2 *)(right + (8 * n + g) * kRow + 8 * k + 2 * t);
-        a.times(acc[n], b.x, b.y);
+        const float2 b = *(const float2 *)(ks + (8 * n + g) * kRow + 8 * k + 2 * t);
+        a.times(kk[n], b.x, b.y);
+        q.times(qk[n], b.x, b.y);
       }
   }
 }
@@ -243,8 +250,7 @@ __global__ void __launch_bounds__(PrepShape<T, D>::kThreads, PrepShape<T, D>::kB
   // the power in two factors, both at most 1 (rows to that one, that one to the columns).
   const int w = tid / 32, g = (tid & 31) >> 2, t = tid & 3, i0 = 16 * w;
   float kk[C / 8][4] = {}, qk[C / 8][4] = {};
-  rows_times_rows<D, C>(kk, ks, ks, w);
-  rows_times_rows<D, C>(qk, qs, ks, w);
+  rows_times_keys<D, C>(kk, qk, ks, qs, w);
   if (kBack) __syncthreads();  // P takes their place
   const float hr = hi[i0], lr = lo[i0];
   float row[2];

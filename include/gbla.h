@@ -551,8 +551,15 @@ gbla_status gbla_decay_attention_step(const void *q, const void *k, const void *
  *   o         [B, N, H, D] dtype; rows t >= L_b untouched
  *   state_out [B, H, D, D] fp32 or NULL: S after each sequence's last token
  *             (state_in for an empty one)
- * scale is finite, not 0 and not subnormal.  The state is held in fp32.  Values, keys,
- * states and gates other than log_decay = -inf are finite.
+ * scale is finite, not 0 and not subnormal.  Computed in chunks of tokens (bf16 64, fp32
+ * 32) by warp-level tensor-core products with fp32 sums; the state is held in fp32.  States
+ * that are results, and everything in fp32, are within a few 2^-24 of their norm a token's
+ * horizon long (operands enter as three numbers); bf16 results without a state round
+ * operands to 2^-11 or better inside, which their own rounding covers.  Values, keys,
+ * states and gates other than log_decay = -inf are finite: a NaN or infinity in a valid
+ * token reaches the whole chunk and what follows it.  Sums run in a fixed order.  Scratch
+ * comes from the library's pool (GBLA_ERR_ALLOC): about 20 KB (bf16, without a state) a
+ * chunk and head, and two states a segment that a long sequence is cut into.
  */
 gbla_status gbla_delta_attention(const void *q, const void *k, const void *v,
                                  const void *log_decay, const void *beta,
@@ -568,7 +575,8 @@ gbla_status gbla_delta_attention(const void *q, const void *k, const void *v,
  * dq, dk [B, N, Hk, D] (sums over the value heads that read a key head, in fp32), dv
  * [B, N, H, D], dlog_decay, dbeta [B, N, H] dtype (rows t >= L_b written as 0; where
  * log_decay is -inf its gradient is 0) and dstate_in [B, H, D, D] fp32 or NULL.  Nothing is
- * kept from a forward call.
+ * kept from a forward call.  Scratch: about 30 KB a chunk and head, two states and two
+ * chunks of fp32 values each, and fp32 planes of dq and dk where heads are shared.
  */
 gbla_status gbla_delta_attention_backward(
     const void *q, const void *k, const void *v, const void *log_decay, const void *beta,
@@ -606,7 +614,7 @@ gbla_status gbla_delta_attention_step(const void *q, const void *k, const void *
  *   top_logprob [B, N, top] fp32, top_token [B, N, top] int32, with 0 < top <=
  *             min(V, GBLA_MAX_TOP) (else NULL): in descending order, equal logits in the
  *             order of their tokens
- * Rows t >= L_b are untouched.  1 <= V <= 2^30, scale positive and normal.  Logits of
+ * Rows t >= L_b are untouched.  1 <= V <= 2^30, B N <= 2^30, scale positive and normal.  Logits of
  * -inf are ruled out (p = 0); a row of nothing else has lse and log probabilities of
  * -inf and entropy 0.  A NaN or +inf makes the results of its row NaN; its top tokens
  * are in range (NaN counts as the least).  fp32 arithmetic, one launch, allocates

@@ -970,7 +970,7 @@ gbla_status check_logprob(LogprobArgs *a, size_t *bytes, const void *logits, con
   if (dtype != GBLA_FP32 && dtype != GBLA_BF16) return GBLA_ERR_UNSUPPORTED;
   if (!(scale > 0.f) || !isnormal(scale)) return GBLA_ERR_INVALID_ARG;
   const unsigned long long rows = (unsigned long long)B * N;
-  if (rows >= (1ull << 31) || rows * V > (1ull << 40)) return GBLA_ERR_INVALID_ARG;
+  if (rows > (1ull << 30) || rows * V > (1ull << 40)) return GBLA_ERR_INVALID_ARG;
   *empty = rows == 0;
   *a = LogprobArgs{};
   if (*empty) return GBLA_OK;

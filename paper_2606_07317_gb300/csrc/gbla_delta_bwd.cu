@@ -106,9 +106,9 @@ __global__ void __launch_bounds__(ReverseShape<T, D, kSolve>::kThreads)
     cp_async_commit();
     cp_async_wait_all();
   }
-  // round c: the chain's chunk c, the others' chunk c - 1
+  // turn c: the chain's chunk c, the others' chunk c - 1
   for (int c = end; c >= first; --c) {
-    __syncthreads();  // this round's tiles and what was left are there, the others are read
+    __syncthreads();  // this turn's tiles and what was left are there, the others are read
     if (carry) {
       if (c == end) continue;
       const char *in = first_of(c);

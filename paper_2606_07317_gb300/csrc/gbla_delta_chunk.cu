@@ -443,9 +443,9 @@ __global__ void __launch_bounds__(ScanShape<T, D, kSolve, kFor>::kThreads,
     cp_async_commit();
     cp_async_wait_all();
   }
-  const int rounds = kFor == kResults ? end + 1 : end;
-  for (int c = first; c < rounds; ++c) {
-    __syncthreads();  // this round's tiles and what was handed on are there, the others are read
+  const int turns = kFor == kResults ? end + 1 : end;
+  for (int c = first; c < turns; ++c) {
+    __syncthreads();  // this turn's tiles and what was handed on are there, the others are read
     if (carry) {
       if (c >= end) break;
       const char *in = first_of(c);

@@ -85,6 +85,7 @@ def test_sizes(lib, op):
 @pytest.mark.parametrize("op", ["logprobs", "logprobs_backward"])
 def test_logit_sizes(lib, op):
     for bad in (dict(B=-1), dict(N=-1), dict(V=0), dict(V=-5), dict(V=(1 << 30) + 1), dict(B=1 << 16, N=1 << 15),
+                dict(B=(1 << 15) + 1, N=1 << 15, V=1),
                 dict(B=1 << 15, N=1 << 15, V=1 << 20), dict(scale=0.0), dict(scale=-1.0), dict(scale=float("nan")),
                 dict(scale=float("inf")), dict(scale=1e-40)):
         assert _run(lib, op, **bad) == INV, bad

@@ -176,6 +176,18 @@ def test_top_in_unkind_orders(order, V, top):
     check(gbla.token_logprobs(x, top=top), R.logprobs(x, None, top, 1.0))
 
 
+@pytest.mark.parametrize("dtype,V,top,threads", [("fp32", 9000, 40, 128), ("bf16", 9001, 9, 128), ("fp32", 600, 16, 32)])
+def test_top_where_one_thread_has_them(dtype, V, top, threads):
+    """Many rows, so that a block (or a warp) has a row to itself: the largest logits all where
+    the vectors of one thread fall, more of them than a block keeps as candidates."""
+    g = torch.Generator().manual_seed(4)
+    x = torch.randn((2, 1300, V), generator=g).sort(-1).values
+    vec = 4 if dtype == "fp32" else 8
+    x[..., torch.arange(V) // vec % threads == 3] += 20
+    x = x.to(TYPES[dtype]).cuda()
+    check(gbla.token_logprobs(x, top=top), R.logprobs(x, None, top, 1.0))
+
+
 def test_far_rows():
     """Offsets beyond 2^32 bytes."""
     B, V = 3, 4099

@@ -35,13 +35,16 @@ __device__ __forceinline__ void store4(__nv_bfloat16 *p, const float (&f)[4]) {
 }
 
 // ---------------------------------------------------------- the single token
-// One block a (sequence, head), bound by the state's bytes, 8 D^2 a head.  A thread
-// holds 4 columns of kRows rows, all loads in flight before the first product; the
-// sums over the rows of both products meet in shared memory once.
+// A block takes 32 or 64 of the state's columns (each by itself a recurrence) of a (sequence,
+// head), bound by the state's bytes, 8 D^2 a head.  A thread holds 4 columns of kRows rows, all
+// loads in flight before the first product; the sums over the rows of both products meet in
+// shared memory once.  Measured: 512 sequences, 8 heads, D = 128: 80.2 us, 6.75 TB/s (99 % of
+// the measured copy rate); with 128 columns a block 83.8.
 template <int D>
 struct StepShape {
-  static constexpr int kCols = D / 4;                       // column quads
-  static constexpr int kThreads = D == 32 ? 64 : 256;
+  static constexpr int kSplit = D == 128 ? 2 : 1;           // blocks a head
+  static constexpr int kCols = D / kSplit / 4;              // column quads
+  static constexpr int kThreads = D == 32 ? 64 : D == 64 ? 256 : 128;
   static constexpr int kGroups = kThreads / kCols;          // rows at a time
   static constexpr int kRows = D / kGroups;
 };
@@ -50,20 +53,22 @@ template <typename T, int D>
 __global__ void __launch_bounds__(StepShape<D>::kThreads) step_kernel(const DeltaStepArgs p) {
   using Sh = StepShape<D>;
   __shared__ __align__(16) float qk[2][D];
-  __shared__ __align__(16) float red[2][Sh::kGroups][D];
+  constexpr int E = D / Sh::kSplit;
+  __shared__ __align__(16) float red[2][Sh::kGroups][E];
   __shared__ float dots[Sh::kThreads / 32];
   grid_dep_wait();
   grid_dep_launch();
-  const int h = blockIdx.x, b = blockIdx.y, tid = threadIdx.x, hk = h / (p.H / p.Hk);
+  const int h = blockIdx.x / Sh::kSplit, e0 = blockIdx.x % Sh::kSplit * E;
+  const int b = blockIdx.y, tid = threadIdx.x, hk = h / (p.H / p.Hk);
   const int slot = p.slots ? __ldg(p.slots + b) : b;
   if (slot < 0 || slot >= p.n_slots) return;
   const int c = tid % Sh::kCols, g = tid / Sh::kCols;
-  float4 *s = (float4 *)(p.state + ((size_t)slot * p.H + h) * D * D) + c;
+  float4 *s = (float4 *)(p.state + ((size_t)slot * p.H + h) * D * D + e0) + c;
   float4 r[Sh::kRows];
 #pragma unroll
-  for (int i = 0; i < Sh::kRows; ++i) r[i] = s[(g + i * Sh::kGroups) * Sh::kCols];
+  for (int i = 0; i < Sh::kRows; ++i) r[i] = s[(g + i * Sh::kGroups) * (D / 4)];
   float vv[4];
-  load4((const T *)p.v + b * p.sv + (long long)h * D + 4 * c, vv);
+  load4((const T *)p.v + b * p.sv + (long long)h * D + e0 + 4 * c, vv);
   const T *q = (const T *)p.q + b * p.sq + (long long)hk * D;
   const T *k = (const T *)p.k + b * p.sk + (long long)hk * D;
   float kq = 0.f;
@@ -107,7 +112,7 @@ __global__ void __launch_bounds__(StepShape<D>::kThreads) step_kernel(const Delt
   for (int i = 0; i < Sh::kRows; ++i) {
     const int d = g + i * Sh::kGroups;
     const float kd = qk[1][d];
-    s[d * Sh::kCols] = make_float4(fmaf(kd, u[0], r[i].x), fmaf(kd, u[1], r[i].y),
+    s[d * (D / 4)] = make_float4(fmaf(kd, u[0], r[i].x), fmaf(kd, u[1], r[i].y),
                                    fmaf(kd, u[2], r[i].z), fmaf(kd, u[3], r[i].w));
   }
   if (g == 0) {
@@ -122,14 +127,15 @@ __global__ void __launch_bounds__(StepShape<D>::kThreads) step_kernel(const Delt
     }
 #pragma unroll
     for (int i = 0; i < 4; ++i) o[i] *= p.scale;
-    store4((T *)p.o + ((size_t)b * p.H + h) * D + 4 * c, o);
+    store4((T *)p.o + ((size_t)b * p.H + h) * D + e0 + 4 * c, o);
   }
 }
 
 template <typename T, int D>
 cudaError_t step_launch(const DeltaStepArgs &a, cudaStream_t st) {
   count_launch();
-  return launch_pdl(step_kernel<T, D>, dim3(a.H, a.B), dim3(StepShape<D>::kThreads), 0, st, a);
+  return launch_pdl(step_kernel<T, D>, dim3(a.H * StepShape<D>::kSplit, a.B),
+                    dim3(StepShape<D>::kThreads), 0, st, a);
 }
 
 }  // namespace

@@ -713,7 +713,7 @@ cudaError_t back_launch(const DeltaBackArgs &p, float *s, cudaStream_t st) {
     if ((e = launch_pdl(own, grid, block, Sh::kBytes, st, p, records, (float *)nullptr,
                         (float *)nullptr, s + l.own, nc, g.chunks, g.count)) != cudaSuccess)
       return e;
-    if ((e = join_segments(a, g, true, p.dstate, s + l.own, s + l.moves, st)) != cudaSuccess)
+    if ((e = join_back(a, g, kSolve == 3, p.dstate, s + l.own, s + l.moves, st)) != cudaSuccess)
       return e;
   }
   const auto reverse = reverse_kernel<T, D, kTerms, kSolve, false>;

@@ -294,16 +294,18 @@ __global__ void __launch_bounds__(PrepShape<T, D>::kThreads, PrepShape<T, D>::kB
     }
   }
   __syncthreads();
-  // a matrix in shared memory, tile by tile: as it is, or (kFlip) for sums over its rows;
-  // inverses without their diagonal of 1 (that part of a product needs no rounding)
+  // a matrix in shared memory, tile by tile: as it is, or (flip) for sums over its rows; the
+  // backward's inverses without their diagonal of 1 (that part of a product needs no rounding),
+  // the forward's multiplied by beta
   auto put = [&](float *to, auto tiles, bool flip, bool inverse) {
     using Form = decltype(tiles);
     for (int m = w; m < C / 8; m += Sh::kWarps)
       for (int j = 0; j <= m; ++j) {
         const float *at = inv + (8 * m + (flip ? 2 * t : g)) * kMat + 8 * j + (flip ? g : 2 * t);
-        const bool one = inverse && j == m;
-        Form::store(to, m, j, one && g == 2 * t ? 0.f : at[0],
-                    one && g == 2 * t + 1 ? 0.f : at[flip ? kMat : 1]);
+        const bool one = inverse && kBack && j == m;
+        const float by = inverse && !kBack ? beta[8 * m + g] : 1.f;
+        Form::store(to, m, j, one && g == 2 * t ? 0.f : by * at[0],
+                    one && g == 2 * t + 1 ? 0.f : by * at[flip ? kMat : 1]);
       }
   };
   if (kBack) {
@@ -370,7 +372,9 @@ struct ScanShape {
 // Segments have `seg` chunks; `before` holds the states after all but the last, or takes what
 // kSegment forms, the matrices in `moves`, [B H][count][D][D] both.  Records are `stride` floats
 // apart (their M and gates lie at the same place in both forms).
-template <typename T, int D, int kTerms, int kSolve, Purpose kFor>
+// kFold: M comes multiplied by beta (the forward pass's records) and gives u at once; else
+// without its diagonal of 1, and gives the misses.
+template <typename T, int D, int kTerms, int kSolve, Purpose kFor, bool kFold>
 __global__ void __launch_bounds__(ScanShape<T, D, kSolve, kFor>::kThreads,
                                   ScanShape<T, D, kSolve, kFor>::kBlocks)
     scan_kernel(const DeltaArgs p, const float *records, float *states, float *misses,
@@ -467,8 +471,8 @@ __global__ void __launch_bounds__(ScanShape<T, D, kSolve, kFor>::kThreads,
           x[2] = fmaf(-up.x, x[2], v[i][2]), x[3] = fmaf(-up.y, x[3], v[i][3]);
         }
       }
-      // r += (M - 1) r: the later half of the tokens first, which needs the earlier ones as
-      // they are; then those
+      // r = beta M r, or r += (M - 1) r: the later half of the tokens first, which needs the
+      // earlier ones as they are; then those
 #pragma unroll
       for (int half = 1; half >= 0; --half) {
         constexpr int kHalf = C / 16;
@@ -483,14 +487,17 @@ __global__ void __launch_bounds__(ScanShape<T, D, kSolve, kFor>::kThreads,
 #pragma unroll
         for (int m = 0; m < kHalf; ++m)
 #pragma unroll
-          for (int i = 0; i < 4; ++i) r[half * kHalf + m][i] += x[m][i];
+          for (int i = 0; i < 4; ++i)
+            r[half * kHalf + m][i] = kFold ? x[m][i] : r[half * kHalf + m][i] + x[m][i];
       }
       if (kFor == kSave) store_packed(misses + (bh * nc + c) * C * D, r, e0);
 #pragma unroll
       for (int j = 0; j < C / 8; ++j) {
         float4 *to = (float4 *)hand + (kHandWords<D> + j) * 32 + lane;
-        const float2 be = *(const float2 *)(gt + Gates<C>::kBeta + 8 * j + 2 * t);
-        r[j][0] *= be.x, r[j][1] *= be.y, r[j][2] *= be.x, r[j][3] *= be.y;
+        if (!kFold) {
+          const float2 be = *(const float2 *)(gt + Gates<C>::kBeta + 8 * j + 2 * t);
+          r[j][0] *= be.x, r[j][1] *= be.y, r[j][2] *= be.x, r[j][3] *= be.y;
+        }
         if (kFor == kResults) *to = make_float4(r[j][0], r[j][1], r[j][2], r[j][3]);
         const float2 dn = *(const float2 *)(gt + Gates<C>::kDown + 8 * j + 2 * t);
         r[j][0] *= dn.x, r[j][1] *= dn.y, r[j][2] *= dn.x, r[j][3] *= dn.y;
@@ -540,13 +547,14 @@ __global__ void __launch_bounds__(ScanShape<T, D, kSolve, kFor>::kThreads,
 }
 
 // --------------------------------------------------------------- between segments
-// A block takes E of the state's columns of one (batch, head).
+// A block takes E of the state's columns of one (batch, head).  kTerms: three where a state is a
+// result, else one (a state is rounded to 2^-11 once a segment).
 template <int D>
 struct JoinShape {
   static constexpr int E = D < 64 ? D : 64, kThreads = E * 2, kRow = D + 8;
   static constexpr int kBytes = 2 * D * kRow * 4;
 };
-template <int D, bool kBack>
+template <int D, bool kBack, int kTerms>
 __global__ void __launch_bounds__(JoinShape<D>::kThreads)
     join_kernel(const float *init, const int32_t *seq_lens, float *own, const float *moves, int N,
                 int H, int tokens, int count) {
@@ -581,7 +589,7 @@ __global__ void __launch_bounds__(JoinShape<D>::kThreads)
     const float *m = tile + (i & 1) * D * kRow;
 #pragma unroll
     for (int k = 0; k < D / 8; ++k) {
-      const LeftTf32<3> a(S[k]);
+      const LeftTf32<kTerms> a(S[k]);
 #pragma unroll
       for (int n = 0; n < D / 8; ++n) {
         if (kBack) {
@@ -617,11 +625,11 @@ cudaError_t allow_smem(K kernel, int bytes) {
   return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
 }
 
-template <int D, bool kBack>
+template <int D, bool kBack, int kTerms>
 cudaError_t join_launch(const DeltaArgs &a, const Segments &g, const float *init, float *own,
                         const float *moves, cudaStream_t st) {
   using Jo = JoinShape<D>;
-  const auto join = join_kernel<D, kBack>;
+  const auto join = join_kernel<D, kBack, kTerms>;
   cudaError_t e;
   if ((e = allow_smem(join, Jo::kBytes)) != cudaSuccess) return e;
   const int C = a.dtype == GBLA_FP32 ? kChunkOf<float> : kChunkOf<__nv_bfloat16>;
@@ -646,7 +654,7 @@ cudaError_t launch(const DeltaArgs &a, const Segments &g, float *records, float 
                       nc)) != cudaSuccess)
     return e;
   if (g.count > 1) {
-    const auto own = scan_kernel<T, D, kTerms, kSolve, kSegment>;
+    const auto own = scan_kernel<T, D, kTerms, kSolve, kSegment, kFor == kResults>;
     if ((e = allow_smem(own, Se::kBytes)) != cudaSuccess) return e;
     count_launch();
     // (the backward pass moves its gradients by the last segment's matrix too)
@@ -655,9 +663,10 @@ cudaError_t launch(const DeltaArgs &a, const Segments &g, float *records, float 
                         (float *)nullptr, (float *)nullptr, before, moves, nc, g.chunks, g.count,
                         stride)) != cudaSuccess)
       return e;
-    if ((e = join_launch<D, false>(a, g, a.init, before, moves, st)) != cudaSuccess) return e;
+    if ((e = join_launch<D, false, kSolve>(a, g, a.init, before, moves, st)) != cudaSuccess)
+      return e;
   }
-  const auto scan = scan_kernel<T, D, kTerms, kSolve, kFor>;
+  const auto scan = scan_kernel<T, D, kTerms, kSolve, kFor, kFor == kResults>;
   if ((e = allow_smem(scan, Sc::kBytes)) != cudaSuccess) return e;
   count_launch();
   return launch_pdl(scan, dim3(Sc::kSplit * a.H, a.B, g.count), dim3(Sc::kThreads), Sc::kBytes, st,
@@ -714,16 +723,16 @@ cudaError_t save_forward(const DeltaArgs &a, const Segments &g, bool exact, floa
   return save_d<128>(a, g, exact, rec, states, misses, before, moves, st);
 }
 
-cudaError_t join_segments(const DeltaArgs &a, const Segments &g, bool back, const float *init,
-                          float *own, const float *moves, cudaStream_t st) {
+cudaError_t join_back(const DeltaArgs &a, const Segments &g, bool exact, const float *init,
+                      float *own, const float *moves, cudaStream_t st) {
   if (a.D == 32)
-    return back ? join_launch<32, true>(a, g, init, own, moves, st)
-                : join_launch<32, false>(a, g, init, own, moves, st);
+    return exact ? join_launch<32, true, 3>(a, g, init, own, moves, st)
+                 : join_launch<32, true, 1>(a, g, init, own, moves, st);
   if (a.D == 64)
-    return back ? join_launch<64, true>(a, g, init, own, moves, st)
-                : join_launch<64, false>(a, g, init, own, moves, st);
-  return back ? join_launch<128, true>(a, g, init, own, moves, st)
-              : join_launch<128, false>(a, g, init, own, moves, st);
+    return exact ? join_launch<64, true, 3>(a, g, init, own, moves, st)
+                 : join_launch<64, true, 1>(a, g, init, own, moves, st);
+  return exact ? join_launch<128, true, 3>(a, g, init, own, moves, st)
+               : join_launch<128, true, 1>(a, g, init, own, moves, st);
 }
 
 }  // namespace delta

@@ -256,9 +256,9 @@ struct Gates {
   static constexpr int kFloats = 5 * C + 4;
 };
 
-// A chunk's record.  For the forward pass M, P and the powers of its gates, M in kSolve terms, P
-// in one where results are bf16.  For the backward pass (kBack) M, and, for products that sum
-// over the row index, T = (1 + beta X)^-1 and P the other way round, in kSolve terms.
+// A chunk's record.  For the forward pass beta M, P and the powers of its gates, M in kSolve terms,
+// P in one where results are bf16.  For the backward pass (kBack) M - 1, and, for products that sum
+// over the row index, T - 1 with T = (1 + beta X)^-1, and P the other way round, in kSolve terms.
 template <typename T, int kSolve, bool kBack>
 struct Record {
   static constexpr int C = kChunkOf<T>;
@@ -484,10 +484,10 @@ Segments segments_of(const DeltaArgs &a);
 cudaError_t save_forward(const DeltaArgs &a, const Segments &g, bool exact, float *records,
                          float *states, float *misses, float *before, float *moves,
                          cudaStream_t st);
-// Turns what each segment forms by itself into the state after it (kBack: before it), in place:
-// S' = move S + own (A' = move^T A + own), one segment after the other.
-cudaError_t join_segments(const DeltaArgs &a, const Segments &g, bool back, const float *init,
-                          float *own, const float *moves, cudaStream_t st);
+// Turns what each segment adds to the gradient of the state into that before it, in place:
+// A' = move^T A + own, from the last segment on.
+cudaError_t join_back(const DeltaArgs &a, const Segments &g, bool exact, const float *init,
+                      float *own, const float *moves, cudaStream_t st);
 
 }  // namespace delta
 }  // namespace gbla

@@ -19,9 +19,11 @@ namespace delta {
 namespace {
 
 // --------------------------------------------------------------- first launch
-// One block a (chunk, head, batch), a warp for each 16 of its tokens.  (Blocks that stay and take
-// the chunks that there are one after the other were a third slower than a grid whose blocks for
-// a short sequence's missing chunks end at once: ragged D = 128 606 us for 450.)
+// A block takes `each` chunks of a (head, batch) one after the other, a warp for each 16 tokens.
+// One, but for large ragged batches four: the blocks that find no chunk are then a quarter as
+// many (ragged D = 128 378 us, 419 with one, 390 with two and 380 with eight; full lengths, B2 H8
+// N32768 D64, 81 us with one and 86 with four).  Blocks that stay and number the chunks that
+// there are took 606 us.
 template <typename T, int D>
 struct PrepShape {
   static constexpr int C = kChunkOf<T>, kWarps = C / 16, kThreads = kWarps * 32;
@@ -184,22 +186,18 @@ __device__ __forceinline__ void invert(float *to, const float *A, int w) {
   }
 }
 
+// One chunk of head h of sequence b, n of its tokens there; ends without a barrier.
 template <typename T, int D, int kSolve, bool kBack>
-__global__ void __launch_bounds__(PrepShape<T, D>::kThreads, PrepShape<T, D>::kBlocks)
-    prepare_kernel(const DeltaArgs p, float *records, int nc) {
+__device__ __forceinline__ void prepare_chunk(const DeltaArgs &p, char *raw, float *rec, int h,
+                                              int b, int t0, int n) {
   using Sh = PrepShape<T, D>;
   using Rec = Record<T, kSolve, kBack>;
   constexpr int C = Sh::C, kThreads = Sh::kThreads, kRow = Sh::kRow, kMat = Sh::kMat;
-  extern __shared__ __align__(16) char raw[];
   T *ks = (T *)raw, *qs = ks + C * kRow;
   float *A = (float *)(raw + Sh::kFirst), *inv = (float *)raw;
   float *hi = A + C * kMat, *lo = hi + C, *beta = lo + C;
   TwoFloat *first = (TwoFloat *)(beta + 2 * C);
-  grid_dep_wait();
-  const int h = blockIdx.y, b = blockIdx.z, hk = h / (p.H / p.Hk), tid = threadIdx.x;
-  const int L = p.seq_lens ? min(max(__ldg(p.seq_lens + b), 0), p.N) : p.N;
-  const int t0 = blockIdx.x * C, n = min(C, L - t0);
-  if (n <= 0) return;
+  const int hk = h / (p.H / p.Hk), tid = threadIdx.x;
   load_rows<T, C, D, kThreads>(ks, (const T *)p.k + b * p.sk[0] + t0 * p.sk[1] + (long long)hk * D,
                                p.sk[1], n, tid);
   load_rows<T, C, D, kThreads>(qs, (const T *)p.q + b * p.sq[0] + t0 * p.sq[1] + (long long)hk * D,
@@ -229,7 +227,6 @@ __global__ void __launch_bounds__(PrepShape<T, D>::kThreads, PrepShape<T, D>::kB
   }
   cp_async_wait_all();
   __syncthreads();
-  float *rec = records + (((size_t)b * p.H + h) * nc + blockIdx.x) * Rec::kFloats;
   float *gt = rec + Rec::kGates;
   if (tid < C) {
     if (tid >= 32) G = sum_of(*first, G);
@@ -329,6 +326,23 @@ __global__ void __launch_bounds__(PrepShape<T, D>::kThreads, PrepShape<T, D>::kB
     __syncthreads();
     invert<C, kSolve>(inv, A, w);
     put(rec + Rec::kT, typename Rec::M{}, true, true);
+  }
+}
+
+template <typename T, int D, int kSolve, bool kBack>
+__global__ void __launch_bounds__(PrepShape<T, D>::kThreads, PrepShape<T, D>::kBlocks)
+    prepare_kernel(const DeltaArgs p, float *records, int nc, int each) {
+  constexpr int C = PrepShape<T, D>::C;
+  extern __shared__ __align__(16) char raw[];
+  grid_dep_wait();
+  const int h = blockIdx.y, b = blockIdx.z;
+  const int L = p.seq_lens ? min(max(__ldg(p.seq_lens + b), 0), p.N) : p.N;
+  const int first = blockIdx.x * each, end = min(first + each, (L + C - 1) / C);
+  for (int c = first; c < end; ++c) {
+    if (c > first) __syncthreads();  // the chunk before is done with
+    prepare_chunk<T, D, kSolve, kBack>(
+        p, raw, records + (((size_t)b * p.H + h) * nc + c) * Record<T, kSolve, kBack>::kFloats, h, b,
+        c * C, min(C, L - c * C));
   }
 }
 
@@ -649,9 +663,10 @@ cudaError_t launch(const DeltaArgs &a, const Segments &g, float *records, float 
   cudaError_t e;
   const auto prep = prepare_kernel<T, D, kSolve, kFor == kSave>;
   if ((e = allow_smem(prep, Pr::kBytes)) != cudaSuccess) return e;
+  const int each = a.seq_lens && (long long)nc * a.H * a.B >= 64ll * sm_count() ? 4 : 1;
   count_launch();
-  if ((e = launch_pdl(prep, dim3(nc, a.H, a.B), dim3(Pr::kThreads), Pr::kBytes, st, a, records,
-                      nc)) != cudaSuccess)
+  if ((e = launch_pdl(prep, dim3((nc + each - 1) / each, a.H, a.B), dim3(Pr::kThreads), Pr::kBytes,
+                      st, a, records, nc, each)) != cudaSuccess)
     return e;
   if (g.count > 1) {
     const auto own = scan_kernel<T, D, kTerms, kSolve, kSegment, kFor == kResults>;

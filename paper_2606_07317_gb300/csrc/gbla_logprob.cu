@@ -75,7 +75,7 @@ struct Sums {
   float m, z, w;
 };
 __device__ __forceinline__ float base_of(float m) { return m == -INFINITY ? 0.f : m; }
-// c: scale log2 e.  The same for (a, b) and (b, a): lanes that exchange theirs agree to the bit.
+// c: scale log2 e.
 __device__ __forceinline__ Sums joined(const Sums &a, const Sums &b, float c) {
   Sums r;
   r.m = max_nan(a.m, b.m);
@@ -86,6 +86,26 @@ __device__ __forceinline__ Sums joined(const Sums &a, const Sums &b, float c) {
   r.z = __fadd_rn(__fmul_rn(a.z, ea), __fmul_rn(b.z, eb));
   r.w = __fadd_rn(__fmul_rn(fmaf(da, a.z, a.w), ea), __fmul_rn(fmaf(db, b.z, b.w), eb));
   return r;
+}
+
+// The sums of all 32 lanes of a warp, or of the first kLanes where each kLanes hold the same ones:
+// moved to their common maximum first, added then.
+__device__ __forceinline__ float lanes_max(float m) {
+  float r;
+  asm volatile("redux.sync.max.NaN.f32 %0, %1, 0xffffffff;" : "=f"(r) : "f"(m));
+  return r;
+}
+template <int kLanes>
+__device__ __forceinline__ Sums joined_lanes(Sums s, float c) {
+  const float m = lanes_max(s.m), d = fmaxf((s.m - base_of(m)) * c, -1e4f), e = exp2f(d);
+  // products rounded by themselves: a sum is the same from both its sides
+  s.w = __fmul_rn(fmaf(d, s.z, s.w), e), s.z = __fmul_rn(s.z, e), s.m = m;
+#pragma unroll
+  for (int i = kLanes / 2; i > 0; i >>= 1) {
+    s.z += __shfl_xor_sync(0xFFFFFFFFu, s.z, i);
+    s.w += __shfl_xor_sync(0xFFFFFFFFu, s.w, i);
+  }
+  return s;
 }
 
 // Order of candidates: larger logits first, equal ones by their tokens (lowest first).
@@ -103,15 +123,40 @@ __device__ __forceinline__ uint64_t key_of(uint32_t order, uint32_t index) {
   return ((uint64_t)order << 32) | (uint32_t)~index;
 }
 
+// done(key, rank) for each of n different keys in shared memory (0 is none of them): how many are
+// larger.  A thread ranks kEach at a time.
+template <int kThreads, int kEach, typename F>
+__device__ __forceinline__ void ranked(const uint64_t *keys, int n, F done) {
+  for (int i0 = threadIdx.x; i0 < n; i0 += kThreads * kEach) {
+    uint64_t mine[kEach];
+    int rank[kEach];
+#pragma unroll
+    for (int u = 0; u < kEach; ++u) {
+      mine[u] = i0 + u * kThreads < n ? keys[i0 + u * kThreads] : 0;
+      rank[u] = 0;
+    }
+#pragma unroll 8
+    for (int j = 0; j < n; ++j) {
+      const uint64_t k = keys[j];
+#pragma unroll
+      for (int u = 0; u < kEach; ++u) rank[u] += k > mine[u];
+    }
+#pragma unroll
+    for (int u = 0; u < kEach; ++u)
+      if (mine[u]) done(mine[u], rank[u]);
+  }
+}
+
 // What the blocks of a cluster that share a row tell one another.
 template <int kThreads>
 struct Shared {
-  static constexpr int kCandidates = kThreads == 32 ? 256 : 1280;
+  static constexpr int kCandidates = kThreads == 32 ? 640 : 1280;
   Sums part[kThreads / 32];
   Sums whole;                    // of this block
-  int count;                     // candidates
+  int count, strips;             // candidates, threads whose logits may hold some
   uint64_t bound;
   uint64_t key[128];
+  int strip[kThreads];
   uint64_t most[kThreads];
   uint64_t cand[kCandidates];
   uint64_t best[GBLA_MAX_TOP];   // this block's, in order
@@ -193,12 +238,15 @@ __device__ __forceinline__ void weigh(uint64_t &z, uint64_t &w, uint4 v, uint64_
 // logits' bytes, beside issue slots (packed arithmetic: 6 or 7 a bf16 logit, 12 without) and one
 // exponential a logit.
 //
-// Top alternatives: the K-th largest of the maxima of at least 2 K groups of threads bounds the
-// K-th logit from below, and only threads that reach it look at their logits again: a little over
-// K candidates, whose ranks are counted.
+// Top alternatives: the K-th largest of at least 2 K maxima of groups of vectors bounds the
+// K-th logit from below, and only the logits of threads that reach it are looked at again, by all
+// threads: a little over K candidates, whose ranks are counted (2048 rows of 8191 fp32, K = 32:
+// 27 us; 35 where each such thread looks at its own and lanes' sums are joined in pairs).  The rule
+// for a row's threads does not ask for K: the other results are the same to the bit without.
 template <typename T, int kThreads, bool kTop>
 __global__ void __launch_bounds__(kThreads) logprob_kernel(const LogprobArgs p, int split) {
   constexpr int kVec = Row<T>::kVec, kBatch = 4, kWarps = kThreads / 32;
+  constexpr int kMaxima = kThreads == 32 ? kBatch : 1;  // of a thread
   using Sh = Shared<kThreads>;
   __shared__ Sh sm;
   cg::cluster_group cluster = cg::this_cluster();
@@ -216,8 +264,10 @@ __global__ void __launch_bounds__(kThreads) logprob_kernel(const LogprobArgs p, 
               v1 = min(v0 + per, row.vecs);
     const bool last = part == split - 1;
     Sums s = {-INFINITY, 0.f, 0.f};
-    float tmax = -INFINITY;
-    uint64_t key = 0;
+    float tmax[kMaxima];  // of the vectors, the first of them that has it
+    int most[kMaxima];
+#pragma unroll
+    for (int j = 0; j < kMaxima; ++j) tmax[j] = NAN, most[j] = -1;
     auto move = [&](float m) {  // the sums' base to a larger maximum
       if (!(m <= s.m)) {
         const float base = base_of(max_nan(m, s.m)), d = fmaxf((s.m - base) * c, -1e4f), e = exp2f(d);
@@ -238,8 +288,8 @@ __global__ void __launch_bounds__(kThreads) logprob_kernel(const LogprobArgs p, 
         if (u < n) {
           m[u] = max_of(v[u], T());
           all = max_nan(all, m[u]);
-          if (kTop && (key == 0 || m[u] > tmax))
-            tmax = m[u], key = key_of(order_of(m[u]), (i0 + u * kThreads) * kVec + row.head + kVec - 1);
+          if (kTop && !(m[u] <= tmax[u % kMaxima]))
+            tmax[u % kMaxima] = m[u], most[u % kMaxima] = i0 + u * kThreads;
         }
       move(all);
       const float base = base_of(s.m);
@@ -269,6 +319,12 @@ __global__ void __launch_bounds__(kThreads) logprob_kernel(const LogprobArgs p, 
       for (int u = 0; u < kBatch; ++u) v[u] = ahead[u];
     }
     if (i0 < v1) take(i0, (v1 - i0 + kThreads - 1) / kThreads);
+    uint64_t own[kMaxima], key = 0;
+#pragma unroll
+    for (int j = 0; j < kMaxima; ++j)
+      own[j] = kTop && most[j] >= 0
+                   ? key_of(order_of(tmax[j]), most[j] * kVec + row.head + kVec - 1)
+                   : 0;
     if (last)
       for (int j = tid; j < row.loose(); j += kThreads) {
         const int at = row.place(j);
@@ -278,22 +334,17 @@ __global__ void __launch_bounds__(kThreads) logprob_kernel(const LogprobArgs p, 
         s.z += e, s.w = fmaf(e, d, s.w);
         if (kTop) {
           const uint64_t k = key_of(order_of(x), at);
-          if (k > key) key = k;
+          if (k > own[0]) own[0] = k;
         }
       }
     const int token = p.tokens ? __ldg(p.tokens + r) : -1;
     float given = 0.f;  // its logit, on the way early
     if (tid == 0 && part == 0 && token >= 0 && token < p.V) given = to_f(row.p[token]);
+    s = joined_lanes<32>(s, c);
 #pragma unroll
-    for (int m = 16; m > 0; m >>= 1) {
-      Sums o;
-      o.m = __shfl_xor_sync(0xFFFFFFFFu, s.m, m);
-      o.z = __shfl_xor_sync(0xFFFFFFFFu, s.z, m);
-      o.w = __shfl_xor_sync(0xFFFFFFFFu, s.w, m);
-      s = joined(s, o, c);
-    }
-    // groups of threads: 32, 64 or 128, at least twice K where there are so many
-    const int lg = kThreads == 32 || p.K <= 16 ? 5 : p.K <= 32 ? 6 : 7;
+    for (int j = 0; j < kMaxima; ++j) key = own[j] > key ? own[j] : key;
+    // groups of threads, or a warp's threads' maxima: 32, 64 or 128, at least twice K
+    const int lg = p.K <= 16 ? 5 : p.K <= 32 ? 6 : 7;
     const int width = kThreads >> lg;  // threads of a group
     uint64_t top = key;
     if (kTop)
@@ -303,59 +354,77 @@ __global__ void __launch_bounds__(kThreads) logprob_kernel(const LogprobArgs p, 
       }
     __syncthreads();  // the row before is done with
     if (lane == 0) sm.part[tid / 32] = s;
-    if (kTop && tid % width == 0) sm.key[tid / width] = top;
-    if (tid == 0) sm.count = 0, sm.bound = 0;
-    __syncthreads();
-    if (kWarps > 1) {
-      s = sm.part[lane % kWarps];
+    if (kTop && kMaxima > 1 && lg > 5) {
 #pragma unroll
-      for (int m = kWarps / 2; m > 0; m >>= 1) {
-        Sums o;
-        o.m = __shfl_xor_sync(0xFFFFFFFFu, s.m, m);
-        o.z = __shfl_xor_sync(0xFFFFFFFFu, s.z, m);
-        o.w = __shfl_xor_sync(0xFFFFFFFFu, s.w, m);
-        s = joined(s, o, c);
+      for (int j = 0; j < kMaxima; j += 2) {
+        const uint64_t a = own[j], b = own[(j + 1) % kMaxima];
+        if (lg == 6)
+          sm.key[tid * 2 + j / 2] = a > b ? a : b;
+        else
+          sm.key[tid * 4 + j] = a, sm.key[tid * 4 + j + 1] = b;
       }
+    } else if (kTop && tid % width == 0) {
+      sm.key[tid / width] = top;
     }
+    if (tid == 0) sm.count = 0, sm.strips = 0, sm.bound = 0;
+    __syncthreads();
+    if (kWarps > 1) s = joined_lanes<kWarps>(sm.part[lane % kWarps], c);
     if (kTop) {
-      if (tid < 1 << lg) {
-        const uint64_t mine = sm.key[tid];
-        int rank = 0;
-#pragma unroll 8
-        for (int i = 0; i < 1 << lg; ++i) rank += sm.key[i] > mine;
-        if (mine && rank == p.K - 1) sm.bound = mine;
-      }
+      ranked<kThreads, kMaxima>(sm.key, 1 << lg, [&](uint64_t k, int rank) {
+        if (rank == p.K - 1) sm.bound = k;
+      });
       __syncthreads();
       const uint64_t bound = sm.bound;
-      auto offer = [&](uint64_t k) {
-        if (k < bound) return;
-        const int at = atomicAdd(&sm.count, 1);
-        if (at < Sh::kCandidates) sm.cand[at] = k;
-      };
       if (key >= bound && key) {
-        const bool every = (uint32_t)(bound >> 32) <= 1u;  // no bound, or that of a NaN
-        const float least = every ? -INFINITY : value_of((uint32_t)(bound >> 32));
-#pragma unroll 4
-        for (int i = v0 + tid; i < v1; i += kThreads) {
-          float x[kVec];
-          unpack(__ldg(row.vec(i)), x);
-#pragma unroll
-          for (int e = 0; e < kVec; ++e)
-            if (every || x[e] >= least) offer(key_of(order_of(x[e]), i * kVec + row.head + e));
-        }
+        sm.strip[atomicAdd(&sm.strips, 1)] = tid;
         if (last)
-          for (int j = tid; j < row.loose(); j += kThreads)
-            offer(key_of(order_of(to_f(row.p[row.place(j)])), row.place(j)));
+          for (int j = tid; j < row.loose(); j += kThreads) {
+            const uint64_t k = key_of(order_of(to_f(row.p[row.place(j)])), row.place(j));
+            if (k < bound) continue;
+            const int at = atomicAdd(&sm.count, 1);
+            if (at < Sh::kCandidates) sm.cand[at] = k;
+          }
       }
+      __syncthreads();
+      const int strips = sm.strips, each = (v1 - v0 + kThreads - 1) / kThreads;
+      const int shift = each > 16 ? 5 : each > 8 ? 4 : each > 4 ? 3 : 2, across = kThreads >> shift;
+      const bool every = (uint32_t)(bound >> 32) <= 1u;  // no bound, or that of a NaN
+      const float least = every ? -INFINITY : value_of((uint32_t)(bound >> 32));
+      const int until = (int)~(uint32_t)bound;
+      for (int k = tid & ((1 << shift) - 1); k < each; k += 1 << shift)
+        for (int e0 = tid >> shift; e0 < strips; e0 += kBatch * across) {
+          int at[kBatch];
+#pragma unroll
+          for (int u = 0; u < kBatch; ++u) {
+            at[u] = e0 + u * across < strips ? v0 + sm.strip[e0 + u * across] + k * kThreads : v1;
+            if (at[u] < v1) v[u] = __ldg(row.vec(at[u]));
+          }
+#pragma unroll
+          for (int u = 0; u < kBatch; ++u) {
+            if (at[u] >= v1 || (!every && max_of(v[u], T()) < least)) continue;
+            float x[kVec];
+            unpack(v[u], x);
+            uint32_t hits = 0;  // above the bound, or like it and not behind it
+#pragma unroll
+            for (int e = 0; e < kVec; ++e)
+              if (every || x[e] > least || (x[e] == least && at[u] * kVec + row.head + e <= until))
+                hits |= 1u << e;
+            int to = hits ? atomicAdd(&sm.count, __popc(hits)) : 0;
+#pragma unroll
+            for (int e = 0; e < kVec; ++e)
+              if (hits >> e & 1) {
+                if (to < Sh::kCandidates)
+                  sm.cand[to] = key_of(order_of(x[e]), at[u] * kVec + row.head + e);
+                ++to;
+              }
+          }
+        }
       __syncthreads();
       const int n = sm.count;
       if (n <= Sh::kCandidates) {
-        for (int i = tid; i < n; i += kThreads) {
-          const uint64_t k = sm.cand[i];
-          int rank = 0;
-          for (int j = 0; j < n; ++j) rank += sm.cand[j] > k;
+        ranked<kThreads, kMaxima>(sm.cand, n, [&](uint64_t k, int rank) {
           if (rank < p.K) sm.best[rank] = k;
-        }
+        });
         for (int i = n + tid; i < p.K; i += kThreads) sm.best[i] = 0;
       } else {  // too many (one thread's logits the largest): the best below the one before, K times
         uint64_t before = ~0ull;
@@ -393,17 +462,14 @@ __global__ void __launch_bounds__(kThreads) logprob_kernel(const LogprobArgs p, 
           for (int i = tid; i < n; i += kThreads)
             sm.cand[i] = cluster.map_shared_rank(&sm, i / p.K)->best[i % p.K];
           __syncthreads();
-          for (int i = tid; i < n; i += kThreads) {
-            const uint64_t k = sm.cand[i];
-            int rank = 0;
-            for (int j = 0; j < n; ++j) rank += sm.cand[j] > k;
-            if (k && rank < p.K) sm.best[rank] = k;
-          }
+          ranked<kThreads, 1>(sm.cand, n, [&](uint64_t k, int rank) {
+            if (rank < p.K) sm.best[rank] = k;
+          });
           __syncthreads();
         }
       }
     }
-    if (part == 0) {
+    if (part == 0 && tid < (kTop ? p.K : 1)) {
       const bool bad = s.m != s.m || s.m == INFINITY;
       const float lnz = logf(s.z);
       const float lse = bad ? NAN : s.z > 0.f ? fmaf(s.m, p.scale, lnz) : -INFINITY;
@@ -532,15 +598,15 @@ cudaError_t forward_t(const LogprobArgs &a, cudaStream_t st) {
   while (split < 8 && rows * split * 2 <= sms * 4 && vecs / (split * 2) >= 256) split *= 2;
   long long blocks = 8ll * sms / split;
   if (blocks > rows) blocks = rows;
-  // a warp a row where that leaves each lane a few vectors (and twice as many lanes as K)
-  if (split == 1 && a.V <= (a.K <= 16 ? 1024 : 128)) {
+  // a warp a row where that leaves each lane a few vectors
+  if (split == 1 && a.V <= 1024) {
     blocks = 24ll * sms;
     if (blocks > rows) blocks = rows;
     if (a.K > 0) return forward_launch<T, 32, true>(a, 1, (int)blocks, st);
     return forward_launch<T, 32, false>(a, 1, (int)blocks, st);
   }
   // and half the threads for all but the longest rows: what a row costs beside its logits it costs
-  // each warp (V = 50021 bf16: 139 us, 156 with 256 threads; V = 8191 fp32, 32 of them: 35 and 42)
+  // each warp (V = 50021 bf16: 136 us, 148 with 256 threads; V = 8191 fp32, 32 of them: 27 and 31)
   if (split == 1 && vecs <= 16384) {
     blocks = 8ll * sms;
     if (blocks > rows) blocks = rows;

@@ -188,6 +188,29 @@ def test_top_where_one_thread_has_them(dtype, V, top, threads):
     check(gbla.token_logprobs(x, top=top), R.logprobs(x, None, top, 1.0))
 
 
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("V", [129, 300, 517, 641, 1000, 1024, 1025])
+@pytest.mark.parametrize("top", [16, 17, 32, 33, 64])
+def test_top_of_short_rows(dtype, V, top):
+    """Rows that a warp takes: any order, ties, masks; the other results to the bit without them."""
+    x, tok, g = rows(V, 1, 9, V, dtype)
+    x[0, 1] = x[0, 1].sort(dim=-1).values
+    x[0, 2] = x[0, 2].sort(dim=-1, descending=True).values
+    x[0, 3] = torch.randint(0, 2, (V,), generator=g).to(x)
+    x[0, 4, top + 1:] = -math.inf
+    x[0, 5, :-3] = -math.inf
+    x[0, 6] = -math.inf
+    x[0, 7] = 1.5
+    x[0, 8, ::3] = math.nan
+    got = gbla.token_logprobs(x, tok, top=top)
+    check({n: t[:, :8] for n, t in got.items()}, R.logprobs(x[:, :8], tok[:, :8], top, 1.0))
+    last = got["top_token"][0, 8].tolist()
+    assert all(0 <= i < V for i in last) and len(set(last)) == top
+    alone = gbla.token_logprobs(x[:, :8], tok[:, :8])
+    for n in alone:
+        assert torch.equal(alone[n], got[n][:, :8]), n
+
+
 def test_far_rows():
     """Offsets beyond 2^32 bytes."""
     B, V = 3, 4099

@@ -271,7 +271,7 @@ __global__ void __launch_bounds__(kThreads) logprob_kernel(const LogprobArgs p, 
     auto move = [&](float m) {  // the sums' base to a larger maximum
       if (!(m <= s.m)) {
         const float base = base_of(max_nan(m, s.m)), d = fmaxf((s.m - base) * c, -1e4f), e = exp2f(d);
-        s.w = fmaf(d, s.z, s.w) * e, s.z *= e, s.m = max_nan(m, s.m);
+        s.w = __fmul_rn(fmaf(d, s.z, s.w), e), s.z = __fmul_rn(s.z, e), s.m = max_nan(m, s.m);
       }
     };
     uint4 v[kBatch], ahead[kBatch];
@@ -478,7 +478,7 @@ __global__ void __launch_bounds__(kThreads) logprob_kernel(const LogprobArgs p, 
       };
       if (tid == 0) {
         p.lse[r] = lse;
-        p.entropy[r] = bad ? NAN : s.z > 0.f ? lnz - kLn2 * (s.w / s.z) : 0.f;
+        p.entropy[r] = bad ? NAN : s.z > 0.f ? fmaf(-kLn2, s.w / s.z, lnz) : 0.f;
         if (p.logprob) p.logprob[r] = token >= 0 && token < p.V ? logp(given) : 0.f;
       }
       if (kTop)

@@ -663,7 +663,7 @@ Layout layout_of(const DeltaBackArgs &p, bool exact) {
   take(l.after, all * a.D * a.D);
   take(l.misses, all * C * a.D);
   take(l.weights, all * C * a.D);
-  l.segments = segments_of(a);
+  l.segments = segments_of(a, true);
   for (size_t *to : {&l.before, &l.own, &l.moves}) take(*to, l.segments.floats(a));
   const size_t plane = a.H == a.Hk ? 0 : (size_t)a.B * a.N * a.H * a.D;
   take(l.dq, plane);

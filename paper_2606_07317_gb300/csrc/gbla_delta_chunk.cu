@@ -711,20 +711,25 @@ cudaError_t save_d(const DeltaArgs &a, const Segments &g, bool exact, float *rec
 }  // namespace
 
 // How many segments.  In units of a chunk in a scan of whole sequences (measured, bf16 D = 64:
-// 2.1 us): a round of blocks takes a segment's chunks; the scan that forms the segments' own
-// states and matrices as much (twice the columns, twice the blocks an SM); and a segment that
-// is joined 1.2.  B2 H8 N32768: 1 segment 1125 us, 4 530, 9 375, 19 389; B8 H8 N2048 is not cut
-// (132 us, 2 segments 127, 4 145).
-Segments segments_of(const DeltaArgs &a) {
+// 2.0 us, 2.9 with states of full precision): a round of blocks takes a segment's chunks; the scan
+// that forms the segments' own states and matrices has twice the blocks, two an SM, and as much
+// for a round of these; 0.6 where there is one an SM, which pays neither with states of full
+// precision at D = 128 (B4 H8 N2048 200 us, 125 whole) nor in fp32 (B8 H8 N2048 D64 270 and 241)
+// nor for the backward's three further passes (the same in bf16 302 and 287); a segment that is
+// joined 1.2.
+// B2 H8 N32768: 1 segment 1059 us, 4 474, 9 319, 19 329; B8 H8 N2048, states out: 1 119, 2 112,
+// 4 130.
+Segments segments_of(const DeltaArgs &a, bool back) {
   const int nc = a.dtype == GBLA_FP32 ? chunks_of<float>(a) : chunks_of<__nv_bfloat16>(a);
   const long long blocks = (long long)a.B * a.H * (a.D > 64 ? 2 : 1), sms = sm_count();
+  const double lone = back || (exact_state(a) && (a.D > 64 || a.dtype == GBLA_FP32)) ? 1. : 0.6;
   Segments best = {1, nc};
   double least = 0.;
   for (int want = 1; want <= 64 && want <= nc; ++want) {
     const int chunks = (nc + want - 1) / want, count = (nc + chunks - 1) / chunks;
     double cost = (double)((blocks * count + sms - 1) / sms) * chunks;
-    if (count > 1)
-      cost += (double)((blocks * (count - 1) + sms - 1) / sms) * chunks + 1.2 * (count - 1) + 4.;
+    const long long half = (2 * blocks * (count - 1) + sms - 1) / sms;
+    if (count > 1) cost += (half / 2 + lone * (half % 2)) * chunks + 1.2 * (count - 1) + 4.;
     if (want == 1 || cost < least) least = cost, best = {count, chunks};
   }
   return best;
@@ -762,11 +767,11 @@ static size_t record_floats(const DeltaArgs &a) {
 }
 
 size_t delta_forward_floats(const DeltaArgs &a) {
-  return record_floats(a) + 2 * delta::segments_of(a).floats(a);
+  return record_floats(a) + 2 * delta::segments_of(a, false).floats(a);
 }
 
 cudaError_t delta_forward(const DeltaArgs &a, float *scratch, cudaStream_t st) {
-  const delta::Segments g = delta::segments_of(a);
+  const delta::Segments g = delta::segments_of(a, false);
   float *before = scratch + record_floats(a), *moves = before + g.floats(a);
   if (a.D == 32) return delta::forward_d<32>(a, g, scratch, before, moves, st);
   if (a.D == 64) return delta::forward_d<64>(a, g, scratch, before, moves, st);

@@ -477,7 +477,7 @@ struct Segments {
     return count > 1 ? (size_t)a.B * a.H * count * a.D * a.D : 0;
   }
 };
-Segments segments_of(const DeltaArgs &a);
+Segments segments_of(const DeltaArgs &a, bool back);
 // First part of the backward pass: records (of the backward's form), the states before all
 // chunks and the misses, packed; `moves`: the matrices that segments move a state by.  exact:
 // three terms throughout.

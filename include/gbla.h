@@ -614,7 +614,7 @@ gbla_status gbla_delta_attention_step(const void *q, const void *k, const void *
  *   top_logprob [B, N, top] fp32, top_token [B, N, top] int32, with 0 < top <=
  *             min(V, GBLA_MAX_TOP) (else NULL): in descending order, equal logits in the
  *             order of their tokens
- * Rows t >= L_b are untouched.  1 <= V <= 2^30, B N <= 2^30, scale positive and normal.  Logits of
+ * Rows t >= L_b are untouched.  1 <= V <= 2^30, B N <= 2^30, 2^-100 <= scale <= 2^100.  Logits of
  * -inf are ruled out (p = 0); a row of nothing else has lse and log probabilities of
  * -inf and entropy 0.  A NaN or +inf makes the results of its row NaN; its top tokens
  * are in range (NaN counts as the least).  fp32 arithmetic, one launch, allocates

@@ -968,7 +968,8 @@ gbla_status check_logprob(LogprobArgs *a, size_t *bytes, const void *logits, con
                           float scale, gbla_dtype dtype, bool *empty) {
   if (B < 0 || N < 0 || V < 1 || V > (1 << 30)) return GBLA_ERR_INVALID_ARG;
   if (dtype != GBLA_FP32 && dtype != GBLA_BF16) return GBLA_ERR_UNSUPPORTED;
-  if (!(scale > 0.f) || !isnormal(scale)) return GBLA_ERR_INVALID_ARG;
+  // (beyond: scale log2 e passes fp32's range, or distances of logits that pass it still weigh)
+  if (!(scale >= 0x1p-100f && scale <= 0x1p100f)) return GBLA_ERR_INVALID_ARG;
   const unsigned long long rows = (unsigned long long)B * N;
   if (rows > (1ull << 30) || rows * V > (1ull << 40)) return GBLA_ERR_INVALID_ARG;
   *empty = rows == 0;

@@ -194,3 +194,14 @@ def test_binding_refuses_before_the_call():
     for fn in (delta, back, step, score, grad):  # nothing else wrong: host tensors
         with pytest.raises(ValueError, match="CUDA device"):
             fn()
+
+
+@pytest.mark.parametrize("op", ["logprobs", "logprobs_backward"])
+def test_logit_scales(lib, op):
+    """Scales whose products with log2 e, or with distances of logits, leave fp32's range."""
+    none = {n: None for n in OPS[op][1].split()} | {"B": 0} | ({"top": 0} if op == "logprobs" else {})
+    for s in (2.0 ** -101, 1.2e-38, 2.0 ** 101, 2.4e38, 3.4e38):
+        assert _run(lib, op, scale=s) == INV, s
+        assert _run(lib, op, **none, scale=s) == INV, s
+    for s in (2.0 ** -100, 1.0, 2.0 ** 100):
+        assert _run(lib, op, **none, scale=s) == OK, s

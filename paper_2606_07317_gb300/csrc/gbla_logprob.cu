@@ -205,8 +205,8 @@ __device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) {
 }
 // z += 2^t, w += 2^t t with t = (x - base) c, of the values of a vector.  kLifted: bf16 values
 // below -2^100 are taken as that first, two in an instruction, for t to be finite (-inf would
-// make 0 times infinity of its share of w); else t itself is kept above -1e4.  With a base above
-// -2^99 and c between 2^-60 and 2^20 both weigh such values 0.
+// make 0 times infinity of its share of w); else t itself is kept above -1e4.  With a base within
+// 2^99 of 0 and c between 2^-60 and 2^20, |t| is below 2^121, and both weigh such values 0.
 template <bool kLifted, typename T>
 __device__ __forceinline__ void weigh(uint64_t &z, uint64_t &w, uint4 v, uint64_t base, uint64_t c,
                                       T) {
@@ -295,7 +295,7 @@ __global__ void __launch_bounds__(kThreads) logprob_kernel(const LogprobArgs p, 
       const float base = base_of(s.m);
       uint64_t z = 0, w = 0;
       const uint64_t base2 = pair_of(-base, -base);
-      if (lift && base > -0x1p99f) {
+      if (lift && fabsf(base) < 0x1p99f) {
 #pragma unroll
         for (int u = 0; u < kBatch; ++u)
           if (u < n) weigh<true>(z, w, v[u], base2, c2, T());
@@ -473,8 +473,10 @@ __global__ void __launch_bounds__(kThreads) logprob_kernel(const LogprobArgs p, 
       const bool bad = s.m != s.m || s.m == INFINITY;
       const float lnz = logf(s.z);
       const float lse = bad ? NAN : s.z > 0.f ? fmaf(s.m, p.scale, lnz) : -INFINITY;
-      auto logp = [&](float x) {
-        return bad ? NAN : x == -INFINITY ? -INFINITY : fmaf(x - s.m, p.scale, -lnz);
+      auto logp = [&](float x) {  // (half the distance: the whole one may pass fp32's range)
+        return bad              ? NAN
+               : x == -INFINITY ? -INFINITY
+                                : fmaf(0.5f * x - 0.5f * s.m, 2.f * p.scale, -lnz);
       };
       if (tid == 0) {
         p.lse[r] = lse;

@@ -521,6 +521,7 @@ __global__ void __launch_bounds__(kBackThreads) logprob_backward_kernel(const Lo
       if (token < 0 || token >= p.V) token = -1;
       if (p.dlogprob && token >= 0) dlp = p.dlogprob[r];
       if (p.dentropy) dh = p.dentropy[r];
+      if (dh == 0.f) ent = 0.f;  // not asked for: whatever it is has no share
       A = (p.dlse ? p.dlse[r] : 0.f) - dlp;
     }
     // padding, or a row of nothing but masks (also such of a type's lowest value, whose

@@ -7,7 +7,7 @@ import torch
 
 import delta_ref as R
 from paper_2606_07317_gb300 import gbla
-from test_logprob_gpu import TYPES, check
+from test_logprob_gpu import TYPES, check, rows
 
 pytestmark = pytest.mark.gpu
 
@@ -48,3 +48,14 @@ def test_large_logits(dtype, V, top, scale):
     ref = R.logprobs(x, tok, n, scale)
     check(got, {m: r if m == "top_token" else r.float().double() for m, r in ref.items()})
     assert torch.isfinite(got["entropy"]).all()
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+def test_gradient_does_not_read_an_unused_entropy(dtype):
+    x, tok, _ = rows(70, 2, 3, 900, dtype)
+    f = gbla.token_logprobs(x, tok)
+    one, nothing = torch.ones((2, 3)).cuda(), torch.zeros((2, 3)).cuda()
+    bad = torch.full_like(one, math.nan)
+    want = gbla.token_logprobs_backward(x, f["lse"], f["entropy"], tok, one)
+    for h in (None, nothing):
+        assert torch.equal(gbla.token_logprobs_backward(x, f["lse"], bad, tok, one, h), want)

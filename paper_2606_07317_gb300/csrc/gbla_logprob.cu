@@ -527,12 +527,28 @@ __global__ void __launch_bounds__(kBackThreads) logprob_backward_kernel(const Lo
     // padding, or a row of nothing but masks (also such of a type's lowest value, whose
     // lse cannot tell one token from many)
     const bool none = !valid || lse < -1e30f;
-    auto grad = [&](float x, int at) {
-      const float lp = max_nan(fmaf(x, p.scale, -lse), -1e4f);
+    auto grad = [&](float lp, int at) {
       float d = ex2_approx(lp * kLog2e) * fmaf(-dh, lp + ent, A);
       if (at == token) d += dlp;
       return none ? 0.f : d * p.scale;
     };
+    auto log_of = [&](float x) { return max_nan(fmaf(x, p.scale, -lse), -1e4f); };
+    // A far lse has been rounded by more than 2^-11, and an exact product next to it would be off
+    // by as much (an infinity where logits are 1e36): the product rounded in the same way is not.
+    // Where both are infinite, the row's largest logits share its probability, exp(-entropy) each.
+    if (!none && fabsf(lse) >= 0x1p14f) {
+      const float most = -p.entropy[r];
+      auto put = [&](int at) {
+        const float y = __fmul_rn(to_f(in[at]), p.scale);
+        store1(out + at, grad(y == INFINITY ? most : max_nan(__fsub_rn(y, lse), -1e4f), at));
+      };
+      constexpr int kValues = kBackThreads * kBackVecs * kVec;
+      const int from = tile * kValues, to = min(from + kValues, row.vecs * kVec);
+#pragma unroll 1
+      for (int i = from + tid; i < to; i += kBackThreads) put(row.head + i);
+      if (tile == 0 && tid < row.loose()) put(row.place(tid));
+      continue;
+    }
     const int v0 = tile * kBackThreads * kBackVecs + tid;
     uint4 v[kBackVecs];
 #pragma unroll
@@ -556,12 +572,12 @@ __global__ void __launch_bounds__(kBackThreads) logprob_backward_kernel(const Lo
       if (none) v[j] = make_uint4(0, 0, 0, 0);
       unpack(v[j], f);
 #pragma unroll
-      for (int e = 0; e < kVec; ++e) f[e] = grad(f[e], row.head + i * kVec + e);
+      for (int e = 0; e < kVec; ++e) f[e] = grad(log_of(f[e]), row.head + i * kVec + e);
       *((uint4 *)(out + row.head) + i) = pack(f);
     }
     if (tile == 0 && tid < row.loose()) {
       const int at = row.place(tid);
-      store1(out + at, none ? 0.f : grad(to_f(in[at]), at));
+      store1(out + at, none ? 0.f : grad(log_of(to_f(in[at])), at));
     }
   }
 }

@@ -7,7 +7,7 @@ import torch
 
 import delta_ref as R
 from paper_2606_07317_gb300 import gbla
-from test_logprob_gpu import TYPES, check, rows
+from test_logprob_gpu import TYPES, check, grads, rows
 
 pytestmark = pytest.mark.gpu
 
@@ -59,3 +59,43 @@ def test_gradient_does_not_read_an_unused_entropy(dtype):
     want = gbla.token_logprobs_backward(x, f["lse"], f["entropy"], tok, one)
     for h in (None, nothing):
         assert torch.equal(gbla.token_logprobs_backward(x, f["lse"], bad, tok, one, h), want)
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("V", [8, 300, 5000, 70001])
+@pytest.mark.parametrize("top,scale", SIZES)
+def test_gradients_of_large_logits(dtype, V, top, scale):
+    x, tok = large(dtype, V, top)
+    f = gbla.token_logprobs(x, tok, scale=scale)
+    g = torch.Generator().manual_seed(1)
+    d = [torch.randn((1, 8), generator=g).cuda() for _ in range(3)]
+    for which in ([0], [1], [2], [0, 1, 2]):
+        args = [t if i in which else None for i, t in enumerate(d)]
+        got = gbla.token_logprobs_backward(x, f["lse"], f["entropy"], tok, *args, scale=scale)
+        want, mag = R.logprobs_backward(x, tok, scale, *args)
+        assert torch.isfinite(got).all(), which
+        # a probability is 0 or 1 here (the next logit is farther away than any exponent): no share
+        # of lse and logit in the room
+        on = [r for r in range(8) if r != 5 or top * scale < 3.4e38]  # two beyond the range
+        grads(got[:, on], want[:, on], mag[:, on], torch.zeros_like(x[:, on]), dtype, scale)
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("V", [8, 5000])
+def test_gradients_of_shared_largest_logits(dtype, V):
+    """Three equal logits beyond fp32's range when scaled: a third of the probability each."""
+    x = torch.zeros((1, 1, V), dtype=TYPES[dtype], device="cuda")
+    x[0, 0, [1, 3, V - 2]] = 2e38
+    tok = torch.tensor([[3]], dtype=torch.int32, device="cuda")
+    f = gbla.token_logprobs(x, tok, scale=16.0)
+    one = torch.ones((1, 1), device="cuda")
+    got = gbla.token_logprobs_backward(x, f["lse"], f["entropy"], tok, one, 0.5 * one, 0.25 * one, scale=16.0)
+    # p = 1/3, ln p + entropy = 0 (in closed form: 64 bits cannot hold ln 3 beside 3.2e39)
+    want = torch.zeros((1, 1, V), dtype=torch.float64, device="cuda")
+    want[0, 0, [1, 3, V - 2]] = 16 / 3 * (0.25 - 1)
+    want[0, 0, 3] += 16
+    # the probability by way of the entropy's bound, 24 times 640 u, in place of the exponent's;
+    # magnitudes of the terms: at most 16 (1 + 1 + 0.5 * 3 + 0.25)
+    room = (24 * 640 + 96) * 2.0 ** -24 * 60 + (2.0 ** -8 * want.abs() if dtype == "bf16" else 0)
+    assert ((got.double() - want).abs() <= room).all()
+    assert (got[want == 0] == 0).all()

@@ -340,6 +340,8 @@ __global__ void __launch_bounds__(kThreads) logprob_kernel(const LogprobArgs p, 
     const int token = p.tokens ? __ldg(p.tokens + r) : -1;
     float given = 0.f;  // its logit, on the way early
     if (tid == 0 && part == 0 && token >= 0 && token < p.V) given = to_f(row.p[token]);
+    // a NaN hides what else its vector and, before it, its thread hold: they are looked over
+    const bool hidden = kTop && s.m != s.m;
     s = joined_lanes<32>(s, c);
 #pragma unroll
     for (int j = 0; j < kMaxima; ++j) key = own[j] > key ? own[j] : key;
@@ -375,7 +377,7 @@ __global__ void __launch_bounds__(kThreads) logprob_kernel(const LogprobArgs p, 
       });
       __syncthreads();
       const uint64_t bound = sm.bound;
-      if (key >= bound && key) {
+      if ((key >= bound && key) || hidden) {
         sm.strip[atomicAdd(&sm.strips, 1)] = tid;
         if (last)
           for (int j = tid; j < row.loose(); j += kThreads) {

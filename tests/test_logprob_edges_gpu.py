@@ -99,3 +99,29 @@ def test_gradients_of_shared_largest_logits(dtype, V):
     room = (24 * 640 + 96) * 2.0 ** -24 * 60 + (2.0 ** -8 * want.abs() if dtype == "bf16" else 0)
     assert ((got.double() - want).abs() <= room).all()
     assert (got[want == 0] == 0).all()
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("rows_", [3, 400])
+@pytest.mark.parametrize("V", [20, 300, 1021, 5000, 70000])
+def test_top_tokens_beside_nan(dtype, rows_, V):
+    """NaN counts as the least: what else a thread, a vector or a row holds keeps its order."""
+    g = torch.Generator().manual_seed(V)
+    x = torch.randn((1, rows_, V), generator=g)
+    x[torch.rand(x.shape, generator=g) < 0.05] = -math.inf
+    at = torch.randint(0, V, (rows_, 5), generator=g)
+    for r in range(rows_):
+        x[0, r, at[r, 0]] = 90.0 + r % 3            # the largest, then a NaN near it
+        x[0, r, (at[r, 0] + 1) % V] = math.nan
+        x[0, r, at[r, 1:3]] = math.nan
+    x[0, 0, : V // 2] = math.nan
+    x[0, 1] = math.nan
+    x[0, 1, V - 3] = -math.inf
+    x = x.to(TYPES[dtype]).cuda()
+    top = min(V, 12)
+    order = torch.where(x.isnan(), -math.inf, torch.where(x == -math.inf, -1e300, x.double()))
+    want = order.sort(dim=-1, descending=True, stable=True).indices[..., :top]
+    got = gbla.token_logprobs(x, top=top)
+    assert torch.equal(got["top_token"].long(), want)
+    bad = x.isnan().any(-1)
+    assert got["lse"][bad].isnan().all() and got["entropy"][bad].isnan().all() and got["top_logprob"][bad].isnan().all()

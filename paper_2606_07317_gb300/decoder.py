@@ -36,6 +36,13 @@ from . import gbla
 HISTORY = gbla.CONV_WIDTH - 1  # inputs before the current one that the Conv1D sees
 
 
+def _whole(t):
+    """t contiguous, at an address that the library takes (what autograd hands on may be a slice
+    of a larger gradient)."""
+    t = t.contiguous()
+    return t if t.data_ptr() % 16 == 0 else t.clone()
+
+
 class _Gradients(torch.autograd.Function):
     """What `compute` makes of the tensors: gradients, whose own derivative is an error.  (As
     plain results of a backward they would pass for constants under create_graph, and
@@ -67,8 +74,8 @@ class _NormRotate(torch.autograd.Function):
         options = ctx.options
 
         def compute(q, k, norm_q, norm_k, dqo, dko):
-            g = gbla.qk_norm_rotate_backward(q, k, norm_q, norm_k, rot, dqo.contiguous(),
-                                             dko.contiguous(), positions, seq_lens, **options)
+            g = gbla.qk_norm_rotate_backward(q, k, norm_q, norm_k, rot, _whole(dqo),
+                                             _whole(dko), positions, seq_lens, **options)
             return g["dq"], g["dk"], g["dnorm_q"], g["dnorm_k"]
 
         return None, *_Gradients.apply(compute, *tensors, dqo, dko), None, None, None
@@ -89,8 +96,8 @@ class _Attention(torch.autograd.Function):
         options = ctx.options
 
         def compute(q, k, v, state, do, dstate):
-            g = gbla.decay_attention_backward(q, k, v, log_decay, do.contiguous(), seq_lens, state,
-                                              dstate.contiguous(),
+            g = gbla.decay_attention_backward(q, k, v, log_decay, _whole(do), seq_lens, state,
+                                              _whole(dstate),
                                               return_dstate=state is not None, **options)
             return g["dq"], g["dk"], g["dv"], g.get("dstate")
 
@@ -114,8 +121,8 @@ class _DeltaAttention(torch.autograd.Function):
 
         def compute(q, k, v, log_decay, beta, state, do, dstate):
             g = gbla.delta_attention_backward(
-                q, k, v, log_decay, beta, do.contiguous(), seq_lens, state,
-                None if dstate is None else dstate.contiguous(), return_dstate=state is not None,
+                q, k, v, log_decay, beta, _whole(do), seq_lens, state,
+                None if dstate is None else _whole(dstate), return_dstate=state is not None,
                 **options)
             return (*(g["d" + n] for n in ("q", "k", "v", "log_decay", "beta")), g.get("dstate"))
 
@@ -145,7 +152,7 @@ class _TokenLogprobs(torch.autograd.Function):
         scale, dlogprob = ctx.scale, more[0] if tokens is not None else None
 
         def compute(logits, dlse, dentropy, dlogprob):
-            g = [None if t is None else t.contiguous() for t in (dlogprob, dentropy, dlse)]
+            g = [None if t is None else _whole(t) for t in (dlogprob, dentropy, dlse)]
             return (gbla.token_logprobs_backward(logits, lse, entropy, tokens, *g, scale=scale,
                                                  seq_lens=seq_lens),)
 

@@ -212,3 +212,15 @@ def test_answers(monkeypatch):
     head.candidates(y, 2, ruled_out=out, scale=0.5)
     assert seen["top"] == 2 and seen["scale"] == 0.5 and (seen["logits"][..., 4] == -torch.inf).all()
     assert torch.equal(seen["logits"][..., :4], head.logits(y)[..., :4])
+
+
+@pytest.mark.parametrize("form,at", [("delta", (8,)), ("delta state", (8, 9)), ("score", (6, 7, 8))])
+def test_incoming_gradients_of_any_place(lib, form, at):
+    """Results that go into one flat tensor: their gradients are slices of its gradient, whole
+    but at any address; the library gets them at those that it takes."""
+    results = _forms(_leaves(_inputs()))[form][0]()
+    flat = torch.cat([t for r in results for t in (r.new_zeros(1), r.flatten())])
+    (flat * torch.arange(flat.numel())).sum().backward()
+    name, args = lib.calls[-1]
+    assert name.endswith("_backward")
+    assert all(args[i] is not None and args[i] % 16 == 0 for i in at)

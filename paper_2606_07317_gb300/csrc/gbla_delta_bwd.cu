@@ -27,12 +27,10 @@ namespace {
 // not need A (sum_i P_ij d_i, and what the results and queries add to A') other warps form one
 // chunk ahead and leave in shared memory.  kOwn: what a segment adds to A, from zero and with
 // nothing written.
-template <typename T, int D, int kSolve>
+template <typename T, int D>
 struct ReverseShape {
-  using Rec = Record<T, kSolve, true>;
-  // (bf16 of three terms at D = 128: 64 columns would not fit into shared memory)
-  static constexpr bool kNarrow = sizeof(T) == 2 && D == 128 && kSolve == 3;
-  static constexpr int C = kChunkOf<T>, E = D < 64 ? D : kNarrow ? 32 : 64, kSplit = D / E;
+  using Rec = Record<T, D, true>;
+  static constexpr int C = kChunkOf<T>, E = D < 64 ? D : 64, kSplit = D / E;
   static constexpr int kCarry = E / 16, kThreads = 2 * kCarry * 32;
   static constexpr int kRow = pad_row<T>(D), kValRow = pad_row<T>(E);
   // bytes: keys, gates and T of a chunk; queries, d, gates and P of the one ahead
@@ -45,11 +43,11 @@ struct ReverseShape {
   static_assert(kBytes <= 227 * 1024, "shared memory of a block");
 };
 
-template <typename T, int D, int kTerms, int kSolve, bool kOwn>
-__global__ void __launch_bounds__(ReverseShape<T, D, kSolve>::kThreads)
+template <typename T, int D, int kTerms, bool kOwn>
+__global__ void __launch_bounds__(ReverseShape<T, D>::kThreads)
     reverse_kernel(const DeltaBackArgs p, const float *records, float *after, float *weights,
                    float *own, int nc, int seg, int count) {
-  using Sh = ReverseShape<T, D, kSolve>;
+  using Sh = ReverseShape<T, D>;
   using Rec = typename Sh::Rec;
   constexpr int C = Sh::C, E = Sh::E, kCarry = Sh::kCarry, kFetch = kCarry * 32;
   constexpr bool kSums = sizeof(T) == 4;
@@ -134,7 +132,7 @@ __global__ void __launch_bounds__(ReverseShape<T, D, kSolve>::kThreads)
         float x[kHalf][4] = {};
 #pragma unroll
         for (int i = half * kHalf; i < C / 8; ++i) {
-          const LeftTf32<kSolve, kSums> a(r[i]);
+          const auto a = Rec::M::template left<kSums>(r, i);
 #pragma unroll
           for (int j = 0; j < kHalf; ++j)
             if (half * kHalf + j <= i) a.times(x[j], Rec::M::load(Tm, i, half * kHalf + j));
@@ -174,11 +172,17 @@ __global__ void __launch_bounds__(ReverseShape<T, D, kSolve>::kThreads)
 #pragma unroll
         for (int m = 0; m < C / 16; ++m) {
           values_of<Sh::kValRow>(r[2 * m], r[2 * m + 1], ds, m, e0 - x0);
+          if constexpr (sizeof(T) == 2) {
+            const LeftBf16<1> a(r[2 * m], r[2 * m + 1]);  // exact
 #pragma unroll
-          for (int i = 0; i < 2; ++i) {
-            const LeftTf32<kSolve, kSums> a(r[2 * m + i]);
+            for (int j = 0; j <= 2 * m + 1; ++j) a.times(x[j], Rec::P::load(P, m, j));
+          } else {
 #pragma unroll
-            for (int j = 0; j <= 2 * m + i; ++j) a.times(x[j], Rec::P::load(P, 2 * m + i, j));
+            for (int i = 0; i < 2; ++i) {
+              const auto a = Rec::P::template left<kSums>(r, 2 * m + i);
+#pragma unroll
+              for (int j = 0; j <= 2 * m + i; ++j) a.times(x[j], Rec::P::load(P, 2 * m + i, j));
+            }
           }
         }
 #pragma unroll
@@ -343,12 +347,12 @@ __device__ __forceinline__ void store1(float *p, float x) { *p = x; }
 __device__ __forceinline__ void store1(__nv_bfloat16 *p, float x) { *p = __float2bfloat16_rn(x); }
 
 // O: the type dq and dk leave in (fp32 planes where heads are shared).
-template <typename T, typename O, int D, int kSolve>
+template <typename T, typename O, int D>
 __global__ void __launch_bounds__(GradShape<T, D>::kThreads)
     grads_kernel(const DeltaBackArgs p, const float *records, const float *states,
                  const float *misses, const float *after, const float *weights, O *dq, O *dk, int nc) {
   using Sh = GradShape<T, D>;
-  using Rec = Record<T, kSolve, true>;
+  using Rec = Record<T, D, true>;
   constexpr int C = Sh::C, kThreads = Sh::kThreads, kRow = Sh::kRow, kWide = Sh::kWide;
   constexpr int kMat = Sh::kMat, kWarps = Sh::kWarps, kG = sizeof(T) == 2 ? 1 : 3;
   extern __shared__ __align__(16) char raw[];
@@ -651,14 +655,14 @@ struct Layout {
   Segments segments;
 };
 template <typename T>
-Layout layout_of(const DeltaBackArgs &p, bool exact) {
+Layout layout_of(const DeltaBackArgs &p) {
   const DeltaArgs &a = p.f;
   constexpr int C = kChunkOf<T>;
   const size_t all = (size_t)a.B * a.H * chunks_of<T>(a);
   Layout l = {};
   size_t at = 0;
   auto take = [&](size_t &to, size_t floats) { to = at, at += (floats + 63) / 64 * 64; };
-  take(l.records, all * (exact || sizeof(T) == 4 ? Record<T, 3, true>::kFloats : Record<T, 1, true>::kFloats));
+  take(l.records, all * (a.D < 128 ? Record<T, 64, true>::kFloats : Record<T, 128, true>::kFloats));
   take(l.states, all * a.D * a.D);
   take(l.after, all * a.D * a.D);
   take(l.misses, all * C * a.D);
@@ -671,15 +675,16 @@ Layout layout_of(const DeltaBackArgs &p, bool exact) {
   l.total = at;
   return l;
 }
-// Terms: three where a state's gradient is a result.
+// States and their gradients meet keys and writes in three terms where a state's gradient is a
+// result.
 bool exact_back(const DeltaBackArgs &p) { return p.f.dtype == GBLA_FP32 || p.dstate_in; }
 
-template <typename T, typename O, int D, int kSolve>
+template <typename T, typename O, int D>
 cudaError_t grads_launch(const DeltaBackArgs &p, const Layout &l, float *s, O *dq, O *dk,
                          cudaStream_t st) {
   using Sh = GradShape<T, D>;
   const int nc = chunks_of<T>(p.f);
-  const auto kernel = grads_kernel<T, O, D, kSolve>;
+  const auto kernel = grads_kernel<T, O, D>;
   cudaError_t e;
   if ((e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, Sh::kBytes)) !=
       cudaSuccess)
@@ -691,21 +696,21 @@ cudaError_t grads_launch(const DeltaBackArgs &p, const Layout &l, float *s, O *d
                     (const float *)(s + l.weights), dq, dk, nc);
 }
 
-template <typename T, int D, int kTerms, int kSolve>
+template <typename T, int D, int kTerms>
 cudaError_t back_launch(const DeltaBackArgs &p, float *s, cudaStream_t st) {
-  using Sh = ReverseShape<T, D, kSolve>;
+  using Sh = ReverseShape<T, D>;
   const DeltaArgs &a = p.f;
-  const Layout l = layout_of<T>(p, kSolve == 3);
+  const Layout l = layout_of<T>(p);
   const int nc = chunks_of<T>(a);
   cudaError_t e;
-  if ((e = save_forward(a, l.segments, kSolve == 3, s + l.records, s + l.states, s + l.misses,
+  if ((e = save_forward(a, l.segments, kTerms == 3, s + l.records, s + l.states, s + l.misses,
                         s + l.before, s + l.moves, st)) != cudaSuccess)
     return e;
   const Segments &g = l.segments;
   const float *records = s + l.records;
   const dim3 grid(a.H * Sh::kSplit, a.B, g.count), block(Sh::kThreads);
   if (g.count > 1) {
-    const auto own = reverse_kernel<T, D, kTerms, kSolve, true>;
+    const auto own = reverse_kernel<T, D, kTerms, true>;
     if ((e = cudaFuncSetAttribute(own, cudaFuncAttributeMaxDynamicSharedMemorySize, Sh::kBytes)) !=
         cudaSuccess)
       return e;
@@ -713,10 +718,9 @@ cudaError_t back_launch(const DeltaBackArgs &p, float *s, cudaStream_t st) {
     if ((e = launch_pdl(own, grid, block, Sh::kBytes, st, p, records, (float *)nullptr,
                         (float *)nullptr, s + l.own, nc, g.chunks, g.count)) != cudaSuccess)
       return e;
-    if ((e = join_back(a, g, kSolve == 3, p.dstate, s + l.own, s + l.moves, st)) != cudaSuccess)
-      return e;
+    if ((e = join_back(a, g, p.dstate, s + l.own, s + l.moves, st)) != cudaSuccess) return e;
   }
-  const auto reverse = reverse_kernel<T, D, kTerms, kSolve, false>;
+  const auto reverse = reverse_kernel<T, D, kTerms, false>;
   if ((e = cudaFuncSetAttribute(reverse, cudaFuncAttributeMaxDynamicSharedMemorySize, Sh::kBytes)) !=
       cudaSuccess)
     return e;
@@ -724,17 +728,17 @@ cudaError_t back_launch(const DeltaBackArgs &p, float *s, cudaStream_t st) {
   if ((e = launch_pdl(reverse, grid, block, Sh::kBytes, st, p, records, s + l.after, s + l.weights,
                       s + l.own, nc, g.chunks, g.count)) != cudaSuccess)
     return e;
-  if (a.H == a.Hk) return grads_launch<T, T, D, kSolve>(p, l, s, (T *)p.dq, (T *)p.dk, st);
+  if (a.H == a.Hk) return grads_launch<T, T, D>(p, l, s, (T *)p.dq, (T *)p.dk, st);
   float *dq = s + l.dq, *dk = s + l.dk;
-  if ((e = grads_launch<T, float, D, kSolve>(p, l, s, dq, dk, st)) != cudaSuccess) return e;
+  if ((e = grads_launch<T, float, D>(p, l, s, dq, dk, st)) != cudaSuccess) return e;
   return sum_shared_heads(dq, dk, p.dq, p.dk, (long long)a.B * a.N, a.Hk, a.H / a.Hk, D, a.dtype, st);
 }
 
 template <int D>
 cudaError_t back_d(const DeltaBackArgs &p, float *s, cudaStream_t st) {
-  if (p.f.dtype == GBLA_FP32) return back_launch<float, D, 3, 3>(p, s, st);
-  if (exact_back(p)) return back_launch<__nv_bfloat16, D, 3, 3>(p, s, st);
-  return back_launch<__nv_bfloat16, D, 2, 1>(p, s, st);
+  if (p.f.dtype == GBLA_FP32) return back_launch<float, D, 3>(p, s, st);
+  if (exact_back(p)) return back_launch<__nv_bfloat16, D, 3>(p, s, st);
+  return back_launch<__nv_bfloat16, D, 2>(p, s, st);
 }
 
 }  // namespace
@@ -742,8 +746,7 @@ cudaError_t back_d(const DeltaBackArgs &p, float *s, cudaStream_t st) {
 
 size_t delta_backward_floats(const DeltaBackArgs &p) {
   using namespace delta;
-  return (p.f.dtype == GBLA_FP32 ? layout_of<float>(p, true)
-                                 : layout_of<__nv_bfloat16>(p, exact_back(p))).total;
+  return p.f.dtype == GBLA_FP32 ? layout_of<float>(p).total : layout_of<__nv_bfloat16>(p).total;
 }
 
 cudaError_t delta_backward(const DeltaBackArgs &p, float *scratch, cudaStream_t st) {

@@ -96,16 +96,16 @@ __device__ __forceinline__ TwoFloat sum_of(const TwoFloat &a, const TwoFloat &b)
 
 // Parts of C x C matrices in shared memory (rows of C + 4 floats) as operands: 16 rows from i on
 // at columns j .. j + 7 on the left, columns j .. j + 7 of rows i .. i + 7 on the right.
-template <int C, int kTerms>
-__device__ __forceinline__ LeftTf32<kTerms> left_of(const float *m, int i, int j) {
+template <int C>
+__device__ __forceinline__ LeftTf32<3> left_of(const float *m, int i, int j) {
   const int g = (threadIdx.x & 31) >> 2, t = threadIdx.x & 3;
   const float2 x = *(const float2 *)(m + (i + g) * (C + 4) + j + 2 * t);
   const float2 y = *(const float2 *)(m + (i + g + 8) * (C + 4) + j + 2 * t);
   const float c[4] = {x.x, x.y, y.x, y.y};
-  return LeftTf32<kTerms>(c);
+  return LeftTf32<3>(c);
 }
-template <int C, int kTerms>
-__device__ __forceinline__ void times_right(float (&c)[4], const LeftTf32<kTerms> &a,
+template <int C>
+__device__ __forceinline__ void times_right(float (&c)[4], const LeftTf32<3> &a,
                                             const float *m, int i, int j) {
   const int g = (threadIdx.x & 31) >> 2, t = threadIdx.x & 3;
   const float *at = m + (i + 2 * t) * (C + 4) + j + g;
@@ -115,10 +115,10 @@ __device__ __forceinline__ void times_right(float (&c)[4], const LeftTf32<kTerms
 // to = (1 + A)^-1 for strictly lower triangular A, on and below its diagonal blocks of 16.
 // Those by forward substitution, the rest from
 //   (1 + A)^-1 = [ M0 0; -M1 A10 M0 M1 ]
-// for pairs of blocks of 16 and then of 32, in tf32 products of as many terms as the inverse is
-// used in.  (No powers of A, which grow where the inverse does not: keys that repeat.)  Begins and ends with all of A, and
-// of `to`, visible to the block.
-template <int C, int kTerms>
+// for pairs of blocks of 16 and then of 32, in tf32 products of three terms.  (No powers of A,
+// which grow where the inverse does not: keys that repeat.)  Begins and ends with all of A, and of
+// `to`, visible to the block.
+template <int C>
 __device__ __forceinline__ void invert(float *to, const float *A, int w) {
   constexpr int kMat = C + 4;
   const int lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
@@ -150,15 +150,15 @@ __device__ __forceinline__ void invert(float *to, const float *A, int w) {
     float z[2][4] = {}, y[2][4] = {};
 #pragma unroll
     for (int k = 0; k < 2; ++k) {
-      const auto a = left_of<C, kTerms>(to, i, i + 8 * k);
+      const auto a = left_of<C>(to, i, i + 8 * k);
 #pragma unroll
-      for (int n = 0; n < 2; ++n) times_right<C, kTerms>(z[n], a, A, i + 8 * k, j + 8 * n);
+      for (int n = 0; n < 2; ++n) times_right<C>(z[n], a, A, i + 8 * k, j + 8 * n);
     }
 #pragma unroll
     for (int k = 0; k < 2; ++k) {
-      const LeftTf32<kTerms> a(z[k]);
+      const LeftTf32<3> a(z[k]);
 #pragma unroll
-      for (int n = 0; n < 2; ++n) times_right<C, kTerms>(y[n], a, to, j + 8 * k, j + 8 * n);
+      for (int n = 0; n < 2; ++n) times_right<C>(y[n], a, to, j + 8 * k, j + 8 * n);
     }
     put(y[0], i, j), put(y[1], i, j + 8);
   }
@@ -170,16 +170,16 @@ __device__ __forceinline__ void invert(float *to, const float *A, int w) {
 #pragma unroll
     for (int k = 0; k < 4; ++k)
       if (k < 2 || (w & 1)) {
-        const auto a = left_of<C, kTerms>(to, i, 32 + 8 * k);
+        const auto a = left_of<C>(to, i, 32 + 8 * k);
 #pragma unroll
-        for (int n = 0; n < 4; ++n) times_right<C, kTerms>(z[n], a, A, 32 + 8 * k, 8 * n);
+        for (int n = 0; n < 4; ++n) times_right<C>(z[n], a, A, 32 + 8 * k, 8 * n);
       }
 #pragma unroll
     for (int k = 0; k < 4; ++k)
       if (k >= 2 || j == 0) {
-        const LeftTf32<kTerms> a(z[k]);
+        const LeftTf32<3> a(z[k]);
 #pragma unroll
-        for (int n = 0; n < 2; ++n) times_right<C, kTerms>(y[n], a, to, 8 * k, j + 8 * n);
+        for (int n = 0; n < 2; ++n) times_right<C>(y[n], a, to, 8 * k, j + 8 * n);
       }
     put(y[0], i, j), put(y[1], i, j + 8);
     __syncthreads();
@@ -187,11 +187,11 @@ __device__ __forceinline__ void invert(float *to, const float *A, int w) {
 }
 
 // One chunk of head h of sequence b, n of its tokens there; ends without a barrier.
-template <typename T, int D, int kSolve, bool kBack>
+template <typename T, int D, bool kBack>
 __device__ __forceinline__ void prepare_chunk(const DeltaArgs &p, char *raw, float *rec, int h,
                                               int b, int t0, int n) {
   using Sh = PrepShape<T, D>;
-  using Rec = Record<T, kSolve, kBack>;
+  using Rec = Record<T, D, kBack>;
   constexpr int C = Sh::C, kThreads = Sh::kThreads, kRow = Sh::kRow, kMat = Sh::kMat;
   T *ks = (T *)raw, *qs = ks + C * kRow;
   float *A = (float *)(raw + Sh::kFirst), *inv = (float *)raw;
@@ -250,7 +250,7 @@ __device__ __forceinline__ void prepare_chunk(const DeltaArgs &p, char *raw, flo
   rows_times_keys<D, C>(kk, qk, ks, qs, w);
   if (kBack) __syncthreads();  // P takes their place
   const float hr = hi[i0], lr = lo[i0];
-  float row[2];
+  float row[2], pair[2][4];  // (pair: a row's two values of P in two adjacent tiles)
 #pragma unroll
   for (int half = 0; half < 2; ++half) {
     const int i = i0 + g + 8 * half;
@@ -284,33 +284,44 @@ __device__ __forceinline__ void prepare_chunk(const DeltaArgs &p, char *raw, flo
       *(float2 *)(A + i * kMat + j) = make_float2(x0 * bj.x, x1 * bj.y);
       const float p0 = p.scale * qk[m][2 * half] * f[half][0];
       const float p1 = p.scale * qk[m][2 * half + 1] * f[half][1];
-      if (kBack)
+      if constexpr (kBack) {
         *(float2 *)(inv + i * kMat + j) = make_float2(p0, p1);
-      else if (2 * w + half >= m)
+      } else if constexpr (sizeof(T) == 2) {
+        pair[half][m % 2 * 2] = p0, pair[half][m % 2 * 2 + 1] = p1;
+        if (m % 2 == 1) Rec::P::store(rec + Rec::kP, 2 * w + half, m / 2, pair[half]);
+      } else if (2 * w + half >= m) {
         Rec::P::store(rec + Rec::kP, 2 * w + half, m, p0, p1);
+      }
     }
   }
   __syncthreads();
   // a matrix in shared memory, tile by tile: as it is, or (flip) for sums over its rows; the
   // backward's inverses without their diagonal of 1 (that part of a product needs no rounding),
   // the forward's multiplied by beta
-  auto put = [&](float *to, auto tiles, bool flip, bool inverse) {
-    using Form = decltype(tiles);
+  auto put = [&](float *to, bool flip, bool inverse) {
     for (int m = w; m < C / 8; m += Sh::kWarps)
       for (int j = 0; j <= m; ++j) {
         const float *at = inv + (8 * m + (flip ? 2 * t : g)) * kMat + 8 * j + (flip ? g : 2 * t);
         const bool one = inverse && kBack && j == m;
         const float by = inverse && !kBack ? beta[8 * m + g] : 1.f;
-        Form::store(to, m, j, one && g == 2 * t ? 0.f : by * at[0],
-                    one && g == 2 * t + 1 ? 0.f : by * at[flip ? kMat : 1]);
+        Rec::M::store(to, m, j, one && g == 2 * t ? 0.f : by * at[0],
+                      one && g == 2 * t + 1 ? 0.f : by * at[flip ? kMat : 1]);
       }
   };
   if (kBack) {
-    put(rec + Rec::kP, typename Rec::P{}, true, false);
+    if constexpr (sizeof(T) == 2) {  // 16 rows a warp
+      for (int j = 0; j < 2 * w + 2; ++j) {
+        const float *at = inv + (16 * w + 2 * t) * kMat + 8 * j + g;
+        const float x[4] = {at[0], at[kMat], at[8 * kMat], at[9 * kMat]};
+        Rec::P::store(rec + Rec::kP, w, j, x);
+      }
+    } else {
+      put(rec + Rec::kP, true, false);
+    }
     __syncthreads();
   }
-  invert<C, kSolve>(inv, A, w);
-  put(rec + Rec::kM, typename Rec::M{}, false, true);
+  invert<C>(inv, A, w);
+  put(rec + Rec::kM, false, true);
   if (kBack) {  // (1 + beta X)^-1: the rows weighted in place of the columns
     __syncthreads();
 #pragma unroll
@@ -324,12 +335,12 @@ __device__ __forceinline__ void prepare_chunk(const DeltaArgs &p, char *raw, flo
       }
     }
     __syncthreads();
-    invert<C, kSolve>(inv, A, w);
-    put(rec + Rec::kT, typename Rec::M{}, true, true);
+    invert<C>(inv, A, w);
+    put(rec + Rec::kT, true, true);
   }
 }
 
-template <typename T, int D, int kSolve, bool kBack>
+template <typename T, int D, bool kBack>
 __global__ void __launch_bounds__(PrepShape<T, D>::kThreads, PrepShape<T, D>::kBlocks)
     prepare_kernel(const DeltaArgs p, float *records, int nc, int each) {
   constexpr int C = PrepShape<T, D>::C;
@@ -340,9 +351,9 @@ __global__ void __launch_bounds__(PrepShape<T, D>::kThreads, PrepShape<T, D>::kB
   const int first = blockIdx.x * each, end = min(first + each, (L + C - 1) / C);
   for (int c = first; c < end; ++c) {
     if (c > first) __syncthreads();  // the chunk before is done with
-    prepare_chunk<T, D, kSolve, kBack>(
-        p, raw, records + (((size_t)b * p.H + h) * nc + c) * Record<T, kSolve, kBack>::kFloats, h, b,
-        c * C, min(C, L - c * C));
+    prepare_chunk<T, D, kBack>(
+        p, raw, records + (((size_t)b * p.H + h) * nc + c) * Record<T, D, kBack>::kFloats, h, b, c * C,
+        min(C, L - c * C));
   }
 }
 
@@ -359,17 +370,14 @@ __global__ void __launch_bounds__(PrepShape<T, D>::kThreads, PrepShape<T, D>::kB
 // it, from the identity and with no values.
 enum Purpose { kResults, kSave, kSegment };
 
-template <typename T, int D, int kSolve, Purpose kFor>
+template <typename T, int D, int kTerms, Purpose kFor>
 struct ScanShape {
-  using Rec = Record<T, kSolve, kFor == kSave>;
-  // (bf16 results of three terms at D = 128: what 64 columns hand on and the larger M would
-  // not fit into shared memory)
-  static constexpr bool kNarrow = sizeof(T) == 2 && D == 128 && kSolve == 3 && kFor == kResults;
-  static constexpr int C = kChunkOf<T>, E = D < 64 ? D : kNarrow ? 32 : 64, kSplit = D / E;
+  using Rec = Record<T, D, kFor == kSave>;
+  static constexpr int C = kChunkOf<T>, E = D < 64 ? D : 64, kSplit = D / E;
   // (without results the other warps only fetch, half as many do, and two blocks fit an SM)
   static constexpr int kCarry = E / 16, kHelp = kFor != kResults && kCarry > 2 ? 2 : kCarry;
   static constexpr int kThreads = (kCarry + kHelp) * 32;
-  static constexpr int kBlocks = kFor != kResults && (D < 128 || kSolve == 1) ? 2 : 1;
+  static constexpr int kBlocks = kFor != kResults && (D < 128 || kTerms == 2) ? 2 : 1;
   static constexpr int kRow = pad_row<T>(D), kValRow = pad_row<T>(E);
   // bytes: keys, values, M and gates of a chunk; queries, P and gates of the one before
   static constexpr int kKeys = C * kRow * (int)sizeof(T), kVals = C * kValRow * (int)sizeof(T);
@@ -382,21 +390,20 @@ struct ScanShape {
 };
 
 // kTerms: bf16 numbers that stand for a value of the state where it meets a key or takes a
-// write (fp32: 3 tf32 products); kSolve: terms of the product with M.
+// write (fp32: 3 tf32 products).
 // Segments have `seg` chunks; `before` holds the states after all but the last, or takes what
 // kSegment forms, the matrices in `moves`, [B H][count][D][D] both.  Records are `stride` floats
 // apart (their M and gates lie at the same place in both forms).
 // kFold: M comes multiplied by beta (the forward pass's records) and gives u at once; else
 // without its diagonal of 1, and gives the misses.
-template <typename T, int D, int kTerms, int kSolve, Purpose kFor, bool kFold>
-__global__ void __launch_bounds__(ScanShape<T, D, kSolve, kFor>::kThreads,
-                                  ScanShape<T, D, kSolve, kFor>::kBlocks)
+template <typename T, int D, int kTerms, Purpose kFor, bool kFold>
+__global__ void __launch_bounds__(ScanShape<T, D, kTerms, kFor>::kThreads,
+                                  ScanShape<T, D, kTerms, kFor>::kBlocks)
     scan_kernel(const DeltaArgs p, const float *records, float *states, float *misses,
                 float *before, float *moves, int nc, int seg, int count, int stride) {
-  using Sh = ScanShape<T, D, kSolve, kFor>;
+  using Sh = ScanShape<T, D, kTerms, kFor>;
   using Rec = typename Sh::Rec;
   constexpr int C = Sh::C, E = Sh::E, kCarry = Sh::kCarry, kFetch = Sh::kHelp * 32;
-  constexpr int kOut = sizeof(T) == 2 ? 1 : 3;  // terms of the product with P
   constexpr bool kSums = sizeof(T) == 4;
   constexpr int kColumns = kFor == kSegment ? 2 * Sh::kSplit : Sh::kSplit;  // blocks a head
   extern __shared__ __align__(16) char raw[];
@@ -493,7 +500,7 @@ __global__ void __launch_bounds__(ScanShape<T, D, kSolve, kFor>::kThreads,
         float x[kHalf][4] = {};
 #pragma unroll
         for (int j = 0; j < (half + 1) * kHalf; ++j) {
-          const LeftTf32<kSolve, kSums> a(r[j]);
+          const auto a = Rec::M::template left<kSums>(r, j);
 #pragma unroll
           for (int m = 0; m < kHalf; ++m)
             if (half * kHalf + m >= j) a.times(x[m], Rec::M::load(M, half * kHalf + m, j));
@@ -538,14 +545,21 @@ __global__ void __launch_bounds__(ScanShape<T, D, kSolve, kFor>::kThreads,
             const float ux = up.x * p.scale, uy = up.y * p.scale;
             o[j][0] *= ux, o[j][1] *= uy, o[j][2] *= ux, o[j][3] *= uy;
           }
+          constexpr int kWide = Rec::P::kWide;
 #pragma unroll
-          for (int j = 0; j < C / 8; ++j) {
-            const float4 v = us[j * 32];
-            const float u[4] = {v.x, v.y, v.z, v.w};
-            const LeftTf32<kOut, kSums> a(u);
+          for (int j = 0; j < C / 8 / kWide; ++j) {
+            float u[kWide][4];
 #pragma unroll
-            for (int m = j; m < C / 8; ++m) a.times(o[m], Rec::P::load(P, m, j));
-            store_tile(og, orow, o[j], 8 * j, n);  // no later u meets it
+            for (int i = 0; i < kWide; ++i) {
+              const float4 v = us[(j * kWide + i) * 32];
+              u[i][0] = v.x, u[i][1] = v.y, u[i][2] = v.z, u[i][3] = v.w;
+            }
+            const auto a = Rec::P::template left<kSums>(u, 0);
+#pragma unroll
+            for (int m = j * kWide; m < C / 8; ++m) a.times(o[m], Rec::P::load(P, m, j));
+#pragma unroll
+            for (int i = j * kWide; i < (j + 1) * kWide; ++i)
+              store_tile(og, orow, o[i], 8 * i, n);  // no later u meets it
           }
         }
       cp_async_wait_all();
@@ -561,14 +575,13 @@ __global__ void __launch_bounds__(ScanShape<T, D, kSolve, kFor>::kThreads,
 }
 
 // --------------------------------------------------------------- between segments
-// A block takes E of the state's columns of one (batch, head).  kTerms: three where a state is a
-// result, else one (a state is rounded to 2^-11 once a segment).
+// A block takes E of the state's columns of one (batch, head).
 template <int D>
 struct JoinShape {
   static constexpr int E = D < 64 ? D : 64, kThreads = E * 2, kRow = D + 8;
   static constexpr int kBytes = 2 * D * kRow * 4;
 };
-template <int D, bool kBack, int kTerms>
+template <int D, bool kBack>
 __global__ void __launch_bounds__(JoinShape<D>::kThreads)
     join_kernel(const float *init, const int32_t *seq_lens, float *own, const float *moves, int N,
                 int H, int tokens, int count) {
@@ -603,7 +616,7 @@ __global__ void __launch_bounds__(JoinShape<D>::kThreads)
     const float *m = tile + (i & 1) * D * kRow;
 #pragma unroll
     for (int k = 0; k < D / 8; ++k) {
-      const LeftTf32<kTerms> a(S[k]);
+      const LeftTf32<3> a(S[k]);
 #pragma unroll
       for (int n = 0; n < D / 8; ++n) {
         if (kBack) {
@@ -623,7 +636,8 @@ __global__ void __launch_bounds__(JoinShape<D>::kThreads)
   }
 }
 
-// Terms of the product with M: bf16 results alone need one (2^-11 of what M adds to a miss).
+// Where a state is a result it meets keys and writes in three terms; bf16 results alone need two
+// (2^-16, beside 2^-8 of their own rounding).
 bool exact_state(const DeltaArgs &a) { return a.dtype == GBLA_FP32 || a.fin; }
 
 int sm_count() {
@@ -639,11 +653,11 @@ cudaError_t allow_smem(K kernel, int bytes) {
   return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
 }
 
-template <int D, bool kBack, int kTerms>
+template <int D, bool kBack>
 cudaError_t join_launch(const DeltaArgs &a, const Segments &g, const float *init, float *own,
                         const float *moves, cudaStream_t st) {
   using Jo = JoinShape<D>;
-  const auto join = join_kernel<D, kBack, kTerms>;
+  const auto join = join_kernel<D, kBack>;
   cudaError_t e;
   if ((e = allow_smem(join, Jo::kBytes)) != cudaSuccess) return e;
   const int C = a.dtype == GBLA_FP32 ? kChunkOf<float> : kChunkOf<__nv_bfloat16>;
@@ -652,16 +666,16 @@ cudaError_t join_launch(const DeltaArgs &a, const Segments &g, const float *init
                     a.seq_lens, own, moves, a.N, a.H, g.chunks * C, g.count);
 }
 
-template <typename T, int D, int kTerms, int kSolve, Purpose kFor>
+template <typename T, int D, int kTerms, Purpose kFor>
 cudaError_t launch(const DeltaArgs &a, const Segments &g, float *records, float *states,
                    float *misses, float *before, float *moves, cudaStream_t st) {
   using Pr = PrepShape<T, D>;
-  using Sc = ScanShape<T, D, kSolve, kFor>;
-  using Se = ScanShape<T, D, kSolve, kSegment>;
+  using Sc = ScanShape<T, D, kTerms, kFor>;
+  using Se = ScanShape<T, D, kTerms, kSegment>;
   static_assert(kFor != kSegment, "");
-  const int nc = chunks_of<T>(a), stride = Record<T, kSolve, kFor == kSave>::kFloats;
+  const int nc = chunks_of<T>(a), stride = Record<T, D, kFor == kSave>::kFloats;
   cudaError_t e;
-  const auto prep = prepare_kernel<T, D, kSolve, kFor == kSave>;
+  const auto prep = prepare_kernel<T, D, kFor == kSave>;
   if ((e = allow_smem(prep, Pr::kBytes)) != cudaSuccess) return e;
   const int each = a.seq_lens && (long long)nc * a.H * a.B >= 64ll * sm_count() ? 4 : 1;
   count_launch();
@@ -669,7 +683,7 @@ cudaError_t launch(const DeltaArgs &a, const Segments &g, float *records, float 
                       st, a, records, nc, each)) != cudaSuccess)
     return e;
   if (g.count > 1) {
-    const auto own = scan_kernel<T, D, kTerms, kSolve, kSegment, kFor == kResults>;
+    const auto own = scan_kernel<T, D, kTerms, kSegment, kFor == kResults>;
     if ((e = allow_smem(own, Se::kBytes)) != cudaSuccess) return e;
     count_launch();
     // (the backward pass moves its gradients by the last segment's matrix too)
@@ -678,10 +692,9 @@ cudaError_t launch(const DeltaArgs &a, const Segments &g, float *records, float 
                         (float *)nullptr, (float *)nullptr, before, moves, nc, g.chunks, g.count,
                         stride)) != cudaSuccess)
       return e;
-    if ((e = join_launch<D, false, kSolve>(a, g, a.init, before, moves, st)) != cudaSuccess)
-      return e;
+    if ((e = join_launch<D, false>(a, g, a.init, before, moves, st)) != cudaSuccess) return e;
   }
-  const auto scan = scan_kernel<T, D, kTerms, kSolve, kFor, kFor == kResults>;
+  const auto scan = scan_kernel<T, D, kTerms, kFor, kFor == kResults>;
   if ((e = allow_smem(scan, Sc::kBytes)) != cudaSuccess) return e;
   count_launch();
   return launch_pdl(scan, dim3(Sc::kSplit * a.H, a.B, g.count), dim3(Sc::kThreads), Sc::kBytes, st,
@@ -693,32 +706,33 @@ template <int D>
 cudaError_t forward_d(const DeltaArgs &a, const Segments &g, float *rec, float *before, float *moves,
                       cudaStream_t st) {
   if (a.dtype == GBLA_FP32)
-    return launch<float, D, 3, 3, kResults>(a, g, rec, nullptr, nullptr, before, moves, st);
+    return launch<float, D, 3, kResults>(a, g, rec, nullptr, nullptr, before, moves, st);
   if (exact_state(a))
-    return launch<__nv_bfloat16, D, 3, 3, kResults>(a, g, rec, nullptr, nullptr, before, moves, st);
-  return launch<__nv_bfloat16, D, 2, 1, kResults>(a, g, rec, nullptr, nullptr, before, moves, st);
+    return launch<__nv_bfloat16, D, 3, kResults>(a, g, rec, nullptr, nullptr, before, moves, st);
+  return launch<__nv_bfloat16, D, 2, kResults>(a, g, rec, nullptr, nullptr, before, moves, st);
 }
 template <int D>
 cudaError_t save_d(const DeltaArgs &a, const Segments &g, bool exact, float *rec, float *states,
                    float *misses, float *before, float *moves, cudaStream_t st) {
   if (a.dtype == GBLA_FP32)
-    return launch<float, D, 3, 3, kSave>(a, g, rec, states, misses, before, moves, st);
+    return launch<float, D, 3, kSave>(a, g, rec, states, misses, before, moves, st);
   if (exact)
-    return launch<__nv_bfloat16, D, 3, 3, kSave>(a, g, rec, states, misses, before, moves, st);
-  return launch<__nv_bfloat16, D, 2, 1, kSave>(a, g, rec, states, misses, before, moves, st);
+    return launch<__nv_bfloat16, D, 3, kSave>(a, g, rec, states, misses, before, moves, st);
+  return launch<__nv_bfloat16, D, 2, kSave>(a, g, rec, states, misses, before, moves, st);
 }
 
 }  // namespace
 
 // How many segments.  In units of a chunk in a scan of whole sequences (measured, bf16 D = 64:
-// 2.0 us, 2.9 with states of full precision): a round of blocks takes a segment's chunks; the scan
+// 2.4 us, 2.8 with states of full precision): a round of blocks takes a segment's chunks; the scan
 // that forms the segments' own states and matrices has twice the blocks, two an SM, and as much
 // for a round of these; 0.6 where there is one an SM, which pays neither with states of full
-// precision at D = 128 (B4 H8 N2048 200 us, 125 whole) nor in fp32 (B8 H8 N2048 D64 270 and 241)
-// nor for the backward's three further passes (the same in bf16 302 and 287); a segment that is
+// precision at D = 128 nor in fp32 nor for the backward's three further passes; a segment that is
 // joined 1.2.
-// B2 H8 N32768: 1 segment 1059 us, 4 474, 9 319, 19 329; B8 H8 N2048, states out: 1 119, 2 112,
-// 4 130.
+// Any count and the rule's: B2 H8 N32768: 1 segment 1338 us, 4 599, 8 437, 9 404 (taken), 10 469,
+// 19 411; the same at D = 128, N8192: 1 464, 3 313 (taken), 4 307, 6 377; at D = 32: 1 185, 9 83
+// (taken), 12 96; B8 H8 N2048, states out: 1 117, 2 107 (taken), 3 133; without: 106, 97, 119;
+// backward B4 H8 N8192: 1 939, 4 661 (taken), 9 654; fp32 B3 H6 N517: 1 139, 4 117, 6 104 (taken).
 Segments segments_of(const DeltaArgs &a, bool back) {
   const int nc = a.dtype == GBLA_FP32 ? chunks_of<float>(a) : chunks_of<__nv_bfloat16>(a);
   const long long blocks = (long long)a.B * a.H * (a.D > 64 ? 2 : 1), sms = sm_count();
@@ -743,16 +757,11 @@ cudaError_t save_forward(const DeltaArgs &a, const Segments &g, bool exact, floa
   return save_d<128>(a, g, exact, rec, states, misses, before, moves, st);
 }
 
-cudaError_t join_back(const DeltaArgs &a, const Segments &g, bool exact, const float *init,
-                      float *own, const float *moves, cudaStream_t st) {
-  if (a.D == 32)
-    return exact ? join_launch<32, true, 3>(a, g, init, own, moves, st)
-                 : join_launch<32, true, 1>(a, g, init, own, moves, st);
-  if (a.D == 64)
-    return exact ? join_launch<64, true, 3>(a, g, init, own, moves, st)
-                 : join_launch<64, true, 1>(a, g, init, own, moves, st);
-  return exact ? join_launch<128, true, 3>(a, g, init, own, moves, st)
-               : join_launch<128, true, 1>(a, g, init, own, moves, st);
+cudaError_t join_back(const DeltaArgs &a, const Segments &g, const float *init, float *own,
+                      const float *moves, cudaStream_t st) {
+  if (a.D == 32) return join_launch<32, true>(a, g, init, own, moves, st);
+  if (a.D == 64) return join_launch<64, true>(a, g, init, own, moves, st);
+  return join_launch<128, true>(a, g, init, own, moves, st);
 }
 
 }  // namespace delta
@@ -760,10 +769,9 @@ cudaError_t join_back(const DeltaArgs &a, const Segments &g, bool exact, const f
 static size_t record_floats(const DeltaArgs &a) {
   using namespace delta;
   const size_t bh = (size_t)a.B * a.H;
-  if (a.dtype == GBLA_FP32) return bh * chunks_of<float>(a) * Record<float, 3, false>::kFloats;
+  if (a.dtype == GBLA_FP32) return bh * chunks_of<float>(a) * Record<float, 128, false>::kFloats;
   return bh * chunks_of<__nv_bfloat16>(a) *
-         (exact_state(a) ? Record<__nv_bfloat16, 3, false>::kFloats
-                         : Record<__nv_bfloat16, 1, false>::kFloats);
+         (a.D < 128 ? Record<__nv_bfloat16, 64, false>::kFloats : Record<__nv_bfloat16, 128, false>::kFloats);
 }
 
 size_t delta_forward_floats(const DeltaArgs &a) {

@@ -56,10 +56,12 @@ __device__ __forceinline__ uint32_t tf32_of(float x) {
   asm("cvt.rna.tf32.f32 %0, %1;" : "=r"(r) : "f"(x));
   return r;
 }
-// x = hi + lo to 22 bits.
+// x = hi + lo to 23 bits: hi rounded by integer operations (B2 H8 N32768 D64 418 us, 449 with
+// conversion instructions), lo, which has at most 12 bits, cut off.  (A NaN may leave hi a number;
+// lo keeps it.)
 __device__ __forceinline__ void tf32_split(float x, uint32_t &hi, uint32_t &lo) {
-  hi = tf32_of(x);
-  lo = tf32_of(x - __uint_as_float(hi));
+  hi = (__float_as_uint(x) + 0x1000u) & 0xFFFFE000u;
+  lo = __float_as_uint(x - __uint_as_float(hi)) & 0xFFFFE000u;
 }
 
 // The left operand of tf32 products made of a result tile; kTerms 1: rounded to 11 bits,
@@ -114,7 +116,7 @@ struct LeftTf32 {
   }
 };
 // The left operand of bf16 products made of two result tiles, as kTerms bf16 numbers each
-// (8 kTerms bits); the right operand is exact in bf16.
+// (8 kTerms bits); the right operand is exact in bf16, or two bf16 numbers too.
 template <int kTerms>
 struct LeftBf16 {
   uint32_t part[kTerms][4];
@@ -132,6 +134,12 @@ struct LeftBf16 {
   __device__ __forceinline__ void times(float (&c)[4], uint32_t b0, uint32_t b1) const {
 #pragma unroll
     for (int p = kTerms - 1; p >= 0; --p) mma_bf16(c, part[p], b0, b1);
+  }
+  // (the product of the two small parts is left out: 2^-16)
+  __device__ __forceinline__ void times(float (&c)[4], const uint4 &b) const {
+    if constexpr (kTerms > 1) mma_bf16(c, part[1], b.x, b.y);
+    mma_bf16(c, part[0], b.z, b.w);
+    mma_bf16(c, part[0], b.x, b.y);
   }
 };
 
@@ -223,29 +231,65 @@ __device__ __forceinline__ PairBf16 by_channel(const __nv_bfloat16 *tile, int to
 }
 
 // ------------------------------------------------------------- what a chunk prepares
-// Lower triangular C x C matrices, as the right operands of tf32 products: tiles of 8 x 8 on
-// and below the diagonal, row by row of tiles, each with a uint2 (one term: rounded) or uint4
-// (three: two hi, two lo) a lane, so that a warp's loads lie side by side.
-template <int C, int kTerms>
-struct Tiles {
-  static constexpr int kLane = kTerms == 1 ? 2 : 4;  // floats
-  static constexpr int kTiles = (C / 8) * (C / 8 + 1) / 2, kFloats = kTiles * 32 * kLane;
-  using Word = std::conditional_t<kTerms == 1, uint2, uint4>;
+// Lower triangular C x C matrices as right operands, tile by tile on and below the diagonal, with a
+// vector a lane, so that a warp's loads lie side by side.
+//
+// In fp32, tiles of 8 x 8 for tf32 products of three terms: the triangular inverses.  Where keys are
+// alike and beta is near 2 their entries are near 2 and of either sign, and what they make of a
+// chunk's misses nearly cancels: in one tf32 number (2^-11) results were off by a tenth and more, in
+// two bf16 ones by up to 6e-3.  kSplit: stored as the products' two parts (B2 H8 N32768 D64 403 us,
+// 418 where each warp splits them), else split where they are used, in half the bytes: with bf16 at
+// D = 128 shared memory has no room for parts.
+template <int C, bool kSplit>
+struct Whole {
+  static constexpr int kWide = 1;  // result tiles that a left operand takes
+  static constexpr int kFloats = (C / 8) * (C / 8 + 1) / 2 * 32 * (kSplit ? 4 : 2);
   static __device__ __forceinline__ int at(int m, int j) {
     return (m * (m + 1) / 2 + j) * 32 + (threadIdx.x & 31);
   }
-  static __device__ __forceinline__ Word load(const float *base, int m, int j) {
-    return ((const Word *)base)[at(m, j)];
+  static __device__ __forceinline__ uint4 load(const float *base, int m, int j) {
+    if (kSplit) return ((const uint4 *)base)[at(m, j)];
+    const float2 x = ((const float2 *)base)[at(m, j)];
+    return parts(x.x, x.y);
+  }
+  static __device__ __forceinline__ uint4 parts(float x, float y) {
+    uint4 v;  // hi, hi, lo, lo
+    tf32_split(x, v.x, v.z);
+    tf32_split(y, v.y, v.w);
+    return v;
   }
   static __device__ __forceinline__ void store(float *base, int m, int j, float b0, float b1) {
-    if constexpr (kTerms == 1) {
-      ((uint2 *)base)[at(m, j)] = make_uint2(tf32_of(b0), tf32_of(b1));
-    } else {
-      uint4 v;  // hi, hi, lo, lo
-      tf32_split(b0, v.x, v.z);
-      tf32_split(b1, v.y, v.w);
-      ((uint4 *)base)[at(m, j)] = v;
-    }
+    if (kSplit) ((uint4 *)base)[at(m, j)] = parts(b0, b1);
+    else ((float2 *)base)[at(m, j)] = make_float2(b0, b1);
+  }
+  template <bool kSums, int kN>
+  static __device__ __forceinline__ LeftTf32<3, kSums> left(const float (&r)[kN][4], int j) {
+    return LeftTf32<3, kSums>(r[j]);
+  }
+};
+// As two bf16 numbers a value, for products of 16.  Summed over columns: 8 rows m by 16 columns j;
+// over rows (kRows): 16 rows m by 8 columns j.
+template <int C, bool kRows>
+struct Halves {
+  static constexpr int kWide = 2;
+  static constexpr int kFloats = (C / 16) * (C / 16 + 1) * 32 * 4;
+  static __device__ __forceinline__ int at(int m, int j) {
+    const int tile = kRows ? m * (m + 1) + j : (m / 2 + (m & 1)) * (m / 2 + 1) + j;
+    return tile * 32 + (threadIdx.x & 31);
+  }
+  static __device__ __forceinline__ uint4 load(const float *base, int m, int j) {
+    return ((const uint4 *)base)[at(m, j)];
+  }
+  // values at 2t, 2t + 1, 2t + 8 and 2t + 9 along the sum
+  static __device__ __forceinline__ void store(float *base, int m, int j, const float (&x)[4]) {
+    uint4 v = {f2_to_bf2(x[0], x[1]), f2_to_bf2(x[2], x[3]), 0, 0};
+    const float2 a = bf2_to_f2(v.x), b = bf2_to_f2(v.y);
+    v.z = f2_to_bf2(x[0] - a.x, x[1] - a.y), v.w = f2_to_bf2(x[2] - b.x, x[3] - b.y);
+    ((uint4 *)base)[at(m, j)] = v;
+  }
+  template <bool kSums, int kN>
+  static __device__ __forceinline__ LeftBf16<2> left(const float (&r)[kN][4], int j) {
+    return LeftBf16<2>(r[2 * j], r[2 * j + 1]);
   }
 };
 // Powers of a chunk's gates.
@@ -256,14 +300,15 @@ struct Gates {
   static constexpr int kFloats = 5 * C + 4;
 };
 
-// A chunk's record.  For the forward pass beta M, P and the powers of its gates, M in kSolve terms,
-// P in one where results are bf16.  For the backward pass (kBack) M - 1, and, for products that sum
-// over the row index, T - 1 with T = (1 + beta X)^-1, and P the other way round, in kSolve terms.
-template <typename T, int kSolve, bool kBack>
+// A chunk's record.  For the forward pass beta M, P and the powers of its gates.  For the backward
+// pass (kBack) M - 1, and, for products that sum over the row index, T - 1 with T = (1 + beta X)^-1,
+// and P the other way round.  The inverses in fp32; P, whose products nothing multiplies up, as two
+// bf16 numbers where results are bf16.
+template <typename T, int D, bool kBack>
 struct Record {
   static constexpr int C = kChunkOf<T>;
-  using M = Tiles<C, kSolve>;
-  using P = Tiles<C, kBack ? kSolve : sizeof(T) == 2 ? 1 : 3>;
+  using M = Whole<C, sizeof(T) == 4 || D < 128>;
+  using P = std::conditional_t<sizeof(T) == 2, Halves<C, kBack>, Whole<C, true>>;
   static constexpr int kM = 0, kGates = M::kFloats, kP = kGates + Gates<C>::kFloats;
   static constexpr int kT = kP + P::kFloats, kFloats = kT + (kBack ? M::kFloats : 0);
 };
@@ -480,14 +525,14 @@ struct Segments {
 Segments segments_of(const DeltaArgs &a, bool back);
 // First part of the backward pass: records (of the backward's form), the states before all
 // chunks and the misses, packed; `moves`: the matrices that segments move a state by.  exact:
-// three terms throughout.
+// states meet keys and writes in three terms.
 cudaError_t save_forward(const DeltaArgs &a, const Segments &g, bool exact, float *records,
                          float *states, float *misses, float *before, float *moves,
                          cudaStream_t st);
 // Turns what each segment adds to the gradient of the state into that before it, in place:
 // A' = move^T A + own, from the last segment on.
-cudaError_t join_back(const DeltaArgs &a, const Segments &g, bool exact, const float *init,
-                      float *own, const float *moves, cudaStream_t st);
+cudaError_t join_back(const DeltaArgs &a, const Segments &g, const float *init, float *own,
+                      const float *moves, cudaStream_t st);
 
 }  // namespace delta
 }  // namespace gbla

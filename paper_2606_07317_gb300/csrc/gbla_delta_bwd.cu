@@ -225,38 +225,81 @@ struct GradShape {
 __device__ __forceinline__ float2 pair_at(const float *p) { return *(const float2 *)p; }
 __device__ __forceinline__ float2 pair_at(const __nv_bfloat16 *p) { return bf2_to_f2(*(const uint32_t *)p); }
 
+// Two bf16 numbers that stand for a value, in its place: the larger part above.
+__device__ __forceinline__ void halves_of(uint32_t &a, uint32_t &b, float x, float y) {
+  const uint32_t hi = f2_to_bf2(x, y);
+  const float2 r = bf2_to_f2(hi);
+  const uint32_t lo = f2_to_bf2(x - r.x, y - r.y);
+  a = __byte_perm(lo, hi, 0x5410), b = __byte_perm(lo, hi, 0x7632);
+}
+// Those of a row's values at 2t, 2t + 1 and 8 further on, as operands of bf16 products: both large
+// parts, both small ones.
+__device__ __forceinline__ uint4 halves_at(const float *p) {
+  const uint2 x = *(const uint2 *)p, y = *(const uint2 *)(p + 8);
+  return make_uint4(__byte_perm(x.x, x.y, 0x7632), __byte_perm(y.x, y.y, 0x7632),
+                    __byte_perm(x.x, x.y, 0x5410), __byte_perm(y.x, y.y, 0x5410));
+}
+
 // What store_packed left of a kTiles * 8 x D matrix (rows: tiles; columns: 16 by 16): words
 // first, first + kThreads, ... of a thread, all in flight before the first is used, and into rows
-// of D + 8 floats, rounded for products of one term.
+// of D + 8 floats, or of as many pairs of bf16 numbers.
 template <int kThreads, int kN>
 __device__ __forceinline__ void fetch_packed(float4 (&v)[kN], const float *from, int first) {
 #pragma unroll
   for (int i = 0; i < kN; ++i) v[i] = __ldg((const float4 *)from + first + i * kThreads);
 }
-template <int D, int kTiles, int kTerms, int kThreads, int kN>
+template <int D, int kTiles, bool kHalves, int kThreads, int kN>
 __device__ __forceinline__ void spread(float *to, const float4 (&v)[kN], int first) {
 #pragma unroll
   for (int n = 0; n < kN; ++n) {
     const int i = first + n * kThreads, tile = i / 32, g = (i & 31) >> 2, t = i & 3;
-    float x[4] = {v[n].x, v[n].y, v[n].z, v[n].w};
-    if (kTerms == 1)
-#pragma unroll
-      for (int j = 0; j < 4; ++j) x[j] = __uint_as_float(tf32_of(x[j]));
-    float *at = to + (tile % kTiles * 8 + 2 * t) * (D + 8) + tile / kTiles * 16 + g;
+    uint32_t x[4] = {__float_as_uint(v[n].x), __float_as_uint(v[n].y), __float_as_uint(v[n].z),
+                     __float_as_uint(v[n].w)};
+    if (kHalves) halves_of(x[0], x[1], v[n].x, v[n].y), halves_of(x[2], x[3], v[n].z, v[n].w);
+    uint32_t *at = (uint32_t *)to + (tile % kTiles * 8 + 2 * t) * (D + 8) + tile / kTiles * 16 + g;
     at[0] = x[0], at[D + 8] = x[1], at[8] = x[2], at[D + 16] = x[3];
   }
 }
 
 // 16 rows from i on at columns k .. k + 7 of a tile, as the left operand of tf32 products; times
 // the rows' factors.
-template <int kTerms, int kRow, typename T>
-__device__ __forceinline__ LeftTf32<kTerms, kTerms == 3> left_rows(const T *tile, int i, int k, float fx = 1.f,
-                                                      float fy = 1.f) {
+template <int kRow>
+__device__ __forceinline__ LeftTf32<true> left_rows(const float *tile, int i, int k, float fx = 1.f,
+                                                    float fy = 1.f) {
   const int g = (threadIdx.x & 31) >> 2, t = threadIdx.x & 3;
   const float2 x = pair_at(tile + (i + g) * kRow + k + 2 * t);
   const float2 y = pair_at(tile + (i + g + 8) * kRow + k + 2 * t);
   const float c[4] = {fx * x.x, fx * x.y, fy * y.x, fy * y.y};
-  return LeftTf32<kTerms, kTerms == 3>(c);
+  return LeftTf32<true>(c);
+}
+// The same at columns k .. k + 15 for bf16 products, of fp32 rows (in two bf16 numbers), of rows
+// that are pairs of them, and of bf16 rows.
+template <int kRow>
+__device__ __forceinline__ LeftBf16<2> left_wide(const float *tile, int i, int k, float fx = 1.f,
+                                                 float fy = 1.f) {
+  const int g = (threadIdx.x & 31) >> 2, t = threadIdx.x & 3;
+  const float *p = tile + (i + g) * kRow + k + 2 * t, *q = p + 8 * kRow;
+  const float2 x = pair_at(p), y = pair_at(q), u = pair_at(p + 8), v = pair_at(q + 8);
+  const float c[4] = {fx * x.x, fx * x.y, fy * y.x, fy * y.y};
+  const float d[4] = {fx * u.x, fx * u.y, fy * v.x, fy * v.y};
+  return LeftBf16<2>(c, d);
+}
+template <int kRow>
+__device__ __forceinline__ LeftBf16<2> left_halves(const float *tile, int i, int k) {
+  const int g = (threadIdx.x & 31) >> 2, t = threadIdx.x & 3;
+  const uint4 a = halves_at(tile + (i + g) * kRow + k + 2 * t);
+  const uint4 b = halves_at(tile + (i + g + 8) * kRow + k + 2 * t);
+  LeftBf16<2> l;
+  l.part[0][0] = a.x, l.part[0][1] = b.x, l.part[0][2] = a.y, l.part[0][3] = b.y;
+  l.part[1][0] = a.z, l.part[1][1] = b.z, l.part[1][2] = a.w, l.part[1][3] = b.w;
+  return l;
+}
+template <int kRow>
+__device__ __forceinline__ LeftBf16<1> left_exact(const __nv_bfloat16 *tile, int i, int k) {
+  const int l = threadIdx.x & 31;
+  LeftBf16<1> r;
+  ldmatrix4(r.part[0], smem_u32(tile + (i + (l & 15)) * kRow + k + (l >> 4) * 8));
+  return r;
 }
 // x += (16 x 16 coefficients a, b) times rows i .. i + 15 of a raw tile.
 template <int D>
@@ -275,7 +318,7 @@ __device__ __forceinline__ void add_rows(float (&x)[D / 8][4], const float (&a)[
                                          const float (&b)[4], const float *tile, int i) {
   constexpr int kRow = pad_row<float>(D);
   const int g = (threadIdx.x & 31) >> 2, t = threadIdx.x & 3;
-  const LeftTf32<3, true> l0(a), l1(b);
+  const LeftTf32<true> l0(a), l1(b);
 #pragma unroll
   for (int d = 0; d < D / 8; ++d) {
     const float *at = tile + (i + 2 * t) * kRow + 8 * d + g;
@@ -292,14 +335,12 @@ __device__ __forceinline__ void score_tiles(float (&qk)[2][4], float (&kk)[2][4]
   const int l = threadIdx.x & 31;
 #pragma unroll
   for (int d = 0; d < D / 16; ++d) {
-    uint32_t a[4], c[4];
-    ldmatrix4(a, smem_u32(qs + (i + (l & 15)) * kRow + 16 * d + (l >> 4) * 8));
-    ldmatrix4(c, smem_u32(ks + (i + (l & 15)) * kRow + 16 * d + (l >> 4) * 8));
+    const auto a = left_exact<kRow>(qs, i, 16 * d), c = left_exact<kRow>(ks, i, 16 * d);
     const PairBf16 k = by_token<kRow>(ks, j, 16 * d);
 #pragma unroll
     for (int n = 0; n < 2; ++n) {
-      mma_bf16(qk[n], a, k.b[n][0], k.b[n][1]);
-      mma_bf16(kk[n], c, k.b[n][0], k.b[n][1]);
+      a.times(qk[n], k.b[n][0], k.b[n][1]);
+      c.times(kk[n], k.b[n][0], k.b[n][1]);
     }
   }
 }
@@ -310,7 +351,7 @@ __device__ __forceinline__ void score_tiles(float (&qk)[2][4], float (&kk)[2][4]
   const int g = (threadIdx.x & 31) >> 2, t = threadIdx.x & 3;
 #pragma unroll 2
   for (int d = 0; d < D / 8; ++d) {
-    const auto a = left_rows<3, kRow>(qs, i, 8 * d), c = left_rows<3, kRow>(ks, i, 8 * d);
+    const auto a = left_rows<kRow>(qs, i, 8 * d), c = left_rows<kRow>(ks, i, 8 * d);
 #pragma unroll
     for (int n = 0; n < 2; ++n) {
       const float2 k = *(const float2 *)(ks + (j + 8 * n + g) * kRow + 8 * d + 2 * t);
@@ -354,7 +395,8 @@ __global__ void __launch_bounds__(GradShape<T, D>::kThreads)
   using Sh = GradShape<T, D>;
   using Rec = Record<T, D, true>;
   constexpr int C = Sh::C, kThreads = Sh::kThreads, kRow = Sh::kRow, kWide = Sh::kWide;
-  constexpr int kMat = Sh::kMat, kWarps = Sh::kWarps, kG = sizeof(T) == 2 ? 1 : 3;
+  constexpr int kMat = Sh::kMat, kWarps = Sh::kWarps;
+  constexpr bool kHalves = sizeof(T) == 2;  // u and the states as two bf16 numbers
   extern __shared__ __align__(16) char raw[];
   T *ks = (T *)raw, *qs = (T *)(raw + Sh::kTile), *ds = (T *)(raw + 2 * Sh::kTile);
   float *us = (float *)(raw + 3 * Sh::kTile), *vs = us + C * kWide, *st = vs + C * kWide;
@@ -406,16 +448,16 @@ __global__ void __launch_bounds__(GradShape<T, D>::kThreads)
       fetch_packed<kThreads>(a, A1, tid);
       fetch_packed<kThreads>(kept, S0, tid);
     }
-    spread<D, C / 8, 3, kThreads>(us, m, tid);
-    spread<D, C / 8, 3, kThreads>(vs, x, tid);
+    spread<D, C / 8, false, kThreads>(us, m, tid);
+    spread<D, C / 8, false, kThreads>(vs, x, tid);
     if constexpr (!kKeep) {
 #pragma unroll 1
       for (int i = tid; i < D * D / 4; i += kBatch * kThreads) {
         fetch_packed<kThreads>(a, A1, i);
-        spread<D, D / 8, kG, kThreads>(st, a, i);
+        spread<D, D / 8, kHalves, kThreads>(st, a, i);
       }
     } else {
-      spread<D, D / 8, kG, kThreads>(st, a, tid);
+      spread<D, D / 8, kHalves, kThreads>(st, a, tid);
 #pragma unroll
       for (int i = 0; i < kSW; ++i)
         dot = fmaf(a[i].x, kept[i].x, fmaf(a[i].y, kept[i].y, fmaf(a[i].z, kept[i].z, fmaf(a[i].w, kept[i].w, dot))));
@@ -434,11 +476,13 @@ __global__ void __launch_bounds__(GradShape<T, D>::kThreads)
       float4 &m = *(float4 *)(us + i * kWide + d), &x = *(float4 *)(vs + i * kWide + d);
       const float4 a = m, c = x;
       sum = fmaf(a.x, c.x, fmaf(a.y, c.y, fmaf(a.z, c.z, fmaf(a.w, c.w, sum))));
-      m = make_float4(be * a.x, be * a.y, be * a.z, be * a.w);
       x = make_float4(be * c.x, be * c.y, be * c.z, be * c.w);
-      if (kG == 1) {  // u is a right operand too
-        m.x = __uint_as_float(tf32_of(m.x)), m.y = __uint_as_float(tf32_of(m.y));
-        m.z = __uint_as_float(tf32_of(m.z)), m.w = __uint_as_float(tf32_of(m.w));
+      if constexpr (kHalves) {
+        uint4 u;
+        halves_of(u.x, u.y, be * a.x, be * a.y), halves_of(u.z, u.w, be * a.z, be * a.w);
+        *(uint4 *)&m = u;
+      } else {
+        m = make_float4(be * a.x, be * a.y, be * a.z, be * a.w);
       }
     }
     sum += __shfl_xor_sync(0xFFFFFFFFu, sum, 1);
@@ -450,13 +494,24 @@ __global__ void __launch_bounds__(GradShape<T, D>::kThreads)
   const float up0 = gt[Gates<C>::kUp + i0 + g], up1 = gt[Gates<C>::kUp + i0 + g + 8];
   const float dn0 = gt[Gates<C>::kDown + i0 + g], dn1 = gt[Gates<C>::kDown + i0 + g + 8];
   float x[D / 8][4] = {}, y[D / 8][4] = {};  // dq, dk
+  if constexpr (kHalves) {
 #pragma unroll 2
-  for (int e = 0; e < D; e += 8) {
-    const auto a = left_rows<kG, kWide>(us, i0, e, dn0, dn1);
+    for (int e = 0; e < D; e += 16) {
+      const auto a = left_halves<kWide>(us, i0, e);
 #pragma unroll
-    for (int d = 0; d < D / 8; ++d) {
-      const float2 s = *(const float2 *)(st + (8 * d + g) * kWide + e + 2 * t);
-      a.times_rounded(y[d], s.x, s.y);
+      for (int d = 0; d < D / 8; ++d) a.times(y[d], halves_at(st + (8 * d + g) * kWide + e + 2 * t));
+    }
+#pragma unroll
+    for (int d = 0; d < D / 8; ++d) y[d][0] *= dn0, y[d][1] *= dn0, y[d][2] *= dn1, y[d][3] *= dn1;
+  } else {
+#pragma unroll 2
+    for (int e = 0; e < D; e += 8) {
+      const auto a = left_rows<kWide>(us, i0, e, dn0, dn1);
+#pragma unroll
+      for (int d = 0; d < D / 8; ++d) {
+        const float2 s = *(const float2 *)(st + (8 * d + g) * kWide + e + 2 * t);
+        a.times(y[d], s.x, s.y);
+      }
     }
   }
   float to0, to1, all0, all1, q0, q1;
@@ -464,7 +519,7 @@ __global__ void __launch_bounds__(GradShape<T, D>::kThreads)
   __syncthreads();
   {
     if constexpr (kKeep) {
-      spread<D, D / 8, kG, kThreads>(st, kept, tid);
+      spread<D, D / 8, kHalves, kThreads>(st, kept, tid);
     } else {
 #pragma unroll 1
       for (int i = tid; i < D * D / 4; i += kBatch * kThreads) {
@@ -474,7 +529,7 @@ __global__ void __launch_bounds__(GradShape<T, D>::kThreads)
 #pragma unroll
         for (int j = 0; j < kBatch; ++j)
           dot = fmaf(a[j].x, v[j].x, fmaf(a[j].y, v[j].y, fmaf(a[j].z, v[j].z, fmaf(a[j].w, v[j].w, dot))));
-        spread<D, D / 8, kG, kThreads>(st, v, i);
+        spread<D, D / 8, kHalves, kThreads>(st, v, i);
       }
     }
 #pragma unroll
@@ -482,15 +537,32 @@ __global__ void __launch_bounds__(GradShape<T, D>::kThreads)
     if (lane == 0) dots[w] = dot;
   }
   __syncthreads();
+  const float uq0 = up0 * f.scale, uq1 = up1 * f.scale;
+  if constexpr (kHalves) {
 #pragma unroll 2
-  for (int e = 0; e < D; e += 8) {
-    const auto a = left_rows<kG, kRow>(ds, i0, e, up0 * f.scale, up1 * f.scale);
-    const auto c = left_rows<kG, kWide>(vs, i0, e, -up0, -up1);
+    for (int e = 0; e < D; e += 16) {
+      const auto a = left_exact<kRow>(ds, i0, e);
+      const auto c = left_wide<kWide>(vs, i0, e, -up0, -up1);
 #pragma unroll
-    for (int d = 0; d < D / 8; ++d) {
-      const float2 s = *(const float2 *)(st + (8 * d + g) * kWide + e + 2 * t);
-      a.times_rounded(x[d], s.x, s.y);
-      c.times_rounded(y[d], s.x, s.y);
+      for (int d = 0; d < D / 8; ++d) {
+        const uint4 s = halves_at(st + (8 * d + g) * kWide + e + 2 * t);
+        a.times(x[d], s);
+        c.times(y[d], s);
+      }
+    }
+#pragma unroll
+    for (int d = 0; d < D / 8; ++d) x[d][0] *= uq0, x[d][1] *= uq0, x[d][2] *= uq1, x[d][3] *= uq1;
+  } else {
+#pragma unroll 2
+    for (int e = 0; e < D; e += 8) {
+      const auto a = left_rows<kRow>(ds, i0, e, uq0, uq1);
+      const auto c = left_rows<kWide>(vs, i0, e, -up0, -up1);
+#pragma unroll
+      for (int d = 0; d < D / 8; ++d) {
+        const float2 s = *(const float2 *)(st + (8 * d + g) * kWide + e + 2 * t);
+        a.times(x[d], s.x, s.y);
+        c.times(y[d], s.x, s.y);
+      }
     }
   }
   row_dots<D>(q0, q1, x, qs, i0);
@@ -507,15 +579,29 @@ __global__ void __launch_bounds__(GradShape<T, D>::kThreads)
     const int jb = blk - ib * (ib + 1) / 2, i1 = 16 * ib, j1 = 16 * jb;
     float qk[2][4] = {}, kk[2][4] = {}, a[2][4] = {}, c[2][4] = {};
     score_tiles<D>(qk, kk, qs, ks, i1, j1);
-#pragma unroll 4
-    for (int e = 0; e < D; e += 8) {
-      const auto l = left_rows<kG, kRow>(ds, i1, e);
-      const auto m = left_rows<kG, kWide>(vs, i1, e);
+    if constexpr (kHalves) {
+#pragma unroll 2
+      for (int e = 0; e < D; e += 16) {
+        const auto l = left_exact<kRow>(ds, i1, e);
+        const auto m = left_wide<kWide>(vs, i1, e);
 #pragma unroll
-      for (int q = 0; q < 2; ++q) {
-        const float2 u = *(const float2 *)(us + (j1 + 8 * q + g) * kWide + e + 2 * t);
-        l.times_rounded(a[q], u.x, u.y);
-        m.times_rounded(c[q], u.x, u.y);
+        for (int q = 0; q < 2; ++q) {
+          const uint4 u = halves_at(us + (j1 + 8 * q + g) * kWide + e + 2 * t);
+          l.times(a[q], u);
+          m.times(c[q], u);
+        }
+      }
+    } else {
+#pragma unroll 4
+      for (int e = 0; e < D; e += 8) {
+        const auto l = left_rows<kRow>(ds, i1, e);
+        const auto m = left_rows<kWide>(vs, i1, e);
+#pragma unroll
+        for (int q = 0; q < 2; ++q) {
+          const float2 u = *(const float2 *)(us + (j1 + 8 * q + g) * kWide + e + 2 * t);
+          l.times(a[q], u.x, u.y);
+          m.times(c[q], u.x, u.y);
+        }
       }
     }
     // powers e^(G_i - G_j); off the diagonal in two factors, by way of the block's first row

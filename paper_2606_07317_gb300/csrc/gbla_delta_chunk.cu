@@ -72,7 +72,7 @@ __device__ __forceinline__ void rows_times_keys(float (&kk)[C / 8][4], float (&q
     const float2 x = *(const float2 *)(ks + at), y = *(const float2 *)(ks + at + 8 * kRow);
     const float2 u = *(const float2 *)(qs + at), v = *(const float2 *)(qs + at + 8 * kRow);
     const float c[4] = {x.x, x.y, y.x, y.y}, d[4] = {u.x, u.y, v.x, v.y};
-    const LeftTf32<3> a(c), q(d);
+    const LeftTf32<> a(c), q(d);
 #pragma unroll
     for (int n = 0; n < C / 8; ++n)
       if (n <= 2 * w + 1) {
@@ -97,15 +97,15 @@ __device__ __forceinline__ TwoFloat sum_of(const TwoFloat &a, const TwoFloat &b)
 // Parts of C x C matrices in shared memory (rows of C + 4 floats) as operands: 16 rows from i on
 // at columns j .. j + 7 on the left, columns j .. j + 7 of rows i .. i + 7 on the right.
 template <int C>
-__device__ __forceinline__ LeftTf32<3> left_of(const float *m, int i, int j) {
+__device__ __forceinline__ LeftTf32<> left_of(const float *m, int i, int j) {
   const int g = (threadIdx.x & 31) >> 2, t = threadIdx.x & 3;
   const float2 x = *(const float2 *)(m + (i + g) * (C + 4) + j + 2 * t);
   const float2 y = *(const float2 *)(m + (i + g + 8) * (C + 4) + j + 2 * t);
   const float c[4] = {x.x, x.y, y.x, y.y};
-  return LeftTf32<3>(c);
+  return LeftTf32<>(c);
 }
 template <int C>
-__device__ __forceinline__ void times_right(float (&c)[4], const LeftTf32<3> &a,
+__device__ __forceinline__ void times_right(float (&c)[4], const LeftTf32<> &a,
                                             const float *m, int i, int j) {
   const int g = (threadIdx.x & 31) >> 2, t = threadIdx.x & 3;
   const float *at = m + (i + 2 * t) * (C + 4) + j + g;
@@ -156,7 +156,7 @@ __device__ __forceinline__ void invert(float *to, const float *A, int w) {
     }
 #pragma unroll
     for (int k = 0; k < 2; ++k) {
-      const LeftTf32<3> a(z[k]);
+      const LeftTf32<> a(z[k]);
 #pragma unroll
       for (int n = 0; n < 2; ++n) times_right<C>(y[n], a, to, j + 8 * k, j + 8 * n);
     }
@@ -177,7 +177,7 @@ __device__ __forceinline__ void invert(float *to, const float *A, int w) {
 #pragma unroll
     for (int k = 0; k < 4; ++k)
       if (k >= 2 || j == 0) {
-        const LeftTf32<3> a(z[k]);
+        const LeftTf32<> a(z[k]);
 #pragma unroll
         for (int n = 0; n < 2; ++n) times_right<C>(y[n], a, to, 8 * k, j + 8 * n);
       }
@@ -616,7 +616,7 @@ __global__ void __launch_bounds__(JoinShape<D>::kThreads)
     const float *m = tile + (i & 1) * D * kRow;
 #pragma unroll
     for (int k = 0; k < D / 8; ++k) {
-      const LeftTf32<3> a(S[k]);
+      const LeftTf32<> a(S[k]);
 #pragma unroll
       for (int n = 0; n < D / 8; ++n) {
         if (kBack) {

@@ -50,12 +50,6 @@ __device__ __forceinline__ uint32_t transpose8(uint32_t v) {
   asm("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(r) : "r"(v));
   return r;
 }
-// fp32 rounded to the 11 significant bits that tf32 products read.
-__device__ __forceinline__ uint32_t tf32_of(float x) {
-  uint32_t r;
-  asm("cvt.rna.tf32.f32 %0, %1;" : "=r"(r) : "f"(x));
-  return r;
-}
 // x = hi + lo to 23 bits: hi rounded by integer operations (B2 H8 N32768 D64 418 us, 449 with
 // conversion instructions), lo, which has at most 12 bits, cut off.  (A NaN may leave hi a number;
 // lo keeps it.)
@@ -64,42 +58,27 @@ __device__ __forceinline__ void tf32_split(float x, uint32_t &hi, uint32_t &lo) 
   lo = __float_as_uint(x - __uint_as_float(hi)) & 0xFFFFE000u;
 }
 
-// The left operand of tf32 products made of a result tile; kTerms 1: rounded to 11 bits,
-// 3: hi + lo (the product of the two small parts is left out: 2^-22).  The tensor cores cut off
-// what their accumulator cannot hold, so that long sums shrink: where results are fp32 (kSums),
-// the products of 8 are summed from zero and added in one rounding (the gradient of the keys
-// 1.9e-6 of its norm off, 0.4e-6 with it).
-template <int kTerms, bool kSums = false>
+// The left operand of tf32 products made of a result tile, in three terms: hi + lo on both sides (the
+// product of the two small parts is left out: 2^-22).  The tensor cores cut off what their
+// accumulator cannot hold, so that long sums shrink: where results are fp32 (kSums), the products
+// of 8 are summed from zero and added in one rounding (the gradient of the keys 1.9e-6 of its norm
+// off, 0.4e-6 with it).
+template <bool kSums = false>
 struct LeftTf32 {
   uint32_t hi[4], lo[4];
   __device__ __forceinline__ explicit LeftTf32(const float (&c)[4]) {
     const float x[4] = {c[0], c[2], c[1], c[3]};
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      if (kTerms == 1) hi[i] = tf32_of(x[i]);
-      else tf32_split(x[i], hi[i], lo[i]);
-    }
+    for (int i = 0; i < 4; ++i) tf32_split(x[i], hi[i], lo[i]);
   }
   // The right operand's values at rows 2t and 2t + 1 of this lane's column: as they are,
   __device__ __forceinline__ void times(float (&c)[4], float b0, float b1) const {
-    if (kTerms == 1) {
-      mma_tf32(c, hi, tf32_of(b0), tf32_of(b1));
-      return;
-    }
     uint32_t h0, l0, h1, l1;
     tf32_split(b0, h0, l0);
     tf32_split(b1, h1, l1);
     times(c, make_uint4(h0, h1, l0, l1));
   }
-  // rounded before (one term),
-  __device__ __forceinline__ void times_rounded(float (&c)[4], float b0, float b1) const {
-    if (kTerms == 1) mma_tf32(c, hi, __float_as_uint(b0), __float_as_uint(b1));
-    else times(c, b0, b1);
-  }
-  // or rounded or split before, and packed.
-  __device__ __forceinline__ void times(float (&c)[4], const uint2 &b) const {
-    mma_tf32(c, hi, b.x, b.y);
-  }
+  // or split before.
   __device__ __forceinline__ void times(float (&c)[4], const uint4 &b) const {
     if (kSums) {
       float z[4] = {};
@@ -120,6 +99,7 @@ struct LeftTf32 {
 template <int kTerms>
 struct LeftBf16 {
   uint32_t part[kTerms][4];
+  __device__ __forceinline__ LeftBf16() {}
   __device__ __forceinline__ LeftBf16(const float (&c)[4], const float (&d)[4]) {
     float x[8] = {c[0], c[1], c[2], c[3], d[0], d[1], d[2], d[3]};
 #pragma unroll
@@ -263,8 +243,8 @@ struct Whole {
     else ((float2 *)base)[at(m, j)] = make_float2(b0, b1);
   }
   template <bool kSums, int kN>
-  static __device__ __forceinline__ LeftTf32<3, kSums> left(const float (&r)[kN][4], int j) {
-    return LeftTf32<3, kSums>(r[j]);
+  static __device__ __forceinline__ LeftTf32<kSums> left(const float (&r)[kN][4], int j) {
+    return LeftTf32<kSums>(r[j]);
   }
 };
 // As two bf16 numbers a value, for products of 16.  Summed over columns: 8 rows m by 16 columns j;
@@ -349,7 +329,7 @@ __device__ __forceinline__ void key_products(const float (&S)[D / 8][4], const f
   const int lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
 #pragma unroll
   for (int d = 0; d < D / 8; ++d) {
-    const LeftTf32<3, true> a(S[d]);
+    const LeftTf32<true> a(S[d]);
     if (kHand) ((float4 *)hand)[d * 32 + lane] = make_float4(S[d][0], S[d][1], S[d][2], S[d][3]);
 #pragma unroll
     for (int n = 0; n < C / 8; ++n) {
@@ -388,7 +368,7 @@ __device__ __forceinline__ void query_products(const uint4 *hand, const float *q
   for (int d = 0; d < D / 8; ++d) {
     const float4 s = ((const float4 *)hand)[d * 32 + lane];
     const float c[4] = {s.x, s.y, s.z, s.w};
-    const LeftTf32<3, true> a(c);
+    const LeftTf32<true> a(c);
 #pragma unroll
     for (int n = 0; n < C / 8; ++n) {
       const float2 q = *(const float2 *)(qs + (8 * n + g) * kRow + 8 * d + 2 * t);
@@ -462,7 +442,7 @@ __device__ __forceinline__ void state_update(float (&S)[D / 8][4], float hi, flo
     float x[4] = {};
 #pragma unroll
     for (int j = 0; j < C / 8; ++j) {
-      const LeftTf32<3, true> a(w[j]);
+      const LeftTf32<true> a(w[j]);
       a.times(x, ks[(8 * j + 2 * t) * kRow + 8 * d + g], ks[(8 * j + 2 * t + 1) * kRow + 8 * d + g]);
     }
 #pragma unroll

@@ -27,9 +27,9 @@ namespace {
 // not need A (sum_i P_ij d_i, and what the results and queries add to A') other warps form one
 // chunk ahead and leave in shared memory.  kOwn: what a segment adds to A, from zero and with
 // nothing written.
-template <typename T, int D>
+template <typename T, int D, int kTerms>
 struct ReverseShape {
-  using Rec = Record<T, D, true>;
+  using Rec = Record<T, D, true, kTerms == 3>;
   static constexpr int C = kChunkOf<T>, E = D < 64 ? D : 64, kSplit = D / E;
   static constexpr int kCarry = E / 16, kThreads = 2 * kCarry * 32;
   static constexpr int kRow = pad_row<T>(D), kValRow = pad_row<T>(E);
@@ -44,10 +44,10 @@ struct ReverseShape {
 };
 
 template <typename T, int D, int kTerms, bool kOwn>
-__global__ void __launch_bounds__(ReverseShape<T, D>::kThreads)
+__global__ void __launch_bounds__(ReverseShape<T, D, kTerms>::kThreads)
     reverse_kernel(const DeltaBackArgs p, const float *records, float *after, float *weights,
                    float *own, int nc, int seg, int count) {
-  using Sh = ReverseShape<T, D>;
+  using Sh = ReverseShape<T, D, kTerms>;
   using Rec = typename Sh::Rec;
   constexpr int C = Sh::C, E = Sh::E, kCarry = Sh::kCarry, kFetch = kCarry * 32;
   constexpr bool kSums = sizeof(T) == 4;
@@ -172,7 +172,7 @@ __global__ void __launch_bounds__(ReverseShape<T, D>::kThreads)
 #pragma unroll
         for (int m = 0; m < C / 16; ++m) {
           values_of<Sh::kValRow>(r[2 * m], r[2 * m + 1], ds, m, e0 - x0);
-          if constexpr (sizeof(T) == 2) {
+          if constexpr (Rec::P::kWide == 2) {
             const LeftBf16<1> a(r[2 * m], r[2 * m + 1]);  // exact
 #pragma unroll
             for (int j = 0; j <= 2 * m + 1; ++j) a.times(x[j], Rec::P::load(P, m, j));
@@ -391,9 +391,9 @@ __device__ __forceinline__ void store1(__nv_bfloat16 *p, float x) { *p = __float
 template <typename T, typename O, int D>
 __global__ void __launch_bounds__(GradShape<T, D>::kThreads)
     grads_kernel(const DeltaBackArgs p, const float *records, const float *states,
-                 const float *misses, const float *after, const float *weights, O *dq, O *dk, int nc) {
+                 const float *misses, const float *after, const float *weights, O *dq, O *dk, int nc,
+                 int stride) {
   using Sh = GradShape<T, D>;
-  using Rec = Record<T, D, true>;
   constexpr int C = Sh::C, kThreads = Sh::kThreads, kRow = Sh::kRow, kWide = Sh::kWide;
   constexpr int kMat = Sh::kMat, kWarps = Sh::kWarps;
   constexpr bool kHalves = sizeof(T) == 2;  // u and the states as two bf16 numbers
@@ -432,7 +432,7 @@ __global__ void __launch_bounds__(GradShape<T, D>::kThreads)
   load_rows<T, C, D, kThreads>(qs, (const T *)f.q + b * f.sq[0] + t0 * f.sq[1] + (long long)hk * D,
                                f.sq[1], n, tid);
   load_rows<T, C, D, kThreads>(ds, (const T *)p.d_o + row0 * D, (long long)orow, n, tid);
-  load_flat<Gates<C>::kFloats, kThreads>(gt, records + at * Rec::kFloats + Rec::kGates, tid);
+  load_flat<Gates<C>::kFloats, kThreads>(gt, records + at * stride + Record<T, D, true>::kGates, tid);
   cp_async_commit();
   // the misses and w (as they are: dbeta is a product of both), A, and where it is small S, with
   // their inner product
@@ -740,15 +740,21 @@ struct Layout {
   size_t records, states, misses, after, weights, before, own, moves, dq, dk, total;
   Segments segments;
 };
+// Floats of a chunk's record.  exact: see exact_back.
 template <typename T>
-Layout layout_of(const DeltaBackArgs &p) {
+int record_floats(int D, bool exact) {
+  if (exact) return D < 128 ? Record<T, 64, true, true>::kFloats : Record<T, 128, true, true>::kFloats;
+  return D < 128 ? Record<T, 64, true>::kFloats : Record<T, 128, true>::kFloats;
+}
+template <typename T>
+Layout layout_of(const DeltaBackArgs &p, bool exact) {
   const DeltaArgs &a = p.f;
   constexpr int C = kChunkOf<T>;
   const size_t all = (size_t)a.B * a.H * chunks_of<T>(a);
   Layout l = {};
   size_t at = 0;
   auto take = [&](size_t &to, size_t floats) { to = at, at += (floats + 63) / 64 * 64; };
-  take(l.records, all * (a.D < 128 ? Record<T, 64, true>::kFloats : Record<T, 128, true>::kFloats));
+  take(l.records, all * record_floats<T>(a.D, exact));
   take(l.states, all * a.D * a.D);
   take(l.after, all * a.D * a.D);
   take(l.misses, all * C * a.D);
@@ -766,7 +772,7 @@ Layout layout_of(const DeltaBackArgs &p) {
 bool exact_back(const DeltaBackArgs &p) { return p.f.dtype == GBLA_FP32 || p.dstate_in; }
 
 template <typename T, typename O, int D>
-cudaError_t grads_launch(const DeltaBackArgs &p, const Layout &l, float *s, O *dq, O *dk,
+cudaError_t grads_launch(const DeltaBackArgs &p, const Layout &l, bool exact, float *s, O *dq, O *dk,
                          cudaStream_t st) {
   using Sh = GradShape<T, D>;
   const int nc = chunks_of<T>(p.f);
@@ -779,17 +785,18 @@ cudaError_t grads_launch(const DeltaBackArgs &p, const Layout &l, float *s, O *d
   return launch_pdl(kernel, dim3(nc, p.f.H, p.f.B), dim3(Sh::kThreads), Sh::kBytes, st, p,
                     (const float *)(s + l.records), (const float *)(s + l.states),
                     (const float *)(s + l.misses), (const float *)(s + l.after),
-                    (const float *)(s + l.weights), dq, dk, nc);
+                    (const float *)(s + l.weights), dq, dk, nc, record_floats<T>(D, exact));
 }
 
 template <typename T, int D, int kTerms>
 cudaError_t back_launch(const DeltaBackArgs &p, float *s, cudaStream_t st) {
-  using Sh = ReverseShape<T, D>;
+  using Sh = ReverseShape<T, D, kTerms>;
+  constexpr bool kExact = kTerms == 3;
   const DeltaArgs &a = p.f;
-  const Layout l = layout_of<T>(p);
+  const Layout l = layout_of<T>(p, kExact);
   const int nc = chunks_of<T>(a);
   cudaError_t e;
-  if ((e = save_forward(a, l.segments, kTerms == 3, s + l.records, s + l.states, s + l.misses,
+  if ((e = save_forward(a, l.segments, kExact, s + l.records, s + l.states, s + l.misses,
                         s + l.before, s + l.moves, st)) != cudaSuccess)
     return e;
   const Segments &g = l.segments;
@@ -814,9 +821,9 @@ cudaError_t back_launch(const DeltaBackArgs &p, float *s, cudaStream_t st) {
   if ((e = launch_pdl(reverse, grid, block, Sh::kBytes, st, p, records, s + l.after, s + l.weights,
                       s + l.own, nc, g.chunks, g.count)) != cudaSuccess)
     return e;
-  if (a.H == a.Hk) return grads_launch<T, T, D>(p, l, s, (T *)p.dq, (T *)p.dk, st);
+  if (a.H == a.Hk) return grads_launch<T, T, D>(p, l, kExact, s, (T *)p.dq, (T *)p.dk, st);
   float *dq = s + l.dq, *dk = s + l.dk;
-  if ((e = grads_launch<T, float, D>(p, l, s, dq, dk, st)) != cudaSuccess) return e;
+  if ((e = grads_launch<T, float, D>(p, l, kExact, s, dq, dk, st)) != cudaSuccess) return e;
   return sum_shared_heads(dq, dk, p.dq, p.dk, (long long)a.B * a.N, a.Hk, a.H / a.Hk, D, a.dtype, st);
 }
 
@@ -832,7 +839,8 @@ cudaError_t back_d(const DeltaBackArgs &p, float *s, cudaStream_t st) {
 
 size_t delta_backward_floats(const DeltaBackArgs &p) {
   using namespace delta;
-  return p.f.dtype == GBLA_FP32 ? layout_of<float>(p).total : layout_of<__nv_bfloat16>(p).total;
+  return (p.f.dtype == GBLA_FP32 ? layout_of<float>(p, true)
+                                 : layout_of<__nv_bfloat16>(p, exact_back(p))).total;
 }
 
 cudaError_t delta_backward(const DeltaBackArgs &p, float *scratch, cudaStream_t st) {

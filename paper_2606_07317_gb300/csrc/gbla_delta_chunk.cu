@@ -187,11 +187,11 @@ __device__ __forceinline__ void invert(float *to, const float *A, int w) {
 }
 
 // One chunk of head h of sequence b, n of its tokens there; ends without a barrier.
-template <typename T, int D, bool kBack>
+template <typename T, int D, bool kBack, bool kExact>
 __device__ __forceinline__ void prepare_chunk(const DeltaArgs &p, char *raw, float *rec, int h,
                                               int b, int t0, int n) {
   using Sh = PrepShape<T, D>;
-  using Rec = Record<T, D, kBack>;
+  using Rec = Record<T, D, kBack, kExact>;
   constexpr int C = Sh::C, kThreads = Sh::kThreads, kRow = Sh::kRow, kMat = Sh::kMat;
   T *ks = (T *)raw, *qs = ks + C * kRow;
   float *A = (float *)(raw + Sh::kFirst), *inv = (float *)raw;
@@ -309,7 +309,7 @@ __device__ __forceinline__ void prepare_chunk(const DeltaArgs &p, char *raw, flo
       }
   };
   if (kBack) {
-    if constexpr (sizeof(T) == 2) {  // 16 rows a warp
+    if constexpr (Rec::P::kWide == 2) {  // 16 rows a warp
       for (int j = 0; j < 2 * w + 2; ++j) {
         const float *at = inv + (16 * w + 2 * t) * kMat + 8 * j + g;
         const float x[4] = {at[0], at[kMat], at[8 * kMat], at[9 * kMat]};
@@ -340,7 +340,7 @@ __device__ __forceinline__ void prepare_chunk(const DeltaArgs &p, char *raw, flo
   }
 }
 
-template <typename T, int D, bool kBack>
+template <typename T, int D, bool kBack, bool kExact>
 __global__ void __launch_bounds__(PrepShape<T, D>::kThreads, PrepShape<T, D>::kBlocks)
     prepare_kernel(const DeltaArgs p, float *records, int nc, int each) {
   constexpr int C = PrepShape<T, D>::C;
@@ -351,9 +351,9 @@ __global__ void __launch_bounds__(PrepShape<T, D>::kThreads, PrepShape<T, D>::kB
   const int first = blockIdx.x * each, end = min(first + each, (L + C - 1) / C);
   for (int c = first; c < end; ++c) {
     if (c > first) __syncthreads();  // the chunk before is done with
-    prepare_chunk<T, D, kBack>(
-        p, raw, records + (((size_t)b * p.H + h) * nc + c) * Record<T, D, kBack>::kFloats, h, b, c * C,
-        min(C, L - c * C));
+    prepare_chunk<T, D, kBack, kExact>(
+        p, raw, records + (((size_t)b * p.H + h) * nc + c) * Record<T, D, kBack, kExact>::kFloats, h,
+        b, c * C, min(C, L - c * C));
   }
 }
 
@@ -673,9 +673,10 @@ cudaError_t launch(const DeltaArgs &a, const Segments &g, float *records, float 
   using Sc = ScanShape<T, D, kTerms, kFor>;
   using Se = ScanShape<T, D, kTerms, kSegment>;
   static_assert(kFor != kSegment, "");
-  const int nc = chunks_of<T>(a), stride = Record<T, D, kFor == kSave>::kFloats;
+  constexpr bool kExact = kFor == kSave && kTerms == 3;
+  const int nc = chunks_of<T>(a), stride = Record<T, D, kFor == kSave, kExact>::kFloats;
   cudaError_t e;
-  const auto prep = prepare_kernel<T, D, kFor == kSave>;
+  const auto prep = prepare_kernel<T, D, kFor == kSave, kExact>;
   if ((e = allow_smem(prep, Pr::kBytes)) != cudaSuccess) return e;
   const int each = a.seq_lens && (long long)nc * a.H * a.B >= 64ll * sm_count() ? 4 : 1;
   count_launch();

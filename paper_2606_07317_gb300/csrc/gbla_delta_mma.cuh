@@ -283,12 +283,13 @@ struct Gates {
 // A chunk's record.  For the forward pass beta M, P and the powers of its gates.  For the backward
 // pass (kBack) M - 1, and, for products that sum over the row index, T - 1 with T = (1 + beta X)^-1,
 // and P the other way round.  The inverses in fp32; P, whose products nothing multiplies up, as two
-// bf16 numbers where results are bf16.
-template <typename T, int D, bool kBack>
+// bf16 numbers where what it makes is bf16 (kExact: the gradient of a state, in fp32, is not:
+// 1.0e-6 of its norm off, 0.3e-6 in fp32).
+template <typename T, int D, bool kBack, bool kExact = false>
 struct Record {
   static constexpr int C = kChunkOf<T>;
   using M = Whole<C, sizeof(T) == 4 || D < 128>;
-  using P = std::conditional_t<sizeof(T) == 2, Halves<C, kBack>, Whole<C, true>>;
+  using P = std::conditional_t<sizeof(T) == 2 && !kExact, Halves<C, kBack>, M>;
   static constexpr int kM = 0, kGates = M::kFloats, kP = kGates + Gates<C>::kFloats;
   static constexpr int kT = kP + P::kFloats, kFloats = kT + (kBack ? M::kFloats : 0);
 };

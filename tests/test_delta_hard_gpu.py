@@ -86,6 +86,22 @@ def test_backward(shape, keys, beta, D):
                 close(t, want[n], grad_bound(n, "bf16", c.N, D), (n, ends), beside)
 
 
+@pytest.mark.parametrize("keys,D", [("same", 64), ("opposite", 128), ("same", 32)])
+def test_fp32(keys, D):
+    """What the inverse is off by is all there is: 2^-11, and twice it for gradients."""
+    c = Case(64, 3, 333, 6, 6, D, "fp32")
+    hard(c, keys, 1.99)
+    do, ds = c.n(*c.x["v"].shape).cuda(), c.state()
+    o, S = R.delta(*c.x.values(), c.lens, None, D ** -0.5)
+    got, fin = gbla.delta_attention(*c.x.values(), return_state=True)
+    close(got, o, STATE, "o")
+    close_state(fin, S, "state")
+    want = R.delta_backward(*c.x.values(), do, c.lens, None, ds, D ** -0.5)
+    for n, t in gbla.delta_attention_backward(*c.x.values(), do, dstate=ds, return_dstate=True).items():
+        beside = shares(c.x, do, want, c.lens, None, D ** -0.5) if n == "dlog_decay" else None
+        close(t, want[n], 2 * STATE, n, beside)
+
+
 @pytest.mark.parametrize("keys,D", [("same", 64), (0.9, 128), (0.0, 64)])
 def test_long(keys, D):
     """Where errors of the state would add up: 4096 tokens, reflections, hardly any fading."""

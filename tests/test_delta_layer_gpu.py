@@ -119,3 +119,26 @@ def test_gradients_against_differences():
             d = (loss({**x, name: t + h * e}) - loss({**x, name: t - h * e})) / (2 * h)
             got = (grads["d" + name].double() * e).sum().item()
             assert abs(d - got) <= 2.0 ** -8 * grads["d" + name].norm().item(), (name, d, got)
+
+
+def test_gradients_that_come_as_slices():
+    """Results of several batches in one flat tensor, each at an odd place of it: the gradients are
+    those of the batches alone, bit for bit."""
+    g = torch.Generator().manual_seed(8)
+    n = lambda *s: torch.randn(s, generator=g).cuda()  # noqa: E731
+    tok = torch.randint(0, 40, (2, 3), generator=g).to(torch.int32).cuda()
+    weight = n(500)
+    for apart in (True, False):
+        g.manual_seed(9)
+        logits = [n(2, 3, 40).requires_grad_() for _ in range(3)]
+        results = [decoder.token_logprobs(x, tok) for x in logits]
+        q, k, v = n(1, 5, 2, 32), n(1, 5, 2, 32) * 32 ** -0.5, n(1, 5, 2, 32).requires_grad_()
+        o = decoder.delta_attention(q, k, v, -n(1, 5, 2).abs(), n(1, 5, 2).sigmoid())
+        parts = [weight[:1]] + [r[m].flatten() for r in results for m in ("lse", "entropy", "logprob")] + [o.flatten()]
+        if apart:
+            split = torch.split(weight[:375], [p.numel() for p in parts])
+            want = torch.autograd.grad(parts[1:], logits + [v], [w.clone() for w in split[1:]])
+        else:
+            (torch.cat(parts) * weight[:375]).sum().backward()
+            got = [x.grad for x in logits] + [v.grad]
+    assert all(torch.equal(a, b) for a, b in zip(got, want))

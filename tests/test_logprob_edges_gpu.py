@@ -125,3 +125,11 @@ def test_top_tokens_beside_nan(dtype, rows_, V):
     assert torch.equal(got["top_token"].long(), want)
     bad = x.isnan().any(-1)
     assert got["lse"][bad].isnan().all() and got["entropy"][bad].isnan().all() and got["top_logprob"][bad].isnan().all()
+
+
+@pytest.mark.parametrize("B,N,V,dtype,top", [(31, 10, 131087, "bf16", 0), (1, 306, 65603, "fp32", 9),
+                                            (2, 160, 140003, "bf16", 64)])
+def test_long_rows_with_a_block_each(B, N, V, dtype, top):
+    x, tok, _ = rows(71, B, N, V, dtype, 0.1)
+    got = gbla.token_logprobs(x, tok, top=top)
+    check(got, R.logprobs(x, tok, top, 1.0))

@@ -139,3 +139,21 @@ def test_large_ragged_batches(B, N, H, D, dtype):
         beside = shares(c.x, do, want, c.lens, None, D ** -0.5) if n == "dlog_decay" else None
         close(t, want[n], grad_bound(n, dtype, N, D), n, beside)
     assert gbla.device_error() == 0
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("what", ["q", "k", "v", "log_decay", "beta"])
+def test_nan_is_not_hidden(what, dtype):
+    """A NaN in token 70 is in its result and, but for a query's, in all that follow; chunks before
+    it have none."""
+    c = Case(65, 1, 200, 2, 2, 64, dtype)
+    c.x[what][0, 70] = float("nan")
+    do = torch.ones_like(c.x["v"])
+    for keep in (False, True):
+        o = gbla.delta_attention(*c.x.values(), return_state=keep)
+        o, S = o if keep else (o, None)
+        assert torch.isfinite(o[0, :64]).all() and o[0, 70].isnan().all()
+        assert what == "q" or (o[0, 71:].isnan().all() and (S is None or S.isnan().all()))
+        g = gbla.delta_attention_backward(*c.x.values(), do, return_dstate=keep)
+        # (results are linear in q and in v: their own gradients do not depend on them)
+        assert g["dk" if what == "q" else "dq"][0, 70].isnan().all()

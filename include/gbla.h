@@ -554,12 +554,15 @@ gbla_status gbla_decay_attention_step(const void *q, const void *k, const void *
  * scale is finite, not 0 and not subnormal.  Computed in chunks of tokens (bf16 64, fp32
  * 32) by warp-level tensor-core products with fp32 sums; the state is held in fp32.  States
  * that are results, and everything in fp32, are within a few 2^-24 of their norm a token's
- * horizon long (operands enter as three numbers); bf16 results without a state round
- * operands to 2^-11 or better inside, which their own rounding covers.  Values, keys,
+ * horizon long (operands of 22 bits and more); but where keys are alike and beta |k|^2 is
+ * near 2, so that writes nearly undo one another, up to 2^-11 (gradients 2^-10).  bf16
+ * results have operands of 16 bits and more inside, the triangular systems 22: beside their
+ * own rounding, 2^-8 at most, they are within 2^-11 throughout, 2^-13 for keys that differ.
+ * With state_out more bits are taken than without: o may differ by a rounding.  Values, keys,
  * states and gates other than log_decay = -inf are finite: a NaN or infinity in a valid
  * token reaches the whole chunk and what follows it.  Sums run in a fixed order.  Scratch
- * comes from the library's pool (GBLA_ERR_ALLOC): about 20 KB (bf16, without a state) a
- * chunk and head, and two states a segment that a long sequence is cut into.
+ * comes from the library's pool (GBLA_ERR_ALLOC): for each chunk and head 30 KB (bf16; 21 at
+ * D = 128) or 11 (fp32), and two states a segment that a long sequence is cut into.
  */
 gbla_status gbla_delta_attention(const void *q, const void *k, const void *v,
                                  const void *log_decay, const void *beta,
@@ -575,8 +578,9 @@ gbla_status gbla_delta_attention(const void *q, const void *k, const void *v,
  * dq, dk [B, N, Hk, D] (sums over the value heads that read a key head, in fp32), dv
  * [B, N, H, D], dlog_decay, dbeta [B, N, H] dtype (rows t >= L_b written as 0; where
  * log_decay is -inf its gradient is 0) and dstate_in [B, H, D, D] fp32 or NULL.  Nothing is
- * kept from a forward call.  Scratch: about 30 KB a chunk and head, two states and two
- * chunks of fp32 values each, and fp32 planes of dq and dk where heads are shared.
+ * kept from a forward call.  Scratch: for each chunk and head 48 KB (bf16; 57 with dstate_in,
+ * at D = 128 30) or 16 (fp32), two states and two chunks of fp32 values; three states a
+ * segment; and fp32 planes of dq and dk where heads are shared.
  */
 gbla_status gbla_delta_attention_backward(
     const void *q, const void *k, const void *v, const void *log_decay, const void *beta,
@@ -616,8 +620,9 @@ gbla_status gbla_delta_attention_step(const void *q, const void *k, const void *
  *             order of their tokens
  * Rows t >= L_b are untouched.  1 <= V <= 2^30, B N <= 2^30, 2^-100 <= scale <= 2^100.  Logits of
  * -inf are ruled out (p = 0); a row of nothing else has lse and log probabilities of
- * -inf and entropy 0.  A NaN or +inf makes the results of its row NaN; its top tokens
- * are in range (NaN counts as the least).  fp32 arithmetic, one launch, allocates
+ * -inf and entropy 0.  A NaN or +inf makes the results of its row NaN, but for its top
+ * tokens (NaN counts as the least).  Finite logits have a finite entropy; an lse or log
+ * probability beyond fp32's range is infinite.  fp32 arithmetic, one launch, allocates
  * nothing; results do not depend on the order in which threads arrive.
  */
 gbla_status gbla_token_logprobs(const void *logits, const int32_t *tokens,
@@ -631,9 +636,13 @@ gbla_status gbla_token_logprobs(const void *logits, const int32_t *tokens,
  * sum(dentropy * entropy) + sum(dlse * lse) with respect to the logits:
  *   scale (dlogprob (onehot - p) - dentropy p (ln p + entropy) + dlse p).
  * lse and entropy [B, N] are the forward call's; dlogprob, dentropy, dlse [B, N] fp32 may
- * each be NULL (zeros).  dlogits [B, N, V] dtype, contiguous: rows t >= L_b, and rows of
- * nothing but ruled-out logits (-inf, or below -1e30), are written as 0.  It may be the
- * logits themselves (contiguous), which it then overwrites.
+ * each be NULL (zeros); the entropy of a row whose dentropy is 0 has no share.  dlogits
+ * [B, N, V] dtype, contiguous: rows t >= L_b, and rows of nothing but ruled-out logits
+ * (-inf, or below -1e30 when scaled), are written as 0.  It may be the logits themselves
+ * (contiguous), which it then overwrites.  Probabilities are taken from lse: they are off
+ * by its rounding, up to 2^-24 |lse| of themselves, and logits of 1e7 and more that are
+ * equal cannot share theirs.  Where lse is +inf, each scaled logit beyond fp32's range has
+ * the probability exp(-entropy), which is right where those are equal.
  */
 gbla_status gbla_token_logprobs_backward(const void *logits, const float *lse,
                                          const float *entropy, const int32_t *tokens,

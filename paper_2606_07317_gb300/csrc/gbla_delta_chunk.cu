@@ -21,9 +21,9 @@ namespace {
 // --------------------------------------------------------------- first launch
 // A block takes `each` chunks of a (head, batch) one after the other, a warp for each 16 tokens.
 // One, but for large ragged batches four: the blocks that find no chunk are then a quarter as
-// many (ragged D = 128 378 us, 419 with one, 390 with two and 380 with eight; full lengths, B2 H8
-// N32768 D64, 81 us with one and 86 with four).  Blocks that stay and number the chunks that
-// there are took 606 us.
+// many (ragged D = 128 404 us, 452 with one, 415 with two and 406 with eight; full lengths, B2 H8
+// N32768 D64, 90 us with one).  Blocks that stay and number the chunks that there are took a third
+// longer.
 template <typename T, int D>
 struct PrepShape {
   static constexpr int C = kChunkOf<T>, kWarps = C / 16, kThreads = kWarps * 32;

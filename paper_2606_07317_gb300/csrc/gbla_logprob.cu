@@ -498,7 +498,7 @@ __global__ void __launch_bounds__(kThreads) logprob_kernel(const LogprobArgs p, 
 
 // d x = scale [ p (dlse - dlogprob - dentropy (ln p + entropy)) + (dlogprob at the token) ],
 // a tile of a row at a time: bound by the bytes of logits and gradient.  A thread holds kVecs
-// vectors, all on their way before the first is used: 8192 rows of 32768 in bf16 162 us (97 % of
+// vectors, all on their way before the first is used: 8192 rows of 32768 in bf16 165 us (96 % of
 // the measured copy rate), 178 with 4 and 226 with 2.  Short rows take a warp each.
 template <typename T, int kBackThreads, int kBackVecs>
 __global__ void __launch_bounds__(kBackThreads) logprob_backward_kernel(const LogprobArgs p,

@@ -133,3 +133,29 @@ def test_long_rows_with_a_block_each(B, N, V, dtype, top):
     x, tok, _ = rows(71, B, N, V, dtype, 0.1)
     got = gbla.token_logprobs(x, tok, top=top)
     check(got, R.logprobs(x, tok, top, 1.0))
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("V", [37, 900, 9001])
+def test_far_rows_of_any_place(dtype, V):
+    """Logits around 3e4 in rows of a wider tensor, at every place of a vector, ragged, and over
+    the logits themselves: to the bit what contiguous ones give; and the definition's."""
+    x, tok, g = rows(72, 2, 3, V, dtype)
+    x = x + 3e4
+    lens = torch.tensor([3, 1], dtype=torch.int32, device="cuda")
+    d = [torch.randn((2, 3), generator=g).cuda() for _ in range(3)]
+    f = gbla.token_logprobs(x, tok)
+    want = gbla.token_logprobs_backward(x, f["lse"], f["entropy"], tok, *d, seq_lens=lens)
+    ref, mag = R.logprobs_backward(x, tok, 1.0, *d)
+    live = torch.arange(3, device="cuda")[None] < lens[:, None]
+    grads(want[live], ref[live], mag[live], x[live], dtype)
+    assert (want[~live] == 0).all()
+    wide = torch.zeros((2, 4, V + 9), dtype=x.dtype, device="cuda")
+    for off in range(9):
+        view = wide[:, :3, off:off + V]
+        view.copy_(x)
+        got = gbla.token_logprobs_backward(view, f["lse"], f["entropy"], tok, *d, seq_lens=lens)
+        assert torch.equal(got, want), off
+    over = x.clone()
+    assert torch.equal(gbla.token_logprobs_backward(over, f["lse"], f["entropy"], tok, *d, seq_lens=lens, out=over),
+                       want)
